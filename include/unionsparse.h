@@ -276,6 +276,47 @@ us_status us_launch_info(const us_handle* h, int32_t N, int32_t* grid, int32_t* 
  * us_spmm_ahead_kernel; chained calls may, too. */
 const char* us_launch_kernel(const us_handle* h, int32_t N, void* stream);
 
+/*
+ * MX4: dense matrices in microscaled 4-bit floating point, for projections that are not pruned and calls of any number
+ * of tokens (no counterpart in the paper; formats as in the OCP Microscaling specification v1.0, MXFP4).
+ *
+ * A row's columns form blocks of 32 (the last may be shorter) that share a scale 2^e, held as the byte e + 127:
+ *     a = max|x| of the block,  e = clamp(floor(log2 a) - 2, -127, 127)  (a = 0: -127)
+ *     code = E2M1 value nearest to x * 2^-e, ties to the even code, saturating at 6
+ * so the codes are reproducible bit for bit. A block with an infinity or NaN gets the scale byte 255: all its values, and every
+ * product with them, are NaN. E2M1 code c: sign bit 3, then {0, 0.5, 1, 1.5, 2, 3, 4, 6}.
+ *
+ * The library holds a matrix in tiles of its own (us_mx4_bytes(rows, K) bytes of device memory, 16-byte aligned; -1 for a shape that
+ * is out of range). us_mx4_quantize makes it from rows of us_type values; us_mx4_pack from codes and scale bytes that the
+ * caller has (codes: ceil(K/2) bytes a row, even column in the low nibble; scales: ceil(K/32) bytes a row); us_mx4_unpack and
+ * us_mx4_dequantize are their inverses. Rows have strides ld* (elements; bytes for codes and scales); 16-byte aligned rows take
+ * the vector path. Values that a us_type cannot hold overflow as a conversion does.
+ *
+ * us_mx4_matmul: Y[n][m] = RN_y_type(sum_k x[n][k] w[m][k]) for N rows x and M rows w of K columns, products exact, sums in fp32.
+ * us_mx4_linear: the same on activations of x_type that are quantised within the call (as us_mx4_quantize does), into `scratch`
+ *   of at least us_mx4_linear_scratch(N, M, K) bytes (0 for few tokens: no scratch; also valid: NULL). One call may use a scratch at a time.
+ * flags: US_MX4_W_STABLE promises that the weights were complete before the stream's latest work was launched and stay as they
+ *   are, so that they may be read while that work still runs.
+ * rows, N = 0 is a call that does nothing. Y must not overlap the inputs. All calls are enqueue-only on `stream`, work on the current
+ * device and keep nothing; us_mx4_last_error synchronises it and reports (and clears) a bounded wait that ran out in a product.
+ * Errors: INVALID_ARG, SCRATCH_TOO_SMALL, CUDA.
+ */
+typedef enum us_type { US_F16 = 0, US_BF16 = 1, US_F32 = 2 } us_type;
+#define US_MX4_W_STABLE 1u
+int64_t us_mx4_bytes(int64_t rows, int64_t K);
+us_status us_mx4_quantize(const void* X, int32_t x_type, int64_t ldx, int64_t rows, int64_t K, void* mx, void* stream);
+us_status us_mx4_dequantize(const void* mx, int64_t rows, int64_t K, void* out, int32_t type, int64_t ldo, void* stream);
+us_status us_mx4_pack(const void* codes, int64_t ldc, const void* scales, int64_t lds, int64_t rows, int64_t K, void* mx,
+                      void* stream);
+us_status us_mx4_unpack(const void* mx, int64_t rows, int64_t K, void* codes, int64_t ldc, void* scales, int64_t lds,
+                        void* stream);
+us_status us_mx4_matmul(const void* x_mx, int64_t N, const void* w_mx, int64_t M, int64_t K, void* Y, int32_t y_type, int64_t ldy,
+                        uint32_t flags, void* stream);
+int64_t us_mx4_linear_scratch(int64_t N, int64_t M, int64_t K);
+us_status us_mx4_linear(const void* X, int32_t x_type, int64_t ldx, int64_t N, const void* w_mx, int64_t M, int64_t K, void* Y,
+                        int32_t y_type, int64_t ldy, void* scratch, int64_t scratch_bytes, uint32_t flags, void* stream);
+us_status us_mx4_last_error(void);
+
 const char* us_status_string(us_status s);
 
 #ifdef __cplusplus

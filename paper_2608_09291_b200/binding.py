@@ -29,6 +29,8 @@ US_ENCODE_W2 = 8
 EXPORTS = ["us_encode", "us_get_stats", "us_decode", "us_get_row_order", "us_spmm", "us_spmm_static_scratch",
            "us_spmm_requant", "us_absmax_f16", "us_quantize_f16",
            "us_last_error", "us_debug_withhold_copy", "us_stage_timers", "us_destroy", "us_spmm_bytes", "us_launch_info", "us_launch_kernel",
+           "us_mx4_bytes", "us_mx4_quantize", "us_mx4_dequantize", "us_mx4_pack", "us_mx4_unpack", "us_mx4_matmul",
+           "us_mx4_linear_scratch", "us_mx4_linear", "us_mx4_last_error",
            "us_status_string"]
 
 
@@ -66,6 +68,18 @@ _lib.us_spmm_bytes.restype = ctypes.c_int64
 _lib.us_launch_info.argtypes = [_vp, ctypes.c_int32] + [ctypes.POINTER(ctypes.c_int32)] * 3
 _lib.us_launch_kernel.argtypes = [_vp, ctypes.c_int32, _vp]
 _lib.us_launch_kernel.restype = ctypes.c_char_p
+_i32, _i64 = ctypes.c_int32, ctypes.c_int64
+_lib.us_mx4_bytes.argtypes = [_i64, _i64]
+_lib.us_mx4_bytes.restype = _i64
+_lib.us_mx4_quantize.argtypes = [_vp, _i32, _i64, _i64, _i64, _vp, _vp]
+_lib.us_mx4_dequantize.argtypes = [_vp, _i64, _i64, _vp, _i32, _i64, _vp]
+_lib.us_mx4_pack.argtypes = [_vp, _i64, _vp, _i64, _i64, _i64, _vp, _vp]
+_lib.us_mx4_unpack.argtypes = [_vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp]
+_lib.us_mx4_matmul.argtypes = [_vp, _i64, _vp, _i64, _i64, _vp, _i32, _i64, ctypes.c_uint32, _vp]
+_lib.us_mx4_linear_scratch.argtypes = [_i64, _i64, _i64]
+_lib.us_mx4_linear_scratch.restype = _i64
+_lib.us_mx4_linear.argtypes = [_vp, _i32, _i64, _i64, _vp, _i64, _i64, _vp, _i32, _i64, _vp, _i64, ctypes.c_uint32, _vp]
+_lib.us_mx4_last_error.argtypes = []
 _lib.us_status_string.argtypes = [ctypes.c_int]
 _lib.us_status_string.restype = ctypes.c_char_p
 
@@ -318,3 +332,86 @@ class SparseWeight:
             self.close()
         except Exception:
             pass
+
+
+# ---- MX4: dense matrices in microscaled 4-bit floating point ----
+
+def mx4_bytes(rows: int, K: int) -> int:
+    """Bytes of device memory that the tiles of a rows x K matrix take."""
+    n = int(_lib.us_mx4_bytes(int(rows), int(K)))
+    if n < 0:
+        raise UsError(1, "us_mx4_bytes")
+    return n
+
+
+class Mx4:
+    """A dense (rows, K) matrix of E2M1 values with a power-of-two scale for 32 columns of a row, on a CUDA device, in the library's
+    tiles (``data``, uint8). Made by ``mx4_quantize`` and ``mx4_from_codes``."""
+
+    def __init__(self, rows: int, K: int, data=None, device="cuda"):
+        import torch
+        _native()
+        need = mx4_bytes(rows, K)
+        if data is None:
+            data = torch.empty(need, device=device, dtype=torch.uint8)
+        elif data.dtype != torch.uint8 or data.numel() != need or not data.is_contiguous() or not data.is_cuda:
+            raise ValueError(f"data must be {need} contiguous bytes (uint8) on a CUDA device")
+        self.rows, self.K, self.data, self.frozen = int(rows), int(K), data, False
+
+    def freeze(self):
+        """Declares the matrix complete and constant (a weight): waits for its device, and from then on products may read it while
+        the stream's earlier work still runs. Not during a stream capture. Returns the matrix."""
+        import torch
+        torch.cuda.synchronize(self.data.device)
+        self.frozen = True
+        return self
+
+    def dequantize(self, dtype=None, out=None, stream=None):
+        """The (rows, K) values, float32 unless another type is asked for (float16 may overflow). bfloat16 holds them exactly."""
+        return _ext.mx4_dequantize(self.data, self.rows, self.K, dtype, out, stream)
+
+    def codes(self, stream=None):
+        """(codes uint8 (rows, ceil(K/2)), even column in the low nibble; scale bytes uint8 (rows, ceil(K/32)))."""
+        return _ext.mx4_unpack(self.data, self.rows, self.K, stream)
+
+
+def mx4_quantize(X, out: Mx4 | None = None, stream=None) -> Mx4:
+    """MX4 form of a device float16, bfloat16 or float32 (rows, K) tensor or view (unit column stride). An `out` that is given is
+    written over (not one that is frozen)."""
+    ext = _ext or _native()
+    if out is None:
+        m = Mx4.__new__(Mx4)
+        m.rows, m.K = X.shape
+        m.frozen = False
+        m.data = ext.mx4_quantize(X, None, stream)
+        return m
+    if out.frozen or (out.rows, out.K) != tuple(X.shape):
+        raise ValueError("out must be an unfrozen Mx4 of X's shape")
+    ext.mx4_quantize(X, out.data, stream)
+    return out
+
+
+def mx4_from_codes(codes, scales, K: int, stream=None) -> Mx4:
+    """A matrix from E2M1 codes (uint8 (rows, ceil(K/2)), even column in the low nibble) and scale bytes (uint8 (rows, ceil(K/32))),
+    both on the device with unit column stride: a checkpoint's weight. The result is frozen (the call waits for the device)."""
+    m = Mx4.__new__(Mx4)
+    m.rows, m.K, m.frozen = int(codes.shape[0]), int(K), False
+    m.data = (_ext or _native()).mx4_pack(codes, scales, K, stream)
+    return m.freeze()
+
+
+def mx4_linear(X, w: Mx4, out=None, dtype=None, stream=None):
+    """(N, M) product of activations and the transposed (M, K) weight. X: device float16, bfloat16 or float32 (N, K) tensor or view
+    (unit column stride), quantised to MX4 within the call, or an Mx4. The result has `dtype`, by default X's (float16 for an Mx4);
+    `out` may have any row stride."""
+    ext = _ext or _native()
+    if isinstance(X, Mx4):
+        if X.K != w.K:
+            raise ValueError("X and w differ in K")
+        return ext.mx4_linear(X.data, X.rows, w.data, w.rows, w.K, out, dtype, w.frozen, stream)
+    return ext.mx4_linear(X, -1, w.data, w.rows, w.K, out, dtype, w.frozen, stream)
+
+
+def mx4_check():
+    """Waits for the current device and raises if a product on it gave up a bounded wait."""
+    _check(_lib.us_mx4_last_error(), "us_mx4_last_error")

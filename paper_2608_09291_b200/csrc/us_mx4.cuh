@@ -1,0 +1,499 @@
+// MX4: dense matrices in microscaled 4-bit floating point (E2M1 values, one E8M0 scale for 32 of a row), their
+// quantisation and their product on the block-scaled tensor-core path of sm_100a.
+//
+// Held form ("tiles"): a matrix of rows x K is cut in tiles of 128 rows x 256 columns, row tiles outermost. A tile is 17 KB in one
+// piece, in the order that the tensor core reads it from shared memory, so that one untiled bulk copy brings an operand stage:
+//   [0, 1024)      scale bytes: half h (128 columns), row r, 32-column block b of the half: 512 h + 16 (r % 32) + 4 (r / 32) + b
+//   [1024, 17408)  codes: row r, block c (0..7) of 16 bytes at 128 r + 16 (c ^ (r % 8)); even column in the low bits of a byte
+// Columns past K in the last tile are zero codes with scale byte 0. Rows past the last one are never written: a row of an operand
+// meets only its own row (column) of the product, and those are not stored.
+#pragma once
+#include "us_spmm_tc.cuh"
+
+#include <cuda_bf16.h>
+
+namespace us {
+
+constexpr int kMxScales = 1024, kMxCodes = 16384, kMxTile = kMxScales + kMxCodes;   // bytes
+
+__host__ __device__ __forceinline__ int64_t mx4_tiles(int64_t n, int64_t per) { return (n + per - 1) / per; }
+__device__ __forceinline__ uint32_t mx4_code_off(uint32_t r, uint32_t c) { return (uint32_t)kMxScales + 128u * r + 16u * (c ^ (r & 7u)); }
+__device__ __forceinline__ uint32_t mx4_scale_off(uint32_t r, uint32_t half) { return 512u * half + 16u * (r & 31u) + 4u * (r >> 5); }
+
+// ---- quantisation ----------------------------------------------------------------------------------------------------
+// Scale byte of a block whose largest magnitude has these fp32 bits: e = floor(log2 a) - 2 clamped to [-127, 127], + 127. With the
+// biased exponent x of a that is x - 2 (subnormal and 0: 0); Inf and NaN: 255, the scale's NaN.
+__device__ __forceinline__ uint32_t mx4_scale_byte(uint32_t amax_bits)
+{
+    const uint32_t x = amax_bits >> 23;
+    return x >= 255u ? 255u : (x > 2u ? x - 2u : 0u);
+}
+// 2^(127 - byte), exact; 0 for the NaN scale (whose codes are all 0)
+__device__ __forceinline__ float mx4_inverse(uint32_t byte) { return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23); }
+// eight values -> eight codes, element e in nibble e (the conversion rounds to nearest even and saturates at 6)
+__device__ __forceinline__ uint32_t mx4_codes8(const float (&v)[8], float inv)
+{
+    uint32_t w;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(w)
+        : "f"(v[0] * inv), "f"(v[1] * inv), "f"(v[2] * inv), "f"(v[3] * inv), "f"(v[4] * inv), "f"(v[5] * inv), "f"(v[6] * inv), "f"(v[7] * inv));
+    return w;
+}
+
+template <class T> __device__ __forceinline__ float to_f32(T v);
+template <> __device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
+template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <class T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+
+// Eight elements of a row as they are; `whole`: 16-byte aligned and inside the row.
+template <class T>
+struct Eight {
+    T v[8];
+};
+template <class T>
+__device__ __forceinline__ Eight<T> load8(const T* p, int64_t left, bool whole)
+{
+    Eight<T> r;
+    if (whole) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(Eight<T>) / 16; ++i) reinterpret_cast<uint4*>(&r)[i] = __ldcg(reinterpret_cast<const uint4*>(p) + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = i < left ? p[i] : from_f32<T>(0.f);
+    }
+    return r;
+}
+
+// A warp quantises the 256 columns of one row of one tile: four lanes a block, eight columns a lane. Returns the lane's word of
+// codes; `sc` has, in lanes 0 and 16, the four scale bytes of the half that begins there.
+template <class T>
+__device__ __forceinline__ uint32_t mx4_quantize_row(const Eight<T>& x, uint32_t& sc)
+{
+    float f[8];
+    uint32_t big = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        f[i] = to_f32(x.v[i]);
+        big = max(big, __float_as_uint(f[i]) & 0x7FFFFFFFu);
+    }
+    big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+    big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+    const uint32_t byte = mx4_scale_byte(big);
+    if (byte == 255u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = 0.f;
+    const uint32_t codes = mx4_codes8(f, mx4_inverse(byte));
+    uint32_t s = byte | (__shfl_down_sync(0xffffffffu, byte, 4) << 8);
+    sc = s | (__shfl_down_sync(0xffffffffu, s, 8) << 16);
+    return codes;
+}
+
+// X (rows x K, row stride ldx) -> tiles. A warp takes one row of kUnroll consecutive tiles at a time: all loads first. Memory bound
+// (8192 x 8192 bf16: 170 MB).
+constexpr int kMxUnroll = 4;
+template <class T>
+__global__ void __launch_bounds__(256) us_mx4_quantize_kernel(const T* X, int64_t ldx, int64_t rows, int64_t K, uint8_t* mx, int vec)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t kt = mx4_tiles(K, 256), groups = mx4_tiles(kt, kMxUnroll);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int64_t u = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; u < rows * groups; u += ((int64_t)gridDim.x * blockDim.x) >> 5) {
+        const int64_t r = u / groups, j0 = (u - r * groups) * kMxUnroll;
+        Eight<T> x[kMxUnroll];
+#pragma unroll
+        for (int i = 0; i < kMxUnroll; ++i) {
+            const int64_t k = 256 * (j0 + i) + 8 * lane;
+            x[i] = load8(X + r * ldx + k, K - k, vec && k + 8 <= K);
+        }
+        uint8_t* tile = mx + ((r >> 7) * kt + j0) * kMxTile;
+        const uint32_t rr = (uint32_t)(r & 127);
+#pragma unroll
+        for (int i = 0; i < kMxUnroll; ++i) {
+            if (j0 + i >= kt) break;
+            uint32_t sc;
+            const uint32_t codes = mx4_quantize_row(x[i], sc);
+            *reinterpret_cast<uint32_t*>(tile + mx4_code_off(rr, lane >> 2) + 4 * (lane & 3)) = codes;
+            if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(tile + mx4_scale_off(rr, lane >> 4)) = sc;
+            tile += kMxTile;
+        }
+    }
+}
+
+// E2M1 -> fp32: 3 bits of exponent and mantissa over 1 (values below 1: 0 and 0.5)
+__device__ __forceinline__ float mx4_value(uint32_t code)
+{
+    const uint32_t m = code & 7u;
+    const float a = m < 2u ? 0.5f * (float)m : __uint_as_float(((126u + (m >> 1)) << 23) | ((m & 1u) << 22));
+    return (code & 8u) ? -a : a;
+}
+// 2^(byte - 127)
+__device__ __forceinline__ float mx4_scale(uint32_t byte)
+{
+    return byte == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(byte ? byte << 23 : 0x00400000u);
+}
+
+// Tiles -> values, a warp a row of a tile, eight columns a lane.
+template <class T>
+__global__ void __launch_bounds__(256) us_mx4_dequantize_kernel(const uint8_t* mx, int64_t rows, int64_t K, T* out, int64_t ldo, int vec)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t kt = mx4_tiles(K, 256), groups = mx4_tiles(kt, kMxUnroll);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int64_t u = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; u < rows * groups; u += ((int64_t)gridDim.x * blockDim.x) >> 5) {
+        const int64_t r = u / groups, j0 = (u - r * groups) * kMxUnroll;
+        const uint8_t* tile = mx + ((r >> 7) * kt + j0) * kMxTile;
+        const uint32_t rr = (uint32_t)(r & 127);
+        uint32_t w[kMxUnroll], b[kMxUnroll];
+#pragma unroll
+        for (int i = 0; i < kMxUnroll; ++i) {
+            const bool in = j0 + i < kt;
+            w[i] = in ? __ldcg(reinterpret_cast<const uint32_t*>(tile + i * kMxTile + mx4_code_off(rr, lane >> 2) + 4 * (lane & 3))) : 0u;
+            b[i] = in ? __ldcg(tile + i * kMxTile + mx4_scale_off(rr, lane >> 4) + ((lane >> 2) & 3)) : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < kMxUnroll; ++i) {
+            const int64_t k = 256 * (j0 + i) + 8 * lane;
+            if (k >= K) break;
+            const float s = mx4_scale(b[i]);
+            Eight<T> y;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y.v[e] = from_f32<T>(mx4_value(w[i] >> (4 * e)) * s);
+            T* dst = out + r * ldo + k;
+            if (vec && k + 8 <= K) {
+#pragma unroll
+                for (int q = 0; q < (int)sizeof(Eight<T>) / 16; ++q) reinterpret_cast<uint4*>(dst)[q] = reinterpret_cast<const uint4*>(&y)[q];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (k + e < K) dst[e] = y.v[e];
+            }
+        }
+    }
+}
+
+// Row-major codes (two a byte) and scale bytes <-> tiles: a warp a row of a tile, byte by byte (loading, not computing).
+template <bool PACK>
+__global__ void __launch_bounds__(256) us_mx4_repack_kernel(uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, int64_t rows, int64_t K, uint8_t* mx)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t kt = mx4_tiles(K, 256);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int64_t u = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; u < rows * kt; u += ((int64_t)gridDim.x * blockDim.x) >> 5) {
+        const int64_t r = u / kt, j = u - r * kt;
+        uint8_t* tile = mx + ((r >> 7) * kt + j) * kMxTile;
+        const uint32_t rr = (uint32_t)(r & 127);
+        uint32_t* word = reinterpret_cast<uint32_t*>(tile + mx4_code_off(rr, lane >> 2) + 4 * (lane & 3));
+        const int64_t k0 = 256 * j + 8 * lane, b = 8 * j + lane;
+        uint32_t w = PACK ? 0u : *word;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t k = k0 + 2 * i;
+            if (k >= K) break;
+            uint8_t* c = codes + r * ldc + (k >> 1);
+            const uint32_t keep = k + 1 < K ? 0xFFu : 0x0Fu;
+            if (PACK) w |= ((uint32_t)*c & keep) << (8 * i);
+            else *c = (uint8_t)((w >> (8 * i)) & keep);
+        }
+        if (PACK) *word = w;
+        if (lane < 8) {
+            uint8_t* s = tile + mx4_scale_off(rr, lane >> 2) + (lane & 3);
+            if (PACK) *s = 32 * b < K ? scales[r * lds + b] : (uint8_t)0;
+            else if (32 * b < K) scales[r * lds + b] = *s;
+        }
+    }
+}
+
+// ---- the product ---------------------------------------------------------------------------------------------------------
+// D (128 weight rows x NB tokens, fp32, tensor memory) += W tile * X tile^T, 64 columns an instruction, the scale bytes copied from
+// shared to tensor memory in front of the four instructions of a 256-column stage. One warp copies (untiled bulk copies into a ring
+// of stages), one issues, four read the sums back and store.
+//   * Weights are the M side: every lane of tensor memory has a weight row, whatever the number of tokens; N = 16 .. 256.
+//   * Few row tiles: the columns are split over a cluster of up to 16 CTAs, whose sums are added through distributed shared memory
+//     in the order of the ranks: no workspace, no atomics, the same result every time.
+//   * Few tokens (FUSE): the CTA quantises its own columns of X while its weights are on the way: one launch instead of two.
+struct Mx4Params {
+    const uint8_t* w;
+    const uint8_t* x;      // tiles, or
+    const void* X;         // (FUSE) rows of x_type
+    void* Y;
+    int64_t ldx, ldy;
+    int32_t M, N, K, kt;
+    int32_t split, col_tiles;
+    int32_t stages;        // ring stages
+    int32_t x_type, y_type;
+    int32_t x_vec;         // rows of X take 16-byte loads
+    int32_t w_stable;      // the weights are complete whatever the stream's earlier work does
+    uint32_t* err;
+};
+enum { kF16 = 0, kBF16 = 1, kF32 = 2 };
+constexpr uint32_t kMxWait = 2000000u;   // bounded waits, ns >> 10
+
+template <int NB, bool FUSE>
+struct Mx4Shape {
+    static constexpr int kGroups = (NB + 127) / 128;                       // 128-token groups of scales
+    static constexpr int kXTile = kGroups * kMxScales + NB * 128;          // bytes of a stage's activations
+    static constexpr int kStage = kMxTile + (FUSE ? 0 : kXTile);
+    static constexpr int kSfCols = 8 + 8 * kGroups;                        // tensor-memory columns of a stage's scales
+    static constexpr int kCols = NB + 2 * kSfCols <= 64 ? 64 : NB + 2 * kSfCols <= 128 ? 128 : NB + 2 * kSfCols <= 256 ? 256 : 512;
+    static constexpr int kMaxStages = 12;
+};
+
+__device__ __forceinline__ uint64_t mx4_desc(uint32_t addr, uint32_t sbo, uint32_t swizzle)
+{
+    return ((uint64_t)1 << 16) | ((uint64_t)(sbo >> 4) << 32) | (1ull << 46) | ((uint64_t)swizzle << 61) | (uint64_t)((addr & 0x3FFFFu) >> 4);
+}
+__device__ __forceinline__ void mx4_mma(uint32_t elected, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %7, 0;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(elected) : "memory");
+}
+// 512 bytes of scales (128 rows, 4 blocks) -> 4 columns, the same in all four lane quarters
+__device__ __forceinline__ void mx4_copy_scales(uint32_t elected, uint32_t d, uint64_t s)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}"
+                 ::"r"(d), "l"(s), "r"(elected) : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t addr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float ld_cluster_f32(uint32_t local, uint32_t rank)
+{
+    uint32_t a;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(local), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void mx4_store(const Mx4Params& p, int64_t n, int64_t m, float v)
+{
+    if (p.y_type == kF32) static_cast<float*>(p.Y)[n * p.ldy + m] = v;
+    else if (p.y_type == kF16) static_cast<__half*>(p.Y)[n * p.ldy + m] = __float2half_rn(v);
+    else static_cast<__nv_bfloat16*>(p.Y)[n * p.ldy + m] = __float2bfloat16_rn(v);
+}
+
+// (FUSE) warps w of nw: the CTA's columns [256 t0, 256 t1) of the N tokens, quantised into operand tiles in shared memory
+template <class T, int NB>
+__device__ __forceinline__ void mx4_quantize_slice(const Mx4Params& p, uint8_t* xs, int t0, int t1, int w, int nw, int lane)
+{
+    constexpr int U = 4;
+    const int units = (t1 - t0) * p.N;
+#pragma unroll 1
+    for (int u0 = w; u0 < units; u0 += U * nw) {
+        Eight<T> x[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int u = u0 + i * nw, n = u % p.N, t = u / p.N;
+            const int64_t k = 256 * (int64_t)(t0 + t) + 8 * lane;
+            if (u < units) x[i] = load8(static_cast<const T*>(p.X) + n * p.ldx + k, p.K - k, p.x_vec && k + 8 <= p.K);
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int u = u0 + i * nw, n = u % p.N, t = u / p.N;
+            if (u >= units) break;
+            uint32_t sc;
+            const uint32_t codes = mx4_quantize_row(x[i], sc);
+            uint8_t* tile = xs + t * Mx4Shape<NB, true>::kXTile;
+            *reinterpret_cast<uint32_t*>(tile + mx4_code_off(n, lane >> 2) + 4 * (lane & 3)) = codes;
+            if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(tile + mx4_scale_off(n, lane >> 4)) = sc;
+        }
+    }
+}
+
+template <int NB, bool FUSE>
+__global__ void __launch_bounds__(192, 1) us_mx4_product_kernel(const __grid_constant__ Mx4Params p)
+{
+    using S = Mx4Shape<NB, FUSE>;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * S::kMaxStages + 2];
+    __shared__ uint32_t misc[2];   // tensor-memory address, dead
+    uint8_t* ring = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint8_t* xs = ring + (size_t)p.stages * S::kStage;   // (FUSE)
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8u * S::kMaxStages, b_x = b_empty + 8u * S::kMaxStages, b_done = b_x + 8u;
+    volatile uint32_t* dead = misc + 1;
+    const int rank = (int)blockIdx.x % p.split, tile = (int)blockIdx.x / p.split;
+    const int mt = tile / p.col_tiles, nt = tile - mt * p.col_tiles;
+    const int t0 = (int)((int64_t)rank * p.kt / p.split), t1 = (int)((int64_t)(rank + 1) * p.kt / p.split);
+    const int n0 = nt * NB, nn = min(NB, p.N - n0);
+    if (warp == 1) {
+        if (lane < S::kMaxStages) { mbar_init(b_full + 8u * lane, 1); mbar_init(b_empty + 8u * lane, 1); }
+        if (lane == 0) { mbar_init(b_x, 4); mbar_init(b_done, 1); misc[1] = 0; }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        __syncwarp();
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc)), "n"(S::kCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    // Only now: a dependent's CTA that fits beside this one takes tensor memory of its own, and then waits for this kernel.
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const uint32_t tm = *(volatile uint32_t*)misc;
+    bool ok = true;
+    if (warp == 0) {
+        // ---- copies ----
+        if (lane == 0) {
+            const uint8_t* w = p.w + ((int64_t)mt * p.kt + t0) * kMxTile;
+            const int n = t1 - t0;
+            const bool early = p.w_stable != 0;
+            int issued = 0;
+            // activations: rows of the tile(s) that hold tokens, rounded up to whole 8-row groups (the others' sums are not stored)
+            const int rows0 = min(128, (nn + 7) & ~7), rows1 = NB > 128 ? min(128, max(0, (nn - 128 + 7) & ~7)) : 0;
+            const uint32_t x_bytes = FUSE ? 0u : (uint32_t)(kMxScales + 128 * rows0 + (rows1 ? kMxScales + 128 * rows1 : 0));
+            const uint8_t* x0 = p.x + ((int64_t)(n0 >> 7) * p.kt + t0) * kMxTile;
+            const uint8_t* x1 = x0 + (int64_t)p.kt * kMxTile;
+            auto copy_w = [&](int i, int s) {
+                mbar_expect_tx(b_full + 8u * s, (uint32_t)kMxTile + x_bytes);
+                bulk_g2s(smem_u32(ring + (size_t)s * S::kStage), w + (int64_t)i * kMxTile, kMxTile, b_full + 8u * s);
+            };
+            auto copy_x = [&](int i, int s) {
+                const uint32_t d = smem_u32(ring + (size_t)s * S::kStage + kMxTile), b = b_full + 8u * s;
+                const uint8_t* a = x0 + (int64_t)i * kMxTile;
+                if (NB <= 128) {
+                    bulk_g2s(d, a, x_bytes, b);
+                } else {
+                    bulk_g2s(d, a, kMxScales, b);
+                    bulk_g2s(d + 2 * kMxScales, a + kMxScales, 128u * rows0, b);
+                    if (rows1) {
+                        const uint8_t* c = x1 + (int64_t)i * kMxTile;
+                        bulk_g2s(d + kMxScales, c, kMxScales, b);
+                        bulk_g2s(d + 2 * kMxScales + kMxCodes, c + kMxScales, 128u * rows1, b);
+                    }
+                }
+            };
+            const int first = min(n, p.stages);
+            if (early) for (int i = 0; i < first; ++i) copy_w(i, i);
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            for (int i = 0; i < first; ++i) {
+                if (!early) copy_w(i, i);
+                if (!FUSE) copy_x(i, i);
+            }
+            issued = first;
+            int s = 0;
+            uint32_t par = 0;
+            for (int i = first; i < n; ++i) {
+                if (!mbar_wait_bounded(b_empty + 8u * s, par, kMxWait)) { ok = false; break; }
+                copy_w(i, s);
+                if (!FUSE) copy_x(i, s);
+                ++issued;
+                if (++s == p.stages) { s = 0; par ^= 1u; }
+            }
+            // (nothing may be in flight when the CTA ends: the last copies are waited for here if the other warps gave up)
+            if (!ok)
+                for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait_bounded(b_full + 8u * (i % p.stages), (uint32_t)(i / p.stages) & 1u, kMxWait);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---- MMA issue: the whole warp walks the loop, one elected lane issues ----
+        const uint32_t leader = tc_elect();
+        // D = fp32; A, B = E2M1, K-major; scales E8M0 (bit 23); scale bytes 0, 1 of a column's four, or (| kUpper) 2, 3
+        const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(NB / 8) << 17) | (1u << 23) | (8u << 24);
+        const uint32_t kUpper = (2u << 4) | (2u << 29);
+        if (FUSE) {
+            ok = tc_wait_warp(b_x, 0, kMxWait, dead, true);
+            tc_fence_after();
+        }
+        int s = 0;
+        uint32_t par = 0;
+        for (int t = t0; t < t1 && ok; ++t) {
+            ok = tc_wait_warp(b_full + 8u * s, par, kMxWait, dead, true);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t a = smem_u32(ring + (size_t)s * S::kStage);
+            const uint32_t x = FUSE ? smem_u32(xs + (size_t)(t - t0) * S::kXTile) : a + kMxTile;
+            const uint32_t sf = tm + NB + (uint32_t)((t - t0) & 1) * S::kSfCols;   // (the other half may still be read)
+            const uint64_t sa = mx4_desc(a, 128, 0), sx = mx4_desc(x, 128, 0);
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {
+                mx4_copy_scales(leader, sf + 4u * h, sa + 32u * h);
+#pragma unroll
+                for (uint32_t g = 0; g < S::kGroups; ++g)
+                    mx4_copy_scales(leader, sf + 8u + 4u * (S::kGroups * h + g), sx + 32u * h + (kMxScales / 16) * g);
+            }
+            const uint64_t da = mx4_desc(a + kMxScales, 1024, 2), db = mx4_desc(x + S::kGroups * kMxScales, 1024, 2);
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j)
+                mx4_mma(leader, tm, da + 2u * j, db + 2u * j, idesc | ((j & 1u) ? kUpper : 0u), sf + 4u * (j >> 1),
+                        sf + 8u + 4u * S::kGroups * (j >> 1), t > t0 || j > 0);
+            tc_commit(leader, b_empty + 8u * s);
+            if (++s == p.stages) { s = 0; par ^= 1u; }
+        }
+        if (!ok) *dead = 1;
+        tc_commit(leader, b_done);
+        __syncwarp();
+    } else {
+        const int w = warp - 2;
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (FUSE) {
+            if (p.x_type == kF16) mx4_quantize_slice<__half, NB>(p, xs, t0, t1, w, 4, lane);
+            else if (p.x_type == kBF16) mx4_quantize_slice<__nv_bfloat16, NB>(p, xs, t0, t1, w, 4, lane);
+            else mx4_quantize_slice<float, NB>(p, xs, t0, t1, w, 4, lane);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_x);
+        }
+        ok = tc_wait_warp(b_done, 0, 4 * kMxWait, dead);
+        tc_fence_after();
+        const uint32_t quarter = (uint32_t)(warp & 3);
+        const int row = 32 * (int)quarter + lane;
+        const int64_t m = 128 * (int64_t)mt + row;
+        // (the ring is free: all copies have landed and have been read)
+        float* part = reinterpret_cast<float*>(ring);
+        if (ok && !*dead) {
+#pragma unroll 1
+            for (int c = 0; c < nn; c += 16) {
+                uint32_t r[16];
+                tc_ld16(tm + (quarter << 21) + (uint32_t)c, r);
+                if (p.split > 1) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) part[(c + i) * 128 + row] = __uint_as_float(r[i]);
+                } else if (m < p.M) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (c + i < nn) mx4_store(p, n0 + c + i, m, __uint_as_float(r[i]));
+                }
+            }
+        }
+        tc_fence_before();
+    }
+    if (!ok && lane == 0) {
+        *dead = 1;
+        atomicExch(p.err, kErrTimeout);
+    }
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "n"(S::kCols));
+    if (p.split > 1) {
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        // each rank adds the sums of a share of the tile's (token, row) pairs
+        const int total = nn * 128, per = (total / p.split + 31) & ~31, lo = min(total, rank * per), hi = rank == p.split - 1 ? total : min(total, lo + per);
+        const uint32_t part = smem_u32(ring);
+        for (int i = lo + (int)threadIdx.x; i < hi; i += 192) {
+            float v = 0.f;
+            for (int r = 0; r < p.split; ++r) v += ld_cluster_f32(part + 4u * i, (uint32_t)r);
+            const int64_t m = 128 * (int64_t)mt + (i & 127);
+            if (m < p.M) mx4_store(p, n0 + (i >> 7), m, v);
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+}
+
+}  // namespace us

@@ -7,7 +7,11 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
+
+#include <optional>
 
 #include "../../include/unionsparse.h"
 
@@ -164,6 +168,231 @@ PyObject* absmax_f16(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- MX4 ----
+
+// What a call runs on: the device of its first tensor made current, and the stream. A stream that the caller names becomes the current
+// one for the call, so that scratch and results come from its memory.
+struct Place {
+    std::optional<c10::cuda::CUDAGuard> device;
+    std::optional<c10::cuda::CUDAStreamGuard> guard;
+    void* stream = nullptr;
+    bool enter(PyObject* st, const at::Tensor& on)
+    {
+        if (!on.is_cuda()) {
+            PyErr_SetString(PyExc_ValueError, "expected a tensor on a CUDA device");
+            return false;
+        }
+        device.emplace(on.device());
+        if (!stream_of(st, on, &stream)) return false;
+        if (stream != (void*)c10::cuda::getCurrentCUDAStream(on.device().index()).stream())
+            guard.emplace(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), on.device().index()));
+        return true;
+    }
+};
+
+int type_of(at::ScalarType t) { return t == at::kHalf ? US_F16 : t == at::kBFloat16 ? US_BF16 : t == at::kFloat ? US_F32 : -1; }
+
+// Rows of a float type with unit column stride.
+bool is_rows(const at::Tensor& t)
+{
+    return t.dim() == 2 && type_of(t.scalar_type()) >= 0 && (t.stride(1) == 1 || t.size(1) <= 1) && t.size(1) >= 1 &&
+           (t.size(0) <= 1 || t.stride(0) >= t.size(1));
+}
+bool is_byte_rows(const at::Tensor& t, int64_t cols)
+{
+    return t.dim() == 2 && t.scalar_type() == at::kByte && t.size(1) == cols && (t.stride(1) == 1 || cols == 1) && (t.size(0) <= 1 || t.stride(0) >= cols);
+}
+// The tiles of a matrix: its bytes, on the device of `on`.
+bool is_mx(const at::Tensor& t, int64_t rows, int64_t K, const at::Tensor& on)
+{
+    return t.scalar_type() == at::kByte && t.is_contiguous() && t.device() == on.device() && us_mx4_bytes(rows, K) >= 0 && t.numel() == us_mx4_bytes(rows, K);
+}
+PyObject* bad(const char* text)
+{
+    PyErr_SetString(PyExc_ValueError, text);
+    return nullptr;
+}
+// The type asked for: None gives `otherwise`.
+bool dtype_of(PyObject* o, at::ScalarType otherwise, at::ScalarType* out)
+{
+    *out = otherwise;
+    if (o == Py_None) return true;
+    if (!THPDtype_Check(o)) {
+        PyErr_SetString(PyExc_TypeError, "dtype must be a torch.dtype");
+        return false;
+    }
+    *out = reinterpret_cast<THPDtype*>(o)->scalar_type;
+    if (type_of(*out) < 0) {
+        PyErr_SetString(PyExc_ValueError, "dtype must be float16, bfloat16 or float32");
+        return false;
+    }
+    return true;
+}
+// The caller's (rows, cols) output, or a new one of the type asked for.
+const at::Tensor* rows_out(PyObject* o, PyObject* dtype, at::ScalarType otherwise, const at::Tensor& on, int64_t rows, int64_t cols, at::Tensor* fresh)
+{
+    at::ScalarType type;
+    if (!dtype_of(dtype, otherwise, &type)) return nullptr;
+    if (o == Py_None) {
+        *fresh = new_output(on, rows, cols, type);
+        return fresh;
+    }
+    const at::Tensor* t = tensor(o, "out");
+    if (!t) return nullptr;
+    if (!is_rows(*t) || t->size(0) != rows || t->size(1) != cols || t->device() != on.device() || (dtype != Py_None && t->scalar_type() != type)) {
+        PyErr_Format(PyExc_ValueError, "out must be a (%lld, %lld) float tensor with unit column stride on the inputs' device", (long long)rows, (long long)cols);
+        return nullptr;
+    }
+    return t;
+}
+int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+PyObject* give(PyObject* o, at::Tensor&& fresh)
+{
+    if (o == Py_None) return THPVariable_Wrap(std::move(fresh));
+    Py_INCREF(o);
+    return o;
+}
+
+// mx4_quantize(X, mx, stream) -> the tiles
+PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 3) return PyErr_Format(PyExc_TypeError, "mx4_quantize takes 3 arguments");
+    HANDLE_TH_ERRORS
+    const at::Tensor* X = tensor(a[0], "X");
+    if (!X) return nullptr;
+    if (!is_rows(*X)) return bad("X must be a float16, bfloat16 or float32 (rows, K) tensor with unit column stride");
+    const int64_t rows = X->size(0), K = X->size(1);
+    Place at_;
+    if (!at_.enter(a[2], *X)) return nullptr;
+    at::Tensor fresh;
+    const at::Tensor* mx = &fresh;
+    if (a[1] == Py_None) {
+        const int64_t bytes = us_mx4_bytes(rows, K);
+        if (bytes < 0) return fail(US_ERR_INVALID_ARG, "us_mx4_quantize");
+        fresh = at::detail::empty_cuda({bytes}, at::kByte, X->device(), std::nullopt);
+    } else {
+        mx = tensor(a[1], "out");
+        if (!mx) return nullptr;
+        if (!is_mx(*mx, rows, K, *X)) return bad("out does not hold a matrix of X's shape on X's device");
+    }
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_mx4_quantize(X->data_ptr(), type_of(X->scalar_type()), row_stride(*X), rows, K, mx->data_ptr(), at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_mx4_quantize");
+    return give(a[1], std::move(fresh));
+    END_HANDLE_TH_ERRORS
+}
+
+// mx4_dequantize(mx, rows, K, dtype, out, stream) -> the values
+PyObject* mx4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 6) return PyErr_Format(PyExc_TypeError, "mx4_dequantize takes 6 arguments");
+    HANDLE_TH_ERRORS
+    const at::Tensor* mx = tensor(a[0], "data");
+    const int64_t rows = PyLong_AsLongLong(a[1]), K = PyLong_AsLongLong(a[2]);
+    if (!mx || PyErr_Occurred()) return nullptr;
+    Place at_;
+    if (!at_.enter(a[5], *mx)) return nullptr;
+    if (!is_mx(*mx, rows, K, *mx)) return bad("data does not hold a matrix of this shape");
+    at::Tensor fresh;
+    const at::Tensor* out = rows_out(a[4], a[3], at::kFloat, *mx, rows, K, &fresh);
+    if (!out) return nullptr;
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_mx4_dequantize(mx->data_ptr(), rows, K, out->data_ptr(), type_of(out->scalar_type()), row_stride(*out), at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_mx4_dequantize");
+    return give(a[4], std::move(fresh));
+    END_HANDLE_TH_ERRORS
+}
+
+// mx4_pack(codes, scales, K, stream) -> the tiles
+PyObject* mx4_pack(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 4) return PyErr_Format(PyExc_TypeError, "mx4_pack takes 4 arguments");
+    HANDLE_TH_ERRORS
+    const at::Tensor *codes = tensor(a[0], "codes"), *scales = codes ? tensor(a[1], "scales") : nullptr;
+    const int64_t K = PyLong_AsLongLong(a[2]);
+    if (!scales || PyErr_Occurred()) return nullptr;
+    if (K < 1 || K > (1ll << 30) || !is_byte_rows(*codes, (K + 1) / 2) || !is_byte_rows(*scales, (K + 31) / 32) || codes->size(0) != scales->size(0) ||
+        codes->device() != scales->device())
+        return bad("codes and scales must be uint8 (rows, ceil(K/2)) and (rows, ceil(K/32)) tensors with unit column stride on one device");
+    const int64_t rows = codes->size(0), bytes = us_mx4_bytes(rows, K);
+    if (bytes < 0) return fail(US_ERR_INVALID_ARG, "us_mx4_pack");
+    Place at_;
+    if (!at_.enter(a[3], *codes)) return nullptr;
+    at::Tensor mx = at::detail::empty_cuda({bytes}, at::kByte, codes->device(), std::nullopt);
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_mx4_pack(codes->data_ptr(), row_stride(*codes), scales->data_ptr(), row_stride(*scales), rows, K, mx.data_ptr(), at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_mx4_pack");
+    return THPVariable_Wrap(std::move(mx));
+    END_HANDLE_TH_ERRORS
+}
+
+// mx4_unpack(mx, rows, K, stream) -> (codes, scales)
+PyObject* mx4_unpack(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 4) return PyErr_Format(PyExc_TypeError, "mx4_unpack takes 4 arguments");
+    HANDLE_TH_ERRORS
+    const at::Tensor* mx = tensor(a[0], "data");
+    const int64_t rows = PyLong_AsLongLong(a[1]), K = PyLong_AsLongLong(a[2]);
+    if (!mx || PyErr_Occurred()) return nullptr;
+    Place at_;
+    if (!at_.enter(a[3], *mx)) return nullptr;
+    if (!is_mx(*mx, rows, K, *mx)) return bad("data does not hold a matrix of this shape");
+    at::Tensor codes = new_output(*mx, rows, (K + 1) / 2, at::kByte), scales = new_output(*mx, rows, (K + 31) / 32, at::kByte);
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_mx4_unpack(mx->data_ptr(), rows, K, codes.data_ptr(), (K + 1) / 2, scales.data_ptr(), (K + 31) / 32, at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_mx4_unpack");
+    PyObject *c = THPVariable_Wrap(std::move(codes)), *sc = THPVariable_Wrap(std::move(scales));
+    return Py_BuildValue("NN", c, sc);
+    END_HANDLE_TH_ERRORS
+}
+
+// mx4_linear(X, rows, w, M, K, out, dtype, stable, stream) -> the product; rows >= 0: X holds the tiles of that many rows
+PyObject* mx4_linear(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "mx4_linear takes 9 arguments");
+    HANDLE_TH_ERRORS
+    const at::Tensor *X = tensor(a[0], "X"), *w = X ? tensor(a[2], "w") : nullptr;
+    const int64_t rows = PyLong_AsLongLong(a[1]), M = PyLong_AsLongLong(a[3]), K = PyLong_AsLongLong(a[4]);
+    if (!w || PyErr_Occurred()) return nullptr;
+    Place at_;
+    if (!at_.enter(a[8], *X)) return nullptr;
+    if (!is_mx(*w, M, K, *X)) return bad("w does not hold a matrix of this shape on X's device");
+    if (rows >= 0 ? !is_mx(*X, rows, K, *X) : (!is_rows(*X) || X->size(1) != K))
+        return bad("X must be a float16, bfloat16 or float32 (N, K) tensor with unit column stride, K as the weight's");
+    const int64_t N = rows >= 0 ? rows : X->size(0);
+    at::Tensor fresh, scratch;
+    const at::Tensor* out = rows_out(a[5], a[6], rows >= 0 ? at::kHalf : X->scalar_type(), *X, N, M, &fresh);
+    if (!out) return nullptr;
+    const uint32_t flags = a[7] == Py_True ? US_MX4_W_STABLE : 0u;
+    const int yt = type_of(out->scalar_type());
+    const int64_t ldy = row_stride(*out);
+    void* y = out->data_ptr();
+    us_status s;
+    if (rows >= 0) {
+        Py_BEGIN_ALLOW_THREADS
+        s = us_mx4_matmul(X->data_ptr(), N, w->data_ptr(), M, K, y, yt, ldy, flags, at_.stream);
+        Py_END_ALLOW_THREADS
+    } else {
+        const int64_t bytes = us_mx4_linear_scratch(N, M, K);
+        if (bytes > 0) scratch = at::detail::empty_cuda({bytes}, at::kByte, X->device(), std::nullopt);
+        Py_BEGIN_ALLOW_THREADS
+        s = us_mx4_linear(X->data_ptr(), type_of(X->scalar_type()), row_stride(*X), N, w->data_ptr(), M, K, y, yt, ldy,
+                          bytes > 0 ? scratch.data_ptr() : nullptr, bytes, flags, at_.stream);
+        Py_END_ALLOW_THREADS
+    }
+    if (s != US_OK) return fail(s, "us_mx4_linear");
+    return give(a[5], std::move(fresh));
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject* set_error(PyObject*, PyObject* cls)
 {
     Py_XDECREF(g_error);
@@ -179,6 +408,11 @@ PyMethodDef methods[] = {
     {"spmm", fast(spmm), METH_FASTCALL, nullptr},
     {"spmm_requant", fast(spmm_requant), METH_FASTCALL, nullptr},
     {"absmax_f16", fast(absmax_f16), METH_FASTCALL, nullptr},
+    {"mx4_quantize", fast(mx4_quantize), METH_FASTCALL, nullptr},
+    {"mx4_dequantize", fast(mx4_dequantize), METH_FASTCALL, nullptr},
+    {"mx4_pack", fast(mx4_pack), METH_FASTCALL, nullptr},
+    {"mx4_unpack", fast(mx4_unpack), METH_FASTCALL, nullptr},
+    {"mx4_linear", fast(mx4_linear), METH_FASTCALL, nullptr},
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
