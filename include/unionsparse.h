@@ -28,8 +28,10 @@ typedef enum us_status {
     US_ERR_ALLOC = 5,         /* host or device allocation failed                           */
     US_ERR_CUDA = 6,          /* a CUDA runtime call failed (see us_last_error)             */
     US_ERR_DEVICE_TIMEOUT = 7,/* a bounded wait inside a kernel gave up (no hang, no trap)  */
-    US_ERR_SCRATCH_TOO_SMALL = 8 /* us_spmm_static_scratch: the problem needs more scratch than
-                                    the library's fixed device array holds                   */
+    US_ERR_SCRATCH_TOO_SMALL = 8,/* us_spmm_static_scratch: the problem needs more scratch than
+                                    the library's fixed device array holds; or than was given */
+    US_ERR_DEVICE_INDEX = 9   /* a block number, length or token count on the device is out of
+                                 range (us_kv_last_error)                                    */
 } us_status;
 
 /*
@@ -316,6 +318,64 @@ int64_t us_mx4_linear_scratch(int64_t N, int64_t M, int64_t K);
 us_status us_mx4_linear(const void* X, int32_t x_type, int64_t ldx, int64_t N, const void* w_mx, int64_t M, int64_t K, void* Y,
                         int32_t y_type, int64_t ldy, void* scratch, int64_t scratch_bytes, uint32_t flags, void* stream);
 us_status us_mx4_last_error(void);
+
+/*
+ * The cache of keys and values in 8 bits, and attention over it (no counterpart in the paper): what stands between the
+ * Q/K/V projection of a decoder layer and its O projection.
+ *
+ * A pool of blocks of block_tokens tokens (16, 32, 64, 128 or 256): codes int8 [n_blocks][n_kv_heads][block_tokens][head_dim]
+ * (head_dim 64 or 128), one fp32 step >= 0 for each (block, head), [n_blocks][n_kv_heads]; K and V apart. value = code * step.
+ * us_kv_create describes a pool that the caller owns (device memory, codes 16-byte aligned); the handle holds no device memory, and
+ * any number of calls on it may be in flight. A pool has fewer than 2^31 (token, head) places.
+ *
+ * A batch of sequences (us_kv_seqs; all arrays on the device, read by the kernels when they run):
+ *   block_table  n_seqs rows (stride table_stride) of table_width block numbers: token t of a sequence is at place t % block_tokens of
+ *                block table[t / block_tokens]. Entries that no token in question needs are not read as block numbers.
+ *   lengths      tokens of each sequence, this call's new ones included.
+ *   cu_tokens    n_seqs + 1 entries: rows [cu[s], cu[s + 1]) of the call's N rows are the new tokens of sequence s, its last ones.
+ *                NULL: one row each (N = n_seqs).
+ * Where an entry does not fit (a block number outside the pool, a length below 0 or beyond the table, more new tokens
+ * than the length, cu_tokens that fall or pass N), kernels leave out what it stands for, touch nothing outside the arrays, and
+ * us_kv_last_error, which synchronises the device, reports (and clears) US_ERR_DEVICE_INDEX; US_ERR_DEVICE_TIMEOUT as elsewhere.
+ *
+ * us_kv_append: writes the new tokens. For each block and head that gets some:
+ *     step' = RN_f32(max|new| / 127), and at least step if older tokens of the sequence are in the block
+ *     older codes become RNE(code * step / step') (quotient exact), where step' > step
+ *     new codes = clamp(RNE(x / step'), -127, 127) (quotient exact; 0 where step' = 0)
+ *   Infinities and NaN do not count in max|new|; they are stored as +-127 (0 where step' = 0) and 0. K, V: us_type rows (token, head) of
+ *   head_dim elements, strides in elements. A block that gets tokens must belong to one sequence only. Places behind the
+ *   sequence's end keep what they hold.
+ * us_kv_read: the values of the first `tokens` places of every sequence, [n_seqs][tokens][n_kv_heads][head_dim] of us_type; zero
+ *   from a sequence's end on. cu_tokens is not read.
+ * us_kv_attention: for each new token and query head (n_heads, a multiple of n_kv_heads: head h reads cache head
+ *   h / (n_heads / n_kv_heads)), out = sum_t p_t v_t / sum_t p_t, p_t = exp(scale q.k_t), over the tokens t that the query at place i of its
+ *   sequence sees: t < length; with causal, t <= i; with window > 0, t > i - window. A query that sees nothing gives 0. The new tokens'
+ *   keys and values are read from the cache: append them first. Q and out: US_F16 or US_BF16 (both the same), rows (token, head),
+ *   strides in elements; rows past cu_tokens[n_seqs] are left as they are. lse (N x n_heads fp32, or NULL): the logarithm
+ *   of the sum of exp(scale q.k_t), -inf where nothing is seen. scratch: us_kv_attention_scratch bytes, 16-byte aligned,
+ *   for one call at a time; need not be cleared. Blocks wholly in front of every window may be gone (any table entry).
+ * All three are enqueue-only on `stream` on the current device. N or n_seqs = 0: nothing is done.
+ * Errors: INVALID_ARG, UNSUPPORTED, SCRATCH_TOO_SMALL, CUDA.
+ */
+typedef struct us_kv us_kv;
+typedef struct us_kv_seqs {
+    const int32_t* block_table;
+    int64_t table_stride;
+    const int32_t* lengths;
+    const int32_t* cu_tokens;
+    int32_t n_seqs, table_width;
+} us_kv_seqs;
+us_status us_kv_create(void* k_codes, void* v_codes, void* k_steps, void* v_steps, int64_t n_blocks, int32_t n_kv_heads,
+                       int32_t block_tokens, int32_t head_dim, us_kv** out);
+us_status us_kv_append(us_kv* h, const us_kv_seqs* seqs, int64_t N, const void* K, const void* V, int32_t type,
+                       int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, void* stream);
+us_status us_kv_read(us_kv* h, const us_kv_seqs* seqs, int64_t tokens, void* K, void* V, int32_t type, void* stream);
+int64_t us_kv_attention_scratch(const us_kv* h, int64_t N, int32_t n_seqs, int32_t n_heads);
+us_status us_kv_attention(us_kv* h, const us_kv_seqs* seqs, int64_t N, const void* Q, int32_t type, int32_t n_heads,
+                          int64_t q_token_stride, int64_t q_head_stride, float scale, int32_t causal, int32_t window, void* out,
+                          int64_t o_token_stride, int64_t o_head_stride, float* lse, void* scratch, int64_t scratch_bytes, void* stream);
+us_status us_kv_last_error(void);
+us_status us_kv_destroy(us_kv* h);
 
 const char* us_status_string(us_status s);
 

@@ -31,6 +31,7 @@ EXPORTS = ["us_encode", "us_get_stats", "us_decode", "us_get_row_order", "us_spm
            "us_last_error", "us_debug_withhold_copy", "us_stage_timers", "us_destroy", "us_spmm_bytes", "us_launch_info", "us_launch_kernel",
            "us_mx4_bytes", "us_mx4_quantize", "us_mx4_dequantize", "us_mx4_pack", "us_mx4_unpack", "us_mx4_matmul",
            "us_mx4_linear_scratch", "us_mx4_linear", "us_mx4_last_error",
+           "us_kv_create", "us_kv_append", "us_kv_read", "us_kv_attention_scratch", "us_kv_attention", "us_kv_last_error", "us_kv_destroy",
            "us_status_string"]
 
 
@@ -80,6 +81,21 @@ _lib.us_mx4_linear_scratch.argtypes = [_i64, _i64, _i64]
 _lib.us_mx4_linear_scratch.restype = _i64
 _lib.us_mx4_linear.argtypes = [_vp, _i32, _i64, _i64, _vp, _i64, _i64, _vp, _i32, _i64, _vp, _i64, ctypes.c_uint32, _vp]
 _lib.us_mx4_last_error.argtypes = []
+
+
+class us_kv_seqs(ctypes.Structure):
+    _fields_ = [("block_table", _vp), ("table_stride", _i64), ("lengths", _vp), ("cu_tokens", _vp), ("n_seqs", _i32), ("table_width", _i32)]
+
+
+_seqs = ctypes.POINTER(us_kv_seqs)
+_lib.us_kv_create.argtypes = [_vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, ctypes.POINTER(_vp)]
+_lib.us_kv_append.argtypes = [_vp, _seqs, _i64, _vp, _vp, _i32, _i64, _i64, _i64, _i64, _vp]
+_lib.us_kv_read.argtypes = [_vp, _seqs, _i64, _vp, _vp, _i32, _vp]
+_lib.us_kv_attention_scratch.argtypes = [_vp, _i64, _i32, _i32]
+_lib.us_kv_attention_scratch.restype = _i64
+_lib.us_kv_attention.argtypes = [_vp, _seqs, _i64, _vp, _i32, _i32, _i64, _i64, ctypes.c_float, _i32, _i32, _vp, _i64, _i64, _vp, _vp, _i64, _vp]
+_lib.us_kv_last_error.argtypes = []
+_lib.us_kv_destroy.argtypes = [_vp]
 _lib.us_status_string.argtypes = [ctypes.c_int]
 _lib.us_status_string.restype = ctypes.c_char_p
 
@@ -415,3 +431,81 @@ def mx4_linear(X, w: Mx4, out=None, dtype=None, stream=None):
 def mx4_check():
     """Waits for the current device and raises if a product on it gave up a bounded wait."""
     _check(_lib.us_mx4_last_error(), "us_mx4_last_error")
+
+
+# ---- the cache of keys and values in 8 bits ----
+
+def us_kv_create(k_codes_ptr: int, v_codes_ptr: int, k_steps_ptr: int, v_steps_ptr: int, n_blocks: int, n_kv_heads: int, block_tokens: int,
+                 head_dim: int) -> int:
+    """Raw call: device pointers as integers. Returns the handle; the memory stays the caller's."""
+    h = _vp()
+    _check(_lib.us_kv_create(k_codes_ptr, v_codes_ptr, k_steps_ptr, v_steps_ptr, int(n_blocks), int(n_kv_heads), int(block_tokens), int(head_dim),
+                             ctypes.byref(h)), "us_kv_create")
+    return h.value
+
+
+class KVCache:
+    """Keys and values of a pool of token blocks as int8 codes with a float32 step for each (block, head): value = code * step.
+
+    Device tensors, contiguous: codes (n_blocks, n_kv_heads, block_tokens, head_dim), steps (n_blocks, n_kv_heads). block_tokens 16, 32,
+    64, 128 or 256; head_dim 64 or 128. The tensors are the caller's to copy, move between blocks or save.
+
+    The calls take a batch of sequences: block_table (S, width) int32, the sequence's blocks in order; lengths (S,) int32, this call's new
+    tokens included; cu_tokens (S + 1,) int32, where each sequence's rows begin among the call's, or None for one row each."""
+
+    def __init__(self, k_codes, v_codes, k_steps, v_steps):
+        import torch
+        self.handle = None
+        _native()
+        for c in (k_codes, v_codes):
+            if c.dtype != torch.int8 or c.dim() != 4 or not c.is_contiguous() or not c.is_cuda or c.shape != k_codes.shape or c.device != k_codes.device:
+                raise ValueError("codes must be two contiguous int8 (n_blocks, n_kv_heads, block_tokens, head_dim) tensors on one CUDA device")
+        for s in (k_steps, v_steps):
+            if s.dtype != torch.float32 or tuple(s.shape) != tuple(k_codes.shape[:2]) or not s.is_contiguous() or s.device != k_codes.device:
+                raise ValueError("steps must be two contiguous float32 (n_blocks, n_kv_heads) tensors on the codes' device")
+        self.k_codes, self.v_codes, self.k_steps, self.v_steps = k_codes, v_codes, k_steps, v_steps
+        self.n_blocks, self.n_kv_heads, self.block_tokens, self.head_dim = k_codes.shape
+        self.handle = us_kv_create(k_codes.data_ptr(), v_codes.data_ptr(), k_steps.data_ptr(), v_steps.data_ptr(), self.n_blocks, self.n_kv_heads,
+                                   self.block_tokens, self.head_dim)
+
+    @classmethod
+    def new(cls, n_blocks: int, n_kv_heads: int, head_dim: int, block_tokens: int = 64, device="cuda"):
+        """A pool of its own memory, all zero."""
+        import torch
+        codes = [torch.zeros((n_blocks, n_kv_heads, block_tokens, head_dim), dtype=torch.int8, device=device) for _ in range(2)]
+        steps = [torch.zeros((n_blocks, n_kv_heads), dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(*codes, *steps)
+
+    def append(self, k, v, block_table, lengths, cu_tokens=None, stream=None):
+        """Writes new tokens, the last ones of their sequences: k, v (N, n_kv_heads, head_dim) float16, bfloat16 or float32 (any token and
+        head strides). Finite values are expected; others do not count for a step."""
+        _ext.kv_append(self.handle, self.k_codes, k, v, block_table, lengths, cu_tokens, stream)
+
+    def read(self, block_table, lengths, tokens: int, dtype=None, stream=None):
+        """(K, V): values of the first `tokens` places of each sequence, (S, tokens, n_kv_heads, head_dim), float32 unless another type is
+        asked for; zero behind a sequence's end."""
+        return _ext.kv_read(self.handle, self.k_codes, block_table, lengths, int(tokens), dtype, stream)
+
+    def attention(self, q, block_table, lengths, cu_tokens=None, scale=None, causal=True, window=0, out=None, lse=None, stream=None):
+        """Attention of q (N, n_heads, head_dim), float16 or bfloat16, over the sequences' cached tokens, their new ones (appended before)
+        included. scale: head_dim ** -0.5 unless given. causal: a token sees itself and those before it, else its whole sequence;
+        window > 0: none further back than window - 1. out: like q; lse: float32 (N, n_heads), gets the logarithm of the softmax's sum."""
+        return _ext.kv_attention(self.handle, self.k_codes, q, block_table, lengths, cu_tokens, self.head_dim ** -0.5 if scale is None else scale,
+                                 causal, window, out, lse, stream)
+
+    def check(self):
+        """Waits for the device and raises if a call on it met a block number, length or token count out of range."""
+        import torch
+        with torch.cuda.device(self.k_codes.device):
+            _check(_lib.us_kv_last_error(), "us_kv_last_error")
+
+    def close(self):
+        if self.handle:
+            _lib.us_kv_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

@@ -1270,6 +1270,7 @@ const char* us_status_string(us_status s)
         case US_ERR_CUDA: return "CUDA error";
         case US_ERR_DEVICE_TIMEOUT: return "bounded device wait ran out";
         case US_ERR_SCRATCH_TOO_SMALL: return "problem needs more scratch than the fixed device array holds";
+        case US_ERR_DEVICE_INDEX: return "a kernel met a block number, length or token count out of range";
     }
     return "unknown status";
 }

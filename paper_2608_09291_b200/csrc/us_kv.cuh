@@ -1,0 +1,825 @@
+// The cache of keys and values in 8 bits: append, read back, and attention over it.
+//
+// Pool of blocks of T tokens; codes int8 [block][kv head][T][D], one fp32 step for each (block, kv head), K and V apart:
+// value = code * step. A sequence's token t lies in block table[s][t / T] at place t % T.
+#pragma once
+#include "us_mx4.cuh"
+
+#include <cuda.h>
+
+namespace us {
+
+constexpr uint32_t kErrIndex = 2;   // a block number outside the pool, a length beyond the table, token counts that do not add up
+
+struct KvSeqs {
+    const int32_t* table;     // S rows of `width` block numbers
+    int64_t table_stride;
+    const int32_t* lengths;   // S, the new tokens included
+    const int32_t* cu;        // S + 1 sums of the new tokens of the sequences before, or nullptr: one each
+    int32_t S, width;
+    int64_t N;                // new tokens
+};
+
+struct KvPool {
+    int8_t *k, *v;
+    float *k_step, *v_step;
+    int32_t blocks, Hkv, T, D;
+    uint32_t* err;
+};
+
+struct KvSeq {
+    int64_t first;      // row of its first new token
+    int32_t len, n;     // tokens in all, new ones
+};
+// Sequence s with everything that memory depends on brought into range; `wrong`: something was not.
+__device__ __forceinline__ KvSeq kv_seq(const KvSeqs& q, const KvPool& p, int s, bool& wrong)
+{
+    KvSeq r;
+    const int64_t most = (int64_t)q.width * p.T;
+    const int32_t len = __ldcg(q.lengths + s);
+    int64_t a = s, b = (int64_t)s + 1;
+    if (q.cu) { a = __ldcg(q.cu + s); b = __ldcg(q.cu + s + 1); }
+    wrong = len < 0 || len > most || a < 0 || b < a || b > q.N || b - a > len;
+    r.len = (int32_t)max((int64_t)0, min((int64_t)len, most));
+    r.first = max((int64_t)0, min(a, q.N));
+    r.n = (int32_t)max((int64_t)0, min(min(b, q.N) - r.first, (int64_t)r.len));
+    return r;
+}
+
+// ---- append --------------------------------------------------------------------------------------------------------------
+// code = RNE(x / s) for the exact quotient: the rounded product x * (1 / s) is off by at most one, and the sign of a fused
+// multiply-add says on which side of the border next to it x lies (exact: a rounded sum is never on the other side of 0).
+__device__ __forceinline__ int kv_code(float x, float s, float inv)
+{
+    if (s < 1e-30f) {   // (borders that fp32 would lose to underflow)
+        const double q = s > 0.f ? rint((double)x / (double)s) : 0.0;
+        return q != q ? 0 : (int)fmin(fmax(q, -127.0), 127.0);
+    }
+    float r = rintf(x * inv);
+    const float up = fmaf(-(r + 0.5f), s, x), down = fmaf(-(r - 0.5f), s, x);
+    const bool odd = (r - 2.f * truncf(0.5f * r)) != 0.f;
+    if (up > 0.f || (up == 0.f && odd)) r += 1.f;
+    else if (down < 0.f || (down == 0.f && odd)) r -= 1.f;
+    return r != r ? 0 : (int)fminf(fmaxf(r, -127.f), 127.f);
+}
+
+struct KvAppend {
+    KvPool pool;
+    KvSeqs seqs;
+    const void* x[2];              // K, V: new tokens
+    int64_t token_stride[2], head_stride[2];
+    int32_t vec;                   // rows take 16-byte loads
+};
+
+// A CTA takes one block that gets tokens, one head, K or V: largest magnitude, step, the older codes if the step grew, the new codes.
+// Bound by the bytes of the new tokens where there are many, by latency for single ones.
+template <class T_>
+__global__ void __launch_bounds__(128) us_kv_append_kernel(const __grid_constant__ KvAppend a)
+{
+    __shared__ uint32_t red[4];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const KvPool& p = a.pool;
+    const int lane = threadIdx.x & 31, h = blockIdx.y, which = blockIdx.z;
+    // which sequence's which block
+    int s = -1, j = 0;
+    int64_t before = 0;
+    bool any_wrong = false;
+    for (int base = 0; base < a.seqs.S; base += 32) {
+        int cnt = 0;
+        if (base + lane < a.seqs.S) {
+            bool wrong;
+            const KvSeq q = kv_seq(a.seqs, p, base + lane, wrong);
+            any_wrong |= wrong;
+            if (q.n > 0 && !wrong) cnt = (q.len - 1) / p.T - (q.len - q.n) / p.T + 1;
+        }
+        int sum = cnt;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        const bool here = (int64_t)blockIdx.x >= before + sum - cnt && (int64_t)blockIdx.x < before + sum;
+        const uint32_t who = __ballot_sync(0xffffffffu, here);
+        if (who) {
+            const int l = __ffs(who) - 1;
+            s = base + l;
+            j = (int)((int64_t)blockIdx.x - before) - __shfl_sync(0xffffffffu, sum - cnt, l);
+            break;
+        }
+        before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    if (any_wrong) atomicExch(p.err, kErrIndex);
+    if (s < 0) return;
+    bool wrong;
+    const KvSeq q = kv_seq(a.seqs, p, s, wrong);
+    const int start = q.len - q.n, bi = start / p.T + j;
+    const int lo = max(start, bi * p.T), hi = min(q.len, (bi + 1) * p.T), held = lo - bi * p.T, n = hi - lo;
+    const int32_t blk = __ldcg(a.seqs.table + (int64_t)s * a.seqs.table_stride + bi);
+    if (blk < 0 || blk >= p.blocks) {
+        if (threadIdx.x == 0) atomicExch(p.err, kErrIndex);
+        return;
+    }
+    const int D = p.D, per = D / 8;   // lanes a row
+    const int64_t place = (int64_t)blk * p.Hkv + h;
+    float* step_at = (which ? p.v_step : p.k_step) + place;
+    int8_t* codes = (which ? p.v : p.k) + place * p.T * D;
+    const float old = held ? *step_at : 0.f;
+    const T_* x = static_cast<const T_*>(a.x[which]) + (q.first + lo - start) * a.token_stride[which] + (int64_t)h * a.head_stride[which];
+    const int units = n * per;
+    constexpr int KEEP = 4;
+    Eight<T_> kept[KEEP];
+    uint32_t big = 0;
+    auto load = [&](int u) {
+        const int r = u / per, c = u - r * per;
+        return load8(x + r * a.token_stride[which] + 8 * c, 8, a.vec != 0);
+    };
+    auto take = [&](const Eight<T_>& e) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t b = __float_as_uint(to_f32(e.v[i])) & 0x7FFFFFFFu;
+            if (b < 0x7F800000u) big = max(big, b);   // (infinities and NaN do not count)
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+        if ((int)threadIdx.x + 128 * i < units) kept[i] = load(threadIdx.x + 128 * i);
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+        if ((int)threadIdx.x + 128 * i < units) take(kept[i]);
+    for (int u = threadIdx.x + 128 * KEEP; u < units; u += 128) take(load(u));
+    big = __reduce_max_sync(0xffffffffu, big);
+    if (lane == 0) red[threadIdx.x >> 5] = big;
+    __syncthreads();
+    big = max(max(red[0], red[1]), max(red[2], red[3]));
+    const float step = fmaxf(old, __fdiv_rn(__uint_as_float(big), 127.f));
+    if (threadIdx.x == 0) *step_at = step;
+    const float inv = step > 0.f ? __fdiv_rn(1.f, step) : 0.f;
+    auto put = [&](int u, const Eight<T_>& e) {
+        uint32_t w[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i >> 2] |= ((uint32_t)kv_code(to_f32(e.v[i]), step, inv) & 0xFFu) << (8 * (i & 3));
+        *reinterpret_cast<uint2*>(codes + (int64_t)held * D + 8 * (int64_t)u) = make_uint2(w[0], w[1]);
+    };
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+        if ((int)threadIdx.x + 128 * i < units) put(threadIdx.x + 128 * i, kept[i]);
+    for (int u = threadIdx.x + 128 * KEEP; u < units; u += 128) put(u, load(u));
+    if (step > old && held) {   // the tokens that were there, in the larger step: RNE(code * old / step), the border decided in 64 bits
+        for (int u = threadIdx.x; u < held * D / 4; u += 128) {
+            uint32_t* at = reinterpret_cast<uint32_t*>(codes) + u;
+            const uint32_t w = *at;
+            uint32_t o = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const double c = (double)(int8_t)(w >> (8 * i)) * (double)old;
+                o |= ((uint32_t)(int)rint(c / (double)step) & 0xFFu) << (8 * i);
+            }
+            *at = o;
+        }
+    }
+}
+
+// ---- read ------------------------------------------------------------------------------------------------------------------
+// K and V of the first `tokens` places of every sequence as values, [s][t][head][D]; 0 from a sequence's end on. A warp a row pair.
+template <class T_>
+__global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int64_t tokens, T_* k_out, T_* v_out)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int per = p.D / 8;
+    const int64_t total = (int64_t)q.S * tokens * p.Hkv * per;
+    const int64_t most = (int64_t)q.width * p.T;
+    for (int64_t u = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; u < total; u += (int64_t)gridDim.x * blockDim.x) {
+        const int c = (int)(u % per);
+        const int64_t row = u / per, st = row / p.Hkv;
+        const int h = (int)(row - st * p.Hkv), s = (int)(st / tokens);
+        const int64_t t = st - s * tokens;
+        const int32_t len = __ldcg(q.lengths + s);
+        Eight<T_> e[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[0].v[i] = e[1].v[i] = from_f32<T_>(0.f);
+        if (t < len && t < most) {
+            const int32_t blk = __ldcg(q.table + (int64_t)s * q.table_stride + t / p.T);
+            if (blk >= 0 && blk < p.blocks) {
+                const int64_t place = (int64_t)blk * p.Hkv + h, at = (place * p.T + t % p.T) * p.D + 8 * c;
+                const uint2 w[2] = {__ldcg(reinterpret_cast<const uint2*>(p.k + at)), __ldcg(reinterpret_cast<const uint2*>(p.v + at))};
+                const float f[2] = {__ldcg(p.k_step + place), __ldcg(p.v_step + place)};
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) e[b].v[i] = from_f32<T_>((float)(int8_t)((i < 4 ? w[b].x : w[b].y) >> (8 * (i & 3))) * f[b]);
+            } else {
+                atomicExch(p.err, kErrIndex);
+            }
+        } else if (t < len || len < 0) {
+            atomicExch(p.err, kErrIndex);
+        }
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(Eight<T_>) / 16; ++i) {
+            reinterpret_cast<uint4*>(k_out + row * p.D + 8 * c)[i] = reinterpret_cast<const uint4*>(&e[0])[i];
+            reinterpret_cast<uint4*>(v_out + row * p.D + 8 * c)[i] = reinterpret_cast<const uint4*>(&e[1])[i];
+        }
+    }
+}
+
+// ---- attention: few query rows a cache head (decode) ---------------------------------------------------------------------------
+// out = sum_t p_t v_t / sum_t p_t, p_t = 2^(s_t - m), s = scale log2(e) q.k, in one pass with the running maximum m of each row.
+//   * The rows of a tile are the query heads that share a cache head (times the sequence's new tokens): 8 NT of them are the N side
+//     of mma.sync m16n8k16, 16 tokens (then 16 of D) the M side: the cache's bytes are read once for all of them.
+//   * Codes become fp16 in registers, exactly (0x6400 | byte is 1024 + byte); a step is one number for 16 tokens, so K's is
+//     a factor of the scores and V's a factor of p. p is rounded to fp16 with 2^7 in front and V's step relative to the
+//     largest so far: what a row sums stays between 2^-24 and 2^15 of the largest term; sums are fp32.
+//   * m follows the true maximum only where it is 2^8 behind, so most tiles need no reduction over lanes and no rescaling.
+//   * All (sequence, row tile, head) items in a row, 64 tokens a unit: every CTA takes the same number of units, whatever the lengths.
+//     An item that is cut leaves its parts in scratch, and a second kernel joins them in the order of the CTAs.
+// A warp copies (TMA, swizzled so that the fragment loads meet no bank twice); four read, 16 tokens of a unit each, with
+// sums of their own that are joined at an item's end.
+constexpr int kKvTile = 64;
+struct KvAttend {
+    CUtensorMap k_map, v_map;
+    KvPool pool;
+    KvSeqs seqs;
+    const void* q;
+    int64_t q_token, q_head;
+    void* out;
+    int64_t o_token, o_head;
+    float* lse;
+    float* part;             // two parts a CTA: rows x D sums, then rows x {m, l}
+    float scale2;            // scale log2(e)
+    int32_t Hq, G;           // query heads, a cache head's
+    int32_t causal, window;
+    int32_t q_vec;
+    int32_t stages;
+    int32_t ctas;
+};
+
+struct KvItem {
+    KvSeq seq;
+    int32_t rows;        // query rows of a head
+    int32_t row_tiles;
+    int32_t lo;          // first token that any of its queries sees
+    int32_t t_lo, tiles; // first unit of 64 tokens, units (1 if it sees nothing)
+};
+template <int R>
+__device__ __forceinline__ KvItem kv_item(const KvAttend& a, int s, bool& wrong)
+{
+    KvItem r;
+    r.seq = kv_seq(a.seqs, a.pool, s, wrong);
+    r.rows = r.seq.n * a.G;
+    r.row_tiles = (r.rows + R - 1) / R;
+    r.lo = a.window > 0 ? max(0, r.seq.len - r.seq.n - a.window + 1) : 0;
+    r.t_lo = r.lo / kKvTile;
+    r.tiles = max(1, (r.seq.len + kKvTile - 1) / kKvTile - r.t_lo);
+    return r;
+}
+
+// Where a CTA's units begin and end.
+struct KvRange {
+    long long total, u0, u1;
+    int s;                // sequence of unit u0
+    long long in_seq;     // u0 from its first unit
+};
+template <int R>
+__device__ KvRange kv_range(const KvAttend& a, int cta, int lane)
+{
+    KvRange r;
+    r.total = 0;
+    bool any = false;
+    for (int base = 0; base < a.seqs.S; base += 32) {
+        long long c = 0;
+        if (base + lane < a.seqs.S) {
+            bool wrong;
+            const KvItem it = kv_item<R>(a, base + lane, wrong);
+            any |= wrong;
+            c = (long long)it.row_tiles * a.pool.Hkv * it.tiles;
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+        r.total += c;
+    }
+    if (any) atomicExch(a.pool.err, kErrIndex);
+    r.u0 = r.total * cta / a.ctas;
+    r.u1 = r.total * (cta + 1) / a.ctas;
+    r.s = a.seqs.S;
+    r.in_seq = 0;
+    if (r.u0 >= r.u1) return r;
+    long long before = 0;
+    for (int base = 0; base < a.seqs.S; base += 32) {
+        long long c = 0;
+        if (base + lane < a.seqs.S) {
+            bool wrong;
+            const KvItem it = kv_item<R>(a, base + lane, wrong);
+            c = (long long)it.row_tiles * a.pool.Hkv * it.tiles;
+        }
+        long long sum = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        const uint32_t who = __ballot_sync(0xffffffffu, r.u0 < before + sum);
+        if (who) {
+            const int l = __ffs(who) - 1;
+            r.s = base + l;
+            r.in_seq = r.u0 - before - __shfl_sync(0xffffffffu, sum - c, l);
+            break;
+        }
+        before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    return r;
+}
+
+__device__ __forceinline__ uint32_t f16_low(uint32_t w)    // bytes 0, 1 of (code ^ 0x80) -> two fp16
+{
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&(w = prmt(w, 0x64646464u, 0x4140u))), __floats2half2_rn(1152.f, 1152.f));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t f16_high(uint32_t w)   // bytes 2, 3
+{
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&(w = prmt(w, 0x64646464u, 0x4342u))), __floats2half2_rn(1152.f, 1152.f));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int32_t row, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(bar) : "memory");
+}
+// Barrier of the four reading warps: whether any of them says `fail`.
+__device__ __forceinline__ bool bar_consumers(bool fail = false)
+{
+    uint32_t any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any) : "r"((uint32_t)fail) : "memory");
+    return any != 0;
+}
+
+// fp16 pair of q, times a power of two
+template <bool BF16>
+__device__ __forceinline__ float q_at(const void* q, int64_t i) { return BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(q)[i]) : __half2float(static_cast<const __half*>(q)[i]); }
+
+template <int D, int NT>
+struct KvShape {
+    static constexpr int R = 8 * NT;
+    static constexpr int kHalf = kKvTile * D;                 // bytes of a stage's K (or V)
+    static constexpr int kStage = 2 * kHalf;
+    static constexpr int kPitch = D + 4;                      // floats of a row of the warps' sums
+    static constexpr int kMerge = 4 * R * kPitch * 4 + 4 * R * 2 * 4;
+    static constexpr int kMaxStages = 16;
+    static constexpr int kPart = R * (D + 2);                 // floats of a part
+};
+
+template <int D, int NT, bool BF16>
+__global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_constant__ KvAttend a)
+{
+    using S = KvShape<D, NT>;
+    constexpr int R = S::R, KS = D / 16, MT = D / 16;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * S::kMaxStages];
+    __shared__ float2 steps[S::kMaxStages][4];
+    __shared__ uint32_t dead_word;
+    uint8_t* ring = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    float* sums = reinterpret_cast<float*>(ring + (size_t)a.stages * S::kStage);   // [warp][row][pitch]
+    float2* stats = reinterpret_cast<float2*>(sums + 4 * R * S::kPitch);           // [warp][row] m, l
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8u * S::kMaxStages;
+    volatile uint32_t* dead = &dead_word;
+    if (threadIdx.x < (unsigned)a.stages) { mbar_init(b_full + 8u * threadIdx.x, 1); mbar_init(b_empty + 8u * threadIdx.x, 4); }
+    if (threadIdx.x == 0) dead_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncthreads();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const KvPool& p = a.pool;
+    const KvRange range = kv_range<R>(a, blockIdx.x, lane);
+    long long left = range.u1 - range.u0;
+    bool ok = true, wrong;
+    int stage = 0;
+    uint32_t par = 0;
+    int s = range.s;
+    KvItem it;
+    int item = 0, tile = 0;   // item of the sequence (row tile * Hkv + head), unit of the item
+    if (left > 0) {
+        it = kv_item<R>(a, s, wrong);
+        item = (int)(range.in_seq / it.tiles);
+        tile = (int)(range.in_seq - (long long)item * it.tiles);
+    }
+    auto next_seq = [&]() {   // (the units of this CTA end before the sequences do)
+        if (item < it.row_tiles * p.Hkv) return;
+        item = 0;
+        do {
+            if (++s >= a.seqs.S) { left = 0; return; }
+            it = kv_item<R>(a, s, wrong);
+        } while (it.rows == 0);
+    };
+    if (warp == 4) {
+        // ---- copies ----
+        const int box = min(p.T, kKvTile), nb = kKvTile / box;   // tokens of a copy, copies of a unit
+        long long issued = 0;
+        while (left > 0 && ok) {
+            const int n = (int)min((long long)(it.tiles - tile), left);
+            const int h = item % p.Hkv;
+            const int32_t* row = a.seqs.table + (int64_t)s * a.seqs.table_stride;
+            // 32 copies' block numbers and steps at a time, a lane each
+            for (int i0 = 0; i0 < n && ok; i0 += 32 / nb) {
+                const int t = (it.t_lo + tile + i0) * kKvTile + lane * box;   // the lane's first token
+                int32_t blk = -1;
+                float sk = -1.f, sv = 0.f;
+                if (lane < nb * (n - i0) && t < it.seq.len && t + box > it.lo) {   // (blocks in front of every window may be gone)
+                    blk = __ldcg(row + t / p.T);
+                    if (blk < 0 || blk >= p.blocks) {
+                        atomicExch(p.err, kErrIndex);
+                        blk = -1;
+                    } else {
+                        sk = __ldcg(p.k_step + (int64_t)blk * p.Hkv + h);
+                        sv = __ldcg(p.v_step + (int64_t)blk * p.Hkv + h);
+                    }
+                }
+                const int m = min(32 / nb, n - i0);
+                for (int i = 0; i < m; ++i) {
+                    ok = tc_wait_warp(b_empty + 8u * stage, par ^ 1u, kMxWait, dead);
+                    if (!ok) break;
+                    // the steps of the unit's four 16-token groups
+                    const int from = i * nb + (lane & 3) * 16 / box;
+                    const float gk = __shfl_sync(0xffffffffu, sk, from), gv = __shfl_sync(0xffffffffu, sv, from);
+                    if (lane < 4) steps[stage][lane] = make_float2(gk, gv);
+                    const uint32_t valid = __popc(__ballot_sync(0xffffffffu, blk >= 0 && lane / nb == i));
+                    const uint32_t bar = b_full + 8u * stage;
+                    __syncwarp();
+                    if (lane == 0) mbar_expect_tx(bar, valid * 2u * (uint32_t)(box * D));
+                    __syncwarp();
+                    if (blk >= 0 && lane / nb == i) {
+                        const int32_t y = (blk * p.Hkv + h) * p.T + t % p.T;
+                        const uint32_t dst = smem_u32(ring + (size_t)stage * S::kStage) + (uint32_t)((lane - i * nb) * box * D);
+                        tma_rows(dst, &a.k_map, y, bar);
+                        tma_rows(dst + S::kHalf, &a.v_map, y, bar);
+                    }
+                    ++issued;
+                    if (++stage == a.stages) { stage = 0; par ^= 1u; }
+                }
+            }
+            left -= n;
+            tile = 0;
+            ++item;
+            if (left > 0) next_seq();
+        }
+        // (nothing may be in flight when the CTA ends)
+        if (!ok)
+            for (long long i = max(0ll, issued - a.stages); i < issued; ++i) mbar_wait_bounded(b_full + 8u * (uint32_t)(i % a.stages), (uint32_t)(i / a.stages) & 1u, kMxWait);
+        __syncwarp();
+    } else {
+        const int g = lane >> 2, t = lane & 3;
+        // Shared-memory offsets of the lane's fragments in a stage (see the layout of TMA's swizzles: 128 bytes for D = 128, 64 for 64)
+        const int kr = 16 * warp + g;
+        while (left > 0 && ok) {
+            const int n = (int)min((long long)(it.tiles - tile), left);
+            const int h = item % p.Hkv, row0 = item / p.Hkv * R;
+            // Q fragments: rows g of every 8, the lane's D/4 columns; fp16 times a power of two that brings bf16 into range
+            uint32_t qf[NT][KS][2];
+            float f[NT][2];
+            int lo[NT][2], hi[NT][2];
+            const int pos0 = it.seq.len - it.seq.n;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int r = row0 + 8 * nt + g;
+                float v[D / 4];
+                const bool in = r < it.rows;
+                const int tok = in ? r / a.G : 0, qh = h * a.G + (in ? r - tok * a.G : 0);
+                const int64_t at = (it.seq.first + tok) * a.q_token + (int64_t)qh * a.q_head + t * (D / 4);
+                if (in && a.q_vec) {
+                    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + at);
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        const uint4 w = __ldcg(src + i);
+                        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (BF16) {
+                                v[8 * i + 2 * j] = __uint_as_float(ww[j] << 16);
+                                v[8 * i + 2 * j + 1] = __uint_as_float(ww[j] & 0xFFFF0000u);
+                            } else {
+                                const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&ww[j]));
+                                v[8 * i + 2 * j] = u.x;
+                                v[8 * i + 2 * j + 1] = u.y;
+                            }
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < D / 4; ++i) v[i] = in ? q_at<BF16>(a.q, at + i) : 0.f;
+                }
+                float mul = 1.f, back = 1.f;
+                if (BF16) {
+                    uint32_t big = 0;
+#pragma unroll
+                    for (int i = 0; i < D / 4; ++i) big = max(big, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+                    big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+                    big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+                    // largest magnitude in [2^14, 2^15); exponents so that both factors are normal numbers
+                    const int e = max(-112, min(114, (int)(big >> 23) - 127 - 14));
+                    mul = __uint_as_float((uint32_t)(127 - e) << 23);
+                    back = __uint_as_float((uint32_t)(127 + e) << 23);
+                }
+#pragma unroll
+                for (int j = 0; j < KS; ++j) {
+                    const __half2 x = __floats2half2_rn(v[4 * j] * mul, v[4 * j + 1] * mul), y = __floats2half2_rn(v[4 * j + 2] * mul, v[4 * j + 3] * mul);
+                    qf[nt][j][0] = *reinterpret_cast<const uint32_t*>(&x);
+                    qf[nt][j][1] = *reinterpret_cast<const uint32_t*>(&y);
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    f[nt][c] = __shfl_sync(0xffffffffu, back, 4 * (2 * t + c)) * a.scale2;
+                    const int rr = row0 + 8 * nt + 2 * t + c;
+                    const int pos = pos0 + rr / a.G;
+                    const bool real = rr < it.rows;   // (rows past the last are zero queries that see everything; never stored)
+                    hi[nt][c] = real ? (a.causal ? pos + 1 : it.seq.len) : 0x7FFFFFFF;
+                    lo[nt][c] = real && a.window > 0 ? pos - a.window + 1 : -0x7FFFFFFF;
+                }
+            }
+            float m[NT][2], l[NT][2], o[MT][NT][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) { m[nt][c] = -INFINITY; l[nt][c] = 0.f; }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) o[i][nt][c] = 0.f;
+            float ref = 0.f;   // V's largest step so far
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) {
+                ok = tc_wait_warp(b_full + 8u * stage, par, kMxWait, dead);
+                if (!ok) break;
+                const float2 st = steps[stage][warp];
+                const int tok0 = (it.t_lo + tile + i) * kKvTile + 16 * warp;
+                bool see = false;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) see |= row0 + 8 * nt + 2 * t + c < it.rows && lo[nt][c] < tok0 + 16 && hi[nt][c] > tok0;
+                if (st.x < 0.f) see = false;   // (a block that was not fetched)
+                if (__any_sync(0xffffffffu, see)) {
+                    const uint32_t kb = smem_u32(ring + (size_t)stage * S::kStage), vb = kb + S::kHalf;
+                    float sc[NT][4];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) sc[nt][c] = 0.f;
+                    // scores: 16 tokens x 8 NT rows
+#pragma unroll
+                    for (int c = 0; c < D / 64; ++c) {
+                        const int chunk = D == 128 ? ((2 * t + c) ^ (kr & 7)) : (t ^ ((kr >> 1) & 3));
+                        const uint4 x = lds128(kb + (uint32_t)(kr * D + 16 * chunk)), y = lds128(kb + (uint32_t)((kr + 8) * D + 16 * chunk));
+                        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t xw = xs[j] ^ 0x80808080u, yw = ys[j] ^ 0x80808080u;
+                            const uint32_t a0 = f16_low(xw), a1 = f16_low(yw), a2 = f16_high(xw), a3 = f16_high(yw);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma_f16(sc[nt], a0, a1, a2, a3, qf[nt][4 * c + j][0], qf[nt][4 * c + j][1]);
+                        }
+                    }
+                    bool edge = false;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) edge |= lo[nt][c] > tok0 || hi[nt][c] < tok0 + 16;
+                    edge = __any_sync(0xffffffffu, edge);
+                    bool behind = false;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            float v = sc[nt][c] * (f[nt][c & 1] * st.x);
+                            if (edge) {
+                                const int tk = tok0 + g + 8 * (c >> 1);
+                                if (tk < lo[nt][c & 1] || tk >= hi[nt][c & 1]) v = -INFINITY;
+                            }
+                            sc[nt][c] = v;
+                            behind |= v > m[nt][c & 1] + 8.f;
+                        }
+                    if (__any_sync(0xffffffffu, behind)) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                float x = fmaxf(sc[nt][c], sc[nt][c + 2]);
+                                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                                x = fmaxf(x, m[nt][c]);
+                                const float alpha = x == -INFINITY ? 1.f : exp2_fast(m[nt][c] - x);
+                                m[nt][c] = x;
+                                l[nt][c] *= alpha;
+#pragma unroll
+                                for (int k = 0; k < MT; ++k) { o[k][nt][c] *= alpha; o[k][nt][c + 2] *= alpha; }
+                            }
+                    }
+                    if (st.y > ref) {
+                        const float b = ref / st.y;
+                        ref = st.y;
+#pragma unroll
+                        for (int k = 0; k < MT; ++k)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) o[k][nt][c] *= b;
+                    }
+                    const float rel = st.y == ref ? 1.f : __fdiv_rn(st.y, ref);   // (NaN: NaN)
+                    uint32_t pf[NT][2];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float e[4];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            e[c] = exp2_fast(sc[nt][c] - (m[nt][c & 1] == -INFINITY ? 0.f : m[nt][c & 1] - 7.f));
+                            l[nt][c & 1] += e[c];
+                        }
+                        const __half2 x = __floats2half2_rn(e[0] * rel, e[1] * rel), y = __floats2half2_rn(e[2] * rel, e[3] * rel);
+                        pf[nt][0] = transpose8(*reinterpret_cast<const uint32_t*>(&x));
+                        pf[nt][1] = transpose8(*reinterpret_cast<const uint32_t*>(&y));
+                    }
+                    // sums: 16 of D x 8 NT rows at a time; a lane holds the same D columns of its four tokens
+                    const int v0 = 16 * warp + 2 * t;
+                    uint32_t w[4][D / 32];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int r = v0 + (q & 1) + 8 * (q >> 1);
+                        if (D == 128) {
+                            const uint4 x = lds128(vb + (uint32_t)(r * D + 16 * (g ^ (r & 7))));
+                            w[q][0] = x.x; w[q][1] = x.y; w[q][D / 32 - 2] = x.z; w[q][D / 32 - 1] = x.w;
+                        } else {
+                            const uint2 x = lds64(vb + (uint32_t)(r * D + 16 * ((g >> 1) ^ ((r >> 1) & 3)) + 8 * (g & 1)));
+                            w[q][0] = x.x; w[q][1] = x.y;
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < D / 32; ++k) {
+                        const uint32_t x0 = prmt(w[0][k], w[1][k], 0x5140u) ^ 0x80808080u, x1 = prmt(w[0][k], w[1][k], 0x7362u) ^ 0x80808080u;
+                        const uint32_t y0 = prmt(w[2][k], w[3][k], 0x5140u) ^ 0x80808080u, y1 = prmt(w[2][k], w[3][k], 0x7362u) ^ 0x80808080u;
+                        const uint32_t a0 = f16_low(x0), a1 = f16_high(x0), a2 = f16_low(y0), a3 = f16_high(y0);
+                        const uint32_t b0 = f16_low(x1), b1 = f16_high(x1), b2 = f16_low(y1), b3 = f16_high(y1);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma_f16(o[2 * k][nt], a0, a1, a2, a3, pf[nt][0], pf[nt][1]);
+                            mma_f16(o[2 * k + 1][nt], b0, b1, b2, b3, pf[nt][0], pf[nt][1]);
+                        }
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_empty + 8u * stage);
+                if (++stage == a.stages) { stage = 0; par ^= 1u; }
+            }
+            // the four warps' sums together
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float x = l[nt][c];
+                    x += __shfl_xor_sync(0xffffffffu, x, 4);
+                    x += __shfl_xor_sync(0xffffffffu, x, 8);
+                    x += __shfl_xor_sync(0xffffffffu, x, 16);
+                    if (g == 0) stats[warp * R + 8 * nt + 2 * t + c] = make_float2(m[nt][c], x);
+                }
+            // (place (2 j + e) * 8 + g of a row holds d = (D / 8) g + 2 j + e: a warp's 32 stores meet 32 banks)
+#pragma unroll
+            for (int k = 0; k < MT; ++k)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        sums[(warp * R + 8 * nt + 2 * t + (c & 1)) * S::kPitch + (2 * k + (c >> 1)) * 8 + g] = o[k][nt][c] * ref;
+            if (bar_consumers(!ok)) {   // (a warp gave up: all four do, at the same place)
+                ok = false;
+                break;
+            }
+            const bool whole = n == it.tiles;
+            float* part = a.part + ((int64_t)blockIdx.x * 2 + (tile == 0 ? 1 : 0)) * S::kPart;   // 1: the item begins here
+            const int rows = min(R, it.rows - row0);
+            for (int i = threadIdx.x; i < rows * D; i += 128) {
+                const int r = i / D, d = i - r * D;
+                float big = -INFINITY, sum = 0.f, acc = 0.f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) big = fmaxf(big, stats[w * R + r].x);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float2 x = stats[w * R + r];
+                    const float e = x.x == -INFINITY && x.y == 0.f ? 0.f : exp2_fast(x.x - (big == -INFINITY ? 0.f : big));
+                    sum += e * x.y;
+                    acc += e == 0.f ? 0.f : e * sums[(w * R + r) * S::kPitch + (d % (D / 8)) * 8 + d / (D / 8)];
+                }
+                if (whole) {
+                    const int tok = (row0 + r) / a.G, qh = h * a.G + (row0 + r) - tok * a.G;
+                    const float y = sum == 0.f ? 0.f : acc / sum;
+                    const int64_t at = (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + d;
+                    if (BF16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(y);
+                    else static_cast<__half*>(a.out)[at] = __float2half_rn(y);
+                    if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = sum == 0.f ? -INFINITY : (big + log2f(sum) - 7.f) * 0.69314718f;
+                } else {
+                    part[r * D + d] = acc;
+                    if (d == 0) {
+                        part[R * D + 2 * r] = big;
+                        part[R * D + 2 * r + 1] = sum;
+                    }
+                }
+            }
+            bar_consumers();
+            left -= n;
+            tile = 0;
+            ++item;
+            if (left > 0) next_seq();
+        }
+    }
+    if (!ok && lane == 0) {
+        *dead = 1;
+        atomicExch(p.err, kErrTimeout);
+    }
+    __syncthreads();
+}
+
+// Joins the parts of the item that begins in CTA blockIdx.x of the kernel before and ends in a later one; row blockIdx.y of its tile.
+template <int D, int NT, bool BF16>
+__global__ void __launch_bounds__(D) us_kv_join_kernel(const __grid_constant__ KvAttend a)
+{
+    using S = KvShape<D, NT>;
+    constexpr int R = S::R;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31, d = threadIdx.x, r = blockIdx.y;
+    const KvRange range = kv_range<R>(a, blockIdx.x, lane);
+    if (range.u0 >= range.u1) return;
+    // the item that the CTA's last unit belongs to
+    int s = range.s;
+    bool wrong;
+    KvItem it = kv_item<R>(a, s, wrong);
+    long long start = range.u0 - range.in_seq;   // first unit of the sequence
+    long long units = (long long)it.row_tiles * a.pool.Hkv * it.tiles;
+    while (start + units <= range.u1 - 1) {
+        start += units;
+        if (++s >= a.seqs.S) return;
+        it = kv_item<R>(a, s, wrong);
+        units = (long long)it.row_tiles * a.pool.Hkv * it.tiles;
+    }
+    const int item = (int)((range.u1 - 1 - start) / it.tiles);
+    const long long first = start + (long long)item * it.tiles, end = first + it.tiles;
+    if (first < range.u0 || end <= range.u1) return;   // begins in an earlier CTA, or is whole
+    const int h = item % a.pool.Hkv, row0 = item / a.pool.Hkv * R;
+    if (row0 + r >= it.rows) return;
+    int last = blockIdx.x;   // the CTA of the item's last unit
+    while (range.total * (last + 1) / a.ctas < end) ++last;
+    float big = -INFINITY, sum = 0.f, acc = 0.f;
+    for (int c0 = blockIdx.x; c0 <= last; c0 += 8) {
+        float x[8], m[8], l[8], top = big;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            m[i] = -INFINITY; l[i] = 0.f; x[i] = 0.f;
+            const int c = c0 + i;
+            if (c <= last && range.total * c / a.ctas < range.total * (c + 1) / a.ctas) {
+                const float* part = a.part + ((int64_t)c * 2 + (c == (int)blockIdx.x ? 1 : 0)) * S::kPart;
+                x[i] = __ldcg(part + r * D + d);
+                m[i] = __ldcg(part + R * D + 2 * r);
+                l[i] = __ldcg(part + R * D + 2 * r + 1);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, m[i]);
+        const float base = top == -INFINITY ? 0.f : top;
+        const float keep = big == -INFINITY ? 1.f : exp2_fast(big - base);   // (nothing is there yet, or NaN that has to stay)
+        sum *= keep;
+        acc *= keep;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float e = m[i] == -INFINITY && l[i] == 0.f ? 0.f : exp2_fast(m[i] - base);
+            sum += e * l[i];
+            acc += e == 0.f ? 0.f : e * x[i];
+        }
+        big = top;
+    }
+    const int tok = (row0 + r) / a.G, qh = h * a.G + (row0 + r) - tok * a.G;
+    const float y = sum == 0.f ? 0.f : acc / sum;
+    const int64_t at = (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + d;
+    if (BF16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(y);
+    else static_cast<__half*>(a.out)[at] = __float2half_rn(y);
+    if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = sum == 0.f ? -INFINITY : (big + log2f(sum) - 7.f) * 0.69314718f;
+}
+
+}  // namespace us

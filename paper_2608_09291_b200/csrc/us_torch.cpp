@@ -393,6 +393,166 @@ PyObject* mx4_linear(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the 8-bit cache ----
+
+bool is_ints(const at::Tensor& t, const at::Tensor& on) { return t.scalar_type() == at::kInt && t.device() == on.device(); }
+
+// A batch of sequences from (block_table, lengths, cu_tokens); N: the call's rows, or -1 where it has none.
+bool take_seqs(PyObject* table, PyObject* lengths, PyObject* cu, int64_t N, const at::Tensor& on, us_kv_seqs* q)
+{
+    const at::Tensor *t = tensor(table, "block_table"), *l = t ? tensor(lengths, "lengths") : nullptr;
+    if (!l) return false;
+    if (t->dim() != 2 || !is_ints(*t, on) || (t->stride(1) != 1 && t->size(1) > 1) || (t->size(0) > 1 && t->stride(0) < t->size(1)) || t->size(0) >= (1ll << 31) ||
+        t->size(1) >= (1ll << 31)) {
+        PyErr_SetString(PyExc_ValueError, "block_table must be an int32 (sequences, width) tensor with unit column stride on the cache's device");
+        return false;
+    }
+    if (l->dim() != 1 || !is_ints(*l, on) || l->size(0) != t->size(0) || !l->is_contiguous()) {
+        PyErr_SetString(PyExc_ValueError, "lengths must be a contiguous int32 tensor with an entry for each row of block_table, on the cache's device");
+        return false;
+    }
+    *q = us_kv_seqs{};
+    q->block_table = static_cast<const int32_t*>(t->data_ptr());
+    q->table_stride = row_stride(*t);
+    q->lengths = static_cast<const int32_t*>(l->data_ptr());
+    q->n_seqs = (int32_t)t->size(0);
+    q->table_width = (int32_t)t->size(1);
+    if (cu == Py_None) {
+        if (N >= 0 && N != t->size(0)) {
+            PyErr_SetString(PyExc_ValueError, "without cu_tokens there is one row for each sequence");
+            return false;
+        }
+        return true;
+    }
+    const at::Tensor* c = tensor(cu, "cu_tokens");
+    if (!c) return false;
+    if (c->dim() != 1 || !is_ints(*c, on) || c->size(0) != t->size(0) + 1 || !c->is_contiguous()) {
+        PyErr_SetString(PyExc_ValueError, "cu_tokens must be a contiguous int32 tensor with one entry more than block_table has rows, on the cache's device");
+        return false;
+    }
+    q->cu_tokens = static_cast<const int32_t*>(c->data_ptr());
+    return true;
+}
+// (N, heads, D) rows of a float type, any token and head strides that do not overlap.
+bool is_heads(const at::Tensor& t, int64_t D, const at::Tensor& on)
+{
+    return t.dim() == 3 && type_of(t.scalar_type()) >= 0 && t.size(2) == D && t.stride(2) == 1 && t.device() == on.device() &&
+           (t.size(0) <= 1 || t.stride(0) >= D) && (t.size(1) <= 1 || t.stride(1) >= D);
+}
+int64_t token_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : 0; }
+int64_t head_stride(const at::Tensor& t) { return t.size(1) > 1 ? t.stride(1) : 0; }
+
+// kv_append(handle, pool, k, v, table, lengths, cu, stream)
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "kv_append takes 8 arguments");
+    HANDLE_TH_ERRORS
+    void* h = a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor *pool = tensor(a[1], "pool"), *k = pool ? tensor(a[2], "k") : nullptr, *v = k ? tensor(a[3], "v") : nullptr;
+    if (!v) return nullptr;
+    if (!h) return fail(US_ERR_INVALID_ARG, "us_kv_append");
+    Place at_;
+    if (!at_.enter(a[7], *pool)) return nullptr;
+    if (!is_heads(*k, pool->size(3), *pool) || !is_heads(*v, pool->size(3), *pool) || k->size(1) != pool->size(1) || v->size(1) != pool->size(1) ||
+        k->size(0) != v->size(0) || k->scalar_type() != v->scalar_type())
+        return bad("k and v must be (N, n_kv_heads, head_dim) tensors of one type (float16, bfloat16 or float32) with unit last stride on the cache's device");
+    us_kv_seqs q;
+    if (!take_seqs(a[4], a[5], a[6], k->size(0), *pool, &q)) return nullptr;
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_kv_append(static_cast<us_kv*>(h), &q, k->size(0), k->data_ptr(), v->data_ptr(), type_of(k->scalar_type()), token_stride(*k), head_stride(*k),
+                     token_stride(*v), head_stride(*v), at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_kv_append");
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_read(handle, pool, table, lengths, tokens, dtype, stream) -> (K, V)
+PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "kv_read takes 7 arguments");
+    HANDLE_TH_ERRORS
+    void* h = a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]);
+    const int64_t tokens = PyLong_AsLongLong(a[4]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor* pool = tensor(a[1], "pool");
+    if (!pool) return nullptr;
+    if (!h || tokens < 0) return fail(US_ERR_INVALID_ARG, "us_kv_read");
+    at::ScalarType type;
+    if (!dtype_of(a[5], at::kFloat, &type)) return nullptr;
+    Place at_;
+    if (!at_.enter(a[6], *pool)) return nullptr;
+    us_kv_seqs q;
+    if (!take_seqs(a[2], a[3], Py_None, -1, *pool, &q)) return nullptr;
+    if (tokens > (int64_t)q.table_width * pool->size(2)) return fail(US_ERR_INVALID_ARG, "us_kv_read");
+    const int64_t shape[4] = {q.n_seqs, tokens, pool->size(1), pool->size(3)};
+    at::Tensor K = at::detail::empty_cuda(shape, type, pool->device(), std::nullopt), V = at::detail::empty_cuda(shape, type, pool->device(), std::nullopt);
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_kv_read(static_cast<us_kv*>(h), &q, tokens, K.data_ptr(), V.data_ptr(), type_of(type), at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_kv_read");
+    PyObject *k = THPVariable_Wrap(std::move(K)), *v = THPVariable_Wrap(std::move(V));
+    return Py_BuildValue("NN", k, v);
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_attention(handle, pool, q, table, lengths, cu, scale, causal, window, out, lse, stream) -> out
+PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 12) return PyErr_Format(PyExc_TypeError, "kv_attention takes 12 arguments");
+    HANDLE_TH_ERRORS
+    void* h = a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]);
+    const double scale = PyFloat_AsDouble(a[6]);
+    const int causal = PyObject_IsTrue(a[7]);
+    const int64_t window = PyLong_AsLongLong(a[8]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor *pool = tensor(a[1], "pool"), *Q = pool ? tensor(a[2], "q") : nullptr;
+    if (!Q) return nullptr;
+    if (!h) return fail(US_ERR_INVALID_ARG, "us_kv_attention");
+    Place at_;
+    if (!at_.enter(a[11], *pool)) return nullptr;
+    if (!is_heads(*Q, pool->size(3), *pool) || Q->scalar_type() == at::kFloat || Q->size(1) < 1 || Q->size(1) % pool->size(1) || Q->size(1) >= (1ll << 31))
+        return bad("q must be a float16 or bfloat16 (N, n_heads, head_dim) tensor, n_heads a multiple of n_kv_heads, with unit last stride on the cache's device");
+    if (window < 0 || window > 0x7FFFFFFF) return bad("window must be 0 (none) or a number of tokens");
+    const int64_t N = Q->size(0), H = Q->size(1), D = Q->size(2);
+    us_kv_seqs q;
+    if (!take_seqs(a[3], a[4], a[5], N, *pool, &q)) return nullptr;
+    at::Tensor fresh, scratch;
+    const at::Tensor* out = &fresh;
+    if (a[9] == Py_None) {
+        const int64_t shape[3] = {N, H, D};
+        fresh = at::detail::empty_cuda(shape, Q->scalar_type(), pool->device(), std::nullopt);
+    } else {
+        out = tensor(a[9], "out");
+        if (!out) return nullptr;
+        if (!is_heads(*out, D, *pool) || out->scalar_type() != Q->scalar_type() || out->size(0) != N || out->size(1) != H)
+            return bad("out must be a tensor of q's shape and type with unit last stride on the cache's device");
+    }
+    void* lse = nullptr;
+    if (a[10] != Py_None) {
+        const at::Tensor* l = tensor(a[10], "lse");
+        if (!l) return nullptr;
+        if (l->dim() != 2 || l->scalar_type() != at::kFloat || l->size(0) != N || l->size(1) != H || !l->is_contiguous() || l->device() != pool->device())
+            return bad("lse must be a contiguous float32 (N, n_heads) tensor on the cache's device");
+        lse = l->data_ptr();
+    }
+    const int64_t bytes = us_kv_attention_scratch(static_cast<us_kv*>(h), N, q.n_seqs, (int32_t)H);
+    if (bytes < 0) return fail(US_ERR_INVALID_ARG, "us_kv_attention");
+    if (bytes > 0) scratch = at::detail::empty_cuda({bytes}, at::kByte, pool->device(), std::nullopt);
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_kv_attention(static_cast<us_kv*>(h), &q, N, Q->data_ptr(), type_of(Q->scalar_type()), (int32_t)H, token_stride(*Q), head_stride(*Q), (float)scale,
+                        causal, (int32_t)window, out->data_ptr(), token_stride(*out), head_stride(*out), static_cast<float*>(lse),
+                        bytes > 0 ? scratch.data_ptr() : nullptr, bytes, at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_kv_attention");
+    return give(a[9], std::move(fresh));
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject* set_error(PyObject*, PyObject* cls)
 {
     Py_XDECREF(g_error);
@@ -413,6 +573,9 @@ PyMethodDef methods[] = {
     {"mx4_pack", fast(mx4_pack), METH_FASTCALL, nullptr},
     {"mx4_unpack", fast(mx4_unpack), METH_FASTCALL, nullptr},
     {"mx4_linear", fast(mx4_linear), METH_FASTCALL, nullptr},
+    {"kv_append", fast(kv_append), METH_FASTCALL, nullptr},
+    {"kv_read", fast(kv_read), METH_FASTCALL, nullptr},
+    {"kv_attention", fast(kv_attention), METH_FASTCALL, nullptr},
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
