@@ -1,7 +1,8 @@
 // The 8-bit cache's entry points: checks, launch plans.
-#include "us_kv.cuh"
+#include "us_kv_prompt.cuh"
 #include "us_ops.h"
 
+#include <cmath>
 #include <mutex>
 #include <new>
 
@@ -101,8 +102,24 @@ bool rows_vec(const void* x, int32_t type, int64_t token, int64_t head)
 struct AttendPlan {
     const void *kernel, *join;
     int rows, stages, smem, ctas;
+    int splits;        // (prompts) of the cache's length
+    int64_t tiles;     // (prompts) row tiles, at most; 0: the kernel for few rows
     int64_t scratch;
 };
+template <int D, bool BF16>
+AttendPlan prompt_shape(int64_t N, int64_t S, int64_t G, int64_t Hkv, int sms)
+{
+    AttendPlan p = {};
+    p.kernel = (const void*)us_kv_prompt_kernel<D, BF16>;
+    p.join = (const void*)us_kv_prompt_join_kernel<D, BF16>;
+    p.smem = PrShape<D>::kSmem;
+    p.tiles = N * G / kPrRows + S;
+    // a tile's walk over the cache is split where the tiles would leave SMs idle
+    const int64_t likely = std::max(S, (N * G + kPrRows - 1) / kPrRows) * Hkv;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(16, sms / likely));
+    p.scratch = p.splits > 1 ? p.tiles * Hkv * p.splits * PrShape<D>::kPart * 4 : 0;
+    return p;
+}
 template <int D, int NT, bool BF16>
 AttendPlan attend_shape(int sms)
 {
@@ -119,8 +136,12 @@ AttendPlan attend_shape(int sms)
 }
 template <int D, int NT>
 AttendPlan attend_shape(bool bf16, int sms) { return bf16 ? attend_shape<D, NT, true>(sms) : attend_shape<D, NT, false>(sms); }
-AttendPlan attend_plan(int D, bool bf16, int64_t N, int64_t S, int64_t G, int sms)
+AttendPlan attend_plan(int D, bool bf16, int64_t N, int64_t S, int64_t G, int64_t Hkv, int sms)
 {
+    if (N * G > 32 * S) {
+        if (D == 128) return bf16 ? prompt_shape<128, true>(N, S, G, Hkv, sms) : prompt_shape<128, false>(N, S, G, Hkv, sms);
+        return bf16 ? prompt_shape<64, true>(N, S, G, Hkv, sms) : prompt_shape<64, false>(N, S, G, Hkv, sms);
+    }
     // rows a cache head has on average: 8 a tile are enough for them, or 16
     const bool few = N * G <= 8 * S;
     if (D == 128) return few ? attend_shape<128, 1>(bf16, sms) : attend_shape<128, 2>(bf16, sms);
@@ -211,7 +232,7 @@ int64_t us_kv_attention_scratch(const us_kv* h, int64_t N, int32_t n_seqs, int32
 {
     if (!h || N < 0 || n_seqs < 0 || n_heads < 1 || n_heads % h->pool.Hkv) return -1;
     if (N == 0 || n_seqs == 0) return 0;
-    return attend_plan(h->pool.D, false, N, n_seqs, n_heads / h->pool.Hkv, ops_sms()).scratch;
+    return attend_plan(h->pool.D, false, N, n_seqs, n_heads / h->pool.Hkv, h->pool.Hkv, ops_sms()).scratch;
 }
 
 us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* Q, int32_t type, int32_t n_heads, int64_t q_token_stride,
@@ -225,8 +246,35 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
         !aligned(lse, 4)) return US_ERR_INVALID_ARG;
     const int64_t G = n_heads / h->pool.Hkv;
     if (N * G >= (1ll << 31) - (1 << 16)) return US_ERR_UNSUPPORTED;
-    const AttendPlan pl = attend_plan(h->pool.D, type == US_BF16, N, q->n_seqs, G, ops_sms());
-    if (!scratch || !aligned(scratch, 16) || scratch_bytes < pl.scratch) return US_ERR_SCRATCH_TOO_SMALL;
+    const AttendPlan pl = attend_plan(h->pool.D, type == US_BF16, N, q->n_seqs, G, h->pool.Hkv, ops_sms());
+    if (pl.scratch > 0 && (!scratch || !aligned(scratch, 16) || scratch_bytes < pl.scratch)) return US_ERR_SCRATCH_TOO_SMALL;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (pl.tiles > 0) {
+        const int64_t blocks = pl.tiles * h->pool.Hkv * std::max(pl.splits, kPrRows / 8);
+        if (blocks >= (1ll << 31)) return US_ERR_UNSUPPORTED;
+        KvPrompt a = {};
+        a.pool = h->pool;
+        a.seqs = seqs(q, N);
+        a.q = Q; a.q_token = q_token_stride; a.q_head = q_head_stride;
+        a.out = out; a.o_token = o_token_stride; a.o_head = o_head_stride;
+        a.lse = lse;
+        a.part = static_cast<float*>(scratch);
+        a.scale2 = (float)(std::fabs((double)scale) * 1.4426950408889634);
+        a.negative = scale < 0.f;
+        a.Hq = n_heads; a.G = (int32_t)G;
+        a.causal = causal != 0; a.window = window;
+        a.q_vec = rows_vec(Q, type, q_token_stride, q_head_stride);
+        a.o_vec = rows_vec(out, type, o_token_stride, o_head_stride);
+        a.splits = pl.splits;
+        us_status s = error_word(&a.pool.err);
+        if (s != US_OK) return s;
+        void* args[] = {&a};
+        cudaError_t e = ops_kernel_allow(pl.kernel);
+        const int threads = PrShape<128>::kThreads;
+        if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.splits)), threads, pl.smem, st, args);
+        if (e == cudaSuccess && pl.splits > 1) e = ops_launch(pl.join, dim3((unsigned)(pl.tiles * h->pool.Hkv * (kPrRows / 8))), 256, 0, st, args);
+        return cuda(e);
+    }
     if (!maps(h)) return US_ERR_CUDA;
     KvAttend a = {};
     a.k_map = h->k_map; a.v_map = h->v_map;
@@ -245,7 +293,6 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
     us_status s = error_word(&a.pool.err);
     if (s != US_OK) return s;
     cudaError_t e = ops_kernel_allow(pl.kernel);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
     void* args[] = {&a};
     if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)pl.ctas), 160, pl.smem, st, args);
     if (e == cudaSuccess) e = ops_launch(pl.join, dim3((unsigned)pl.ctas, (unsigned)pl.rows), h->pool.D, 0, st, args);

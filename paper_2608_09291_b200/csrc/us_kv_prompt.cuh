@@ -1,0 +1,657 @@
+// Attention over the 8-bit cache for many query rows a cache head (prompts): the 5th-generation tensor cores.
+//
+// A CTA takes up to 256 query rows (tokens x the query heads that share a cache head) of one (sequence, head) in two tiles of 128, and walks
+// its 128-token units of the cache:
+//   convert   four warps load the codes of a unit, a unit ahead, and write them as fp16 (exact) where the MMA reads: K with D contiguous
+//             (K-major), V as it lies (MN-major), both swizzled over 128 bytes.
+//   MMA       one warp: S = Q K^T into tensor memory, O += P V with P from tensor memory, for the two tiles in turn: while one tile's
+//             scores are being turned into P the other tile's products run.
+//   softmax   four warps a tile, a thread a row: no exchange between lanes. Steps: one number for 16 tokens, K's a factor of the
+//             scores, V's in the exponent of p (relative to the largest so far), so that a unit's P V needs no scaling. P takes the place of S.
+// m follows the true maximum only where it is 2^8 behind; p carries 2^7, see us_kv.cuh. The scores' conversions, the
+// 16384 exponentials (16 a cycle) and the two products (1024 cycles) of a tile and unit are near balance: each about 1000 cycles.
+#pragma once
+#include "us_kv.cuh"
+
+namespace us {
+
+constexpr int kPrRows = 256, kPrTile = 128;
+
+struct KvPrompt {
+    KvPool pool;
+    KvSeqs seqs;
+    const void* q;
+    int64_t q_token, q_head;
+    void* out;
+    int64_t o_token, o_head;
+    float* lse;
+    float* part;             // [row tile][head][split]: 256 x D sums, then 256 x {m, l}
+    float scale2;            // |scale| log2(e); the sign goes to the queries
+    int32_t negative;
+    int32_t Hq, G;
+    int32_t causal, window;
+    int32_t q_vec, o_vec;
+    int32_t splits;
+};
+
+template <int D>
+struct PrShape {
+    static constexpr int kQ = 128 * D * 2, kKV = kPrTile * D * 2;   // bytes
+    static constexpr int kSmem = 1024 + 2 * kQ + 4 * kKV;
+    static constexpr int64_t kPart = kPrRows * (D + 2);
+    static constexpr int kThreads = 13 * 32;
+};
+
+__device__ __forceinline__ void tc_mma_f16(uint32_t elected, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %5, 0;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(elected) : "memory");
+}
+__device__ __forceinline__ void tc_mma_f16_ts(uint32_t elected, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %5, 0;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(elected) : "memory");
+}
+#define US_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define US_I8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+// 32 columns of the thread's lane, fetched without waiting
+__device__ __forceinline__ void tc_ld32(uint32_t addr, uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
+                 "%27,%28,%29,%30,%31}, [%32];" : US_R8(r, 0), US_R8(r, 8), US_R8(r, 16), US_R8(r, 24) : "r"(addr));
+}
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
+                 "%27,%28,%29,%30,%31};" ::US_I8(r, 0), US_I8(r, 8), US_I8(r, 16), US_I8(r, 24), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tc_st16_lanes(uint32_t addr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 ::US_I8(r, 0), US_I8(r, 8), "r"(addr) : "memory");
+}
+// (values that an asynchronous load writes must not be moved in front of its wait)
+__device__ __forceinline__ void pin32(uint32_t (&r)[32])
+{
+#pragma unroll
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i])::"memory");
+}
+__device__ __forceinline__ uint64_t f32x2(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void f32x2_split(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t half2_bits(float a, float b)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// The sequence and row tile of row tile `index` of the batch; row tiles of a sequence with the latest tokens (that see most) first.
+// rows: query rows of a head in the tile.
+struct PrItem {
+    KvSeq seq;
+    int s, row0, rows;
+};
+__device__ __forceinline__ bool pr_item(const KvPrompt& a, int64_t index, int lane, PrItem& it, bool report)
+{
+    int64_t before = 0;
+    bool any = false, found = false;
+    for (int base = 0; base < a.seqs.S; base += 32) {
+        int64_t cnt = 0;
+        if (base + lane < a.seqs.S) {
+            bool wrong;
+            const KvSeq q = kv_seq(a.seqs, a.pool, base + lane, wrong);
+            any |= wrong;
+            cnt = ((int64_t)q.n * a.G + kPrRows - 1) / kPrRows;
+        }
+        int64_t sum = cnt;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        const uint32_t who = __ballot_sync(0xffffffffu, index >= before + sum - cnt && index < before + sum);
+        if (who) {
+            const int l = __ffs(who) - 1;
+            it.s = base + l;
+            const int64_t tiles = __shfl_sync(0xffffffffu, cnt, l), j = index - before - __shfl_sync(0xffffffffu, sum - cnt, l);
+            bool wrong;
+            it.seq = kv_seq(a.seqs, a.pool, it.s, wrong);
+            it.row0 = (int)((tiles - 1 - j) * kPrRows);
+            it.rows = min(kPrRows, it.seq.n * a.G - it.row0);
+            found = true;
+            break;
+        }
+        before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    if (any && report) atomicExch(a.pool.err, kErrIndex);
+    return found;
+}
+// First and last + 1 unit of 128 tokens that the tile's rows see.
+__device__ __forceinline__ void pr_units(const KvPrompt& a, const PrItem& it, int& u0, int& u1)
+{
+    const int pos0 = it.seq.len - it.seq.n, first = pos0 + it.row0 / a.G, last = pos0 + (it.row0 + it.rows - 1) / a.G;
+    const int hi = a.causal ? last + 1 : it.seq.len, lo = a.window > 0 ? max(0, first - a.window + 1) : 0;
+    u0 = lo / kPrTile;
+    u1 = hi > lo ? (hi + kPrTile - 1) / kPrTile : u0;
+}
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(const __grid_constant__ KvPrompt a)
+{
+    using S = PrShape<D>;
+    constexpr int HALVES = D / 64;   // 128-byte columns of fp16
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bars[24];
+    __shared__ float4 steps[4][8];   // of a unit's 16-token groups: K's step (-1: not there), V's, its log2, its inverse
+    __shared__ uint32_t misc[2];
+    uint8_t* sq = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint8_t* sk = sq + 2 * S::kQ;
+    uint8_t* sv = sk + 2 * S::kKV;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t bar = smem_u32(bars);
+    const uint32_t b_q = bar, b_kf = bar + 16, b_ke = bar + 32, b_vf = bar + 48, b_ve = bar + 64, b_s = bar + 80, b_p = bar + 96, b_o = bar + 112, b_st = bar + 128, b_end = bar + 160;
+    volatile uint32_t* dead = misc + 1;
+    if (warp == 12) {
+        if (lane == 0) {
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(b_q + 8u * i, 4);
+                mbar_init(b_kf + 8u * i, 4); mbar_init(b_ke + 8u * i, 1);
+                mbar_init(b_vf + 8u * i, 4); mbar_init(b_ve + 8u * i, 1);
+                mbar_init(b_s + 8u * i, 1); mbar_init(b_p + 8u * i, 4); mbar_init(b_o + 8u * i, 1);
+            }
+            for (int i = 0; i < 4; ++i) mbar_init(b_st + 8u * i, 4);
+            mbar_init(b_end, 1);
+            misc[1] = 0;
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        __syncwarp();
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(misc)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (after the allocation: see us_mx4.cuh)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const uint32_t tm = *(volatile uint32_t*)misc;
+    const KvPool& p = a.pool;
+    const int split = (int)(blockIdx.x % a.splits), h = (int)(blockIdx.x / a.splits) % p.Hkv;
+    const int64_t index = blockIdx.x / ((unsigned)a.splits * p.Hkv);
+    PrItem it;
+    const bool have = pr_item(a, index, lane, it, threadIdx.x < 32);
+    bool ok = true;
+    int u0 = 0, u1 = 0;
+    if (have) {
+        pr_units(a, it, u0, u1);
+        const int n = u1 - u0;
+        u1 = u0 + (int)((int64_t)n * (split + 1) / a.splits);
+        u0 = u0 + (int)((int64_t)n * split / a.splits);
+    }
+    const int n = u1 - u0, nq = have && it.rows > 128 ? 2 : 1;
+    if (have && warp < 8) {
+        // ================= softmax: a thread a row =================
+        const int qi = warp >> 2, r = it.row0 + 128 * qi + 32 * (warp & 3) + lane, local = r - it.row0;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+        const uint32_t t_s = tm + lanes + 128u * qi, t_o = tm + lanes + 256u + 128u * qi;
+        const bool real = local < it.rows;
+        const int tok = real ? r / a.G : 0, qh = h * a.G + (real ? r - tok * a.G : 0);
+        const int pos = it.seq.len - it.seq.n + tok;
+        // (rows past the last are zero queries that see everything; never stored)
+        const int hi = real ? (a.causal ? pos + 1 : it.seq.len) : 0x7FFFFFFF, lo = real && a.window > 0 ? pos - a.window + 1 : -0x7FFFFFFF;
+        float m = -INFINITY, l = 0.f, ref = 0.f, lref = 0.f, f = a.scale2;
+        if (qi < nq && n > 0) {
+            // the row as fp16, bf16 times a power of two that brings it into range, to its place in the operand
+            const uint16_t* src = static_cast<const uint16_t*>(a.q) + (it.seq.first + tok) * a.q_token + (int64_t)qh * a.q_head;
+            float mul = a.negative ? -1.f : 1.f;
+            auto load = [&](int c) -> uint4 {
+                if (!real) return make_uint4(0, 0, 0, 0);
+                if (a.q_vec) return __ldcg(reinterpret_cast<const uint4*>(src) + c);
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = (uint32_t)src[8 * c + 2 * i] | ((uint32_t)src[8 * c + 2 * i + 1] << 16);
+                return make_uint4(w[0], w[1], w[2], w[3]);
+            };
+            if (BF16) {
+                uint32_t big = 0;
+#pragma unroll 4
+                for (int c = 0; c < D / 8; ++c) {
+                    const uint4 x = load(c);
+                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) big = max(big, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+                }
+                const int e = max(-112, min(114, (int)(big >> 7) - 127 - 14));
+                mul *= __uint_as_float((uint32_t)(127 - e) << 23);
+                f *= __uint_as_float((uint32_t)(127 + e) << 23);
+            }
+            const int rr = 32 * (warp & 3) + lane;
+            uint8_t* dst = sq + qi * S::kQ + rr * 128;
+#pragma unroll 4
+            for (int c = 0; c < D / 8; ++c) {
+                const uint4 x = load(c);
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                uint32_t y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (BF16) y[i] = half2_bits(__uint_as_float(w[i] << 16) * mul, __uint_as_float(w[i] & 0xFFFF0000u) * mul);
+                    else y[i] = a.negative ? w[i] ^ 0x80008000u : w[i];
+                }
+                *reinterpret_cast<uint4*>(dst + (c >> 3) * (128 * 128) + 16 * ((c & 7) ^ (rr & 7))) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_q + 8u * qi);
+#pragma unroll 1
+            for (int j = 0; j < n; ++j) {
+                ok = tc_wait_warp(b_st + 8u * (j & 3), (uint32_t)(j >> 2) & 1u, kMxWait, dead);
+                if (ok) ok = tc_wait_warp(b_s + 8u * qi, (uint32_t)j & 1u, kMxWait, dead);
+                if (!ok) break;
+                tc_fence_after();
+                const float4* st = steps[j & 3];
+                const int tok0 = (u0 + j) * kPrTile;
+                // V's steps: the largest so far is the reference; the fast path needs all of the unit's within 2^13 of it
+                float top = 0.f, least = INFINITY, grow = 1.f;
+                bool there = true;
+#pragma unroll
+                for (int g = 0; g < 8; ++g) {
+                    const float2 x = *reinterpret_cast<const float2*>(&st[g]);
+                    there = there && x.x >= 0.f;
+                    top = fmaxf(top, x.y);
+                    least = fminf(least, x.y == x.y ? x.y : -1.f);
+                }
+                if (top > ref) {
+                    grow = ref / top;
+                    ref = top;
+                    lref = log2f(top);
+                }
+                const bool fast = __all_sync(0xffffffffu, there && least >= ref * 0x1p-13f && least > 1e-30f && ref < 1e30f && lo <= tok0 && hi >= tok0 + kPrTile);
+                uint32_t x[32];
+                float mx = -INFINITY;
+                if (fast) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        tc_ld32(t_s + 32u * c, x);
+                        tc_wait_ld();
+                        pin32(x);
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) {
+                            float v = __uint_as_float(x[16 * g]);
+#pragma unroll
+                            for (int i = 1; i < 16; ++i) v = fmaxf(v, __uint_as_float(x[16 * g + i]));
+                            mx = fmaxf(mx, v * (f * st[2 * c + g].x));
+                        }
+                    }
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        tc_ld32(t_s + 32u * c, x);
+                        tc_wait_ld();
+                        pin32(x);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const float k = st[2 * c + (i >> 4)].x;
+                            const int t = tok0 + 32 * c + i;
+                            if (!(k < 0.f) && t >= lo && t < hi) mx = fmaxf(mx, __uint_as_float(x[i]) * (f * k));
+                        }
+                    }
+                }
+                // a new maximum, only where the old one is 2^8 behind
+                float alpha = grow;
+                if (mx > m + 8.f) {
+                    alpha *= m == -INFINITY ? 0.f : exp2_fast(m - mx);
+                    l *= m == -INFINITY ? 0.f : exp2_fast(m - mx);
+                    m = mx;
+                }
+                if (__any_sync(0xffffffffu, alpha != 1.f) && j > 0) {   // (the sums so far are complete: their product was issued before S's)
+#pragma unroll 1
+                    for (int c = 0; c < D / 32; ++c) {
+                        tc_ld32(t_o + 32u * c, x);
+                        tc_wait_ld();
+                        pin32(x);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * alpha);
+                        tc_st32(t_o + 32u * c, x);
+                    }
+                    tc_wait_st();
+                }
+                const float base = 7.f - (m == -INFINITY ? 0.f : m);
+                if (fast) {
+                    uint64_t sum = 0;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        tc_ld32(t_s + 32u * c, x);
+                        tc_wait_ld();
+                        pin32(x);
+                        uint32_t y[16];
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) {
+                            const float4 s4 = st[2 * c + g];
+                            const float k = f * s4.x, b = base + (s4.z - lref);
+                            const uint64_t k2 = f32x2(k, k), b2 = f32x2(b, b);
+                            uint64_t part = 0;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                float e0, e1;
+                                f32x2_split(fma2(f32x2(__uint_as_float(x[16 * g + 2 * i]), __uint_as_float(x[16 * g + 2 * i + 1])), k2, b2), e0, e1);
+                                e0 = exp2_fast(e0);
+                                e1 = exp2_fast(e1);
+                                part = add2(part, f32x2(e0, e1));
+                                y[8 * g + i] = half2_bits(e0, e1);
+                            }
+                            const float w = ref * s4.w;   // (p without V's step)
+                            sum = fma2(part, f32x2(w, w), sum);
+                        }
+                        tc_st16_lanes(t_s + 16u * c, y);
+                    }
+                    float s0, s1;
+                    f32x2_split(sum, s0, s1);
+                    l += s0 + s1;
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        tc_ld32(t_s + 32u * c, x);
+                        tc_wait_ld();
+                        pin32(x);
+                        uint32_t y[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float e[2];
+#pragma unroll
+                            for (int b = 0; b < 2; ++b) {
+                                const float2 kv = *reinterpret_cast<const float2*>(&st[2 * c + (i >> 3)]);
+                                const int t = tok0 + 32 * c + 2 * i + b;
+                                const bool sees = !(kv.x < 0.f) && t >= lo && t < hi;
+                                const float v = sees ? exp2_fast(__uint_as_float(x[2 * i + b]) * (f * kv.x) + base) : 0.f;
+                                l += v;
+                                e[b] = sees ? v * (kv.y == ref ? 1.f : __fdiv_rn(kv.y, ref)) : 0.f;
+                            }
+                            y[i] = half2_bits(e[0], e[1]);
+                        }
+                        tc_st16_lanes(t_s + 16u * c, y);
+                    }
+                }
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_p + 8u * qi);
+            }
+            if (ok) ok = tc_wait_warp(b_o + 8u * qi, 0, kMxWait, dead);
+            tc_fence_after();
+        }
+        if (qi < nq && ok) {
+            const float inv = l == 0.f ? 0.f : ref / l;
+            float* part = a.part + ((index * p.Hkv + h) * a.splits + split) * S::kPart;
+            if (real && a.splits > 1) {
+                part[kPrRows * D + 2 * local] = m;
+                part[kPrRows * D + 2 * local + 1] = l;
+            } else if (real && a.lse) {
+                a.lse[(it.seq.first + tok) * a.Hq + qh] = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(l) - 7.f) * 0.69314718f;
+            }
+            uint16_t* dst = static_cast<uint16_t*>(a.out) + (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head;
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t x[32];
+                if (n > 0) {
+                    tc_ld32(t_o + 32u * c, x);
+                    tc_wait_ld();
+                    pin32(x);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] = 0;
+                }
+                if (!real) continue;
+                if (a.splits > 1) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        *reinterpret_cast<float4*>(part + local * D + 32 * c + 4 * i) =
+                            make_float4(__uint_as_float(x[4 * i]) * ref, __uint_as_float(x[4 * i + 1]) * ref, __uint_as_float(x[4 * i + 2]) * ref, __uint_as_float(x[4 * i + 3]) * ref);
+                    continue;
+                }
+                uint32_t y[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float v0 = l == 0.f ? 0.f : __uint_as_float(x[2 * i]) * inv, v1 = l == 0.f ? 0.f : __uint_as_float(x[2 * i + 1]) * inv;
+                    if (BF16) {
+                        const __nv_bfloat162 b = __floats2bfloat162_rn(v0, v1);
+                        y[i] = *reinterpret_cast<const uint32_t*>(&b);
+                    } else {
+                        y[i] = half2_bits(v0, v1);
+                    }
+                }
+                if (a.o_vec) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(dst + 32 * c + 8 * i) = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) { dst[32 * c + 2 * i] = (uint16_t)y[i]; dst[32 * c + 2 * i + 1] = (uint16_t)(y[i] >> 16); }
+                }
+            }
+            tc_fence_before();
+        }
+    } else if (have && warp < 12 && n > 0) {
+        // ================= codes -> fp16 operands =================
+        // Warp w has tokens 32 w .. 32 w + 31 of a unit: two groups of 16, each in one block of the cache.
+        const int w = warp - 8;
+        const int32_t* row = a.seqs.table + (int64_t)it.s * a.seqs.table_stride;
+        const int first_seen = a.window > 0 ? max(0, it.seq.len - it.seq.n + it.row0 / a.G - a.window + 1) : 0;
+        int64_t at[2];      // first byte of the two groups, -1: not there
+        float4 st[2];
+        auto look = [&](int j) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const int t = (u0 + j) * kPrTile + 32 * w + 16 * g;
+                at[g] = -1;
+                st[g] = make_float4(-1.f, 0.f, 0.f, 0.f);
+                if (j < n && t < it.seq.len && t + 16 > first_seen) {   // (blocks in front of every window may be gone)
+                    const int32_t blk = __ldcg(row + t / p.T);
+                    if (blk >= 0 && blk < p.blocks) {
+                        const int64_t place = (int64_t)blk * p.Hkv + h;
+                        at[g] = (place * p.T + t % p.T) * D;
+                        st[g].x = __ldcg(p.k_step + place);
+                        st[g].y = __ldcg(p.v_step + place);
+                    } else {
+                        atomicExch(p.err, kErrIndex);
+                    }
+                }
+            }
+        };
+        // 16-byte pieces: rows of 4 lanes (64 bytes of D), 8 tokens an instruction, so that the stores below meet every bank once
+        constexpr int IN = 4 * HALVES;
+        auto fetch = [&](const int8_t* base, uint4 (&x)[IN]) {
+#pragma unroll
+            for (int i = 0; i < IN; ++i) {
+                const int half = i % HALVES, t8 = i / HALVES;   // tokens 8 t8 .. of the warp's 32
+                const int64_t b = at[t8 >> 1];
+                x[i] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
+                if (b >= 0) {
+                    x[i] = __ldcg(reinterpret_cast<const uint4*>(base + b + (8 * (t8 & 1) + (lane >> 2)) * D + 64 * half + 16 * (lane & 3)));
+                    x[i].x ^= 0x80808080u; x[i].y ^= 0x80808080u; x[i].z ^= 0x80808080u; x[i].w ^= 0x80808080u;
+                }
+            }
+        };
+        auto store = [&](uint8_t* base, const uint4 (&x)[IN]) {
+#pragma unroll
+            for (int i = 0; i < IN; ++i) {
+                const int half = i % HALVES, t8 = i / HALVES, t = 32 * w + 8 * t8 + (lane >> 2);
+                uint8_t* d = base + half * (kPrTile * 128) + t * 128;
+                const int c = 2 * (lane & 3);
+                *reinterpret_cast<uint4*>(d + 16 * (c ^ (t & 7))) = make_uint4(f16_low(x[i].x), f16_high(x[i].x), f16_low(x[i].y), f16_high(x[i].y));
+                *reinterpret_cast<uint4*>(d + 16 * ((c + 1) ^ (t & 7))) = make_uint4(f16_low(x[i].z), f16_high(x[i].z), f16_low(x[i].w), f16_high(x[i].w));
+            }
+        };
+        uint4 kx[IN], vx[IN];
+        look(0);
+        fetch(p.k, kx);
+        fetch(p.v, vx);
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+            const int slot = j & 1;
+            const uint32_t par = ((uint32_t)(j >> 1) & 1u) ^ 1u;
+            float4 here[2] = {st[0], st[1]};
+            look(j + 1);
+            ok = tc_wait_warp(b_ke + 8u * slot, par, kMxWait, dead);
+            if (!ok) break;
+            if (lane < 2) {
+                float4 s4 = lane ? here[1] : here[0];
+                s4.z = log2f(s4.y);
+                s4.w = 1.f / s4.y;
+                steps[j & 3][2 * w + lane] = s4;
+            }
+            store(sk + slot * S::kKV, kx);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) { mbar_arrive(b_st + 8u * (j & 3)); mbar_arrive(b_kf + 8u * slot); }
+            fetch(p.k, kx);
+            ok = tc_wait_warp(b_ve + 8u * slot, par, kMxWait, dead);
+            if (!ok) break;
+            store(sv + slot * S::kKV, vx);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_vf + 8u * slot);
+            fetch(p.v, vx);
+        }
+    } else if (have && warp == 12 && n > 0) {
+        // ================= MMA issue =================
+        const uint32_t leader = tc_elect();
+        const uint32_t id_s = (1u << 4) | (16u << 17) | (8u << 24);                              // fp32 += fp16 x fp16, both K-major, N = 128
+        const uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D / 8) << 17) | (8u << 24);   // B (V) MN-major, N = D
+        auto scores = [&](int i, int slot) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const uint32_t o = (uint32_t)((k >> 2) * (128 * 128) + (k & 3) * 32);
+                tc_mma_f16(leader, tm + 128u * i, mx4_desc(smem_u32(sq + i * S::kQ) + o, 1024, 2), mx4_desc(smem_u32(sk + slot * S::kKV) + o, 1024, 2), id_s, k > 0);
+            }
+        };
+        auto output = [&](int i, int slot, bool more) {
+            // V: 64 columns of D a swizzled row of 128 bytes; the next 64 after all tokens (leading offset), 8 tokens in 1024 bytes
+            const uint64_t lead = ((uint64_t)((kPrTile * 128) >> 4) << 16) - (1ull << 16);
+#pragma unroll
+            for (int k = 0; k < kPrTile / 16; ++k)
+                tc_mma_f16_ts(leader, tm + 256u + 128u * i, tm + 128u * i + 8u * k, mx4_desc(smem_u32(sv + slot * S::kKV) + 2048u * k, 1024, 2) + lead, id_o, more || k > 0);
+        };
+        for (int i = 0; i < nq && ok; ++i) ok = tc_wait_warp(b_q + 8u * i, 0, kMxWait, dead);
+        if (ok) ok = tc_wait_warp(b_kf, 0, kMxWait, dead);
+        tc_fence_after();
+        if (ok) {
+            for (int i = 0; i < nq; ++i) {
+                scores(i, 0);
+                tc_commit(leader, b_s + 8u * i);
+            }
+            tc_commit(leader, b_ke);
+        }
+        for (int j = 0; j < n && ok; ++j) {
+            const int slot = j & 1;
+            ok = tc_wait_warp(b_vf + 8u * slot, (uint32_t)(j >> 1) & 1u, kMxWait, dead);
+            for (int i = 0; i < nq && ok; ++i) {
+                ok = tc_wait_warp(b_p + 8u * i, (uint32_t)j & 1u, kMxWait, dead);
+                if (!ok) break;
+                tc_fence_after();
+                output(i, slot, j > 0);
+                if (i == nq - 1) tc_commit(leader, b_ve + 8u * slot);
+                if (j + 1 < n) {
+                    const int next = slot ^ 1;
+                    if (i == 0) {
+                        ok = tc_wait_warp(b_kf + 8u * next, (uint32_t)((j + 1) >> 1) & 1u, kMxWait, dead);
+                        if (!ok) break;
+                        tc_fence_after();
+                    }
+                    scores(i, next);
+                    tc_commit(leader, b_s + 8u * i);
+                    if (i == nq - 1) tc_commit(leader, b_ke + 8u * next);
+                } else {
+                    tc_commit(leader, b_o + 8u * i);
+                }
+            }
+        }
+        if (!ok) *dead = 1;
+        // nothing is in flight when the tensor memory is given back
+        tc_commit(leader, b_end);
+        mbar_wait_bounded(b_end, 0, kMxWait);
+        __syncwarp();
+    }
+    if (!ok && lane == 0) {
+        *dead = 1;
+        atomicExch(p.err, kErrTimeout);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
+}
+
+// Joins the parts of a row tile that was split over the cache's length: block (row tile, head, 8 rows), a warp a row.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) us_kv_prompt_join_kernel(const __grid_constant__ KvPrompt a)
+{
+    using S = PrShape<D>;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31, local = 8 * (int)(blockIdx.x % (kPrRows / 8)) + ((int)threadIdx.x >> 5);
+    const int64_t u = blockIdx.x / (kPrRows / 8), index = u / a.pool.Hkv;
+    const int h = (int)(u - index * a.pool.Hkv);
+    PrItem it;
+    if (!pr_item(a, index, lane, it, false) || local >= it.rows) return;
+    const float* part = a.part + u * a.splits * S::kPart;
+    float m[2], l[2];   // of parts lane and lane + 32
+    float big = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        m[i] = -INFINITY; l[i] = 0.f;
+        if (lane + 32 * i < a.splits) {
+            m[i] = __ldcg(part + (lane + 32 * i) * S::kPart + kPrRows * D + 2 * local);
+            l[i] = __ldcg(part + (lane + 32 * i) * S::kPart + kPrRows * D + 2 * local + 1);
+        }
+        big = fmaxf(big, m[i]);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+    const float base = big == -INFINITY ? 0.f : big;
+    float e[2], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        e[i] = m[i] == -INFINITY && l[i] == 0.f ? 0.f : exp2_fast(m[i] - base);
+        sum += e[i] * l[i];
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    constexpr int C = D / 32;
+    float acc[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) acc[i] = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float w = __shfl_sync(0xffffffffu, s < 32 ? e[0] : e[1], s & 31);
+        if (w == 0.f) continue;
+#pragma unroll
+        for (int i = 0; i < C; ++i) acc[i] += w * __ldcg(part + s * S::kPart + local * D + lane + 32 * i);
+    }
+    const int r = it.row0 + local, tok = r / a.G, qh = h * a.G + r - tok * a.G;
+    const int64_t at = (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const float y = sum == 0.f ? 0.f : acc[i] / sum;
+        if (BF16) static_cast<__nv_bfloat16*>(a.out)[at + lane + 32 * i] = __float2bfloat16_rn(y);
+        else static_cast<__half*>(a.out)[at + lane + 32 * i] = __float2half_rn(y);
+    }
+    if (a.lse && lane == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = sum == 0.f ? -INFINITY : (base + log2f(sum) - 7.f) * 0.69314718f;
+}
+
+}  // namespace us
