@@ -266,6 +266,7 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
         a.q_vec = rows_vec(Q, type, q_token_stride, q_head_stride);
         a.o_vec = rows_vec(out, type, o_token_stride, o_head_stride);
         a.splits = pl.splits;
+        while ((1 << a.log2_T) < h->pool.T) ++a.log2_T;
         us_status s = error_word(&a.pool.err);
         if (s != US_OK) return s;
         void* args[] = {&a};

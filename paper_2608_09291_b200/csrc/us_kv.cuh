@@ -454,7 +454,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                 }
                 const int m = min(32 / nb, n - i0);
                 for (int i = 0; i < m; ++i) {
-                    ok = tc_wait_warp(b_empty + 8u * stage, par ^ 1u, kMxWait, dead);
+                    ok = ops_wait_warp(b_empty + 8u * stage, par ^ 1u, kMxWait, dead);
                     if (!ok) break;
                     // the steps of the unit's four 16-token groups
                     const int from = i * nb + (lane & 3) * 16 / box;
@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
         }
         // (nothing may be in flight when the CTA ends)
         if (!ok)
-            for (long long i = max(0ll, issued - a.stages); i < issued; ++i) mbar_wait_bounded(b_full + 8u * (uint32_t)(i % a.stages), (uint32_t)(i / a.stages) & 1u, kMxWait);
+            for (long long i = max(0ll, issued - a.stages); i < issued; ++i) ops_wait(b_full + 8u * (uint32_t)(i % a.stages), (uint32_t)(i / a.stages) & 1u, kMxWait);
         __syncwarp();
     } else {
         const int g = lane >> 2, t = lane & 3;
@@ -567,7 +567,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
             float ref = 0.f;   // V's largest step so far
 #pragma unroll 1
             for (int i = 0; i < n; ++i) {
-                ok = tc_wait_warp(b_full + 8u * stage, par, kMxWait, dead);
+                ok = ops_wait_warp(b_full + 8u * stage, par, kMxWait, dead);
                 if (!ok) break;
                 const float2 st = steps[stage][warp];
                 const int tok0 = (it.t_lo + tile + i) * kKvTile + 16 * warp;

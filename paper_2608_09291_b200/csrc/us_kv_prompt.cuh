@@ -31,6 +31,7 @@ struct KvPrompt {
     int32_t Hq, G;
     int32_t causal, window;
     int32_t q_vec, o_vec;
+    int32_t log2_T;
     int32_t splits;
 };
 
@@ -39,7 +40,7 @@ struct PrShape {
     static constexpr int kQ = 128 * D * 2, kKV = kPrTile * D * 2;   // bytes
     static constexpr int kSmem = 1024 + 2 * kQ + 4 * kKV;
     static constexpr int64_t kPart = kPrRows * (D + 2);
-    static constexpr int kThreads = 13 * 32;
+    static constexpr int kThreads = 16 * 32;   // softmax 2 x 4 warps, conversion 4, MMA issue 1 (and three that only fill its group)
 };
 
 __device__ __forceinline__ void tc_mma_f16(uint32_t elected, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
@@ -72,6 +73,12 @@ __device__ __forceinline__ void tc_st16_lanes(uint32_t addr, const uint32_t (&r)
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
                  ::US_I8(r, 0), US_I8(r, 8), "r"(addr) : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 // (values that an asynchronous load writes must not be moved in front of its wait)
 __device__ __forceinline__ void pin32(uint32_t (&r)[32])
@@ -168,7 +175,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
     uint8_t* sv = sk + 2 * S::kKV;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t bar = smem_u32(bars);
-    const uint32_t b_q = bar, b_kf = bar + 16, b_ke = bar + 32, b_vf = bar + 48, b_ve = bar + 64, b_s = bar + 80, b_p = bar + 96, b_o = bar + 112, b_st = bar + 128, b_end = bar + 160;
+    const uint32_t b_q = bar, b_kf = bar + 16, b_ke = bar + 32, b_vf = bar + 48, b_ve = bar + 64, b_s = bar + 80, b_p = bar + 96, b_o = bar + 128, b_st = bar + 144, b_end = bar + 176;
     volatile uint32_t* dead = misc + 1;
     if (warp == 12) {
         if (lane == 0) {
@@ -176,7 +183,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                 mbar_init(b_q + 8u * i, 4);
                 mbar_init(b_kf + 8u * i, 4); mbar_init(b_ke + 8u * i, 1);
                 mbar_init(b_vf + 8u * i, 4); mbar_init(b_ve + 8u * i, 1);
-                mbar_init(b_s + 8u * i, 1); mbar_init(b_p + 8u * i, 4); mbar_init(b_o + 8u * i, 1);
+                mbar_init(b_s + 8u * i, 1); mbar_init(b_p + 16u * i, 4); mbar_init(b_p + 16u * i + 8, 4); mbar_init(b_o + 8u * i, 1);
             }
             for (int i = 0; i < 4; ++i) mbar_init(b_st + 8u * i, 4);
             mbar_init(b_end, 1);
@@ -207,7 +214,10 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
         u0 = u0 + (int)((int64_t)n * split / a.splits);
     }
     const int n = u1 - u0, nq = have && it.rows > 128 ? 2 : 1;
-    if (have && warp < 8) {
+    // Registers of a thread: 128 at launch, 16 warps; 2 x 176 + 96 + 64 = 4 x 128.
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        if (have) {
         // ================= softmax: a thread a row =================
         const int qi = warp >> 2, r = it.row0 + 128 * qi + 32 * (warp & 3) + lane, local = r - it.row0;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
@@ -230,12 +240,14 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                 for (int i = 0; i < 4; ++i) w[i] = (uint32_t)src[8 * c + 2 * i] | ((uint32_t)src[8 * c + 2 * i + 1] << 16);
                 return make_uint4(w[0], w[1], w[2], w[3]);
             };
+            uint4 row[D / 8];
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) row[c] = load(c);
             if (BF16) {
                 uint32_t big = 0;
-#pragma unroll 4
+#pragma unroll
                 for (int c = 0; c < D / 8; ++c) {
-                    const uint4 x = load(c);
-                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    const uint32_t w[4] = {row[c].x, row[c].y, row[c].z, row[c].w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) big = max(big, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
                 }
@@ -245,10 +257,9 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             }
             const int rr = 32 * (warp & 3) + lane;
             uint8_t* dst = sq + qi * S::kQ + rr * 128;
-#pragma unroll 4
+#pragma unroll
             for (int c = 0; c < D / 8; ++c) {
-                const uint4 x = load(c);
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                const uint32_t w[4] = {row[c].x, row[c].y, row[c].z, row[c].w};
                 uint32_t y[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -262,139 +273,132 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             if (lane == 0) mbar_arrive(b_q + 8u * qi);
 #pragma unroll 1
             for (int j = 0; j < n; ++j) {
-                ok = tc_wait_warp(b_st + 8u * (j & 3), (uint32_t)(j >> 2) & 1u, kMxWait, dead);
-                if (ok) ok = tc_wait_warp(b_s + 8u * qi, (uint32_t)j & 1u, kMxWait, dead);
+                ok = ops_wait_warp(b_st + 8u * (j & 3), (uint32_t)(j >> 2) & 1u, kMxWait, dead);
+                if (ok) ok = ops_wait_warp(b_s + 8u * qi, (uint32_t)j & 1u, kMxWait, dead);
                 if (!ok) break;
                 tc_fence_after();
                 const float4* st = steps[j & 3];
                 const int tok0 = (u0 + j) * kPrTile;
                 // V's steps: the largest so far is the reference; the fast path needs all of the unit's within 2^13 of it
-                float top = 0.f, least = INFINITY, grow = 1.f;
-                bool there = true;
-#pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    const float2 x = *reinterpret_cast<const float2*>(&st[g]);
-                    there = there && x.x >= 0.f;
-                    top = fmaxf(top, x.y);
-                    least = fminf(least, x.y == x.y ? x.y : -1.f);
-                }
+                const float2 mine = *reinterpret_cast<const float2*>(&st[lane & 7]);
+                float top = fmaxf(mine.y, 0.f), grow = 1.f;
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                 if (top > ref) {
                     grow = ref / top;
                     ref = top;
                     lref = log2f(top);
                 }
-                const bool fast = __all_sync(0xffffffffu, there && least >= ref * 0x1p-13f && least > 1e-30f && ref < 1e30f && lo <= tok0 && hi >= tok0 + kPrTile);
-                uint32_t x[32];
+                const bool fast = __all_sync(0xffffffffu, mine.x >= 0.f && mine.y >= ref * 0x1p-13f && mine.y > 1e-30f && ref < 1e30f && lo <= tok0 && hi >= tok0 + kPrTile);
+                uint32_t x[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tc_ld32(t_s + 32u * c, x[c]);
+                tc_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) pin32(x[c]);
+                // which of the unit's tokens the row sees
+                uint32_t sees[4];
                 float mx = -INFINITY;
-                if (fast) {
+                if (!fast) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        tc_ld32(t_s + 32u * c, x);
-                        tc_wait_ld();
-                        pin32(x);
+                        const int t = tok0 + 32 * c;
+                        const uint32_t from = lo <= t ? ~0u : lo - t >= 32 ? 0u : ~0u << (lo - t), to = hi - t >= 32 ? ~0u : hi <= t ? 0u : ~(~0u << (hi - t));
+                        sees[c] = from & to & (st[2 * c].x < 0.f ? 0xFFFF0000u : ~0u) & (st[2 * c + 1].x < 0.f ? 0x0000FFFFu : ~0u);
 #pragma unroll
-                        for (int g = 0; g < 2; ++g) {
-                            float v = __uint_as_float(x[16 * g]);
-#pragma unroll
-                            for (int i = 1; i < 16; ++i) v = fmaxf(v, __uint_as_float(x[16 * g + i]));
-                            mx = fmaxf(mx, v * (f * st[2 * c + g].x));
-                        }
-                    }
-                } else {
-#pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        tc_ld32(t_s + 32u * c, x);
-                        tc_wait_ld();
-                        pin32(x);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const float k = st[2 * c + (i >> 4)].x;
-                            const int t = tok0 + 32 * c + i;
-                            if (!(k < 0.f) && t >= lo && t < hi) mx = fmaxf(mx, __uint_as_float(x[i]) * (f * k));
-                        }
+                        for (int i = 0; i < 32; ++i)
+                            if (!(sees[c] & (1u << i))) x[c][i] = 0xFF800000u;
                     }
                 }
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        float v = __uint_as_float(x[c][16 * g + 15]);
+#pragma unroll
+                        for (int i = 0; i < 14; i += 2) v = max3(v, __uint_as_float(x[c][16 * g + i]), __uint_as_float(x[c][16 * g + i + 1]));
+                        v = fmaxf(v, __uint_as_float(x[c][16 * g + 14]));
+                        mx = fmaxf(mx, v * (f * fmaxf(st[2 * c + g].x, 0.f)));   // (a group that is not there: -inf x 0, no maximum)
+                    }
                 // a new maximum, only where the old one is 2^8 behind
                 float alpha = grow;
                 if (mx > m + 8.f) {
-                    alpha *= m == -INFINITY ? 0.f : exp2_fast(m - mx);
-                    l *= m == -INFINITY ? 0.f : exp2_fast(m - mx);
+                    const float e = m == -INFINITY ? 0.f : exp2_fast(m - mx);
+                    alpha *= e;
+                    l *= e;
                     m = mx;
                 }
                 if (__any_sync(0xffffffffu, alpha != 1.f) && j > 0) {   // (the sums so far are complete: their product was issued before S's)
 #pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {
-                        tc_ld32(t_o + 32u * c, x);
-                        tc_wait_ld();
-                        pin32(x);
+                    for (int c = 0; c < D / 16; ++c) {
+                        uint32_t o[16];
+                        tc_ld16(t_o + 16u * c, o);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * alpha);
-                        tc_st32(t_o + 32u * c, x);
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                        tc_st16_lanes(t_o + 16u * c, o);
                     }
                     tc_wait_st();
                 }
+                auto publish = [&](int half) {   // P of 64 tokens is in place: their product can begin
+                    tc_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(b_p + 16u * qi + 8u * half);
+                };
                 const float base = 7.f - (m == -INFINITY ? 0.f : m);
                 if (fast) {
-                    uint64_t sum = 0;
+                    float sum = 0.f;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        tc_ld32(t_s + 32u * c, x);
-                        tc_wait_ld();
-                        pin32(x);
                         uint32_t y[16];
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
                             const float4 s4 = st[2 * c + g];
                             const float k = f * s4.x, b = base + (s4.z - lref);
-                            const uint64_t k2 = f32x2(k, k), b2 = f32x2(b, b);
-                            uint64_t part = 0;
+                            float p0 = 0.f, p1 = 0.f;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
-                                float e0, e1;
-                                f32x2_split(fma2(f32x2(__uint_as_float(x[16 * g + 2 * i]), __uint_as_float(x[16 * g + 2 * i + 1])), k2, b2), e0, e1);
-                                e0 = exp2_fast(e0);
-                                e1 = exp2_fast(e1);
-                                part = add2(part, f32x2(e0, e1));
+                                const float e0 = exp2_fast(fmaf(__uint_as_float(x[c][16 * g + 2 * i]), k, b)), e1 = exp2_fast(fmaf(__uint_as_float(x[c][16 * g + 2 * i + 1]), k, b));
+                                p0 += e0;
+                                p1 += e1;
                                 y[8 * g + i] = half2_bits(e0, e1);
                             }
-                            const float w = ref * s4.w;   // (p without V's step)
-                            sum = fma2(part, f32x2(w, w), sum);
+                            sum = fmaf(p0 + p1, ref * s4.w, sum);   // (p without V's step)
                         }
                         tc_st16_lanes(t_s + 16u * c, y);
+                        if (c == 1) publish(0);
                     }
-                    float s0, s1;
-                    f32x2_split(sum, s0, s1);
-                    l += s0 + s1;
+                    l += sum;
                 } else {
-#pragma unroll 1
+#pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        tc_ld32(t_s + 32u * c, x);
-                        tc_wait_ld();
-                        pin32(x);
                         uint32_t y[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            float e[2];
+                        for (int g = 0; g < 2; ++g) {
+                            const float2 kv = *reinterpret_cast<const float2*>(&st[2 * c + g]);
+                            const float k = f * kv.x, rel = kv.y == ref ? 1.f : __fdiv_rn(kv.y, ref);
 #pragma unroll
-                            for (int b = 0; b < 2; ++b) {
-                                const float2 kv = *reinterpret_cast<const float2*>(&st[2 * c + (i >> 3)]);
-                                const int t = tok0 + 32 * c + 2 * i + b;
-                                const bool sees = !(kv.x < 0.f) && t >= lo && t < hi;
-                                const float v = sees ? exp2_fast(__uint_as_float(x[2 * i + b]) * (f * kv.x) + base) : 0.f;
-                                l += v;
-                                e[b] = sees ? v * (kv.y == ref ? 1.f : __fdiv_rn(kv.y, ref)) : 0.f;
+                            for (int i = 0; i < 8; ++i) {
+                                float e[2];
+#pragma unroll
+                                for (int b = 0; b < 2; ++b) {
+                                    const int at = 16 * g + 2 * i + b;
+                                    e[b] = exp2_fast(__uint_as_float(x[c][at]) * k + base);
+                                    if (!(sees[c] & (1u << at))) e[b] = 0.f;
+                                    l += e[b];
+                                }
+                                // (a group that is not there has no step)
+                                y[8 * g + i] = (sees[c] >> (16 * g)) & 0xFFFFu ? half2_bits(e[0] == 0.f ? 0.f : e[0] * rel, e[1] == 0.f ? 0.f : e[1] * rel) : 0u;
                             }
-                            y[i] = half2_bits(e[0], e[1]);
                         }
                         tc_st16_lanes(t_s + 16u * c, y);
+                        if (c == 1) publish(0);
                     }
                 }
-                tc_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(b_p + 8u * qi);
+                publish(1);
             }
-            if (ok) ok = tc_wait_warp(b_o + 8u * qi, 0, kMxWait, dead);
+            if (ok) ok = ops_wait_warp(b_o + 8u * qi, 0, kMxWait, dead);
             tc_fence_after();
         }
         if (qi < nq && ok) {
@@ -447,29 +451,42 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             }
             tc_fence_before();
         }
-    } else if (have && warp < 12 && n > 0) {
+        }
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        if (have && n > 0) {
         // ================= codes -> fp16 operands =================
         // Warp w has tokens 32 w .. 32 w + 31 of a unit: two groups of 16, each in one block of the cache.
         const int w = warp - 8;
         const int32_t* row = a.seqs.table + (int64_t)it.s * a.seqs.table_stride;
         const int first_seen = a.window > 0 ? max(0, it.seq.len - it.seq.n + it.row0 / a.G - a.window + 1) : 0;
-        int64_t at[2];      // first byte of the two groups, -1: not there
-        float4 st[2];
+        // The block numbers of a unit are loaded two units ahead, its steps one: nothing here waits for a load that was just issued.
+        int32_t blk[2] = {-1, -1};
+        int64_t at[2] = {-1, -1};   // first byte of the two groups, -1: not there
+        float2 st[2];
+        bool missing = false;
+        auto token = [&](int j, int g) { return (u0 + j) * kPrTile + 32 * w + 16 * g; };
+        auto needed = [&](int j, int t) { return j < n && t < it.seq.len && t + 16 > first_seen; };   // (blocks in front of every window may be gone)
         auto look = [&](int j) {
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-                const int t = (u0 + j) * kPrTile + 32 * w + 16 * g;
+                const int t = token(j, g);
+                blk[g] = needed(j, t) ? __ldcg(row + (t >> a.log2_T)) : 0;
+            }
+        };
+        auto locate = [&](int j) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const int t = token(j, g);
+                const bool in = (uint32_t)blk[g] < (uint32_t)p.blocks;
                 at[g] = -1;
-                st[g] = make_float4(-1.f, 0.f, 0.f, 0.f);
-                if (j < n && t < it.seq.len && t + 16 > first_seen) {   // (blocks in front of every window may be gone)
-                    const int32_t blk = __ldcg(row + t / p.T);
-                    if (blk >= 0 && blk < p.blocks) {
-                        const int64_t place = (int64_t)blk * p.Hkv + h;
-                        at[g] = (place * p.T + t % p.T) * D;
-                        st[g].x = __ldcg(p.k_step + place);
-                        st[g].y = __ldcg(p.v_step + place);
-                    } else {
-                        atomicExch(p.err, kErrIndex);
+                st[g] = make_float2(-1.f, 0.f);
+                if (needed(j, t)) {
+                    missing |= !in;
+                    if (in) {
+                        const int64_t place = (int64_t)blk[g] * p.Hkv + h;
+                        at[g] = ((place << a.log2_T) + (t & (p.T - 1))) * D;
+                        st[g] = make_float2(__ldcg(p.k_step + place), __ldcg(p.v_step + place));
                     }
                 }
             }
@@ -481,11 +498,8 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             for (int i = 0; i < IN; ++i) {
                 const int half = i % HALVES, t8 = i / HALVES;   // tokens 8 t8 .. of the warp's 32
                 const int64_t b = at[t8 >> 1];
-                x[i] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
-                if (b >= 0) {
-                    x[i] = __ldcg(reinterpret_cast<const uint4*>(base + b + (8 * (t8 & 1) + (lane >> 2)) * D + 64 * half + 16 * (lane & 3)));
-                    x[i].x ^= 0x80808080u; x[i].y ^= 0x80808080u; x[i].z ^= 0x80808080u; x[i].w ^= 0x80808080u;
-                }
+                x[i] = make_uint4(0, 0, 0, 0);
+                if (b >= 0) x[i] = __ldcg(reinterpret_cast<const uint4*>(base + b + (8 * (t8 & 1) + (lane >> 2)) * D + 64 * half + 16 * (lane & 3)));
             }
         };
         auto store = [&](uint8_t* base, const uint4 (&x)[IN]) {
@@ -494,34 +508,37 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                 const int half = i % HALVES, t8 = i / HALVES, t = 32 * w + 8 * t8 + (lane >> 2);
                 uint8_t* d = base + half * (kPrTile * 128) + t * 128;
                 const int c = 2 * (lane & 3);
-                *reinterpret_cast<uint4*>(d + 16 * (c ^ (t & 7))) = make_uint4(f16_low(x[i].x), f16_high(x[i].x), f16_low(x[i].y), f16_high(x[i].y));
-                *reinterpret_cast<uint4*>(d + 16 * ((c + 1) ^ (t & 7))) = make_uint4(f16_low(x[i].z), f16_high(x[i].z), f16_low(x[i].w), f16_high(x[i].w));
+                // (the loads are a unit old: nothing touches them before)
+                const uint32_t x0 = x[i].x ^ 0x80808080u, x1 = x[i].y ^ 0x80808080u, x2 = x[i].z ^ 0x80808080u, x3 = x[i].w ^ 0x80808080u;
+                *reinterpret_cast<uint4*>(d + 16 * (c ^ (t & 7))) = make_uint4(f16_low(x0), f16_high(x0), f16_low(x1), f16_high(x1));
+                *reinterpret_cast<uint4*>(d + 16 * ((c + 1) ^ (t & 7))) = make_uint4(f16_low(x2), f16_high(x2), f16_low(x3), f16_high(x3));
             }
         };
         uint4 kx[IN], vx[IN];
         look(0);
+        locate(0);
+        look(1);
         fetch(p.k, kx);
         fetch(p.v, vx);
 #pragma unroll 1
         for (int j = 0; j < n; ++j) {
             const int slot = j & 1;
             const uint32_t par = ((uint32_t)(j >> 1) & 1u) ^ 1u;
-            float4 here[2] = {st[0], st[1]};
-            look(j + 1);
-            ok = tc_wait_warp(b_ke + 8u * slot, par, kMxWait, dead);
+            const float2 here[2] = {st[0], st[1]};
+            locate(j + 1);
+            look(j + 2);
+            ok = ops_wait_warp(b_ke + 8u * slot, par, kMxWait, dead);
             if (!ok) break;
             if (lane < 2) {
-                float4 s4 = lane ? here[1] : here[0];
-                s4.z = log2f(s4.y);
-                s4.w = 1.f / s4.y;
-                steps[j & 3][2 * w + lane] = s4;
+                const float2 s2 = lane ? here[1] : here[0];
+                steps[j & 3][2 * w + lane] = make_float4(s2.x, s2.y, log2f(s2.y), 1.f / s2.y);
             }
             store(sk + slot * S::kKV, kx);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) { mbar_arrive(b_st + 8u * (j & 3)); mbar_arrive(b_kf + 8u * slot); }
             fetch(p.k, kx);
-            ok = tc_wait_warp(b_ve + 8u * slot, par, kMxWait, dead);
+            ok = ops_wait_warp(b_ve + 8u * slot, par, kMxWait, dead);
             if (!ok) break;
             store(sv + slot * S::kKV, vx);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -529,27 +546,32 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             if (lane == 0) mbar_arrive(b_vf + 8u * slot);
             fetch(p.v, vx);
         }
-    } else if (have && warp == 12 && n > 0) {
+        if (missing) atomicExch(p.err, kErrIndex);
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (have && warp == 12 && n > 0) {
         // ================= MMA issue =================
         const uint32_t leader = tc_elect();
         const uint32_t id_s = (1u << 4) | (16u << 17) | (8u << 24);                              // fp32 += fp16 x fp16, both K-major, N = 128
         const uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D / 8) << 17) | (8u << 24);   // B (V) MN-major, N = D
+        const uint64_t dq = mx4_desc(smem_u32(sq), 1024, 2), dk = mx4_desc(smem_u32(sk), 1024, 2);
+        // V: 64 columns of D a swizzled row of 128 bytes; the next 64 after all tokens (leading offset), 8 tokens in 1024 bytes
+        const uint64_t dv = mx4_desc(smem_u32(sv), 1024, 2) + (((uint64_t)((kPrTile * 128) >> 4) << 16) - (1ull << 16));
         auto scores = [&](int i, int slot) {
+            const uint64_t a0 = dq + (uint32_t)(i * (S::kQ >> 4)), b0 = dk + (uint32_t)(slot * (S::kKV >> 4));
+            const uint32_t d = tm + 128u * i;
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const uint32_t o = (uint32_t)((k >> 2) * (128 * 128) + (k & 3) * 32);
-                tc_mma_f16(leader, tm + 128u * i, mx4_desc(smem_u32(sq + i * S::kQ) + o, 1024, 2), mx4_desc(smem_u32(sk + slot * S::kKV) + o, 1024, 2), id_s, k > 0);
-            }
+            for (int k = 0; k < D / 16; ++k) tc_mma_f16(leader, d, a0 + ((k >> 2) * 1024 + (k & 3) * 2), b0 + ((k >> 2) * 1024 + (k & 3) * 2), id_s, k > 0);
         };
-        auto output = [&](int i, int slot, bool more) {
-            // V: 64 columns of D a swizzled row of 128 bytes; the next 64 after all tokens (leading offset), 8 tokens in 1024 bytes
-            const uint64_t lead = ((uint64_t)((kPrTile * 128) >> 4) << 16) - (1ull << 16);
+        auto output = [&](int i, int slot, int half, bool more) {
+            const uint64_t b0 = dv + (uint32_t)(slot * (S::kKV >> 4) + 512 * half);
+            const uint32_t d = tm + 256u + 128u * i, a0 = tm + 128u * i + 32u * half;
 #pragma unroll
-            for (int k = 0; k < kPrTile / 16; ++k)
-                tc_mma_f16_ts(leader, tm + 256u + 128u * i, tm + 128u * i + 8u * k, mx4_desc(smem_u32(sv + slot * S::kKV) + 2048u * k, 1024, 2) + lead, id_o, more || k > 0);
+            for (int k = 0; k < 4; ++k) tc_mma_f16_ts(leader, d, a0 + 8u * k, b0 + 128u * k, id_o, more || half > 0 || k > 0);
         };
-        for (int i = 0; i < nq && ok; ++i) ok = tc_wait_warp(b_q + 8u * i, 0, kMxWait, dead);
-        if (ok) ok = tc_wait_warp(b_kf, 0, kMxWait, dead);
+        for (int i = 0; i < nq && ok; ++i) ok = ops_wait_warp(b_q + 8u * i, 0, kMxWait, dead);
+        if (ok) ok = ops_wait_warp(b_kf, 0, kMxWait, dead);
         tc_fence_after();
         if (ok) {
             for (int i = 0; i < nq; ++i) {
@@ -559,21 +581,20 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             tc_commit(leader, b_ke);
         }
         for (int j = 0; j < n && ok; ++j) {
-            const int slot = j & 1;
-            ok = tc_wait_warp(b_vf + 8u * slot, (uint32_t)(j >> 1) & 1u, kMxWait, dead);
+            const int slot = j & 1, next = slot ^ 1;
+            // (first what has long been there, so that nothing but P is waited for between the softmax and its products)
+            ok = ops_wait_warp(b_vf + 8u * slot, (uint32_t)(j >> 1) & 1u, kMxWait, dead);
+            if (ok && j + 1 < n) ok = ops_wait_warp(b_kf + 8u * next, (uint32_t)((j + 1) >> 1) & 1u, kMxWait, dead);
             for (int i = 0; i < nq && ok; ++i) {
-                ok = tc_wait_warp(b_p + 8u * i, (uint32_t)j & 1u, kMxWait, dead);
+                for (int half = 0; half < 2 && ok; ++half) {
+                    ok = ops_wait_warp(b_p + 16u * i + 8u * half, (uint32_t)j & 1u, kMxWait, dead);
+                    if (!ok) break;
+                    tc_fence_after();
+                    output(i, slot, half, j > 0);
+                }
                 if (!ok) break;
-                tc_fence_after();
-                output(i, slot, j > 0);
                 if (i == nq - 1) tc_commit(leader, b_ve + 8u * slot);
                 if (j + 1 < n) {
-                    const int next = slot ^ 1;
-                    if (i == 0) {
-                        ok = tc_wait_warp(b_kf + 8u * next, (uint32_t)((j + 1) >> 1) & 1u, kMxWait, dead);
-                        if (!ok) break;
-                        tc_fence_after();
-                    }
                     scores(i, next);
                     tc_commit(leader, b_s + 8u * i);
                     if (i == nq - 1) tc_commit(leader, b_ke + 8u * next);
@@ -585,8 +606,9 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
         if (!ok) *dead = 1;
         // nothing is in flight when the tensor memory is given back
         tc_commit(leader, b_end);
-        mbar_wait_bounded(b_end, 0, kMxWait);
+        ops_wait(b_end, 0, kMxWait);
         __syncwarp();
+        }
     }
     if (!ok && lane == 0) {
         *dead = 1;

@@ -20,6 +20,26 @@ __host__ __device__ __forceinline__ int64_t mx4_tiles(int64_t n, int64_t per) { 
 __device__ __forceinline__ uint32_t mx4_code_off(uint32_t r, uint32_t c) { return (uint32_t)kMxScales + 128u * r + 16u * (c ^ (r & 7u)); }
 __device__ __forceinline__ uint32_t mx4_scale_off(uint32_t r, uint32_t half) { return 512u * half + 16u * (r & 31u) + 4u * (r >> 5); }
 
+// Bounded wait of a whole warp: a few hundred tries, each of which sleeps on the barrier, before the clock is first read (reading it
+// costs more than most of these waits take; behind it as tc_wait_warp, which see).
+__device__ __forceinline__ bool ops_wait_warp(uint32_t bar, uint32_t parity, uint32_t limit_hi, volatile uint32_t* dead, bool after = false)
+{
+#pragma unroll 1
+    for (int i = 0; i < 256; ++i) {
+        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+        if (__any_sync(0xffffffffu, *dead)) return false;
+    }
+    return tc_wait_warp(bar, parity, limit_hi, dead, after);
+}
+// The same for one thread.
+__device__ __forceinline__ bool ops_wait(uint32_t bar, uint32_t parity, uint32_t limit_hi)
+{
+#pragma unroll 1
+    for (int i = 0; i < 256; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    return mbar_wait_bounded(bar, parity, limit_hi);
+}
+
 // ---- quantisation ----------------------------------------------------------------------------------------------------
 // Scale byte of a block whose largest magnitude has these fp32 bits: e = floor(log2 a) - 2 clamped to [-127, 127], + 127. With the
 // biased exponent x of a that is x - 2 (subnormal and 0: 0); Inf and NaN: 255, the scale's NaN.
@@ -390,7 +410,7 @@ __global__ void __launch_bounds__(192, 1) us_mx4_product_kernel(const __grid_con
             int s = 0;
             uint32_t par = 0;
             for (int i = first; i < n; ++i) {
-                if (!mbar_wait_bounded(b_empty + 8u * s, par, kMxWait)) { ok = false; break; }
+                if (!ops_wait(b_empty + 8u * s, par, kMxWait)) { ok = false; break; }
                 copy_w(i, s);
                 if (!FUSE) copy_x(i, s);
                 ++issued;
@@ -398,7 +418,7 @@ __global__ void __launch_bounds__(192, 1) us_mx4_product_kernel(const __grid_con
             }
             // (nothing may be in flight when the CTA ends: the last copies are waited for here if the other warps gave up)
             if (!ok)
-                for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait_bounded(b_full + 8u * (i % p.stages), (uint32_t)(i / p.stages) & 1u, kMxWait);
+                for (int i = max(0, issued - p.stages); i < issued; ++i) ops_wait(b_full + 8u * (i % p.stages), (uint32_t)(i / p.stages) & 1u, kMxWait);
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -408,13 +428,13 @@ __global__ void __launch_bounds__(192, 1) us_mx4_product_kernel(const __grid_con
         const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(NB / 8) << 17) | (1u << 23) | (8u << 24);
         const uint32_t kUpper = (2u << 4) | (2u << 29);
         if (FUSE) {
-            ok = tc_wait_warp(b_x, 0, kMxWait, dead, true);
+            ok = ops_wait_warp(b_x, 0, kMxWait, dead, true);
             tc_fence_after();
         }
         int s = 0;
         uint32_t par = 0;
         for (int t = t0; t < t1 && ok; ++t) {
-            ok = tc_wait_warp(b_full + 8u * s, par, kMxWait, dead, true);
+            ok = ops_wait_warp(b_full + 8u * s, par, kMxWait, dead, true);
             if (!ok) break;
             tc_fence_after();
             const uint32_t a = smem_u32(ring + (size_t)s * S::kStage);
@@ -450,7 +470,7 @@ __global__ void __launch_bounds__(192, 1) us_mx4_product_kernel(const __grid_con
             __syncwarp();
             if (lane == 0) mbar_arrive(b_x);
         }
-        ok = tc_wait_warp(b_done, 0, 4 * kMxWait, dead);
+        ok = ops_wait_warp(b_done, 0, 4 * kMxWait, dead);
         tc_fence_after();
         const uint32_t quarter = (uint32_t)(warp & 3);
         const int row = 32 * (int)quarter + lane;
