@@ -352,7 +352,7 @@ us_status us_mx4_last_error(void);
  *   sequence sees: t < length; with causal, t <= i; with window > 0, t > i - window. A query that sees nothing gives 0. The new tokens'
  *   keys and values are read from the cache: append them first. Q and out: US_F16 or US_BF16 (both the same), rows (token, head),
  *   strides in elements; rows past cu_tokens[n_seqs] are left as they are. lse (N x n_heads fp32, or NULL): the logarithm
- *   of the sum of exp(scale q.k_t), -inf where nothing is seen. scratch: us_kv_attention_scratch bytes, 16-byte aligned,
+ *   of the sum of exp(scale q.k_t), -inf where nothing is seen. scratch: us_kv_attention_scratch bytes (-1: bad arguments), 16-byte aligned,
  *   for one call at a time; need not be cleared. Blocks wholly in front of every window may be gone (any table entry).
  * All three are enqueue-only on `stream` on the current device. N or n_seqs = 0: nothing is done.
  * Errors: INVALID_ARG, UNSUPPORTED, SCRATCH_TOO_SMALL, CUDA.
@@ -370,7 +370,7 @@ us_status us_kv_create(void* k_codes, void* v_codes, void* k_steps, void* v_step
 us_status us_kv_append(us_kv* h, const us_kv_seqs* seqs, int64_t N, const void* K, const void* V, int32_t type,
                        int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, void* stream);
 us_status us_kv_read(us_kv* h, const us_kv_seqs* seqs, int64_t tokens, void* K, void* V, int32_t type, void* stream);
-int64_t us_kv_attention_scratch(const us_kv* h, int64_t N, int32_t n_seqs, int32_t n_heads);
+int64_t us_kv_attention_scratch(const us_kv* h, const us_kv_seqs* seqs, int64_t N, int32_t n_heads);
 us_status us_kv_attention(us_kv* h, const us_kv_seqs* seqs, int64_t N, const void* Q, int32_t type, int32_t n_heads,
                           int64_t q_token_stride, int64_t q_head_stride, float scale, int32_t causal, int32_t window, void* out,
                           int64_t o_token_stride, int64_t o_head_stride, float* lse, void* scratch, int64_t scratch_bytes, void* stream);

@@ -91,7 +91,7 @@ _seqs = ctypes.POINTER(us_kv_seqs)
 _lib.us_kv_create.argtypes = [_vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, ctypes.POINTER(_vp)]
 _lib.us_kv_append.argtypes = [_vp, _seqs, _i64, _vp, _vp, _i32, _i64, _i64, _i64, _i64, _vp]
 _lib.us_kv_read.argtypes = [_vp, _seqs, _i64, _vp, _vp, _i32, _vp]
-_lib.us_kv_attention_scratch.argtypes = [_vp, _i64, _i32, _i32]
+_lib.us_kv_attention_scratch.argtypes = [_vp, _seqs, _i64, _i32]
 _lib.us_kv_attention_scratch.restype = _i64
 _lib.us_kv_attention.argtypes = [_vp, _seqs, _i64, _vp, _i32, _i32, _i64, _i64, ctypes.c_float, _i32, _i32, _vp, _i64, _i64, _vp, _vp, _i64, _vp]
 _lib.us_kv_last_error.argtypes = []

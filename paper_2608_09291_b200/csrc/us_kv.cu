@@ -107,16 +107,16 @@ struct AttendPlan {
     int64_t scratch;
 };
 template <int D, bool BF16>
-AttendPlan prompt_shape(int64_t N, int64_t S, int64_t G, int64_t Hkv, int sms)
+AttendPlan prompt_shape(int64_t N, int64_t S, int64_t G, int64_t Hkv, int64_t longest, int sms)
 {
     AttendPlan p = {};
     p.kernel = (const void*)us_kv_prompt_kernel<D, BF16>;
     p.join = (const void*)us_kv_prompt_join_kernel<D, BF16>;
     p.smem = PrShape<D>::kSmem;
     p.tiles = N * G / kPrRows + S;
-    // a tile's walk over the cache is split where the tiles would leave SMs idle
+    // a tile's walk over the cache is split where the tiles would leave SMs idle, in parts of at least four units
     const int64_t likely = std::max(S, (N * G + kPrRows - 1) / kPrRows) * Hkv;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(16, sms / likely));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({16, sms / likely, longest / (4 * kPrTile)}));
     p.scratch = p.splits > 1 ? p.tiles * Hkv * p.splits * PrShape<D>::kPart * 4 : 0;
     return p;
 }
@@ -128,7 +128,7 @@ AttendPlan attend_shape(int sms)
     p.kernel = (const void*)us_kv_attend_kernel<D, NT, BF16>;
     p.join = (const void*)us_kv_join_kernel<D, NT, BF16>;
     p.rows = S::R;
-    p.stages = std::min(S::kMaxStages, (112 * 1024 - 1024 - S::kMerge) / S::kStage);   // two CTAs an SM
+    p.stages = std::min(S::kMaxStages, (111 * 1024 - 1024 - S::kMerge) / S::kStage);   // two CTAs an SM
     p.smem = 1024 + p.stages * S::kStage + S::kMerge;
     p.ctas = 2 * sms;
     p.scratch = (int64_t)p.ctas * 2 * S::kPart * 4;
@@ -136,11 +136,11 @@ AttendPlan attend_shape(int sms)
 }
 template <int D, int NT>
 AttendPlan attend_shape(bool bf16, int sms) { return bf16 ? attend_shape<D, NT, true>(sms) : attend_shape<D, NT, false>(sms); }
-AttendPlan attend_plan(int D, bool bf16, int64_t N, int64_t S, int64_t G, int64_t Hkv, int sms)
+AttendPlan attend_plan(int D, bool bf16, int64_t N, int64_t S, int64_t G, int64_t Hkv, int64_t longest, int sms)
 {
     if (N * G > 32 * S) {
-        if (D == 128) return bf16 ? prompt_shape<128, true>(N, S, G, Hkv, sms) : prompt_shape<128, false>(N, S, G, Hkv, sms);
-        return bf16 ? prompt_shape<64, true>(N, S, G, Hkv, sms) : prompt_shape<64, false>(N, S, G, Hkv, sms);
+        if (D == 128) return bf16 ? prompt_shape<128, true>(N, S, G, Hkv, longest, sms) : prompt_shape<128, false>(N, S, G, Hkv, longest, sms);
+        return bf16 ? prompt_shape<64, true>(N, S, G, Hkv, longest, sms) : prompt_shape<64, false>(N, S, G, Hkv, longest, sms);
     }
     // rows a cache head has on average: 8 a tile are enough for them, or 16
     const bool few = N * G <= 8 * S;
@@ -228,11 +228,11 @@ us_status us_kv_read(us_kv* h, const us_kv_seqs* q, int64_t tokens, void* K, voi
     return cuda(ops_launch(k, grid, 256, 0, static_cast<cudaStream_t>(stream), args));
 }
 
-int64_t us_kv_attention_scratch(const us_kv* h, int64_t N, int32_t n_seqs, int32_t n_heads)
+int64_t us_kv_attention_scratch(const us_kv* h, const us_kv_seqs* q, int64_t N, int32_t n_heads)
 {
-    if (!h || N < 0 || n_seqs < 0 || n_heads < 1 || n_heads % h->pool.Hkv) return -1;
-    if (N == 0 || n_seqs == 0) return 0;
-    return attend_plan(h->pool.D, false, N, n_seqs, n_heads / h->pool.Hkv, h->pool.Hkv, ops_sms()).scratch;
+    if (!seqs_ok(h, q, N) || n_heads < 1 || n_heads % h->pool.Hkv) return -1;
+    if (N == 0 || q->n_seqs == 0) return 0;
+    return attend_plan(h->pool.D, false, N, q->n_seqs, n_heads / h->pool.Hkv, h->pool.Hkv, (int64_t)q->table_width * h->pool.T, ops_sms()).scratch;
 }
 
 us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* Q, int32_t type, int32_t n_heads, int64_t q_token_stride,
@@ -246,11 +246,11 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
         !aligned(lse, 4)) return US_ERR_INVALID_ARG;
     const int64_t G = n_heads / h->pool.Hkv;
     if (N * G >= (1ll << 31) - (1 << 16)) return US_ERR_UNSUPPORTED;
-    const AttendPlan pl = attend_plan(h->pool.D, type == US_BF16, N, q->n_seqs, G, h->pool.Hkv, ops_sms());
+    const AttendPlan pl = attend_plan(h->pool.D, type == US_BF16, N, q->n_seqs, G, h->pool.Hkv, (int64_t)q->table_width * h->pool.T, ops_sms());
     if (pl.scratch > 0 && (!scratch || !aligned(scratch, 16) || scratch_bytes < pl.scratch)) return US_ERR_SCRATCH_TOO_SMALL;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (pl.tiles > 0) {
-        const int64_t blocks = pl.tiles * h->pool.Hkv * std::max(pl.splits, kPrRows / 8);
+        const int64_t blocks = pl.tiles * h->pool.Hkv * std::max(pl.splits, h->pool.D / 16);
         if (blocks >= (1ll << 31)) return US_ERR_UNSUPPORTED;
         KvPrompt a = {};
         a.pool = h->pool;
@@ -273,7 +273,7 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
         cudaError_t e = ops_kernel_allow(pl.kernel);
         const int threads = PrShape<128>::kThreads;
         if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.splits)), threads, pl.smem, st, args);
-        if (e == cudaSuccess && pl.splits > 1) e = ops_launch(pl.join, dim3((unsigned)(pl.tiles * h->pool.Hkv * (kPrRows / 8))), 256, 0, st, args);
+        if (e == cudaSuccess && pl.splits > 1) e = ops_launch(pl.join, dim3((unsigned)(pl.tiles * h->pool.Hkv * (h->pool.D / 16))), kPrRows, 0, st, args);
         return cuda(e);
     }
     if (!maps(h)) return US_ERR_CUDA;
@@ -291,12 +291,13 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
     a.q_vec = rows_vec(Q, type, q_token_stride, q_head_stride);
     a.stages = pl.stages;
     a.ctas = pl.ctas;
+    while ((1 << a.log2_T) < h->pool.T) ++a.log2_T;
     us_status s = error_word(&a.pool.err);
     if (s != US_OK) return s;
     cudaError_t e = ops_kernel_allow(pl.kernel);
     void* args[] = {&a};
     if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)pl.ctas), 160, pl.smem, st, args);
-    if (e == cudaSuccess) e = ops_launch(pl.join, dim3((unsigned)pl.ctas, (unsigned)pl.rows), h->pool.D, 0, st, args);
+    if (e == cudaSuccess) e = ops_launch(pl.join, dim3((unsigned)pl.ctas), 256, 0, st, args);
     return cuda(e);
 }
 

@@ -230,12 +230,12 @@ __global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int
 //   * Codes become fp16 in registers, exactly (0x6400 | byte is 1024 + byte); a step is one number for 16 tokens, so K's is
 //     a factor of the scores and V's a factor of p. p is rounded to fp16 with 2^7 in front and V's step relative to the
 //     largest so far: what a row sums stays between 2^-24 and 2^15 of the largest term; sums are fp32.
-//   * m follows the true maximum only where it is 2^8 behind, so most tiles need no reduction over lanes and no rescaling.
-//   * All (sequence, row tile, head) items in a row, 64 tokens a unit: every CTA takes the same number of units, whatever the lengths.
+//   * m follows the true maximum only where it is 2^8 behind, so most units need no reduction over lanes and no rescaling.
+//   * All (sequence, row tile, head) items in a row, 128 tokens a unit: every CTA takes the same number of units, whatever the lengths.
 //     An item that is cut leaves its parts in scratch, and a second kernel joins them in the order of the CTAs.
-// A warp copies (TMA, swizzled so that the fragment loads meet no bank twice); four read, 16 tokens of a unit each, with
-// sums of their own that are joined at an item's end.
-constexpr int kKvTile = 64;
+// A warp copies (TMA, swizzled so that the fragment loads meet no bank twice); four read, 32 tokens of a unit each (two groups side by
+// side: their chains of products overlap), with sums of their own that are joined at an item's end.
+constexpr int kKvTile = 128;
 struct KvAttend {
     CUtensorMap k_map, v_map;
     KvPool pool;
@@ -252,6 +252,7 @@ struct KvAttend {
     int32_t q_vec;
     int32_t stages;
     int32_t ctas;
+    int32_t log2_T;
 };
 
 struct KvItem {
@@ -259,13 +260,13 @@ struct KvItem {
     int32_t rows;        // query rows of a head
     int32_t row_tiles;
     int32_t lo;          // first token that any of its queries sees
-    int32_t t_lo, tiles; // first unit of 64 tokens, units (1 if it sees nothing)
+    int32_t t_lo, tiles; // first unit of the cache, units (1 if it sees nothing)
 };
 template <int R>
-__device__ __forceinline__ KvItem kv_item(const KvAttend& a, int s, bool& wrong)
+__device__ __forceinline__ KvItem kv_item(const KvAttend& a, const KvSeq& seq)
 {
     KvItem r;
-    r.seq = kv_seq(a.seqs, a.pool, s, wrong);
+    r.seq = seq;
     r.rows = r.seq.n * a.G;
     r.row_tiles = (r.rows + R - 1) / R;
     r.lo = a.window > 0 ? max(0, r.seq.len - r.seq.n - a.window + 1) : 0;
@@ -273,62 +274,92 @@ __device__ __forceinline__ KvItem kv_item(const KvAttend& a, int s, bool& wrong)
     r.tiles = max(1, (r.seq.len + kKvTile - 1) / kKvTile - r.t_lo);
     return r;
 }
+template <int R>
+__device__ __forceinline__ KvItem kv_item(const KvAttend& a, int s)
+{
+    bool wrong;
+    return kv_item<R>(a, kv_seq(a.seqs, a.pool, s, wrong));
+}
 
-// Where a CTA's units begin and end.
+// The units of all items in a row, cut in equal shares: CTA c has [begin(c), begin(c + 1)).
+struct KvShares {
+    long long total, each;
+    int more;             // the first `more` CTAs have one unit more
+    __device__ __forceinline__ long long begin(int c) const { return each * c + min(c, more); }
+    __device__ __forceinline__ int owner(long long unit) const
+    {
+        const long long cut = (each + 1) * more;
+        return (int)(unit < cut ? unit / (each + 1) : more + (unit - cut) / each);
+    }
+};
+// Its own share, and where that begins. (All lanes of a warp; one trip to the lengths for up to 32 sequences.)
 struct KvRange {
-    long long total, u0, u1;
+    KvShares shares;
+    long long u0, u1;
     int s;                // sequence of unit u0
     long long in_seq;     // u0 from its first unit
+    KvItem item;          // of that sequence
 };
 template <int R>
-__device__ KvRange kv_range(const KvAttend& a, int cta, int lane)
+__device__ __forceinline__ KvRange kv_range(const KvAttend& a, int cta, int lane, bool report)
 {
     KvRange r;
-    r.total = 0;
+    r.shares.total = 0;
     bool any = false;
-    for (int base = 0; base < a.seqs.S; base += 32) {
-        long long c = 0;
+    KvSeq mine = {0, 0, 0};   // of the last sequences looked at
+    long long c = 0, sum = 0;
+    auto look = [&](int base) {
+        c = 0;
         if (base + lane < a.seqs.S) {
             bool wrong;
-            const KvItem it = kv_item<R>(a, base + lane, wrong);
+            mine = kv_seq(a.seqs, a.pool, base + lane, wrong);
             any |= wrong;
+            const KvItem it = kv_item<R>(a, mine);
             c = (long long)it.row_tiles * a.pool.Hkv * it.tiles;
         }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
-        r.total += c;
-    }
-    if (any) atomicExch(a.pool.err, kErrIndex);
-    r.u0 = r.total * cta / a.ctas;
-    r.u1 = r.total * (cta + 1) / a.ctas;
-    r.s = a.seqs.S;
-    r.in_seq = 0;
-    if (r.u0 >= r.u1) return r;
-    long long before = 0;
-    for (int base = 0; base < a.seqs.S; base += 32) {
-        long long c = 0;
-        if (base + lane < a.seqs.S) {
-            bool wrong;
-            const KvItem it = kv_item<R>(a, base + lane, wrong);
-            c = (long long)it.row_tiles * a.pool.Hkv * it.tiles;
-        }
-        long long sum = c;
+        sum = c;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const long long v = __shfl_up_sync(0xffffffffu, sum, o);
             if (lane >= o) sum += v;
         }
+    };
+    for (int base = 0; base < a.seqs.S; base += 32) {
+        look(base);
+        r.shares.total += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    if (any && report) atomicExch(a.pool.err, kErrIndex);
+    if (r.shares.total >> 32) {
+        r.shares.each = r.shares.total / a.ctas;
+    } else {
+        r.shares.each = (uint32_t)r.shares.total / (uint32_t)a.ctas;
+    }
+    r.shares.more = (int)(r.shares.total - r.shares.each * a.ctas);
+    r.u0 = r.shares.begin(cta);
+    r.u1 = r.shares.begin(cta + 1);
+    r.s = a.seqs.S;
+    r.in_seq = 0;
+    if (r.u0 >= r.u1) return r;
+    long long before = 0;
+    for (int base = 0; base < a.seqs.S; base += 32) {
+        if (a.seqs.S > 32) look(base);
         const uint32_t who = __ballot_sync(0xffffffffu, r.u0 < before + sum);
         if (who) {
             const int l = __ffs(who) - 1;
             r.s = base + l;
             r.in_seq = r.u0 - before - __shfl_sync(0xffffffffu, sum - c, l);
+            KvSeq q;
+            q.first = __shfl_sync(0xffffffffu, mine.first, l);
+            q.len = __shfl_sync(0xffffffffu, mine.len, l);
+            q.n = __shfl_sync(0xffffffffu, mine.n, l);
+            r.item = kv_item<R>(a, q);
             break;
         }
         before += __shfl_sync(0xffffffffu, sum, 31);
     }
     return r;
 }
+__device__ __forceinline__ int kv_div(long long a, int b) { return a >> 31 ? (int)(a / b) : (int)((uint32_t)a / (uint32_t)b); }
 
 __device__ __forceinline__ uint32_t f16_low(uint32_t w)    // bytes 0, 1 of (code ^ 0x80) -> two fp16
 {
@@ -357,6 +388,11 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ uint32_t half2_bits(float a, float b)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int32_t row, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
@@ -370,10 +406,18 @@ __device__ __forceinline__ bool bar_consumers(bool fail = false)
                  : "=r"(any) : "r"((uint32_t)fail) : "memory");
     return any != 0;
 }
-
-// fp16 pair of q, times a power of two
 template <bool BF16>
 __device__ __forceinline__ float q_at(const void* q, int64_t i) { return BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(q)[i]) : __half2float(static_cast<const __half*>(q)[i]); }
+template <bool BF16>
+__device__ __forceinline__ void o_put(void* out, int64_t i, float y)
+{
+    if (BF16) static_cast<__nv_bfloat16*>(out)[i] = __float2bfloat16_rn(y);
+    else static_cast<__half*>(out)[i] = __float2half_rn(y);
+}
+// log of the softmax's sum from a maximum (or -inf) and a sum that carries 2^7
+__device__ __forceinline__ float kv_lse(float m, float l) { return l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(l) - 7.f) * 0.69314718f; }
+// 2^(m - base) for a part with this maximum and sum; 0 for one that saw nothing
+__device__ __forceinline__ float kv_weight(float m, float l, float base) { return m == -INFINITY && l == 0.f ? 0.f : exp2_fast(m - base); }
 
 template <int D, int NT>
 struct KvShape {
@@ -381,8 +425,8 @@ struct KvShape {
     static constexpr int kHalf = kKvTile * D;                 // bytes of a stage's K (or V)
     static constexpr int kStage = 2 * kHalf;
     static constexpr int kPitch = D + 4;                      // floats of a row of the warps' sums
-    static constexpr int kMerge = 4 * R * kPitch * 4 + 4 * R * 2 * 4;
-    static constexpr int kMaxStages = 16;
+    static constexpr int kMerge = R * kPitch * 4 + 4 * R * 2 * 4;
+    static constexpr int kMaxStages = 8;
     static constexpr int kPart = R * (D + 2);                 // floats of a part
 };
 
@@ -393,11 +437,11 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
     constexpr int R = S::R, KS = D / 16, MT = D / 16;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * S::kMaxStages];
-    __shared__ float2 steps[S::kMaxStages][4];
+    __shared__ float2 steps[S::kMaxStages][8];   // of a unit's 16-token groups: K's (-1: not there), V's
     __shared__ uint32_t dead_word;
     uint8_t* ring = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    float* sums = reinterpret_cast<float*>(ring + (size_t)a.stages * S::kStage);   // [warp][row][pitch]
-    float2* stats = reinterpret_cast<float2*>(sums + 4 * R * S::kPitch);           // [warp][row] m, l
+    float* sums = reinterpret_cast<float*>(ring + (size_t)a.stages * S::kStage);   // [row][pitch]
+    float2* stats = reinterpret_cast<float2*>(sums + R * S::kPitch);               // [warp][row] m, l
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8u * S::kMaxStages;
     volatile uint32_t* dead = &dead_word;
@@ -405,20 +449,20 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
     if (threadIdx.x == 0) dead_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // The kernel that joins the parts may start once this one's CTAs are past the wait: it reads lengths and token counts before its own.
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const KvPool& p = a.pool;
-    const KvRange range = kv_range<R>(a, blockIdx.x, lane);
+    const KvRange range = kv_range<R>(a, blockIdx.x, lane, warp == 0);
     long long left = range.u1 - range.u0;
-    bool ok = true, wrong;
+    bool ok = true;
     int stage = 0;
     uint32_t par = 0;
     int s = range.s;
-    KvItem it;
+    KvItem it = range.item;
     int item = 0, tile = 0;   // item of the sequence (row tile * Hkv + head), unit of the item
     if (left > 0) {
-        it = kv_item<R>(a, s, wrong);
-        item = (int)(range.in_seq / it.tiles);
+        item = kv_div(range.in_seq, it.tiles);
         tile = (int)(range.in_seq - (long long)item * it.tiles);
     }
     auto next_seq = [&]() {   // (the units of this CTA end before the sequences do)
@@ -426,7 +470,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
         item = 0;
         do {
             if (++s >= a.seqs.S) { left = 0; return; }
-            it = kv_item<R>(a, s, wrong);
+            it = kv_item<R>(a, s);
         } while (it.rows == 0);
     };
     if (warp == 4) {
@@ -443,7 +487,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                 int32_t blk = -1;
                 float sk = -1.f, sv = 0.f;
                 if (lane < nb * (n - i0) && t < it.seq.len && t + box > it.lo) {   // (blocks in front of every window may be gone)
-                    blk = __ldcg(row + t / p.T);
+                    blk = __ldcg(row + (t >> a.log2_T));
                     if (blk < 0 || blk >= p.blocks) {
                         atomicExch(p.err, kErrIndex);
                         blk = -1;
@@ -456,17 +500,17 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                 for (int i = 0; i < m; ++i) {
                     ok = ops_wait_warp(b_empty + 8u * stage, par ^ 1u, kMxWait, dead);
                     if (!ok) break;
-                    // the steps of the unit's four 16-token groups
-                    const int from = i * nb + (lane & 3) * 16 / box;
+                    // the steps of the unit's eight 16-token groups
+                    const int from = i * nb + (lane & 7) * 16 / box;
                     const float gk = __shfl_sync(0xffffffffu, sk, from), gv = __shfl_sync(0xffffffffu, sv, from);
-                    if (lane < 4) steps[stage][lane] = make_float2(gk, gv);
+                    if (lane < 8) steps[stage][lane] = make_float2(gk, gv);
                     const uint32_t valid = __popc(__ballot_sync(0xffffffffu, blk >= 0 && lane / nb == i));
                     const uint32_t bar = b_full + 8u * stage;
                     __syncwarp();
                     if (lane == 0) mbar_expect_tx(bar, valid * 2u * (uint32_t)(box * D));
                     __syncwarp();
                     if (blk >= 0 && lane / nb == i) {
-                        const int32_t y = (blk * p.Hkv + h) * p.T + t % p.T;
+                        const int32_t y = (blk * p.Hkv + h) * p.T + (t & (p.T - 1));
                         const uint32_t dst = smem_u32(ring + (size_t)stage * S::kStage) + (uint32_t)((lane - i * nb) * box * D);
                         tma_rows(dst, &a.k_map, y, bar);
                         tma_rows(dst + S::kHalf, &a.v_map, y, bar);
@@ -486,8 +530,6 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
         __syncwarp();
     } else {
         const int g = lane >> 2, t = lane & 3;
-        // Shared-memory offsets of the lane's fragments in a stage (see the layout of TMA's swizzles: 128 bytes for D = 128, 64 for 64)
-        const int kr = 16 * warp + g;
         while (left > 0 && ok) {
             const int n = (int)min((long long)(it.tiles - tile), left);
             const int h = item % p.Hkv, row0 = item / p.Hkv * R;
@@ -539,9 +581,8 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                 }
 #pragma unroll
                 for (int j = 0; j < KS; ++j) {
-                    const __half2 x = __floats2half2_rn(v[4 * j] * mul, v[4 * j + 1] * mul), y = __floats2half2_rn(v[4 * j + 2] * mul, v[4 * j + 3] * mul);
-                    qf[nt][j][0] = *reinterpret_cast<const uint32_t*>(&x);
-                    qf[nt][j][1] = *reinterpret_cast<const uint32_t*>(&y);
+                    qf[nt][j][0] = half2_bits(v[4 * j] * mul, v[4 * j + 1] * mul);
+                    qf[nt][j][1] = half2_bits(v[4 * j + 2] * mul, v[4 * j + 3] * mul);
                 }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -553,6 +594,15 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                     lo[nt][c] = real && a.window > 0 ? pos - a.window + 1 : -0x7FFFFFFF;
                 }
             }
+            // tokens that no row sees are in front of it.lo or from the last row's bound on; all rows see [all_lo, all_hi)
+            int all_lo = -0x7FFFFFFF, all_hi = 0x7FFFFFFF;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) { all_lo = max(all_lo, lo[nt][c]); all_hi = min(all_hi, hi[nt][c]); }
+            all_lo = __reduce_max_sync(0xffffffffu, all_lo);
+            all_hi = __reduce_min_sync(0xffffffffu, all_hi);
+            const int last_hi = a.causal ? pos0 + (min(row0 + R, it.rows) - 1) / a.G + 1 : it.seq.len;
             float m[NT][2], l[NT][2], o[MT][NT][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -565,64 +615,65 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
 #pragma unroll
                     for (int c = 0; c < 4; ++c) o[i][nt][c] = 0.f;
             float ref = 0.f;   // V's largest step so far
+            int tok0 = (it.t_lo + tile) * kKvTile + 32 * warp;
 #pragma unroll 1
-            for (int i = 0; i < n; ++i) {
+            for (int i = 0; i < n; ++i, tok0 += kKvTile) {
                 ok = ops_wait_warp(b_full + 8u * stage, par, kMxWait, dead);
                 if (!ok) break;
-                const float2 st = steps[stage][warp];
-                const int tok0 = (it.t_lo + tile + i) * kKvTile + 16 * warp;
-                bool see = false;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) see |= row0 + 8 * nt + 2 * t + c < it.rows && lo[nt][c] < tok0 + 16 && hi[nt][c] > tok0;
-                if (st.x < 0.f) see = false;   // (a block that was not fetched)
-                if (__any_sync(0xffffffffu, see)) {
+                const float2 st0 = steps[stage][2 * warp], st1 = steps[stage][2 * warp + 1];
+                const float stk[2] = {st0.x, st1.x}, stv[2] = {st0.y, st1.y};
+                if (tok0 + 32 > it.lo && tok0 < last_hi && !(st0.x < 0.f && st1.x < 0.f)) {
+                    const bool edge = tok0 < all_lo || tok0 + 32 > all_hi || st0.x < 0.f || st1.x < 0.f;
                     const uint32_t kb = smem_u32(ring + (size_t)stage * S::kStage), vb = kb + S::kHalf;
-                    float sc[NT][4];
+                    float sc[2][NT][4];
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int b = 0; b < 2; ++b)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) sc[nt][c] = 0.f;
-                    // scores: 16 tokens x 8 NT rows
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) sc[b][nt][c] = 0.f;
+                    // scores: two times 16 tokens x 8 NT rows
 #pragma unroll
                     for (int c = 0; c < D / 64; ++c) {
-                        const int chunk = D == 128 ? ((2 * t + c) ^ (kr & 7)) : (t ^ ((kr >> 1) & 3));
-                        const uint4 x = lds128(kb + (uint32_t)(kr * D + 16 * chunk)), y = lds128(kb + (uint32_t)((kr + 8) * D + 16 * chunk));
-                        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+                        uint32_t xs[2][4], ys[2][4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint32_t xw = xs[j] ^ 0x80808080u, yw = ys[j] ^ 0x80808080u;
-                            const uint32_t a0 = f16_low(xw), a1 = f16_low(yw), a2 = f16_high(xw), a3 = f16_high(yw);
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma_f16(sc[nt], a0, a1, a2, a3, qf[nt][4 * c + j][0], qf[nt][4 * c + j][1]);
+                        for (int b = 0; b < 2; ++b) {
+                            const int kr = 32 * warp + 16 * b + g, chunk = D == 128 ? ((2 * t + c) ^ (kr & 7)) : (t ^ ((kr >> 1) & 3));
+                            const uint4 x = lds128(kb + (uint32_t)(kr * D + 16 * chunk)), y = lds128(kb + (uint32_t)((kr + 8) * D + 16 * chunk));
+                            xs[b][0] = x.x; xs[b][1] = x.y; xs[b][2] = x.z; xs[b][3] = x.w;
+                            ys[b][0] = y.x; ys[b][1] = y.y; ys[b][2] = y.z; ys[b][3] = y.w;
                         }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int b = 0; b < 2; ++b) {
+                                const uint32_t xw = xs[b][j] ^ 0x80808080u, yw = ys[b][j] ^ 0x80808080u;
+                                const uint32_t a0 = f16_low(xw), a1 = f16_low(yw), a2 = f16_high(xw), a3 = f16_high(yw);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) mma_f16(sc[b][nt], a0, a1, a2, a3, qf[nt][4 * c + j][0], qf[nt][4 * c + j][1]);
+                            }
                     }
-                    bool edge = false;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) edge |= lo[nt][c] > tok0 || hi[nt][c] < tok0 + 16;
-                    edge = __any_sync(0xffffffffu, edge);
                     bool behind = false;
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int b = 0; b < 2; ++b)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            float v = sc[nt][c] * (f[nt][c & 1] * st.x);
-                            if (edge) {
-                                const int tk = tok0 + g + 8 * (c >> 1);
-                                if (tk < lo[nt][c & 1] || tk >= hi[nt][c & 1]) v = -INFINITY;
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                float v = sc[b][nt][c] * (f[nt][c & 1] * stk[b]);
+                                if (edge) {
+                                    const int tk = tok0 + 16 * b + g + 8 * (c >> 1);
+                                    if (tk < lo[nt][c & 1] || tk >= hi[nt][c & 1] || stk[b] < 0.f) v = -INFINITY;
+                                }
+                                sc[b][nt][c] = v;
+                                behind |= v > m[nt][c & 1] + 8.f;
                             }
-                            sc[nt][c] = v;
-                            behind |= v > m[nt][c & 1] + 8.f;
-                        }
                     if (__any_sync(0xffffffffu, behind)) {
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int c = 0; c < 2; ++c) {
-                                float x = fmaxf(sc[nt][c], sc[nt][c + 2]);
+                                float x = fmaxf(fmaxf(sc[0][nt][c], sc[0][nt][c + 2]), fmaxf(sc[1][nt][c], sc[1][nt][c + 2]));
                                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
@@ -634,9 +685,10 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                                 for (int k = 0; k < MT; ++k) { o[k][nt][c] *= alpha; o[k][nt][c + 2] *= alpha; }
                             }
                     }
-                    if (st.y > ref) {
-                        const float b = ref / st.y;
-                        ref = st.y;
+                    const float top = fmaxf(stk[0] < 0.f ? 0.f : stv[0], stk[1] < 0.f ? 0.f : stv[1]);
+                    if (top > ref) {
+                        const float b = ref / top;
+                        ref = top;
 #pragma unroll
                         for (int k = 0; k < MT; ++k)
 #pragma unroll
@@ -644,44 +696,49 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
 #pragma unroll
                                 for (int c = 0; c < 4; ++c) o[k][nt][c] *= b;
                     }
-                    const float rel = st.y == ref ? 1.f : __fdiv_rn(st.y, ref);   // (NaN: NaN)
-                    uint32_t pf[NT][2];
+                    uint32_t pf[2][NT][2];
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        float e[4];
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            e[c] = exp2_fast(sc[nt][c] - (m[nt][c & 1] == -INFINITY ? 0.f : m[nt][c & 1] - 7.f));
-                            l[nt][c & 1] += e[c];
-                        }
-                        const __half2 x = __floats2half2_rn(e[0] * rel, e[1] * rel), y = __floats2half2_rn(e[2] * rel, e[3] * rel);
-                        pf[nt][0] = transpose8(*reinterpret_cast<const uint32_t*>(&x));
-                        pf[nt][1] = transpose8(*reinterpret_cast<const uint32_t*>(&y));
-                    }
-                    // sums: 16 of D x 8 NT rows at a time; a lane holds the same D columns of its four tokens
-                    const int v0 = 16 * warp + 2 * t;
-                    uint32_t w[4][D / 32];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int r = v0 + (q & 1) + 8 * (q >> 1);
-                        if (D == 128) {
-                            const uint4 x = lds128(vb + (uint32_t)(r * D + 16 * (g ^ (r & 7))));
-                            w[q][0] = x.x; w[q][1] = x.y; w[q][D / 32 - 2] = x.z; w[q][D / 32 - 1] = x.w;
-                        } else {
-                            const uint2 x = lds64(vb + (uint32_t)(r * D + 16 * ((g >> 1) ^ ((r >> 1) & 3)) + 8 * (g & 1)));
-                            w[q][0] = x.x; w[q][1] = x.y;
-                        }
-                    }
-#pragma unroll
-                    for (int k = 0; k < D / 32; ++k) {
-                        const uint32_t x0 = prmt(w[0][k], w[1][k], 0x5140u) ^ 0x80808080u, x1 = prmt(w[0][k], w[1][k], 0x7362u) ^ 0x80808080u;
-                        const uint32_t y0 = prmt(w[2][k], w[3][k], 0x5140u) ^ 0x80808080u, y1 = prmt(w[2][k], w[3][k], 0x7362u) ^ 0x80808080u;
-                        const uint32_t a0 = f16_low(x0), a1 = f16_high(x0), a2 = f16_low(y0), a3 = f16_high(y0);
-                        const uint32_t b0 = f16_low(x1), b1 = f16_high(x1), b2 = f16_low(y1), b3 = f16_high(y1);
+                    for (int b = 0; b < 2; ++b) {
+                        const float rel = stk[b] < 0.f ? 0.f : stv[b] == ref ? 1.f : __fdiv_rn(stv[b], ref);   // (NaN: NaN)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            mma_f16(o[2 * k][nt], a0, a1, a2, a3, pf[nt][0], pf[nt][1]);
-                            mma_f16(o[2 * k + 1][nt], b0, b1, b2, b3, pf[nt][0], pf[nt][1]);
+                            float e[4];
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                e[c] = exp2_fast(sc[b][nt][c] - (m[nt][c & 1] == -INFINITY ? 0.f : m[nt][c & 1] - 7.f));
+                                l[nt][c & 1] += e[c];
+                            }
+                            pf[b][nt][0] = transpose8(half2_bits(e[0] * rel, e[1] * rel));
+                            pf[b][nt][1] = transpose8(half2_bits(e[2] * rel, e[3] * rel));
+                        }
+                    }
+                    // sums: 16 of D x 8 NT rows at a time; a lane holds the same D columns of its four tokens
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int v0 = 32 * warp + 16 * b + 2 * t;
+                        uint32_t w[4][D / 32];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int r = v0 + (q & 1) + 8 * (q >> 1);
+                            if (D == 128) {
+                                const uint4 x = lds128(vb + (uint32_t)(r * D + 16 * (g ^ (r & 7))));
+                                w[q][0] = x.x; w[q][1] = x.y; w[q][D / 32 - 2] = x.z; w[q][D / 32 - 1] = x.w;
+                            } else {
+                                const uint2 x = lds64(vb + (uint32_t)(r * D + 16 * ((g >> 1) ^ ((r >> 1) & 3)) + 8 * (g & 1)));
+                                w[q][0] = x.x; w[q][1] = x.y;
+                            }
+                        }
+#pragma unroll
+                        for (int k = 0; k < D / 32; ++k) {
+                            const uint32_t x0 = prmt(w[0][k], w[1][k], 0x5140u) ^ 0x80808080u, x1 = prmt(w[0][k], w[1][k], 0x7362u) ^ 0x80808080u;
+                            const uint32_t y0 = prmt(w[2][k], w[3][k], 0x5140u) ^ 0x80808080u, y1 = prmt(w[2][k], w[3][k], 0x7362u) ^ 0x80808080u;
+                            const uint32_t a0 = f16_low(x0), a1 = f16_high(x0), a2 = f16_low(y0), a3 = f16_high(y0);
+                            const uint32_t b0 = f16_low(x1), b1 = f16_high(x1), b2 = f16_low(y1), b3 = f16_high(y1);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_f16(o[2 * k][nt], a0, a1, a2, a3, pf[b][nt][0], pf[b][nt][1]);
+                                mma_f16(o[2 * k + 1][nt], b0, b1, b2, b3, pf[b][nt][0], pf[b][nt][1]);
+                            }
                         }
                     }
                 }
@@ -700,40 +757,57 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                     x += __shfl_xor_sync(0xffffffffu, x, 16);
                     if (g == 0) stats[warp * R + 8 * nt + 2 * t + c] = make_float2(m[nt][c], x);
                 }
-            // (place (2 j + e) * 8 + g of a row holds d = (D / 8) g + 2 j + e: a warp's 32 stores meet 32 banks)
-#pragma unroll
-            for (int k = 0; k < MT; ++k)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        sums[(warp * R + 8 * nt + 2 * t + (c & 1)) * S::kPitch + (2 * k + (c >> 1)) * 8 + g] = o[k][nt][c] * ref;
             if (bar_consumers(!ok)) {   // (a warp gave up: all four do, at the same place)
                 ok = false;
                 break;
+            }
+            // each in turn adds what it has, relative to the largest maximum; place (2 j + e) * 8 + g of a row holds
+            // d = (D / 8) g + 2 j + e, so that a warp's 32 accesses meet 32 banks
+            float w[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int r = 8 * nt + 2 * t + c;
+                    float big = -INFINITY;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) big = fmaxf(big, stats[k * R + r].x);
+                    const float2 own = stats[warp * R + r];
+                    w[nt][c] = kv_weight(own.x, own.y, big == -INFINITY ? 0.f : big);
+                }
+#pragma unroll 1
+            for (int turn = 0; turn < 4; ++turn) {
+                if (warp == turn)
+#pragma unroll
+                    for (int k = 0; k < MT; ++k)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                float* at = sums + (8 * nt + 2 * t + (c & 1)) * S::kPitch + (2 * k + (c >> 1)) * 8 + g;
+                                const float x = w[nt][c & 1] == 0.f ? 0.f : o[k][nt][c] * ref * w[nt][c & 1];
+                                *at = turn ? *at + x : x;
+                            }
+                bar_consumers();
             }
             const bool whole = n == it.tiles;
             float* part = a.part + ((int64_t)blockIdx.x * 2 + (tile == 0 ? 1 : 0)) * S::kPart;   // 1: the item begins here
             const int rows = min(R, it.rows - row0);
             for (int i = threadIdx.x; i < rows * D; i += 128) {
                 const int r = i / D, d = i - r * D;
-                float big = -INFINITY, sum = 0.f, acc = 0.f;
+                float big = -INFINITY, sum = 0.f;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) big = fmaxf(big, stats[w * R + r].x);
+                for (int k = 0; k < 4; ++k) big = fmaxf(big, stats[k * R + r].x);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const float2 x = stats[w * R + r];
-                    const float e = x.x == -INFINITY && x.y == 0.f ? 0.f : exp2_fast(x.x - (big == -INFINITY ? 0.f : big));
-                    sum += e * x.y;
-                    acc += e == 0.f ? 0.f : e * sums[(w * R + r) * S::kPitch + (d % (D / 8)) * 8 + d / (D / 8)];
+                for (int k = 0; k < 4; ++k) {
+                    const float2 x = stats[k * R + r];
+                    sum += kv_weight(x.x, x.y, big == -INFINITY ? 0.f : big) * x.y;
                 }
+                const float acc = sums[r * S::kPitch + (d % (D / 8)) * 8 + d / (D / 8)];
                 if (whole) {
                     const int tok = (row0 + r) / a.G, qh = h * a.G + (row0 + r) - tok * a.G;
-                    const float y = sum == 0.f ? 0.f : acc / sum;
-                    const int64_t at = (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + d;
-                    if (BF16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(y);
-                    else static_cast<__half*>(a.out)[at] = __float2half_rn(y);
-                    if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = sum == 0.f ? -INFINITY : (big + log2f(sum) - 7.f) * 0.69314718f;
+                    o_put<BF16>(a.out, (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + d, sum == 0.f ? 0.f : acc / sum);
+                    if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(big, sum);
                 } else {
                     part[r * D + d] = acc;
                     if (d == 0) {
@@ -756,70 +830,68 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
     __syncthreads();
 }
 
-// Joins the parts of the item that begins in CTA blockIdx.x of the kernel before and ends in a later one; row blockIdx.y of its tile.
+// Joins the parts of the item that begins in CTA blockIdx.x of the kernel before and ends in a later one. Which that is depends on the
+// lengths alone: it is found out while that kernel runs. A warp a row, D / 32 columns a lane.
 template <int D, int NT, bool BF16>
-__global__ void __launch_bounds__(D) us_kv_join_kernel(const __grid_constant__ KvAttend a)
+__global__ void __launch_bounds__(256) us_kv_join_kernel(const __grid_constant__ KvAttend a)
 {
     using S = KvShape<D, NT>;
-    constexpr int R = S::R;
+    constexpr int R = S::R, C = D / 32;
+    const int lane = threadIdx.x & 31;
+    const KvRange range = kv_range<R>(a, blockIdx.x, lane, false);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lane = threadIdx.x & 31, d = threadIdx.x, r = blockIdx.y;
-    const KvRange range = kv_range<R>(a, blockIdx.x, lane);
     if (range.u0 >= range.u1) return;
     // the item that the CTA's last unit belongs to
     int s = range.s;
-    bool wrong;
-    KvItem it = kv_item<R>(a, s, wrong);
+    KvItem it = range.item;
     long long start = range.u0 - range.in_seq;   // first unit of the sequence
     long long units = (long long)it.row_tiles * a.pool.Hkv * it.tiles;
     while (start + units <= range.u1 - 1) {
         start += units;
         if (++s >= a.seqs.S) return;
-        it = kv_item<R>(a, s, wrong);
+        it = kv_item<R>(a, s);
         units = (long long)it.row_tiles * a.pool.Hkv * it.tiles;
     }
-    const int item = (int)((range.u1 - 1 - start) / it.tiles);
+    const int item = kv_div(range.u1 - 1 - start, it.tiles);
     const long long first = start + (long long)item * it.tiles, end = first + it.tiles;
     if (first < range.u0 || end <= range.u1) return;   // begins in an earlier CTA, or is whole
     const int h = item % a.pool.Hkv, row0 = item / a.pool.Hkv * R;
-    if (row0 + r >= it.rows) return;
-    int last = blockIdx.x;   // the CTA of the item's last unit
-    while (range.total * (last + 1) / a.ctas < end) ++last;
-    float big = -INFINITY, sum = 0.f, acc = 0.f;
-    for (int c0 = blockIdx.x; c0 <= last; c0 += 8) {
-        float x[8], m[8], l[8], top = big;
+    const int last = range.shares.owner(end - 1);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int r = threadIdx.x >> 5; r < R && row0 + r < it.rows; r += 8) {
+        // the largest maximum first: a lane a part
+        float big = -INFINITY;
+        for (int c = blockIdx.x + lane; c <= last; c += 32)
+            big = fmaxf(big, __ldcg(a.part + ((int64_t)c * 2 + (c == (int)blockIdx.x ? 1 : 0)) * S::kPart + R * D + 2 * r));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            m[i] = -INFINITY; l[i] = 0.f; x[i] = 0.f;
-            const int c = c0 + i;
-            if (c <= last && range.total * c / a.ctas < range.total * (c + 1) / a.ctas) {
-                const float* part = a.part + ((int64_t)c * 2 + (c == (int)blockIdx.x ? 1 : 0)) * S::kPart;
-                x[i] = __ldcg(part + r * D + d);
-                m[i] = __ldcg(part + R * D + 2 * r);
-                l[i] = __ldcg(part + R * D + 2 * r + 1);
+        for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+        const float base = big == -INFINITY ? 0.f : big;
+        float sum = 0.f, acc[C];
+#pragma unroll
+        for (int i = 0; i < C; ++i) acc[i] = 0.f;
+#pragma unroll 4
+        for (int c = blockIdx.x; c <= last; ++c) {
+            const float* part = a.part + ((int64_t)c * 2 + (c == (int)blockIdx.x ? 1 : 0)) * S::kPart;
+            const float2 x = __ldcg(reinterpret_cast<const float2*>(part + R * D + 2 * r));
+            float v[C];
+            if (C == 4) {
+                const float4 u = __ldcg(reinterpret_cast<const float4*>(part + r * D + 4 * lane));
+                v[0] = u.x; v[1] = u.y; v[C - 2] = u.z; v[C - 1] = u.w;
+            } else {
+                const float2 u = __ldcg(reinterpret_cast<const float2*>(part + r * D + 2 * lane));
+                v[0] = u.x; v[1] = u.y;
             }
-        }
+            const float e = kv_weight(x.x, x.y, base);
+            sum += e * x.y;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, m[i]);
-        const float base = top == -INFINITY ? 0.f : top;
-        const float keep = big == -INFINITY ? 1.f : exp2_fast(big - base);   // (nothing is there yet, or NaN that has to stay)
-        sum *= keep;
-        acc *= keep;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float e = m[i] == -INFINITY && l[i] == 0.f ? 0.f : exp2_fast(m[i] - base);
-            sum += e * l[i];
-            acc += e == 0.f ? 0.f : e * x[i];
+            for (int i = 0; i < C; ++i) acc[i] += e == 0.f ? 0.f : e * v[i];
         }
-        big = top;
+        const int tok = (row0 + r) / a.G, qh = h * a.G + (row0 + r) - tok * a.G;
+        const int64_t at = (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + C * lane;
+#pragma unroll
+        for (int i = 0; i < C; ++i) o_put<BF16>(a.out, at + i, sum == 0.f ? 0.f : acc[i] / sum);
+        if (a.lse && lane == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(big, sum);
     }
-    const int tok = (row0 + r) / a.G, qh = h * a.G + (row0 + r) - tok * a.G;
-    const float y = sum == 0.f ? 0.f : acc / sum;
-    const int64_t at = (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + d;
-    if (BF16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(y);
-    else static_cast<__half*>(a.out)[at] = __float2half_rn(y);
-    if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = sum == 0.f ? -INFINITY : (big + log2f(sum) - 7.f) * 0.69314718f;
 }
 
 }  // namespace us

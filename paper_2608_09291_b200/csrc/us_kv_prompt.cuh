@@ -25,7 +25,7 @@ struct KvPrompt {
     void* out;
     int64_t o_token, o_head;
     float* lse;
-    float* part;             // [row tile][head][split]: 256 x D sums, then 256 x {m, l}
+    float* part;             // [row tile][head][split]: sums [D / 4][256 rows][4], then m[256], l[256]
     float scale2;            // |scale| log2(e); the sign goes to the queries
     int32_t negative;
     int32_t Hq, G;
@@ -105,43 +105,39 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ uint32_t half2_bits(float a, float b)
-{
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 // The sequence and row tile of row tile `index` of the batch; row tiles of a sequence with the latest tokens (that see most) first.
 // rows: query rows of a head in the tile.
 struct PrItem {
     KvSeq seq;
     int s, row0, rows;
 };
-__device__ __forceinline__ bool pr_item(const KvPrompt& a, int64_t index, int lane, PrItem& it, bool report)
+__device__ __forceinline__ bool pr_item(const KvPrompt& a, uint32_t index, int lane, PrItem& it, bool report)
 {
-    int64_t before = 0;
+    uint32_t before = 0;
     bool any = false, found = false;
     for (int base = 0; base < a.seqs.S; base += 32) {
-        int64_t cnt = 0;
+        uint32_t cnt = 0;
+        KvSeq mine = {0, 0, 0};
         if (base + lane < a.seqs.S) {
             bool wrong;
-            const KvSeq q = kv_seq(a.seqs, a.pool, base + lane, wrong);
+            mine = kv_seq(a.seqs, a.pool, base + lane, wrong);
             any |= wrong;
-            cnt = ((int64_t)q.n * a.G + kPrRows - 1) / kPrRows;
+            cnt = ((uint32_t)mine.n * (uint32_t)a.G + kPrRows - 1) / kPrRows;
         }
-        int64_t sum = cnt;
+        uint32_t sum = cnt;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t v = __shfl_up_sync(0xffffffffu, sum, o);
+            const uint32_t v = __shfl_up_sync(0xffffffffu, sum, o);
             if (lane >= o) sum += v;
         }
         const uint32_t who = __ballot_sync(0xffffffffu, index >= before + sum - cnt && index < before + sum);
         if (who) {
             const int l = __ffs(who) - 1;
             it.s = base + l;
-            const int64_t tiles = __shfl_sync(0xffffffffu, cnt, l), j = index - before - __shfl_sync(0xffffffffu, sum - cnt, l);
-            bool wrong;
-            it.seq = kv_seq(a.seqs, a.pool, it.s, wrong);
+            const uint32_t tiles = __shfl_sync(0xffffffffu, cnt, l), j = index - before - __shfl_sync(0xffffffffu, sum - cnt, l);
+            it.seq.first = __shfl_sync(0xffffffffu, mine.first, l);
+            it.seq.len = __shfl_sync(0xffffffffu, mine.len, l);
+            it.seq.n = __shfl_sync(0xffffffffu, mine.n, l);
             it.row0 = (int)((tiles - 1 - j) * kPrRows);
             it.rows = min(kPrRows, it.seq.n * a.G - it.row0);
             found = true;
@@ -197,12 +193,13 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (after the allocation: see us_mx4.cuh)
+    // After the allocation (see us_mx4.cuh), and after the wait: the kernel that joins the parts reads lengths and token counts before its own.
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t tm = *(volatile uint32_t*)misc;
     const KvPool& p = a.pool;
     const int split = (int)(blockIdx.x % a.splits), h = (int)(blockIdx.x / a.splits) % p.Hkv;
-    const int64_t index = blockIdx.x / ((unsigned)a.splits * p.Hkv);
+    const uint32_t index = blockIdx.x / ((unsigned)a.splits * p.Hkv);
     PrItem it;
     const bool have = pr_item(a, index, lane, it, threadIdx.x < 32);
     bool ok = true;
@@ -210,8 +207,9 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
     if (have) {
         pr_units(a, it, u0, u1);
         const int n = u1 - u0;
-        u1 = u0 + (int)((int64_t)n * (split + 1) / a.splits);
-        u0 = u0 + (int)((int64_t)n * split / a.splits);
+        const int each = n / a.splits, more = n - each * a.splits;   // the first `more` parts have one unit more
+        u0 += each * split + min(split, more);
+        u1 = u0 + each + (split < more ? 1 : 0);
     }
     const int n = u1 - u0, nq = have && it.rows > 128 ? 2 : 1;
     // Registers of a thread: 128 at launch, 16 warps; 2 x 176 + 96 + 64 = 4 x 128.
@@ -403,16 +401,16 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
         }
         if (qi < nq && ok) {
             const float inv = l == 0.f ? 0.f : ref / l;
-            float* part = a.part + ((index * p.Hkv + h) * a.splits + split) * S::kPart;
+            float* part = a.part + (((int64_t)index * p.Hkv + h) * a.splits + split) * S::kPart;
             if (real && a.splits > 1) {
-                part[kPrRows * D + 2 * local] = m;
-                part[kPrRows * D + 2 * local + 1] = l;
+                part[kPrRows * D + local] = m;
+                part[kPrRows * D + kPrRows + local] = l;
             } else if (real && a.lse) {
-                a.lse[(it.seq.first + tok) * a.Hq + qh] = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(l) - 7.f) * 0.69314718f;
+                a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(m, l);
             }
             uint16_t* dst = static_cast<uint16_t*>(a.out) + (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head;
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
+            for (int c = 0; c < (n == 0 && a.splits > 1 ? 0 : D / 32); ++c) {   // (a part without units has no sums)
                 uint32_t x[32];
                 if (n > 0) {
                     tc_ld32(t_o + 32u * c, x);
@@ -426,7 +424,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                 if (a.splits > 1) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        *reinterpret_cast<float4*>(part + local * D + 32 * c + 4 * i) =
+                        *reinterpret_cast<float4*>(part + ((8 * c + i) * kPrRows + local) * 4) =
                             make_float4(__uint_as_float(x[4 * i]) * ref, __uint_as_float(x[4 * i + 1]) * ref, __uint_as_float(x[4 * i + 2]) * ref, __uint_as_float(x[4 * i + 3]) * ref);
                     continue;
                 }
@@ -620,60 +618,50 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
     if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
 }
 
-// Joins the parts of a row tile that was split over the cache's length: block (row tile, head, 8 rows), a warp a row.
+// Joins the parts of a row tile that was split over the cache's length: a thread a row, 16 of D a block.
 template <int D, bool BF16>
-__global__ void __launch_bounds__(256) us_kv_prompt_join_kernel(const __grid_constant__ KvPrompt a)
+__global__ void __launch_bounds__(kPrRows) us_kv_prompt_join_kernel(const __grid_constant__ KvPrompt a)
 {
     using S = PrShape<D>;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lane = threadIdx.x & 31, local = 8 * (int)(blockIdx.x % (kPrRows / 8)) + ((int)threadIdx.x >> 5);
-    const int64_t u = blockIdx.x / (kPrRows / 8), index = u / a.pool.Hkv;
+    const int lane = threadIdx.x & 31, local = threadIdx.x, c0 = 4 * (int)(blockIdx.x % (D / 16));
+    const uint32_t u = blockIdx.x / (D / 16), index = u / (uint32_t)a.pool.Hkv;
     const int h = (int)(u - index * a.pool.Hkv);
     PrItem it;
-    if (!pr_item(a, index, lane, it, false) || local >= it.rows) return;
-    const float* part = a.part + u * a.splits * S::kPart;
-    float m[2], l[2];   // of parts lane and lane + 32
+    const bool have = pr_item(a, index, lane, it, false);   // (lengths and token counts: complete before the kernel that left the parts went past its wait)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!have || local >= it.rows) return;
+    const float* part = a.part + (int64_t)u * a.splits * S::kPart;
     float big = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        m[i] = -INFINITY; l[i] = 0.f;
-        if (lane + 32 * i < a.splits) {
-            m[i] = __ldcg(part + (lane + 32 * i) * S::kPart + kPrRows * D + 2 * local);
-            l[i] = __ldcg(part + (lane + 32 * i) * S::kPart + kPrRows * D + 2 * local + 1);
-        }
-        big = fmaxf(big, m[i]);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) big = fmaxf(big, __ldcg(part + s * S::kPart + kPrRows * D + local));
     const float base = big == -INFINITY ? 0.f : big;
-    float e[2], sum = 0.f;
+    float4 acc[4];
+    float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        e[i] = m[i] == -INFINITY && l[i] == 0.f ? 0.f : exp2_fast(m[i] - base);
-        sum += e[i] * l[i];
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    constexpr int C = D / 32;
-    float acc[C];
-#pragma unroll
-    for (int i = 0; i < C; ++i) acc[i] = 0.f;
+    for (int i = 0; i < 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
     for (int s = 0; s < a.splits; ++s) {
-        const float w = __shfl_sync(0xffffffffu, s < 32 ? e[0] : e[1], s & 31);
-        if (w == 0.f) continue;
+        const float* x = part + s * S::kPart;
+        const float l = __ldcg(x + kPrRows * D + kPrRows + local), w = kv_weight(__ldcg(x + kPrRows * D + local), l, base);
+        if (w == 0.f) continue;   // (a part without units has no sums)
+        sum += w * l;
 #pragma unroll
-        for (int i = 0; i < C; ++i) acc[i] += w * __ldcg(part + s * S::kPart + local * D + lane + 32 * i);
+        for (int i = 0; i < 4; ++i) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(x + ((c0 + i) * kPrRows + local) * 4));
+            acc[i].x += w * v.x; acc[i].y += w * v.y; acc[i].z += w * v.z; acc[i].w += w * v.w;
+        }
     }
     const int r = it.row0 + local, tok = r / a.G, qh = h * a.G + r - tok * a.G;
-    const int64_t at = (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head;
+    const int64_t at = (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + 4 * c0;
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-        const float y = sum == 0.f ? 0.f : acc[i] / sum;
-        if (BF16) static_cast<__nv_bfloat16*>(a.out)[at + lane + 32 * i] = __float2bfloat16_rn(y);
-        else static_cast<__half*>(a.out)[at + lane + 32 * i] = __float2half_rn(y);
+    for (int i = 0; i < 4; ++i) {
+        o_put<BF16>(a.out, at + 4 * i, sum == 0.f ? 0.f : acc[i].x / sum);
+        o_put<BF16>(a.out, at + 4 * i + 1, sum == 0.f ? 0.f : acc[i].y / sum);
+        o_put<BF16>(a.out, at + 4 * i + 2, sum == 0.f ? 0.f : acc[i].z / sum);
+        o_put<BF16>(a.out, at + 4 * i + 3, sum == 0.f ? 0.f : acc[i].w / sum);
     }
-    if (a.lse && lane == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = sum == 0.f ? -INFINITY : (base + log2f(sum) - 7.f) * 0.69314718f;
+    if (a.lse && c0 == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(big, sum);
 }
 
 }  // namespace us

@@ -539,7 +539,7 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
             return bad("lse must be a contiguous float32 (N, n_heads) tensor on the cache's device");
         lse = l->data_ptr();
     }
-    const int64_t bytes = us_kv_attention_scratch(static_cast<us_kv*>(h), N, q.n_seqs, (int32_t)H);
+    const int64_t bytes = us_kv_attention_scratch(static_cast<us_kv*>(h), &q, N, (int32_t)H);
     if (bytes < 0) return fail(US_ERR_INVALID_ARG, "us_kv_attention");
     if (bytes > 0) scratch = at::detail::empty_cuda({bytes}, at::kByte, pool->device(), std::nullopt);
     us_status s;
