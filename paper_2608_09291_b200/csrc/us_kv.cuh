@@ -231,11 +231,14 @@ __global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int
 //     a factor of the scores and V's a factor of p. p is rounded to fp16 with 2^7 in front and V's step relative to the
 //     largest so far: what a row sums stays between 2^-24 and 2^15 of the largest term; sums are fp32.
 //   * m follows the true maximum only where it is 2^8 behind, so most units need no reduction over lanes and no rescaling.
-//   * All (sequence, row tile, head) items in a row, 128 tokens a unit: every CTA takes the same number of units, whatever the lengths.
-//     An item that is cut leaves its parts in scratch, and a second kernel joins them in the order of the CTAs.
+//   * All (sequence, row tile, head) items in a row, 128 tokens a unit and kKvStart units for beginning one: every CTA takes the same
+//     number of units, whatever the lengths. (64 sequences of 1 to 8192 tokens, 64/8 heads: 148 us without the units for beginning,
+//     the CTAs with the short sequences were last.) An item that is cut leaves its parts in scratch, and a second kernel joins
+//     them in the order of the CTAs.
 // A warp copies (TMA, swizzled so that the fragment loads meet no bank twice); four read, 32 tokens of a unit each (two groups side by
 // side: their chains of products overlap), with sums of their own that are joined at an item's end.
 constexpr int kKvTile = 128;
+constexpr int kKvStart = 2;   // what an item's queries, sums and output cost, in units
 struct KvAttend {
     CUtensorMap k_map, v_map;
     KvPool pool;
@@ -261,6 +264,7 @@ struct KvItem {
     int32_t row_tiles;
     int32_t lo;          // first token that any of its queries sees
     int32_t t_lo, tiles; // first unit of the cache, units (1 if it sees nothing)
+    __device__ __forceinline__ int cost() const { return kKvStart + tiles; }
 };
 template <int R>
 __device__ __forceinline__ KvItem kv_item(const KvAttend& a, const KvSeq& seq)
@@ -315,7 +319,7 @@ __device__ __forceinline__ KvRange kv_range(const KvAttend& a, int cta, int lane
             mine = kv_seq(a.seqs, a.pool, base + lane, wrong);
             any |= wrong;
             const KvItem it = kv_item<R>(a, mine);
-            c = (long long)it.row_tiles * a.pool.Hkv * it.tiles;
+            c = (long long)it.row_tiles * a.pool.Hkv * it.cost();
         }
         sum = c;
 #pragma unroll
@@ -460,10 +464,10 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
     uint32_t par = 0;
     int s = range.s;
     KvItem it = range.item;
-    int item = 0, tile = 0;   // item of the sequence (row tile * Hkv + head), unit of the item
+    int item = 0, at_unit = 0;   // item of the sequence (row tile * Hkv + head), unit of the item (kKvStart of them before its first tokens)
     if (left > 0) {
-        item = kv_div(range.in_seq, it.tiles);
-        tile = (int)(range.in_seq - (long long)item * it.tiles);
+        item = kv_div(range.in_seq, it.cost());
+        at_unit = (int)(range.in_seq - (long long)item * it.cost());
     }
     auto next_seq = [&]() {   // (the units of this CTA end before the sequences do)
         if (item < it.row_tiles * p.Hkv) return;
@@ -478,7 +482,8 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
         const int box = min(p.T, kKvTile), nb = kKvTile / box;   // tokens of a copy, copies of a unit
         long long issued = 0;
         while (left > 0 && ok) {
-            const int n = (int)min((long long)(it.tiles - tile), left);
+            const int share = (int)min((long long)(it.cost() - at_unit), left);
+            const int tile = max(0, at_unit - kKvStart), n = max(0, at_unit + share - kKvStart) - tile;   // tokens' units
             const int h = item % p.Hkv;
             const int32_t* row = a.seqs.table + (int64_t)s * a.seqs.table_stride;
             // 32 copies' block numbers and steps at a time, a lane each
@@ -500,27 +505,29 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                 for (int i = 0; i < m; ++i) {
                     ok = ops_wait_warp(b_empty + 8u * stage, par ^ 1u, kMxWait, dead);
                     if (!ok) break;
-                    // the steps of the unit's eight 16-token groups
-                    const int from = i * nb + (lane & 7) * 16 / box;
-                    const float gk = __shfl_sync(0xffffffffu, sk, from), gv = __shfl_sync(0xffffffffu, sv, from);
-                    if (lane < 8) steps[stage][lane] = make_float2(gk, gv);
-                    const uint32_t valid = __popc(__ballot_sync(0xffffffffu, blk >= 0 && lane / nb == i));
+                    const bool mine = blk >= 0 && lane / nb == i;
+                    const uint32_t valid = __popc(__ballot_sync(0xffffffffu, mine));
                     const uint32_t bar = b_full + 8u * stage;
+                    if (lane == 0) mbar_expect_tx_only(bar, valid * 2u * (uint32_t)(box * D));
                     __syncwarp();
-                    if (lane == 0) mbar_expect_tx(bar, valid * 2u * (uint32_t)(box * D));
-                    __syncwarp();
-                    if (blk >= 0 && lane / nb == i) {
+                    if (mine) {
                         const int32_t y = (blk * p.Hkv + h) * p.T + (t & (p.T - 1));
                         const uint32_t dst = smem_u32(ring + (size_t)stage * S::kStage) + (uint32_t)((lane - i * nb) * box * D);
                         tma_rows(dst, &a.k_map, y, bar);
                         tma_rows(dst + S::kHalf, &a.v_map, y, bar);
                     }
+                    // the steps of the unit's eight 16-token groups (their loads take as long as the copies do: not waited for before them)
+                    const int from = i * nb + (lane & 7) * 16 / box;
+                    const float gk = __shfl_sync(0xffffffffu, sk, from), gv = __shfl_sync(0xffffffffu, sv, from);
+                    if (lane < 8) steps[stage][lane] = make_float2(gk, gv);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar);
                     ++issued;
                     if (++stage == a.stages) { stage = 0; par ^= 1u; }
                 }
             }
-            left -= n;
-            tile = 0;
+            left -= share;
+            at_unit = 0;
             ++item;
             if (left > 0) next_seq();
         }
@@ -531,7 +538,9 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
     } else {
         const int g = lane >> 2, t = lane & 3;
         while (left > 0 && ok) {
-            const int n = (int)min((long long)(it.tiles - tile), left);
+            const int share = (int)min((long long)(it.cost() - at_unit), left);
+            const int tile = max(0, at_unit - kKvStart), n = max(0, at_unit + share - kKvStart) - tile;   // tokens' units
+            if (n == 0) break;   // (the share ends with an item that the next CTA begins)
             const int h = item % p.Hkv, row0 = item / p.Hkv * R;
             // Q fragments: rows g of every 8, the lane's D/4 columns; fp16 times a power of two that brings bf16 into range
             uint32_t qf[NT][KS][2];
@@ -817,8 +826,8 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                 }
             }
             bar_consumers();
-            left -= n;
-            tile = 0;
+            left -= share;
+            at_unit = 0;
             ++item;
             if (left > 0) next_seq();
         }
@@ -845,16 +854,16 @@ __global__ void __launch_bounds__(256) us_kv_join_kernel(const __grid_constant__
     int s = range.s;
     KvItem it = range.item;
     long long start = range.u0 - range.in_seq;   // first unit of the sequence
-    long long units = (long long)it.row_tiles * a.pool.Hkv * it.tiles;
+    long long units = (long long)it.row_tiles * a.pool.Hkv * it.cost();
     while (start + units <= range.u1 - 1) {
         start += units;
         if (++s >= a.seqs.S) return;
         it = kv_item<R>(a, s);
-        units = (long long)it.row_tiles * a.pool.Hkv * it.tiles;
+        units = (long long)it.row_tiles * a.pool.Hkv * it.cost();
     }
-    const int item = kv_div(range.u1 - 1 - start, it.tiles);
-    const long long first = start + (long long)item * it.tiles, end = first + it.tiles;
-    if (first < range.u0 || end <= range.u1) return;   // begins in an earlier CTA, or is whole
+    const int item = kv_div(range.u1 - 1 - start, it.cost());
+    const long long first = start + (long long)item * it.cost() + kKvStart, end = first + it.tiles;
+    if (first < range.u0 || first >= range.u1 || end <= range.u1) return;   // begins in an earlier CTA or a later one, or is whole
     const int h = item % a.pool.Hkv, row0 = item / a.pool.Hkv * R;
     const int last = range.shares.owner(end - 1);
     asm volatile("griddepcontrol.wait;" ::: "memory");
