@@ -233,12 +233,12 @@ __global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int
 //   * m follows the true maximum only where it is 2^8 behind, so most units need no reduction over lanes and no rescaling.
 //   * All (sequence, row tile, head) items in a row, 128 tokens a unit and kKvStart units for beginning one: every CTA takes the same
 //     number of units, whatever the lengths. (64 sequences of 1 to 8192 tokens, 64/8 heads: 148 us without the units for beginning,
-//     the CTAs with the short sequences were last.) An item that is cut leaves its parts in scratch, and a second kernel joins
+//     where the CTAs with the short sequences were last, 120 with 2, 110 with 3, 104 with 4.) An item that is cut leaves its parts in scratch, and a second kernel joins
 //     them in the order of the CTAs.
 // A warp copies (TMA, swizzled so that the fragment loads meet no bank twice); four read, 32 tokens of a unit each (two groups side by
 // side: their chains of products overlap), with sums of their own that are joined at an item's end.
 constexpr int kKvTile = 128;
-constexpr int kKvStart = 2;   // what an item's queries, sums and output cost, in units
+constexpr int kKvStart = 4;   // what an item's queries, sums and output cost, in units
 struct KvAttend {
     CUtensorMap k_map, v_map;
     KvPool pool;
@@ -429,7 +429,7 @@ struct KvShape {
     static constexpr int kHalf = kKvTile * D;                 // bytes of a stage's K (or V)
     static constexpr int kStage = 2 * kHalf;
     static constexpr int kPitch = D + 4;                      // floats of a row of the warps' sums
-    static constexpr int kMerge = R * kPitch * 4 + 4 * R * 2 * 4;
+    static constexpr int kMerge = R * kPitch * 4 + 5 * R * 2 * 4;
     static constexpr int kMaxStages = 8;
     static constexpr int kPart = R * (D + 2);                 // floats of a part
 };
@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
     __shared__ uint32_t dead_word;
     uint8_t* ring = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     float* sums = reinterpret_cast<float*>(ring + (size_t)a.stages * S::kStage);   // [row][pitch]
-    float2* stats = reinterpret_cast<float2*>(sums + R * S::kPitch);               // [warp][row] m, l
+    float2* stats = reinterpret_cast<float2*>(sums + R * S::kPitch);               // [warp][row] m, l; then the four together
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8u * S::kMaxStages;
     volatile uint32_t* dead = &dead_word;
@@ -612,18 +612,18 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
             all_lo = __reduce_max_sync(0xffffffffu, all_lo);
             all_hi = __reduce_min_sync(0xffffffffu, all_hi);
             const int last_hi = a.causal ? pos0 + (min(row0 + R, it.rows) - 1) / a.G + 1 : it.seq.len;
-            float m[NT][2], l[NT][2], o[MT][NT][4];
+            float m[NT][2], mb[NT][2], l[NT][2], o[MT][NT][4];   // mb: 7 - m
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) { m[nt][c] = -INFINITY; l[nt][c] = 0.f; }
+                for (int c = 0; c < 2; ++c) { m[nt][c] = -INFINITY; mb[nt][c] = INFINITY; l[nt][c] = 0.f; }
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) o[i][nt][c] = 0.f;
-            float ref = 0.f;   // V's largest step so far
+            float ref = 0.f, inv_ref = 0.f;   // V's largest step so far; its inverse, 0 where that is no good
             int tok0 = (it.t_lo + tile) * kKvTile + 32 * warp;
 #pragma unroll 1
             for (int i = 0; i < n; ++i, tok0 += kKvTile) {
@@ -662,42 +662,63 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                                 for (int nt = 0; nt < NT; ++nt) mma_f16(sc[b][nt], a0, a1, a2, a3, qf[nt][4 * c + j][0], qf[nt][4 * c + j][1]);
                             }
                     }
+                    // e = s - m + 7: more than 15 where m is more than 2^8 behind (or nothing was seen yet)
+                    float e[2][NT][4];
                     bool behind = false;
+                    auto exponents = [&]() {
+#pragma unroll
+                        for (int b = 0; b < 2; ++b)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) e[b][nt][c] = fmaf(sc[b][nt][c], f[nt][c & 1] * stk[b], mb[nt][c & 1]);
+                        if (edge)
+#pragma unroll
+                            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int c = 0; c < 4; ++c) {
+                                        const int tk = tok0 + 16 * b + g + 8 * (c >> 1);
+                                        if (tk < lo[nt][c & 1] || tk >= hi[nt][c & 1] || stk[b] < 0.f) e[b][nt][c] = -INFINITY;
+                                    }
+                    };
+                    exponents();
 #pragma unroll
                     for (int b = 0; b < 2; ++b)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                float v = sc[b][nt][c] * (f[nt][c & 1] * stk[b]);
-                                if (edge) {
-                                    const int tk = tok0 + 16 * b + g + 8 * (c >> 1);
-                                    if (tk < lo[nt][c & 1] || tk >= hi[nt][c & 1] || stk[b] < 0.f) v = -INFINITY;
-                                }
-                                sc[b][nt][c] = v;
-                                behind |= v > m[nt][c & 1] + 8.f;
-                            }
+                            for (int c = 0; c < 4; ++c) behind |= e[b][nt][c] > 15.f;
                     if (__any_sync(0xffffffffu, behind)) {
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int c = 0; c < 2; ++c) {
-                                float x = fmaxf(fmaxf(sc[0][nt][c], sc[0][nt][c + 2]), fmaxf(sc[1][nt][c], sc[1][nt][c + 2]));
+                                float x = -INFINITY;
+#pragma unroll
+                                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                                    for (int q = 0; q < 2; ++q)
+                                        if (e[b][nt][c + 2 * q] > -INFINITY) x = fmaxf(x, sc[b][nt][c + 2 * q] * (f[nt][c] * stk[b]));
                                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
                                 x = fmaxf(x, m[nt][c]);
                                 const float alpha = x == -INFINITY ? 1.f : exp2_fast(m[nt][c] - x);
                                 m[nt][c] = x;
+                                mb[nt][c] = x == -INFINITY ? INFINITY : 7.f - x;
                                 l[nt][c] *= alpha;
 #pragma unroll
                                 for (int k = 0; k < MT; ++k) { o[k][nt][c] *= alpha; o[k][nt][c + 2] *= alpha; }
                             }
+                        exponents();
                     }
                     const float top = fmaxf(stk[0] < 0.f ? 0.f : stv[0], stk[1] < 0.f ? 0.f : stv[1]);
                     if (top > ref) {
                         const float b = ref / top;
                         ref = top;
+                        inv_ref = top > 1e-30f && top < 1e30f ? 1.f / top : 0.f;
 #pragma unroll
                         for (int k = 0; k < MT; ++k)
 #pragma unroll
@@ -708,17 +729,16 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                     uint32_t pf[2][NT][2];
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        const float rel = stk[b] < 0.f ? 0.f : stv[b] == ref ? 1.f : __fdiv_rn(stv[b], ref);   // (NaN: NaN)
+                        const float rel = stk[b] < 0.f ? 0.f : inv_ref > 0.f ? stv[b] * inv_ref : stv[b] == ref ? 1.f : __fdiv_rn(stv[b], ref);   // (NaN: NaN)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            float e[4];
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
-                                e[c] = exp2_fast(sc[b][nt][c] - (m[nt][c & 1] == -INFINITY ? 0.f : m[nt][c & 1] - 7.f));
-                                l[nt][c & 1] += e[c];
+                                e[b][nt][c] = exp2_fast(e[b][nt][c]);
+                                l[nt][c & 1] += e[b][nt][c];
                             }
-                            pf[b][nt][0] = transpose8(half2_bits(e[0] * rel, e[1] * rel));
-                            pf[b][nt][1] = transpose8(half2_bits(e[2] * rel, e[3] * rel));
+                            pf[b][nt][0] = transpose8(half2_bits(e[b][nt][0] * rel, e[b][nt][1] * rel));
+                            pf[b][nt][1] = transpose8(half2_bits(e[b][nt][2] * rel, e[b][nt][3] * rel));
                         }
                     }
                     // sums: 16 of D x 8 NT rows at a time; a lane holds the same D columns of its four tokens
@@ -784,6 +804,17 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                     const float2 own = stats[warp * R + r];
                     w[nt][c] = kv_weight(own.x, own.y, big == -INFINITY ? 0.f : big);
                 }
+            if (threadIdx.x < R) {
+                float big = -INFINITY, sum = 0.f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) big = fmaxf(big, stats[k * R + threadIdx.x].x);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 x = stats[k * R + threadIdx.x];
+                    sum += kv_weight(x.x, x.y, big == -INFINITY ? 0.f : big) * x.y;
+                }
+                stats[4 * R + threadIdx.x] = make_float2(big, sum);
+            }
 #pragma unroll 1
             for (int turn = 0; turn < 4; ++turn) {
                 if (warp == turn)
@@ -804,14 +835,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
             const int rows = min(R, it.rows - row0);
             for (int i = threadIdx.x; i < rows * D; i += 128) {
                 const int r = i / D, d = i - r * D;
-                float big = -INFINITY, sum = 0.f;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) big = fmaxf(big, stats[k * R + r].x);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 x = stats[k * R + r];
-                    sum += kv_weight(x.x, x.y, big == -INFINITY ? 0.f : big) * x.y;
-                }
+                const float big = stats[4 * R + r].x, sum = stats[4 * R + r].y;
                 const float acc = sums[r * S::kPitch + (d % (D / 8)) * 8 + d / (D / 8)];
                 if (whole) {
                     const int tok = (row0 + r) / a.G, qh = h * a.G + (row0 + r) - tok * a.G;
