@@ -298,7 +298,7 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
     void* args[] = {&a};
     if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)pl.ctas), 160, pl.smem, st, args);
     // (an item of one unit is never cut)
-    if (e == cudaSuccess && (int64_t)q->table_width * h->pool.T > kKvTile) e = ops_launch(pl.join, dim3((unsigned)pl.ctas), 256, 0, st, args);
+    if (e == cudaSuccess && (int64_t)q->table_width * h->pool.T > kKvTile) e = ops_launch(pl.join, dim3((unsigned)pl.ctas), 32 * kJoinWarps, 0, st, args);
     return cuda(e);
 }
 
