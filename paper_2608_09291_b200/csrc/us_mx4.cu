@@ -20,8 +20,8 @@ void shape(Plan* p, int64_t slice_tiles, int64_t budget)
     using S = Mx4Shape<NB, FUSE>;
     p->kernel = (const void*)us_mx4_product_kernel<NB, FUSE>;
     const int64_t xs = FUSE ? slice_tiles * S::kXTile : 0;
-    // (the split's partial sums, 128 x NB fp32, take the ring's place)
-    const int64_t least = p->split > 1 ? (128 * 4 * NB + S::kStage - 1) / S::kStage : 1;
+    // (the split's partial sums, 128 x NB fp32, take the ring's place; else two buffers of 32 tokens on their way out)
+    const int64_t least = ((p->split > 1 ? 128 * 4 * NB : 2 * 32 * (512 + 16)) + S::kStage - 1) / S::kStage;
     p->stages = (int)std::max(least, std::min({(int64_t)S::kMaxStages, slice_tiles, (budget - 1024 - xs) / S::kStage}));
     p->smem = 1024 + xs + (int64_t)p->stages * S::kStage;
 }
@@ -84,6 +84,7 @@ us_status product(const void* X, int32_t x_type, int64_t ldx, const void* x_mx, 
     p.split = pl.split; p.col_tiles = pl.col_tiles; p.stages = pl.stages;
     p.x_type = x_type; p.y_type = y_type;
     p.x_vec = X && rows_vec(X, ldx, size_of(x_type));
+    p.y_vec = rows_vec(Y, N > 1 ? ldy : 0, size_of(y_type));
     p.w_stable = (flags & US_MX4_W_STABLE) != 0;
     p.err = err;
     const cudaError_t e = ops_kernel_allow(pl.kernel);

@@ -253,7 +253,7 @@ struct Mx4Params {
     int32_t split, col_tiles;
     int32_t stages;        // ring stages
     int32_t x_type, y_type;
-    int32_t x_vec;         // rows of X take 16-byte loads
+    int32_t x_vec, y_vec;  // rows of X, of Y take 16-byte accesses
     int32_t w_stable;      // the weights are complete whatever the stream's earlier work does
     uint32_t* err;
 };
@@ -286,6 +286,31 @@ __device__ __forceinline__ void mx4_copy_scales(uint32_t elected, uint32_t d, ui
     asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}"
                  ::"r"(d), "l"(s), "r"(elected) : "memory");
 }
+#define US_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define US_I8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+// 32 columns of the thread's lane, fetched without waiting
+__device__ __forceinline__ void tc_ld32(uint32_t addr, uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
+                 "%27,%28,%29,%30,%31}, [%32];" : US_R8(r, 0), US_R8(r, 8), US_R8(r, 16), US_R8(r, 24) : "r"(addr));
+}
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
+                 "%27,%28,%29,%30,%31};" ::US_I8(r, 0), US_I8(r, 8), US_I8(r, 16), US_I8(r, 24), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tc_st16_lanes(uint32_t addr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 ::US_I8(r, 0), US_I8(r, 8), "r"(addr) : "memory");
+}
+// (values that an asynchronous load writes must not be moved in front of its wait)
+__device__ __forceinline__ void pin32(uint32_t (&r)[32])
+{
+#pragma unroll
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i])::"memory");
+}
 __device__ __forceinline__ void tc_ld16(uint32_t addr, uint32_t (&r)[16])
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
@@ -294,19 +319,67 @@ __device__ __forceinline__ void tc_ld16(uint32_t addr, uint32_t (&r)[16])
                  : "r"(addr));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t local, uint32_t rank)
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t local, uint32_t rank)
 {
     uint32_t a;
-    float v;
+    float4 v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(local), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
     return v;
 }
-__device__ __forceinline__ void mx4_store(const Mx4Params& p, int64_t n, int64_t m, float v)
+// Y[n][m .. m + 3] (the matrix ends at M)
+__device__ __forceinline__ void mx4_store4(const Mx4Params& p, int64_t n, int64_t m, const float (&v)[4])
 {
-    if (p.y_type == kF32) static_cast<float*>(p.Y)[n * p.ldy + m] = v;
-    else if (p.y_type == kF16) static_cast<__half*>(p.Y)[n * p.ldy + m] = __float2half_rn(v);
-    else static_cast<__nv_bfloat16*>(p.Y)[n * p.ldy + m] = __float2bfloat16_rn(v);
+    const int64_t at = n * p.ldy + m;
+    const bool whole = p.y_vec && m + 4 <= p.M;
+    if (p.y_type == kF32) {
+        float* y = static_cast<float*>(p.Y) + at;
+        if (whole) *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
+        else for (int i = 0; i < 4; ++i) if (m + i < p.M) y[i] = v[i];
+    } else {
+        uint16_t h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = p.y_type == kF16 ? __half_as_ushort(__float2half_rn(v[i])) : __bfloat16_as_ushort(__float2bfloat16_rn(v[i]));
+        uint16_t* y = static_cast<uint16_t*>(p.Y) + at;
+        if (whole) *reinterpret_cast<uint2*>(y) = make_uint2(h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16));
+        else for (int i = 0; i < 4; ++i) if (m + i < p.M) y[i] = h[i];
+    }
+}
+__device__ __forceinline__ void bar_epilogue() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+// The tile's sums (four warps, lane quarter `quarter`): 32 tokens at a time to shared memory as they are stored, [token][weight row], and
+// from there in whole lines: every thread 16 bytes of a token's 256 (512). Straight from the registers a warp's store of one token is 64
+// bytes; 4096 x 28672 x 8192 took 705 us that way, whatever the products took.
+template <class T>
+__device__ __forceinline__ void mx4_write_tile(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage)
+{
+    constexpr int PITCH = 128 * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = 128 / PER;   // bytes of a token, values of a piece, pieces of a token
+    const int row = 32 * quarter + lane, tid = row;
+    const int m_here = (int)min((int64_t)128, p.M - m0);
+    int buf = 0;
+#pragma unroll 1
+    for (int c = 0; c < nn; c += 32) {
+        uint32_t r[32];
+        tc_ld32(tm + ((uint32_t)quarter << 21) + (uint32_t)c, r);
+        tc_wait_ld();
+        pin32(r);
+        uint8_t* b = stage + buf * (32 * PITCH);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) *reinterpret_cast<T*>(b + i * PITCH + row * sizeof(T)) = from_f32<T>(__uint_as_float(r[i]));
+        bar_epilogue();   // (two buffers: whoever is a chunk behind still reads the other one)
+        const int rows = min(32, nn - c);
+        if (p.y_vec && m_here == 128) {
+#pragma unroll
+            for (int k = 0; k < 32 * ROW / 128; ++k) {
+                const int i = tid + 128 * k, n = i / ROW, piece = i % ROW;
+                if (n < rows) *reinterpret_cast<uint4*>(static_cast<T*>(p.Y) + (n0 + c + n) * p.ldy + m0 + piece * PER) = *reinterpret_cast<const uint4*>(b + n * PITCH + 16 * piece);
+            }
+        } else {
+            for (int n = 0; n < rows; ++n)
+                if (tid < m_here) static_cast<T*>(p.Y)[(n0 + c + n) * p.ldy + m0 + tid] = *reinterpret_cast<const T*>(b + n * PITCH + tid * sizeof(T));
+        }
+        buf ^= 1;
+    }
 }
 
 // (FUSE) warps w of nw: the CTA's columns [256 t0, 256 t1) of the N tokens, quantised into operand tiles in shared memory
@@ -315,18 +388,19 @@ __device__ __forceinline__ void mx4_quantize_slice(const Mx4Params& p, uint8_t* 
 {
     constexpr int U = 4;
     const int units = (t1 - t0) * p.N;
+    const uint32_t inv = ((1u << 24) + p.N - 1) / p.N;   // u / N = u inv / 2^24: N <= 16, and u inv < 2^32 for up to 255 tiles
 #pragma unroll 1
     for (int u0 = w; u0 < units; u0 += U * nw) {
         Eight<T> x[U];
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const int u = u0 + i * nw, n = u % p.N, t = u / p.N;
+            const uint32_t u = u0 + i * nw, t = u * inv >> 24, n = u - t * p.N;
             const int64_t k = 256 * (int64_t)(t0 + t) + 8 * lane;
             if (u < units) x[i] = load8(static_cast<const T*>(p.X) + n * p.ldx + k, p.K - k, p.x_vec && k + 8 <= p.K);
         }
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const int u = u0 + i * nw, n = u % p.N, t = u / p.N;
+            const uint32_t u = u0 + i * nw, t = u * inv >> 24, n = u - t * p.N;
             if (u >= units) break;
             uint32_t sc;
             const uint32_t codes = mx4_quantize_row(x[i], sc);
@@ -338,7 +412,7 @@ __device__ __forceinline__ void mx4_quantize_slice(const Mx4Params& p, uint8_t* 
 }
 
 template <int NB, bool FUSE>
-__global__ void __launch_bounds__(192, 1) us_mx4_product_kernel(const __grid_constant__ Mx4Params p)
+__global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(const __grid_constant__ Mx4Params p)
 {
     using S = Mx4Shape<NB, FUSE>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -474,23 +548,21 @@ __global__ void __launch_bounds__(192, 1) us_mx4_product_kernel(const __grid_con
         tc_fence_after();
         const uint32_t quarter = (uint32_t)(warp & 3);
         const int row = 32 * (int)quarter + lane;
-        const int64_t m = 128 * (int64_t)mt + row;
         // (the ring is free: all copies have landed and have been read)
-        float* part = reinterpret_cast<float*>(ring);
-        if (ok && !*dead) {
+        if (p.split > 1) {
+            float* part = reinterpret_cast<float*>(ring);
+            if (ok)
 #pragma unroll 1
-            for (int c = 0; c < nn; c += 16) {
-                uint32_t r[16];
-                tc_ld16(tm + (quarter << 21) + (uint32_t)c, r);
-                if (p.split > 1) {
+                for (int c = 0; c < nn; c += 16) {
+                    uint32_t r[16];
+                    tc_ld16(tm + (quarter << 21) + (uint32_t)c, r);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) part[(c + i) * 128 + row] = __uint_as_float(r[i]);
-                } else if (m < p.M) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (c + i < nn) mx4_store(p, n0 + c + i, m, __uint_as_float(r[i]));
                 }
-            }
+        } else if (!*dead) {   // (*dead is set before the sums are announced, or never)
+            if (p.y_type == kF32) mx4_write_tile<float>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring);
+            else if (p.y_type == kF16) mx4_write_tile<__half>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring);
+            else mx4_write_tile<__nv_bfloat16>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring);
         }
         tc_fence_before();
     }
@@ -503,14 +575,19 @@ __global__ void __launch_bounds__(192, 1) us_mx4_product_kernel(const __grid_con
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "n"(S::kCols));
     if (p.split > 1) {
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-        // each rank adds the sums of a share of the tile's (token, row) pairs
-        const int total = nn * 128, per = (total / p.split + 31) & ~31, lo = min(total, rank * per), hi = rank == p.split - 1 ? total : min(total, lo + per);
+        // each rank adds the sums of a share of the tile's (token, four rows), four ranks' at a time on their way
+        const int total = nn * 32, per = (total + p.split - 1) / p.split, lo = min(total, rank * per), hi = min(total, lo + per);
         const uint32_t part = smem_u32(ring);
         for (int i = lo + (int)threadIdx.x; i < hi; i += 192) {
-            float v = 0.f;
-            for (int r = 0; r < p.split; ++r) v += ld_cluster_f32(part + 4u * i, (uint32_t)r);
-            const int64_t m = 128 * (int64_t)mt + (i & 127);
-            if (m < p.M) mx4_store(p, n0 + (i >> 7), m, v);
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int r0 = 0; r0 < p.split; r0 += 4) {
+                float4 x[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = r0 + r < p.split ? ld_cluster_f32x4(part + 16u * i, (uint32_t)(r0 + r)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) { v[0] += x[r].x; v[1] += x[r].y; v[2] += x[r].z; v[3] += x[r].w; }
+            }
+            mx4_store4(p, n0 + (i >> 5), 128 * (int64_t)mt + 4 * (i & 31), v);
         }
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
