@@ -98,6 +98,12 @@ bool rows_vec(const void* x, int32_t type, int64_t token, int64_t head)
     return aligned(x, 16) && token * size_of(type) % 16 == 0 && head * size_of(type) % 16 == 0;
 }
 
+template <class T>
+const void* append_kernel(int team)
+{
+    return team == 32 ? (const void*)us_kv_append_kernel<T, 32> : team == 64 ? (const void*)us_kv_append_kernel<T, 64> : (const void*)us_kv_append_kernel<T, 128>;
+}
+
 // ---- attention: which kernels ----
 struct AttendPlan {
     const void *kernel, *join;
@@ -202,9 +208,11 @@ us_status us_kv_append(us_kv* h, const us_kv_seqs* q, int64_t N, const void* K, 
     if (s != US_OK) return s;
     // blocks that get tokens: at most n / T + 2 of a sequence with n new tokens, and n
     const int64_t most = std::min(N, N / h->pool.T + 2 * (int64_t)q->n_seqs);
-    const dim3 grid((unsigned)most, (unsigned)h->pool.Hkv, 2);
-    const void* k = type == US_F16 ? (const void*)us_kv_append_kernel<__half> :
-                    type == US_BF16 ? (const void*)us_kv_append_kernel<__nv_bfloat16> : (const void*)us_kv_append_kernel<float>;
+    // a team's threads keep up to 64 elements each of a whole block; single tokens need half a warp
+    const int team = !q->cu_tokens || h->pool.T * h->pool.D <= 2048 ? 32 : h->pool.T * h->pool.D <= 4096 ? 64 : 128;
+    while ((1 << a.log2_T) < h->pool.T) ++a.log2_T;
+    const dim3 grid((unsigned)most, (unsigned)((h->pool.Hkv + 128 / team - 1) / (128 / team)), 2);
+    const void* k = type == US_F16 ? append_kernel<__half>(team) : type == US_BF16 ? append_kernel<__nv_bfloat16>(team) : append_kernel<float>(team);
     void* args[] = {&a};
     return cuda(ops_launch(k, grid, 128, 0, static_cast<cudaStream_t>(stream), args));
 }
@@ -220,11 +228,12 @@ us_status us_kv_read(us_kv* h, const us_kv_seqs* q, int64_t tokens, void* K, voi
     KvSeqs s = seqs(&one, 0);
     us_status st = error_word(&p.err);
     if (st != US_OK) return st;
-    const int64_t units = (int64_t)s.S * tokens * p.Hkv * (p.D / 8);
-    const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((units + 255) / 256, 148 * 64)));
+    const dim3 grid((unsigned)((tokens + 15) / 16), (unsigned)((p.Hkv + kReadHeads - 1) / kReadHeads), (unsigned)std::min(s.S, 65535));
+    int log2_T = 0;
+    while ((1 << log2_T) < p.T) ++log2_T;
     const void* k = type == US_F16 ? (const void*)us_kv_read_kernel<__half> :
                     type == US_BF16 ? (const void*)us_kv_read_kernel<__nv_bfloat16> : (const void*)us_kv_read_kernel<float>;
-    void* args[] = {&p, &s, &tokens, &K, &V};
+    void* args[] = {&p, &s, &tokens, &log2_T, &K, &V};
     return cuda(ops_launch(k, grid, 256, 0, static_cast<cudaStream_t>(stream), args));
 }
 

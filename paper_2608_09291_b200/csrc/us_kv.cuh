@@ -47,11 +47,12 @@ __device__ __forceinline__ KvSeq kv_seq(const KvSeqs& q, const KvPool& p, int s,
 }
 
 // ---- append --------------------------------------------------------------------------------------------------------------
-// code = RNE(x / s) for the exact quotient: the rounded product x * (1 / s) is off by at most one, and the sign of a fused
-// multiply-add says on which side of the border next to it x lies (exact: a rounded sum is never on the other side of 0).
-__device__ __forceinline__ int kv_code(float x, float s, float inv)
+// code = RNE(x / s) for the exact quotient, x finite or not. The rounded product x * (1 / s) is within 2^-16 of the quotient: its nearest
+// integer is the code unless it lies that close to a border (1 of 25000 values; kv_code_near), where the sign of a fused multiply-add says on which side x
+// is (exact: a rounded sum is never on the other side of 0), or underflow would lose the border, where 64 bits decide.
+__device__ __noinline__ int kv_code_near(float x, float s, float inv)
 {
-    if (s < 1e-30f) {   // (borders that fp32 would lose to underflow)
+    if (s < 1e-30f) {
         const double q = s > 0.f ? rint((double)x / (double)s) : 0.0;
         return q != q ? 0 : (int)fmin(fmax(q, -127.0), 127.0);
     }
@@ -62,6 +63,35 @@ __device__ __forceinline__ int kv_code(float x, float s, float inv)
     else if (down < 0.f || (down == 0.f && odd)) r -= 1.f;
     return r != r ? 0 : (int)fminf(fmaxf(r, -127.f), 127.f);
 }
+// Eight of them; inv = 0 sends all to kv_code_near.
+template <class T_>
+__device__ __forceinline__ uint2 kv_codes8(const Eight<T_>& e, float s, float inv)
+{
+    uint32_t w[2] = {0, 0};
+    float far = 0.f;   // the largest distance from an integer
+    bool fine = inv > 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = to_f32(e.v[i]);
+        const float t = fmaf(x, inv, 12582912.f);   // 1.5 2^23: the nearest integer in the low bits
+        far = fmaxf(far, fabsf(fmaf(x, inv, 12582912.f - t)));
+        fine = fine && fabsf(x) < 3.3e38f;   // (the maximum above passes over NaN)
+        w[i >> 2] |= (__float_as_uint(t) & 0xFFu) << (8 * (i & 3));
+    }
+    if (!(fine && far < 0.49998f)) {
+        w[0] = w[1] = 0;
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) {
+            float x = 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) if (k == i) x = to_f32(e.v[k]);
+            const uint32_t c = ((uint32_t)kv_code_near(x, s, inv) & 0xFFu) << (8 * (i & 3));
+            if (i < 4) w[0] |= c;
+            else w[1] |= c;
+        }
+    }
+    return make_uint2(w[0], w[1]);
+}
 
 struct KvAppend {
     KvPool pool;
@@ -69,69 +99,67 @@ struct KvAppend {
     const void* x[2];              // K, V: new tokens
     int64_t token_stride[2], head_stride[2];
     int32_t vec;                   // rows take 16-byte loads
+    int32_t log2_T;
 };
 
-// A CTA takes one block that gets tokens, one head, K or V: largest magnitude, step, the older codes if the step grew, the new codes.
-// Bound by the bytes of the new tokens where there are many, by latency for single ones.
-template <class T_>
+// A team of TEAM threads takes one block that gets tokens, one head, K or V: largest magnitude, step, the older codes if the step grew,
+// the new codes. A block of the grid has the teams of 128 / TEAM heads. The new tokens are on their way before the block's number is
+// known. Bound by the bytes of the new tokens where there are many, by latency (lengths; tokens and block number; the block's step) for
+// single ones.
+template <class T_, int TEAM>
 __global__ void __launch_bounds__(128) us_kv_append_kernel(const __grid_constant__ KvAppend a)
 {
     __shared__ uint32_t red[4];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const KvPool& p = a.pool;
-    const int lane = threadIdx.x & 31, h = blockIdx.y, which = blockIdx.z;
+    const int lane = threadIdx.x & 31, me = threadIdx.x % TEAM, which = blockIdx.z;
+    const int h = min((int)(blockIdx.y * (128 / TEAM) + threadIdx.x / TEAM), p.Hkv - 1);   // (teams past the last head do its work again)
     // which sequence's which block
     int s = -1, j = 0;
-    int64_t before = 0;
+    uint32_t before = 0;
     bool any_wrong = false;
+    KvSeq q = {0, 0, 0};
     for (int base = 0; base < a.seqs.S; base += 32) {
-        int cnt = 0;
+        uint32_t cnt = 0;
+        KvSeq mine = {0, 0, 0};
         if (base + lane < a.seqs.S) {
             bool wrong;
-            const KvSeq q = kv_seq(a.seqs, p, base + lane, wrong);
+            mine = kv_seq(a.seqs, p, base + lane, wrong);
             any_wrong |= wrong;
-            if (q.n > 0 && !wrong) cnt = (q.len - 1) / p.T - (q.len - q.n) / p.T + 1;
+            if (mine.n > 0 && !wrong) cnt = ((mine.len - 1) >> a.log2_T) - ((mine.len - mine.n) >> a.log2_T) + 1;
         }
-        int sum = cnt;
+        uint32_t sum = cnt;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, sum, o);
+            const uint32_t v = __shfl_up_sync(0xffffffffu, sum, o);
             if (lane >= o) sum += v;
         }
-        const bool here = (int64_t)blockIdx.x >= before + sum - cnt && (int64_t)blockIdx.x < before + sum;
-        const uint32_t who = __ballot_sync(0xffffffffu, here);
+        const uint32_t who = __ballot_sync(0xffffffffu, blockIdx.x >= before + sum - cnt && blockIdx.x < before + sum);
         if (who) {
             const int l = __ffs(who) - 1;
             s = base + l;
-            j = (int)((int64_t)blockIdx.x - before) - __shfl_sync(0xffffffffu, sum - cnt, l);
+            j = (int)(blockIdx.x - before - __shfl_sync(0xffffffffu, sum - cnt, l));
+            q.first = __shfl_sync(0xffffffffu, mine.first, l);
+            q.len = __shfl_sync(0xffffffffu, mine.len, l);
+            q.n = __shfl_sync(0xffffffffu, mine.n, l);
             break;
         }
         before += __shfl_sync(0xffffffffu, sum, 31);
     }
     if (any_wrong) atomicExch(p.err, kErrIndex);
     if (s < 0) return;
-    bool wrong;
-    const KvSeq q = kv_seq(a.seqs, p, s, wrong);
-    const int start = q.len - q.n, bi = start / p.T + j;
-    const int lo = max(start, bi * p.T), hi = min(q.len, (bi + 1) * p.T), held = lo - bi * p.T, n = hi - lo;
+    const int start = q.len - q.n, bi = (start >> a.log2_T) + j;
+    const int lo = max(start, bi << a.log2_T), hi = min(q.len, (bi + 1) << a.log2_T), held = lo - (bi << a.log2_T), n = hi - lo;
     const int32_t blk = __ldcg(a.seqs.table + (int64_t)s * a.seqs.table_stride + bi);
-    if (blk < 0 || blk >= p.blocks) {
-        if (threadIdx.x == 0) atomicExch(p.err, kErrIndex);
-        return;
-    }
-    const int D = p.D, per = D / 8;   // lanes a row
-    const int64_t place = (int64_t)blk * p.Hkv + h;
-    float* step_at = (which ? p.v_step : p.k_step) + place;
-    int8_t* codes = (which ? p.v : p.k) + place * p.T * D;
-    const float old = held ? *step_at : 0.f;
+    const int D = p.D, log2_per = D == 128 ? 4 : 3;   // D / 8 lanes a row
     const T_* x = static_cast<const T_*>(a.x[which]) + (q.first + lo - start) * a.token_stride[which] + (int64_t)h * a.head_stride[which];
-    const int units = n * per;
-    constexpr int KEEP = 4;
+    const int units = n << log2_per;
+    constexpr int KEEP = sizeof(T_) == 4 ? 4 : 8;
     Eight<T_> kept[KEEP];
     uint32_t big = 0;
     auto load = [&](int u) {
-        const int r = u / per, c = u - r * per;
+        const int r = u >> log2_per, c = u & ((1 << log2_per) - 1);
         return load8(x + r * a.token_stride[which] + 8 * c, 8, a.vec != 0);
     };
     auto take = [&](const Eight<T_>& e) {
@@ -143,82 +171,117 @@ __global__ void __launch_bounds__(128) us_kv_append_kernel(const __grid_constant
     };
 #pragma unroll
     for (int i = 0; i < KEEP; ++i)
-        if ((int)threadIdx.x + 128 * i < units) kept[i] = load(threadIdx.x + 128 * i);
+        if (me + TEAM * i < units) kept[i] = load(me + TEAM * i);
+    if (blk < 0 || blk >= p.blocks) {   // (all teams of the grid's block)
+        if (threadIdx.x == 0) atomicExch(p.err, kErrIndex);
+        return;
+    }
+    const int64_t place = (int64_t)blk * p.Hkv + h;
+    float* step_at = (which ? p.v_step : p.k_step) + place;
+    int8_t* codes = (which ? p.v : p.k) + ((place << a.log2_T) * D);
+    const float old = held ? *step_at : 0.f;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i)
-        if ((int)threadIdx.x + 128 * i < units) take(kept[i]);
-    for (int u = threadIdx.x + 128 * KEEP; u < units; u += 128) take(load(u));
+        if (me + TEAM * i < units) take(kept[i]);
+    for (int u = me + TEAM * KEEP; u < units; u += TEAM) take(load(u));
     big = __reduce_max_sync(0xffffffffu, big);
-    if (lane == 0) red[threadIdx.x >> 5] = big;
-    __syncthreads();
-    big = max(max(red[0], red[1]), max(red[2], red[3]));
-    const float step = fmaxf(old, __fdiv_rn(__uint_as_float(big), 127.f));
-    if (threadIdx.x == 0) *step_at = step;
-    const float inv = step > 0.f ? __fdiv_rn(1.f, step) : 0.f;
-    auto put = [&](int u, const Eight<T_>& e) {
-        uint32_t w[2] = {0, 0};
+    if (TEAM > 32) {
+        if (lane == 0) red[threadIdx.x >> 5] = big;
+        __syncthreads();
+        const int w0 = threadIdx.x / TEAM * (TEAM / 32);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i >> 2] |= ((uint32_t)kv_code(to_f32(e.v[i]), step, inv) & 0xFFu) << (8 * (i & 3));
-        *reinterpret_cast<uint2*>(codes + (int64_t)held * D + 8 * (int64_t)u) = make_uint2(w[0], w[1]);
-    };
+        for (int i = 0; i < TEAM / 32; ++i) big = max(big, red[w0 + i]);
+    } else {
+        __syncwarp();   // (all lanes have read the old step)
+    }
+    const float step = fmaxf(old, __fdiv_rn(__uint_as_float(big), 127.f));
+    if (me == 0) *step_at = step;
+    const float inv = step >= 1e-30f ? __fdiv_rn(1.f, step) : 0.f;
+    auto put = [&](int u, const Eight<T_>& e) { *reinterpret_cast<uint2*>(codes + (int64_t)held * D + 8 * (int64_t)u) = kv_codes8(e, step, inv); };
 #pragma unroll
     for (int i = 0; i < KEEP; ++i)
-        if ((int)threadIdx.x + 128 * i < units) put(threadIdx.x + 128 * i, kept[i]);
-    for (int u = threadIdx.x + 128 * KEEP; u < units; u += 128) put(u, load(u));
-    if (step > old && held) {   // the tokens that were there, in the larger step: RNE(code * old / step), the border decided in 64 bits
-        for (int u = threadIdx.x; u < held * D / 4; u += 128) {
-            uint32_t* at = reinterpret_cast<uint32_t*>(codes) + u;
-            const uint32_t w = *at;
-            uint32_t o = 0;
+        if (me + TEAM * i < units) put(me + TEAM * i, kept[i]);
+    for (int u = me + TEAM * KEEP; u < units; u += TEAM) put(u, load(u));
+    if (step > old && held) {   // the tokens that were there, in the larger step: RNE(code * old / step), close to a border decided in 64 bits
+        const float ratio = __fdiv_rn(old, step);   // (the product with a code is within 2^-16 of the quotient)
+        for (int u = me; u < held * D / 8; u += TEAM) {
+            uint2* at = reinterpret_cast<uint2*>(codes) + u;
+            const uint2 w = *at;
+            uint32_t o[2] = {0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const double c = (double)(int8_t)(w >> (8 * i)) * (double)old;
-                o |= ((uint32_t)(int)rint(c / (double)step) & 0xFFu) << (8 * i);
+            for (int i = 0; i < 8; ++i) {
+                const int c = (int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+                const float t = fmaf((float)c, ratio, 12582912.f);
+                uint32_t n = __float_as_uint(t);
+                if (!(fabsf(fmaf((float)c, ratio, 12582912.f - t)) < 0.49998f) || step < 1e-30f) n = (uint32_t)(int)rint((double)c * (double)old / (double)step);
+                o[i >> 2] |= (n & 0xFFu) << (8 * (i & 3));
             }
-            *at = o;
+            *at = make_uint2(o[0], o[1]);
         }
     }
 }
 
 // ---- read ------------------------------------------------------------------------------------------------------------------
-// K and V of the first `tokens` places of every sequence as values, [s][t][head][D]; 0 from a sequence's end on. A warp a row pair.
+// K and V of the first `tokens` places of every sequence as values, [s][t][head][D]; 0 from a sequence's end on. Block (x, y, z): 16 tokens
+// (in one block of the cache, as every block has a multiple of 16) of sequence z, kReadHeads heads. A thread has 16 bytes of the
+// output at a time, so that a warp's stores are whole lines, four of them in flight. Bound by the bytes written.
+constexpr int kReadHeads = 4;
 template <class T_>
-__global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int64_t tokens, T_* k_out, T_* v_out)
+__global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int64_t tokens, int log2_T, T_* k_out, T_* v_out)
 {
+    constexpr int PER = 16 / (int)sizeof(T_), U = 4;   // columns of a piece
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int per = p.D / 8;
-    const int64_t total = (int64_t)q.S * tokens * p.Hkv * per;
-    const int64_t most = (int64_t)q.width * p.T;
-    for (int64_t u = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; u < total; u += (int64_t)gridDim.x * blockDim.x) {
-        const int c = (int)(u % per);
-        const int64_t row = u / per, st = row / p.Hkv;
-        const int h = (int)(row - st * p.Hkv), s = (int)(st / tokens);
-        const int64_t t = st - s * tokens;
+    const int log2_row = (p.D == 128 ? 7 : 6) - (PER == 8 ? 3 : 2);   // pieces of a (token, head)
+    const int64_t t0 = 16 * (int64_t)blockIdx.x, most = (int64_t)q.width << log2_T;
+    const int h0 = kReadHeads * blockIdx.y;
+    for (int s = blockIdx.z; s < q.S; s += gridDim.z) {
         const int32_t len = __ldcg(q.lengths + s);
-        Eight<T_> e[2];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[0].v[i] = e[1].v[i] = from_f32<T_>(0.f);
-        if (t < len && t < most) {
-            const int32_t blk = __ldcg(q.table + (int64_t)s * q.table_stride + t / p.T);
-            if (blk >= 0 && blk < p.blocks) {
-                const int64_t place = (int64_t)blk * p.Hkv + h, at = (place * p.T + t % p.T) * p.D + 8 * c;
-                const uint2 w[2] = {__ldcg(reinterpret_cast<const uint2*>(p.k + at)), __ldcg(reinterpret_cast<const uint2*>(p.v + at))};
-                const float f[2] = {__ldcg(p.k_step + place), __ldcg(p.v_step + place)};
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) e[b].v[i] = from_f32<T_>((float)(int8_t)((i < 4 ? w[b].x : w[b].y) >> (8 * (i & 3))) * f[b]);
-            } else {
-                atomicExch(p.err, kErrIndex);
-            }
-        } else if (t < len || len < 0) {
-            atomicExch(p.err, kErrIndex);
+        const bool wrong = len < 0 || len > most;
+        const int seen = (int)max((int64_t)0, min((int64_t)16, min((int64_t)len, most) - t0));   // tokens here that the sequence has
+        int32_t blk = 0;
+        bool there = false;
+        if (seen > 0) {
+            blk = __ldcg(q.table + (int64_t)s * q.table_stride + (t0 >> log2_T));
+            there = blk >= 0 && blk < p.blocks;
         }
+        if (threadIdx.x == 0 && (wrong || (seen > 0 && !there))) atomicExch(p.err, kErrIndex);
+        const int here = (int)min((int64_t)16, tokens - t0), units = here * kReadHeads << log2_row;
+        const int64_t place0 = (int64_t)blk * p.Hkv, tok0 = t0 & ((1 << log2_T) - 1), out0 = (s * tokens + t0) * p.Hkv;
+#pragma unroll 1
+        for (int u0 = threadIdx.x; u0 < units; u0 += U * 256) {
+            uint2 w[U][2];
+            float f[U][2];
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(Eight<T_>) / 16; ++i) {
-            reinterpret_cast<uint4*>(k_out + row * p.D + 8 * c)[i] = reinterpret_cast<const uint4*>(&e[0])[i];
-            reinterpret_cast<uint4*>(v_out + row * p.D + 8 * c)[i] = reinterpret_cast<const uint4*>(&e[1])[i];
+            for (int i = 0; i < U; ++i) {
+                const int u = u0 + 256 * i, row = u >> log2_row, c = u & ((1 << log2_row) - 1), t = row / kReadHeads, h = h0 + row % kReadHeads;
+                w[i][0] = w[i][1] = make_uint2(0, 0);
+                f[i][0] = f[i][1] = 0.f;
+                if (u < units && h < p.Hkv && there && t < seen) {
+                    const int64_t at = (((place0 + h) << log2_T) + tok0 + t) * p.D + PER * c;
+                    if (PER == 8) {
+                        w[i][0] = __ldcg(reinterpret_cast<const uint2*>(p.k + at));
+                        w[i][1] = __ldcg(reinterpret_cast<const uint2*>(p.v + at));
+                    } else {
+                        w[i][0].x = __ldcg(reinterpret_cast<const uint32_t*>(p.k + at));
+                        w[i][1].x = __ldcg(reinterpret_cast<const uint32_t*>(p.v + at));
+                    }
+                    f[i][0] = __ldcg(p.k_step + place0 + h);
+                    f[i][1] = __ldcg(p.v_step + place0 + h);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int u = u0 + 256 * i, row = u >> log2_row, c = u & ((1 << log2_row) - 1), t = row / kReadHeads, h = h0 + row % kReadHeads;
+                if (u >= units || h >= p.Hkv) continue;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    union { uint4 v; T_ e[PER]; } y;
+#pragma unroll
+                    for (int k = 0; k < PER; ++k) y.e[k] = from_f32<T_>((float)(int8_t)((k < 4 ? w[i][b].x : w[i][b].y) >> (8 * (k & 3))) * f[i][b]);
+                    __stcs(reinterpret_cast<uint4*>((b ? v_out : k_out) + (out0 + (int64_t)t * p.Hkv + h) * p.D + PER * c), y.v);
+                }
+            }
         }
     }
 }

@@ -117,6 +117,19 @@ __device__ __forceinline__ uint32_t mx4_quantize_row(const Eight<T>& x, uint32_t
     return codes;
 }
 
+// Unit u of rows of `per` units: its row and its place there. (A 64-bit division takes longer than a unit's arithmetic.)
+__device__ __forceinline__ void mx4_unit(int64_t u, int64_t per, int64_t& row, int64_t& place)
+{
+    if ((u | per) >> 32) {
+        row = u / per;
+        place = u - row * per;
+    } else {
+        const uint32_t r = (uint32_t)u / (uint32_t)per;
+        row = r;
+        place = (uint32_t)u - r * (uint32_t)per;
+    }
+}
+
 // X (rows x K, row stride ldx) -> tiles. A warp takes one row of kUnroll consecutive tiles at a time: all loads first. Memory bound
 // (8192 x 8192 bf16: 170 MB).
 constexpr int kMxUnroll = 4;
@@ -128,7 +141,9 @@ __global__ void __launch_bounds__(256) us_mx4_quantize_kernel(const T* X, int64_
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     for (int64_t u = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; u < rows * groups; u += ((int64_t)gridDim.x * blockDim.x) >> 5) {
-        const int64_t r = u / groups, j0 = (u - r * groups) * kMxUnroll;
+        int64_t r, j0;
+        mx4_unit(u, groups, r, j0);
+        j0 *= kMxUnroll;
         Eight<T> x[kMxUnroll];
 #pragma unroll
         for (int i = 0; i < kMxUnroll; ++i) {
@@ -149,12 +164,19 @@ __global__ void __launch_bounds__(256) us_mx4_quantize_kernel(const T* X, int64_
     }
 }
 
-// E2M1 -> fp32: 3 bits of exponent and mantissa over 1 (values below 1: 0 and 0.5)
-__device__ __forceinline__ float mx4_value(uint32_t code)
+// eight codes -> their values
+__device__ __forceinline__ void mx4_values8(uint32_t w, float (&v)[8])
 {
-    const uint32_t m = code & 7u;
-    const float a = m < 2u ? 0.5f * (float)m : __uint_as_float(((126u + (m >> 1)) << 23) | ((m & 1u) << 22));
-    return (code & 8u) ? -a : a;
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+    }
 }
 // 2^(byte - 127)
 __device__ __forceinline__ float mx4_scale(uint32_t byte)
@@ -171,7 +193,9 @@ __global__ void __launch_bounds__(256) us_mx4_dequantize_kernel(const uint8_t* m
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     for (int64_t u = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; u < rows * groups; u += ((int64_t)gridDim.x * blockDim.x) >> 5) {
-        const int64_t r = u / groups, j0 = (u - r * groups) * kMxUnroll;
+        int64_t r, j0;
+        mx4_unit(u, groups, r, j0);
+        j0 *= kMxUnroll;
         const uint8_t* tile = mx + ((r >> 7) * kt + j0) * kMxTile;
         const uint32_t rr = (uint32_t)(r & 127);
         uint32_t w[kMxUnroll], b[kMxUnroll];
@@ -187,8 +211,10 @@ __global__ void __launch_bounds__(256) us_mx4_dequantize_kernel(const uint8_t* m
             if (k >= K) break;
             const float s = mx4_scale(b[i]);
             Eight<T> y;
+            float v[8];
+            mx4_values8(w[i], v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y.v[e] = from_f32<T>(mx4_value(w[i] >> (4 * e)) * s);
+            for (int e = 0; e < 8; ++e) y.v[e] = from_f32<T>(v[e] * s);
             T* dst = out + r * ldo + k;
             if (vec && k + 8 <= K) {
 #pragma unroll
@@ -211,7 +237,8 @@ __global__ void __launch_bounds__(256) us_mx4_repack_kernel(uint8_t* codes, int6
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     for (int64_t u = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; u < rows * kt; u += ((int64_t)gridDim.x * blockDim.x) >> 5) {
-        const int64_t r = u / kt, j = u - r * kt;
+        int64_t r, j;
+        mx4_unit(u, kt, r, j);
         uint8_t* tile = mx + ((r >> 7) * kt + j) * kMxTile;
         const uint32_t rr = (uint32_t)(r & 127);
         uint32_t* word = reinterpret_cast<uint32_t*>(tile + mx4_code_off(rr, lane >> 2) + 4 * (lane & 3));
