@@ -61,6 +61,13 @@ bool type_ok(int32_t t) { return t >= 0 && t <= 2; }
 int64_t size_of(int32_t t) { return t == US_F32 ? 4 : 2; }
 bool aligned(const void* p, int64_t b) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)b == 0; }
 bool rows_vec(const void* p, int64_t ld, int64_t size) { return aligned(p, 16) && ld * size % 16 == 0; }
+// Bytes of an access to rows: 32, 16, 8, 4, or 1 (an element at a time).
+int access(const void* p, int64_t ld, int64_t size)
+{
+    for (int b = 32; b >= 4; b /= 2)
+        if (aligned(p, b) && ld * size % b == 0) return b;
+    return 1;
+}
 us_status cuda(cudaError_t e)
 {
     if (e == cudaSuccess) return US_OK;
@@ -116,8 +123,8 @@ us_status us_mx4_quantize(const void* X, int32_t x_type, int64_t ldx, int64_t ro
     if (rows == 1) ldx = 0;   // (a single row's stride means nothing)
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint8_t* out = static_cast<uint8_t*>(mx);
-    int vec = rows_vec(X, ldx, size_of(x_type));
-    const dim3 g = warps_grid(rows * mx4_tiles(mx4_tiles(K, 256), kMxUnroll));
+    int vec = access(X, ldx, size_of(x_type));
+    const dim3 g = warps_grid(rows * mx4_tiles(mx4_tiles(K, 256), 2 * kMxUnroll));
     const void* k = x_type == US_F16 ? (const void*)us_mx4_quantize_kernel<__half> :
                     x_type == US_BF16 ? (const void*)us_mx4_quantize_kernel<__nv_bfloat16> : (const void*)us_mx4_quantize_kernel<float>;
     void* args[] = {&X, &ldx, &rows, &K, &out, &vec};
@@ -130,8 +137,8 @@ us_status us_mx4_dequantize(const void* mx, int64_t rows, int64_t K, void* out, 
     if (rows == 0) return US_OK;
     if (!mx || !out || (rows > 1 && ldo < K) || !aligned(out, size_of(type)) || !aligned(mx, 16)) return US_ERR_INVALID_ARG;
     if (rows == 1) ldo = 0;
-    int vec = rows_vec(out, ldo, size_of(type));
-    const dim3 g = warps_grid(rows * mx4_tiles(mx4_tiles(K, 256), kMxUnroll));
+    int vec = access(out, ldo, size_of(type));
+    const dim3 g = warps_grid(rows * mx4_tiles(mx4_tiles(K, 256), 2 * kMxUnroll));
     const void* k = type == US_F16 ? (const void*)us_mx4_dequantize_kernel<__half> :
                     type == US_BF16 ? (const void*)us_mx4_dequantize_kernel<__nv_bfloat16> : (const void*)us_mx4_dequantize_kernel<float>;
     void* args[] = {&mx, &rows, &K, &out, &ldo, &vec};

@@ -130,36 +130,134 @@ __device__ __forceinline__ void mx4_unit(int64_t u, int64_t per, int64_t& row, i
     }
 }
 
-// X (rows x K, row stride ldx) -> tiles. A warp takes one row of kUnroll consecutive tiles at a time: all loads first. Memory bound
-// (8192 x 8192 bf16: 170 MB).
-constexpr int kMxUnroll = 4;
+// 32 bytes in one access
+__device__ __forceinline__ void load32b(const void* p, uint32_t* w)
+{
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void store32b(void* p, const uint32_t* w)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+// Sixteen elements of a row as they are, in 32-bit words. vec: bytes of an access (32, 16, 8, 4, or 1: one element at a time).
+template <class T>
+struct Sixteen {
+    uint32_t w[4 * sizeof(T)];
+};
+template <class T>
+__device__ __forceinline__ void load16(Sixteen<T>& r, const T* p, int64_t left, int vec)
+{
+    constexpr int W = 4 * (int)sizeof(T);
+    if (left >= 16 && vec == 32) {
+#pragma unroll
+        for (int i = 0; i < W; i += 8) load32b(reinterpret_cast<const uint32_t*>(p) + i, r.w + i);
+    } else if (left >= 16 && vec == 16) {
+#pragma unroll
+        for (int i = 0; i < W; i += 4) {
+            const uint4 v = __ldcg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p) + i));
+            r.w[i] = v.x; r.w[i + 1] = v.y; r.w[i + 2] = v.z; r.w[i + 3] = v.w;
+        }
+    } else if (left >= 16 && vec == 8) {
+#pragma unroll
+        for (int i = 0; i < W; i += 2) {
+            const uint2 v = __ldcg(reinterpret_cast<const uint2*>(reinterpret_cast<const uint32_t*>(p) + i));
+            r.w[i] = v.x; r.w[i + 1] = v.y;
+        }
+    } else if (left >= 16 && vec == 4) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) r.w[i] = __ldcg(reinterpret_cast<const uint32_t*>(p) + i);
+    } else {
+        union { uint32_t w[W]; T v[16]; } u;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) u.v[i] = i < left ? p[i] : from_f32<T>(0.f);
+#pragma unroll
+        for (int i = 0; i < W; ++i) r.w[i] = u.w[i];
+    }
+}
+// The bits of the largest magnitude of sixteen, as an fp32's
+template <class T>
+__device__ __forceinline__ uint32_t amax16(const Sixteen<T>& x)
+{
+    uint32_t m[4 * sizeof(T)];
+#pragma unroll
+    for (int i = 0; i < 4 * (int)sizeof(T); ++i) m[i] = x.w[i] & (sizeof(T) == 2 ? 0x7FFF7FFFu : 0x7FFFFFFFu);
+    if (sizeof(T) == 4) {
+#pragma unroll
+        for (int n = 8; n; n >>= 1)
+#pragma unroll
+            for (int i = 0; i < n; ++i) m[i] = max(m[i], m[(i + n) % (4 * sizeof(T))]);
+        return m[0];
+    }
+#pragma unroll
+    for (int n = 4; n; n >>= 1)   // (magnitudes order like their bits: both halves at once)
+#pragma unroll
+        for (int i = 0; i < n; ++i) m[i] = __vmaxu2(m[i], m[i + n]);
+    const uint32_t b = max(m[0] & 0xFFFFu, m[0] >> 16);
+    return std::is_same<T, __half>::value ? __float_as_uint(__half2float(__ushort_as_half((unsigned short)b))) : b << 16;
+}
+template <class T>
+__device__ __forceinline__ void pair16(const Sixteen<T>& x, int i, float& a, float& b)   // elements 2 i, 2 i + 1
+{
+    if (sizeof(T) == 4) {
+        a = __uint_as_float(x.w[2 * i % (4 * sizeof(T))]);
+        b = __uint_as_float(x.w[(2 * i + 1) % (4 * sizeof(T))]);
+    } else if (std::is_same<T, __half>::value) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x.w[i]));
+        a = f.x;
+        b = f.y;
+    } else {
+        a = __uint_as_float(x.w[i] << 16);
+        b = __uint_as_float(x.w[i] & 0xFFFF0000u);
+    }
+}
+
+// X (rows x K, row stride ldx) -> tiles. A warp takes 512 columns of a row (two tiles), sixteen a lane, two lanes a block; kMxUnroll of
+// them at a time, all loads first. With eight columns a lane the arithmetic around the elements kept the GPU at half its memory's rate
+// (8192 x 8192 bf16, 170 MB: 38 us).
+constexpr int kMxUnroll = 2;
 template <class T>
 __global__ void __launch_bounds__(256) us_mx4_quantize_kernel(const T* X, int64_t ldx, int64_t rows, int64_t K, uint8_t* mx, int vec)
 {
     const int lane = threadIdx.x & 31;
-    const int64_t kt = mx4_tiles(K, 256), groups = mx4_tiles(kt, kMxUnroll);
+    const int64_t kt = mx4_tiles(K, 256), groups = mx4_tiles(kt, 2 * kMxUnroll);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     for (int64_t u = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; u < rows * groups; u += ((int64_t)gridDim.x * blockDim.x) >> 5) {
         int64_t r, j0;
         mx4_unit(u, groups, r, j0);
-        j0 *= kMxUnroll;
-        Eight<T> x[kMxUnroll];
+        j0 = 2 * kMxUnroll * j0 + (lane >> 4);   // the lane's tile
+        const int l = lane & 15;
+        const T* src = X + r * ldx + 256 * j0 + 16 * l;
+        Sixteen<T> x[kMxUnroll];
 #pragma unroll
-        for (int i = 0; i < kMxUnroll; ++i) {
-            const int64_t k = 256 * (j0 + i) + 8 * lane;
-            x[i] = load8(X + r * ldx + k, K - k, vec && k + 8 <= K);
-        }
-        uint8_t* tile = mx + ((r >> 7) * kt + j0) * kMxTile;
+        for (int i = 0; i < kMxUnroll; ++i) load16(x[i], src + 512 * i, K - 256 * (j0 + 2 * i) - 16 * l, vec);
         const uint32_t rr = (uint32_t)(r & 127);
+        uint8_t* tile = mx + ((r >> 7) * kt + j0) * kMxTile;
+        const uint32_t at_code = mx4_code_off(rr, l >> 1) + 8 * (l & 1), at_scale = mx4_scale_off(rr, l >> 3);
 #pragma unroll
         for (int i = 0; i < kMxUnroll; ++i) {
-            if (j0 + i >= kt) break;
-            uint32_t sc;
-            const uint32_t codes = mx4_quantize_row(x[i], sc);
-            *reinterpret_cast<uint32_t*>(tile + mx4_code_off(rr, lane >> 2) + 4 * (lane & 3)) = codes;
-            if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(tile + mx4_scale_off(rr, lane >> 4)) = sc;
-            tile += kMxTile;
+            uint32_t big = amax16(x[i]);
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+            const uint32_t byte = mx4_scale_byte(big);
+            const float inv = mx4_inverse(byte);
+            uint32_t c[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float f[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pair16(x[i], 4 * h + e, f[2 * e], f[2 * e + 1]);
+                c[h] = mx4_codes8(f, inv);
+            }
+            // the four scale bytes of the lane's half, in its first lane of eight
+            uint32_t s = byte | (__shfl_down_sync(0xffffffffu, byte, 2) << 8);
+            s |= __shfl_down_sync(0xffffffffu, s, 4) << 16;
+            if (j0 + 2 * i < kt) {
+                *reinterpret_cast<uint2*>(tile + at_code) = byte == 255u ? make_uint2(0, 0) : make_uint2(c[0], c[1]);
+                if ((l & 7) == 0) *reinterpret_cast<uint32_t*>(tile + at_scale) = s;
+            }
+            tile += 2 * kMxTile;
         }
     }
 }
@@ -184,46 +282,63 @@ __device__ __forceinline__ float mx4_scale(uint32_t byte)
     return byte == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(byte ? byte << 23 : 0x00400000u);
 }
 
-// Tiles -> values, a warp a row of a tile, eight columns a lane.
+// Tiles -> values: 512 columns of a row a warp, sixteen a lane, as above.
 template <class T>
 __global__ void __launch_bounds__(256) us_mx4_dequantize_kernel(const uint8_t* mx, int64_t rows, int64_t K, T* out, int64_t ldo, int vec)
 {
+    constexpr int W = 4 * (int)sizeof(T);
     const int lane = threadIdx.x & 31;
-    const int64_t kt = mx4_tiles(K, 256), groups = mx4_tiles(kt, kMxUnroll);
+    const int64_t kt = mx4_tiles(K, 256), groups = mx4_tiles(kt, 2 * kMxUnroll);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     for (int64_t u = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; u < rows * groups; u += ((int64_t)gridDim.x * blockDim.x) >> 5) {
         int64_t r, j0;
         mx4_unit(u, groups, r, j0);
-        j0 *= kMxUnroll;
-        const uint8_t* tile = mx + ((r >> 7) * kt + j0) * kMxTile;
+        j0 = 2 * kMxUnroll * j0 + (lane >> 4);
+        const int l = lane & 15;
         const uint32_t rr = (uint32_t)(r & 127);
-        uint32_t w[kMxUnroll], b[kMxUnroll];
+        const uint8_t* tile = mx + ((r >> 7) * kt + j0) * kMxTile;
+        const uint32_t at_code = mx4_code_off(rr, l >> 1) + 8 * (l & 1), at_scale = mx4_scale_off(rr, l >> 3) + ((l >> 1) & 3);
+        uint2 w[kMxUnroll];
+        uint32_t b[kMxUnroll];
 #pragma unroll
         for (int i = 0; i < kMxUnroll; ++i) {
-            const bool in = j0 + i < kt;
-            w[i] = in ? __ldcg(reinterpret_cast<const uint32_t*>(tile + i * kMxTile + mx4_code_off(rr, lane >> 2) + 4 * (lane & 3))) : 0u;
-            b[i] = in ? __ldcg(tile + i * kMxTile + mx4_scale_off(rr, lane >> 4) + ((lane >> 2) & 3)) : 0u;
+            const bool in = j0 + 2 * i < kt;
+            w[i] = in ? __ldcg(reinterpret_cast<const uint2*>(tile + 2 * i * kMxTile + at_code)) : make_uint2(0, 0);
+            b[i] = in ? __ldcg(tile + 2 * i * kMxTile + at_scale) : 0u;
         }
+        T* dst = out + r * ldo + 256 * j0 + 16 * l;
 #pragma unroll
         for (int i = 0; i < kMxUnroll; ++i) {
-            const int64_t k = 256 * (j0 + i) + 8 * lane;
-            if (k >= K) break;
+            const int64_t left = K - 256 * (j0 + 2 * i) - 16 * l;
+            if (left <= 0) break;
             const float s = mx4_scale(b[i]);
-            Eight<T> y;
-            float v[8];
-            mx4_values8(w[i], v);
+            union { uint32_t w[W]; T v[16]; } y;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y.v[e] = from_f32<T>(v[e] * s);
-            T* dst = out + r * ldo + k;
-            if (vec && k + 8 <= K) {
+            for (int h = 0; h < 2; ++h) {
+                float v[8];
+                mx4_values8(h ? w[i].y : w[i].x, v);
 #pragma unroll
-                for (int q = 0; q < (int)sizeof(Eight<T>) / 16; ++q) reinterpret_cast<uint4*>(dst)[q] = reinterpret_cast<const uint4*>(&y)[q];
+                for (int e = 0; e < 8; ++e) y.v[8 * h + e] = from_f32<T>(v[e] * s);
+            }
+            if (left >= 16 && vec == 32) {
+#pragma unroll
+                for (int k = 0; k < W; k += 8) store32b(reinterpret_cast<uint32_t*>(dst) + k, y.w + k);
+            } else if (left >= 16 && vec == 16) {
+#pragma unroll
+                for (int k = 0; k < W; k += 4) *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(dst) + k) = make_uint4(y.w[k], y.w[k + 1], y.w[k + 2], y.w[k + 3]);
+            } else if (left >= 16 && vec == 8) {
+#pragma unroll
+                for (int k = 0; k < W; k += 2) *reinterpret_cast<uint2*>(reinterpret_cast<uint32_t*>(dst) + k) = make_uint2(y.w[k], y.w[k + 1]);
+            } else if (left >= 16 && vec == 4) {
+#pragma unroll
+                for (int k = 0; k < W; ++k) reinterpret_cast<uint32_t*>(dst)[k] = y.w[k];
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (k + e < K) dst[e] = y.v[e];
+                for (int e = 0; e < 16; ++e)
+                    if (e < left) dst[e] = y.v[e];
             }
+            dst += 512;
         }
     }
 }
