@@ -334,8 +334,9 @@ us_status us_mx4_last_error(void);
  *   lengths      tokens of each sequence, this call's new ones included.
  *   cu_tokens    n_seqs + 1 entries: rows [cu[s], cu[s + 1]) of the call's N rows are the new tokens of sequence s, its last ones.
  *                NULL: one row each (N = n_seqs).
+ * A sequence of length 0 may have rows (those of a padded batch): nothing is appended for them, and their attention is 0.
  * Where an entry does not fit (a block number outside the pool, a length below 0 or beyond the table, more new tokens
- * than the length, cu_tokens that fall or pass N), kernels leave out what it stands for, touch nothing outside the arrays, and
+ * than a length above 0, cu_tokens that fall or pass N), kernels leave out what it stands for, touch nothing outside the arrays, and
  * us_kv_last_error, which synchronises the device, reports (and clears) US_ERR_DEVICE_INDEX; US_ERR_DEVICE_TIMEOUT as elsewhere.
  *
  * us_kv_append: writes the new tokens. For each block and head that gets some:

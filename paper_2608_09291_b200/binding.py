@@ -364,6 +364,8 @@ class Mx4:
     """A dense (rows, K) matrix of E2M1 values with a power-of-two scale for 32 columns of a row, on a CUDA device, in the library's
     tiles (``data``, uint8). Made by ``mx4_quantize`` and ``mx4_from_codes``."""
 
+    __slots__ = ("rows", "K", "data", "frozen", "__weakref__")
+
     def __init__(self, rows: int, K: int, data=None, device="cuda"):
         import torch
         _native()
@@ -397,9 +399,8 @@ def mx4_quantize(X, out: Mx4 | None = None, stream=None) -> Mx4:
     ext = _ext or _native()
     if out is None:
         m = Mx4.__new__(Mx4)
-        m.rows, m.K = X.shape
+        m.data, m.rows, m.K = ext.mx4_quantize(X, None, stream)
         m.frozen = False
-        m.data = ext.mx4_quantize(X, None, stream)
         return m
     if out.frozen or (out.rows, out.K) != tuple(X.shape):
         raise ValueError("out must be an unfrozen Mx4 of X's shape")

@@ -48,7 +48,8 @@ namespace {
 
 us_status error_word(uint32_t** err)
 {
-    return cuda(cudaGetSymbolAddress((void**)err, g_kv_err));
+    static void* kept[kMaxDevices];
+    return cuda(ops_symbol(kept, &g_kv_err, reinterpret_cast<void**>(err)));
 }
 
 // The codes as rows of D bytes; a copy brings a block's tokens, 64 at most, swizzled over a row's 128 (64) bytes.

@@ -29,9 +29,10 @@ struct KvPool {
 
 struct KvSeq {
     int64_t first;      // row of its first new token
-    int32_t len, n;     // tokens in all, new ones
+    int32_t len, n;     // tokens in all, new ones (which may be more only where the sequence is empty, or wrong)
 };
-// Sequence s with everything that memory depends on brought into range; `wrong`: something was not.
+// Sequence s with everything that memory depends on brought into range; `wrong`: something was not. (An empty sequence may have rows: those
+// of a padded batch.)
 __device__ __forceinline__ KvSeq kv_seq(const KvSeqs& q, const KvPool& p, int s, bool& wrong)
 {
     KvSeq r;
@@ -39,10 +40,10 @@ __device__ __forceinline__ KvSeq kv_seq(const KvSeqs& q, const KvPool& p, int s,
     const int32_t len = __ldcg(q.lengths + s);
     int64_t a = s, b = (int64_t)s + 1;
     if (q.cu) { a = __ldcg(q.cu + s); b = __ldcg(q.cu + s + 1); }
-    wrong = len < 0 || len > most || a < 0 || b < a || b > q.N || b - a > len;
+    wrong = len < 0 || len > most || a < 0 || b < a || b > q.N || (len > 0 && b - a > len);
     r.len = (int32_t)max((int64_t)0, min((int64_t)len, most));
     r.first = max((int64_t)0, min(a, q.N));
-    r.n = (int32_t)max((int64_t)0, min(min(b, q.N) - r.first, (int64_t)r.len));
+    r.n = (int32_t)max((int64_t)0, min(b, q.N) - r.first);
     return r;
 }
 
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(128) us_kv_append_kernel(const __grid_constant
             bool wrong;
             mine = kv_seq(a.seqs, p, base + lane, wrong);
             any_wrong |= wrong;
-            if (mine.n > 0 && !wrong) cnt = ((mine.len - 1) >> a.log2_T) - ((mine.len - mine.n) >> a.log2_T) + 1;
+            if (mine.n > 0 && mine.n <= mine.len && !wrong) cnt = ((mine.len - 1) >> a.log2_T) - ((mine.len - mine.n) >> a.log2_T) + 1;
         }
         uint32_t sum = cnt;
 #pragma unroll

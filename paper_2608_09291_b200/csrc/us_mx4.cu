@@ -83,8 +83,9 @@ bool shape_ok(int64_t rows, int64_t K) { return rows >= 0 && rows < (1ll << 31) 
 us_status product(const void* X, int32_t x_type, int64_t ldx, const void* x_mx, int64_t N, const void* w_mx, int64_t M, int64_t K, void* Y,
                   int32_t y_type, int64_t ldy, const Plan& pl, uint32_t flags, cudaStream_t st)
 {
-    uint32_t* err = nullptr;
-    if (cudaGetSymbolAddress((void**)&err, g_mx4_err) != cudaSuccess) { cudaGetLastError(); return US_ERR_CUDA; }
+    static void* kept[kMaxDevices];
+    void* err = nullptr;
+    if (ops_symbol(kept, &g_mx4_err, &err) != cudaSuccess) { cudaGetLastError(); return US_ERR_CUDA; }
     Mx4Params p = {};
     p.w = static_cast<const uint8_t*>(w_mx);
     p.x = static_cast<const uint8_t*>(x_mx);
@@ -97,7 +98,7 @@ us_status product(const void* X, int32_t x_type, int64_t ldx, const void* x_mx, 
     p.x_vec = X && rows_vec(X, ldx, size_of(x_type));
     p.y_vec = rows_vec(Y, N > 1 ? ldy : 0, size_of(y_type));
     p.w_stable = (flags & US_MX4_W_STABLE) != 0;
-    p.err = err;
+    p.err = static_cast<uint32_t*>(err);
     const cudaError_t e = ops_kernel_allow(pl.kernel);
     if (e != cudaSuccess) return cuda(e);
     void* args[] = {&p};

@@ -16,7 +16,7 @@ bool pdl()
 }
 std::mutex g_lock;
 std::set<std::pair<int, const void*>> g_allowed;
-int g_sms[64];
+int g_sms[kMaxDevices];
 }  // namespace
 
 cudaError_t ops_launch(const void* kernel, dim3 grid, int block, int64_t smem, cudaStream_t st, void** args, unsigned cluster)
@@ -51,10 +51,22 @@ cudaError_t ops_kernel_allow(const void* kernel)
     return e;
 }
 
+cudaError_t ops_symbol(void** kept, const void* symbol, void** address)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaGetSymbolAddress(address, symbol);
+    std::lock_guard<std::mutex> hold(g_lock);
+    if (!kept[dev]) e = cudaGetSymbolAddress(&kept[dev], symbol);
+    *address = kept[dev];
+    return e;
+}
+
 int ops_sms()
 {
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 148; }
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return 148; }
     std::lock_guard<std::mutex> hold(g_lock);
     if (!g_sms[dev] && cudaDeviceGetAttribute(&g_sms[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return 148; }
     return g_sms[dev];

@@ -18,5 +18,8 @@ cudaError_t ops_launch(const void* kernel, dim3 grid, int block, int64_t smem, c
 cudaError_t ops_kernel_allow(const void* kernel);
 // SMs of the current device (148 where there is none).
 int ops_sms();
+// Address of a __device__ variable on the current device; `kept`: the caller's static array of what was found (by device).
+constexpr int kMaxDevices = 64;
+cudaError_t ops_symbol(void** kept, const void* symbol, void** address);
 
 }  // namespace us

@@ -253,7 +253,7 @@ PyObject* give(PyObject* o, at::Tensor&& fresh)
     return o;
 }
 
-// mx4_quantize(X, mx, stream) -> the tiles
+// mx4_quantize(X, mx, stream) -> (the tiles, rows, K)
 PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     if (n != 3) return PyErr_Format(PyExc_TypeError, "mx4_quantize takes 3 arguments");
@@ -280,7 +280,8 @@ PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n)
     s = us_mx4_quantize(X->data_ptr(), type_of(X->scalar_type()), row_stride(*X), rows, K, mx->data_ptr(), at_.stream);
     Py_END_ALLOW_THREADS
     if (s != US_OK) return fail(s, "us_mx4_quantize");
-    return give(a[1], std::move(fresh));
+    PyObject* tiles = give(a[1], std::move(fresh));
+    return tiles ? Py_BuildValue("NLL", tiles, (long long)rows, (long long)K) : nullptr;
     END_HANDLE_TH_ERRORS
 }
 
