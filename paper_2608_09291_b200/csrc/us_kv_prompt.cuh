@@ -61,6 +61,27 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+// two fp32 in one instruction
+__device__ __forceinline__ uint64_t f32x2(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void f32x2_split(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // The sequence and row tile of row tile `index` of the batch; row tiles of a sequence with the latest tokens (that see most) first.
 // rows: query rows of a head in the tile.
 struct PrItem {
@@ -253,7 +274,9 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                 for (int c = 0; c < 4; ++c) pin32(x[c]);
                 // which of the unit's tokens the row sees
                 uint32_t sees[4];
-                float mx = -INFINITY;
+                float mx = -INFINITY, fk[8];
+#pragma unroll
+                for (int g = 0; g < 8; ++g) fk[g] = f * st[g].x;
                 if (!fast) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -273,7 +296,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
 #pragma unroll
                         for (int i = 0; i < 14; i += 2) v = max3(v, __uint_as_float(x[c][16 * g + i]), __uint_as_float(x[c][16 * g + i + 1]));
                         v = fmaxf(v, __uint_as_float(x[c][16 * g + 14]));
-                        mx = fmaxf(mx, v * (f * fmaxf(st[2 * c + g].x, 0.f)));   // (a group that is not there: -inf x 0, no maximum)
+                        mx = fmaxf(mx, v * fmaxf(fk[2 * c + g], 0.f));   // (a group that is not there: -inf x 0, no maximum)
                     }
                 // a new maximum, only where the old one is 2^8 behind
                 float alpha = grow;
@@ -309,15 +332,20 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
                             const float4 s4 = st[2 * c + g];
-                            const float k = f * s4.x, b = base + (s4.z - lref);
-                            float p0 = 0.f, p1 = 0.f;
+                            const float k = fk[2 * c + g], b = base + (s4.z - lref);
+                            const uint64_t k2 = f32x2(k, k), b2 = f32x2(b, b);
+                            uint64_t part = 0;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
-                                const float e0 = exp2_fast(fmaf(__uint_as_float(x[c][16 * g + 2 * i]), k, b)), e1 = exp2_fast(fmaf(__uint_as_float(x[c][16 * g + 2 * i + 1]), k, b));
-                                p0 += e0;
-                                p1 += e1;
+                                float e0, e1;
+                                f32x2_split(fma2(f32x2(__uint_as_float(x[c][16 * g + 2 * i]), __uint_as_float(x[c][16 * g + 2 * i + 1])), k2, b2), e0, e1);
+                                e0 = exp2_fast(e0);
+                                e1 = exp2_fast(e1);
+                                part = add2(part, f32x2(e0, e1));
                                 y[8 * g + i] = half2_bits(e0, e1);
                             }
+                            float p0, p1;
+                            f32x2_split(part, p0, p1);
                             sum = fmaf(p0 + p1, ref * s4.w, sum);   // (p without V's step)
                         }
                         tc_st16_lanes(t_s + 16u * c, y);
@@ -331,7 +359,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
                             const float2 kv = *reinterpret_cast<const float2*>(&st[2 * c + g]);
-                            const float k = f * kv.x, rel = kv.y == ref ? 1.f : __fdiv_rn(kv.y, ref);
+                            const float k = fk[2 * c + g], rel = kv.y == ref ? 1.f : __fdiv_rn(kv.y, ref);
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 float e[2];
@@ -416,7 +444,8 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
         const int first_seen = a.window > 0 ? max(0, it.seq.len - it.seq.n + it.row0 / a.G - a.window + 1) : 0;
         // The block numbers of a unit are loaded two units ahead, its steps one: nothing here waits for a load that was just issued.
         int32_t blk[2] = {-1, -1};
-        int64_t at[2] = {-1, -1};   // first byte of the two groups, -1: not there
+        int64_t at[2] = {0, 0};   // the lane's first byte of the two groups (of the pool's first where a group is not there: its p is 0)
+        const int64_t lane_at = (lane >> 2) * D + 16 * (lane & 3);
         float2 st[2];
         bool missing = false;
         auto token = [&](int j, int g) { return (u0 + j) * kPrTile + 32 * w + 16 * g; };
@@ -433,13 +462,13 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             for (int g = 0; g < 2; ++g) {
                 const int t = token(j, g);
                 const bool in = (uint32_t)blk[g] < (uint32_t)p.blocks;
-                at[g] = -1;
+                at[g] = lane_at;
                 st[g] = make_float2(-1.f, 0.f);
                 if (needed(j, t)) {
                     missing |= !in;
                     if (in) {
                         const int64_t place = (int64_t)blk[g] * p.Hkv + h;
-                        at[g] = ((place << a.log2_T) + (t & (p.T - 1))) * D;
+                        at[g] = ((place << a.log2_T) + (t & (p.T - 1))) * D + lane_at;
                         st[g] = make_float2(__ldcg(p.k_step + place), __ldcg(p.v_step + place));
                     }
                 }
@@ -451,9 +480,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
 #pragma unroll
             for (int i = 0; i < IN; ++i) {
                 const int half = i % HALVES, t8 = i / HALVES;   // tokens 8 t8 .. of the warp's 32
-                const int64_t b = at[t8 >> 1];
-                x[i] = make_uint4(0, 0, 0, 0);
-                if (b >= 0) x[i] = __ldcg(reinterpret_cast<const uint4*>(base + b + (8 * (t8 & 1) + (lane >> 2)) * D + 64 * half + 16 * (lane & 3)));
+                x[i] = __ldcg(reinterpret_cast<const uint4*>(base + at[t8 >> 1] + 8 * (t8 & 1) * D + 64 * half));
             }
         };
         auto store = [&](uint8_t* base, const uint4 (&x)[IN]) {
