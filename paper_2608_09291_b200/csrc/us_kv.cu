@@ -280,7 +280,7 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
         us_status s = error_word(&a.pool.err);
         if (s != US_OK) return s;
         void* args[] = {&a};
-        cudaError_t e = ops_kernel_allow(pl.kernel);
+        cudaError_t e = ops_kernel_allow(pl.kernel, pl.smem);
         const int threads = PrShape<128>::kThreads;
         if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.splits)), threads, pl.smem, st, args);
         if (e == cudaSuccess && pl.splits > 1) e = ops_launch(pl.join, dim3((unsigned)(pl.tiles * h->pool.Hkv * (h->pool.D / 16))), kPrRows, 0, st, args);
@@ -304,7 +304,7 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
     while ((1 << a.log2_T) < h->pool.T) ++a.log2_T;
     us_status s = error_word(&a.pool.err);
     if (s != US_OK) return s;
-    cudaError_t e = ops_kernel_allow(pl.kernel);
+    cudaError_t e = ops_kernel_allow(pl.kernel, pl.smem);
     void* args[] = {&a};
     if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)pl.ctas), 160, pl.smem, st, args);
     // (an item of one unit is never cut)

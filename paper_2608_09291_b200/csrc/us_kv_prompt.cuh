@@ -249,9 +249,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
 #pragma unroll 1
             for (int j = 0; j < n; ++j) {
                 ok = ops_wait_warp(b_st + 8u * (j & 3), (uint32_t)(j >> 2) & 1u, kMxWait, dead);
-                if (ok) ok = ops_wait_warp(b_s + 8u * qi, (uint32_t)j & 1u, kMxWait, dead);
                 if (!ok) break;
-                tc_fence_after();
                 const float4* st = steps[j & 3];
                 const int tok0 = (u0 + j) * kPrTile;
                 // V's steps: the largest so far is the reference; the fast path needs all of the unit's within 2^13 of it
@@ -266,6 +264,13 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                     lref = log2f(top);
                 }
                 const bool fast = __all_sync(0xffffffffu, mine.x >= 0.f && mine.y >= ref * 0x1p-13f && mine.y > 1e-30f && ref < 1e30f && lo <= tok0 && hi >= tok0 + kPrTile);
+                float fk[8];
+#pragma unroll
+                for (int g = 0; g < 8; ++g) fk[g] = f * st[g].x;
+                // (all of this before the scores are waited for)
+                ok = ops_wait_warp(b_s + 8u * qi, (uint32_t)j & 1u, kMxWait, dead);
+                if (!ok) break;
+                tc_fence_after();
                 uint32_t x[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tc_ld32(t_s + 32u * c, x[c]);
@@ -274,9 +279,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                 for (int c = 0; c < 4; ++c) pin32(x[c]);
                 // which of the unit's tokens the row sees
                 uint32_t sees[4];
-                float mx = -INFINITY, fk[8];
-#pragma unroll
-                for (int g = 0; g < 8; ++g) fk[g] = f * st[g].x;
+                float mx = -INFINITY;
                 if (!fast) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -329,24 +332,33 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         uint32_t y[16];
+                        // (step by step over the 32: all arguments, all exponentials, then what uses them)
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
-                            const float4 s4 = st[2 * c + g];
-                            const float k = fk[2 * c + g], b = base + (s4.z - lref);
+                            const float k = fk[2 * c + g], b = base + (st[2 * c + g].z - lref);
                             const uint64_t k2 = f32x2(k, k), b2 = f32x2(b, b);
+#pragma unroll
+                            for (int i = 16 * g; i < 16 * g + 16; i += 2) {
+                                float e0, e1;
+                                f32x2_split(fma2(f32x2(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])), k2, b2), e0, e1);
+                                x[c][i] = __float_as_uint(e0);
+                                x[c][i + 1] = __float_as_uint(e1);
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) x[c][i] = __float_as_uint(exp2_fast(__uint_as_float(x[c][i])));
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) {
                             uint64_t part = 0;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
-                                float e0, e1;
-                                f32x2_split(fma2(f32x2(__uint_as_float(x[c][16 * g + 2 * i]), __uint_as_float(x[c][16 * g + 2 * i + 1])), k2, b2), e0, e1);
-                                e0 = exp2_fast(e0);
-                                e1 = exp2_fast(e1);
+                                const float e0 = __uint_as_float(x[c][16 * g + 2 * i]), e1 = __uint_as_float(x[c][16 * g + 2 * i + 1]);
                                 part = add2(part, f32x2(e0, e1));
                                 y[8 * g + i] = half2_bits(e0, e1);
                             }
                             float p0, p1;
                             f32x2_split(part, p0, p1);
-                            sum = fmaf(p0 + p1, ref * s4.w, sum);   // (p without V's step)
+                            sum = fmaf(p0 + p1, ref * st[2 * c + g].w, sum);   // (p without V's step)
                         }
                         tc_st16_lanes(t_s + 16u * c, y);
                         if (c == 1) publish(0);

@@ -99,7 +99,7 @@ us_status product(const void* X, int32_t x_type, int64_t ldx, const void* x_mx, 
     p.y_vec = rows_vec(Y, N > 1 ? ldy : 0, size_of(y_type));
     p.w_stable = (flags & US_MX4_W_STABLE) != 0;
     p.err = static_cast<uint32_t*>(err);
-    const cudaError_t e = ops_kernel_allow(pl.kernel);
+    const cudaError_t e = ops_kernel_allow(pl.kernel, (int)kWholeSm);
     if (e != cudaSuccess) return cuda(e);
     void* args[] = {&p};
     return cuda(ops_launch(pl.kernel, dim3((unsigned)(pl.tiles * pl.split)), 192, pl.smem, st, args, (unsigned)pl.split));

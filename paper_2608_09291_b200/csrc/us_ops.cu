@@ -38,14 +38,14 @@ cudaError_t ops_launch(const void* kernel, dim3 grid, int block, int64_t smem, c
     return cudaLaunchKernelExC(&cfg, kernel, args);
 }
 
-cudaError_t ops_kernel_allow(const void* kernel)
+cudaError_t ops_kernel_allow(const void* kernel, int most)
 {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     std::lock_guard<std::mutex> hold(g_lock);
     if (g_allowed.count({dev, kernel})) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e == cudaSuccess) g_allowed.insert({dev, kernel});
     return e;
