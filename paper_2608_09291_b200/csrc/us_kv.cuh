@@ -790,7 +790,9 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
 #pragma unroll
                                 for (int c = 0; c < 4; ++c) o[k][nt][c] *= b;
                     }
-                    uint32_t pf[2][NT][2];
+                    // (fp16 output, few rows: what the rounding of p leaves is multiplied, too; else its 2^-12 would be as much as the output's own)
+                    constexpr bool REST = !BF16 && NT == 1;
+                    uint32_t pf[2][NT][2], pr[2][NT][2];
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         const float rel = stk[b] < 0.f ? 0.f : inv_ref > 0.f ? stv[b] * inv_ref : stv[b] == ref ? 1.f : __fdiv_rn(stv[b], ref);   // (NaN: NaN)
@@ -801,8 +803,16 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                                 e[b][nt][c] = exp2_fast(e[b][nt][c]);
                                 l[nt][c & 1] += e[b][nt][c];
                             }
-                            pf[b][nt][0] = transpose8(half2_bits(e[b][nt][0] * rel, e[b][nt][1] * rel));
-                            pf[b][nt][1] = transpose8(half2_bits(e[b][nt][2] * rel, e[b][nt][3] * rel));
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                const float p0 = e[b][nt][2 * c] * rel, p1 = e[b][nt][2 * c + 1] * rel;
+                                const uint32_t h = half2_bits(p0, p1);
+                                pf[b][nt][c] = transpose8(h);
+                                if (REST) {
+                                    const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                                    pr[b][nt][c] = transpose8(half2_bits(p0 - r.x, p1 - r.y));
+                                }
+                            }
                         }
                     }
                     // sums: 16 of D x 8 NT rows at a time; a lane holds the same D columns of its four tokens
@@ -831,6 +841,10 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                             for (int nt = 0; nt < NT; ++nt) {
                                 mma_f16(o[2 * k][nt], a0, a1, a2, a3, pf[b][nt][0], pf[b][nt][1]);
                                 mma_f16(o[2 * k + 1][nt], b0, b1, b2, b3, pf[b][nt][0], pf[b][nt][1]);
+                                if (REST) {
+                                    mma_f16(o[2 * k][nt], a0, a1, a2, a3, pr[b][nt][0], pr[b][nt][1]);
+                                    mma_f16(o[2 * k + 1][nt], b0, b1, b2, b3, pr[b][nt][0], pr[b][nt][1]);
+                                }
                             }
                         }
                     }
