@@ -10,7 +10,7 @@ __device__ uint32_t g_mx4_err;   // first bounded wait that ran out since the la
 struct Plan {
     const void* kernel;
     int nb, split, col_tiles, stages;
-    int64_t smem, tiles;
+    int64_t smem, tiles, blocks;
     bool fuse;
 };
 
@@ -54,6 +54,13 @@ Plan plan(int64_t N, int64_t M, int64_t K, bool can_fuse, int sms)
     else if (p.nb == 64) shape<64, false>(&p, slice, kHalfSm);
     else if (p.nb == 128) shape<128, false>(&p, slice, p.tiles * p.split > sms ? kHalfSm : kWholeSm);
     else shape<256, false>(&p, slice, kWholeSm);
+    // more tiles than SMs: a block an SM that walks over them
+    p.blocks = p.tiles * p.split;
+    if (p.nb == 256 && p.tiles > sms) {
+        p.kernel = (const void*)us_mx4_many_kernel<Mx4Many::kStages>;
+        p.smem = Mx4Many::kSmem;
+        p.blocks = sms;
+    }
     return p;
 }
 
@@ -93,7 +100,7 @@ us_status product(const void* X, int32_t x_type, int64_t ldx, const void* x_mx, 
     p.Y = Y;
     p.ldx = ldx; p.ldy = ldy;
     p.M = (int32_t)M; p.N = (int32_t)N; p.K = (int32_t)K; p.kt = (int32_t)mx4_tiles(K, 256);
-    p.split = pl.split; p.col_tiles = pl.col_tiles; p.stages = pl.stages;
+    p.split = pl.split; p.col_tiles = pl.col_tiles; p.tiles = (int32_t)pl.tiles; p.stages = pl.stages;
     p.x_type = x_type; p.y_type = y_type;
     p.x_vec = X && rows_vec(X, ldx, size_of(x_type));
     p.y_vec = rows_vec(Y, N > 1 ? ldy : 0, size_of(y_type));
@@ -102,7 +109,7 @@ us_status product(const void* X, int32_t x_type, int64_t ldx, const void* x_mx, 
     const cudaError_t e = ops_kernel_allow(pl.kernel, (int)kWholeSm);
     if (e != cudaSuccess) return cuda(e);
     void* args[] = {&p};
-    return cuda(ops_launch(pl.kernel, dim3((unsigned)(pl.tiles * pl.split)), 192, pl.smem, st, args, (unsigned)pl.split));
+    return cuda(ops_launch(pl.kernel, dim3((unsigned)pl.blocks), 192, pl.smem, st, args, (unsigned)pl.split));
 }
 
 }  // namespace

@@ -392,7 +392,7 @@ struct Mx4Params {
     void* Y;
     int64_t ldx, ldy;
     int32_t M, N, K, kt;
-    int32_t split, col_tiles;
+    int32_t split, col_tiles, tiles;   // tiles: of the whole product
     int32_t stages;        // ring stages
     int32_t x_type, y_type;
     int32_t x_vec, y_vec;  // rows of X, of Y take 16-byte accesses
@@ -488,6 +488,14 @@ __device__ __forceinline__ void mx4_store4(const Mx4Params& p, int64_t n, int64_
     }
 }
 __device__ __forceinline__ void bar_epilogue() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// The same barrier, and whether any of its threads says so.
+__device__ __forceinline__ bool bar_any(bool say)
+{
+    uint32_t any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any) : "r"((uint32_t)say) : "memory");
+    return any != 0;
+}
 
 // The tile's sums (four warps, lane quarter `quarter`): 32 tokens at a time to shared memory as they are stored, [token][weight row], and
 // from there in whole lines: every thread 16 bytes of a token's 256 (512). Straight from the registers a warp's store of one token is 64
@@ -733,6 +741,173 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
         }
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
+}
+
+// ---- the product of many tokens -------------------------------------------------------------------------------------------
+// One block an SM walks over tiles of 128 weight rows x 256 tokens (all tokens of a row tile in turn: X stays in L2, W is read about
+// once). Copies run ahead over the tiles' ends, and the sums of a tile leave tensor memory for shared memory, rounded, before the next
+// tile's products begin; they are stored while those run. (A block a tile, which starts with nothing on its way and stores before it
+// ends: 4096 x 28672 x 8192 took 470 us.)
+struct Mx4Many {
+    using S = Mx4Shape<256, false>;
+    static constexpr int kStages = 3, kOut = 256 * (128 * 2 + 16);   // bytes of a tile's sums, 16 bits each (or half of its tokens' in 32)
+    static constexpr int kSmem = 1024 + kStages * S::kStage + kOut;
+    static_assert(kSmem <= 226 * 1024 && 128 * (128 * 4 + 16) <= kOut, "shared memory");
+};
+
+template <class T>
+__device__ __forceinline__ void mx4_many_store(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage, uint32_t b_free)
+{
+    constexpr int PITCH = 128 * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = 128 / PER, PASS = sizeof(T) == 4 ? 128 : 256;
+    const int row = 32 * quarter + lane, m_here = (int)min((int64_t)128, p.M - m0);
+#pragma unroll 1
+    for (int c0 = 0; c0 < nn; c0 += PASS) {
+        const int cols = min(PASS, nn - c0);
+        bar_epilogue();   // (what was here has been stored)
+#pragma unroll 1
+        for (int c = 0; c < cols; c += 32) {
+            uint32_t r[32];
+            tc_ld32(tm + ((uint32_t)quarter << 21) + (uint32_t)(c0 + c), r);
+            tc_wait_ld();
+            pin32(r);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) *reinterpret_cast<T*>(stage + (c + i) * PITCH + row * sizeof(T)) = from_f32<T>(__uint_as_float(r[i]));
+        }
+        if (c0 + PASS >= nn) {   // the sums are out of tensor memory
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_free);
+        }
+        bar_epilogue();
+        if (p.y_vec && m_here == 128) {
+#pragma unroll 4
+            for (int i = row; i < cols * ROW; i += 128) {
+                const int n = i / ROW, piece = i % ROW;
+                *reinterpret_cast<uint4*>(static_cast<T*>(p.Y) + (n0 + c0 + n) * p.ldy + m0 + piece * PER) = *reinterpret_cast<const uint4*>(stage + n * PITCH + 16 * piece);
+            }
+        } else {
+            for (int n = 0; n < cols; ++n)
+                if (row < m_here) static_cast<T*>(p.Y)[(n0 + c0 + n) * p.ldy + m0 + row] = *reinterpret_cast<const T*>(stage + n * PITCH + row * sizeof(T));
+        }
+    }
+}
+
+template <int ST>   // ring stages
+__global__ void __launch_bounds__(192, 1) us_mx4_many_kernel(const __grid_constant__ Mx4Params p)
+{
+    using S = Mx4Many::S;
+    constexpr int NB = 256;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * ST + 3];
+    __shared__ uint32_t misc[2];
+    uint8_t* ring = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint8_t* out = ring + ST * S::kStage;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8u * ST, b_done = b_empty + 8u * ST, b_free = b_done + 8u, b_end = b_free + 8u;
+    volatile uint32_t* dead = misc + 1;
+    if (warp == 1) {
+        if (lane < ST) { mbar_init(b_full + 8u * lane, 1); mbar_init(b_empty + 8u * lane, 1); }
+        if (lane == 0) { mbar_init(b_done, 1); mbar_init(b_free, 4); mbar_init(b_end, 1); misc[1] = 0; }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        __syncwarp();
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(misc)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (after the allocation, as above)
+    const uint32_t tm = *(volatile uint32_t*)misc;
+    bool ok = true;
+    if (warp == 0) {
+        // ---- copies ----
+        if (lane == 0) {
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            uint32_t count = 0;   // stages filled
+            for (int tile = blockIdx.x; tile < p.tiles && ok; tile += gridDim.x) {
+                const int mt = tile / p.col_tiles, n0 = (tile - mt * p.col_tiles) * NB, nn = min(NB, p.N - n0);
+                const int rows0 = min(128, (nn + 7) & ~7), rows1 = max(0, (nn - 128 + 7) & ~7);
+                const uint32_t bytes = (uint32_t)(kMxTile + kMxScales + 128 * rows0 + (rows1 ? kMxScales + 128 * rows1 : 0));
+                const uint8_t* w = p.w + (int64_t)mt * p.kt * kMxTile;
+                const uint8_t* x0 = p.x + (int64_t)(n0 >> 7) * p.kt * kMxTile;
+                const uint8_t* x1 = x0 + (int64_t)p.kt * kMxTile;
+                for (int t = 0; t < p.kt; ++t, ++count) {
+                    const uint32_t s = count % ST;
+                    if (count >= ST && !ops_wait(b_empty + 8u * s, (count / ST - 1u) & 1u, kMxWait)) { ok = false; break; }
+                    const uint32_t b = b_full + 8u * s, d = smem_u32(ring + s * S::kStage);
+                    mbar_expect_tx(b, bytes);
+                    bulk_g2s(d, w + (int64_t)t * kMxTile, kMxTile, b);
+                    bulk_g2s(d + kMxTile, x0 + (int64_t)t * kMxTile, kMxScales, b);
+                    bulk_g2s(d + kMxTile + 2 * kMxScales, x0 + (int64_t)t * kMxTile + kMxScales, 128u * rows0, b);
+                    if (rows1) {
+                        bulk_g2s(d + kMxTile + kMxScales, x1 + (int64_t)t * kMxTile, kMxScales, b);
+                        bulk_g2s(d + kMxTile + 2 * kMxScales + kMxCodes, x1 + (int64_t)t * kMxTile + kMxScales, 128u * rows1, b);
+                    }
+                }
+            }
+            if (!ok)   // (nothing may be in flight when the block ends)
+                for (uint32_t c = count > ST ? count - ST : 0; c < count; ++c) ops_wait(b_full + 8u * (c % ST), (c / ST) & 1u, kMxWait);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---- MMA issue ----
+        const uint32_t leader = tc_elect();
+        const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(NB / 8) << 17) | (1u << 23) | (8u << 24);
+        const uint32_t kUpper = (2u << 4) | (2u << 29);
+        uint32_t count = 0, n = 0, s = 0, par = 0;
+        for (int tile = blockIdx.x; tile < p.tiles && ok; tile += gridDim.x, ++n) {
+            if (n > 0) ok = ops_wait_warp(b_free, (n - 1u) & 1u, kMxWait, dead);
+            for (int t = 0; t < p.kt && ok; ++t, ++count) {
+                ok = ops_wait_warp(b_full + 8u * s, par, kMxWait, dead, true);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t a = smem_u32(ring + s * S::kStage), x = a + kMxTile, sf = tm + NB + (count & 1u) * S::kSfCols;
+                const uint64_t sa = mx4_desc(a, 128, 0), sx = mx4_desc(x, 128, 0);
+#pragma unroll
+                for (uint32_t h = 0; h < 2; ++h) {
+                    mx4_copy_scales(leader, sf + 4u * h, sa + 32u * h);
+#pragma unroll
+                    for (uint32_t g = 0; g < 2; ++g) mx4_copy_scales(leader, sf + 8u + 4u * (2u * h + g), sx + 32u * h + (kMxScales / 16) * g);
+                }
+                const uint64_t da = mx4_desc(a + kMxScales, 1024, 2), db = mx4_desc(x + 2 * kMxScales, 1024, 2);
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j)
+                    mx4_mma(leader, tm, da + 2u * j, db + 2u * j, idesc | ((j & 1u) ? kUpper : 0u), sf + 4u * (j >> 1), sf + 8u + 8u * (j >> 1), t > 0 || j > 0);
+                tc_commit(leader, b_empty + 8u * s);
+                if (++s == ST) { s = 0; par ^= 1u; }
+            }
+            if (ok) tc_commit(leader, b_done);
+        }
+        if (!ok) *dead = 1;
+        tc_commit(leader, b_end);   // nothing is in flight when the tensor memory is given back
+        ops_wait(b_end, 0, kMxWait);
+        __syncwarp();
+    } else {
+        // ---- sums out ----
+        const int quarter = warp & 3;
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        uint32_t n = 0;
+        for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x, ++n) {
+            ok = ops_wait_warp(b_done, n & 1u, 4 * kMxWait, dead);
+            if (bar_any(!ok)) {   // (all four warps leave at the same place)
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            const int mt = tile / p.col_tiles, n0 = (tile - mt * p.col_tiles) * NB, nn = min(NB, p.N - n0);
+            if (p.y_type == kF32) mx4_many_store<float>(p, tm, quarter, lane, 128 * (int64_t)mt, n0, nn, out, b_free);
+            else if (p.y_type == kF16) mx4_many_store<__half>(p, tm, quarter, lane, 128 * (int64_t)mt, n0, nn, out, b_free);
+            else mx4_many_store<__nv_bfloat16>(p, tm, quarter, lane, 128 * (int64_t)mt, n0, nn, out, b_free);
+        }
+    }
+    if (!ok && lane == 0) {
+        *dead = 1;
+        atomicExch(p.err, kErrTimeout);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
 }
 
 }  // namespace us
