@@ -9,7 +9,7 @@ __device__ uint32_t g_mx4_err;   // first bounded wait that ran out since the la
 
 struct Plan {
     const void* kernel;
-    int nb, split, col_tiles, stages;
+    int nb, split, col_tiles, stages, cluster;
     int64_t smem, tiles, blocks;
     bool fuse;
 };
@@ -34,8 +34,9 @@ Plan plan(int64_t N, int64_t M, int64_t K, bool can_fuse, int sms)
     Plan p = {};
     const int64_t kt = mx4_tiles(K, 256), rt = mx4_tiles(M, 128);
     p.nb = N <= 16 ? 16 : N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
-    // (half as many columns a CTA where the tiles would not fill the GPU)
-    if (p.nb == 256 && rt * mx4_tiles(N, 256) < sms) p.nb = 128;
+    // (half as many columns a CTA where the tiles would not fill the GPU, or where tokens that are not there would be more than an eighth of
+    // the work. 28672 x 8192 in tiles of 256, of 128: 256 tokens 38.2, 41.0 us, 300: 63.1, 55.1, 512: 67.0, 74.7)
+    if (p.nb == 256 && (rt * mx4_tiles(N, 256) < sms || 8 * mx4_tiles(N, 256) * 2 > 9 * mx4_tiles(N, 128))) p.nb = 128;
     p.col_tiles = (int)mx4_tiles(N, p.nb);
     p.tiles = rt * p.col_tiles;
     // The columns are split while that fills SMs and leaves every CTA four tiles of them (16 where the sums to exchange are 64 KB). 4096 x
@@ -53,13 +54,14 @@ Plan plan(int64_t N, int64_t M, int64_t K, bool can_fuse, int sms)
     else if (p.nb == 32) shape<32, false>(&p, slice, kHalfSm);
     else if (p.nb == 64) shape<64, false>(&p, slice, kHalfSm);
     else if (p.nb == 128) shape<128, false>(&p, slice, p.tiles * p.split > sms ? kHalfSm : kWholeSm);
-    else shape<256, false>(&p, slice, kWholeSm);
-    // more tiles than SMs: a block an SM that walks over them
     p.blocks = p.tiles * p.split;
-    if (p.nb == 256 && p.tiles > sms) {
-        p.kernel = (const void*)us_mx4_many_kernel<Mx4Many::kStages>;
-        p.smem = Mx4Many::kSmem;
-        p.blocks = sms;
+    p.cluster = p.split;
+    if (p.nb == 256) {   // pairs of blocks that walk over pairs of tiles
+        p.kernel = (const void*)us_mx4_pair_kernel<Mx4Pair::kStages>;
+        p.smem = Mx4Pair::kSmem;
+        p.tiles = mx4_tiles(rt, 2) * p.col_tiles;
+        p.blocks = 2 * std::min<int64_t>(p.tiles, sms / 2);
+        p.cluster = 2;
     }
     return p;
 }
@@ -109,7 +111,7 @@ us_status product(const void* X, int32_t x_type, int64_t ldx, const void* x_mx, 
     const cudaError_t e = ops_kernel_allow(pl.kernel, (int)kWholeSm);
     if (e != cudaSuccess) return cuda(e);
     void* args[] = {&p};
-    return cuda(ops_launch(pl.kernel, dim3((unsigned)pl.blocks), 192, pl.smem, st, args, (unsigned)pl.split));
+    return cuda(ops_launch(pl.kernel, dim3((unsigned)pl.blocks), 192, pl.smem, st, args, (unsigned)pl.cluster));
 }
 
 }  // namespace

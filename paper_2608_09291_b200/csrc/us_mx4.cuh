@@ -404,10 +404,10 @@ constexpr uint32_t kMxWait = 2000000u;   // bounded waits, ns >> 10
 
 template <int NB, bool FUSE>
 struct Mx4Shape {
-    static constexpr int kGroups = (NB + 127) / 128;                       // 128-token groups of scales
-    static constexpr int kXTile = kGroups * kMxScales + NB * 128;          // bytes of a stage's activations
+    static_assert(NB <= 128, "one tile of activations holds the tokens");
+    static constexpr int kXTile = kMxScales + NB * 128;                    // bytes of a stage's activations
     static constexpr int kStage = kMxTile + (FUSE ? 0 : kXTile);
-    static constexpr int kSfCols = 8 + 8 * kGroups;                        // tensor-memory columns of a stage's scales
+    static constexpr int kSfCols = 16;                                     // tensor-memory columns of a stage's scales
     static constexpr int kCols = NB + 2 * kSfCols <= 64 ? 64 : NB + 2 * kSfCols <= 128 ? 128 : NB + 2 * kSfCols <= 256 ? 256 : 512;
     static constexpr int kMaxStages = 12;
 };
@@ -599,29 +599,15 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
             const int n = t1 - t0;
             const bool early = p.w_stable != 0;
             int issued = 0;
-            // activations: rows of the tile(s) that hold tokens, rounded up to whole 8-row groups (the others' sums are not stored)
-            const int rows0 = min(128, (nn + 7) & ~7), rows1 = NB > 128 ? min(128, max(0, (nn - 128 + 7) & ~7)) : 0;
-            const uint32_t x_bytes = FUSE ? 0u : (uint32_t)(kMxScales + 128 * rows0 + (rows1 ? kMxScales + 128 * rows1 : 0));
-            const uint8_t* x0 = p.x + ((int64_t)(n0 >> 7) * p.kt + t0) * kMxTile;
-            const uint8_t* x1 = x0 + (int64_t)p.kt * kMxTile;
+            // activations: the rows that hold tokens, rounded up to whole 8-row groups (the others' sums are not stored)
+            const uint32_t x_bytes = FUSE ? 0u : (uint32_t)(kMxScales + 128 * ((nn + 7) & ~7));
+            const uint8_t* x = p.x + ((int64_t)(n0 >> 7) * p.kt + t0) * kMxTile;
             auto copy_w = [&](int i, int s) {
                 mbar_expect_tx(b_full + 8u * s, (uint32_t)kMxTile + x_bytes);
                 bulk_g2s(smem_u32(ring + (size_t)s * S::kStage), w + (int64_t)i * kMxTile, kMxTile, b_full + 8u * s);
             };
             auto copy_x = [&](int i, int s) {
-                const uint32_t d = smem_u32(ring + (size_t)s * S::kStage + kMxTile), b = b_full + 8u * s;
-                const uint8_t* a = x0 + (int64_t)i * kMxTile;
-                if (NB <= 128) {
-                    bulk_g2s(d, a, x_bytes, b);
-                } else {
-                    bulk_g2s(d, a, kMxScales, b);
-                    bulk_g2s(d + 2 * kMxScales, a + kMxScales, 128u * rows0, b);
-                    if (rows1) {
-                        const uint8_t* c = x1 + (int64_t)i * kMxTile;
-                        bulk_g2s(d + kMxScales, c, kMxScales, b);
-                        bulk_g2s(d + 2 * kMxScales + kMxCodes, c + kMxScales, 128u * rows1, b);
-                    }
-                }
+                bulk_g2s(smem_u32(ring + (size_t)s * S::kStage + kMxTile), x + (int64_t)i * kMxTile, x_bytes, b_full + 8u * s);
             };
             const int first = min(n, p.stages);
             if (early) for (int i = 0; i < first; ++i) copy_w(i, i);
@@ -668,15 +654,13 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
 #pragma unroll
             for (uint32_t h = 0; h < 2; ++h) {
                 mx4_copy_scales(leader, sf + 4u * h, sa + 32u * h);
-#pragma unroll
-                for (uint32_t g = 0; g < S::kGroups; ++g)
-                    mx4_copy_scales(leader, sf + 8u + 4u * (S::kGroups * h + g), sx + 32u * h + (kMxScales / 16) * g);
+                mx4_copy_scales(leader, sf + 8u + 4u * h, sx + 32u * h);
             }
-            const uint64_t da = mx4_desc(a + kMxScales, 1024, 2), db = mx4_desc(x + S::kGroups * kMxScales, 1024, 2);
+            const uint64_t da = mx4_desc(a + kMxScales, 1024, 2), db = mx4_desc(x + kMxScales, 1024, 2);
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j)
                 mx4_mma(leader, tm, da + 2u * j, db + 2u * j, idesc | ((j & 1u) ? kUpper : 0u), sf + 4u * (j >> 1),
-                        sf + 8u + 4u * S::kGroups * (j >> 1), t > t0 || j > 0);
+                        sf + 8u + 4u * (j >> 1), t > t0 || j > 0);
             tc_commit(leader, b_empty + 8u * s);
             if (++s == p.stages) { s = 0; par ^= 1u; }
         }
@@ -744,22 +728,71 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
 }
 
 // ---- the product of many tokens -------------------------------------------------------------------------------------------
-// One block an SM walks over tiles of 128 weight rows x 256 tokens (all tokens of a row tile in turn: X stays in L2, W is read about
-// once). Copies run ahead over the tiles' ends, and the sums of a tile leave tensor memory for shared memory, rounded, before the next
-// tile's products begin; they are stored while those run. (A block a tile, which starts with nothing on its way and stores before it
-// ends: 4096 x 28672 x 8192 took 470 us.)
-struct Mx4Many {
-    using S = Mx4Shape<256, false>;
-    static constexpr int kStages = 3, kOut = 256 * (128 * 2 + 16);   // bytes of a tile's sums, 16 bits each (or half of its tokens' in 32)
-    static constexpr int kSmem = 1024 + kStages * S::kStage + kOut;
-    static_assert(kSmem <= 226 * 1024 && 128 * (128 * 4 + 16) <= kOut, "shared memory");
+// Pairs of blocks (a cluster of two SMs, cta_group::2) walk over tiles of 256 weight rows x 256 tokens, all tokens of the rows in turn: X
+// stays in L2, W is read about once. Each block has 128 of the rows, and loads half of the tokens for both: 35 KB a block and 256
+// columns, 52 KB for a block that works alone (4096 x 28672 x 8192: 410 us = 4.7 PFLOP/s, 445 alone; K = 28672, M = 8192: 445 and 478).
+// Copies run ahead over the tiles' ends, and the sums of a tile leave tensor memory for shared memory, rounded, before the next
+// tile's products begin (half of the tokens at a time); they are stored while those run. What bounds it is the way from L2 to the SMs:
+// alone, it takes 307 us without its copies and 390 with a quarter of its products. 4, 5, 6 stages: 415, 406, 413 us.
+// The first block of a pair issues for both: it learns from the second's idle MMA warp that its stage is full, and tells both when a
+// stage has been read and when a tile is done.
+struct Mx4Pair {
+    static constexpr int kStage = kMxTile + 2 * kMxScales + kMxCodes;            // W: scales, codes; X: scales of 256 tokens, codes of 128
+    static constexpr int kStages = 5, kOut = 128 * (128 * 2 + 16);               // bytes of half a block's sums, 16 bits each (or a quarter's in 32)
+    static constexpr int kSmem = 1024 + kStages * kStage + kOut;
+    static constexpr int kSfCols = 24;                                           // tensor-memory columns of a stage's scales
+    static_assert(kSmem <= 226 * 1024 && 64 * (128 * 4 + 16) <= kOut && 256 + 2 * kSfCols <= 512, "shared and tensor memory");
 };
 
-template <class T>
-__device__ __forceinline__ void mx4_many_store(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage, uint32_t b_free)
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t local, uint32_t rank)
 {
-    constexpr int PITCH = 128 * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = 128 / PER, PASS = sizeof(T) == 4 ? 128 : 256;
-    const int row = 32 * quarter + lane, m_here = (int)min((int64_t)128, p.M - m0);
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(local), "r"(rank));
+    return a;
+}
+// (Relaxed: no thread's writes are handed over, only copies whose end was seen and tensor memory whose reads have ended. A release of
+// cluster scope waits for all that the SM has under way, and took 630 us in place of 400 for 4096 x 28672 x 8192.)
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// Bounded wait of a warp for arrivals from the other block.
+__device__ __forceinline__ bool ops_wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* dead)
+{
+    const uint64_t t0 = global_timer_ns();
+#pragma unroll 1
+    for (uint32_t it = 0; it < (1u << 24); ++it) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (__all_sync(0xffffffffu, ok)) return true;
+        if ((it & 255u) == 255u && __any_sync(0xffffffffu, *dead || ((global_timer_ns() - t0) >> 10) > kMxWait)) break;
+    }
+    return false;
+}
+__device__ __forceinline__ void pair_commit(uint32_t elected, uint32_t bar, uint16_t blocks)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t"
+                 "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(bar), "h"(blocks), "r"(elected) : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t elected, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %7, 0;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(elected) : "memory");
+}
+__device__ __forceinline__ void pair_copy_scales(uint32_t elected, uint32_t d, uint64_t s)   // (in both blocks, each from its own shared memory)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}"
+                 ::"r"(d), "l"(s), "r"(elected) : "memory");
+}
+
+// A block's sums (four warps) to shared memory and out; free_bar: the pair's first block's barrier, told when they are out of tensor memory.
+template <class T>
+__device__ __forceinline__ void mx4_pair_store(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage, uint32_t free_bar)
+{
+    constexpr int PITCH = 128 * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = 128 / PER, PASS = 256 / (int)sizeof(T);
+    const int row = 32 * quarter + lane, m_here = (int)max((int64_t)0, min((int64_t)128, p.M - m0));   // (0: the pair's rows end with its first block)
 #pragma unroll 1
     for (int c0 = 0; c0 < nn; c0 += PASS) {
         const int cols = min(PASS, nn - c0);
@@ -773,10 +806,10 @@ __device__ __forceinline__ void mx4_many_store(const Mx4Params& p, uint32_t tm, 
 #pragma unroll
             for (int i = 0; i < 32; ++i) *reinterpret_cast<T*>(stage + (c + i) * PITCH + row * sizeof(T)) = from_f32<T>(__uint_as_float(r[i]));
         }
-        if (c0 + PASS >= nn) {   // the sums are out of tensor memory
+        if (c0 + PASS >= nn) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(b_free);
+            if (lane == 0) mbar_arrive_cluster(free_bar);
         }
         bar_epilogue();
         if (p.y_vec && m_here == 128) {
@@ -793,28 +826,30 @@ __device__ __forceinline__ void mx4_many_store(const Mx4Params& p, uint32_t tm, 
 }
 
 template <int ST>   // ring stages
-__global__ void __launch_bounds__(192, 1) us_mx4_many_kernel(const __grid_constant__ Mx4Params p)
+__global__ void __launch_bounds__(192, 1) us_mx4_pair_kernel(const __grid_constant__ Mx4Params p)
 {
-    using S = Mx4Many::S;
+    using S = Mx4Pair;
     constexpr int NB = 256;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * ST + 3];
+    __shared__ __align__(8) uint64_t bars[3 * ST + 3];
     __shared__ uint32_t misc[2];
     uint8_t* ring = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t* out = ring + ST * S::kStage;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8u * ST, b_done = b_empty + 8u * ST, b_free = b_done + 8u, b_end = b_free + 8u;
+    const uint32_t b_full = smem_u32(bars), b_other = b_full + 8u * ST, b_empty = b_other + 8u * ST, b_done = b_empty + 8u * ST, b_free = b_done + 8u, b_end = b_free + 8u;
     volatile uint32_t* dead = misc + 1;
+    const int rank = (int)(blockIdx.x & 1u), row_tiles = (int)mx4_tiles(p.M, 128);
     if (warp == 1) {
-        if (lane < ST) { mbar_init(b_full + 8u * lane, 1); mbar_init(b_empty + 8u * lane, 1); }
-        if (lane == 0) { mbar_init(b_done, 1); mbar_init(b_free, 4); mbar_init(b_end, 1); misc[1] = 0; }
+        if (lane < ST) { mbar_init(b_full + 8u * lane, 1); mbar_init(b_other + 8u * lane, 1); mbar_init(b_empty + 8u * lane, 1); }
+        if (lane == 0) { mbar_init(b_done, 1); mbar_init(b_free, 8); mbar_init(b_end, 1); misc[1] = 0; }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         __syncwarp();
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(misc)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(misc)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     tc_fence_after();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (after the allocation, as above)
     const uint32_t tm = *(volatile uint32_t*)misc;
@@ -824,13 +859,16 @@ __global__ void __launch_bounds__(192, 1) us_mx4_many_kernel(const __grid_consta
         if (lane == 0) {
             asm volatile("griddepcontrol.wait;" ::: "memory");
             uint32_t count = 0;   // stages filled
-            for (int tile = blockIdx.x; tile < p.tiles && ok; tile += gridDim.x) {
-                const int mt = tile / p.col_tiles, n0 = (tile - mt * p.col_tiles) * NB, nn = min(NB, p.N - n0);
-                const int rows0 = min(128, (nn + 7) & ~7), rows1 = max(0, (nn - 128 + 7) & ~7);
-                const uint32_t bytes = (uint32_t)(kMxTile + kMxScales + 128 * rows0 + (rows1 ? kMxScales + 128 * rows1 : 0));
+            for (int tile = blockIdx.x >> 1; tile < p.tiles && ok; tile += gridDim.x >> 1) {
+                const int pair = tile / p.col_tiles, n0 = (tile - pair * p.col_tiles) * NB, nn = min(NB, p.N - n0);
+                const int mt = min(2 * pair + rank, row_tiles - 1);   // (past the last row tile: its products are not stored)
+                const int rows = max(0, min(128, (nn - 128 * rank + 7) & ~7));   // this block's tokens, in whole 8-row groups
+                const bool two = nn > 128;
+                const uint32_t bytes = (uint32_t)(kMxTile + kMxScales + (two ? kMxScales : 0) + 128 * rows);
                 const uint8_t* w = p.w + (int64_t)mt * p.kt * kMxTile;
                 const uint8_t* x0 = p.x + (int64_t)(n0 >> 7) * p.kt * kMxTile;
                 const uint8_t* x1 = x0 + (int64_t)p.kt * kMxTile;
+                const uint8_t* xc = (rank ? x1 : x0) + kMxScales;
                 for (int t = 0; t < p.kt; ++t, ++count) {
                     const uint32_t s = count % ST;
                     if (count >= ST && !ops_wait(b_empty + 8u * s, (count / ST - 1u) & 1u, kMxWait)) { ok = false; break; }
@@ -838,66 +876,77 @@ __global__ void __launch_bounds__(192, 1) us_mx4_many_kernel(const __grid_consta
                     mbar_expect_tx(b, bytes);
                     bulk_g2s(d, w + (int64_t)t * kMxTile, kMxTile, b);
                     bulk_g2s(d + kMxTile, x0 + (int64_t)t * kMxTile, kMxScales, b);
-                    bulk_g2s(d + kMxTile + 2 * kMxScales, x0 + (int64_t)t * kMxTile + kMxScales, 128u * rows0, b);
-                    if (rows1) {
-                        bulk_g2s(d + kMxTile + kMxScales, x1 + (int64_t)t * kMxTile, kMxScales, b);
-                        bulk_g2s(d + kMxTile + 2 * kMxScales + kMxCodes, x1 + (int64_t)t * kMxTile + kMxScales, 128u * rows1, b);
-                    }
+                    if (two) bulk_g2s(d + kMxTile + kMxScales, x1 + (int64_t)t * kMxTile, kMxScales, b);
+                    if (rows) bulk_g2s(d + kMxTile + 2 * kMxScales, xc + (int64_t)t * kMxTile, 128u * rows, b);
                 }
             }
-            if (!ok)   // (nothing may be in flight when the block ends)
-                for (uint32_t c = count > ST ? count - ST : 0; c < count; ++c) ops_wait(b_full + 8u * (c % ST), (c / ST) & 1u, kMxWait);
+            // (nothing may be in flight when the block ends: no copies into it, and no word from the first block that a stage has been read)
+            for (uint32_t c = count > ST ? count - ST : 0; c < count; ++c) ops_wait((ok ? b_empty : b_full) + 8u * (c % ST), (c / ST) & 1u, kMxWait);
         }
         __syncwarp();
-    } else if (warp == 1) {
-        // ---- MMA issue ----
+    } else if (warp == 1 && rank == 0) {
+        // ---- MMA issue, for both blocks ----
         const uint32_t leader = tc_elect();
-        const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(NB / 8) << 17) | (1u << 23) | (8u << 24);
+        const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(NB / 8) << 17) | (1u << 23) | (16u << 24);   // M = 256
         const uint32_t kUpper = (2u << 4) | (2u << 29);
         uint32_t count = 0, n = 0, s = 0, par = 0;
-        for (int tile = blockIdx.x; tile < p.tiles && ok; tile += gridDim.x, ++n) {
-            if (n > 0) ok = ops_wait_warp(b_free, (n - 1u) & 1u, kMxWait, dead);
+        for (int tile = blockIdx.x >> 1; tile < p.tiles && ok; tile += gridDim.x >> 1, ++n) {
+            if (n > 0) ok = ops_wait_cluster(b_free, (n - 1u) & 1u, dead);
             for (int t = 0; t < p.kt && ok; ++t, ++count) {
                 ok = ops_wait_warp(b_full + 8u * s, par, kMxWait, dead, true);
+                if (ok) ok = ops_wait_cluster(b_other + 8u * s, par, dead);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t a = smem_u32(ring + s * S::kStage), x = a + kMxTile, sf = tm + NB + (count & 1u) * S::kSfCols;
                 const uint64_t sa = mx4_desc(a, 128, 0), sx = mx4_desc(x, 128, 0);
 #pragma unroll
                 for (uint32_t h = 0; h < 2; ++h) {
-                    mx4_copy_scales(leader, sf + 4u * h, sa + 32u * h);
+                    pair_copy_scales(leader, sf + 4u * h, sa + 32u * h);
 #pragma unroll
-                    for (uint32_t g = 0; g < 2; ++g) mx4_copy_scales(leader, sf + 8u + 4u * (2u * h + g), sx + 32u * h + (kMxScales / 16) * g);
+                    for (uint32_t g = 0; g < 2; ++g) pair_copy_scales(leader, sf + 8u + 4u * (2u * h + g), sx + 32u * h + (kMxScales / 16) * g);
                 }
                 const uint64_t da = mx4_desc(a + kMxScales, 1024, 2), db = mx4_desc(x + 2 * kMxScales, 1024, 2);
 #pragma unroll
                 for (uint32_t j = 0; j < 4; ++j)
-                    mx4_mma(leader, tm, da + 2u * j, db + 2u * j, idesc | ((j & 1u) ? kUpper : 0u), sf + 4u * (j >> 1), sf + 8u + 8u * (j >> 1), t > 0 || j > 0);
-                tc_commit(leader, b_empty + 8u * s);
+                    pair_mma(leader, tm, da + 2u * j, db + 2u * j, idesc | ((j & 1u) ? kUpper : 0u), sf + 4u * (j >> 1), sf + 8u + 8u * (j >> 1), t > 0 || j > 0);
+                pair_commit(leader, b_empty + 8u * s, 3);
                 if (++s == ST) { s = 0; par ^= 1u; }
             }
-            if (ok) tc_commit(leader, b_done);
+            if (ok) pair_commit(leader, b_done, 3);
         }
         if (!ok) *dead = 1;
-        tc_commit(leader, b_end);   // nothing is in flight when the tensor memory is given back
+        pair_commit(leader, b_end, 1);   // nothing is in flight when the tensor memory is given back
         ops_wait(b_end, 0, kMxWait);
         __syncwarp();
+    } else if (warp == 1) {
+        // ---- the second block's stages are announced to the first ----
+        uint32_t s = 0, par = 0;
+        const uint32_t first = cluster_addr(b_other, 0);
+        for (int tile = blockIdx.x >> 1; tile < p.tiles && ok; tile += gridDim.x >> 1)
+            for (int t = 0; t < p.kt && ok; ++t) {
+                ok = ops_wait_warp(b_full + 8u * s, par, kMxWait, dead, true);
+                if (!ok) break;
+                if (lane == 0) mbar_arrive_cluster(first + 8u * s);
+                if (++s == ST) { s = 0; par ^= 1u; }
+            }
     } else {
         // ---- sums out ----
         const int quarter = warp & 3;
+        const uint32_t free_bar = cluster_addr(b_free, 0);
         asm volatile("griddepcontrol.wait;" ::: "memory");
         uint32_t n = 0;
-        for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x, ++n) {
+        for (int tile = blockIdx.x >> 1; tile < p.tiles; tile += gridDim.x >> 1, ++n) {
             ok = ops_wait_warp(b_done, n & 1u, 4 * kMxWait, dead);
             if (bar_any(!ok)) {   // (all four warps leave at the same place)
                 ok = false;
                 break;
             }
             tc_fence_after();
-            const int mt = tile / p.col_tiles, n0 = (tile - mt * p.col_tiles) * NB, nn = min(NB, p.N - n0);
-            if (p.y_type == kF32) mx4_many_store<float>(p, tm, quarter, lane, 128 * (int64_t)mt, n0, nn, out, b_free);
-            else if (p.y_type == kF16) mx4_many_store<__half>(p, tm, quarter, lane, 128 * (int64_t)mt, n0, nn, out, b_free);
-            else mx4_many_store<__nv_bfloat16>(p, tm, quarter, lane, 128 * (int64_t)mt, n0, nn, out, b_free);
+            const int pair = tile / p.col_tiles, n0 = (tile - pair * p.col_tiles) * NB, nn = min(NB, p.N - n0);
+            const int64_t m0 = 128 * (int64_t)(2 * pair + rank);
+            if (p.y_type == kF32) mx4_pair_store<float>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
+            else if (p.y_type == kF16) mx4_pair_store<__half>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
+            else mx4_pair_store<__nv_bfloat16>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
         }
     }
     if (!ok && lane == 0) {
@@ -906,8 +955,10 @@ __global__ void __launch_bounds__(192, 1) us_mx4_many_kernel(const __grid_consta
     }
     tc_fence_before();
     __syncthreads();
+    // (neither block ends while the other may still reach its barriers or operands)
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     tc_fence_after();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm));
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tm));
 }
 
 }  // namespace us

@@ -163,6 +163,46 @@ def test_types_strides_and_out(b, xt, yt, N):
     assert torch.equal(y, b.mx4_linear(x.contiguous(), w, dtype=yt))
 
 
+# enough tiles for the pairs of SMs: an odd number of row tiles, one row or one token past a tile, none for a pair's second block, several tiles a pair
+@pytest.mark.parametrize("N,M,K", [(200, 18945, 300), (129, 19072, 256), (1100, 4097, 2049), (512, 20000, 513), (1153, 4224, 33), (2048, 5120, 1600)])
+@pytest.mark.parametrize("yt", [torch.float16, torch.float32])
+def test_many_tokens(b, N, M, K, yt):
+    x, w = draw(N, K, torch.float16, N), b.mx4_quantize(draw(M, K, torch.bfloat16, M))
+    q = b.mx4_quantize(x)
+    out = torch.full((N + 1, M + 3), 3.0, device="cuda", dtype=yt)
+    y = b.mx4_linear(q, w, out=out[:N, 1:1 + M])
+    b.mx4_check()
+    check_product(y, q.dequantize(), w.dequantize(), K)
+    assert (out[N] == 3).all() and (out[:, 0] == 3).all() and (out[:, 1 + M:] == 3).all()
+    for _ in range(3):
+        assert torch.equal(y, b.mx4_linear(x, w, dtype=yt))
+
+
+def test_many_tokens_on_two_streams(b):
+    """Products whose pairs of SMs share the GPU with each other and with a product of few tokens, back to back and captured."""
+    w = b.mx4_quantize(draw(9728, 1024, torch.float32, 1)).freeze()
+    x = [draw(n, 1024, torch.float16, n) for n in (512, 1024, 5)]
+    want = [b.mx4_linear(t, w) for t in x]
+    streams = [torch.cuda.Stream() for _ in x]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got.append((i, b.mx4_linear(x[i], w)))
+    torch.cuda.synchronize()
+    b.mx4_check()
+    assert all(torch.equal(y, want[i]) for i, y in got)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        y = [b.mx4_linear(t, w) for t in x]
+    for _ in range(3):
+        g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(y, want))
+    del g
+
+
 def test_nan_stays_in_its_row_and_column(b):
     x, w = draw(20, 600, torch.float32, 7), draw(300, 600, torch.float32, 8)
     x[3, 599] = float("nan")
