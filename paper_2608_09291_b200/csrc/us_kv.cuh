@@ -48,6 +48,10 @@ __device__ __forceinline__ KvSeq kv_seq(const KvSeqs& q, const KvPool& p, int s,
 }
 
 // ---- append --------------------------------------------------------------------------------------------------------------
+// A team of 32 to 128 threads has a block and head: the largest new magnitude first, then codes, and the older codes once more where the step
+// grew. Blocks have no order among them. Bound by memory where prompts are written (3 of up to 2000 tokens, 32 heads of 128, and contexts of up to
+// 2500 read back: 86 us for both, 57 at memory's rate), by the chain length -> table -> step -> codes where single tokens are (64, and
+// 300 tokens each read back: 37 us, 27 of them the reading's bytes).
 // code = RNE(x / s) for the exact quotient, x finite or not. The rounded product x * (1 / s) is within 2^-16 of the quotient: its nearest
 // integer is the code unless it lies that close to a border (1 of 25000 values; kv_code_near), where the sign of a fused multiply-add says on which side x
 // is (exact: a rounded sum is never on the other side of 0), or underflow would lose the border, where 64 bits decide.
@@ -223,6 +227,7 @@ __global__ void __launch_bounds__(128) us_kv_append_kernel(const __grid_constant
 }
 
 // ---- read ------------------------------------------------------------------------------------------------------------------
+// value = RN(code * step), 16 tokens of kReadHeads heads a block; bound by the values it writes.
 // K and V of the first `tokens` places of every sequence as values, [s][t][head][D]; 0 from a sequence's end on. Block (x, y, z): 16 tokens
 // (in one block of the cache, as every block has a multiple of 16) of sequence z, kReadHeads heads. A thread has 16 bytes of the
 // output at a time, so that a warp's stores are whole lines, four of them in flight. Bound by the bytes written.
@@ -301,6 +306,7 @@ __global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int
 //     them in the order of the CTAs.
 // A warp copies (TMA, swizzled so that the fragment loads meet no bank twice); four read, 32 tokens of a unit each (two groups side by
 // side: their chains of products overlap), with sums of their own that are joined at an item's end.
+// Bound by memory: 64 sequences of up to 8192 tokens, 64/8 heads: 100 us, 5.4 TB/s; one of 131072 tokens: 52 us, 5.1 TB/s.
 constexpr int kKvTile = 128;
 constexpr int kKvStart = 4;   // what an item's queries, sums and output cost, in units
 struct KvAttend {

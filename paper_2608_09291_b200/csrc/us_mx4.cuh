@@ -215,7 +215,7 @@ __device__ __forceinline__ void pair16(const Sixteen<T>& x, int i, float& a, flo
 
 // X (rows x K, row stride ldx) -> tiles. A warp takes 512 columns of a row (two tiles), sixteen a lane, two lanes a block; kMxUnroll of
 // them at a time, all loads first. With eight columns a lane the arithmetic around the elements kept the GPU at half its memory's rate
-// (8192 x 8192 bf16, 170 MB: 38 us).
+// (8192 x 8192 bf16, 170 MB: 38 us; with sixteen 29, 26 at memory's rate).
 constexpr int kMxUnroll = 2;
 template <class T>
 __global__ void __launch_bounds__(256) us_mx4_quantize_kernel(const T* X, int64_t ldx, int64_t rows, int64_t K, uint8_t* mx, int vec)
@@ -381,9 +381,10 @@ __global__ void __launch_bounds__(256) us_mx4_repack_kernel(uint8_t* codes, int6
 // D (128 weight rows x NB tokens, fp32, tensor memory) += W tile * X tile^T, 64 columns an instruction, the scale bytes copied from
 // shared to tensor memory in front of the four instructions of a 256-column stage. One warp copies (untiled bulk copies into a ring
 // of stages), one issues, four read the sums back and store.
-//   * Weights are the M side: every lane of tensor memory has a weight row, whatever the number of tokens; N = 16 .. 256.
+//   * Weights are the M side: every lane of tensor memory has a weight row, whatever the number of tokens; N = 16 .. 128 (more: pairs, below).
 //   * Few row tiles: the columns are split over a cluster of up to 16 CTAs, whose sums are added through distributed shared memory
 //     in the order of the ranks: no workspace, no atomics, the same result every time.
+//   * Bound by the weights' way from memory: 28672 x 8192, 8 tokens: 22 us, 5.6 TB/s; 4096 x 4096, one token: 4.6 us, most of it latency.
 //   * Few tokens (FUSE): the CTA quantises its own columns of X while its weights are on the way: one launch instead of two.
 struct Mx4Params {
     const uint8_t* w;
