@@ -733,8 +733,9 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
 // stays in L2, W is read about once. Each block has 128 of the rows, and loads half of the tokens for both: 35 KB a block and 256
 // columns, 52 KB for a block that works alone (4096 x 28672 x 8192, the tokens' quantisation included: 410 us = 4.7 PFLOP/s, 445 alone; K = 28672, M = 8192: 445 and 478).
 // Copies run ahead over the tiles' ends, and the sums of a tile leave tensor memory for shared memory, rounded, before the next
-// tile's products begin (half of the tokens at a time); they are stored while those run. What bounds it is the way from L2 to the SMs:
-// alone, it takes 307 us without its copies and 390 with a quarter of its products. 4, 5, 6 stages: 415, 406, 413 us.
+// tile's products begin (half of the tokens at a time); they are stored while those run. What bounds it is the way from L2 to the SMs
+// (a block alone takes 307 us without its copies and 390 with a quarter of its products) and, call after call, the power cap: 991 W at 1620 of
+// 1965 MHz. W in two copies a stage: 3 % slower. 4, 5, 6 stages: 415, 406, 413 us.
 // The first block of a pair issues for both: it learns from the second's idle MMA warp that its stage is full, and tells both when a
 // stage has been read and when a tile is done.
 struct Mx4Pair {
