@@ -731,7 +731,8 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
 // ---- the product of many tokens -------------------------------------------------------------------------------------------
 // Pairs of blocks (a cluster of two SMs, cta_group::2) walk over tiles of 256 weight rows x 256 tokens, all tokens of the rows in turn: X
 // stays in L2, W is read about once. Each block has 128 of the rows, and loads half of the tokens for both: 35 KB a block and 256
-// columns, 52 KB for a block that works alone (4096 x 28672 x 8192, the tokens' quantisation included: 410 us = 4.7 PFLOP/s, 445 alone; K = 28672, M = 8192: 445 and 478).
+// columns, 52 KB for a block that works alone (4096 x 28672 x 8192, the tokens' quantisation included: 410 us = 4.7 PFLOP/s, 445 alone;
+// K = 28672, M = 8192: 445 and 478).
 // Copies run ahead over the tiles' ends, and the sums of a tile leave tensor memory for shared memory, rounded, before the next
 // tile's products begin (half of the tokens at a time); they are stored while those run. What bounds it is the way from L2 to the SMs
 // (a block alone takes 307 us without its copies and 390 with a quarter of its products) and, call after call, the power cap: 991 W at 1620 of
