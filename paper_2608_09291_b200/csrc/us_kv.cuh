@@ -119,7 +119,9 @@ __global__ void __launch_bounds__(128) us_kv_append_kernel(const __grid_constant
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const KvPool& p = a.pool;
     const int lane = threadIdx.x & 31, me = threadIdx.x % TEAM, which = blockIdx.z;
-    const int h = min((int)(blockIdx.y * (128 / TEAM) + threadIdx.x / TEAM), p.Hkv - 1);   // (teams past the last head do its work again)
+    // (A team past the last head has nothing to do but the barrier: codes are rescaled in place, which nobody may do a second time.)
+    const int h = (int)(blockIdx.y * (128 / TEAM) + threadIdx.x / TEAM);
+    const bool real = h < p.Hkv;
     // which sequence's which block
     int s = -1, j = 0;
     uint32_t before = 0;
@@ -159,7 +161,7 @@ __global__ void __launch_bounds__(128) us_kv_append_kernel(const __grid_constant
     const int32_t blk = __ldcg(a.seqs.table + (int64_t)s * a.seqs.table_stride + bi);
     const int D = p.D, log2_per = D == 128 ? 4 : 3;   // D / 8 lanes a row
     const T_* x = static_cast<const T_*>(a.x[which]) + (q.first + lo - start) * a.token_stride[which] + (int64_t)h * a.head_stride[which];
-    const int units = n << log2_per;
+    const int units = real ? n << log2_per : 0;
     constexpr int KEEP = sizeof(T_) == 4 ? 4 : 8;
     Eight<T_> kept[KEEP];
     uint32_t big = 0;
@@ -184,7 +186,7 @@ __global__ void __launch_bounds__(128) us_kv_append_kernel(const __grid_constant
     const int64_t place = (int64_t)blk * p.Hkv + h;
     float* step_at = (which ? p.v_step : p.k_step) + place;
     int8_t* codes = (which ? p.v : p.k) + ((place << a.log2_T) * D);
-    const float old = held ? *step_at : 0.f;
+    const float old = held && real ? *step_at : 0.f;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i)
         if (me + TEAM * i < units) take(kept[i]);
@@ -199,6 +201,7 @@ __global__ void __launch_bounds__(128) us_kv_append_kernel(const __grid_constant
     } else {
         __syncwarp();   // (all lanes have read the old step)
     }
+    if (!real) return;
     const float step = fmaxf(old, __fdiv_rn(__uint_as_float(big), 127.f));
     if (me == 0) *step_at = step;
     const float inv = step >= 1e-30f ? __fdiv_rn(1.f, step) : 0.f;

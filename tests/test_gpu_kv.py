@@ -417,6 +417,37 @@ def test_append_token_by_token(b):
     cache.check()
 
 
+@pytest.mark.parametrize("Hkv", [1, 2, 3, 5])
+@pytest.mark.parametrize("T,D,n", [(256, 64, 1), (256, 128, 1), (32, 128, 2), (64, 64, 3), (16, 128, 2)])
+def test_older_codes_are_rescaled_once(b, T, D, n, Hkv):
+    """Hundreds of sequences whose only block fills up while every call makes its step grow: head counts that leave teams of a block of
+    the grid without a head, for each size of a team. Codes and steps must be equal to the definition's after every call."""
+    S = 400
+    g = gen(Hkv)
+    codes = [torch.randint(-127, 128, (S, Hkv, T, D), device="cuda", generator=g).to(torch.int8) for _ in range(2)]
+    steps = [0.01 + 0.01 * torch.rand(S, Hkv, device="cuda", generator=g) for _ in range(2)]
+    want = [[c.clone(), s.clone()] for c, s in zip(codes, steps)]
+    cache = b.KVCache(codes[0], codes[1], steps[0], steps[1])
+    order = torch.randperm(S, device="cuda", generator=g)
+    table, cu = order.int()[:, None], None if n == 1 else cu_of([n] * S)
+    for L in range(max(n, T - 40 * n), T + 1, n):
+        x = torch.randn(S * n, 2 * Hkv, D, device="cuda", generator=g)
+        for i in range(2):       # the largest magnitude of each new token is above all that the block holds
+            x[:, i * Hkv:(i + 1) * Hkv, L % D] = (want[i][1][order] * 127 * 1.03).repeat_interleave(n, 0)
+        cache.append(x[:, :Hkv], x[:, Hkv:], table, torch.full((S,), L, dtype=torch.int32, device="cuda"), cu)
+        for i, (c, s) in enumerate(want):
+            part = x[:, i * Hkv:(i + 1) * Hkv].view(S, n, Hkv, D).transpose(1, 2)
+            now = torch.maximum(s[order], part.abs().amax((2, 3)) / torch.tensor(127.0, device="cuda"))
+            assert L == n or (now > s[order]).all()
+            d = now.double()[..., None, None]
+            c[order, :, :L - n] = (c[order, :, :L - n].double() * s[order].double()[..., None, None] / d).round().to(torch.int8)
+            c[order, :, L - n:L] = (part.double() / d).round().clamp(-127, 127).to(torch.int8)
+            s[order] = now
+        for got, ref in zip((cache.k_codes, cache.k_steps, cache.v_codes, cache.v_steps), (want[0][0], want[0][1], want[1][0], want[1][1])):
+            assert torch.equal(got, ref)
+    cache.check()
+
+
 def test_offsets_past_32_bits(b):
     """A pool of more than 2^32 bytes of codes, its last blocks in use."""
     blocks, Hkv, T, D = 33000, 8, 128, 128
