@@ -956,6 +956,8 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
 // row's parts by the warps: one trip to memory for up to eight a warp. (One sequence of 131072 tokens, 8 cache heads, 37 parts each:
 // 62 us with the first form alone, 53 with the second; 64 of 4096, 2 or 3 parts each: 95 and 102.) Parts are added in
 // the same order every time.
+// Every block waits for the kernel before, those without a part, too: what follows in the stream waits for this grid alone, so this
+// grid may not end before the sums and outputs of the other one are there.
 constexpr int kJoinWarps = 4, kJoinFew = 4;
 template <int D, int NT, bool BF16>
 __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __grid_constant__ KvAttend a)
@@ -967,12 +969,14 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, me = blockIdx.x;
     const KvRange range = kv_range<R>(a, me, lane, false);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (range.u0 >= range.u1) return;
     bool waited = false;
-    auto join = [&](const KvItem& it, int item, int c0, int c1) {
-        if (c1 - c0 < kJoinFew && me != c0) return;
+    auto wait = [&]() {
         if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
         waited = true;
+    };
+    auto join = [&](const KvItem& it, int item, int c0, int c1) {
+        if (c1 - c0 < kJoinFew && me != c0) return;
+        wait();
         const int h = item % a.pool.Hkv, row0 = item / a.pool.Hkv * R, rows = min(R, it.rows - row0);
         const int np = c1 - c0 + 1;
         if (np <= kJoinFew) {
@@ -1080,29 +1084,33 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
             __syncthreads();
         }
     };
-    // the item that the CTA's first unit belongs to, if it began in an earlier CTA
-    int s = range.s;
-    KvItem it = range.item;
-    long long start = range.u0 - range.in_seq;   // first unit of the sequence
-    {
-        const int item = kv_div(range.in_seq, it.cost());
-        const long long first = start + (long long)item * it.cost() + kKvStart;
-        if (first < range.u0) {
-            join(it, item, range.shares.owner(first), range.shares.owner(first + it.tiles - 1));
-            if (first + it.tiles >= range.u1) return;
+    auto walk = [&]() {
+        // the item that the CTA's first unit belongs to, if it began in an earlier CTA
+        int s = range.s;
+        KvItem it = range.item;
+        long long start = range.u0 - range.in_seq;   // first unit of the sequence
+        {
+            const int item = kv_div(range.in_seq, it.cost());
+            const long long first = start + (long long)item * it.cost() + kKvStart;
+            if (first < range.u0) {
+                join(it, item, range.shares.owner(first), range.shares.owner(first + it.tiles - 1));
+                if (first + it.tiles >= range.u1) return;
+            }
         }
-    }
-    // the item that its last unit belongs to, if it begins here and ends in a later one
-    long long units = (long long)it.row_tiles * a.pool.Hkv * it.cost();
-    while (start + units <= range.u1 - 1) {
-        start += units;
-        if (++s >= a.seqs.S) return;
-        it = kv_item<R>(a, s);
-        units = (long long)it.row_tiles * a.pool.Hkv * it.cost();
-    }
-    const int item = kv_div(range.u1 - 1 - start, it.cost());
-    const long long first = start + (long long)item * it.cost() + kKvStart, end = first + it.tiles;
-    if (first >= range.u0 && first < range.u1 && end > range.u1) join(it, item, me, range.shares.owner(end - 1));
+        // the item that its last unit belongs to, if it begins here and ends in a later one
+        long long units = (long long)it.row_tiles * a.pool.Hkv * it.cost();
+        while (start + units <= range.u1 - 1) {
+            start += units;
+            if (++s >= a.seqs.S) return;
+            it = kv_item<R>(a, s);
+            units = (long long)it.row_tiles * a.pool.Hkv * it.cost();
+        }
+        const int item = kv_div(range.u1 - 1 - start, it.cost());
+        const long long first = start + (long long)item * it.cost() + kKvStart, end = first + it.tiles;
+        if (first >= range.u0 && first < range.u1 && end > range.u1) join(it, item, me, range.shares.owner(end - 1));
+    };
+    if (range.u0 < range.u1) walk();
+    wait();
 }
 
 }  // namespace us

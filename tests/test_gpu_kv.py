@@ -542,6 +542,67 @@ def test_two_streams_at_once(b):
         assert all(torch.equal(y, w) for y in g)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("S,G,n", [(3, 8, 1), (3000, 8, 1), (2000, 2, 3), (1500, 16, 1)])
+def test_what_follows_attention_waits_for_it(b, dtype, S, G, n):
+    """Contexts of at most 128 tokens in a table of 4096: nothing is cut, so the kernel that joins parts has none. What the library launches
+    behind it (a product that reads the output, an append that writes the blocks, the next attention into the same output) gives what it
+    gives with a synchronisation in between."""
+    Hkv, D, T = 2, 128, 64
+    lens = [n + (29 * i) % (128 - n) for i in range(S)]
+    cache, table, lengths = make(b, lens, Hkv, D, T, 3, width=4096 // T)
+    cu = None if n == 1 else cu_of([n] * S)
+    q = [torch.randn(S * n, G * Hkv, D, device="cuda", generator=gen(i)).to(dtype) for i in (4, 5)]
+    w = b.mx4_quantize(torch.randn(128, G * Hkv * D, device="cuda", generator=gen(6)) / 32).freeze()
+    x = torch.randn(S * n, 2 * Hkv, D, device="cuda", generator=gen(7)).to(dtype)
+    held = (cache.k_codes, cache.k_steps, cache.v_codes, cache.v_steps)
+    before = [t.clone() for t in held]
+    out = torch.empty_like(q[0])
+
+    def calls(pause):
+        ys = []
+        for part in q:
+            cache.attention(part, table, lengths, cu, out=out)
+            pause()
+            ys.append(b.mx4_linear(out.flatten(1), w))
+            pause()
+        cache.attention(q[0], table, lengths, cu, out=out)
+        pause()
+        cache.append(x[:, :Hkv], x[:, Hkv:], table, lengths, cu)
+        pause()
+        return ys
+
+    def restore():
+        for t, o in zip(held, before):
+            t.copy_(o)
+        out.fill_(1000)
+        torch.cuda.synchronize()
+
+    restore()
+    want = calls(torch.cuda.synchronize) + [out.clone()]
+    ref, bound, _ = reference(cache_of(b, before), table, lens[:40], [n] * min(S, 40), q[0][:40 * n], D ** -0.5)
+    check(want[2][:40 * n], ref, bound)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = calls(lambda: None)
+    for _ in range(5):
+        restore()
+        got = calls(lambda: None)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(want, got + [out]))
+        restore()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(want, captured + [out]))
+    cache.check()
+    b.mx4_check()
+    del graph
+
+
+def cache_of(b, held):
+    return b.KVCache(held[0], held[2], held[1], held[3])
+
+
 def test_refusals(b):
     cache, table, lengths = make(b, [100, 50], 2, 128, 64, 1)
     q, k = torch.zeros(2, 4, 128, device="cuda").half(), torch.zeros(2, 2, 128, device="cuda").half()
