@@ -642,8 +642,8 @@ __global__ void __launch_bounds__(kPrRows) us_kv_prompt_join_kernel(const __grid
     for (int s = 0; s < a.splits; ++s) {
         const float* x = part + s * S::kPart;
         const float l = __ldcg(x + kPrRows * D + kPrRows + local), w = kv_weight(__ldcg(x + kPrRows * D + local), l, base);
+        sum += w * l;             // (a part that is NaN has no maximum, and so no weight: its NaN comes from here)
         if (w == 0.f) continue;   // (a part without units has no sums)
-        sum += w * l;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float4 v = __ldcg(reinterpret_cast<const float4*>(x + ((c0 + i) * kPrRows + local) * 4));

@@ -206,6 +206,28 @@ def test_nan_stays_in_its_rows(b, new):
     assert torch.isnan(got[2 * new - 1, :4]).all()
 
 
+@pytest.mark.parametrize("new,width", [(1, 4096), (60, 300), (60, 4096), (500, 4096)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_nan_stays_in_its_rows_of_cut_items(b, new, width, D):
+    """A table that is wide enough for the walk over a context to be cut: rows that are NaN are so in both results, the others are as without them."""
+    cache, table, lengths = make(b, [3000], 2, D, 64, 3, width=width // 64 + 45)
+    q = torch.randn(new, 8, D, device="cuda", generator=gen(4)).half()
+    cu, hit = cu_of([new]), torch.zeros(new, 8, dtype=torch.bool, device="cuda")
+    lse = [torch.full((new, 8), 5.0, device="cuda") for _ in range(3)]
+    want = cache.attention(q, table, lengths, cu, lse=lse[0])
+    bad = q.clone()
+    bad[0, 3, 7], bad[new - 1, 5, 40] = float("nan"), float("inf")
+    hit[0, 3] = hit[new - 1, 5] = True
+    got = cache.attention(bad, table, lengths, cu, lse=lse[1])
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], want[~hit])
+    assert torch.isnan(lse[1][hit]).all() and torch.equal(lse[1][~hit], lse[0][~hit])
+    cache.k_steps[table[0, 20].long(), 1] = float("nan")       # all rows of a head see it
+    got = cache.attention(q, table, lengths, cu, lse=lse[2])
+    assert torch.isnan(got[:, 4:]).all() and torch.equal(got[:, :4], want[:, :4])
+    assert torch.isnan(lse[2][:, 4:]).all() and torch.equal(lse[2][:, :4], lse[0][:, :4])
+    cache.check()
+
+
 @pytest.mark.parametrize("new", [[1, 1, 1], [2, 40, 9], [100, 30, 250]])
 def test_strides_and_rows_behind(b, new):
     """q and out as views of wider rows, heads outermost; rows behind the last sequence stay as they are."""
