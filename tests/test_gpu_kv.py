@@ -169,6 +169,52 @@ def test_long(b, L, G, new):
     run(b, [L], [new], G, 1, 128, 64, torch.bfloat16, seed=1)
 
 
+def closely(cache, table, L, n, q, scale=None, causal=True, window=0, exact_p=False):
+    """(out, bound on the error before the last rounding) of one sequence in 64 bits, with a bound that stays below the outputs of long contexts.
+
+    Of each row, with p normalised: the scores' error as above; p's rounding, 2^-11 (fp16; exact_p: it is kept, 2^-22) and 2^-19, of sum p |v|;
+    p below the smallest normal fp16 number: p times V's step carries 2^7 relative to a place that is at most the largest of them, rounded up to
+    a power of two: 2^-25 2^-7 2 max(p step) a token seen, times a code of 127; fp32 sums of numerator and denominator, each addition off by up
+    to 2^-23 of the magnitudes: for up to 32 rows a head four in 128 tokens of a block's share, four warps and the parts of all shares, else one in 16 tokens."""
+    D, Hkv, T = q.shape[2], cache.n_kv_heads, cache.block_tokens
+    scale = D ** -0.5 if scale is None else scale
+    x, rep = q.double(), q.shape[1] // Hkv
+    k, v = [t.repeat_interleave(rep, 1) for t in values(cache, table, L, 0)]
+    step = cache.v_steps[table[0, torch.arange(L, device="cuda") // T].long()].double().repeat_interleave(rep, 1).t()[:, None]    # (H, 1, L)
+    a = torch.einsum("nhd,lhd->hnl", x, k) * scale
+    mag = torch.einsum("nhd,lhd->hnl", x.abs(), k.abs()) * abs(scale)
+    t, pos = torch.arange(L, device="cuda"), torch.arange(L - n, L, device="cuda")[:, None]
+    seen = (t <= pos) if causal else torch.ones(n, L, dtype=torch.bool, device="cuda")
+    if window:
+        seen = seen & (t > pos - window)
+    p = torch.softmax(a.masked_fill(~seen, -math.inf), -1)
+    ds = (D + 4) * 2.0 ** -23 * mag.masked_fill(~seen, 0).amax(-1)
+    if n * rep <= 32:
+        blocks = 2 * torch.cuda.get_device_properties(0).multi_processor_count
+        adds = 4 * -(-(-(-n * rep // 8) * Hkv * (L / 128 + 6)) // blocks) + 4 + min(blocks, L / 128 + 1)
+    else:
+        adds = L / 16 + 64
+    rel = torch.expm1(2 * ds) + (2.0 ** -22 if exact_p else 2.0 ** -11) + 2.0 ** -19 + 2 * adds * 2.0 ** -23
+    # (an exactly 0 p has no weight, whatever its step)
+    absolute = 2.0 ** -31 * 127 * seen.sum(-1) * torch.where(p > 0, p * step, torch.zeros((), dtype=torch.float64, device="cuda")).amax(-1)
+    vs = torch.where((p > 0).any(1).t()[..., None], v, torch.zeros((), dtype=torch.float64, device="cuda"))
+    o, m = torch.einsum("hnl,lhd->nhd", p, vs), torch.einsum("hnl,lhd->nhd", p, vs.abs())
+    return o, rel.t()[..., None] * m + absolute.t()[..., None]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("L,G,Hkv,new,D", [(131072, 1, 1, 1, 128), (131072, 8, 1, 1, 64), (40000, 16, 2, 1, 128), (30000, 5, 2, 3, 128), (20000, 8, 1, 16, 128), (70000, 4, 1, 70, 128)])
+def test_long_contexts_closely(b, dtype, L, G, Hkv, new, D):
+    """Outputs of long contexts are small: with a bound that is smaller still."""
+    cache, table, lengths = make(b, [L], Hkv, D, 64, 2)
+    q = torch.randn(new, G * Hkv, D, device="cuda", generator=gen(3)).to(dtype)
+    out = cache.attention(q, table, lengths, None if new == 1 else cu_of([new]))
+    cache.check()
+    ref, bound = closely(cache, table, L, new, q, exact_p=dtype == torch.float16 and new * G <= 8)
+    assert bound.square().mean() < ref.square().mean() / 9
+    check(out, ref, bound)
+
+
 def test_many_sequences(b):
     lens = [(37 * i) % 300 for i in range(1, 101)] + [0, 5000, 0, 1]
     run(b, lens, [1] * 104, 16, 2, 128, 64, torch.float16)
