@@ -300,9 +300,10 @@ __global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int
 //   * The rows of a tile are the query heads that share a cache head (times the sequence's new tokens): 8 NT of them are the N side
 //     of mma.sync m16n8k16, 16 tokens (then 16 of D) the M side: the cache's bytes are read once for all of them.
 //   * Codes become fp16 in registers, exactly (0x6400 | byte is 1024 + byte); a step is one number for 16 tokens, so K's is
-//     a factor of the scores and V's a factor of p. p is rounded to fp16 with 2^7 in front and V's step relative to the
-//     largest so far: what a row sums stays between 2^-24 and 2^15 of the largest term; sums are fp32.
-//   * m follows the true maximum only where it is 2^8 behind, so most units need no reduction over lanes and no rescaling.
+//     a factor of the scores and V's a factor of p. What is rounded to fp16 is p v_step 2^7 relative to a second running maximum of
+//     each row, that of s_t + log2 v_step: terms down to 2^-21 of a row's largest keep their 11 bits, whatever the steps of tokens
+//     are that it does not see or that have no weight in it. sum p v is held relative to that one, sum p relative to m; both are fp32.
+//   * Both follow the true maximum only where one is 2^8 behind, so most units need no reduction over lanes and no rescaling.
 //   * All (sequence, row tile, head) items in a row, 128 tokens a unit and kKvStart units for beginning one: every CTA takes the same
 //     number of units, whatever the lengths. (64 sequences of 1 to 8192 tokens, 64/8 heads: 148 us without the units for beginning,
 //     where the CTAs with the short sequences were last, 120 with 2, 110 with 3, 104 with 4.) An item that is cut leaves its parts in scratch, and a second kernel joins
@@ -483,6 +484,8 @@ __device__ __forceinline__ bool bar_consumers(bool fail = false)
                  : "=r"(any) : "r"((uint32_t)fail) : "memory");
     return any != 0;
 }
+// A number that log2 of a step is at most; -126 at least, so that what it is added to is not lost
+__device__ __forceinline__ float kv_log2_above(float step) { return (float)((int)((__float_as_uint(step) >> 23) & 0xFFu) - 126); }
 template <bool BF16>
 __device__ __forceinline__ float q_at(const void* q, int64_t i) { return BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(q)[i]) : __half2float(static_cast<const __half*>(q)[i]); }
 template <bool BF16>
@@ -685,18 +688,17 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
             all_lo = __reduce_max_sync(0xffffffffu, all_lo);
             all_hi = __reduce_min_sync(0xffffffffu, all_hi);
             const int last_hi = a.causal ? pos0 + (min(row0 + R, it.rows) - 1) / a.G + 1 : it.seq.len;
-            float m[NT][2], mb[NT][2], l[NT][2], o[MT][NT][4];   // mb: 7 - m
+            float m[NT][2], r[NT][2], l[NT][2], o[MT][NT][4];   // r: m less the reference of p times V's step
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) { m[nt][c] = -INFINITY; mb[nt][c] = INFINITY; l[nt][c] = 0.f; }
+                for (int c = 0; c < 2; ++c) { m[nt][c] = -INFINITY; r[nt][c] = l[nt][c] = 0.f; }
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) o[i][nt][c] = 0.f;
-            float ref = 0.f, inv_ref = 0.f;   // V's largest step so far; its inverse, 0 where that is no good
             int tok0 = (it.t_lo + tile) * kKvTile + 32 * warp;
 #pragma unroll 1
             for (int i = 0; i < n; ++i, tok0 += kKvTile) {
@@ -735,7 +737,8 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                                 for (int nt = 0; nt < NT; ++nt) mma_f16(sc[b][nt], a0, a1, a2, a3, qf[nt][4 * c + j][0], qf[nt][4 * c + j][1]);
                             }
                     }
-                    // e = s - m + 7: more than 15 where m is more than 2^8 behind (or nothing was seen yet)
+                    // e = s - m + 7: more than 15 where m is more than 2^8 behind (or nothing was seen yet), or with V's step and r added
+                    const float lv[2] = {kv_log2_above(stv[0]), kv_log2_above(stv[1])};
                     float e[2][NT][4];
                     bool behind = false;
                     auto exponents = [&]() {
@@ -744,7 +747,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                for (int c = 0; c < 4; ++c) e[b][nt][c] = fmaf(sc[b][nt][c], f[nt][c & 1] * stk[b], mb[nt][c & 1]);
+                                for (int c = 0; c < 4; ++c) e[b][nt][c] = fmaf(sc[b][nt][c], f[nt][c & 1] * stk[b], 7.f - m[nt][c & 1]);
                         if (edge)
 #pragma unroll
                             for (int b = 0; b < 2; ++b)
@@ -762,51 +765,52 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) behind |= e[b][nt][c] > 15.f;
+                            for (int c = 0; c < 4; ++c) behind |= e[b][nt][c] > fminf(15.f, 15.f - (lv[b] + r[nt][c & 1]));
                     if (__any_sync(0xffffffffu, behind)) {
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int c = 0; c < 2; ++c) {
-                                float x = -INFINITY;
+                                float x = -INFINITY, y = -INFINITY;   // largest scores, and with V's steps
 #pragma unroll
                                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                                     for (int q = 0; q < 2; ++q)
-                                        if (e[b][nt][c + 2 * q] > -INFINITY) x = fmaxf(x, sc[b][nt][c + 2 * q] * (f[nt][c] * stk[b]));
-                                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-                                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                                        if (e[b][nt][c + 2 * q] > -INFINITY) {
+                                            const float sco = sc[b][nt][c + 2 * q] * (f[nt][c] * stk[b]);
+                                            x = fmaxf(x, sco);
+                                            y = fmaxf(y, sco + lv[b]);
+                                        }
+#pragma unroll
+                                for (int i = 4; i <= 16; i *= 2) {
+                                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, i));
+                                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, i));
+                                }
                                 x = fmaxf(x, m[nt][c]);
-                                const float alpha = x == -INFINITY ? 1.f : exp2_fast(m[nt][c] - x);
+                                y = fmaxf(y, m[nt][c] - r[nt][c]);
+                                const float rn = x == -INFINITY ? 0.f : fmaxf(x - y, -126.f);   // (at most 126: kv_log2_above)
+                                const float by = x == -INFINITY ? 0.f : m[nt][c] - x, alpha = exp2_fast(by + (rn - r[nt][c]));
+                                l[nt][c] *= exp2_fast(by);
                                 m[nt][c] = x;
-                                mb[nt][c] = x == -INFINITY ? INFINITY : 7.f - x;
-                                l[nt][c] *= alpha;
+                                r[nt][c] = rn;
 #pragma unroll
                                 for (int k = 0; k < MT; ++k) { o[k][nt][c] *= alpha; o[k][nt][c + 2] *= alpha; }
                             }
                         exponents();
-                    }
-                    const float top = fmaxf(stk[0] < 0.f ? 0.f : stv[0], stk[1] < 0.f ? 0.f : stv[1]);
-                    if (top > ref) {
-                        const float b = ref / top;
-                        ref = top;
-                        inv_ref = top > 1e-30f && top < 1e30f ? 1.f / top : 0.f;
-#pragma unroll
-                        for (int k = 0; k < MT; ++k)
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) o[k][nt][c] *= b;
                     }
                     // (fp16 output, few rows: what the rounding of p leaves is multiplied, too; else its 2^-12 would be as much as the output's own)
                     constexpr bool REST = !BF16 && NT == 1;
                     uint32_t pf[2][NT][2], pr[2][NT][2];
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        const float rel = stk[b] < 0.f ? 0.f : inv_ref > 0.f ? stv[b] * inv_ref : stv[b] == ref ? 1.f : __fdiv_rn(stv[b], ref);   // (NaN: NaN)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
+                            float rel[2];   // V's step for each row; where a row sees none of the group 0, whatever the step is
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                rel[c] = stv[b] * exp2_fast(r[nt][c]);
+                                if (edge && (tok0 + 16 * b >= hi[nt][c] || tok0 + 16 * b + 16 <= lo[nt][c] || stk[b] < 0.f)) rel[c] = 0.f;
+                            }
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
                                 e[b][nt][c] = exp2_fast(e[b][nt][c]);
@@ -814,7 +818,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                             }
 #pragma unroll
                             for (int c = 0; c < 2; ++c) {
-                                const float p0 = e[b][nt][2 * c] * rel, p1 = e[b][nt][2 * c + 1] * rel;
+                                const float p0 = e[b][nt][2 * c] * rel[0], p1 = e[b][nt][2 * c + 1] * rel[1];
                                 const uint32_t h = half2_bits(p0, p1);
                                 pf[b][nt][c] = transpose8(h);
                                 if (REST) {
@@ -912,7 +916,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
                                 float* at = sums + (8 * nt + 2 * t + (c & 1)) * S::kPitch + (2 * k + (c >> 1)) * 8 + g;
-                                const float x = w[nt][c & 1] == 0.f ? 0.f : o[k][nt][c] * ref * w[nt][c & 1];
+                                const float x = w[nt][c & 1] == 0.f ? 0.f : o[k][nt][c] * exp2_fast(-r[nt][c & 1]) * w[nt][c & 1];
                                 *at = turn ? *at + x : x;
                             }
                 bar_consumers();

@@ -215,6 +215,59 @@ def test_long_contexts_closely(b, dtype, L, G, Hkv, new, D):
     check(out, ref, bound)
 
 
+# new tokens, query heads a cache head, blocks of the table: up to 32 rows a cache head take the kernel of single tokens
+KINDS = [(3, 2, 60), (8, 2, 60), (16, 2, 60), (32, 1, 2000)]
+
+
+@pytest.mark.parametrize("new,G,width", KINDS)
+@pytest.mark.parametrize("D,T", [(128, 16), (64, 64)])
+@pytest.mark.parametrize("power", [12, 24, 60])
+@pytest.mark.parametrize("window", [0, 100])
+def test_steps_of_tokens_that_a_row_does_not_see(b, new, G, width, D, T, power, window):
+    """Values of later tokens (and of ones in front of the window) that are larger by any factor: each row is as exact as its own tokens allow."""
+    L = 900
+    cache, table, lengths = make(b, [L], 2, D, T, 5, width=width)
+    cache.v_steps[table[0, (L - 1) // T].long()] *= 2.0 ** power          # the last block: only the last rows see it
+    if window:
+        cache.v_steps[table[0, (L - new - 90) // T].long()] *= 2.0 ** power     # in front of the last rows' window, where there are enough rows
+    q = torch.randn(new, 2 * G, D, device="cuda", generator=gen(1)).bfloat16()
+    out = cache.attention(q, table, lengths, cu_of([new]), window=window)
+    cache.check()
+    ref, bound = closely(cache, table, L, new, q, window=window)
+    check(out, ref, bound)
+    # (a NaN among what a row does not see is none of its business)
+    cache.v_steps[table[0, (L - 1) // T].long()] = float("nan")
+    got = cache.attention(q, table, lengths, cu_of([new]), window=window)
+    blind = L - new + torch.arange(new, device="cuda") < (L - 1) // T * T
+    assert blind.any() == (new > 4)
+    check(got[blind], ref[blind], bound[blind])
+    assert torch.isnan(got[~blind]).all()
+
+
+@pytest.mark.parametrize("new,G,width", [(1, 1, 60), (1, 8, 2000), (1, 16, 60)] + KINDS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("away,power", [(30, 24), (90, 40), (90, 100), (1000, 60), (12, 20)])
+def test_steps_of_tokens_without_weight(b, new, G, width, D, away, power):
+    """A block whose values are 2^power larger and whose scores are `away` below the others': what it adds counts for what it is."""
+    L, T = 700, 16
+    cache, table, lengths = make(b, [L], 1, D, T, 6, width=width)
+    q = torch.randn(new, G, D, device="cuda", generator=gen(1))
+    q[..., 0] = 4.0
+    for i in (3, 30):
+        blk = table[0, i].long()
+        cache.k_codes[blk] = 0
+        cache.k_codes[blk, :, :, 0] = -127
+        cache.k_steps[blk] = away / (127 * 4.0 * D ** -0.5)
+        cache.v_steps[blk] *= 2.0 ** power
+    q = q.half()
+    out = cache.attention(q, table, lengths, None if new == 1 else cu_of([new]))
+    cache.check()
+    ref, bound = closely(cache, table, L, new, q)
+    ok = ref.abs() + bound < 60000                   # (fp16 holds them)
+    assert not torch.isnan(out).any()
+    check(out[ok], ref[ok], bound[ok])
+
+
 def test_many_sequences(b):
     lens = [(37 * i) % 300 for i in range(1, 101)] + [0, 5000, 0, 1]
     run(b, lens, [1] * 104, 16, 2, 128, 64, torch.float16)
