@@ -7,7 +7,8 @@
 //   MMA       one warp: S = Q K^T into tensor memory, O += P V with P from tensor memory, for the two tiles in turn: while one tile's
 //             scores are being turned into P the other tile's products run.
 //   softmax   four warps a tile, a thread a row: no exchange between lanes. Steps: one number for 16 tokens, K's a factor of the
-//             scores, V's in the exponent of p (relative to the largest so far), so that a unit's P V needs no scaling. P takes the place of S.
+//             scores, V's in the exponent of p (relative to a second running maximum of each row, see us_kv.cuh), so that a unit's P V
+//             needs no scaling. P takes the place of S.
 // m follows the true maximum only where it is 2^8 behind; p carries 2^7, see us_kv.cuh. The scores' conversions, the
 // 16384 exponentials (16 a cycle) and the two products (1024 cycles) of a tile and unit are each about 1000 cycles, and overlap.
 // Three prompts of up to 2000 tokens, to contexts of up to 4500 (64/8 heads of 128, bf16): 720 us; one of 8192 tokens: 1275 us, 863 TFLOP/s. What
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
     constexpr int HALVES = D / 64;   // 128-byte columns of fp16
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[24];
-    __shared__ float4 steps[4][8];   // of a unit's 16-token groups: K's step (-1: not there), V's, its log2, its inverse
+    __shared__ float4 steps[4][8];   // of a unit's 16-token groups: K's step (-1: not there), V's, its log2 (-126 to 128), its inverse
     __shared__ uint32_t misc[2];
     uint8_t* sq = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t* sk = sq + 2 * S::kQ;
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
         const int pos = it.seq.len - it.seq.n + tok;
         // (rows past the last are zero queries that see everything; never stored)
         const int hi = real ? (a.causal ? pos + 1 : it.seq.len) : 0x7FFFFFFF, lo = real && a.window > 0 ? pos - a.window + 1 : -0x7FFFFFFF;
-        float m = -INFINITY, l = 0.f, ref = 0.f, lref = 0.f, f = a.scale2;
+        float m = -INFINITY, l = 0.f, lead = 0.f, most = 0.f, f = a.scale2;   // lead: m less the reference of p times V's step; most: V's largest step so far
         if (qi < nq && n > 0) {
             // the row as fp16, bf16 times a power of two that brings it into range, to its place in the operand
             const uint16_t* src = static_cast<const uint16_t*>(a.q) + (it.seq.first + tok) * a.q_token + (int64_t)qh * a.q_head;
@@ -255,18 +256,13 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                 if (!ok) break;
                 const float4* st = steps[j & 3];
                 const int tok0 = (u0 + j) * kPrTile;
-                // V's steps: the largest so far is the reference; the fast path needs all of the unit's within 2^13 of it
+                // V's steps: the fast path has the sum of p from p times the step, and needs all of the unit's within 2^60 of the largest so far
                 const float2 mine = *reinterpret_cast<const float2*>(&st[lane & 7]);
-                float top = fmaxf(mine.y, 0.f), grow = 1.f;
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-                if (top > ref) {
-                    grow = ref / top;
-                    ref = top;
-                    lref = log2f(top);
-                }
-                const bool fast = __all_sync(0xffffffffu, mine.x >= 0.f && mine.y >= ref * 0x1p-13f && mine.y > 1e-30f && ref < 1e30f && lo <= tok0 && hi >= tok0 + kPrTile);
+                most = fmaxf(most, mine.y);
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 4));
+                const bool fast = __all_sync(0xffffffffu, mine.x >= 0.f && mine.y >= most * 0x1p-60f && mine.y > 1e-30f && most < 1e30f && lo <= tok0 && hi >= tok0 + kPrTile);
                 float fk[8];
 #pragma unroll
                 for (int g = 0; g < 8; ++g) fk[g] = f * st[g].x;
@@ -282,7 +278,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                 for (int c = 0; c < 4; ++c) pin32(x[c]);
                 // which of the unit's tokens the row sees
                 uint32_t sees[4];
-                float mx = -INFINITY;
+                float mx = -INFINITY, my = -INFINITY;   // largest scores, and with V's steps
                 if (!fast) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -302,15 +298,19 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
 #pragma unroll
                         for (int i = 0; i < 14; i += 2) v = max3(v, __uint_as_float(x[c][16 * g + i]), __uint_as_float(x[c][16 * g + i + 1]));
                         v = fmaxf(v, __uint_as_float(x[c][16 * g + 14]));
-                        mx = fmaxf(mx, v * fmaxf(fk[2 * c + g], 0.f));   // (a group that is not there: -inf x 0, no maximum)
+                        v *= fmaxf(fk[2 * c + g], 0.f);   // (a group that is not there: -inf x 0, no maximum)
+                        mx = fmaxf(mx, v);
+                        my = fmaxf(my, v + st[2 * c + g].z);
                     }
-                // a new maximum, only where the old one is 2^8 behind
-                float alpha = grow;
-                if (mx > m + 8.f) {
-                    const float e = m == -INFINITY ? 0.f : exp2_fast(m - mx);
-                    alpha *= e;
-                    l *= e;
-                    m = mx;
+                // new maxima, only where an old one is 2^8 behind
+                float alpha = 1.f;
+                if (mx > m + 8.f || my > m - lead + 8.f) {
+                    const float to = fmaxf(mx, m), now = fmaxf(to - fmaxf(my, m - lead), -126.f);   // (at most 126: no step's logarithm is below -126)
+                    const float by = m - to;
+                    alpha = exp2_fast(by + (now - lead));
+                    l *= exp2_fast(by);
+                    m = to;
+                    lead = now;
                 }
                 if (__any_sync(0xffffffffu, alpha != 1.f) && j > 0) {   // (the sums so far are complete: their product was issued before S's)
 #pragma unroll 1
@@ -331,6 +331,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                 };
                 const float base = 7.f - (m == -INFINITY ? 0.f : m);
                 if (fast) {
+                    const float back = exp2_fast(-lead);
                     float sum = 0.f;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                         // (step by step over the 32: all arguments, all exponentials, then what uses them)
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
-                            const float k = fk[2 * c + g], b = base + (st[2 * c + g].z - lref);
+                            const float k = fk[2 * c + g], b = base + (st[2 * c + g].z + lead);
                             const uint64_t k2 = f32x2(k, k), b2 = f32x2(b, b);
 #pragma unroll
                             for (int i = 16 * g; i < 16 * g + 16; i += 2) {
@@ -361,20 +362,21 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                             }
                             float p0, p1;
                             f32x2_split(part, p0, p1);
-                            sum = fmaf(p0 + p1, ref * st[2 * c + g].w, sum);   // (p without V's step)
+                            sum = fmaf(p0 + p1, back * st[2 * c + g].w, sum);   // (p without V's step)
                         }
                         tc_st16_lanes(t_s + 16u * c, y);
                         if (c == 1) publish(0);
                     }
                     l += sum;
                 } else {
+                    const float away = exp2_fast(lead);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         uint32_t y[16];
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
                             const float2 kv = *reinterpret_cast<const float2*>(&st[2 * c + g]);
-                            const float k = fk[2 * c + g], rel = kv.y == ref ? 1.f : __fdiv_rn(kv.y, ref);
+                            const float k = fk[2 * c + g], rel = kv.y * away;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 float e[2];
@@ -399,7 +401,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             tc_fence_after();
         }
         if (qi < nq && ok) {
-            const float inv = l == 0.f ? 0.f : ref / l;
+            const float back = exp2_fast(-lead), inv = l == 0.f ? 0.f : back / l;
             float* part = a.part + (((int64_t)index * p.Hkv + h) * a.splits + split) * S::kPart;
             if (real && a.splits > 1) {
                 part[kPrRows * D + local] = m;
@@ -424,7 +426,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         *reinterpret_cast<float4*>(part + ((8 * c + i) * kPrRows + local) * 4) =
-                            make_float4(__uint_as_float(x[4 * i]) * ref, __uint_as_float(x[4 * i + 1]) * ref, __uint_as_float(x[4 * i + 2]) * ref, __uint_as_float(x[4 * i + 3]) * ref);
+                            make_float4(__uint_as_float(x[4 * i]) * back, __uint_as_float(x[4 * i + 1]) * back, __uint_as_float(x[4 * i + 2]) * back, __uint_as_float(x[4 * i + 3]) * back);
                     continue;
                 }
                 uint32_t y[16];
@@ -527,7 +529,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             if (!ok) break;
             if (lane < 2) {
                 const float2 s2 = lane ? here[1] : here[0];
-                steps[j & 3][2 * w + lane] = make_float4(s2.x, s2.y, log2f(s2.y), 1.f / s2.y);
+                steps[j & 3][2 * w + lane] = make_float4(s2.x, s2.y, fminf(fmaxf(log2f(s2.y), -126.f), 128.f), 1.f / s2.y);
             }
             store(sk + slot * S::kKV, kx);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

@@ -215,8 +215,9 @@ def test_long_contexts_closely(b, dtype, L, G, Hkv, new, D):
     check(out, ref, bound)
 
 
-# new tokens, query heads a cache head, blocks of the table: up to 32 rows a cache head take the kernel of single tokens
-KINDS = [(3, 2, 60), (8, 2, 60), (16, 2, 60), (32, 1, 2000)]
+# new tokens, query heads a cache head, blocks of the table: up to 32 rows a cache head take the kernel of single tokens, more the one of
+# prompts; a table that is wide enough cuts its walk
+KINDS = [(3, 2, 60), (8, 2, 60), (16, 2, 60), (32, 1, 2000), (60, 2, 60), (60, 2, 2000), (300, 1, 60)]
 
 
 @pytest.mark.parametrize("new,G,width", KINDS)
