@@ -355,6 +355,9 @@ us_status us_mx4_last_error(void);
  *   strides in elements; rows past cu_tokens[n_seqs] are left as they are. lse (N x n_heads fp32, or NULL): the logarithm
  *   of the sum of exp(scale q.k_t), -inf where nothing is seen. scratch: us_kv_attention_scratch bytes (-1: bad arguments), 16-byte aligned,
  *   for one call at a time; need not be cleared. Blocks wholly in front of every window may be gone (any table entry).
+ *   Scores and sums are held in fp32. p times V's step is rounded to 11 bits for the product with V's codes, relative to the largest that
+ *   the row sees; US_F16 calls with N n_heads / n_kv_heads <= 32 n_seqs multiply what that rounding leaves, too, so that
+ *   the output's own is all that shows (2.1e-4 of the output's norm; larger US_F16 calls 2.9e-4; US_BF16 1.7e-3, its own, in either kind).
  * All three are enqueue-only on `stream` on the current device. N or n_seqs = 0: nothing is done.
  * Errors: INVALID_ARG, UNSUPPORTED, SCRATCH_TOO_SMALL, CUDA.
  */

@@ -490,7 +490,10 @@ class KVCache:
     def attention(self, q, block_table, lengths, cu_tokens=None, scale=None, causal=True, window=0, out=None, lse=None, stream=None):
         """Attention of q (N, n_heads, head_dim), float16 or bfloat16, over the sequences' cached tokens, their new ones (appended before)
         included. scale: head_dim ** -0.5 unless given. causal: a token sees itself and those before it, else its whole sequence;
-        window > 0: none further back than window - 1. out: like q; lse: float32 (N, n_heads), gets the logarithm of the softmax's sum."""
+        window > 0: none further back than window - 1. out: like q; lse: float32 (N, n_heads), gets the logarithm of the softmax's sum.
+
+        The softmax's weights have 11 bits in the product with V; what is left is multiplied, too, for float16 and up to 32 rows (tokens x
+        query heads) a sequence and cache head."""
         return _ext.kv_attention(self.handle, self.k_codes, q, block_table, lengths, cu_tokens, self.head_dim ** -0.5 if scale is None else scale,
                                  causal, window, out, lse, stream)
 

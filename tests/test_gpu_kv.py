@@ -202,6 +202,19 @@ def closely(cache, table, L, n, q, scale=None, causal=True, window=0, exact_p=Fa
     return o, rel.t()[..., None] * m + absolute.t()[..., None]
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G,new", [(1, 1), (3, 1), (8, 1), (9, 1), (16, 1), (32, 1), (5, 3), (2, 16)])
+def test_float16_of_few_rows_is_off_by_its_own_rounding(b, G, new, D):
+    """Up to 32 rows a cache head: p's rounding does not show. Scores are small, so that their own error does not either."""
+    L = 40
+    cache, table, lengths = make(b, [L], 4, D, 16, G)
+    q = (torch.randn(new, 4 * G, D, device="cuda", generator=gen(3)) * 0.02).half()
+    out = cache.attention(q, table, lengths, None if new == 1 else cu_of([new]))
+    cache.check()
+    ref, bound = closely(cache, table, L, new, q, exact_p=True)
+    check(out, ref, bound)
+
+
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("L,G,Hkv,new,D", [(131072, 1, 1, 1, 128), (131072, 8, 1, 1, 64), (40000, 16, 2, 1, 128), (30000, 5, 2, 3, 128), (20000, 8, 1, 16, 128), (70000, 4, 1, 70, 128)])
 def test_long_contexts_closely(b, dtype, L, G, Hkv, new, D):
@@ -210,7 +223,7 @@ def test_long_contexts_closely(b, dtype, L, G, Hkv, new, D):
     q = torch.randn(new, G * Hkv, D, device="cuda", generator=gen(3)).to(dtype)
     out = cache.attention(q, table, lengths, None if new == 1 else cu_of([new]))
     cache.check()
-    ref, bound = closely(cache, table, L, new, q, exact_p=dtype == torch.float16 and new * G <= 8)
+    ref, bound = closely(cache, table, L, new, q, exact_p=dtype == torch.float16 and new * G <= 32)
     assert bound.square().mean() < ref.square().mean() / 9
     check(out, ref, bound)
 
