@@ -325,8 +325,8 @@ us_status us_mx4_last_error(void);
  *
  * A pool of blocks of block_tokens tokens (16, 32, 64, 128 or 256): codes int8 [n_blocks][n_kv_heads][block_tokens][head_dim]
  * (head_dim 64 or 128), one fp32 step >= 0 for each (block, head), [n_blocks][n_kv_heads]; K and V apart. value = code * step.
- * us_kv_create describes a pool that the caller owns (device memory, codes 16-byte aligned); the handle holds no device memory, and
- * any number of calls on it may be in flight. A pool has fewer than 2^31 (token, head) places.
+ * us_kv_create describes a pool that the caller owns (memory of one device, codes 16-byte aligned); the handle holds no device memory, and
+ * any number of calls on it may be in flight, with the pool's device current (else INVALID_ARG). A pool has fewer than 2^31 (token, head) places.
  *
  * A batch of sequences (us_kv_seqs; all arrays on the device, read by the kernels when they run):
  *   block_table  n_seqs rows (stride table_stride) of table_width block numbers: token t of a sequence is at place t % block_tokens of

@@ -38,6 +38,7 @@ EncodeTiled encode_tiled()
 
 struct us_kv {
     us::KvPool pool{};
+    int device = -1;      // that the pool lies on; -1: not known (no driver, or memory that is not one device's)
     std::mutex lock;      // of the maps: made by the first attention call
     bool mapped = false;
     CUtensorMap k_map, v_map;
@@ -68,6 +69,23 @@ bool maps(us_kv* h)
     std::lock_guard<std::mutex> hold(h->lock);
     if (!h->mapped) h->mapped = encode_map(&h->k_map, h->pool.k, h->pool) && encode_map(&h->v_map, h->pool.v, h->pool);
     return h->mapped;
+}
+
+// The device that an address lies on, or -1.
+int device_of(const void* p)
+{
+    cudaPointerAttributes a = {};
+    if (cudaPointerGetAttributes(&a, p) != cudaSuccess) cudaGetLastError();
+    else if (a.type == cudaMemoryTypeDevice) return a.device;
+    return -1;
+}
+// Whether the current device is the pool's: every call that launches asks.
+us_status on_device(const us_kv* h)
+{
+    if (h->device < 0) return US_OK;
+    int dev = -1;
+    const us_status s = cuda(cudaGetDevice(&dev));
+    return s != US_OK ? s : dev == h->device ? US_OK : US_ERR_INVALID_ARG;
 }
 
 bool seqs_ok(const us_kv* h, const us_kv_seqs* q, int64_t N)
@@ -171,8 +189,12 @@ us_status us_kv_create(void* k_codes, void* v_codes, void* k_steps, void* v_step
     if ((head_dim != 64 && head_dim != 128) || (block_tokens != 16 && block_tokens != 32 && block_tokens != 64 && block_tokens != 128 && block_tokens != 256))
         return US_ERR_UNSUPPORTED;
     if (n_blocks >= (1ll << 31) || n_blocks > ((1ll << 31) - 1) / n_kv_heads / block_tokens) return US_ERR_UNSUPPORTED;
+    const int device = device_of(k_codes);
+    for (const void* p : {(const void*)v_codes, (const void*)k_steps, (const void*)v_steps})
+        if (device_of(p) != device) return US_ERR_INVALID_ARG;
     us_kv* h = new (std::nothrow) us_kv();
     if (!h) return US_ERR_ALLOC;
+    h->device = device;
     h->pool.k = static_cast<int8_t*>(k_codes);
     h->pool.v = static_cast<int8_t*>(v_codes);
     h->pool.k_step = static_cast<float*>(k_steps);
@@ -198,6 +220,8 @@ us_status us_kv_append(us_kv* h, const us_kv_seqs* q, int64_t N, const void* K, 
     if (N == 0 || q->n_seqs == 0) return US_OK;
     if (!strides_ok(K, type, k_token_stride, k_head_stride, N, h->pool.Hkv, h->pool.D) ||
         !strides_ok(V, type, v_token_stride, v_head_stride, N, h->pool.Hkv, h->pool.D)) return US_ERR_INVALID_ARG;
+    us_status s = on_device(h);
+    if (s != US_OK) return s;
     KvAppend a = {};
     a.pool = h->pool;
     a.seqs = seqs(q, N);
@@ -205,7 +229,7 @@ us_status us_kv_append(us_kv* h, const us_kv_seqs* q, int64_t N, const void* K, 
     a.token_stride[0] = k_token_stride; a.token_stride[1] = v_token_stride;
     a.head_stride[0] = k_head_stride; a.head_stride[1] = v_head_stride;
     a.vec = rows_vec(K, type, k_token_stride, k_head_stride) && rows_vec(V, type, v_token_stride, v_head_stride);
-    us_status s = error_word(&a.pool.err);
+    s = error_word(&a.pool.err);
     if (s != US_OK) return s;
     // blocks that get tokens: at most n / T + 2 of a sequence with n new tokens, and n
     const int64_t most = std::min(N, N / h->pool.T + 2 * (int64_t)q->n_seqs);
@@ -227,7 +251,8 @@ us_status us_kv_read(us_kv* h, const us_kv_seqs* q, int64_t tokens, void* K, voi
     if (!seqs_ok(h, &one, one.n_seqs) || !K || !V || !aligned(K, 16) || !aligned(V, 16) || tokens > (int64_t)q->table_width * h->pool.T) return US_ERR_INVALID_ARG;
     KvPool p = h->pool;
     KvSeqs s = seqs(&one, 0);
-    us_status st = error_word(&p.err);
+    us_status st = on_device(h);
+    if (st == US_OK) st = error_word(&p.err);
     if (st != US_OK) return st;
     const dim3 grid((unsigned)((tokens + 15) / 16), (unsigned)((p.Hkv + kReadHeads - 1) / kReadHeads), (unsigned)std::min(s.S, 65535));
     int log2_T = 0;
@@ -254,6 +279,8 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
     if (N == 0 || q->n_seqs == 0) return US_OK;
     if (!strides_ok(Q, type, q_token_stride, q_head_stride, N, n_heads, h->pool.D) || !strides_ok(out, type, o_token_stride, o_head_stride, N, n_heads, h->pool.D) ||
         !aligned(lse, 4)) return US_ERR_INVALID_ARG;
+    us_status s = on_device(h);
+    if (s != US_OK) return s;
     const int64_t G = n_heads / h->pool.Hkv;
     if (N * G >= (1ll << 31) - (1 << 16)) return US_ERR_UNSUPPORTED;
     const AttendPlan pl = attend_plan(h->pool.D, type == US_BF16, N, q->n_seqs, G, h->pool.Hkv, (int64_t)q->table_width * h->pool.T, ops_sms());
@@ -277,7 +304,7 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
         a.o_vec = rows_vec(out, type, o_token_stride, o_head_stride);
         a.splits = pl.splits;
         while ((1 << a.log2_T) < h->pool.T) ++a.log2_T;
-        us_status s = error_word(&a.pool.err);
+        s = error_word(&a.pool.err);
         if (s != US_OK) return s;
         void* args[] = {&a};
         cudaError_t e = ops_kernel_allow(pl.kernel, pl.smem);
@@ -302,7 +329,7 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* 
     a.stages = pl.stages;
     a.ctas = pl.ctas;
     while ((1 << a.log2_T) < h->pool.T) ++a.log2_T;
-    us_status s = error_word(&a.pool.err);
+    s = error_word(&a.pool.err);
     if (s != US_OK) return s;
     cudaError_t e = ops_kernel_allow(pl.kernel, pl.smem);
     void* args[] = {&a};

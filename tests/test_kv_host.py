@@ -82,6 +82,54 @@ def test_attention_refuses(b, h, kw, st):
     assert _attend(b, h, _seqs(b), **kw) == st
 
 
+FAKE = r"""
+#include <cuda_runtime_api.h>
+#include <stdlib.h>
+#include <string.h>
+/* Two devices: an address below 16 MB lies on device 0, one below 32 MB on device 1; FAKE_DEVICE is the current one. */
+cudaError_t cudaGetDevice(int* d) { *d = atoi(getenv("FAKE_DEVICE")); return cudaSuccess; }
+cudaError_t cudaPointerGetAttributes(struct cudaPointerAttributes* a, const void* p)
+{
+    memset(a, 0, sizeof *a);
+    a->type = cudaMemoryTypeDevice;
+    a->device = (int)((size_t)p >> 24);
+    return cudaSuccess;
+}
+"""
+CALLS = """
+import ctypes, os, sys
+from paper_2608_09291_b200 import binding as b
+lib, P0, P1 = b._lib, 1 << 20, (1 << 24) + (1 << 20)
+out = ctypes.c_void_p()
+print([lib.us_kv_create(k, v, s, t, 100, 2, 64, 128, ctypes.byref(out)) for k, v, s, t in ((P1, P0, P1, P1), (P1, P1, P0, P1), (P1, P1, P1, P0), (P1, P1, P1, P1))])
+q, h = b.us_kv_seqs(block_table=P1, table_stride=10, lengths=P1, cu_tokens=None, n_seqs=3, table_width=10), out.value
+for n in (0, 1):
+    os.environ["FAKE_DEVICE"] = str(n)
+    ctypes.CDLL(None).setenv(b"FAKE_DEVICE", str(n).encode(), 1)
+    print([lib.us_kv_append(h, ctypes.byref(q), 3, P1, P1, 0, 256, 128, 256, 128, None),
+           lib.us_kv_read(h, ctypes.byref(q), 5, P1, P1, 2, None),
+           lib.us_kv_attention(h, ctypes.byref(q), 3, P1, 0, 8, 1024, 128, 0.1, 1, 0, P1, 1024, 128, None, P1, 1 << 40, None)])
+"""
+
+
+def test_a_cache_belongs_to_a_device(tmp_path):
+    """With another device current than the one that the pool lies on, the calls that launch refuse; a pool on two devices is none. On a
+    fake of the two runtime calls that say what lies where: on the device the calls go on, and fail for want of a GPU here."""
+    import os
+    import subprocess
+    import sys
+    from pathlib import Path
+    (tmp_path / "fake.c").write_text(FAKE)
+    subprocess.run(["gcc", "-shared", "-fPIC", "-I/usr/local/cuda/include", "fake.c", "-o", "fake.so"], cwd=tmp_path, check=True)
+    env = dict(os.environ, LD_PRELOAD=str(tmp_path / "fake.so"), FAKE_DEVICE="1", CUDA_VISIBLE_DEVICES="")
+    r = subprocess.run([sys.executable, "-c", CALLS], cwd=Path(__file__).resolve().parent.parent, env=env, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
+    made, elsewhere, there = [eval(line) for line in r.stdout.split("\n")[:3]]
+    assert made == [INVALID, INVALID, INVALID, 0]
+    assert elsewhere == [INVALID, INVALID, INVALID]
+    assert all(s not in (0, INVALID) for s in there)
+
+
 def test_read_refuses(b, h):
     q = _seqs(b)
     for tokens, K, V, t in ((641, P, P, 2), (-1, P, P, 2), (5, None, P, 2), (5, P, P + 8, 2), (5, P, P, 3)):
