@@ -2,6 +2,7 @@
 
 #include <cstdlib>
 #include <mutex>
+#include <new>
 #include <set>
 #include <utility>
 
@@ -47,7 +48,11 @@ cudaError_t ops_kernel_allow(const void* kernel, int most)
     if (g_allowed.count({dev, kernel})) return cudaSuccess;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e == cudaSuccess) g_allowed.insert({dev, kernel});
+    if (e != cudaSuccess) return e;
+    try {
+        g_allowed.insert({dev, kernel});
+    } catch (const std::bad_alloc&) {   // (the next call sets the attributes again)
+    }
     return e;
 }
 

@@ -71,6 +71,52 @@ def test_linear_wants_its_scratch(b):
     assert b._lib.us_mx4_linear_scratch(-1, 256, 512) == -1 and b._lib.us_mx4_linear_scratch(4, 0, 512) == -1
 
 
+FAKE = r"""
+#include <cuda_runtime_api.h>
+#include <cstdlib>
+#include <new>
+/* A runtime whose launches do nothing, and a heap that is full when it is told so. */
+extern "C" {
+int full = 0, launches = 0;
+cudaError_t cudaGetDevice(int* d) { *d = 0; return cudaSuccess; }
+cudaError_t cudaGetSymbolAddress(void** p, const void*) { *p = &launches; return cudaSuccess; }
+cudaError_t cudaFuncSetAttribute(const void*, cudaFuncAttribute, int) { return cudaSuccess; }
+cudaError_t cudaLaunchKernelExC(const cudaLaunchConfig_t*, const void*, void**) { ++launches; return cudaSuccess; }
+}
+void* operator new(size_t n)
+{
+    void* p = full ? nullptr : malloc(n);
+    if (!p) throw std::bad_alloc();
+    return p;
+}
+"""
+CALLS = """
+import ctypes
+from paper_2608_09291_b200 import binding as b
+P, me = 1 << 20, ctypes.CDLL(None)
+full, launches = (ctypes.c_int.in_dll(me, n) for n in ("full", "launches"))
+for n in (1, 0):
+    full.value = n
+    status = b._lib.us_mx4_matmul(P, 5, P, 256, 512, P, 0, 256, 0, None)
+    full.value = 0
+    print(status, launches.value)
+"""
+
+
+def test_no_exception_leaves_a_call_that_launches(tmp_path):
+    """Where there is no memory for a note of the host's, a product is launched all the same. On a fake of the runtime calls."""
+    import os
+    import subprocess
+    import sys
+    from pathlib import Path
+    (tmp_path / "fake.cpp").write_text(FAKE)
+    subprocess.run(["g++", "-shared", "-fPIC", "-I/usr/local/cuda/include", "fake.cpp", "-o", "fake.so"], cwd=tmp_path, check=True)
+    env = dict(os.environ, LD_PRELOAD=str(tmp_path / "fake.so"))
+    r = subprocess.run([sys.executable, "-c", CALLS], cwd=Path(__file__).resolve().parent.parent, env=env, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, (r.returncode, r.stderr[-500:])
+    assert r.stdout.split() == ["0", "1", "0", "2"]
+
+
 def test_nothing_to_do(b):
     assert b._lib.us_mx4_quantize(None, 0, 0, 0, 64, None, None) == 0
     assert b._lib.us_mx4_dequantize(None, 0, 64, None, 0, 0, None) == 0
