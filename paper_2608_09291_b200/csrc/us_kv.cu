@@ -9,7 +9,7 @@
 namespace us {
 namespace {
 
-__device__ uint32_t g_kv_err;   // the first failure that a kernel met since the last us_kv_last_error
+__device__ uint32_t g_kv_err;   // the last failure that a kernel met since us_kv_last_error was asked
 
 us_status cuda(cudaError_t e)
 {
@@ -163,6 +163,8 @@ template <int D, int NT>
 AttendPlan attend_shape(bool bf16, int sms) { return bf16 ? attend_shape<D, NT, true>(sms) : attend_shape<D, NT, false>(sms); }
 AttendPlan attend_plan(int D, bool bf16, int64_t N, int64_t S, int64_t G, int64_t Hkv, int64_t longest, int sms)
 {
+    // Rows a cache head has on average decide. 64 sequences of 4096 tokens, 8 cache heads of 128, bf16, this kernel and the other one: 16 rows 154, 341 us, 32
+    // rows 288, 342, 40 rows 414, 343, 128 rows 1082, 349; four sequences of 32768: 32 rows 140, 170, 40 rows 191, 172. (64 of 300: 24 rows 76, 66.)
     if (N * G > 32 * S) {
         if (D == 128) return bf16 ? prompt_shape<128, true>(N, S, G, Hkv, longest, sms) : prompt_shape<128, false>(N, S, G, Hkv, longest, sms);
         return bf16 ? prompt_shape<64, true>(N, S, G, Hkv, longest, sms) : prompt_shape<64, false>(N, S, G, Hkv, longest, sms);

@@ -50,8 +50,8 @@ __device__ __forceinline__ KvSeq kv_seq(const KvSeqs& q, const KvPool& p, int s,
 // ---- append --------------------------------------------------------------------------------------------------------------
 // A team of 32 to 128 threads has a block and head: the largest new magnitude first, then codes, and the older codes once more where the step
 // grew. Blocks have no order among them. Bound by memory where prompts are written (3 of up to 2000 tokens, 32 heads of 128, and contexts of up to
-// 2500 read back: 86 us for both, 57 at memory's rate), by the chain length -> table -> step -> codes where single tokens are (64, and
-// 300 tokens each read back: 37 us, 27 of them the reading's bytes).
+// 2500 read back: 86 us for both, 57 at memory's rate; the writing alone 35, 11 at that rate: blocks of 16 tokens, a team each), by the chain length -> table
+// -> step -> codes where single tokens are (64: 4.8 us; with 300 tokens each read back 37, 27 of them the reading's bytes).
 // code = RNE(x / s) for the exact quotient, x finite or not. The rounded product x * (1 / s) is within 2^-16 of the quotient: its nearest
 // integer is the code unless it lies that close to a border (1 of 25000 values; kv_code_near), where the sign of a fused multiply-add says on which side x
 // is (exact: a rounded sum is never on the other side of 0), or underflow would lose the border, where 64 bits decide.
@@ -305,12 +305,13 @@ __global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int
 //     are that it does not see or that have no weight in it. sum p v is held relative to that one, sum p relative to m; both are fp32.
 //   * Both follow the true maximum only where one is 2^8 behind, so most units need no reduction over lanes and no rescaling.
 //   * All (sequence, row tile, head) items in a row, 128 tokens a unit and kKvStart units for beginning one: every CTA takes the same
-//     number of units, whatever the lengths. (64 sequences of 1 to 8192 tokens, 64/8 heads: 148 us without the units for beginning,
+//     number of units, whatever the lengths. (64 sequences of 1 to 8192 tokens, 64/8 heads, inside a graph: 148 us without the units for beginning,
 //     where the CTAs with the short sequences were last, 120 with 2, 110 with 3, 104 with 4.) An item that is cut leaves its parts in scratch, and a second kernel joins
 //     them in the order of the CTAs.
 // A warp copies (TMA, swizzled so that the fragment loads meet no bank twice); four read, 32 tokens of a unit each (two groups side by
 // side: their chains of products overlap), with sums of their own that are joined at an item's end.
-// Bound by memory: 64 sequences of up to 8192 tokens, 64/8 heads: 100 us, 5.4 TB/s; one of 131072 tokens: 52 us, 5.1 TB/s.
+// Bound by memory: 64 sequences of up to 8192 tokens, 64/8 heads, bf16: 98 us inside a graph, 5.7 TB/s (109 called); one of 131072 tokens, fp16:
+// 55 us, 4.9 TB/s (59 called).
 constexpr int kKvTile = 128;
 constexpr int kKvStart = 4;   // what an item's queries, sums and output cost, in units
 struct KvAttend {
@@ -956,12 +957,12 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
     __syncthreads();
 }
 
-// Joins the parts of the items that the kernel before has cut. Which those are depends on the lengths alone: it is found out while
-// that kernel runs (a block fits beside its CTAs: four warps of up to 102 registers). An item of up to kJoinFew parts is joined by the
-// block of the CTA that begins it, a warp a row. The rows of one of more parts are shared by the blocks of all CTAs that have one, and a
-// row's parts by the warps: one trip to memory for up to eight a warp. (One sequence of 131072 tokens, 8 cache heads, 37 parts each:
-// 62 us with the first form alone, 53 with the second; 64 of 4096, 2 or 3 parts each: 95 and 102.) Parts are added in
-// the same order every time.
+// Joins the parts of the items that the kernel before has cut. Which those are depends on the lengths alone: a block finds it out before it
+// waits for that kernel, beside its last CTAs (beside two of them, with the 168 registers a thread of D = 128, there is no room). An item of
+// up to kJoinFew parts is joined by the block of the CTA that begins it, a warp a row. The rows of one of more parts are shared by the
+// blocks of all CTAs that have one, and a row's parts by the warps: one trip to memory for up to eight a warp. (One sequence of 131072
+// tokens, 8 cache heads, 37 parts each, inside a graph: 62 us with the first form alone, 53 with the second; 64 of 4096, 2 or 3 parts
+// each: 95 and 102.) Parts are added in the same order every time.
 // Every block waits for the kernel before, those without a part, too: what follows in the stream waits for this grid alone, so this
 // grid may not end before the sums and outputs of the other one are there.
 constexpr int kJoinWarps = 4, kJoinFew = 4;

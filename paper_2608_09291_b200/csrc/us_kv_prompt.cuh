@@ -14,9 +14,10 @@
 // V's codes are rounded to half a 127th of their largest.
 // m follows the true maximum only where it is 2^8 behind; p carries 2^7, see us_kv.cuh. The scores' conversions, the
 // 16384 exponentials (16 a cycle) and the two products (1024 cycles) of a tile and unit are each about 1000 cycles, and overlap.
-// Three prompts of up to 2000 tokens, to contexts of up to 4500 (64/8 heads of 128, bf16): 720 us; one of 8192 tokens: 1275 us, 863 TFLOP/s. What
+// Three prompts of up to 2000 tokens, to contexts of up to 4500 (64/8 heads of 128, bf16): 723 us, 696 inside a graph; one of 8192 tokens: 1250 to
+// 1281 us, 858 to 880 TFLOP/s. What
 // bounds it is the softmax threads' own chain from scores to P. Slower: 16 softmax warps (914 us), units of 64 tokens (816), exponentials
-// partly as polynomials (748 to 795), the maximum of the unit before in place of the unit's own (spills).
+// partly as polynomials (748 to 795). The softmax threads spill about 100 bytes.
 #pragma once
 #include "us_kv.cuh"
 

@@ -5,7 +5,7 @@
 namespace us {
 namespace {
 
-__device__ uint32_t g_mx4_err;   // first bounded wait that ran out since the last us_mx4_last_error
+__device__ uint32_t g_mx4_err;   // whether a bounded wait has run out since us_mx4_last_error was asked
 
 struct Plan {
     const void* kernel;

@@ -343,7 +343,8 @@ __global__ void __launch_bounds__(256) us_mx4_dequantize_kernel(const uint8_t* m
     }
 }
 
-// Row-major codes (two a byte) and scale bytes <-> tiles: a warp a row of a tile, byte by byte (loading, not computing).
+// Row-major codes (two a byte) and scale bytes <-> tiles: a warp a row of a tile, byte by byte. What a checkpoint's loading does once: 28672 x 8192,
+// 250 MB there and back: 220 us, unpacked 196, where memory's rate would give 38.
 template <bool PACK>
 __global__ void __launch_bounds__(256) us_mx4_repack_kernel(uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, int64_t rows, int64_t K, uint8_t* mx)
 {
@@ -731,7 +732,8 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
 // ---- the product of many tokens -------------------------------------------------------------------------------------------
 // Pairs of blocks (a cluster of two SMs, cta_group::2) walk over tiles of 256 weight rows x 256 tokens, all tokens of the rows in turn: X
 // stays in L2, W is read about once. Each block has 128 of the rows, and loads half of the tokens for both: 35 KB a block and 256
-// columns, 52 KB for a block that works alone (4096 x 28672 x 8192, the tokens' quantisation included: 410 us = 4.7 PFLOP/s, 445 alone;
+// columns, 52 KB for a block that works alone (4096 x 28672 x 8192, the tokens' quantisation included, on a GPU that was idle before: 384 to 410 us =
+// 5.0 to 4.7 PFLOP/s, 445 alone; call after call 453 under the power cap, below;
 // K = 28672, M = 8192: 445 and 478).
 // Copies run ahead over the tiles' ends, and the sums of a tile leave tensor memory for shared memory, rounded, before the next
 // tile's products begin (half of the tokens at a time); they are stored while those run. What bounds it is the way from L2 to the SMs
