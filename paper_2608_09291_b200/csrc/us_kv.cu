@@ -191,9 +191,12 @@ us_status us_kv_create(void* k_codes, void* v_codes, void* k_steps, void* v_step
     if ((head_dim != 64 && head_dim != 128) || (block_tokens != 16 && block_tokens != 32 && block_tokens != 64 && block_tokens != 128 && block_tokens != 256))
         return US_ERR_UNSUPPORTED;
     if (n_blocks >= (1ll << 31) || n_blocks > ((1ll << 31) - 1) / n_kv_heads / block_tokens) return US_ERR_UNSUPPORTED;
-    const int device = device_of(k_codes);
-    for (const void* p : {(const void*)v_codes, (const void*)k_steps, (const void*)v_steps})
-        if (device_of(p) != device) return US_ERR_INVALID_ARG;
+    int device = -1;
+    for (const void* p : {(const void*)k_codes, (const void*)v_codes, (const void*)k_steps, (const void*)v_steps}) {
+        const int d = device_of(p);
+        if (d >= 0 && device >= 0 && d != device) return US_ERR_INVALID_ARG;
+        if (d >= 0) device = d;
+    }
     us_kv* h = new (std::nothrow) us_kv();
     if (!h) return US_ERR_ALLOC;
     h->device = device;

@@ -86,12 +86,12 @@ FAKE = r"""
 #include <cuda_runtime_api.h>
 #include <stdlib.h>
 #include <string.h>
-/* Two devices: an address below 16 MB lies on device 0, one below 32 MB on device 1; FAKE_DEVICE is the current one. */
+/* Two devices: an address below 16 MB lies on device 0, one below 32 MB on device 1, others are managed; FAKE_DEVICE is the current one. */
 cudaError_t cudaGetDevice(int* d) { *d = atoi(getenv("FAKE_DEVICE")); return cudaSuccess; }
 cudaError_t cudaPointerGetAttributes(struct cudaPointerAttributes* a, const void* p)
 {
     memset(a, 0, sizeof *a);
-    a->type = cudaMemoryTypeDevice;
+    a->type = (size_t)p >> 25 ? cudaMemoryTypeManaged : cudaMemoryTypeDevice;
     a->device = (int)((size_t)p >> 24);
     return cudaSuccess;
 }
@@ -99,9 +99,10 @@ cudaError_t cudaPointerGetAttributes(struct cudaPointerAttributes* a, const void
 CALLS = """
 import ctypes, os, sys
 from paper_2608_09291_b200 import binding as b
-lib, P0, P1 = b._lib, 1 << 20, (1 << 24) + (1 << 20)
+lib, P0, P1, P2 = b._lib, 1 << 20, (1 << 24) + (1 << 20), 1 << 26
 out = ctypes.c_void_p()
-print([lib.us_kv_create(k, v, s, t, 100, 2, 64, 128, ctypes.byref(out)) for k, v, s, t in ((P1, P0, P1, P1), (P1, P1, P0, P1), (P1, P1, P1, P0), (P1, P1, P1, P1))])
+print([lib.us_kv_create(k, v, s, t, 100, 2, 64, 128, ctypes.byref(out)) for k, v, s, t in
+       ((P1, P0, P1, P1), (P1, P1, P0, P1), (P2, P1, P1, P0), (P2, P2, P2, P2), (P2, P2, P1, P1))])
 q, h = b.us_kv_seqs(block_table=P1, table_stride=10, lengths=P1, cu_tokens=None, n_seqs=3, table_width=10), out.value
 for n in (0, 1):
     os.environ["FAKE_DEVICE"] = str(n)
@@ -125,7 +126,7 @@ def test_a_cache_belongs_to_a_device(tmp_path):
     r = subprocess.run([sys.executable, "-c", CALLS], cwd=Path(__file__).resolve().parent.parent, env=env, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr
     made, elsewhere, there = [eval(line) for line in r.stdout.split("\n")[:3]]
-    assert made == [INVALID, INVALID, INVALID, 0]
+    assert made == [INVALID, INVALID, INVALID, 0, 0]
     assert elsewhere == [INVALID, INVALID, INVALID]
     assert all(s not in (0, INVALID) for s in there)
 
