@@ -30,8 +30,10 @@ typedef enum us_status {
     US_ERR_DEVICE_TIMEOUT = 7,/* a bounded wait inside a kernel gave up (no hang, no trap)  */
     US_ERR_SCRATCH_TOO_SMALL = 8,/* us_spmm_static_scratch: the problem needs more scratch than
                                     the library's fixed device array holds; or than was given */
-    US_ERR_DEVICE_INDEX = 9   /* a block number, length or token count on the device is out of
+    US_ERR_DEVICE_INDEX = 9,  /* a block number, length or token count on the device is out of
                                  range (us_kv_last_error)                                    */
+    US_ERR_OUT_OF_BLOCKS = 10 /* us_kv_extend found fewer free blocks than its sequences need
+                                 (us_kv_last_error)                                          */
 } us_status;
 
 /*
@@ -380,6 +382,66 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* seqs, int64_t N, const voi
                           int64_t o_token_stride, int64_t o_head_stride, float* lse, void* scratch, int64_t scratch_bytes, void* stream);
 us_status us_kv_last_error(void);
 us_status us_kv_destroy(us_kv* h);
+
+/*
+ * Blocks of the cache that sequences share. refs (device, n_blocks int32, 16-byte aligned, the caller's; 0 at first): how many entries of tables hold a
+ * block; 0: it is free. The calls keep that up as tables change; everything is decided on the device, from the call's data alone, and in
+ * order: the same data give the same blocks. Calls that use one refs follow one another on the device. Of a table, the entries of a sequence's ceil(length /
+ * block_tokens) blocks count. Errors on the device are reported by us_kv_last_error, as above.
+ *
+ * us_kv_fork: row i of table (n_children rows of seqs->table_width entries, table_stride apart) and lengths[i] become those of sequence parents[i] (-1: an
+ *   empty one); 0 behind its blocks. The children's entries are counted and, with keep = 0, the parents' no more (their table is not to be used from then on). The
+ *   new table and lengths do not overlap the old ones. A parent out of range gives an empty sequence.
+ * us_kv_release: the sequences' entries are counted no more. Table and lengths are left as they are.
+ * us_kv_extend: room for tokens[s] more (device int32, or NULL: tokens_each for all) tokens of each sequence: free blocks, the lowest first, sequence by
+ *   sequence, go to the table, and lengths[s] grows. Before that, a last block that is partly filled and that other entries hold, too, is replaced by a copy (of the
+ *   tokens held and the steps; the first free block of the sequence's share): new tokens may be appended. Where the sequences of the call are the only ones that hold it, the first of
+ *   them keeps it. If the free blocks do not suffice (US_ERR_OUT_OF_BLOCKS), the first sequence that does not fit and all behind it that need blocks stay as they are; so does a
+ *   sequence with an entry or length that does not fit. scratch: us_kv_extend_scratch bytes, 16-byte aligned, for one call at a time; need not be cleared.
+ * us_kv_compact: the blocks in use become the pool's first `used` (device int32) ones: those behind move to the free places in front, both in order. map[b]
+ *   (device, n_blocks int32) is where block b's tokens are now (b itself where it did not move): us_kv_remap takes every table there. scratch: us_kv_compact_scratch.
+ * us_kv_copy_blocks: block src[i] (all its tokens and steps) to block dst[i], i < n; dst[i] = -1: nothing. No block is twice in dst, or in dst and src.
+ * All are enqueue-only on `stream`. Errors: INVALID_ARG, SCRATCH_TOO_SMALL, CUDA.
+ */
+us_status us_kv_fork(us_kv* h, int32_t* refs, const us_kv_seqs* seqs, const int32_t* parents, int32_t n_children, int32_t* table,
+                     int64_t table_stride, int32_t* lengths, int32_t keep, void* stream);
+us_status us_kv_release(us_kv* h, int32_t* refs, const us_kv_seqs* seqs, void* stream);
+int64_t us_kv_extend_scratch(const us_kv* h, int32_t n_seqs);
+us_status us_kv_extend(us_kv* h, int32_t* refs, int32_t* table, int64_t table_stride, int32_t table_width, int32_t* lengths, int32_t n_seqs,
+                       const int32_t* tokens, int32_t tokens_each, void* scratch, int64_t scratch_bytes, void* stream);
+int64_t us_kv_compact_scratch(const us_kv* h);
+us_status us_kv_compact(us_kv* h, int32_t* refs, int32_t* map, int32_t* used, void* scratch, int64_t scratch_bytes, void* stream);
+us_status us_kv_remap(us_kv* h, const int32_t* map, int32_t* table, int64_t table_stride, int32_t table_width, const int32_t* lengths, int32_t n_seqs,
+                      void* stream);
+us_status us_kv_copy_blocks(us_kv* h, const int32_t* src, const int32_t* dst, int64_t n, void* stream);
+
+/*
+ * Norms of query and key heads and the rotation of their positions, in one pass (no counterpart in the paper).
+ *
+ * For each token n and head x (head_dim values, even, at most 256): y = x / sqrt(mean x^2 + eps) * weight where the call has weights, else
+ * y = x; then of the first rotary_dim values the pairs (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if `interleaved`, i < rotary_dim / 2, are turned:
+ *     y_a' = y_a cos t - y_b sin t,  y_b' = y_b cos t + y_a sin t,  t = positions[axis[i]][n] * frequency_i
+ * computed in fp32 and rounded once. turns[i] (device) is frequency_i / (2 pi) turns in units of 2^-64, modulo 1, so that t is exact for every
+ * position. axis (device; may be NULL with axes = 1): the axis of each pair, below `axes`; a larger one reads outside the positions. turns and axis have
+ * to be complete before the stream's latest work was launched, and stay as they are.
+ * positions: axes rows of N int32 values, axis_stride apart. q, k: rows (token, head) of `type`, strides in elements; k may be NULL; out may be x
+ * itself, otherwise they do not overlap. weight: head_dim values of weight_type, or NULL. Errors: INVALID_ARG, CUDA.
+ */
+typedef struct us_rotary {
+    const uint64_t* turns;
+    const uint8_t* axis;
+    int32_t rotary_dim, axes, interleaved;
+} us_rotary;
+typedef struct us_heads {
+    const void* x;
+    int64_t token_stride, head_stride;
+    void* out;
+    int64_t out_token_stride, out_head_stride;
+    const void* weight;
+    int32_t weight_type, heads;
+} us_heads;
+us_status us_qk_norm_rope(const us_rotary* rotary, const int32_t* positions, int64_t axis_stride, int64_t N, int32_t head_dim, int32_t type,
+                          const us_heads* q, const us_heads* k, float eps, void* stream);
 
 const char* us_status_string(us_status s);
 

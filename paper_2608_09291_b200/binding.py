@@ -32,6 +32,8 @@ EXPORTS = ["us_encode", "us_get_stats", "us_decode", "us_get_row_order", "us_spm
            "us_mx4_bytes", "us_mx4_quantize", "us_mx4_dequantize", "us_mx4_pack", "us_mx4_unpack", "us_mx4_matmul",
            "us_mx4_linear_scratch", "us_mx4_linear", "us_mx4_last_error",
            "us_kv_create", "us_kv_append", "us_kv_read", "us_kv_attention_scratch", "us_kv_attention", "us_kv_last_error", "us_kv_destroy",
+           "us_kv_fork", "us_kv_release", "us_kv_extend_scratch", "us_kv_extend", "us_kv_compact_scratch", "us_kv_compact", "us_kv_remap", "us_kv_copy_blocks",
+           "us_qk_norm_rope",
            "us_status_string"]
 
 
@@ -96,6 +98,28 @@ _lib.us_kv_attention_scratch.restype = _i64
 _lib.us_kv_attention.argtypes = [_vp, _seqs, _i64, _vp, _i32, _i32, _i64, _i64, ctypes.c_float, _i32, _i32, _vp, _i64, _i64, _vp, _vp, _i64, _vp]
 _lib.us_kv_last_error.argtypes = []
 _lib.us_kv_destroy.argtypes = [_vp]
+_lib.us_kv_fork.argtypes = [_vp, _vp, _seqs, _vp, _i32, _vp, _i64, _vp, _i32, _vp]
+_lib.us_kv_release.argtypes = [_vp, _vp, _seqs, _vp]
+_lib.us_kv_extend_scratch.argtypes = [_vp, _i32]
+_lib.us_kv_extend_scratch.restype = _i64
+_lib.us_kv_extend.argtypes = [_vp, _vp, _vp, _i64, _i32, _vp, _i32, _vp, _i32, _vp, _i64, _vp]
+_lib.us_kv_compact_scratch.argtypes = [_vp]
+_lib.us_kv_compact_scratch.restype = _i64
+_lib.us_kv_compact.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _vp]
+_lib.us_kv_remap.argtypes = [_vp, _vp, _vp, _i64, _i32, _vp, _i32, _vp]
+_lib.us_kv_copy_blocks.argtypes = [_vp, _vp, _vp, _i64, _vp]
+
+
+class us_rotary(ctypes.Structure):
+    _fields_ = [("turns", _vp), ("axis", _vp), ("rotary_dim", _i32), ("axes", _i32), ("interleaved", _i32)]
+
+
+class us_heads(ctypes.Structure):
+    _fields_ = [("x", _vp), ("token_stride", _i64), ("head_stride", _i64), ("out", _vp), ("out_token_stride", _i64), ("out_head_stride", _i64),
+                ("weight", _vp), ("weight_type", _i32), ("heads", _i32)]
+
+
+_lib.us_qk_norm_rope.argtypes = [ctypes.POINTER(us_rotary), _vp, _i64, _i64, _i32, _i32, ctypes.POINTER(us_heads), ctypes.POINTER(us_heads), ctypes.c_float, _vp]
 _lib.us_status_string.argtypes = [ctypes.c_int]
 _lib.us_status_string.restype = ctypes.c_char_p
 
@@ -434,6 +458,54 @@ def mx4_check():
     _check(_lib.us_mx4_last_error(), "us_mx4_last_error")
 
 
+# ---- norms and rotation of heads ----
+
+class Rotary:
+    """How positions turn the heads of queries and keys: pair i of the first `rotary_dim` values (all `head_dim` unless given) by position * base ** (-2 i /
+    rotary_dim), or by `frequencies` (radians a place, one for each pair). Pairs are (i, i + rotary_dim / 2), or neighbours (2 i, 2 i + 1) if `interleaved`.
+
+    Positions with several axes (time, height, width): `sections`, how many pairs each axis turns, in order (a list of rotary_dim / 2 in all), or
+    `pair_axis`, the axis of each pair. The table lies on the device, complete and constant (the constructor waits for it)."""
+
+    def __init__(self, head_dim: int, base: float = 10000.0, rotary_dim: int | None = None, interleaved: bool = False, sections=None, pair_axis=None,
+                 frequencies=None, device="cuda"):
+        import torch
+        rotary_dim = head_dim if rotary_dim is None else int(rotary_dim)
+        if not 2 <= head_dim <= 256 or head_dim % 2 or not 2 <= rotary_dim <= head_dim or rotary_dim % 2:
+            raise ValueError("head_dim must be even and at most 256, rotary_dim even and at most head_dim")
+        pairs = rotary_dim // 2
+        f = [float(x) for x in frequencies] if frequencies is not None else [float(base) ** (-2.0 * i / rotary_dim) for i in range(pairs)]
+        if len(f) != pairs or not all(np.isfinite(f)):
+            raise ValueError(f"{pairs} finite frequencies are needed")
+        if sections is not None and pair_axis is not None:
+            raise ValueError("sections or pair_axis, not both")
+        if sections is not None:
+            if any(int(n) < 0 for n in sections):
+                raise ValueError("sections are numbers of pairs")
+            pair_axis = [a for a, n in enumerate(sections) for _ in range(int(n))]
+        axes = 1 if pair_axis is None else len(sections) if sections is not None else max(pair_axis, default=-1) + 1
+        if pair_axis is not None and (len(pair_axis) != pairs or not 1 <= axes <= 255 or not all(0 <= int(a) < axes for a in pair_axis)):
+            raise ValueError(f"an axis for each of the {pairs} pairs is needed, 255 axes at most")
+        self.head_dim, self.rotary_dim, self.interleaved, self.axes = int(head_dim), rotary_dim, bool(interleaved), int(axes)
+        # turns a place, in units of 2^-64: the quotient's 53 bits, of which whole turns are left out
+        turns = [int(np.ldexp(abs(x) / (2 * np.pi) % 1.0, 64)) * (1 if x >= 0 else -1) % (1 << 64) for x in f]
+        self.turns = torch.from_numpy(np.array(turns, dtype=np.uint64).view(np.int64)).to(device)
+        self.pair_axis = torch.tensor([int(a) for a in pair_axis], dtype=torch.uint8).to(device) if self.axes > 1 else None
+        if self.turns.is_cuda:
+            torch.cuda.synchronize(self.turns.device)
+
+
+def qk_norm_rope(q, k, positions, rotary: Rotary, q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None, k_out=None, stream=None):
+    """(q, k) with every head normed (x / sqrt(mean x^2 + eps) * weight; a part without a weight is not) and turned to its position, in one pass. q (N, n_heads,
+    head_dim), k (N, n_kv_heads, head_dim) or None: float16, bfloat16 or float32, any token and head strides: columns of a stacked projection's output
+    need no copy. positions: int32 (N,), or (axes, N) for a rotary of several axes; any value. Weights: (head_dim,) of any of the types. q_out and k_out
+    may be q and k themselves."""
+    if q.dim() != 3 or q.size(2) != rotary.head_dim:
+        raise ValueError("q must be a (N, heads, head_dim) tensor, head_dim as the rotary's")
+    return (_ext or _native()).qk_norm_rope(q, k, positions, rotary.turns, rotary.pair_axis, rotary.axes, rotary.rotary_dim, rotary.interleaved, q_weight, k_weight,
+                                            eps, q_out, k_out, stream)
+
+
 # ---- the cache of keys and values in 8 bits ----
 
 def us_kv_create(k_codes_ptr: int, v_codes_ptr: int, k_steps_ptr: int, v_steps_ptr: int, n_blocks: int, n_kv_heads: int, block_tokens: int,
@@ -497,6 +569,10 @@ class KVCache:
         return _ext.kv_attention(self.handle, self.k_codes, q, block_table, lengths, cu_tokens, self.head_dim ** -0.5 if scale is None else scale,
                                  causal, window, out, lse, stream)
 
+    def copy_blocks(self, src, dst, stream=None):
+        """Copies block src[i], its codes and steps, to block dst[i] (int32 tensors; dst[i] = -1: nothing). No block is twice in dst, or in dst and src."""
+        _ext.kv_copy_blocks(self.handle, self.k_codes, src, dst, stream)
+
     def check(self):
         """Waits for the device and raises if a call on it met a block number, length or token count out of range."""
         import torch
@@ -513,3 +589,42 @@ class KVCache:
             self.close()
         except Exception:
             pass
+
+
+class KVPages:
+    """Which blocks of a cache are in use: `refs`, int32 (n_blocks,) on the cache's device, how many table entries hold each. Sequences may share blocks; a
+    block that nobody holds is free. Calls that need free blocks take the lowest ones, sequence by sequence. Nothing waits for the host, and every call can
+    be captured into a graph; calls on one KVPages follow one another on the device.
+
+    A batch starts with a table of zeros and lengths of 0; `extend` makes room for new tokens, `KVCache.append` then writes them."""
+
+    def __init__(self, cache: KVCache, refs=None):
+        import torch
+        if refs is None:
+            refs = torch.zeros(cache.n_blocks, dtype=torch.int32, device=cache.k_codes.device)
+        elif refs.dtype != torch.int32 or tuple(refs.shape) != (cache.n_blocks,) or not refs.is_contiguous() or refs.device != cache.k_codes.device or refs.data_ptr() % 16:
+            raise ValueError("refs must be a contiguous int32 (n_blocks,) tensor on the cache's device, 16-byte aligned")
+        self.cache, self.refs = cache, refs
+
+    def extend(self, block_table, lengths, tokens=1, stream=None):
+        """Room for `tokens` (a number, or int32 (S,)) more tokens of each sequence: block_table and lengths are written. A last block that would be written into
+        and that others hold, too, is replaced by a copy. Sequences for which the pool has no blocks left stay as they are (see `check`)."""
+        _ext.kv_extend(self.cache.handle, self.cache.k_codes, self.refs, block_table, lengths, tokens, stream)
+
+    def fork(self, block_table, lengths, parents, keep=False, stream=None):
+        """(block_table, lengths) of a new batch: row i continues sequence parents[i] (int32; -1: an empty one) and shares its blocks. The old batch is given up
+        unless `keep`. Beams are reordered, samples of a prompt begun, and finished sequences dropped this way."""
+        return _ext.kv_fork(self.cache.handle, self.cache.k_codes, self.refs, block_table, lengths, parents, keep, stream)
+
+    def release(self, block_table, lengths, stream=None):
+        """Gives the sequences' blocks up; those that nobody else holds are free from then on. The tensors are left as they are."""
+        _ext.kv_release(self.cache.handle, self.cache.k_codes, self.refs, block_table, lengths, stream)
+
+    def compact(self, tables, stream=None):
+        """Moves the blocks in use to the front of the pool. tables: (block_table, lengths) pairs, every table that is in use: their entries are rewritten. Returns how
+        many blocks are in use, an int32 scalar on the device."""
+        return _ext.kv_compact(self.cache.handle, self.cache.k_codes, self.refs, tuple((t, n) for t, n in tables), stream)
+
+    def check(self):
+        """Waits for the device and raises if the pool had too few free blocks, or a call met an entry, length or count out of range."""
+        self.cache.check()

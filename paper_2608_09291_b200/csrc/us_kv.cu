@@ -1,9 +1,8 @@
 // The 8-bit cache's entry points: checks, launch plans.
+#include "us_kv_host.h"
 #include "us_kv_prompt.cuh"
-#include "us_ops.h"
 
 #include <cmath>
-#include <mutex>
 #include <new>
 
 namespace us {
@@ -11,14 +10,13 @@ namespace {
 
 __device__ uint32_t g_kv_err;   // the last failure that a kernel met since us_kv_last_error was asked
 
-us_status cuda(cudaError_t e)
-{
-    if (e == cudaSuccess) return US_OK;
-    cudaGetLastError();
-    return US_ERR_CUDA;
-}
-bool aligned(const void* p, int64_t b) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)b == 0; }
+us_status cuda(cudaError_t e) { return kv_cuda(e); }
+bool aligned(const void* p, int64_t b) { return kv_aligned(p, b); }
 int64_t size_of(int32_t t) { return t == US_F32 ? 4 : 2; }
+us_status on_device(const us_kv* h) { return kv_on_device(h); }
+bool seqs_ok(const us_kv* h, const us_kv_seqs* q, int64_t N) { return kv_seqs_ok(h, q, N); }
+KvSeqs seqs(const us_kv_seqs* q, int64_t N) { return kv_seqs(q, N); }
+us_status error_word(uint32_t** err) { return kv_error_word(err); }
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -34,24 +32,14 @@ EncodeTiled encode_tiled()
 }
 
 }  // namespace
-}  // namespace us
 
-struct us_kv {
-    us::KvPool pool{};
-    int device = -1;      // that the pool lies on; -1: not known (no driver, or memory that is not one device's)
-    std::mutex lock;      // of the maps: made by the first attention call
-    bool mapped = false;
-    CUtensorMap k_map, v_map;
-};
-
-namespace us {
-namespace {
-
-us_status error_word(uint32_t** err)
+us_status kv_error_word(uint32_t** err)
 {
     static void* kept[kMaxDevices];
-    return cuda(ops_symbol(kept, &g_kv_err, reinterpret_cast<void**>(err)));
+    return kv_cuda(ops_symbol(kept, &g_kv_err, reinterpret_cast<void**>(err)));
 }
+
+namespace {
 
 // The codes as rows of D bytes; a copy brings a block's tokens, 64 at most, swizzled over a row's 128 (64) bytes.
 bool encode_map(CUtensorMap* map, void* base, const KvPool& p)
@@ -78,34 +66,6 @@ int device_of(const void* p)
     if (cudaPointerGetAttributes(&a, p) != cudaSuccess) cudaGetLastError();
     else if (a.type == cudaMemoryTypeDevice) return a.device;
     return -1;
-}
-// Whether the current device is the pool's: every call that launches asks.
-us_status on_device(const us_kv* h)
-{
-    if (h->device < 0) return US_OK;
-    int dev = -1;
-    const us_status s = cuda(cudaGetDevice(&dev));
-    return s != US_OK ? s : dev == h->device ? US_OK : US_ERR_INVALID_ARG;
-}
-
-bool seqs_ok(const us_kv* h, const us_kv_seqs* q, int64_t N)
-{
-    if (!h || !q || N < 0 || N >= (1ll << 31) || q->n_seqs < 0 || (!q->cu_tokens && N != q->n_seqs)) return false;
-    if (q->n_seqs == 0 || N == 0) return true;
-    return q->block_table && q->lengths && q->table_width >= 1 && (int64_t)q->table_width * h->pool.T < (1ll << 31) - (1 << 16) &&
-           (q->n_seqs == 1 || q->table_stride >= q->table_width) && aligned(q->block_table, 4) && aligned(q->lengths, 4) && aligned(q->cu_tokens, 4);
-}
-KvSeqs seqs(const us_kv_seqs* q, int64_t N)
-{
-    KvSeqs r = {};
-    r.table = q->block_table;
-    r.table_stride = q->table_stride;
-    r.lengths = q->lengths;
-    r.cu = q->cu_tokens;
-    r.S = q->n_seqs;
-    r.width = q->table_width;
-    r.N = N;
-    return r;
 }
 // Rows (token, head, D): every stride holds a row, and the 16-byte path's condition.
 bool strides_ok(const void* x, int32_t type, int64_t token, int64_t head, int64_t N, int64_t heads, int32_t D)
@@ -352,5 +312,5 @@ us_status us_kv_last_error(void)
     if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&flag, g_kv_err, 4);
     if (e == cudaSuccess && flag) e = cudaMemcpyToSymbol(g_kv_err, &zero, 4);
     if (e != cudaSuccess) return cuda(e);
-    return flag == 0 ? US_OK : flag == kErrIndex ? US_ERR_DEVICE_INDEX : US_ERR_DEVICE_TIMEOUT;
+    return flag == 0 ? US_OK : flag == kErrIndex ? US_ERR_DEVICE_INDEX : flag == kErrFull ? US_ERR_OUT_OF_BLOCKS : US_ERR_DEVICE_TIMEOUT;
 }

@@ -55,7 +55,7 @@ __device__ __forceinline__ KvSeq kv_seq(const KvSeqs& q, const KvPool& p, int s,
 // code = RNE(x / s) for the exact quotient, x finite or not. The rounded product x * (1 / s) is within 2^-16 of the quotient: its nearest
 // integer is the code unless it lies that close to a border (1 of 25000 values; kv_code_near), where the sign of a fused multiply-add says on which side x
 // is (exact: a rounded sum is never on the other side of 0), or underflow would lose the border, where 64 bits decide.
-__device__ __noinline__ int kv_code_near(float x, float s, float inv)
+static __device__ __noinline__ int kv_code_near(float x, float s, float inv)
 {
     if (s < 1e-30f) {
         const double q = s > 0.f ? rint((double)x / (double)s) : 0.0;

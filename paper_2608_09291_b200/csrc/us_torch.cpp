@@ -12,6 +12,7 @@
 #include <torch/csrc/Dtype.h>
 
 #include <optional>
+#include <vector>
 
 #include "../../include/unionsparse.h"
 
@@ -554,6 +555,260 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- blocks of the cache ----
+
+// The counts of a pool's blocks.
+int32_t* take_refs(PyObject* o, const at::Tensor& pool)
+{
+    const at::Tensor* r = tensor(o, "refs");
+    if (!r) return nullptr;
+    if (r->dim() != 1 || !is_ints(*r, pool) || r->size(0) != pool.size(0) || !r->is_contiguous()) {
+        PyErr_SetString(PyExc_ValueError, "refs must be a contiguous int32 tensor with an entry for each block, on the cache's device");
+        return nullptr;
+    }
+    return static_cast<int32_t*>(r->data_ptr());
+}
+bool is_int_row(const at::Tensor& t, int64_t n, const at::Tensor& on) { return t.dim() == 1 && is_ints(t, on) && t.size(0) == n && t.is_contiguous(); }
+
+// kv_copy_blocks(handle, pool, src, dst, stream)
+PyObject* kv_copy_blocks(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "kv_copy_blocks takes 5 arguments");
+    HANDLE_TH_ERRORS
+    void* h = a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor *pool = tensor(a[1], "pool"), *src = pool ? tensor(a[2], "src") : nullptr, *dst = src ? tensor(a[3], "dst") : nullptr;
+    if (!dst) return nullptr;
+    if (!h) return fail(US_ERR_INVALID_ARG, "us_kv_copy_blocks");
+    Place at_;
+    if (!at_.enter(a[4], *pool)) return nullptr;
+    if (src->dim() != 1 || !is_int_row(*src, src->size(0), *pool) || !is_int_row(*dst, src->size(0), *pool))
+        return bad("src and dst must be contiguous int32 tensors of one length on the cache's device");
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_kv_copy_blocks(static_cast<us_kv*>(h), static_cast<const int32_t*>(src->data_ptr()), static_cast<const int32_t*>(dst->data_ptr()), src->size(0), at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_kv_copy_blocks");
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_fork(handle, pool, refs, table, lengths, parents, keep, stream) -> (table, lengths)
+PyObject* kv_fork(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "kv_fork takes 8 arguments");
+    HANDLE_TH_ERRORS
+    void* h = a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]);
+    const int keep = PyObject_IsTrue(a[6]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor *pool = tensor(a[1], "pool"), *parents = pool ? tensor(a[5], "parents") : nullptr;
+    if (!parents) return nullptr;
+    if (!h) return fail(US_ERR_INVALID_ARG, "us_kv_fork");
+    Place at_;
+    if (!at_.enter(a[7], *pool)) return nullptr;
+    int32_t* refs = take_refs(a[2], *pool);
+    us_kv_seqs q;
+    if (!refs || !take_seqs(a[3], a[4], Py_None, -1, *pool, &q)) return nullptr;
+    if (parents->dim() != 1 || !is_int_row(*parents, parents->size(0), *pool) || parents->size(0) >= (1ll << 31))
+        return bad("parents must be a contiguous int32 tensor on the cache's device");
+    const int64_t C = parents->size(0);
+    at::Tensor table = new_output(*pool, C, q.table_width, at::kInt), lengths = at::detail::empty_cuda({C}, at::kInt, pool->device(), std::nullopt);
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_kv_fork(static_cast<us_kv*>(h), refs, &q, static_cast<const int32_t*>(parents->data_ptr()), (int32_t)C, static_cast<int32_t*>(table.data_ptr()), q.table_width,
+                   static_cast<int32_t*>(lengths.data_ptr()), keep, at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_kv_fork");
+    PyObject *t = THPVariable_Wrap(std::move(table)), *l = THPVariable_Wrap(std::move(lengths));
+    return Py_BuildValue("NN", t, l);
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_release(handle, pool, refs, table, lengths, stream)
+PyObject* kv_release(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 6) return PyErr_Format(PyExc_TypeError, "kv_release takes 6 arguments");
+    HANDLE_TH_ERRORS
+    void* h = a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor* pool = tensor(a[1], "pool");
+    if (!pool) return nullptr;
+    if (!h) return fail(US_ERR_INVALID_ARG, "us_kv_release");
+    Place at_;
+    if (!at_.enter(a[5], *pool)) return nullptr;
+    int32_t* refs = take_refs(a[2], *pool);
+    us_kv_seqs q;
+    if (!refs || !take_seqs(a[3], a[4], Py_None, -1, *pool, &q)) return nullptr;
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_kv_release(static_cast<us_kv*>(h), refs, &q, at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_kv_release");
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_extend(handle, pool, refs, table, lengths, tokens, stream); tokens: a number, or one for each sequence
+PyObject* kv_extend(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "kv_extend takes 7 arguments");
+    HANDLE_TH_ERRORS
+    void* h = a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor* pool = tensor(a[1], "pool");
+    if (!pool) return nullptr;
+    if (!h) return fail(US_ERR_INVALID_ARG, "us_kv_extend");
+    Place at_;
+    if (!at_.enter(a[6], *pool)) return nullptr;
+    int32_t* refs = take_refs(a[2], *pool);
+    us_kv_seqs q;
+    if (!refs || !take_seqs(a[3], a[4], Py_None, -1, *pool, &q)) return nullptr;
+    const int32_t* tokens = nullptr;
+    int64_t each = 0;
+    if (THPVariable_Check(a[5])) {
+        const at::Tensor* t = tensor(a[5], "tokens");
+        if (!is_int_row(*t, q.n_seqs, *pool)) return bad("tokens must be a number or a contiguous int32 tensor with an entry for each sequence, on the cache's device");
+        tokens = static_cast<const int32_t*>(t->data_ptr());
+    } else {
+        each = PyLong_AsLongLong(a[5]);
+        if (PyErr_Occurred()) return nullptr;
+        if (each < 0 || each > 0x7FFFFFFF) return bad("tokens must be 0 or more");
+    }
+    at::Tensor scratch;
+    const int64_t bytes = us_kv_extend_scratch(static_cast<us_kv*>(h), q.n_seqs);
+    if (q.n_seqs > 0) scratch = at::detail::empty_cuda({bytes}, at::kByte, pool->device(), std::nullopt);
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_kv_extend(static_cast<us_kv*>(h), refs, const_cast<int32_t*>(q.block_table), q.table_stride, q.table_width, const_cast<int32_t*>(q.lengths), q.n_seqs, tokens,
+                     (int32_t)each, q.n_seqs > 0 ? scratch.data_ptr() : nullptr, bytes, at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_kv_extend");
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_compact(handle, pool, refs, ((table, lengths), ...), stream) -> blocks in use
+PyObject* kv_compact(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "kv_compact takes 5 arguments");
+    HANDLE_TH_ERRORS
+    void* h = a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor* pool = tensor(a[1], "pool");
+    if (!pool) return nullptr;
+    if (!h) return fail(US_ERR_INVALID_ARG, "us_kv_compact");
+    Place at_;
+    if (!at_.enter(a[4], *pool)) return nullptr;
+    int32_t* refs = take_refs(a[2], *pool);
+    if (!refs) return nullptr;
+    if (!PyTuple_Check(a[3])) return bad("tables must be (table, lengths) pairs");
+    const Py_ssize_t tables = PyTuple_GET_SIZE(a[3]);
+    std::vector<us_kv_seqs> q((size_t)tables);
+    for (Py_ssize_t i = 0; i < tables; ++i) {   // (all of them are looked at before a block moves)
+        PyObject* t = PyTuple_GET_ITEM(a[3], i);
+        if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 2) return bad("tables must be (table, lengths) pairs");
+        if (!take_seqs(PyTuple_GET_ITEM(t, 0), PyTuple_GET_ITEM(t, 1), Py_None, -1, *pool, &q[(size_t)i])) return nullptr;
+        if (q[(size_t)i].n_seqs > 0 && (q[(size_t)i].table_width < 1 || (int64_t)q[(size_t)i].table_width * pool->size(2) >= (1ll << 31) - (1 << 16)))
+            return bad("a table is empty or too wide");
+    }
+    const int64_t bytes = us_kv_compact_scratch(static_cast<us_kv*>(h));
+    at::Tensor scratch = at::detail::empty_cuda({bytes}, at::kByte, pool->device(), std::nullopt);
+    at::Tensor map = at::detail::empty_cuda({pool->size(0)}, at::kInt, pool->device(), std::nullopt);
+    at::Tensor used = at::detail::empty_cuda(at::IntArrayRef{}, at::kInt, pool->device(), std::nullopt);
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    const int32_t* to = static_cast<const int32_t*>(map.data_ptr());
+    s = us_kv_compact(static_cast<us_kv*>(h), refs, static_cast<int32_t*>(map.data_ptr()), static_cast<int32_t*>(used.data_ptr()), scratch.data_ptr(), bytes, at_.stream);
+    for (const us_kv_seqs& t : q)
+        if (s == US_OK)
+            s = us_kv_remap(static_cast<us_kv*>(h), to, const_cast<int32_t*>(t.block_table), t.table_stride, t.table_width, t.lengths, t.n_seqs, at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_kv_compact");
+    return THPVariable_Wrap(std::move(used));
+    END_HANDLE_TH_ERRORS
+}
+
+// ---- norms and rotation of heads ----
+
+// qk_norm_rope(q, k, positions, turns, axis, axes, rotary_dim, interleaved, q_weight, k_weight, eps, q_out, k_out, stream) -> (q, k)
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 14) return PyErr_Format(PyExc_TypeError, "qk_norm_rope takes 14 arguments");
+    HANDLE_TH_ERRORS
+    const at::Tensor *Q = tensor(a[0], "q"), *K = nullptr, *pos = Q ? tensor(a[2], "positions") : nullptr, *turns = pos ? tensor(a[3], "turns") : nullptr;
+    if (!turns || (a[1] != Py_None && !(K = tensor(a[1], "k")))) return nullptr;
+    const at::Tensor* axis = nullptr;
+    if (a[4] != Py_None && !(axis = tensor(a[4], "axis"))) return nullptr;
+    us_rotary r = {};
+    r.axes = (int32_t)PyLong_AsLong(a[5]);
+    r.rotary_dim = (int32_t)PyLong_AsLong(a[6]);
+    r.interleaved = PyObject_IsTrue(a[7]);
+    const double eps = PyFloat_AsDouble(a[10]);
+    if (PyErr_Occurred()) return nullptr;
+    Place at_;
+    if (!at_.enter(a[13], *Q)) return nullptr;
+    if (turns->device() != Q->device()) return bad("the rotary table lies on another device");
+    r.turns = static_cast<const uint64_t*>(turns->data_ptr());
+    r.axis = axis ? static_cast<const uint8_t*>(axis->data_ptr()) : nullptr;
+    if (Q->dim() != 3 || (K && K->dim() != 3)) return bad("q and k must be (N, heads, head_dim) tensors");
+    const int64_t N = Q->size(0), D = Q->size(2);
+    if (!is_heads(*Q, D, *Q) || (K && (!is_heads(*K, D, *Q) || K->size(0) != N || K->scalar_type() != Q->scalar_type())) || N >= (1ll << 31) || D > 256)
+        return bad("q and k must be (N, heads, head_dim) tensors of one type (float16, bfloat16 or float32) with unit last stride on one device, head_dim at most 256");
+    const bool flat = pos->dim() == 1;
+    if (!is_ints(*pos, *Q) || pos->dim() < 1 || pos->dim() > 2 || (flat ? r.axes != 1 : pos->size(0) != r.axes) || pos->size(flat ? 0 : 1) != N ||
+        (N > 1 && pos->stride(flat ? 0 : 1) != 1) || (!flat && pos->stride(0) < 0))
+        return bad("positions must be an int32 (N,) or (axes, N) tensor with unit last stride on q's device");
+    us_heads h[2] = {};
+    at::Tensor fresh[2];
+    for (int i = 0; i < 2; ++i) {
+        const at::Tensor* x = i ? K : Q;
+        if (!x) {
+            if (a[12] != Py_None) return bad("k_out without k");
+            continue;
+        }
+        PyObject *w = a[8 + i], *o = a[11 + i];
+        h[i].x = x->data_ptr();
+        h[i].token_stride = token_stride(*x);
+        h[i].head_stride = head_stride(*x);
+        h[i].heads = (int32_t)x->size(1);
+        if (x->size(1) > 65535) return bad("at most 65535 heads");
+        if (w != Py_None) {
+            const at::Tensor* t = tensor(w, i ? "k_weight" : "q_weight");
+            if (!t) return nullptr;
+            if (t->dim() != 1 || t->size(0) != D || type_of(t->scalar_type()) < 0 || !t->is_contiguous() || t->device() != Q->device())
+                return bad("a weight must be a contiguous (head_dim,) tensor of float16, bfloat16 or float32 on q's device");
+            h[i].weight = t->data_ptr();
+            h[i].weight_type = type_of(t->scalar_type());
+        }
+        const at::Tensor* out = &fresh[i];
+        if (o == Py_None) {
+            const int64_t shape[3] = {N, x->size(1), D};
+            fresh[i] = at::detail::empty_cuda(shape, x->scalar_type(), x->device(), std::nullopt);
+        } else {
+            out = tensor(o, i ? "k_out" : "q_out");
+            if (!out) return nullptr;
+            if (!is_heads(*out, D, *Q) || out->scalar_type() != x->scalar_type() || out->size(0) != N || out->size(1) != x->size(1))
+                return bad("an output must be a tensor of its input's shape and type with unit last stride on its device");
+        }
+        h[i].out = out->data_ptr();
+        h[i].out_token_stride = token_stride(*out);
+        h[i].out_head_stride = head_stride(*out);
+    }
+    const int64_t axis_stride = flat || r.axes == 1 ? 0 : pos->stride(0);
+    us_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = us_qk_norm_rope(&r, static_cast<const int32_t*>(pos->data_ptr()), axis_stride, N, (int32_t)D, type_of(Q->scalar_type()), &h[0], K ? &h[1] : nullptr, (float)eps, at_.stream);
+    Py_END_ALLOW_THREADS
+    if (s != US_OK) return fail(s, "us_qk_norm_rope");
+    PyObject* q = give(a[11], std::move(fresh[0]));
+    if (!K) {
+        Py_INCREF(Py_None);
+        return Py_BuildValue("NN", q, Py_None);
+    }
+    return Py_BuildValue("NN", q, give(a[12], std::move(fresh[1])));
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject* set_error(PyObject*, PyObject* cls)
 {
     Py_XDECREF(g_error);
@@ -577,6 +832,12 @@ PyMethodDef methods[] = {
     {"kv_append", fast(kv_append), METH_FASTCALL, nullptr},
     {"kv_read", fast(kv_read), METH_FASTCALL, nullptr},
     {"kv_attention", fast(kv_attention), METH_FASTCALL, nullptr},
+    {"kv_copy_blocks", fast(kv_copy_blocks), METH_FASTCALL, nullptr},
+    {"kv_fork", fast(kv_fork), METH_FASTCALL, nullptr},
+    {"kv_release", fast(kv_release), METH_FASTCALL, nullptr},
+    {"kv_extend", fast(kv_extend), METH_FASTCALL, nullptr},
+    {"kv_compact", fast(kv_compact), METH_FASTCALL, nullptr},
+    {"qk_norm_rope", fast(qk_norm_rope), METH_FASTCALL, nullptr},
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
