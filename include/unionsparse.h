@@ -322,6 +322,27 @@ us_status us_mx4_linear(const void* X, int32_t x_type, int64_t ldx, int64_t N, c
 us_status us_mx4_last_error(void);
 
 /*
+ * The same products with what follows a projection in their epilogue: with v = sum_k x[n][k] w[m][k] in fp32,
+ *     Y[n][m] = RN_y_type(f(v_m + bias_m) + residual[n][m]),   or, gated (M even; Y and residual have M / 2 columns),
+ *     Y[n][j] = RN_y_type(f(v_2j + bias_2j) * (v_2j+1 + bias_2j+1) + residual[n][j]):
+ * rows 2 j and 2 j + 1 of the weight are gate and up row j. f: nothing, max(z, 0), z / (1 + e^-z), z (1 + erf(z / sqrt 2)) / 2, or z (1 + tanh(sqrt(2 / pi)
+ * (z + 0.044715 z^3))) / 2, in fp32; for 16-bit Y its quotients below 2^-126 are 0. bias (M values) and residual (N rows, ldr elements apart) are of any
+ * us_type, or NULL. The residual may be Y itself (same address, type and row stride); otherwise they do not overlap. e = NULL: no epilogue. Scratch, flags and errors as above.
+ */
+typedef enum us_act { US_ACT_NONE = 0, US_ACT_RELU = 1, US_ACT_SILU = 2, US_ACT_GELU = 3, US_ACT_GELU_TANH = 4 } us_act;
+typedef struct us_mx4_epilogue {
+    const void* bias;
+    const void* residual;
+    int64_t ldr;
+    int32_t bias_type, residual_type, act, gated;
+} us_mx4_epilogue;
+us_status us_mx4_matmul_epilogue(const void* x_mx, int64_t N, const void* w_mx, int64_t M, int64_t K, const us_mx4_epilogue* e, void* Y,
+                                 int32_t y_type, int64_t ldy, uint32_t flags, void* stream);
+us_status us_mx4_linear_epilogue(const void* X, int32_t x_type, int64_t ldx, int64_t N, const void* w_mx, int64_t M, int64_t K,
+                                 const us_mx4_epilogue* e, void* Y, int32_t y_type, int64_t ldy, void* scratch, int64_t scratch_bytes,
+                                 uint32_t flags, void* stream);
+
+/*
  * The cache of keys and values in 8 bits, and attention over it (no counterpart in the paper): what stands between the
  * Q/K/V projection of a decoder layer and its O projection.
  *

@@ -30,7 +30,7 @@ EXPORTS = ["us_encode", "us_get_stats", "us_decode", "us_get_row_order", "us_spm
            "us_spmm_requant", "us_absmax_f16", "us_quantize_f16",
            "us_last_error", "us_debug_withhold_copy", "us_stage_timers", "us_destroy", "us_spmm_bytes", "us_launch_info", "us_launch_kernel",
            "us_mx4_bytes", "us_mx4_quantize", "us_mx4_dequantize", "us_mx4_pack", "us_mx4_unpack", "us_mx4_matmul",
-           "us_mx4_linear_scratch", "us_mx4_linear", "us_mx4_last_error",
+           "us_mx4_linear_scratch", "us_mx4_linear", "us_mx4_matmul_epilogue", "us_mx4_linear_epilogue", "us_mx4_last_error",
            "us_kv_create", "us_kv_append", "us_kv_read", "us_kv_attention_scratch", "us_kv_attention", "us_kv_last_error", "us_kv_destroy",
            "us_kv_fork", "us_kv_release", "us_kv_extend_scratch", "us_kv_extend", "us_kv_compact_scratch", "us_kv_compact", "us_kv_remap", "us_kv_copy_blocks",
            "us_qk_norm_rope",
@@ -82,6 +82,14 @@ _lib.us_mx4_matmul.argtypes = [_vp, _i64, _vp, _i64, _i64, _vp, _i32, _i64, ctyp
 _lib.us_mx4_linear_scratch.argtypes = [_i64, _i64, _i64]
 _lib.us_mx4_linear_scratch.restype = _i64
 _lib.us_mx4_linear.argtypes = [_vp, _i32, _i64, _i64, _vp, _i64, _i64, _vp, _i32, _i64, _vp, _i64, ctypes.c_uint32, _vp]
+
+
+class us_mx4_epilogue(ctypes.Structure):
+    _fields_ = [("bias", _vp), ("residual", _vp), ("ldr", _i64), ("bias_type", _i32), ("residual_type", _i32), ("act", _i32), ("gated", _i32)]
+
+
+_lib.us_mx4_matmul_epilogue.argtypes = [_vp, _i64, _vp, _i64, _i64, ctypes.POINTER(us_mx4_epilogue), _vp, _i32, _i64, ctypes.c_uint32, _vp]
+_lib.us_mx4_linear_epilogue.argtypes = [_vp, _i32, _i64, _i64, _vp, _i64, _i64, ctypes.POINTER(us_mx4_epilogue), _vp, _i32, _i64, _vp, _i64, ctypes.c_uint32, _vp]
 _lib.us_mx4_last_error.argtypes = []
 
 
@@ -441,16 +449,25 @@ def mx4_from_codes(codes, scales, K: int, stream=None) -> Mx4:
     return m.freeze()
 
 
-def mx4_linear(X, w: Mx4, out=None, dtype=None, stream=None):
+ACTIVATIONS = {None: 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+
+
+def mx4_linear(X, w: Mx4, out=None, dtype=None, stream=None, bias=None, act=None, gated=False, residual=None):
     """(N, M) product of activations and the transposed (M, K) weight. X: device float16, bfloat16 or float32 (N, K) tensor or view
     (unit column stride), quantised to MX4 within the call, or an Mx4. The result has `dtype`, by default X's (float16 for an Mx4);
-    `out` may have any row stride."""
+    `out` may have any row stride.
+
+    What follows the product is done on its sums: y = act(x w^T + bias) + residual. act: None, "relu", "silu", "gelu" or "gelu_tanh". gated: rows
+    2 j and 2 j + 1 of w (and of bias) are gate and up projection of column j, y = act(gate) * up + residual, (N, M / 2). bias (M,) and residual (N, columns of the
+    result; any row stride) may be of any of the three types; the residual may be `out` itself, and otherwise does not overlap it."""
     ext = _ext or _native()
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {list(ACTIVATIONS)}")
     if isinstance(X, Mx4):
         if X.K != w.K:
             raise ValueError("X and w differ in K")
-        return ext.mx4_linear(X.data, X.rows, w.data, w.rows, w.K, out, dtype, w.frozen, stream)
-    return ext.mx4_linear(X, -1, w.data, w.rows, w.K, out, dtype, w.frozen, stream)
+        return ext.mx4_linear(X.data, X.rows, w.data, w.rows, w.K, out, dtype, w.frozen, stream, bias, ACTIVATIONS[act], gated, residual)
+    return ext.mx4_linear(X, -1, w.data, w.rows, w.K, out, dtype, w.frozen, stream, bias, ACTIVATIONS[act], gated, residual)
 
 
 def mx4_check():

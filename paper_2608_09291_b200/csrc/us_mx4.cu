@@ -15,10 +15,10 @@ struct Plan {
 };
 
 template <int NB, bool FUSE>
-void shape(Plan* p, int64_t slice_tiles, int64_t budget)
+void shape(Plan* p, int64_t slice_tiles, int64_t budget, int epi)
 {
     using S = Mx4Shape<NB, FUSE>;
-    p->kernel = (const void*)us_mx4_product_kernel<NB, FUSE>;
+    p->kernel = epi == 2 ? (const void*)us_mx4_product_kernel<NB, FUSE, 2> : epi == 1 ? (const void*)us_mx4_product_kernel<NB, FUSE, 1> : (const void*)us_mx4_product_kernel<NB, FUSE>;
     const int64_t xs = FUSE ? slice_tiles * S::kXTile : 0;
     // (the split's partial sums, 128 x NB fp32, take the ring's place; else two buffers of 32 tokens on their way out)
     const int64_t least = ((p->split > 1 ? 128 * 4 * NB : 2 * 32 * (512 + 16)) + S::kStage - 1) / S::kStage;
@@ -28,8 +28,8 @@ void shape(Plan* p, int64_t slice_tiles, int64_t budget)
 
 constexpr int64_t kHalfSm = 112 * 1024, kWholeSm = 226 * 1024;   // shared memory of a CTA with and without room for a second one
 
-// How a product of N tokens is cut. can_fuse: the activations are rows in 16 or 32 bits.
-Plan plan(int64_t N, int64_t M, int64_t K, bool can_fuse, int sms)
+// How a product of N tokens is cut. can_fuse: the activations are rows in 16 or 32 bits; epi: without an epilogue (0), with one (1), gated (2).
+Plan plan(int64_t N, int64_t M, int64_t K, bool can_fuse, int sms, int epi = 0)
 {
     Plan p = {};
     const int64_t kt = mx4_tiles(K, 256), rt = mx4_tiles(M, 128);
@@ -49,15 +49,16 @@ Plan plan(int64_t N, int64_t M, int64_t K, bool can_fuse, int sms)
     // A CTA quantises its activations itself where that is one trip to memory for its four warps (four tiles of a token each); beyond, every
     // CTA's own copy of the work takes longer than a launch for all (11008 x 4096, 8 tokens: 11.2 us against 6.9).
     p.fuse = can_fuse && p.nb == 16 && slice * N <= 16;
-    if (p.fuse) shape<16, true>(&p, slice, kHalfSm);
-    else if (p.nb == 16) shape<16, false>(&p, slice, kHalfSm);
-    else if (p.nb == 32) shape<32, false>(&p, slice, kHalfSm);
-    else if (p.nb == 64) shape<64, false>(&p, slice, kHalfSm);
-    else if (p.nb == 128) shape<128, false>(&p, slice, p.tiles * p.split > sms ? kHalfSm : kWholeSm);
+    if (p.fuse) shape<16, true>(&p, slice, kHalfSm, epi);
+    else if (p.nb == 16) shape<16, false>(&p, slice, kHalfSm, epi);
+    else if (p.nb == 32) shape<32, false>(&p, slice, kHalfSm, epi);
+    else if (p.nb == 64) shape<64, false>(&p, slice, kHalfSm, epi);
+    else if (p.nb == 128) shape<128, false>(&p, slice, p.tiles * p.split > sms ? kHalfSm : kWholeSm, epi);
     p.blocks = p.tiles * p.split;
     p.cluster = p.split;
     if (p.nb == 256) {   // pairs of blocks that walk over pairs of tiles
-        p.kernel = (const void*)us_mx4_pair_kernel<Mx4Pair::kStages>;
+        p.kernel = epi == 2 ? (const void*)us_mx4_pair_kernel<Mx4Pair::kStages, 2> : epi == 1 ? (const void*)us_mx4_pair_kernel<Mx4Pair::kStages, 1> :
+                                                                                     (const void*)us_mx4_pair_kernel<Mx4Pair::kStages>;
         p.smem = Mx4Pair::kSmem;
         p.tiles = mx4_tiles(rt, 2) * p.col_tiles;
         p.blocks = 2 * std::min<int64_t>(p.tiles, sms / 2);
@@ -90,7 +91,7 @@ dim3 warps_grid(int64_t warps) { return dim3((unsigned)std::max<int64_t>(1, std:
 bool shape_ok(int64_t rows, int64_t K) { return rows >= 0 && rows < (1ll << 31) && K >= 1 && K <= (1ll << 30); }
 
 us_status product(const void* X, int32_t x_type, int64_t ldx, const void* x_mx, int64_t N, const void* w_mx, int64_t M, int64_t K, void* Y,
-                  int32_t y_type, int64_t ldy, const Plan& pl, uint32_t flags, cudaStream_t st)
+                  int32_t y_type, int64_t ldy, const us_mx4_epilogue* e, const Plan& pl, uint32_t flags, cudaStream_t st)
 {
     static void* kept[kMaxDevices];
     void* err = nullptr;
@@ -108,8 +109,13 @@ us_status product(const void* X, int32_t x_type, int64_t ldx, const void* x_mx, 
     p.y_vec = rows_vec(Y, N > 1 ? ldy : 0, size_of(y_type));
     p.w_stable = (flags & US_MX4_W_STABLE) != 0;
     p.err = static_cast<uint32_t*>(err);
-    const cudaError_t e = ops_kernel_allow(pl.kernel, (int)kWholeSm);
-    if (e != cudaSuccess) return cuda(e);
+    if (e) {
+        p.e.bias = e->bias; p.e.bias_type = e->bias_type;
+        p.e.residual = e->residual; p.e.r_type = e->residual_type; p.e.ldr = N > 1 ? e->ldr : 0;
+        p.e.act = e->act;
+    }
+    const cudaError_t er = ops_kernel_allow(pl.kernel, (int)kWholeSm);
+    if (er != cudaSuccess) return cuda(er);
     void* args[] = {&p};
     return cuda(ops_launch(pl.kernel, dim3((unsigned)pl.blocks), 192, pl.smem, st, args, (unsigned)pl.cluster));
 }
@@ -173,18 +179,33 @@ us_status us_mx4_unpack(const void* mx, int64_t rows, int64_t K, void* codes, in
     return repack(false, codes, ldc, scales, lds, rows, K, const_cast<void*>(mx), stream);
 }
 
-static bool product_ok(int64_t N, const void* w_mx, int64_t M, int64_t K, const void* Y, int32_t y_type, int64_t ldy)
+// Columns of the output, and whether an epilogue is one.
+static int64_t columns(int64_t M, const us_mx4_epilogue* e) { return e && e->gated ? M / 2 : M; }
+static bool epilogue_ok(const us_mx4_epilogue* e, int64_t N, int64_t M)
 {
-    return shape_ok(N, K) && shape_ok(M, K) && M >= 1 && type_ok(y_type) &&
-           (N == 0 || (w_mx && aligned(w_mx, 16) && Y && aligned(Y, size_of(y_type)) && (N == 1 || ldy >= M))) &&
+    if (!e) return true;
+    return e->act >= US_ACT_NONE && e->act <= US_ACT_GELU_TANH && !(e->gated && M % 2) && (!e->bias || (type_ok(e->bias_type) && aligned(e->bias, size_of(e->bias_type)))) &&
+           (!e->residual || (type_ok(e->residual_type) && aligned(e->residual, size_of(e->residual_type)) && (N <= 1 || e->ldr >= columns(M, e))));
+}
+static int kind(const us_mx4_epilogue* e) { return !e ? 0 : e->gated ? 2 : e->bias || e->residual || e->act != US_ACT_NONE ? 1 : 0; }
+
+static bool product_ok(int64_t N, const void* w_mx, int64_t M, int64_t K, const us_mx4_epilogue* e, const void* Y, int32_t y_type, int64_t ldy)
+{
+    return shape_ok(N, K) && shape_ok(M, K) && M >= 1 && type_ok(y_type) && epilogue_ok(e, N, M) &&
+           (N == 0 || (w_mx && aligned(w_mx, 16) && Y && aligned(Y, size_of(y_type)) && (N == 1 || ldy >= columns(M, e)))) &&
            us::mx4_tiles(M, 128) * us::mx4_tiles(N, 16) * 16 < (1ll << 31);
 }
 
+us_status us_mx4_matmul_epilogue(const void* x_mx, int64_t N, const void* w_mx, int64_t M, int64_t K, const us_mx4_epilogue* e, void* Y, int32_t y_type, int64_t ldy,
+                                 uint32_t flags, void* stream)
+{
+    if (!product_ok(N, w_mx, M, K, e, Y, y_type, ldy) || (N && (!x_mx || !aligned(x_mx, 16)))) return US_ERR_INVALID_ARG;
+    if (N == 0) return US_OK;
+    return product(nullptr, 0, 0, x_mx, N, w_mx, M, K, Y, y_type, ldy, e, plan(N, M, K, false, ops_sms(), kind(e)), flags, static_cast<cudaStream_t>(stream));
+}
 us_status us_mx4_matmul(const void* x_mx, int64_t N, const void* w_mx, int64_t M, int64_t K, void* Y, int32_t y_type, int64_t ldy, uint32_t flags, void* stream)
 {
-    if (!product_ok(N, w_mx, M, K, Y, y_type, ldy) || (N && (!x_mx || !aligned(x_mx, 16)))) return US_ERR_INVALID_ARG;
-    if (N == 0) return US_OK;
-    return product(nullptr, 0, 0, x_mx, N, w_mx, M, K, Y, y_type, ldy, plan(N, M, K, false, ops_sms()), flags, static_cast<cudaStream_t>(stream));
+    return us_mx4_matmul_epilogue(x_mx, N, w_mx, M, K, nullptr, Y, y_type, ldy, flags, stream);
 }
 
 int64_t us_mx4_linear_scratch(int64_t N, int64_t M, int64_t K)
@@ -193,20 +214,25 @@ int64_t us_mx4_linear_scratch(int64_t N, int64_t M, int64_t K)
     return N == 0 || plan(N, M, K, true, ops_sms()).fuse ? 0 : us_mx4_bytes(N, K);
 }
 
-us_status us_mx4_linear(const void* X, int32_t x_type, int64_t ldx, int64_t N, const void* w_mx, int64_t M, int64_t K, void* Y, int32_t y_type,
-                        int64_t ldy, void* scratch, int64_t scratch_bytes, uint32_t flags, void* stream)
+us_status us_mx4_linear_epilogue(const void* X, int32_t x_type, int64_t ldx, int64_t N, const void* w_mx, int64_t M, int64_t K, const us_mx4_epilogue* e, void* Y,
+                                 int32_t y_type, int64_t ldy, void* scratch, int64_t scratch_bytes, uint32_t flags, void* stream)
 {
-    if (!type_ok(x_type) || !product_ok(N, w_mx, M, K, Y, y_type, ldy)) return US_ERR_INVALID_ARG;
+    if (!type_ok(x_type) || !product_ok(N, w_mx, M, K, e, Y, y_type, ldy)) return US_ERR_INVALID_ARG;
     if (N == 0) return US_OK;
     if (!X || !aligned(X, size_of(x_type)) || (N > 1 && ldx < K)) return US_ERR_INVALID_ARG;
     if (N == 1) ldx = 0;
-    const Plan pl = plan(N, M, K, true, ops_sms());
+    const Plan pl = plan(N, M, K, true, ops_sms(), kind(e));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (pl.fuse) return product(X, x_type, ldx, nullptr, N, w_mx, M, K, Y, y_type, ldy, pl, flags, st);
+    if (pl.fuse) return product(X, x_type, ldx, nullptr, N, w_mx, M, K, Y, y_type, ldy, e, pl, flags, st);
     if (!scratch || !aligned(scratch, 16) || scratch_bytes < us_mx4_bytes(N, K)) return US_ERR_SCRATCH_TOO_SMALL;
     const us_status s = us_mx4_quantize(X, x_type, ldx, N, K, scratch, stream);
     if (s != US_OK) return s;
-    return product(nullptr, 0, 0, scratch, N, w_mx, M, K, Y, y_type, ldy, pl, flags, st);
+    return product(nullptr, 0, 0, scratch, N, w_mx, M, K, Y, y_type, ldy, e, pl, flags, st);
+}
+us_status us_mx4_linear(const void* X, int32_t x_type, int64_t ldx, int64_t N, const void* w_mx, int64_t M, int64_t K, void* Y, int32_t y_type,
+                        int64_t ldy, void* scratch, int64_t scratch_bytes, uint32_t flags, void* stream)
+{
+    return us_mx4_linear_epilogue(X, x_type, ldx, N, w_mx, M, K, nullptr, Y, y_type, ldy, scratch, scratch_bytes, flags, stream);
 }
 
 us_status us_mx4_last_error(void)

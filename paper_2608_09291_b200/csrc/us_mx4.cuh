@@ -12,6 +12,8 @@
 
 #include <cuda_bf16.h>
 
+#include "../../include/unionsparse.h"
+
 namespace us {
 
 constexpr int kMxScales = 1024, kMxCodes = 16384, kMxTile = kMxScales + kMxCodes;   // bytes
@@ -387,7 +389,13 @@ __global__ void __launch_bounds__(256) us_mx4_repack_kernel(uint8_t* codes, int6
 //     in the order of the ranks: no workspace, no atomics, the same result every time.
 //   * Bound by the weights' way from memory: 28672 x 8192, 8 tokens: 22 us, 5.6 TB/s; 4096 x 4096, one token: 4.6 us, most of it latency.
 //   * Few tokens (FUSE): the CTA quantises its own columns of X while its weights are on the way: one launch instead of two.
+struct Mx4Epilogue {
+    const void *bias, *residual;   // or nullptr
+    int64_t ldr;
+    int32_t bias_type, r_type, act;
+};
 struct Mx4Params {
+    Mx4Epilogue e;
     const uint8_t* w;
     const uint8_t* x;      // tiles, or
     const void* X;         // (FUSE) rows of x_type
@@ -489,6 +497,126 @@ __device__ __forceinline__ void mx4_store4(const Mx4Params& p, int64_t n, int64_
         else for (int i = 0; i < 4; ++i) if (m + i < p.M) y[i] = h[i];
     }
 }
+// ---- what follows a product, on its sums in fp32: y = f(v + bias) + residual, or (gated) rows 2 j and 2 j + 1 of the weight give y_j = f(v + bias) * (v' + bias')
+// + residual. Rounded once, at the end. Kernels come without an epilogue (EPI = 0), with one (1), and gated (2).
+__device__ __forceinline__ float mx4_scalar(const void* p, int32_t type, int64_t i)
+{
+    if (type == kF32) return __ldcg(static_cast<const float*>(p) + i);
+    const uint16_t h = __ldcg(static_cast<const uint16_t*>(p) + i);
+    return type == kF16 ? __half2float(__ushort_as_half(h)) : __uint_as_float((uint32_t)h << 16);
+}
+// x / (1 + e^-z). FAST (16-bit results): approximate exponential and reciprocal, each good to 2^-22; quotients below 2^-126 are 0.
+template <bool FAST>
+__device__ __forceinline__ float mx4_sigmoid_times(float x, float z)
+{
+    if (!FAST) return x / (1.f + expf(-z));
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return x * r;
+}
+template <bool FAST, int N>
+__device__ __forceinline__ void mx4_activate(int32_t act, float (&v)[N])
+{
+    if (act == US_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
+    } else if (act == US_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = mx4_sigmoid_times<FAST>(v[i], v[i]);
+    } else if (act == US_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * erfcf(v[i] * -0.70710678f);
+    } else if (act == US_ACT_GELU_TANH) {   // (1 + tanh z) / 2 = 1 / (1 + e^-2z)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = mx4_sigmoid_times<FAST>(v[i], 1.59576912f * v[i] * fmaf(0.044715f * v[i], v[i], 1.f));
+    }
+}
+// A thread's part of the residual for CH tokens of its weight row m: fetched ahead, as it is. (Gated: two lanes share an output column; the even one
+// has the even tokens.)
+template <int EPI, int CH>
+struct Mx4Residual {
+    static constexpr int K = EPI == 2 ? CH / 2 : CH;
+    uint32_t x[EPI ? K : 1];
+    __device__ __forceinline__ void load(const Mx4Params& p, int64_t n, int tokens, int64_t m)
+    {
+        if (!EPI || !p.e.residual) return;
+        const int64_t col = EPI == 2 ? m >> 1 : m;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int t = EPI == 2 ? 2 * k + (int)(m & 1) : k;
+            if (t >= tokens || m >= p.M) continue;
+            const int64_t at = (n + t) * p.e.ldr + col;
+            x[k] = p.e.r_type == kF32 ? __ldcg(static_cast<const uint32_t*>(p.e.residual) + at) : __ldcg(static_cast<const uint16_t*>(p.e.residual) + at);
+        }
+    }
+    __device__ __forceinline__ float at(const Mx4Params& p, int k) const
+    {
+        return p.e.r_type == kF32 ? __uint_as_float(x[k]) : p.e.r_type == kF16 ? __half2float(__ushort_as_half((unsigned short)x[k])) : __uint_as_float(x[k] << 16);
+    }
+};
+// CH tokens' sums of weight row `row` of the tile (m of the matrix), finished and rounded, to their places [token][column] in shared memory.
+template <class T, int EPI, int CH>
+__device__ __forceinline__ void mx4_finish(const Mx4Params& p, const uint32_t (&r)[CH], const Mx4Residual<EPI, CH>& res, float bias, int row, uint8_t* b, int pitch)
+{
+    if (EPI == 0) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) *reinterpret_cast<T*>(b + i * pitch + row * sizeof(T)) = from_f32<T>(__uint_as_float(r[i]));
+        return;
+    }
+    constexpr bool FAST = sizeof(T) == 2;
+    constexpr int K = EPI == 2 ? CH / 2 : CH;
+    float v[K], up[EPI == 2 ? K : 1];
+    const bool odd = row & 1;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (EPI == 2) {
+            const float x = __uint_as_float(r[2 * k]) + bias, y = __uint_as_float(r[2 * k + 1]) + bias;
+            const float got = __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
+            v[k] = odd ? got : x;
+            up[k] = odd ? y : got;
+        } else {
+            v[k] = __uint_as_float(r[k]) + bias;
+        }
+    }
+    mx4_activate<FAST>(p.e.act, v);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (EPI == 2) v[k] *= up[k];
+        if (p.e.residual) v[k] += res.at(p, k);
+        const int t = EPI == 2 ? 2 * k + (odd ? 1 : 0) : k, c = EPI == 2 ? row >> 1 : row;
+        *reinterpret_cast<T*>(b + t * pitch + c * sizeof(T)) = from_f32<T>(v[k]);
+    }
+}
+// Token n, weight rows m .. m + 3 (of which the matrix has at least the first): finished and stored.
+template <int EPI>
+__device__ __forceinline__ void mx4_finish4(const Mx4Params& p, int64_t n, int64_t m, float (&v)[4])
+{
+    if (EPI == 0) return mx4_store4(p, n, m, v);
+    if (m >= p.M) return;
+    if (p.e.bias)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (m + i < p.M) v[i] += mx4_scalar(p.e.bias, p.e.bias_type, m + i);
+    if (EPI == 1) {
+        mx4_activate<false>(p.e.act, v);
+        if (p.e.residual)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (m + i < p.M) v[i] += mx4_scalar(p.e.residual, p.e.r_type, n * p.e.ldr + m + i);
+        return mx4_store4(p, n, m, v);
+    }
+    float y[2] = {v[0], v[2]};
+    mx4_activate<false>(p.e.act, y);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (m + 2 * i >= p.M) break;
+        const int64_t c = (m >> 1) + i, at = n * p.ldy + c;
+        y[i] *= v[2 * i + 1];
+        if (p.e.residual) y[i] += mx4_scalar(p.e.residual, p.e.r_type, n * p.e.ldr + c);
+        if (p.y_type == kF32) static_cast<float*>(p.Y)[at] = y[i];
+        else if (p.y_type == kF16) static_cast<__half*>(p.Y)[at] = __float2half_rn(y[i]);
+        else static_cast<__nv_bfloat16*>(p.Y)[at] = __float2bfloat16_rn(y[i]);
+    }
+}
 __device__ __forceinline__ void bar_epilogue() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 // The same barrier, and whether any of its threads says so.
 __device__ __forceinline__ bool bar_any(bool say)
@@ -502,33 +630,40 @@ __device__ __forceinline__ bool bar_any(bool say)
 // The tile's sums (four warps, lane quarter `quarter`): 32 tokens at a time to shared memory as they are stored, [token][weight row], and
 // from there in whole lines: every thread 16 bytes of a token's 256 (512). Straight from the registers a warp's store of one token is 64
 // bytes; 4096 x 28672 x 8192 took 705 us that way, whatever the products took.
-template <class T>
-__device__ __forceinline__ void mx4_write_tile(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage)
+template <class T, int EPI, int CH>
+__device__ __forceinline__ void mx4_write_tile(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage, Mx4Residual<EPI, CH>& res)
 {
-    constexpr int PITCH = 128 * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = 128 / PER;   // bytes of a token, values of a piece, pieces of a token
+    constexpr int COLS = EPI == 2 ? 64 : 128;   // columns of the output
+    constexpr int PITCH = COLS * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = COLS / PER;   // bytes of a token, values of a piece, pieces of a token
     const int row = 32 * quarter + lane, tid = row;
-    const int m_here = (int)min((int64_t)128, p.M - m0);
+    const int64_t c0 = EPI == 2 ? m0 >> 1 : m0;
+    const int m_here = (int)min((int64_t)COLS, (EPI == 2 ? p.M >> 1 : p.M) - c0);
+    const float bias = EPI && p.e.bias && m0 + row < p.M ? mx4_scalar(p.e.bias, p.e.bias_type, m0 + row) : 0.f;
     int buf = 0;
 #pragma unroll 1
-    for (int c = 0; c < nn; c += 32) {
-        uint32_t r[32];
-        tc_ld32(tm + ((uint32_t)quarter << 21) + (uint32_t)c, r);
-        tc_wait_ld();
-        pin32(r);
-        uint8_t* b = stage + buf * (32 * PITCH);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) *reinterpret_cast<T*>(b + i * PITCH + row * sizeof(T)) = from_f32<T>(__uint_as_float(r[i]));
+    for (int c = 0; c < nn; c += CH) {
+        uint32_t r[CH];
+        if constexpr (CH == 32) {
+            tc_ld32(tm + ((uint32_t)quarter << 21) + (uint32_t)c, r);
+            tc_wait_ld();
+            pin32(r);
+        } else {
+            tc_ld16(tm + ((uint32_t)quarter << 21) + (uint32_t)c, r);
+        }
+        uint8_t* b = stage + buf * (CH * PITCH);
+        mx4_finish<T, EPI, CH>(p, r, res, bias, row, b, PITCH);
+        if (EPI && c + CH < nn) res.load(p, n0 + c + CH, nn - c - CH, m0 + row);
         bar_epilogue();   // (two buffers: whoever is a chunk behind still reads the other one)
-        const int rows = min(32, nn - c);
-        if (p.y_vec && m_here == 128) {
+        const int rows = min(CH, nn - c);
+        if (p.y_vec && m_here == COLS) {
 #pragma unroll
-            for (int k = 0; k < 32 * ROW / 128; ++k) {
+            for (int k = 0; k < CH * ROW / 128; ++k) {
                 const int i = tid + 128 * k, n = i / ROW, piece = i % ROW;
-                if (n < rows) *reinterpret_cast<uint4*>(static_cast<T*>(p.Y) + (n0 + c + n) * p.ldy + m0 + piece * PER) = *reinterpret_cast<const uint4*>(b + n * PITCH + 16 * piece);
+                if (n < rows) *reinterpret_cast<uint4*>(static_cast<T*>(p.Y) + (n0 + c + n) * p.ldy + c0 + piece * PER) = *reinterpret_cast<const uint4*>(b + n * PITCH + 16 * piece);
             }
         } else {
             for (int n = 0; n < rows; ++n)
-                if (tid < m_here) static_cast<T*>(p.Y)[(n0 + c + n) * p.ldy + m0 + tid] = *reinterpret_cast<const T*>(b + n * PITCH + tid * sizeof(T));
+                if (tid < m_here) static_cast<T*>(p.Y)[(n0 + c + n) * p.ldy + c0 + tid] = *reinterpret_cast<const T*>(b + n * PITCH + tid * sizeof(T));
         }
         buf ^= 1;
     }
@@ -563,7 +698,7 @@ __device__ __forceinline__ void mx4_quantize_slice(const Mx4Params& p, uint8_t* 
     }
 }
 
-template <int NB, bool FUSE>
+template <int NB, bool FUSE, int EPI = 0>
 __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(const __grid_constant__ Mx4Params p)
 {
     using S = Mx4Shape<NB, FUSE>;
@@ -680,10 +815,12 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
             __syncwarp();
             if (lane == 0) mbar_arrive(b_x);
         }
-        ok = ops_wait_warp(b_done, 0, 4 * kMxWait, dead);
-        tc_fence_after();
         const uint32_t quarter = (uint32_t)(warp & 3);
         const int row = 32 * (int)quarter + lane;
+        Mx4Residual<EPI, EPI ? 16 : 32> res;
+        if (EPI && p.split == 1) res.load(p, n0, nn, 128 * (int64_t)mt + row);
+        ok = ops_wait_warp(b_done, 0, 4 * kMxWait, dead);
+        tc_fence_after();
         // (the ring is free: all copies have landed and have been read)
         if (p.split > 1) {
             float* part = reinterpret_cast<float*>(ring);
@@ -696,9 +833,9 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
                     for (int i = 0; i < 16; ++i) part[(c + i) * 128 + row] = __uint_as_float(r[i]);
                 }
         } else if (!*dead) {   // (*dead is set before the sums are announced, or never)
-            if (p.y_type == kF32) mx4_write_tile<float>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring);
-            else if (p.y_type == kF16) mx4_write_tile<__half>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring);
-            else mx4_write_tile<__nv_bfloat16>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring);
+            if (p.y_type == kF32) mx4_write_tile<float>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring, res);
+            else if (p.y_type == kF16) mx4_write_tile<__half>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring, res);
+            else mx4_write_tile<__nv_bfloat16>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring, res);
         }
         tc_fence_before();
     }
@@ -711,6 +848,7 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "n"(S::kCols));
     if (p.split > 1) {
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (EPI) asm volatile("griddepcontrol.wait;" ::: "memory");   // (bias and residual: every thread that reads them has waited)
         // each rank adds the sums of a share of the tile's (token, four rows), four ranks' at a time on their way
         const int total = nn * 32, per = (total + p.split - 1) / p.split, lo = min(total, rank * per), hi = min(total, lo + per);
         const uint32_t part = smem_u32(ring);
@@ -723,7 +861,7 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
 #pragma unroll
                 for (int r = 0; r < 4; ++r) { v[0] += x[r].x; v[1] += x[r].y; v[2] += x[r].z; v[3] += x[r].w; }
             }
-            mx4_store4(p, n0 + (i >> 5), 128 * (int64_t)mt + 4 * (i & 31), v);
+            mx4_finish4<EPI>(p, n0 + (i >> 5), 128 * (int64_t)mt + 4 * (i & 31), v);
         }
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
@@ -793,11 +931,15 @@ __device__ __forceinline__ void pair_copy_scales(uint32_t elected, uint32_t d, u
 }
 
 // A block's sums (four warps) to shared memory and out; free_bar: the pair's first block's barrier, told when they are out of tensor memory.
-template <class T>
-__device__ __forceinline__ void mx4_pair_store(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage, uint32_t free_bar)
+template <class T, int EPI>
+__device__ __forceinline__ void mx4_pair_store(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage, uint32_t free_bar,
+                                               Mx4Residual<EPI, 32>& res, float bias)
 {
-    constexpr int PITCH = 128 * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = 128 / PER, PASS = 256 / (int)sizeof(T);
-    const int row = 32 * quarter + lane, m_here = (int)max((int64_t)0, min((int64_t)128, p.M - m0));   // (0: the pair's rows end with its first block)
+    constexpr int COLS = EPI == 2 ? 64 : 128;   // columns of the output
+    constexpr int PITCH = COLS * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = COLS / PER, PASS = 256 / (int)sizeof(T);
+    const int row = 32 * quarter + lane;
+    const int64_t col0 = EPI == 2 ? m0 >> 1 : m0;
+    const int m_here = (int)max((int64_t)0, min((int64_t)COLS, (EPI == 2 ? p.M >> 1 : p.M) - col0));   // (0: the pair's rows end with its first block)
 #pragma unroll 1
     for (int c0 = 0; c0 < nn; c0 += PASS) {
         const int cols = min(PASS, nn - c0);
@@ -808,8 +950,8 @@ __device__ __forceinline__ void mx4_pair_store(const Mx4Params& p, uint32_t tm, 
             tc_ld32(tm + ((uint32_t)quarter << 21) + (uint32_t)(c0 + c), r);
             tc_wait_ld();
             pin32(r);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) *reinterpret_cast<T*>(stage + (c + i) * PITCH + row * sizeof(T)) = from_f32<T>(__uint_as_float(r[i]));
+            mx4_finish<T, EPI, 32>(p, r, res, bias, row, stage + c * PITCH, PITCH);
+            if (EPI) res.load(p, n0 + c0 + c + 32, nn - c0 - c - 32, m0 + row);
         }
         if (c0 + PASS >= nn) {
             tc_fence_before();
@@ -817,20 +959,20 @@ __device__ __forceinline__ void mx4_pair_store(const Mx4Params& p, uint32_t tm, 
             if (lane == 0) mbar_arrive_cluster(free_bar);
         }
         bar_epilogue();
-        if (p.y_vec && m_here == 128) {
+        if (p.y_vec && m_here == COLS) {
 #pragma unroll 4
             for (int i = row; i < cols * ROW; i += 128) {
                 const int n = i / ROW, piece = i % ROW;
-                *reinterpret_cast<uint4*>(static_cast<T*>(p.Y) + (n0 + c0 + n) * p.ldy + m0 + piece * PER) = *reinterpret_cast<const uint4*>(stage + n * PITCH + 16 * piece);
+                *reinterpret_cast<uint4*>(static_cast<T*>(p.Y) + (n0 + c0 + n) * p.ldy + col0 + piece * PER) = *reinterpret_cast<const uint4*>(stage + n * PITCH + 16 * piece);
             }
         } else {
             for (int n = 0; n < cols; ++n)
-                if (row < m_here) static_cast<T*>(p.Y)[(n0 + c0 + n) * p.ldy + m0 + row] = *reinterpret_cast<const T*>(stage + n * PITCH + row * sizeof(T));
+                if (row < m_here) static_cast<T*>(p.Y)[(n0 + c0 + n) * p.ldy + col0 + row] = *reinterpret_cast<const T*>(stage + n * PITCH + row * sizeof(T));
         }
     }
 }
 
-template <int ST>   // ring stages
+template <int ST, int EPI = 0>   // ring stages
 __global__ void __launch_bounds__(192, 1) us_mx4_pair_kernel(const __grid_constant__ Mx4Params p)
 {
     using S = Mx4Pair;
@@ -941,17 +1083,24 @@ __global__ void __launch_bounds__(192, 1) us_mx4_pair_kernel(const __grid_consta
         asm volatile("griddepcontrol.wait;" ::: "memory");
         uint32_t n = 0;
         for (int tile = blockIdx.x >> 1; tile < p.tiles; tile += gridDim.x >> 1, ++n) {
+            const int pair = tile / p.col_tiles, n0 = (tile - pair * p.col_tiles) * NB, nn = min(NB, p.N - n0);
+            const int64_t m0 = 128 * (int64_t)(2 * pair + rank);
+            Mx4Residual<EPI, 32> res;
+            float bias = 0.f;
+            if (EPI) {   // (on their way while the tile's products run)
+                const int64_t m = m0 + 32 * quarter + lane;
+                if (p.e.bias && m < p.M) bias = mx4_scalar(p.e.bias, p.e.bias_type, m);
+                res.load(p, n0, nn, m);
+            }
             ok = ops_wait_warp(b_done, n & 1u, 4 * kMxWait, dead);
             if (bar_any(!ok)) {   // (all four warps leave at the same place)
                 ok = false;
                 break;
             }
             tc_fence_after();
-            const int pair = tile / p.col_tiles, n0 = (tile - pair * p.col_tiles) * NB, nn = min(NB, p.N - n0);
-            const int64_t m0 = 128 * (int64_t)(2 * pair + rank);
-            if (p.y_type == kF32) mx4_pair_store<float>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
-            else if (p.y_type == kF16) mx4_pair_store<__half>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
-            else mx4_pair_store<__nv_bfloat16>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
+            if (p.y_type == kF32) mx4_pair_store<float, EPI>(p, tm, quarter, lane, m0, n0, nn, out, free_bar, res, bias);
+            else if (p.y_type == kF16) mx4_pair_store<__half, EPI>(p, tm, quarter, lane, m0, n0, nn, out, free_bar, res, bias);
+            else mx4_pair_store<__nv_bfloat16, EPI>(p, tm, quarter, lane, m0, n0, nn, out, free_bar, res, bias);
         }
     }
     if (!ok && lane == 0) {

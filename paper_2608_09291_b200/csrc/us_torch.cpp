@@ -356,22 +356,44 @@ PyObject* mx4_unpack(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// mx4_linear(X, rows, w, M, K, out, dtype, stable, stream) -> the product; rows >= 0: X holds the tiles of that many rows
+// mx4_linear(X, rows, w, M, K, out, dtype, stable, stream, bias, act, gated, residual) -> the product; rows >= 0: X holds the tiles of that many rows
 PyObject* mx4_linear(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    if (n != 9) return PyErr_Format(PyExc_TypeError, "mx4_linear takes 9 arguments");
+    if (n != 13) return PyErr_Format(PyExc_TypeError, "mx4_linear takes 13 arguments");
     HANDLE_TH_ERRORS
     const at::Tensor *X = tensor(a[0], "X"), *w = X ? tensor(a[2], "w") : nullptr;
     const int64_t rows = PyLong_AsLongLong(a[1]), M = PyLong_AsLongLong(a[3]), K = PyLong_AsLongLong(a[4]);
     if (!w || PyErr_Occurred()) return nullptr;
+    us_mx4_epilogue e = {};
+    e.act = (int32_t)PyLong_AsLong(a[10]);
+    e.gated = PyObject_IsTrue(a[11]);
+    if (PyErr_Occurred()) return nullptr;
     Place at_;
     if (!at_.enter(a[8], *X)) return nullptr;
     if (!is_mx(*w, M, K, *X)) return bad("w does not hold a matrix of this shape on X's device");
     if (rows >= 0 ? !is_mx(*X, rows, K, *X) : (!is_rows(*X) || X->size(1) != K))
         return bad("X must be a float16, bfloat16 or float32 (N, K) tensor with unit column stride, K as the weight's");
-    const int64_t N = rows >= 0 ? rows : X->size(0);
+    const int64_t N = rows >= 0 ? rows : X->size(0), cols = e.gated ? M / 2 : M;
+    if (e.gated && M % 2) return bad("a gated product needs a weight of an even number of rows: gate and up rows in turn");
+    if (a[9] != Py_None) {
+        const at::Tensor* t = tensor(a[9], "bias");
+        if (!t) return nullptr;
+        if (t->dim() != 1 || t->size(0) != M || type_of(t->scalar_type()) < 0 || !t->is_contiguous() || t->device() != X->device())
+            return bad("bias must be a contiguous (M,) tensor of float16, bfloat16 or float32 on X's device");
+        e.bias = t->data_ptr();
+        e.bias_type = type_of(t->scalar_type());
+    }
+    if (a[12] != Py_None) {
+        const at::Tensor* t = tensor(a[12], "residual");
+        if (!t) return nullptr;
+        if (!is_rows(*t) || t->size(0) != N || t->size(1) != cols || t->device() != X->device())
+            return PyErr_Format(PyExc_ValueError, "residual must be a (%lld, %lld) float tensor with unit column stride on X's device", (long long)N, (long long)cols);
+        e.residual = t->data_ptr();
+        e.residual_type = type_of(t->scalar_type());
+        e.ldr = row_stride(*t);
+    }
     at::Tensor fresh, scratch;
-    const at::Tensor* out = rows_out(a[5], a[6], rows >= 0 ? at::kHalf : X->scalar_type(), *X, N, M, &fresh);
+    const at::Tensor* out = rows_out(a[5], a[6], rows >= 0 ? at::kHalf : X->scalar_type(), *X, N, cols, &fresh);
     if (!out) return nullptr;
     const uint32_t flags = a[7] == Py_True ? US_MX4_W_STABLE : 0u;
     const int yt = type_of(out->scalar_type());
@@ -380,14 +402,14 @@ PyObject* mx4_linear(PyObject*, PyObject* const* a, Py_ssize_t n)
     us_status s;
     if (rows >= 0) {
         Py_BEGIN_ALLOW_THREADS
-        s = us_mx4_matmul(X->data_ptr(), N, w->data_ptr(), M, K, y, yt, ldy, flags, at_.stream);
+        s = us_mx4_matmul_epilogue(X->data_ptr(), N, w->data_ptr(), M, K, &e, y, yt, ldy, flags, at_.stream);
         Py_END_ALLOW_THREADS
     } else {
         const int64_t bytes = us_mx4_linear_scratch(N, M, K);
         if (bytes > 0) scratch = at::detail::empty_cuda({bytes}, at::kByte, X->device(), std::nullopt);
         Py_BEGIN_ALLOW_THREADS
-        s = us_mx4_linear(X->data_ptr(), type_of(X->scalar_type()), row_stride(*X), N, w->data_ptr(), M, K, y, yt, ldy,
-                          bytes > 0 ? scratch.data_ptr() : nullptr, bytes, flags, at_.stream);
+        s = us_mx4_linear_epilogue(X->data_ptr(), type_of(X->scalar_type()), row_stride(*X), N, w->data_ptr(), M, K, &e, y, yt, ldy,
+                                   bytes > 0 ? scratch.data_ptr() : nullptr, bytes, flags, at_.stream);
         Py_END_ALLOW_THREADS
     }
     if (s != US_OK) return fail(s, "us_mx4_linear");

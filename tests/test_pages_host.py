@@ -104,3 +104,23 @@ def test_rotary_tables(b):
                dict(head_dim=64, sections=[16, 16], pair_axis=[0] * 32), dict(head_dim=64, frequencies=[1.0] * 31), dict(head_dim=64, frequencies=[math.inf] * 32)):
         with pytest.raises(ValueError):
             b.Rotary(device="cpu", **kw)
+
+
+def _product(b, N=4, M=64, K=64, e=None, ldy=64, linear=True, y=P, **kw):
+    a = dict(bias=P, residual=P, ldr=64, bias_type=0, residual_type=0, act=2, gated=0)
+    a.update(kw)
+    s = b.us_mx4_epilogue(**a)
+    if linear:
+        return b._lib.us_mx4_linear_epilogue(P, 0, K, N, P, M, K, ctypes.byref(s), y, 0, ldy, P, 1 << 40, 0, None)
+    return b._lib.us_mx4_matmul_epilogue(P, N, P, M, K, ctypes.byref(s), y, 0, ldy, 0, None)
+
+
+@pytest.mark.parametrize("linear", [False, True])
+@pytest.mark.parametrize("kw", [dict(act=-1), dict(act=5), dict(bias_type=3), dict(bias=P + 1), dict(residual_type=-1), dict(residual=P + 1), dict(residual_type=2, residual=P + 2), dict(ldr=63),
+                                dict(gated=1, M=63), dict(gated=1, ldr=31), dict(gated=1, ldy=31), dict(ldy=63), dict(y=None), dict(M=0), dict(N=-1)])
+def test_epilogue_refuses(b, linear, kw):
+    assert _product(b, linear=linear, **kw) == INVALID
+
+
+def test_epilogue_nothing_to_do(b):
+    assert _product(b, N=0, y=None) == 0 and _product(b, N=0, y=None, linear=False) == 0
