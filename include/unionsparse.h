@@ -401,6 +401,18 @@ int64_t us_kv_attention_scratch(const us_kv* h, const us_kv_seqs* seqs, int64_t 
 us_status us_kv_attention(us_kv* h, const us_kv_seqs* seqs, int64_t N, const void* Q, int32_t type, int32_t n_heads,
                           int64_t q_token_stride, int64_t q_head_stride, float scale, int32_t causal, int32_t window, void* out,
                           int64_t o_token_stride, int64_t o_head_stride, float* lse, void* scratch, int64_t scratch_bytes, void* stream);
+/*
+ * us_kv_shared_attention: the same for sequences that share prefixes, whose keys and values are read once for all of them. prefixes describes n_seqs groups: block
+ *   table and lengths (0 or more tokens) of each one's prefix, and in cu_tokens n_seqs + 1 entries: sequences [cu[g], cu[g + 1]) of `seqs` are group g's. Sequences that are
+ *   in no group have no prefix; n_seqs = 0: none have. A token of a sequence sees its group's whole prefix and, of its sequence's own tokens (seqs: lengths and
+ *   table are of those; new tokens included), what it sees above. A sequence of length 0 may have rows: they give 0. No windows. If cu entries fall or pass the
+ *   number of sequences (US_ERR_DEVICE_INDEX), the outputs of the call may be anything. scratch: us_kv_shared_attention_scratch bytes.
+ *   Accuracy as above, where US_F16 calls of few rows are those with N n_heads / n_kv_heads <= 32 n_seqs for prefixes and sequences both.
+ */
+int64_t us_kv_shared_attention_scratch(const us_kv* h, const us_kv_seqs* prefixes, const us_kv_seqs* seqs, int64_t N, int32_t n_heads);
+us_status us_kv_shared_attention(us_kv* h, const us_kv_seqs* prefixes, const us_kv_seqs* seqs, int64_t N, const void* Q, int32_t type, int32_t n_heads,
+                                 int64_t q_token_stride, int64_t q_head_stride, float scale, int32_t causal, void* out, int64_t o_token_stride,
+                                 int64_t o_head_stride, float* lse, void* scratch, int64_t scratch_bytes, void* stream);
 us_status us_kv_last_error(void);
 us_status us_kv_destroy(us_kv* h);
 

@@ -31,7 +31,8 @@ EXPORTS = ["us_encode", "us_get_stats", "us_decode", "us_get_row_order", "us_spm
            "us_last_error", "us_debug_withhold_copy", "us_stage_timers", "us_destroy", "us_spmm_bytes", "us_launch_info", "us_launch_kernel",
            "us_mx4_bytes", "us_mx4_quantize", "us_mx4_dequantize", "us_mx4_pack", "us_mx4_unpack", "us_mx4_matmul",
            "us_mx4_linear_scratch", "us_mx4_linear", "us_mx4_matmul_epilogue", "us_mx4_linear_epilogue", "us_mx4_last_error",
-           "us_kv_create", "us_kv_append", "us_kv_read", "us_kv_attention_scratch", "us_kv_attention", "us_kv_last_error", "us_kv_destroy",
+           "us_kv_create", "us_kv_append", "us_kv_read", "us_kv_attention_scratch", "us_kv_attention", "us_kv_shared_attention_scratch",
+           "us_kv_shared_attention", "us_kv_last_error", "us_kv_destroy",
            "us_kv_fork", "us_kv_release", "us_kv_extend_scratch", "us_kv_extend", "us_kv_compact_scratch", "us_kv_compact", "us_kv_remap", "us_kv_copy_blocks",
            "us_qk_norm_rope",
            "us_status_string"]
@@ -104,6 +105,9 @@ _lib.us_kv_read.argtypes = [_vp, _seqs, _i64, _vp, _vp, _i32, _vp]
 _lib.us_kv_attention_scratch.argtypes = [_vp, _seqs, _i64, _i32]
 _lib.us_kv_attention_scratch.restype = _i64
 _lib.us_kv_attention.argtypes = [_vp, _seqs, _i64, _vp, _i32, _i32, _i64, _i64, ctypes.c_float, _i32, _i32, _vp, _i64, _i64, _vp, _vp, _i64, _vp]
+_lib.us_kv_shared_attention_scratch.argtypes = [_vp, _seqs, _seqs, _i64, _i32]
+_lib.us_kv_shared_attention_scratch.restype = _i64
+_lib.us_kv_shared_attention.argtypes = [_vp, _seqs, _seqs, _i64, _vp, _i32, _i32, _i64, _i64, ctypes.c_float, _i32, _vp, _i64, _i64, _vp, _vp, _i64, _vp]
 _lib.us_kv_last_error.argtypes = []
 _lib.us_kv_destroy.argtypes = [_vp]
 _lib.us_kv_fork.argtypes = [_vp, _vp, _seqs, _vp, _i32, _vp, _i64, _vp, _i32, _vp]
@@ -585,6 +589,16 @@ class KVCache:
         query heads) a sequence and cache head."""
         return _ext.kv_attention(self.handle, self.k_codes, q, block_table, lengths, cu_tokens, self.head_dim ** -0.5 if scale is None else scale,
                                  causal, window, out, lse, stream)
+
+    def shared_attention(self, q, prefix_table, prefix_lengths, cu_seqs, block_table, lengths, cu_tokens=None, scale=None, causal=True, out=None, lse=None,
+                         stream=None):
+        """Attention of sequences behind prefixes that groups of them share: a prefix's keys and values are read once for its group. prefix_table (groups, width)
+        and prefix_lengths (groups,) describe the prefixes, cu_seqs int32 (groups + 1,) says whose sequences are whose: [cu_seqs[g], cu_seqs[g + 1]). block_table, lengths
+        and cu_tokens are of the sequences' own tokens, the new ones included; the rest is as for `attention`.
+
+        After `KVPages.fork` of a prompt of p whole blocks: prefix_table = table[:1, :p], block_table = table[:, p:], lengths - p * block_tokens."""
+        return _ext.kv_shared_attention(self.handle, self.k_codes, q, block_table, lengths, cu_tokens, self.head_dim ** -0.5 if scale is None else scale,
+                                        causal, 0, out, lse, stream, prefix_table, prefix_lengths, cu_seqs)
 
     def copy_blocks(self, src, dst, stream=None):
         """Copies block src[i], its codes and steps, to block dst[i] (int32 tensors; dst[i] = -1: nothing). No block is twice in dst, or in dst and src."""

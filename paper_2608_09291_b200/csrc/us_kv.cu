@@ -1,8 +1,7 @@
 // The 8-bit cache's entry points: checks, launch plans.
 #include "us_kv_host.h"
-#include "us_kv_prompt.cuh"
+#include "us_kv_plan.cuh"
 
-#include <cmath>
 #include <new>
 
 namespace us {
@@ -12,7 +11,6 @@ __device__ uint32_t g_kv_err;   // the last failure that a kernel met since us_k
 
 us_status cuda(cudaError_t e) { return kv_cuda(e); }
 bool aligned(const void* p, int64_t b) { return kv_aligned(p, b); }
-int64_t size_of(int32_t t) { return t == US_F32 ? 4 : 2; }
 us_status on_device(const us_kv* h) { return kv_on_device(h); }
 bool seqs_ok(const us_kv* h, const us_kv_seqs* q, int64_t N) { return kv_seqs_ok(h, q, N); }
 KvSeqs seqs(const us_kv_seqs* q, int64_t N) { return kv_seqs(q, N); }
@@ -52,12 +50,16 @@ bool encode_map(CUtensorMap* map, void* base, const KvPool& p)
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool maps(us_kv* h)
+}  // namespace
+
+bool kv_maps(us_kv* h)
 {
     std::lock_guard<std::mutex> hold(h->lock);
     if (!h->mapped) h->mapped = encode_map(&h->k_map, h->pool.k, h->pool) && encode_map(&h->v_map, h->pool.v, h->pool);
     return h->mapped;
 }
+
+namespace {
 
 // The device that an address lies on, or -1.
 int device_of(const void* p)
@@ -67,72 +69,10 @@ int device_of(const void* p)
     else if (a.type == cudaMemoryTypeDevice) return a.device;
     return -1;
 }
-// Rows (token, head, D): every stride holds a row, and the 16-byte path's condition.
-bool strides_ok(const void* x, int32_t type, int64_t token, int64_t head, int64_t N, int64_t heads, int32_t D)
-{
-    return x && aligned(x, size_of(type)) && (N == 1 || token >= D) && (heads == 1 || head >= D) && token >= 0 && head >= 0;
-}
-bool rows_vec(const void* x, int32_t type, int64_t token, int64_t head)
-{
-    return aligned(x, 16) && token * size_of(type) % 16 == 0 && head * size_of(type) % 16 == 0;
-}
-
 template <class T>
 const void* append_kernel(int team)
 {
     return team == 32 ? (const void*)us_kv_append_kernel<T, 32> : team == 64 ? (const void*)us_kv_append_kernel<T, 64> : (const void*)us_kv_append_kernel<T, 128>;
-}
-
-// ---- attention: which kernels ----
-struct AttendPlan {
-    const void *kernel, *join;
-    int rows, stages, smem, ctas;
-    int splits;        // (prompts) of the cache's length
-    int64_t tiles;     // (prompts) row tiles, at most; 0: the kernel for few rows
-    int64_t scratch;
-};
-template <int D, bool BF16>
-AttendPlan prompt_shape(int64_t N, int64_t S, int64_t G, int64_t Hkv, int64_t longest, int sms)
-{
-    AttendPlan p = {};
-    p.kernel = (const void*)us_kv_prompt_kernel<D, BF16>;
-    p.join = (const void*)us_kv_prompt_join_kernel<D, BF16>;
-    p.smem = PrShape<D>::kSmem;
-    p.tiles = N * G / kPrRows + S;
-    // a tile's walk over the cache is split where the tiles would leave SMs idle, in parts of at least four units
-    const int64_t likely = std::max(S, (N * G + kPrRows - 1) / kPrRows) * Hkv;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({16, sms / likely, longest / (4 * kPrTile)}));
-    p.scratch = p.splits > 1 ? p.tiles * Hkv * p.splits * PrShape<D>::kPart * 4 : 0;
-    return p;
-}
-template <int D, int NT, bool BF16>
-AttendPlan attend_shape(int sms)
-{
-    using S = KvShape<D, NT>;
-    AttendPlan p = {};
-    p.kernel = (const void*)us_kv_attend_kernel<D, NT, BF16>;
-    p.join = (const void*)us_kv_join_kernel<D, NT, BF16>;
-    p.rows = S::R;
-    p.stages = std::min(S::kMaxStages, (111 * 1024 - 1024 - S::kMerge) / S::kStage);   // two CTAs an SM
-    p.smem = 1024 + p.stages * S::kStage + S::kMerge;
-    p.ctas = 2 * sms;
-    p.scratch = (int64_t)p.ctas * 2 * S::kPart * 4;
-    return p;
-}
-template <int D, int NT>
-AttendPlan attend_shape(bool bf16, int sms) { return bf16 ? attend_shape<D, NT, true>(sms) : attend_shape<D, NT, false>(sms); }
-AttendPlan attend_plan(int D, bool bf16, int64_t N, int64_t S, int64_t G, int64_t Hkv, int64_t longest, int sms)
-{
-    // Rows a cache head has on average decide. 64 sequences of 4096 tokens, 8 cache heads of 128, bf16, this kernel and the other one: 16 rows 154, 341 us, 32
-    // rows 288, 342, 40 rows 414, 343, 128 rows 1082, 349; four sequences of 32768: 32 rows 140, 170, 40 rows 191, 172. (64 of 300: 24 rows 76, 66.)
-    if (N * G > 32 * S) {
-        if (D == 128) return bf16 ? prompt_shape<128, true>(N, S, G, Hkv, longest, sms) : prompt_shape<128, false>(N, S, G, Hkv, longest, sms);
-        return bf16 ? prompt_shape<64, true>(N, S, G, Hkv, longest, sms) : prompt_shape<64, false>(N, S, G, Hkv, longest, sms);
-    }
-    // rows a cache head has on average: 8 a tile are enough for them, or 16
-    const bool few = N * G <= 8 * S;
-    if (D == 128) return few ? attend_shape<128, 1>(bf16, sms) : attend_shape<128, 2>(bf16, sms);
-    return few ? attend_shape<64, 1>(bf16, sms) : attend_shape<64, 2>(bf16, sms);
 }
 
 }  // namespace
@@ -232,76 +172,20 @@ int64_t us_kv_attention_scratch(const us_kv* h, const us_kv_seqs* q, int64_t N, 
 {
     if (!seqs_ok(h, q, N) || n_heads < 1 || n_heads % h->pool.Hkv) return -1;
     if (N == 0 || q->n_seqs == 0) return 0;
-    return attend_plan(h->pool.D, false, N, q->n_seqs, n_heads / h->pool.Hkv, h->pool.Hkv, (int64_t)q->table_width * h->pool.T, ops_sms()).scratch;
+    return attend_plan<kAlone>(h->pool.D, false, N, q->n_seqs, n_heads / h->pool.Hkv, h->pool.Hkv, (int64_t)q->table_width * h->pool.T, ops_sms()).scratch;
 }
 
 us_status us_kv_attention(us_kv* h, const us_kv_seqs* q, int64_t N, const void* Q, int32_t type, int32_t n_heads, int64_t q_token_stride,
                           int64_t q_head_stride, float scale, int32_t causal, int32_t window, void* out, int64_t o_token_stride, int64_t o_head_stride,
                           float* lse, void* scratch, int64_t scratch_bytes, void* stream)
 {
-    if (!seqs_ok(h, q, N) || n_heads < 1 || n_heads % h->pool.Hkv || window < 0 || !(scale == scale) || scale > 3e38f || scale < -3e38f) return US_ERR_INVALID_ARG;
-    if (type != US_F16 && type != US_BF16) return type == US_F32 ? US_ERR_UNSUPPORTED : US_ERR_INVALID_ARG;
-    if (N == 0 || q->n_seqs == 0) return US_OK;
-    if (!strides_ok(Q, type, q_token_stride, q_head_stride, N, n_heads, h->pool.D) || !strides_ok(out, type, o_token_stride, o_head_stride, N, n_heads, h->pool.D) ||
-        !aligned(lse, 4)) return US_ERR_INVALID_ARG;
-    us_status s = on_device(h);
-    if (s != US_OK) return s;
+    AttendArgs x = {Q, q_token_stride, q_head_stride, out, o_token_stride, o_head_stride, lse, type, n_heads, scale, causal, window};
+    us_status s = attend_check(h, q, N, x);
+    if (s != US_OK || N == 0 || q->n_seqs == 0) return s;
     const int64_t G = n_heads / h->pool.Hkv;
-    if (N * G >= (1ll << 31) - (1 << 16)) return US_ERR_UNSUPPORTED;
-    const AttendPlan pl = attend_plan(h->pool.D, type == US_BF16, N, q->n_seqs, G, h->pool.Hkv, (int64_t)q->table_width * h->pool.T, ops_sms());
+    const AttendPlan pl = attend_plan<kAlone>(h->pool.D, type == US_BF16, N, q->n_seqs, G, h->pool.Hkv, (int64_t)q->table_width * h->pool.T, ops_sms());
     if (pl.scratch > 0 && (!scratch || !aligned(scratch, 16) || scratch_bytes < pl.scratch)) return US_ERR_SCRATCH_TOO_SMALL;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (pl.tiles > 0) {
-        const int64_t blocks = pl.tiles * h->pool.Hkv * std::max(pl.splits, h->pool.D / 16);
-        if (blocks >= (1ll << 31)) return US_ERR_UNSUPPORTED;
-        KvPrompt a = {};
-        a.pool = h->pool;
-        a.seqs = seqs(q, N);
-        a.q = Q; a.q_token = q_token_stride; a.q_head = q_head_stride;
-        a.out = out; a.o_token = o_token_stride; a.o_head = o_head_stride;
-        a.lse = lse;
-        a.part = static_cast<float*>(scratch);
-        a.scale2 = (float)(std::fabs((double)scale) * 1.4426950408889634);
-        a.negative = scale < 0.f;
-        a.Hq = n_heads; a.G = (int32_t)G;
-        a.causal = causal != 0; a.window = window;
-        a.q_vec = rows_vec(Q, type, q_token_stride, q_head_stride);
-        a.o_vec = rows_vec(out, type, o_token_stride, o_head_stride);
-        a.splits = pl.splits;
-        while ((1 << a.log2_T) < h->pool.T) ++a.log2_T;
-        s = error_word(&a.pool.err);
-        if (s != US_OK) return s;
-        void* args[] = {&a};
-        cudaError_t e = ops_kernel_allow(pl.kernel, pl.smem);
-        const int threads = PrShape<128>::kThreads;
-        if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.splits)), threads, pl.smem, st, args);
-        if (e == cudaSuccess && pl.splits > 1) e = ops_launch(pl.join, dim3((unsigned)(pl.tiles * h->pool.Hkv * (h->pool.D / 16))), kPrRows, 0, st, args);
-        return cuda(e);
-    }
-    if (!maps(h)) return US_ERR_CUDA;
-    KvAttend a = {};
-    a.k_map = h->k_map; a.v_map = h->v_map;
-    a.pool = h->pool;
-    a.seqs = seqs(q, N);
-    a.q = Q; a.q_token = q_token_stride; a.q_head = q_head_stride;
-    a.out = out; a.o_token = o_token_stride; a.o_head = o_head_stride;
-    a.lse = lse;
-    a.part = static_cast<float*>(scratch);
-    a.scale2 = (float)((double)scale * 1.4426950408889634);
-    a.Hq = n_heads; a.G = (int32_t)G;
-    a.causal = causal != 0; a.window = window;
-    a.q_vec = rows_vec(Q, type, q_token_stride, q_head_stride);
-    a.stages = pl.stages;
-    a.ctas = pl.ctas;
-    while ((1 << a.log2_T) < h->pool.T) ++a.log2_T;
-    s = error_word(&a.pool.err);
-    if (s != US_OK) return s;
-    cudaError_t e = ops_kernel_allow(pl.kernel, pl.smem);
-    void* args[] = {&a};
-    if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)pl.ctas), 160, pl.smem, st, args);
-    // (an item of one unit is never cut)
-    if (e == cudaSuccess && (int64_t)q->table_width * h->pool.T > kKvTile) e = ops_launch(pl.join, dim3((unsigned)pl.ctas), 32 * kJoinWarps, 0, st, args);
-    return cuda(e);
+    return attend_run(h, seqs(q, N), x, pl, KvRows{}, scratch, static_cast<cudaStream_t>(stream));
 }
 
 us_status us_kv_last_error(void)

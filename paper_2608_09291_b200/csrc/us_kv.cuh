@@ -18,7 +18,12 @@ struct KvSeqs {
     const int32_t* cu;        // S + 1 sums of the new tokens of the sequences before, or nullptr: one each
     int32_t S, width;
     int64_t N;                // new tokens
+    const int32_t* groups;    // (kGroups) S + 1 sums of the sequences of the groups before: a group is one long row of its sequences' new tokens
+    int32_t members;          // sequences of all groups
 };
+// What attention is part of: itself (kAlone); of attention behind shared prefixes, the groups over their prefixes, whose sums go to rows (kGroups), or the sequences over
+// their own tokens, whose sums are joined with those (kOwn).
+enum { kAlone = 0, kGroups = 1, kOwn = 2 };
 
 struct KvPool {
     int8_t *k, *v;
@@ -33,14 +38,23 @@ struct KvSeq {
 };
 // Sequence s with everything that memory depends on brought into range; `wrong`: something was not. (An empty sequence may have rows: those
 // of a padded batch.)
+template <int MODE = kAlone>
 __device__ __forceinline__ KvSeq kv_seq(const KvSeqs& q, const KvPool& p, int s, bool& wrong)
 {
     KvSeq r;
     const int64_t most = (int64_t)q.width * p.T;
     const int32_t len = __ldcg(q.lengths + s);
     int64_t a = s, b = (int64_t)s + 1;
-    if (q.cu) { a = __ldcg(q.cu + s); b = __ldcg(q.cu + s + 1); }
-    wrong = len < 0 || len > most || a < 0 || b < a || b > q.N || (len > 0 && b - a > len);
+    bool off = false;
+    if (MODE == kGroups) {
+        a = __ldcg(q.groups + s);
+        b = __ldcg(q.groups + s + 1);
+        off = a < 0 || b < a || b > q.members;
+        a = max((int64_t)0, min(a, (int64_t)q.members));
+        b = max(a, min(b, (int64_t)q.members));
+    }
+    if (q.cu) { a = __ldcg(q.cu + a); b = __ldcg(q.cu + b); }
+    wrong = off || len < 0 || len > most || a < 0 || b < a || b > q.N || (MODE != kGroups && len > 0 && b - a > len);
     r.len = (int32_t)max((int64_t)0, min((int64_t)len, most));
     r.first = max((int64_t)0, min(a, q.N));
     r.n = (int32_t)max((int64_t)0, min(b, q.N) - r.first);
@@ -312,6 +326,17 @@ __global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int
 // side: their chains of products overlap), with sums of their own that are joined at an item's end.
 // Bound by memory: 64 sequences of up to 8192 tokens, 64/8 heads, bf16: 98 us inside a graph, 5.7 TB/s (109 called); one of 131072 tokens, fp16:
 // 55 us, 4.9 TB/s (59 called).
+// The sums over a prefix, for each (new token, query head): D sums, then their maximum and sum; kOwn: for the sequences that are in a group.
+struct KvRows {
+    float* at;
+    const int32_t* groups;
+    int32_t n_groups, pitch;
+};
+template <int MODE>
+__device__ __forceinline__ bool kv_has_prefix(const KvRows& r, int s, int len)
+{
+    return MODE == kOwn && len > 0 && s >= __ldcg(r.groups) && s < __ldcg(r.groups + r.n_groups);
+}
 constexpr int kKvTile = 128;
 constexpr int kKvStart = 4;   // what an item's queries, sums and output cost, in units
 struct KvAttend {
@@ -331,6 +356,7 @@ struct KvAttend {
     int32_t stages;
     int32_t ctas;
     int32_t log2_T;
+    KvRows rows;
 };
 
 struct KvItem {
@@ -353,11 +379,11 @@ __device__ __forceinline__ KvItem kv_item(const KvAttend& a, const KvSeq& seq)
     r.tiles = max(1, (r.seq.len + kKvTile - 1) / kKvTile - r.t_lo);
     return r;
 }
-template <int R>
+template <int R, int MODE>
 __device__ __forceinline__ KvItem kv_item(const KvAttend& a, int s)
 {
     bool wrong;
-    return kv_item<R>(a, kv_seq(a.seqs, a.pool, s, wrong));
+    return kv_item<R>(a, kv_seq<MODE>(a.seqs, a.pool, s, wrong));
 }
 
 // The units of all items in a row, cut in equal shares: CTA c has [begin(c), begin(c + 1)).
@@ -379,7 +405,7 @@ struct KvRange {
     long long in_seq;     // u0 from its first unit
     KvItem item;          // of that sequence
 };
-template <int R>
+template <int R, int MODE>
 __device__ __forceinline__ KvRange kv_range(const KvAttend& a, int cta, int lane, bool report)
 {
     KvRange r;
@@ -391,7 +417,7 @@ __device__ __forceinline__ KvRange kv_range(const KvAttend& a, int cta, int lane
         c = 0;
         if (base + lane < a.seqs.S) {
             bool wrong;
-            mine = kv_seq(a.seqs, a.pool, base + lane, wrong);
+            mine = kv_seq<MODE>(a.seqs, a.pool, base + lane, wrong);
             any |= wrong;
             const KvItem it = kv_item<R>(a, mine);
             c = (long long)it.row_tiles * a.pool.Hkv * it.cost();
@@ -500,6 +526,16 @@ __device__ __forceinline__ float kv_lse(float m, float l) { return l == 0.f ? -I
 // 2^(m - base) for a part with this maximum and sum; 0 for one that saw nothing
 __device__ __forceinline__ float kv_weight(float m, float l, float base) { return m == -INFINITY && l == 0.f ? 0.f : exp2_fast(m - base); }
 
+// Sums with maximum `big` (sum, acc) and another part's together.
+__device__ __forceinline__ void kv_add_part(float& big, float& sum, float& acc, float2 stat, float x)
+{
+    const float top = fmaxf(big, stat.x), base = top == -INFINITY ? 0.f : top;
+    const float e = kv_weight(big, sum, base), f = kv_weight(stat.x, stat.y, base);
+    sum = e * sum + f * stat.y;   // (a part that is NaN has no maximum, and so no weight: its NaN comes from here)
+    acc = (e == 0.f ? 0.f : e * acc) + (f == 0.f ? 0.f : f * x);
+    big = top;
+}
+
 template <int D, int NT>
 struct KvShape {
     static constexpr int R = 8 * NT;
@@ -511,7 +547,7 @@ struct KvShape {
     static constexpr int kPart = R * (D + 2);                 // floats of a part
 };
 
-template <int D, int NT, bool BF16>
+template <int D, int NT, bool BF16, int MODE = kAlone>
 __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_constant__ KvAttend a)
 {
     using S = KvShape<D, NT>;
@@ -534,7 +570,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const KvPool& p = a.pool;
-    const KvRange range = kv_range<R>(a, blockIdx.x, lane, warp == 0);
+    const KvRange range = kv_range<R, MODE>(a, blockIdx.x, lane, warp == 0);
     long long left = range.u1 - range.u0;
     bool ok = true;
     int stage = 0;
@@ -551,7 +587,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
         item = 0;
         do {
             if (++s >= a.seqs.S) { left = 0; return; }
-            it = kv_item<R>(a, s);
+            it = kv_item<R, MODE>(a, s);
         } while (it.rows == 0);
     };
     if (warp == 4) {
@@ -927,12 +963,20 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
             const bool whole = n == it.tiles;
             float* part = a.part + ((int64_t)blockIdx.x * 2 + (tile == 0 ? 1 : 0)) * S::kPart;   // 1: the item begins here
             const int rows = min(R, it.rows - row0);
+            const bool joined = whole && kv_has_prefix<MODE>(a.rows, s, it.seq.len);
             for (int i = threadIdx.x; i < rows * D; i += 128) {
                 const int r = i / D, d = i - r * D;
-                const float big = stats[4 * R + r].x, sum = stats[4 * R + r].y;
-                const float acc = sums[r * S::kPitch + (d % (D / 8)) * 8 + d / (D / 8)];
+                float big = stats[4 * R + r].x, sum = stats[4 * R + r].y;
+                float acc = sums[r * S::kPitch + (d % (D / 8)) * 8 + d / (D / 8)];
                 if (whole) {
                     const int tok = (row0 + r) / a.G, qh = h * a.G + (row0 + r) - tok * a.G;
+                    float* row = MODE == kAlone ? nullptr : a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+                    if (MODE == kGroups) {
+                        row[d] = acc;
+                        if (d == 0) *reinterpret_cast<float2*>(row + D) = make_float2(big, sum);
+                        continue;
+                    }
+                    if (MODE == kOwn && joined) kv_add_part(big, sum, acc, __ldcg(reinterpret_cast<const float2*>(row + D)), __ldcg(row + d));
                     o_put<BF16>(a.out, (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + d, sum == 0.f ? 0.f : acc / sum);
                     if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(big, sum);
                 } else {
@@ -966,7 +1010,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
 // Every block waits for the kernel before, those without a part, too: what follows in the stream waits for this grid alone, so this
 // grid may not end before the sums and outputs of the other one are there.
 constexpr int kJoinWarps = 4, kJoinFew = 4;
-template <int D, int NT, bool BF16>
+template <int D, int NT, bool BF16, int MODE = kAlone>
 __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __grid_constant__ KvAttend a)
 {
     using S = KvShape<D, NT>;
@@ -974,18 +1018,19 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
     __shared__ float2 stat[kJoinWarps];
     __shared__ float accs[kJoinWarps][D];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, me = blockIdx.x;
-    const KvRange range = kv_range<R>(a, me, lane, false);
+    const KvRange range = kv_range<R, MODE>(a, me, lane, false);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     bool waited = false;
     auto wait = [&]() {
         if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
         waited = true;
     };
-    auto join = [&](const KvItem& it, int item, int c0, int c1) {
+    auto join = [&](const KvItem& it, int s, int item, int c0, int c1) {
         if (c1 - c0 < kJoinFew && me != c0) return;
         wait();
         const int h = item % a.pool.Hkv, row0 = item / a.pool.Hkv * R, rows = min(R, it.rows - row0);
         const int np = c1 - c0 + 1;
+        const bool joined = kv_has_prefix<MODE>(a.rows, s, it.seq.len);
         if (np <= kJoinFew) {
 #pragma unroll 1
             for (int r0 = warp; r0 < rows; r0 += 2 * kJoinWarps) {   // two rows a warp at a time: all loads first
@@ -1023,6 +1068,23 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
                         for (int i = 0; i < C; ++i) y[i] += e == 0.f ? 0.f : e * x[b][k][i];
                     }
                     const int tok = (row0 + r) / a.G, qh = h * a.G + (row0 + r) - tok * a.G;
+                    float* row = MODE == kAlone ? nullptr : a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+                    if (MODE == kGroups) {
+#pragma unroll
+                        for (int i = 0; i < C; ++i) row[lane + 32 * i] = y[i];
+                        if (lane == 0) *reinterpret_cast<float2*>(row + D) = make_float2(all, total);
+                        continue;
+                    }
+                    if (MODE == kOwn && joined) {
+                        const float2 stat = __ldcg(reinterpret_cast<const float2*>(row + D));
+                        const float big = all, sum = total;
+#pragma unroll
+                        for (int i = 0; i < C; ++i) {
+                            all = big;
+                            total = sum;
+                            kv_add_part(all, total, y[i], stat, __ldcg(row + lane + 32 * i));
+                        }
+                    }
                     const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
                     for (int i = 0; i < C; ++i) o_put<BF16>(a.out, (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + lane + 32 * i, total == 0.f ? 0.f : y[i] * inv);
@@ -1085,6 +1147,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
                     y += e == 0.f ? 0.f : e * accs[k][d];
                 }
                 const int tok = (row0 + row) / a.G, qh = h * a.G + (row0 + row) - tok * a.G;
+                float* own = MODE == kAlone ? nullptr : a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+                if (MODE == kGroups) {
+                    own[d] = y;
+                    if (d == 0) *reinterpret_cast<float2*>(own + D) = make_float2(all, total);
+                    continue;
+                }
+                if (MODE == kOwn && joined) kv_add_part(all, total, y, __ldcg(reinterpret_cast<const float2*>(own + D)), __ldcg(own + d));
                 o_put<BF16>(a.out, (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + d, total == 0.f ? 0.f : y / total);
                 if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(all, total);
             }
@@ -1100,7 +1169,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
             const int item = kv_div(range.in_seq, it.cost());
             const long long first = start + (long long)item * it.cost() + kKvStart;
             if (first < range.u0) {
-                join(it, item, range.shares.owner(first), range.shares.owner(first + it.tiles - 1));
+                join(it, s, item, range.shares.owner(first), range.shares.owner(first + it.tiles - 1));
                 if (first + it.tiles >= range.u1) return;
             }
         }
@@ -1109,12 +1178,12 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
         while (start + units <= range.u1 - 1) {
             start += units;
             if (++s >= a.seqs.S) return;
-            it = kv_item<R>(a, s);
+            it = kv_item<R, MODE>(a, s);
             units = (long long)it.row_tiles * a.pool.Hkv * it.cost();
         }
         const int item = kv_div(range.u1 - 1 - start, it.cost());
         const long long first = start + (long long)item * it.cost() + kKvStart, end = first + it.tiles;
-        if (first >= range.u0 && first < range.u1 && end > range.u1) join(it, item, me, range.shares.owner(end - 1));
+        if (first >= range.u0 && first < range.u1 && end > range.u1) join(it, s, item, me, range.shares.owner(end - 1));
     };
     if (range.u0 < range.u1) walk();
     wait();

@@ -41,6 +41,7 @@ struct KvPrompt {
     int32_t q_vec, o_vec;
     int32_t log2_T;
     int32_t splits;
+    KvRows rows;
 };
 
 template <int D>
@@ -96,6 +97,7 @@ struct PrItem {
     KvSeq seq;
     int s, row0, rows;
 };
+template <int MODE>
 __device__ __forceinline__ bool pr_item(const KvPrompt& a, uint32_t index, int lane, PrItem& it, bool report)
 {
     uint32_t before = 0;
@@ -105,7 +107,7 @@ __device__ __forceinline__ bool pr_item(const KvPrompt& a, uint32_t index, int l
         KvSeq mine = {0, 0, 0};
         if (base + lane < a.seqs.S) {
             bool wrong;
-            mine = kv_seq(a.seqs, a.pool, base + lane, wrong);
+            mine = kv_seq<MODE>(a.seqs, a.pool, base + lane, wrong);
             any |= wrong;
             cnt = ((uint32_t)mine.n * (uint32_t)a.G + kPrRows - 1) / kPrRows;
         }
@@ -142,7 +144,7 @@ __device__ __forceinline__ void pr_units(const KvPrompt& a, const PrItem& it, in
     u1 = hi > lo ? (hi + kPrTile - 1) / kPrTile : u0;
 }
 
-template <int D, bool BF16>
+template <int D, bool BF16, int MODE = kAlone>
 __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(const __grid_constant__ KvPrompt a)
 {
     using S = PrShape<D>;
@@ -186,7 +188,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
     const int split = (int)(blockIdx.x % a.splits), h = (int)(blockIdx.x / a.splits) % p.Hkv;
     const uint32_t index = blockIdx.x / ((unsigned)a.splits * p.Hkv);
     PrItem it;
-    const bool have = pr_item(a, index, lane, it, threadIdx.x < 32);
+    const bool have = pr_item<MODE>(a, index, lane, it, threadIdx.x < 32);
     bool ok = true;
     int u0 = 0, u1 = 0;
     if (have) {
@@ -405,11 +407,26 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             tc_fence_after();
         }
         if (qi < nq && ok) {
-            const float back = exp2_fast(-lead), inv = l == 0.f ? 0.f : back / l;
+            const float back = exp2_fast(-lead);
+            // (kGroups, kOwn: the row's sums over a prefix)
+            float* row = MODE == kAlone ? nullptr : a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+            float keep = back, more = 0.f;   // factors of the sums here and there
+            if (MODE == kOwn && a.splits == 1 && real && kv_has_prefix<MODE>(a.rows, it.s, it.seq.len)) {
+                const float2 stat = __ldcg(reinterpret_cast<const float2*>(row + D));
+                const float top = fmaxf(m, stat.x), base = top == -INFINITY ? 0.f : top, e = kv_weight(m, l, base);
+                more = kv_weight(stat.x, stat.y, base);
+                l = e * l + more * stat.y;
+                keep *= e;
+                m = top;
+            }
+            const float inv = l == 0.f ? 0.f : keep / l;
+            if (MODE == kOwn) more = l == 0.f ? 0.f : more / l;
             float* part = a.part + (((int64_t)index * p.Hkv + h) * a.splits + split) * S::kPart;
             if (real && a.splits > 1) {
                 part[kPrRows * D + local] = m;
                 part[kPrRows * D + kPrRows + local] = l;
+            } else if (MODE == kGroups) {
+                if (real) *reinterpret_cast<float2*>(row + D) = make_float2(m, l);
             } else if (real && a.lse) {
                 a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(m, l);
             }
@@ -433,10 +450,27 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                             make_float4(__uint_as_float(x[4 * i]) * back, __uint_as_float(x[4 * i + 1]) * back, __uint_as_float(x[4 * i + 2]) * back, __uint_as_float(x[4 * i + 3]) * back);
                     continue;
                 }
+                if (MODE == kGroups) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        *reinterpret_cast<float4*>(row + 32 * c + 4 * i) =
+                            make_float4(__uint_as_float(x[4 * i]) * back, __uint_as_float(x[4 * i + 1]) * back, __uint_as_float(x[4 * i + 2]) * back, __uint_as_float(x[4 * i + 3]) * back);
+                    continue;
+                }
+                if (MODE == kOwn) {   // (a factor of 0 leaves sums out, whatever they are; l is NaN where a part is)
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const float4 o = more == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : __ldcg(reinterpret_cast<const float4*>(row + 32 * c + i));
+                        const float z[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[i + k] = __float_as_uint((inv == 0.f ? 0.f : __uint_as_float(x[i + k]) * inv) + (more == 0.f ? 0.f : z[k] * more));
+                    }
+                }
                 uint32_t y[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float v0 = l == 0.f ? 0.f : __uint_as_float(x[2 * i]) * inv, v1 = l == 0.f ? 0.f : __uint_as_float(x[2 * i + 1]) * inv;
+                    const float v0 = l == 0.f ? 0.f : MODE == kOwn ? __uint_as_float(x[2 * i]) : __uint_as_float(x[2 * i]) * inv;
+                    const float v1 = l == 0.f ? 0.f : MODE == kOwn ? __uint_as_float(x[2 * i + 1]) : __uint_as_float(x[2 * i + 1]) * inv;
                     if (BF16) {
                         const __nv_bfloat162 b = __floats2bfloat162_rn(v0, v1);
                         y[i] = *reinterpret_cast<const uint32_t*>(&b);
@@ -623,7 +657,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
 }
 
 // Joins the parts of a row tile that was split over the cache's length: a thread a row, 16 of D a block.
-template <int D, bool BF16>
+template <int D, bool BF16, int MODE = kAlone>
 __global__ void __launch_bounds__(kPrRows) us_kv_prompt_join_kernel(const __grid_constant__ KvPrompt a)
 {
     using S = PrShape<D>;
@@ -631,7 +665,7 @@ __global__ void __launch_bounds__(kPrRows) us_kv_prompt_join_kernel(const __grid
     const uint32_t u = blockIdx.x / (D / 16), index = u / (uint32_t)a.pool.Hkv;
     const int h = (int)(u - index * a.pool.Hkv);
     PrItem it;
-    const bool have = pr_item(a, index, lane, it, false);   // (lengths and token counts: complete before the kernel that left the parts went past its wait)
+    const bool have = pr_item<MODE>(a, index, lane, it, false);   // (lengths and token counts: complete before the kernel that left the parts went past its wait)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (!have || local >= it.rows) return;
@@ -657,6 +691,28 @@ __global__ void __launch_bounds__(kPrRows) us_kv_prompt_join_kernel(const __grid
         }
     }
     const int r = it.row0 + local, tok = r / a.G, qh = h * a.G + r - tok * a.G;
+    if (MODE != kAlone) {
+        float* row = a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+        if (MODE == kGroups) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(row + 4 * (c0 + i)) = acc[i];
+            if (c0 == 0) *reinterpret_cast<float2*>(row + D) = make_float2(big, sum);
+            return;
+        }
+        if (kv_has_prefix<MODE>(a.rows, it.s, it.seq.len)) {
+            const float2 stat = __ldcg(reinterpret_cast<const float2*>(row + D));
+            const float own = big, own_sum = sum;
+            float z[16] = {acc[0].x, acc[0].y, acc[0].z, acc[0].w, acc[1].x, acc[1].y, acc[1].z, acc[1].w, acc[2].x, acc[2].y, acc[2].z, acc[2].w, acc[3].x, acc[3].y, acc[3].z, acc[3].w};
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                big = own;
+                sum = own_sum;
+                kv_add_part(big, sum, z[i], stat, __ldcg(row + 4 * c0 + i));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] = make_float4(z[4 * i], z[4 * i + 1], z[4 * i + 2], z[4 * i + 3]);
+        }
+    }
     const int64_t at = (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + 4 * c0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {

@@ -1,0 +1,85 @@
+// Attention of sequences that share prefixes: entry points.
+//
+// A softmax over a prefix and own tokens is the join of two: for each query and head, sums relative to a maximum over either. The sequences of a group read their
+// prefix as one long row of queries, so its keys and values come from memory once for all of them (and their products fill the tensor cores'
+// tiles); the own tokens are read as ever, and what writes an output joins the two.
+#include "us_kv_plan.cuh"
+
+namespace us {
+namespace {
+
+struct SharedPlan {
+    AttendPlan groups, own;
+    int64_t rows, first, bytes;   // bytes of the rows; where the own part's scratch begins; in all
+};
+int64_t pitch(const us_kv* h) { return h->pool.D + 4; }
+int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
+SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q, int64_t N, int32_t heads, bool bf16)
+{
+    SharedPlan r = {};
+    const int64_t G = heads / h->pool.Hkv, T = h->pool.T;
+    const int sms = ops_sms();
+    r.own = attend_plan<kOwn>(h->pool.D, bf16, N, q->n_seqs, G, h->pool.Hkv, q->table_width * T, sms);
+    if (p->n_seqs > 0) {
+        r.groups = attend_plan<kGroups>(h->pool.D, bf16, N, p->n_seqs, G, h->pool.Hkv, p->table_width * T, sms);
+        r.rows = N * heads * pitch(h) * 4;
+    }
+    r.first = up16(r.rows) + up16(r.groups.scratch);
+    r.bytes = r.first + r.own.scratch;
+    return r;
+}
+// The prefixes: cu_tokens has the groups' sequences.
+bool groups_ok(const us_kv* h, const us_kv_seqs* p)
+{
+    if (!p || p->n_seqs < 0) return false;
+    if (p->n_seqs == 0) return true;
+    return p->cu_tokens && kv_seqs_ok(h, p, 1);
+}
+bool shared_ok(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q, int64_t N, int32_t heads)
+{
+    return kv_seqs_ok(h, q, N) && groups_ok(h, p) && heads >= 1 && heads % h->pool.Hkv == 0;
+}
+
+}  // namespace
+}  // namespace us
+
+using namespace us;
+
+int64_t us_kv_shared_attention_scratch(const us_kv* h, const us_kv_seqs* prefixes, const us_kv_seqs* q, int64_t N, int32_t n_heads)
+{
+    if (!shared_ok(h, prefixes, q, N, n_heads)) return -1;
+    if (N == 0 || q->n_seqs == 0) return 0;
+    return shared_plan(h, prefixes, q, N, n_heads, false).bytes;
+}
+
+us_status us_kv_shared_attention(us_kv* h, const us_kv_seqs* prefixes, const us_kv_seqs* q, int64_t N, const void* Q, int32_t type, int32_t n_heads,
+                                 int64_t q_token_stride, int64_t q_head_stride, float scale, int32_t causal, void* out, int64_t o_token_stride, int64_t o_head_stride,
+                                 float* lse, void* scratch, int64_t scratch_bytes, void* stream)
+{
+    if (!shared_ok(h, prefixes, q, N, n_heads)) return US_ERR_INVALID_ARG;
+    if (prefixes->n_seqs == 0)   // (nobody shares anything)
+        return us_kv_attention(h, q, N, Q, type, n_heads, q_token_stride, q_head_stride, scale, causal, 0, out, o_token_stride, o_head_stride, lse, scratch, scratch_bytes, stream);
+    AttendArgs x = {Q, q_token_stride, q_head_stride, out, o_token_stride, o_head_stride, lse, type, n_heads, scale, causal, 0};
+    us_status s = attend_check(h, q, N, x);
+    if (s != US_OK || N == 0 || q->n_seqs == 0) return s;
+    const SharedPlan pl = shared_plan(h, prefixes, q, N, n_heads, type == US_BF16);
+    if (pl.bytes > 0 && (!scratch || !kv_aligned(scratch, 16) || scratch_bytes < pl.bytes)) return US_ERR_SCRATCH_TOO_SMALL;
+    uint8_t* mem = static_cast<uint8_t*>(scratch);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    KvRows rows = {};
+    rows.pitch = (int32_t)pitch(h);
+    rows.at = static_cast<float*>(scratch);
+    rows.groups = prefixes->cu_tokens;
+    rows.n_groups = prefixes->n_seqs;
+    KvSeqs g = kv_seqs(prefixes, N);
+    g.cu = q->cu_tokens;
+    g.groups = prefixes->cu_tokens;
+    g.members = q->n_seqs;
+    AttendArgs y = x;
+    y.causal = 0;
+    y.out = nullptr;
+    y.lse = nullptr;
+    s = attend_run(h, g, y, pl.groups, rows, mem + up16(pl.rows), st);
+    if (s != US_OK) return s;
+    return attend_run(h, kv_seqs(q, N), x, pl.own, rows, mem + pl.first, st);
+}

@@ -523,11 +523,11 @@ PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// kv_attention(handle, pool, q, table, lengths, cu, scale, causal, window, out, lse, stream) -> out
-PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+// kv_attention(handle, pool, q, table, lengths, cu, scale, causal, window, out, lse, stream) -> out;
+// kv_shared_attention(..., stream, prefix_table, prefix_lengths, cu_seqs) -> out
+PyObject* attention(PyObject* const* a, bool shared)
 {
-    if (n != 12) return PyErr_Format(PyExc_TypeError, "kv_attention takes 12 arguments");
-    HANDLE_TH_ERRORS
+    const char* where = shared ? "us_kv_shared_attention" : "us_kv_attention";
     void* h = a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]);
     const double scale = PyFloat_AsDouble(a[6]);
     const int causal = PyObject_IsTrue(a[7]);
@@ -535,15 +535,19 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
     if (PyErr_Occurred()) return nullptr;
     const at::Tensor *pool = tensor(a[1], "pool"), *Q = pool ? tensor(a[2], "q") : nullptr;
     if (!Q) return nullptr;
-    if (!h) return fail(US_ERR_INVALID_ARG, "us_kv_attention");
+    if (!h) return fail(US_ERR_INVALID_ARG, where);
     Place at_;
     if (!at_.enter(a[11], *pool)) return nullptr;
     if (!is_heads(*Q, pool->size(3), *pool) || Q->scalar_type() == at::kFloat || Q->size(1) < 1 || Q->size(1) % pool->size(1) || Q->size(1) >= (1ll << 31))
         return bad("q must be a float16 or bfloat16 (N, n_heads, head_dim) tensor, n_heads a multiple of n_kv_heads, with unit last stride on the cache's device");
     if (window < 0 || window > 0x7FFFFFFF) return bad("window must be 0 (none) or a number of tokens");
     const int64_t N = Q->size(0), H = Q->size(1), D = Q->size(2);
-    us_kv_seqs q;
+    us_kv_seqs q, p = {};
     if (!take_seqs(a[3], a[4], a[5], N, *pool, &q)) return nullptr;
+    if (shared) {
+        if (a[14] == Py_None) return bad("cu_seqs must be a contiguous int32 tensor with one entry more than there are prefixes, on the cache's device");
+        if (!take_seqs(a[12], a[13], a[14], -1, *pool, &p)) return nullptr;
+    }
     at::Tensor fresh, scratch;
     const at::Tensor* out = &fresh;
     if (a[9] == Py_None) {
@@ -563,17 +567,35 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
             return bad("lse must be a contiguous float32 (N, n_heads) tensor on the cache's device");
         lse = l->data_ptr();
     }
-    const int64_t bytes = us_kv_attention_scratch(static_cast<us_kv*>(h), &q, N, (int32_t)H);
-    if (bytes < 0) return fail(US_ERR_INVALID_ARG, "us_kv_attention");
+    us_kv* cache = static_cast<us_kv*>(h);
+    const int64_t bytes = shared ? us_kv_shared_attention_scratch(cache, &p, &q, N, (int32_t)H) : us_kv_attention_scratch(cache, &q, N, (int32_t)H);
+    if (bytes < 0) return fail(US_ERR_INVALID_ARG, where);
     if (bytes > 0) scratch = at::detail::empty_cuda({bytes}, at::kByte, pool->device(), std::nullopt);
+    void* mem = bytes > 0 ? scratch.data_ptr() : nullptr;
     us_status s;
     Py_BEGIN_ALLOW_THREADS
-    s = us_kv_attention(static_cast<us_kv*>(h), &q, N, Q->data_ptr(), type_of(Q->scalar_type()), (int32_t)H, token_stride(*Q), head_stride(*Q), (float)scale,
-                        causal, (int32_t)window, out->data_ptr(), token_stride(*out), head_stride(*out), static_cast<float*>(lse),
-                        bytes > 0 ? scratch.data_ptr() : nullptr, bytes, at_.stream);
+    if (shared)
+        s = us_kv_shared_attention(cache, &p, &q, N, Q->data_ptr(), type_of(Q->scalar_type()), (int32_t)H, token_stride(*Q), head_stride(*Q), (float)scale, causal,
+                                   out->data_ptr(), token_stride(*out), head_stride(*out), static_cast<float*>(lse), mem, bytes, at_.stream);
+    else
+        s = us_kv_attention(cache, &q, N, Q->data_ptr(), type_of(Q->scalar_type()), (int32_t)H, token_stride(*Q), head_stride(*Q), (float)scale, causal, (int32_t)window,
+                            out->data_ptr(), token_stride(*out), head_stride(*out), static_cast<float*>(lse), mem, bytes, at_.stream);
     Py_END_ALLOW_THREADS
-    if (s != US_OK) return fail(s, "us_kv_attention");
+    if (s != US_OK) return fail(s, where);
     return give(a[9], std::move(fresh));
+}
+PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 12) return PyErr_Format(PyExc_TypeError, "kv_attention takes 12 arguments");
+    HANDLE_TH_ERRORS
+    return attention(a, false);
+    END_HANDLE_TH_ERRORS
+}
+PyObject* kv_shared_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 15) return PyErr_Format(PyExc_TypeError, "kv_shared_attention takes 15 arguments");
+    HANDLE_TH_ERRORS
+    return attention(a, true);
     END_HANDLE_TH_ERRORS
 }
 
@@ -854,6 +876,7 @@ PyMethodDef methods[] = {
     {"kv_append", fast(kv_append), METH_FASTCALL, nullptr},
     {"kv_read", fast(kv_read), METH_FASTCALL, nullptr},
     {"kv_attention", fast(kv_attention), METH_FASTCALL, nullptr},
+    {"kv_shared_attention", fast(kv_shared_attention), METH_FASTCALL, nullptr},
     {"kv_copy_blocks", fast(kv_copy_blocks), METH_FASTCALL, nullptr},
     {"kv_fork", fast(kv_fork), METH_FASTCALL, nullptr},
     {"kv_release", fast(kv_release), METH_FASTCALL, nullptr},

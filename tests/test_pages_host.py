@@ -124,3 +124,32 @@ def test_epilogue_refuses(b, linear, kw):
 
 def test_epilogue_nothing_to_do(b):
     assert _product(b, N=0, y=None) == 0 and _product(b, N=0, y=None, linear=False) == 0
+
+
+def _shared(b, h, prefixes=True, seqs=True, N=3, Q=P, t=0, heads=8, qt=1024, scale=0.1, out=P, scratch=P, size=1 << 40, pre=None, **kw):
+    a = dict(block_table=P, table_stride=10, lengths=P, cu_tokens=None, n_seqs=3, table_width=10)
+    a.update(kw)
+    c = dict(block_table=P, table_stride=10, lengths=P, cu_tokens=P, n_seqs=2, table_width=10)
+    c.update(pre or {})
+    s, p = ctypes.byref(b.us_kv_seqs(**a)) if seqs else None, ctypes.byref(b.us_kv_seqs(**c)) if prefixes else None
+    return (b._lib.us_kv_shared_attention(h, p, s, N, Q, t, heads, qt, 128, scale, 1, out, 1024, 128, None, scratch, size, None),
+            b._lib.us_kv_shared_attention_scratch(h, p, s, N, heads))
+
+
+@pytest.mark.parametrize("kw", [dict(prefixes=False), dict(seqs=False), dict(pre=dict(cu_tokens=None)), dict(pre=dict(cu_tokens=P + 1)), dict(pre=dict(n_seqs=-1)), dict(pre=dict(block_table=None)),
+                                dict(pre=dict(lengths=None)), dict(pre=dict(table_width=0)), dict(pre=dict(table_stride=3)), dict(pre=dict(table_width=1 << 25)), dict(n_seqs=4), dict(heads=7),
+                                dict(heads=0), dict(block_table=None), dict(N=-1)])
+def test_shared_attention_refuses(b, h, kw):
+    assert _shared(b, h, **kw) == (INVALID, -1)
+
+
+@pytest.mark.parametrize("kw,st", [(dict(Q=None), INVALID), (dict(out=None), INVALID), (dict(t=2), 4), (dict(t=5), INVALID), (dict(qt=100), INVALID), (dict(scale=math.nan), INVALID),
+                                   (dict(scratch=None), TOO_SMALL), (dict(scratch=P + 4), TOO_SMALL), (dict(size=3 * 8 * 132 * 4), TOO_SMALL)])
+def test_shared_attention_refuses_data(b, h, kw, st):
+    got, need = _shared(b, h, **kw)
+    assert got == st and need > 3 * 8 * 130 * 4
+
+
+def test_shared_attention_nothing_to_do(b, h):
+    assert _shared(b, h, N=0, n_seqs=0, block_table=None, lengths=None, Q=None, out=None, scratch=None, size=0) == (0, 0)
+    assert _shared(b, None) == (INVALID, -1)
