@@ -9,7 +9,7 @@ __device__ uint32_t g_mx4_err;   // whether a bounded wait has run out since us_
 
 struct Plan {
     const void* kernel;
-    int nb, split, col_tiles, stages, cluster;
+    int nb, split, col_tiles, stages, cluster, threads;
     int64_t smem, tiles, blocks;
     bool fuse;
 };
@@ -56,10 +56,12 @@ Plan plan(int64_t N, int64_t M, int64_t K, bool can_fuse, int sms, int epi = 0)
     else if (p.nb == 128) shape<128, false>(&p, slice, p.tiles * p.split > sms ? kHalfSm : kWholeSm, epi);
     p.blocks = p.tiles * p.split;
     p.cluster = p.split;
+    p.threads = 192;
     if (p.nb == 256) {   // pairs of blocks that walk over pairs of tiles
-        p.kernel = epi == 2 ? (const void*)us_mx4_pair_kernel<Mx4Pair::kStages, 2> : epi == 1 ? (const void*)us_mx4_pair_kernel<Mx4Pair::kStages, 1> :
-                                                                                     (const void*)us_mx4_pair_kernel<Mx4Pair::kStages>;
-        p.smem = Mx4Pair::kSmem;
+        p.kernel = epi == 2 ? (const void*)us_mx4_pair_kernel<Mx4Pair::kEpiStages, 2> : epi == 1 ? (const void*)us_mx4_pair_kernel<Mx4Pair::kEpiStages, 1> :
+                                                                                        (const void*)us_mx4_pair_kernel<Mx4Pair::kStages>;
+        p.smem = epi ? Mx4Pair::kEpiSmem : Mx4Pair::kSmem;
+        p.threads = epi ? 384 : 192;   // (twice as many warps have the sums)
         p.tiles = mx4_tiles(rt, 2) * p.col_tiles;
         p.blocks = 2 * std::min<int64_t>(p.tiles, sms / 2);
         p.cluster = 2;
@@ -112,12 +114,15 @@ us_status product(const void* X, int32_t x_type, int64_t ldx, const void* x_mx, 
     if (e) {
         p.e.bias = e->bias; p.e.bias_type = e->bias_type;
         p.e.residual = e->residual; p.e.r_type = e->residual_type; p.e.ldr = N > 1 ? e->ldr : 0;
+        p.e.r_vec = e->residual && rows_vec(e->residual, p.e.ldr, size_of(e->residual_type));
         p.e.act = e->act;
+const int64_t slot = 64 * ((e->gated ? 64 : 128) * size_of(e->residual_type) + 16), fit = Mx4Pair::kAhead / slot;
+        p.e.slots = fit >= 4 ? 4 : fit >= 2 ? 2 : 1;
     }
     const cudaError_t er = ops_kernel_allow(pl.kernel, (int)kWholeSm);
     if (er != cudaSuccess) return cuda(er);
     void* args[] = {&p};
-    return cuda(ops_launch(pl.kernel, dim3((unsigned)pl.blocks), 192, pl.smem, st, args, (unsigned)pl.cluster));
+    return cuda(ops_launch(pl.kernel, dim3((unsigned)pl.blocks), pl.threads, pl.smem, st, args, (unsigned)pl.cluster));
 }
 
 }  // namespace

@@ -12,6 +12,8 @@
 
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "../../include/unionsparse.h"
 
 namespace us {
@@ -393,6 +395,8 @@ struct Mx4Epilogue {
     const void *bias, *residual;   // or nullptr
     int64_t ldr;
     int32_t bias_type, r_type, act;
+    int32_t r_vec;                 // rows of the residual take 16-byte accesses
+    int32_t slots;                 // (pairs) 64 tokens' residuals under way, 1, 2 or 4
 };
 struct Mx4Params {
     Mx4Epilogue e;
@@ -515,6 +519,28 @@ __device__ __forceinline__ float mx4_sigmoid_times(float x, float z)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
     return x * r;
 }
+// x (1 + erf(x / sqrt 2)) / 2. With a = |x| / sqrt 2 and t = 1 / (1 + a / 2): erfc(a) = t 2^(Q(t) - a^2 log2 e); Q is a polynomial fitted here to log2(erfc(a) e^(a^2) / t) over
+// a = 0 .. 14, so that the tail is as exact relative to itself (2^-22, in fp32 arithmetic) as the middle. A third of erfcf's instructions: 4096 x 22016 x 4096
+// with it, 16-bit results.
+__device__ __forceinline__ float mx4_gelu_fast(float x)
+{
+    const float a = fabsf(x), d = fmaf(a, 0.35355339f, 1.f);
+    float t, e;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(d));
+    float q = 0.232262944f;
+    q = fmaf(q, t, -1.1080044f);
+    q = fmaf(q, t, 1.96354799f);
+    q = fmaf(q, t, -1.39462283f);
+    q = fmaf(q, t, 0.20458526f);
+    q = fmaf(q, t, -0.166827013f);
+    q = fmaf(q, t, 0.106588912f);
+    q = fmaf(q, t, 0.546135507f);
+    q = fmaf(q, t, 1.44205302f);
+    q = fmaf(q, t, -2.82571931f);   // (half of erfc)
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(-0.72134752f * a, a, q)));
+    const float tail = fminf(a, 1e30f) * (t * e);
+    return x > 0.f ? x - tail : -tail;
+}
 template <bool FAST, int N>
 __device__ __forceinline__ void mx4_activate(int32_t act, float (&v)[N])
 {
@@ -526,66 +552,110 @@ __device__ __forceinline__ void mx4_activate(int32_t act, float (&v)[N])
         for (int i = 0; i < N; ++i) v[i] = mx4_sigmoid_times<FAST>(v[i], v[i]);
     } else if (act == US_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * erfcf(v[i] * -0.70710678f);
+        for (int i = 0; i < N; ++i) v[i] = FAST ? mx4_gelu_fast(v[i]) : 0.5f * v[i] * erfcf(v[i] * -0.70710678f);
     } else if (act == US_ACT_GELU_TANH) {   // (1 + tanh z) / 2 = 1 / (1 + e^-2z)
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = mx4_sigmoid_times<FAST>(v[i], 1.59576912f * v[i] * fmaf(0.044715f * v[i], v[i], 1.f));
     }
 }
-// A thread's part of the residual for CH tokens of its weight row m: fetched ahead, as it is. (Gated: two lanes share an output column; the even one
-// has the even tokens.)
-template <int EPI, int CH>
-struct Mx4Residual {
-    static constexpr int K = EPI == 2 ? CH / 2 : CH;
-    uint32_t x[EPI ? K : 1];
-    __device__ __forceinline__ void load(const Mx4Params& p, int64_t n, int tokens, int64_t m)
-    {
-        if (!EPI || !p.e.residual) return;
-        const int64_t col = EPI == 2 ? m >> 1 : m;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int t = EPI == 2 ? 2 * k + (int)(m & 1) : k;
-            if (t >= tokens || m >= p.M) continue;
-            const int64_t at = (n + t) * p.e.ldr + col;
-            x[k] = p.e.r_type == kF32 ? __ldcg(static_cast<const uint32_t*>(p.e.residual) + at) : __ldcg(static_cast<const uint16_t*>(p.e.residual) + at);
-        }
-    }
-    __device__ __forceinline__ float at(const Mx4Params& p, int k) const
-    {
-        return p.e.r_type == kF32 ? __uint_as_float(x[k]) : p.e.r_type == kF16 ? __half2float(__ushort_as_half((unsigned short)x[k])) : __uint_as_float(x[k] << 16);
-    }
-};
-// CH tokens' sums of weight row `row` of the tile (m of the matrix), finished and rounded, to their places [token][column] in shared memory.
-template <class T, int EPI, int CH>
-__device__ __forceinline__ void mx4_finish(const Mx4Params& p, const uint32_t (&r)[CH], const Mx4Residual<EPI, CH>& res, float bias, int row, uint8_t* b, int pitch)
+// Sums of a tile wait in shared memory as they are, fp32 [token][weight row]: pieces of four rows in an order in which neither a warp's stores (32 rows of a
+// token) nor its loads (8 rows or 16 a lane) meet a bank twice.
+constexpr int kMxPitch = 132;
+__device__ __forceinline__ int mx4_place(int row) { return row ^ (((row >> 5) & 3) << 2); }
+// What follows the product, on `tokens` tokens of a tile, and out in whole lines: a thread has 16 bytes of a token's output at a time, always the same columns. This way
+// its code is there once for all tokens, whatever f is.
+template <int EPI>
+__device__ __forceinline__ int mx4_columns(const Mx4Params& p, int64_t m0)   // of the output that the tile has (0: a pair's rows end with its first block)
 {
-    if (EPI == 0) {
-#pragma unroll
-        for (int i = 0; i < CH; ++i) *reinterpret_cast<T*>(b + i * pitch + row * sizeof(T)) = from_f32<T>(__uint_as_float(r[i]));
-        return;
-    }
+    return (int)max((int64_t)0, min((int64_t)(128 / EPI), (EPI == 2 ? p.M >> 1 : p.M) - (EPI == 2 ? m0 >> 1 : m0)));
+}
+template <int EPI>
+__device__ __forceinline__ bool mx4_whole(const Mx4Params& p, int64_t m0) { return p.y_vec && mx4_columns<EPI>(p, m0) == 128 / EPI && (!p.e.residual || p.e.r_vec); }
+template <class T, int EPI, int THREADS>
+__device__ __forceinline__ void mx4_finish(const Mx4Params& p, const float* b, int tokens, int64_t n0, int64_t m0, int tid)
+{
+    constexpr int COLS = 128 / EPI, PER = 16 / (int)sizeof(T), ROW = COLS / PER, IN = EPI * PER, U = 2;   // output columns, of a piece; pieces of a token; sums of a piece
     constexpr bool FAST = sizeof(T) == 2;
-    constexpr int K = EPI == 2 ? CH / 2 : CH;
-    float v[K], up[EPI == 2 ? K : 1];
-    const bool odd = row & 1;
+    const int64_t c0 = EPI == 2 ? m0 >> 1 : m0;
+    const int m_here = mx4_columns<EPI>(p, m0);
+    if (mx4_whole<EPI>(p, m0)) {
+        const int piece = tid % ROW;
+        const bool wide = p.e.r_type == kF32;
+        float bias[IN];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        if (EPI == 2) {
-            const float x = __uint_as_float(r[2 * k]) + bias, y = __uint_as_float(r[2 * k + 1]) + bias;
-            const float got = __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
-            v[k] = odd ? got : x;
-            up[k] = odd ? y : got;
-        } else {
-            v[k] = __uint_as_float(r[k]) + bias;
+        for (int i = 0; i < IN; ++i) bias[i] = p.e.bias ? mx4_scalar(p.e.bias, p.e.bias_type, m0 + piece * IN + i) : 0.f;
+#pragma unroll 1
+        for (int n = tid / ROW; n < tokens; n += U * (THREADS / ROW)) {
+            uint4 r[U][2];
+            if (p.e.residual)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int t = n + u * (THREADS / ROW);
+                    if (t >= tokens) break;
+                    const uint8_t* at = static_cast<const uint8_t*>(p.e.residual) + ((n0 + t) * p.e.ldr + c0 + piece * PER) * (wide ? 4 : 2);
+                    if (PER == 4 && !wide) {
+                        const uint2 x = __ldcg(reinterpret_cast<const uint2*>(at));
+                        r[u][0].x = x.x;
+                        r[u][0].y = x.y;
+                    } else {
+                        r[u][0] = __ldcg(reinterpret_cast<const uint4*>(at));
+                        if (PER == 8 && wide) r[u][1] = __ldcg(reinterpret_cast<const uint4*>(at) + 1);
+                    }
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int t = n + u * (THREADS / ROW);
+                if (t >= tokens) break;
+                float z[IN], v[PER];
+#pragma unroll
+                for (int i = 0; i < IN; i += 4) {
+                    const float4 x = *reinterpret_cast<const float4*>(b + t * kMxPitch + mx4_place(piece * IN + i));
+                    z[i] = x.x + bias[i]; z[i + 1] = x.y + bias[i + 1]; z[i + 2] = x.z + bias[i + 2]; z[i + 3] = x.w + bias[i + 3];
+                }
+#pragma unroll
+                for (int k = 0; k < PER; ++k) v[k] = z[EPI * k];
+                mx4_activate<FAST>(p.e.act, v);
+                if (EPI == 2)
+#pragma unroll
+                    for (int k = 0; k < PER; ++k) v[k] *= z[EPI * k + EPI - 1];
+                if (p.e.residual) {
+                    const uint32_t w[8] = {r[u][0].x, r[u][0].y, r[u][0].z, r[u][0].w, r[u][1].x, r[u][1].y, r[u][1].z, r[u][1].w};
+#pragma unroll
+                    for (int k = 0; k < PER; ++k) {
+                        const uint32_t h = w[k >> 1] >> (16 * (k & 1));
+                        v[k] += wide ? __uint_as_float(w[k]) : p.e.r_type == kF16 ? __half2float(__ushort_as_half((unsigned short)h)) : __uint_as_float(h << 16);
+                    }
+                }
+                union { uint4 q; T e[PER]; } y;
+#pragma unroll
+                for (int k = 0; k < PER; ++k) y.e[k] = from_f32<T>(v[k]);
+                *reinterpret_cast<uint4*>(static_cast<T*>(p.Y) + (n0 + t) * p.ldy + c0 + piece * PER) = y.q;
+            }
         }
-    }
-    mx4_activate<FAST>(p.e.act, v);
+    } else {   // a column a thread, four tokens' residuals on their way
+        const int c = tid % COLS;
+        if (c >= m_here) return;
+        float bias[EPI];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        if (EPI == 2) v[k] *= up[k];
-        if (p.e.residual) v[k] += res.at(p, k);
-        const int t = EPI == 2 ? 2 * k + (odd ? 1 : 0) : k, c = EPI == 2 ? row >> 1 : row;
-        *reinterpret_cast<T*>(b + t * pitch + c * sizeof(T)) = from_f32<T>(v[k]);
+        for (int i = 0; i < EPI; ++i) bias[i] = p.e.bias ? mx4_scalar(p.e.bias, p.e.bias_type, m0 + EPI * c + i) : 0.f;
+#pragma unroll 1
+        for (int n = tid / COLS; n < tokens; n += 4 * (THREADS / COLS)) {
+            float r[4], v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int t = n + u * (THREADS / COLS);
+                r[u] = p.e.residual && t < tokens ? mx4_scalar(p.e.residual, p.e.r_type, (n0 + t) * p.e.ldr + c0 + c) : 0.f;
+                v[u] = t < tokens ? b[t * kMxPitch + mx4_place(EPI * c)] + bias[0] : 0.f;
+            }
+            mx4_activate<FAST>(p.e.act, v);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int t = n + u * (THREADS / COLS);
+                if (t >= tokens) break;
+                if (EPI == 2) v[u] *= b[t * kMxPitch + mx4_place(EPI * c + EPI - 1)] + bias[EPI - 1];
+                static_cast<T*>(p.Y)[(n0 + t) * p.ldy + c0 + c] = from_f32<T>(p.e.residual ? v[u] + r[u] : v[u]);
+            }
+        }
     }
 }
 // Token n, weight rows m .. m + 3 (of which the matrix has at least the first): finished and stored.
@@ -619,53 +689,70 @@ __device__ __forceinline__ void mx4_finish4(const Mx4Params& p, int64_t n, int64
 }
 __device__ __forceinline__ void bar_epilogue() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 // The same barrier, and whether any of its threads says so.
+template <int THREADS = 128>
 __device__ __forceinline__ bool bar_any(bool say)
 {
     uint32_t any;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(any) : "r"((uint32_t)say) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any) : "r"((uint32_t)say), "n"(THREADS) : "memory");
     return any != 0;
 }
 
 // The tile's sums (four warps, lane quarter `quarter`): 32 tokens at a time to shared memory as they are stored, [token][weight row], and
 // from there in whole lines: every thread 16 bytes of a token's 256 (512). Straight from the registers a warp's store of one token is 64
 // bytes; 4096 x 28672 x 8192 took 705 us that way, whatever the products took.
-template <class T, int EPI, int CH>
-__device__ __forceinline__ void mx4_write_tile(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage, Mx4Residual<EPI, CH>& res)
+template <class T>
+__device__ __forceinline__ void mx4_write_tile(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage)
 {
-    constexpr int COLS = EPI == 2 ? 64 : 128;   // columns of the output
-    constexpr int PITCH = COLS * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = COLS / PER;   // bytes of a token, values of a piece, pieces of a token
+    constexpr int PITCH = 128 * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = 128 / PER;   // bytes of a token, values of a piece, pieces of a token
     const int row = 32 * quarter + lane, tid = row;
-    const int64_t c0 = EPI == 2 ? m0 >> 1 : m0;
-    const int m_here = (int)min((int64_t)COLS, (EPI == 2 ? p.M >> 1 : p.M) - c0);
-    const float bias = EPI && p.e.bias && m0 + row < p.M ? mx4_scalar(p.e.bias, p.e.bias_type, m0 + row) : 0.f;
+    const int m_here = (int)min((int64_t)128, p.M - m0);
     int buf = 0;
 #pragma unroll 1
-    for (int c = 0; c < nn; c += CH) {
-        uint32_t r[CH];
-        if constexpr (CH == 32) {
-            tc_ld32(tm + ((uint32_t)quarter << 21) + (uint32_t)c, r);
-            tc_wait_ld();
-            pin32(r);
-        } else {
-            tc_ld16(tm + ((uint32_t)quarter << 21) + (uint32_t)c, r);
-        }
-        uint8_t* b = stage + buf * (CH * PITCH);
-        mx4_finish<T, EPI, CH>(p, r, res, bias, row, b, PITCH);
-        if (EPI && c + CH < nn) res.load(p, n0 + c + CH, nn - c - CH, m0 + row);
-        bar_epilogue();   // (two buffers: whoever is a chunk behind still reads the other one)
-        const int rows = min(CH, nn - c);
-        if (p.y_vec && m_here == COLS) {
+    for (int c = 0; c < nn; c += 32) {
+        uint32_t r[32];
+        tc_ld32(tm + ((uint32_t)quarter << 21) + (uint32_t)c, r);
+        tc_wait_ld();
+        pin32(r);
+        uint8_t* b = stage + buf * (32 * PITCH);
 #pragma unroll
-            for (int k = 0; k < CH * ROW / 128; ++k) {
+        for (int i = 0; i < 32; ++i) *reinterpret_cast<T*>(b + i * PITCH + row * sizeof(T)) = from_f32<T>(__uint_as_float(r[i]));
+        bar_epilogue();   // (two buffers: whoever is a chunk behind still reads the other one)
+        const int rows = min(32, nn - c);
+        if (p.y_vec && m_here == 128) {
+#pragma unroll
+            for (int k = 0; k < 32 * ROW / 128; ++k) {
                 const int i = tid + 128 * k, n = i / ROW, piece = i % ROW;
-                if (n < rows) *reinterpret_cast<uint4*>(static_cast<T*>(p.Y) + (n0 + c + n) * p.ldy + c0 + piece * PER) = *reinterpret_cast<const uint4*>(b + n * PITCH + 16 * piece);
+                if (n < rows) *reinterpret_cast<uint4*>(static_cast<T*>(p.Y) + (n0 + c + n) * p.ldy + m0 + piece * PER) = *reinterpret_cast<const uint4*>(b + n * PITCH + 16 * piece);
             }
         } else {
             for (int n = 0; n < rows; ++n)
-                if (tid < m_here) static_cast<T*>(p.Y)[(n0 + c + n) * p.ldy + c0 + tid] = *reinterpret_cast<const T*>(b + n * PITCH + tid * sizeof(T));
+                if (tid < m_here) static_cast<T*>(p.Y)[(n0 + c + n) * p.ldy + m0 + tid] = *reinterpret_cast<const T*>(b + n * PITCH + tid * sizeof(T));
         }
         buf ^= 1;
+    }
+}
+// With an epilogue: 64 tokens at a time.
+template <int EPI>
+__device__ __forceinline__ void mx4_finish_tile(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage)
+{
+    const int row = 32 * quarter + lane;
+    float* b = reinterpret_cast<float*>(stage);
+#pragma unroll 1
+    for (int t = 0; t < nn; t += 64) {
+        const int tokens = min(64, nn - t);
+        if (t) bar_epilogue();
+#pragma unroll 1
+        for (int c = 0; c < tokens; c += 16) {
+            uint32_t r[16];
+            tc_ld16(tm + ((uint32_t)quarter << 21) + (uint32_t)(t + c), r);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) b[(c + i) * kMxPitch + mx4_place(row)] = __uint_as_float(r[i]);
+        }
+        bar_epilogue();
+        if (p.y_type == kF32) mx4_finish<float, EPI, 128>(p, b, tokens, n0 + t, m0, row);
+        else if (p.y_type == kF16) mx4_finish<__half, EPI, 128>(p, b, tokens, n0 + t, m0, row);
+        else mx4_finish<__nv_bfloat16, EPI, 128>(p, b, tokens, n0 + t, m0, row);
     }
 }
 
@@ -817,8 +904,6 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
         }
         const uint32_t quarter = (uint32_t)(warp & 3);
         const int row = 32 * (int)quarter + lane;
-        Mx4Residual<EPI, EPI ? 16 : 32> res;
-        if (EPI && p.split == 1) res.load(p, n0, nn, 128 * (int64_t)mt + row);
         ok = ops_wait_warp(b_done, 0, 4 * kMxWait, dead);
         tc_fence_after();
         // (the ring is free: all copies have landed and have been read)
@@ -833,9 +918,13 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
                     for (int i = 0; i < 16; ++i) part[(c + i) * 128 + row] = __uint_as_float(r[i]);
                 }
         } else if (!*dead) {   // (*dead is set before the sums are announced, or never)
-            if (p.y_type == kF32) mx4_write_tile<float>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring, res);
-            else if (p.y_type == kF16) mx4_write_tile<__half>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring, res);
-            else mx4_write_tile<__nv_bfloat16>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring, res);
+            if constexpr (EPI) {
+                mx4_finish_tile<EPI>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring);
+            } else {
+                if (p.y_type == kF32) mx4_write_tile<float>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring);
+                else if (p.y_type == kF16) mx4_write_tile<__half>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring);
+                else mx4_write_tile<__nv_bfloat16>(p, tm, (int)quarter, lane, 128 * (int64_t)mt, n0, nn, ring);
+            }
         }
         tc_fence_before();
     }
@@ -883,8 +972,9 @@ struct Mx4Pair {
     static constexpr int kStage = kMxTile + 2 * kMxScales + kMxCodes;            // W: scales, codes; X: scales of 256 tokens, codes of 128
     static constexpr int kStages = 5, kOut = 128 * (128 * 2 + 16);               // bytes of half a block's sums, 16 bits each (or a quarter's in 32)
     static constexpr int kSmem = 1024 + kStages * kStage + kOut;
+    static constexpr int kEpiStages = kStages - 1, kAhead = 48 * 1024, kEpiSmem = 1024 + kEpiStages * kStage + kOut + kAhead;   // (4 stages are as fast as 5)
     static constexpr int kSfCols = 24;                                           // tensor-memory columns of a stage's scales
-    static_assert(kSmem <= 226 * 1024 && 64 * (128 * 4 + 16) <= kOut && 256 + 2 * kSfCols <= 512, "shared and tensor memory");
+    static_assert(kSmem <= 226 * 1024 && kEpiSmem <= 226 * 1024 && 64 * kMxPitch * 4 <= kOut && 256 + 2 * kSfCols <= 512, "shared and tensor memory");
 };
 
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t local, uint32_t rank)
@@ -931,15 +1021,11 @@ __device__ __forceinline__ void pair_copy_scales(uint32_t elected, uint32_t d, u
 }
 
 // A block's sums (four warps) to shared memory and out; free_bar: the pair's first block's barrier, told when they are out of tensor memory.
-template <class T, int EPI>
-__device__ __forceinline__ void mx4_pair_store(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage, uint32_t free_bar,
-                                               Mx4Residual<EPI, 32>& res, float bias)
+template <class T>
+__device__ __forceinline__ void mx4_pair_store(const Mx4Params& p, uint32_t tm, int quarter, int lane, int64_t m0, int64_t n0, int nn, uint8_t* stage, uint32_t free_bar)
 {
-    constexpr int COLS = EPI == 2 ? 64 : 128;   // columns of the output
-    constexpr int PITCH = COLS * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = COLS / PER, PASS = 256 / (int)sizeof(T);
-    const int row = 32 * quarter + lane;
-    const int64_t col0 = EPI == 2 ? m0 >> 1 : m0;
-    const int m_here = (int)max((int64_t)0, min((int64_t)COLS, (EPI == 2 ? p.M >> 1 : p.M) - col0));   // (0: the pair's rows end with its first block)
+    constexpr int PITCH = 128 * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = 128 / PER, PASS = 256 / (int)sizeof(T);
+    const int row = 32 * quarter + lane, m_here = (int)max((int64_t)0, min((int64_t)128, p.M - m0));   // (0: the pair's rows end with its first block)
 #pragma unroll 1
     for (int c0 = 0; c0 < nn; c0 += PASS) {
         const int cols = min(PASS, nn - c0);
@@ -950,8 +1036,8 @@ __device__ __forceinline__ void mx4_pair_store(const Mx4Params& p, uint32_t tm, 
             tc_ld32(tm + ((uint32_t)quarter << 21) + (uint32_t)(c0 + c), r);
             tc_wait_ld();
             pin32(r);
-            mx4_finish<T, EPI, 32>(p, r, res, bias, row, stage + c * PITCH, PITCH);
-            if (EPI) res.load(p, n0 + c0 + c + 32, nn - c0 - c - 32, m0 + row);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) *reinterpret_cast<T*>(stage + (c + i) * PITCH + row * sizeof(T)) = from_f32<T>(__uint_as_float(r[i]));
         }
         if (c0 + PASS >= nn) {
             tc_fence_before();
@@ -959,21 +1045,167 @@ __device__ __forceinline__ void mx4_pair_store(const Mx4Params& p, uint32_t tm, 
             if (lane == 0) mbar_arrive_cluster(free_bar);
         }
         bar_epilogue();
-        if (p.y_vec && m_here == COLS) {
+        if (p.y_vec && m_here == 128) {
 #pragma unroll 4
             for (int i = row; i < cols * ROW; i += 128) {
                 const int n = i / ROW, piece = i % ROW;
-                *reinterpret_cast<uint4*>(static_cast<T*>(p.Y) + (n0 + c0 + n) * p.ldy + col0 + piece * PER) = *reinterpret_cast<const uint4*>(stage + n * PITCH + 16 * piece);
+                *reinterpret_cast<uint4*>(static_cast<T*>(p.Y) + (n0 + c0 + n) * p.ldy + m0 + piece * PER) = *reinterpret_cast<const uint4*>(stage + n * PITCH + 16 * piece);
             }
         } else {
             for (int n = 0; n < cols; ++n)
-                if (row < m_here) static_cast<T*>(p.Y)[(n0 + c0 + n) * p.ldy + col0 + row] = *reinterpret_cast<const T*>(stage + n * PITCH + row * sizeof(T));
+                if (row < m_here) static_cast<T*>(p.Y)[(n0 + c0 + n) * p.ldy + m0 + row] = *reinterpret_cast<const T*>(stage + n * PITCH + row * sizeof(T));
         }
     }
 }
+// With an epilogue: eight warps, `half` 0 or 1 with 32 tokens of every 64, a thread a weight row. All sums go to registers at once (128 a thread), so that the next
+// tile's products begin before anything is computed from them. What follows is computed there, too, 64 tokens at a time, and passes rounded through shared
+// memory on its way out: the products' operands take three quarters of shared memory's bandwidth (through it in fp32, with one pass of all that
+// follows behind it: 204 us for 4096 x 22016 x 4096 gated silu, REPLACED). The residual of 64 tokens comes to a slot of shared memory by asynchronous
+// copies; as many slots as there is room for (p.e.slots) are under way while the products run.
+__device__ __forceinline__ void bar_finish() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+template <class T, int EPI>
+struct Mx4PairFinish {
+    static constexpr int COLS = 128 / EPI, PITCH = COLS * (int)sizeof(T) + 16, PER = 16 / (int)sizeof(T), ROW = COLS / PER, K = 32 / EPI;   // bytes of a token; values of a piece, pieces of a token
+    const Mx4Params& p;
+    uint8_t *stage, *slots;
+    int lane, row, tid, half, size, pitch;   // size: bytes of a residual's value; pitch: of a token's in a slot
+    __device__ __forceinline__ Mx4PairFinish(const Mx4Params& p_, uint8_t* out, int warp, int lane_) : p(p_), stage(out), slots(out + Mx4Pair::kOut), lane(lane_)
+    {
+        row = 32 * (warp & 3) + lane;
+        half = (warp - 4) >> 2;
+        tid = 128 * half + row;
+        size = p.e.r_type == kF32 ? 4 : 2;
+        pitch = COLS * size + 16;
+    }
+    __device__ __forceinline__ uint8_t* slot(int j) const { return slots + j % p.e.slots * 64 * pitch; }
+    __device__ __forceinline__ void fetch(int j, int64_t n0, int nn, int64_t m0) const
+    {
+        const int tokens = min(64, nn - 64 * j);
+        const uint8_t* src = static_cast<const uint8_t*>(p.e.residual) + ((n0 + 64 * j) * p.e.ldr + (EPI == 2 ? m0 >> 1 : m0)) * size;
+        const uint32_t dst = smem_u32(slot(j));
+        auto copy = [&](auto pieces) {   // 16-byte pieces of a token
+            constexpr int P = decltype(pieces)::value;
+            const int c = tid % P;
+#pragma unroll
+            for (int i = 0; i < 64 * P / 256; ++i) {
+                const int t = tid / P + i * (256 / P);
+                if (t < tokens) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + t * pitch + 16 * c), "l"(src + t * p.e.ldr * size + 16 * c) : "memory");
+            }
+        };
+        if (size == 4) copy(std::integral_constant<int, COLS / 4>{});
+        else copy(std::integral_constant<int, COLS / 8>{});
+    }
+    __device__ __forceinline__ void commit() const { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    __device__ __forceinline__ void wait() const   // the oldest of `slots` groups has landed
+    {
+        if (p.e.slots == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        else if (p.e.slots == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+    // Whether a tile's rows take 16-byte accesses throughout: its first residuals are sent for.
+    __device__ __forceinline__ bool begin(int64_t n0, int nn, int64_t m0) const
+    {
+        const bool whole = mx4_whole<EPI>(p, m0);
+        if (whole && p.e.residual)
+            for (int j = 0; j < p.e.slots; ++j) {
+                fetch(j, n0, nn, m0);
+                commit();
+            }
+        return whole;
+    }
+    __device__ __forceinline__ void tile(uint32_t tm, int64_t m0, int64_t n0, int nn, uint32_t free_bar, float bias, bool whole) const
+    {
+        const int64_t c0 = EPI == 2 ? m0 >> 1 : m0;
+        const int m_here = mx4_columns<EPI>(p, m0), col = row / EPI;
+        const bool odd = EPI == 2 && (row & 1);
+        uint32_t r[4][32];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (64 * j + 32 * half < nn) tc_ld32(tm + ((uint32_t)(row >> 5) << 21) + (uint32_t)(64 * j + 32 * half), r[j]);
+        tc_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pin32(r[j]);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(free_bar);
+#pragma unroll 1
+        for (int j = 0; j < 4 && 64 * j < nn; ++j) {
+            const int tokens = min(64, nn - 64 * j);
+            // (gated: two lanes share a column and a group of eight tokens; the even one has the first four, so that their accesses below meet no bank twice)
+            float z[32], v[K], up[EPI == 2 ? K : 1];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (j == k)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(r[k][i]);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) z[i] += bias;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                if (EPI == 2) {
+                    const int t = 8 * (k >> 2) + (k & 3);
+                    const float got = __shfl_xor_sync(0xffffffffu, odd ? z[t] : z[t + 4], 1);
+                    v[k] = odd ? got : z[t];
+                    up[k] = odd ? z[t + 4] : got;
+                } else {
+                    v[k] = z[k];
+                }
+            }
+            mx4_activate<sizeof(T) == 2>(p.e.act, v);
+            if (EPI == 2)
+#pragma unroll
+                for (int k = 0; k < K; ++k) v[k] *= up[k];
+            const int t0 = 32 * half + (odd ? 4 : 0);   // token of v[k]: t0 + place(k)
+            auto place = [](int k) { return EPI == 2 ? 8 * (k >> 2) + (k & 3) : k; };
+            if (p.e.residual && whole) wait();
+            bar_finish();   // (what was here has been stored; the residuals of all threads have landed)
+            if (p.e.residual) {
+                if (whole && size == 4) {
+                    const uint8_t* at = slot(j) + t0 * pitch + 4 * col;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) v[k] += *reinterpret_cast<const float*>(at + place(k) * pitch);
+                } else if (whole) {
+                    const uint8_t* at = slot(j) + t0 * pitch + 2 * col;
+                    const bool half_type = p.e.r_type == kF16;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        const unsigned short h = *reinterpret_cast<const unsigned short*>(at + place(k) * pitch);
+                        v[k] += half_type ? __half2float(__ushort_as_half(h)) : __uint_as_float((uint32_t)h << 16);
+                    }
+                } else if (col < m_here) {
+                    float x[K];
+#pragma unroll
+                    for (int k = 0; k < K; ++k) x[k] = t0 + place(k) < tokens ? mx4_scalar(p.e.residual, p.e.r_type, (n0 + 64 * j + t0 + place(k)) * p.e.ldr + c0 + col) : 0.f;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) v[k] += x[k];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k) *reinterpret_cast<T*>(stage + (t0 + place(k)) * PITCH + col * sizeof(T)) = from_f32<T>(v[k]);
+            bar_finish();
+            T* y = static_cast<T*>(p.Y) + (n0 + 64 * j) * p.ldy + c0;
+            if (p.y_vec && m_here == COLS) {
+                const int c = tid % ROW;
+#pragma unroll
+                for (int i = 0; i < 64 * ROW / 256; ++i) {
+                    const int t = tid / ROW + i * (256 / ROW);
+                    if (t < tokens) *reinterpret_cast<uint4*>(y + t * p.ldy + c * PER) = *reinterpret_cast<const uint4*>(stage + t * PITCH + 16 * c);
+                }
+            } else {
+                const int c = tid % COLS;
+                for (int t = tid / COLS; t < tokens; t += 256 / COLS)
+                    if (c < m_here) y[t * p.ldy + c] = *reinterpret_cast<const T*>(stage + t * PITCH + c * sizeof(T));
+            }
+            if (p.e.residual && whole) {
+                if (j + p.e.slots < 4) fetch(j + p.e.slots, n0, nn, m0);   // (all have read the slot)
+                commit();
+            }
+        }
+    }
+};
 
 template <int ST, int EPI = 0>   // ring stages
-__global__ void __launch_bounds__(192, 1) us_mx4_pair_kernel(const __grid_constant__ Mx4Params p)
+__global__ void __launch_bounds__(EPI ? 384 : 192, 1) us_mx4_pair_kernel(const __grid_constant__ Mx4Params p)
 {
     using S = Mx4Pair;
     constexpr int NB = 256;
@@ -988,7 +1220,7 @@ __global__ void __launch_bounds__(192, 1) us_mx4_pair_kernel(const __grid_consta
     const int rank = (int)(blockIdx.x & 1u), row_tiles = (int)mx4_tiles(p.M, 128);
     if (warp == 1) {
         if (lane < ST) { mbar_init(b_full + 8u * lane, 1); mbar_init(b_other + 8u * lane, 1); mbar_init(b_empty + 8u * lane, 1); }
-        if (lane == 0) { mbar_init(b_done, 1); mbar_init(b_free, 8); mbar_init(b_end, 1); misc[1] = 0; }
+        if (lane == 0) { mbar_init(b_done, 1); mbar_init(b_free, EPI ? 16 : 8); mbar_init(b_end, 1); misc[1] = 0; }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         __syncwarp();
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(misc)) : "memory");
@@ -1001,6 +1233,39 @@ __global__ void __launch_bounds__(192, 1) us_mx4_pair_kernel(const __grid_consta
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (after the allocation, as above)
     const uint32_t tm = *(volatile uint32_t*)misc;
     bool ok = true;
+    auto sums = [&](auto finish) {
+        const int quarter = warp & 3;
+        const uint32_t free_bar = cluster_addr(b_free, 0);
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        uint32_t n = 0;
+        for (int tile = blockIdx.x >> 1; tile < p.tiles; tile += gridDim.x >> 1, ++n) {
+            const int pair = tile / p.col_tiles, n0 = (tile - pair * p.col_tiles) * NB, nn = min(NB, p.N - n0);
+            const int64_t m0 = 128 * (int64_t)(2 * pair + rank);
+            float bias = 0.f;   // (on its way while the tile's products run)
+            bool whole = false;
+            if constexpr (EPI > 0) {
+                const int64_t m = m0 + finish.row;
+                if (p.e.bias && m < p.M) bias = mx4_scalar(p.e.bias, p.e.bias_type, m);
+                whole = finish.begin(n0, nn, m0);
+            }
+            ok = ops_wait_warp(b_done, n & 1u, 4 * kMxWait, dead);
+            if (bar_any<EPI ? 256 : 128>(!ok)) {   // (all these warps leave at the same place)
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            if constexpr (EPI > 0) {
+                finish.tile(tm, m0, n0, nn, free_bar, bias, whole);
+            } else {
+                if (p.y_type == kF32) mx4_pair_store<float>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
+                else if (p.y_type == kF16) mx4_pair_store<__half>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
+                else mx4_pair_store<__nv_bfloat16>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
+            }
+        }
+    };
+    // With an epilogue the warps from 4 on have the sums, 2 and 3 only fill their group. Registers of a thread: 168 at launch; 128 x 72 + 256 x 216 = 384 x 168.
+    if (!EPI || warp < 4) {
+    if (EPI) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0) {
         // ---- copies ----
         if (lane == 0) {
@@ -1076,32 +1341,14 @@ __global__ void __launch_bounds__(192, 1) us_mx4_pair_kernel(const __grid_consta
                 if (lane == 0) mbar_arrive_cluster(first + 8u * s);
                 if (++s == ST) { s = 0; par ^= 1u; }
             }
-    } else {
-        // ---- sums out ----
-        const int quarter = warp & 3;
-        const uint32_t free_bar = cluster_addr(b_free, 0);
-        asm volatile("griddepcontrol.wait;" ::: "memory");
-        uint32_t n = 0;
-        for (int tile = blockIdx.x >> 1; tile < p.tiles; tile += gridDim.x >> 1, ++n) {
-            const int pair = tile / p.col_tiles, n0 = (tile - pair * p.col_tiles) * NB, nn = min(NB, p.N - n0);
-            const int64_t m0 = 128 * (int64_t)(2 * pair + rank);
-            Mx4Residual<EPI, 32> res;
-            float bias = 0.f;
-            if (EPI) {   // (on their way while the tile's products run)
-                const int64_t m = m0 + 32 * quarter + lane;
-                if (p.e.bias && m < p.M) bias = mx4_scalar(p.e.bias, p.e.bias_type, m);
-                res.load(p, n0, nn, m);
-            }
-            ok = ops_wait_warp(b_done, n & 1u, 4 * kMxWait, dead);
-            if (bar_any(!ok)) {   // (all four warps leave at the same place)
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            if (p.y_type == kF32) mx4_pair_store<float, EPI>(p, tm, quarter, lane, m0, n0, nn, out, free_bar, res, bias);
-            else if (p.y_type == kF16) mx4_pair_store<__half, EPI>(p, tm, quarter, lane, m0, n0, nn, out, free_bar, res, bias);
-            else mx4_pair_store<__nv_bfloat16, EPI>(p, tm, quarter, lane, m0, n0, nn, out, free_bar, res, bias);
-        }
+    } else if constexpr (!EPI) {
+        sums(0);
+    }
+    } else if constexpr (EPI > 0) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        if (p.y_type == kF32) sums(Mx4PairFinish<float, EPI>(p, out, warp, lane));
+        else if (p.y_type == kF16) sums(Mx4PairFinish<__half, EPI>(p, out, warp, lane));
+        else sums(Mx4PairFinish<__nv_bfloat16, EPI>(p, out, warp, lane));
     }
     if (!ok && lane == 0) {
         *dead = 1;
