@@ -658,35 +658,62 @@ __device__ __forceinline__ void mx4_finish(const Mx4Params& p, const float* b, i
         }
     }
 }
-// Token n, weight rows m .. m + 3 (of which the matrix has at least the first): finished and stored.
-template <int EPI>
-__device__ __forceinline__ void mx4_finish4(const Mx4Params& p, int64_t n, int64_t m, float (&v)[4])
+// N values of a us_type array from i on (those below `end`; 0 behind), all on their way before the first is needed.
+template <int N>
+__device__ __forceinline__ void mx4_scalars(const void* p, int32_t type, int64_t i, int64_t end, float (&v)[N])
 {
-    if (EPI == 0) return mx4_store4(p, n, m, v);
-    if (m >= p.M) return;
-    if (p.e.bias)
+    if (type == kF32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) if (m + i < p.M) v[i] += mx4_scalar(p.e.bias, p.e.bias_type, m + i);
-    if (EPI == 1) {
-        mx4_activate<false>(p.e.act, v);
-        if (p.e.residual)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) if (m + i < p.M) v[i] += mx4_scalar(p.e.residual, p.e.r_type, n * p.e.ldr + m + i);
-        return mx4_store4(p, n, m, v);
+        for (int k = 0; k < N; ++k) v[k] = i + k < end ? __ldcg(static_cast<const float*>(p) + i + k) : 0.f;
+        return;
     }
-    float y[2] = {v[0], v[2]};
-    mx4_activate<false>(p.e.act, y);
+    uint16_t h[N];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (m + 2 * i >= p.M) break;
-        const int64_t c = (m >> 1) + i, at = n * p.ldy + c;
-        y[i] *= v[2 * i + 1];
-        if (p.e.residual) y[i] += mx4_scalar(p.e.residual, p.e.r_type, n * p.e.ldr + c);
-        if (p.y_type == kF32) static_cast<float*>(p.Y)[at] = y[i];
-        else if (p.y_type == kF16) static_cast<__half*>(p.Y)[at] = __float2half_rn(y[i]);
-        else static_cast<__nv_bfloat16*>(p.Y)[at] = __float2bfloat16_rn(y[i]);
-    }
+    for (int k = 0; k < N; ++k) h[k] = i + k < end ? __ldcg(static_cast<const uint16_t*>(p) + i + k) : (uint16_t)0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = type == kF16 ? __half2float(__ushort_as_half(h[k])) : __uint_as_float((uint32_t)h[k] << 16);
 }
+// Weight rows m .. m + 3 of a split product (of which the matrix has some): a thread always has the same, so that their bias is fetched once, and the residual of its first
+// tokens while it waits for the other ranks.
+template <int EPI>
+struct Mx4Four {
+    static constexpr int K = 4 / (EPI ? EPI : 1), AHEAD = 3;
+    float bias[4], res[AHEAD][K];
+    __device__ __forceinline__ int64_t columns(const Mx4Params& p) const { return EPI == 2 ? p.M >> 1 : p.M; }
+    __device__ __forceinline__ void residual(const Mx4Params& p, int64_t n, int64_t m, float (&v)[K]) const
+    {
+        const int64_t c = EPI == 2 ? m >> 1 : m;
+        mx4_scalars(p.e.residual, p.e.r_type, n * p.e.ldr + c, n * p.e.ldr + columns(p), v);
+    }
+    __device__ __forceinline__ void store(const Mx4Params& p, int64_t n, int64_t m, float (&v)[4], const float (&r)[K]) const
+    {
+        if (m >= p.M) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += bias[i];
+        float y[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) y[i] = v[EPI * i];
+        if (p.y_type == kF32) mx4_activate<false>(p.e.act, y);
+        else mx4_activate<true>(p.e.act, y);
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            if (EPI == 2) y[i] *= v[2 * i + 1];
+            if (p.e.residual) y[i] += r[i];
+        }
+        if (EPI == 1) {
+            const float all[4] = {y[0], y[1], y[K - 2], y[K - 1]};
+            return mx4_store4(p, n, m, all);
+        }
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const int64_t c = (m >> 1) + i, at = n * p.ldy + c;
+            if (c >= p.M >> 1) break;
+            if (p.y_type == kF32) static_cast<float*>(p.Y)[at] = y[i];
+            else if (p.y_type == kF16) static_cast<__half*>(p.Y)[at] = __float2half_rn(y[i]);
+            else static_cast<__nv_bfloat16*>(p.Y)[at] = __float2bfloat16_rn(y[i]);
+        }
+    }
+};
 __device__ __forceinline__ void bar_epilogue() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 // The same barrier, and whether any of its threads says so.
 template <int THREADS = 128>
@@ -936,13 +963,27 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
     tc_fence_after();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "n"(S::kCols));
     if (p.split > 1) {
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if (EPI) asm volatile("griddepcontrol.wait;" ::: "memory");   // (bias and residual: every thread that reads them has waited)
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         // each rank adds the sums of a share of the tile's (token, four rows), four ranks' at a time on their way
         const int total = nn * 32, per = (total + p.split - 1) / p.split, lo = min(total, rank * per), hi = min(total, lo + per);
         const uint32_t part = smem_u32(ring);
-        for (int i = lo + (int)threadIdx.x; i < hi; i += 192) {
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
+        int i = lo + (int)threadIdx.x;
+        const int64_t m = 128 * (int64_t)mt + 4 * (i & 31);   // (192 threads: the same rows every time)
+        Mx4Four<EPI> four;
+        if constexpr (EPI > 0) {
+            asm volatile("griddepcontrol.wait;" ::: "memory");   // (bias and residual: every thread that reads them has waited)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) four.bias[k] = 0.f;
+            if (p.e.bias && i < hi) mx4_scalars(p.e.bias, p.e.bias_type, m, p.M, four.bias);
+            if (p.e.residual)
+#pragma unroll
+                for (int k = 0; k < four.AHEAD; ++k)
+                    if (i + 192 * k < hi) four.residual(p, n0 + ((i + 192 * k) >> 5), m, four.res[k]);
+        }
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        auto sum = [&](int i, float (&v)[4]) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = 0.f;
             for (int r0 = 0; r0 < p.split; r0 += 4) {
                 float4 x[4];
 #pragma unroll
@@ -950,7 +991,27 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
 #pragma unroll
                 for (int r = 0; r < 4; ++r) { v[0] += x[r].x; v[1] += x[r].y; v[2] += x[r].z; v[3] += x[r].w; }
             }
-            mx4_finish4<EPI>(p, n0 + (i >> 5), 128 * (int64_t)mt + 4 * (i & 31), v);
+        };
+        float v[4];
+        if constexpr (EPI > 0) {
+#pragma unroll
+            for (int k = 0; k < four.AHEAD; ++k) {
+                if (i >= hi) break;
+                sum(i, v);
+                four.store(p, n0 + (i >> 5), m, v, four.res[k]);
+                i += 192;
+            }
+            for (; i < hi; i += 192) {
+                float r[four.K];
+                if (p.e.residual) four.residual(p, n0 + (i >> 5), m, r);
+                sum(i, v);
+                four.store(p, n0 + (i >> 5), m, v, r);
+            }
+        } else {
+            for (; i < hi; i += 192) {
+                sum(i, v);
+                mx4_store4(p, n0 + (i >> 5), 128 * (int64_t)mt + 4 * (i & 31), v);
+            }
         }
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
