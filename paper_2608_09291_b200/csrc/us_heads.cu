@@ -11,7 +11,7 @@ namespace {
 //     one's (in 32-bit arithmetic 131072 radians are known to 2^-7). What is left after quarter turns goes through two short polynomials.
 //   * A lane has eight pairs in registers, as two pieces of eight values: both ends of a pair are its own. 1 to 16 lanes have a head (a power of two, D / 16
 //     of them have values), a warp 32 / lanes heads at a time: a round. The sines and cosines of a lane's pairs are found once for all rounds that the warp
-//     walks over; the values of the next round are on their way meanwhile. Weights wait in shared memory.
+//     walks over; the values of the next round are on their way meanwhile. Sines, cosines and weights wait in shared memory.
 //   * Pairs behind the rotated ones are values that only the norm touches.
 // Bound by memory where there are many tokens, by launch and two trips to memory for a single one (MEASURED).
 struct Heads {
@@ -31,7 +31,7 @@ struct HeadsCall {
     int64_t axis_stride;
     int64_t N;
     int32_t D, rotary, log2_lanes, per_token;   // per_token: warps that share a token's heads
-    float eps;
+    float eps, one_over_D;
 };
 
 __device__ __forceinline__ float weight_at(const void* w, int32_t type, int i)
@@ -81,22 +81,84 @@ __device__ __forceinline__ void put(T* p, const T* v)
     else *reinterpret_cast<uint16_t*>(p) = *reinterpret_cast<const uint16_t*>(v);
 }
 
-// V: pairs that lie side by side in memory (8, 4 or 1), which divide rotary / 2 and D / 2.
+// two fp32 in one instruction
+__device__ __forceinline__ uint64_t two(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void split(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+template <class T>
+__device__ __forceinline__ uint64_t widen(const T* v) { return two(to_f32(v[0]), to_f32(v[1])); }
+template <>
+__device__ __forceinline__ uint64_t widen<__nv_bfloat16>(const __nv_bfloat16* v)
+{
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(v);
+    return two(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+template <class T>
+__device__ __forceinline__ void narrow(uint64_t x, T* v)
+{
+    float a, b;
+    split(x, a, b);
+    v[0] = from_f32<T>(a);
+    v[1] = from_f32<T>(b);
+}
+template <>
+__device__ __forceinline__ void narrow<__nv_bfloat16>(uint64_t x, __nv_bfloat16* v)
+{
+    float a, b;
+    split(x, a, b);
+    *reinterpret_cast<__nv_bfloat162*>(v) = __floats2bfloat162_rn(a, b);
+}
+template <>
+__device__ __forceinline__ void narrow<__half>(uint64_t x, __half* v)
+{
+    float a, b;
+    split(x, a, b);
+    *reinterpret_cast<__half2*>(v) = __floats2half2_rn(a, b);
+}
+
+// V: pairs that lie side by side in memory (8, 4 or 1), which divide rotary / 2 and D / 2. A lane's values: v[0 .. 7] the first ends of its pairs, v[8 .. 15] the
+// others; interleaved, V of the 2 V values of a group each. Weight, sine and cosine are one factor each: with own = w cos and cross = +- (the other end's w) sin
+// y = x own + (the other end's x) cross, two values an instruction.
 template <class T, int V, bool INTERLEAVED>
 __global__ void __launch_bounds__(kHeadsThreads) us_heads_kernel(const __grid_constant__ HeadsCall a)
 {
-    __shared__ __align__(16) float weights[2][256];   // of lane l: its 16 at 16 l
+    constexpr int G = 8 / V;
+    __shared__ float weights[2][256];   // of lane l: its 16 at l + 16 i
+    __shared__ float turned[16][kHeadsThreads];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, lanes = 1 << a.log2_lanes, slot = lane >> a.log2_lanes, slots = 32 >> a.log2_lanes;
     const int l = lane & (lanes - 1), p0 = 8 * l, half = a.rotary / 2;   // the lane's first pair
-    const int64_t warp = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    const int64_t n = warp / a.per_token;
+    const uint32_t warp = blockIdx.x * (kHeadsThreads / 32) + (threadIdx.x >> 5);   // (fewer than 2^31: more than one a token only where there are few)
+    const uint32_t n = warp / (uint32_t)a.per_token;
     const int share = (int)(warp - n * a.per_token);
-    // places of the first values of pair group g of V pairs, and of their other ends
-    auto in = [&](int g) { return p0 + V * g < a.D / 2; };
-    auto turns = [&](int g) { return p0 + V * g < half; };
-    auto at = [&](int g) { return INTERLEAVED || !turns(g) ? 2 * (p0 + V * g) : p0 + V * g; };
-    auto other = [&](int g) { return INTERLEAVED || !turns(g) ? 2 * (p0 + V * g) + V : p0 + V * g + half; };
+    const bool real = n < a.N;
+    // places of the first values of pair group g, and of their other ends
+    int at[G], other[G];
+    bool in[G], turns[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const int p = p0 + V * g;
+        in[g] = real && p < a.D / 2;
+        turns[g] = p < half;
+        at[g] = INTERLEAVED || !turns[g] ? 2 * p : p;
+        other[g] = INTERLEAVED || !turns[g] ? 2 * p + V : p + half;
+    }
     uint64_t step[8];
     uint32_t axis[2] = {0, 0};   // of the pairs, a byte each
 #pragma unroll
@@ -105,38 +167,38 @@ __global__ void __launch_bounds__(kHeadsThreads) us_heads_kernel(const __grid_co
         if (a.axis && p0 + i < half) axis[i >> 2] |= (uint32_t)__ldg(a.axis + p0 + i) << (8 * (i & 3));
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    // rounds: queries' first, then keys'
-    const int first = (a.part[0].heads + slots - 1) >> (5 - a.log2_lanes), rounds = first + ((a.part[1].heads + slots - 1) >> (5 - a.log2_lanes));
     struct Values { __align__(16) T v[16]; };
-    auto fetch = [&](int round, Values& x) {
-        const int which = round >= first, h = (round - (which ? first : 0)) * slots + slot;
-        const Heads& p = a.part[which];
+    auto fetch = [&](const T* src, bool there, Values& x) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) x.v[i] = from_f32<T>(0.f);
-        if (n >= a.N || round >= rounds || h >= p.heads) return;
-        const T* src = static_cast<const T*>(p.x) + n * p.token + h * p.head;
+        if (!there) return;
 #pragma unroll
-        for (int g = 0; g < 8 / V; ++g)
-            if (in(g)) {
-                get<T, V>(src + at(g), x.v + V * g);
-                get<T, V>(src + other(g), x.v + 8 + V * g);
+        for (int g = 0; g < G; ++g)
+            if (in[g]) {
+                get<T, V>(src + at[g], x.v + V * g);
+                get<T, V>(src + other[g], x.v + 8 + V * g);
             }
     };
+    // rounds: queries' first, then keys'
+    const int first = (a.part[0].heads + slots - 1) >> (5 - a.log2_lanes), rounds = first + ((a.part[1].heads + slots - 1) >> (5 - a.log2_lanes));
     Values x, ahead;
-    fetch(share, x);
-    // weights: place 16 l + i is value at(i / V) + i % V, 16 l + 8 + i its pair's other end
-    for (int i = threadIdx.x; i < 2 * 8 * lanes; i += blockDim.x) {
-        const int which = i >= 8 * lanes, q = i - (which ? 8 * lanes : 0), g = q / V * V;
-        const Heads& p = a.part[which];
-        if (!p.weight || q >= a.D / 2) continue;
-        const bool turned = g < half;
-        const int from = (INTERLEAVED || !turned ? 2 * g : g) + q % V, to = INTERLEAVED || !turned ? 2 * g + V + q % V : g + half + q % V;
-        weights[which][(q >> 3) * 16 + (q & 7)] = weight_at(p.weight, p.w_type, from);
-        weights[which][(q >> 3) * 16 + 8 + (q & 7)] = weight_at(p.weight, p.w_type, to);
+    {
+        const bool keys = share >= first;
+        const Heads& p = keys ? a.part[1] : a.part[0];
+        const int h = (share - (keys ? first : 0)) * slots + slot;
+        fetch(static_cast<const T*>(p.x) + n * p.token + h * p.head, h < p.heads, x);
     }
-    float c[8], s[8];
-    if (n < a.N) {
-        int64_t pos[8];
+    // weights: place i of lane l is value at(i / V) + i % V, place 8 + i its pair's other end
+    for (int i = threadIdx.x; i < 2 * 8 * lanes; i += kHeadsThreads) {
+        const int which = i >= 8 * lanes, q = i - (which ? 8 * lanes : 0), g = q / V * V;
+        const Heads& p = which ? a.part[1] : a.part[0];
+        const bool apart = INTERLEAVED || g >= half;
+        const bool has = p.weight && q < a.D / 2;
+        weights[which][(q >> 3) + 16 * (q & 7)] = has ? weight_at(p.weight, p.w_type, (apart ? 2 * g : g) + q % V) : 1.f;
+        weights[which][(q >> 3) + 16 * (8 + (q & 7))] = has ? weight_at(p.weight, p.w_type, (apart ? 2 * g + V : g + half) + q % V) : 1.f;
+    }
+    if (real) {
+        int32_t pos[8];
         if (a.axis) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) pos[i] = __ldcg(a.positions + (int64_t)((axis[i >> 2] >> (8 * (i & 3))) & 0xFFu) * a.axis_stride + n);
@@ -146,67 +208,96 @@ __global__ void __launch_bounds__(kHeadsThreads) us_heads_kernel(const __grid_co
             for (int i = 1; i < 8; ++i) pos[i] = pos[0];
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) turn((uint64_t)pos[i] * step[i], c[i], s[i]);
+        for (int i = 0; i < 8; ++i) turn((uint64_t)(int64_t)pos[i] * step[i], turned[i][threadIdx.x], turned[8 + i][threadIdx.x]);
     }
     __syncthreads();
-    if (n >= a.N) return;
+    if (!real) return;
+    int round = share;
 #pragma unroll 1
-    for (int round = share; round < rounds; round += a.per_token) {
-        fetch(round + a.per_token, ahead);
-        const int which = round >= first, h = (round - (which ? first : 0)) * slots + slot;
-        const Heads& p = a.part[which];
-        float f[16];
+    for (int which = 0; which < 2; ++which) {
+        const int base = which ? first : 0, end = which ? rounds : first;
+        if (round >= end) continue;
+        const Heads& p = which ? a.part[1] : a.part[0];
+        // factors of values 2 j and 2 j + 1 of the lane's 16 (V = 1: of each apart)
+        uint64_t own[8], cross[8];
+        {
+            float o[16], r[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) f[i] = to_f32(x.v[i]);
-        if (p.weight) {
-            float sum = 0.f;
+            for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum = fmaf(f[i], f[i], sum);
-            for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const float inv = __frsqrt_rn(sum / (float)a.D + a.eps);
+                for (int i = 0; i < V; ++i) {   // pair V g + i: its two values
+                    const int u = INTERLEAVED && V > 1 ? (2 * i < V ? V * g + 2 * i : 8 + V * g + 2 * i - V) : V * g + i, v = INTERLEAVED && V > 1 ? u + 1 : u + 8;
+                    const float c = turned[V * g + i][threadIdx.x], sn = turned[8 + V * g + i][threadIdx.x], wu = weights[which][l + 16 * u], wv = weights[which][l + 16 * v];
+                    o[u] = wu * c;
+                    r[u] = -wv * sn;
+                    o[v] = wv * c;
+                    r[v] = wu * sn;
+                }
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const float4 w = *reinterpret_cast<const float4*>(&weights[which][16 * l + i]);
-                f[i] = f[i] * inv * w.x;
-                f[i + 1] = f[i + 1] * inv * w.y;
-                f[i + 2] = f[i + 2] * inv * w.z;
-                f[i + 3] = f[i + 3] * inv * w.w;
+            for (int j = 0; j < 8; ++j) {
+                own[j] = two(o[2 * j], o[2 * j + 1]);
+                cross[j] = two(r[2 * j], r[2 * j + 1]);
             }
         }
+        const bool norm = p.weight != nullptr;
+        const int64_t step_x = (int64_t)a.per_token * slots * p.head, step_o = (int64_t)a.per_token * slots * p.o_head;
+        int h = (round - base) * slots + slot;
+        const T* src = static_cast<const T*>(p.x) + n * p.token + h * p.head;
+        T* dst = static_cast<T*>(p.out) + n * p.o_token + h * p.o_head;
+        if (round != share) fetch(src, h < p.heads, x);   // (the first of the keys' rounds)
+#pragma unroll 1
+        for (; round < end; round += a.per_token) {
+            src += step_x;
+            const int later = h + a.per_token * slots;
+            fetch(src, round + a.per_token < end && later < p.heads, ahead);
+            uint64_t f[8];
 #pragma unroll
-        for (int g = 0; g < 8 / V; ++g)
-            if (turns(g)) {
-                const int b = V * g;
-                if (INTERLEAVED) {   // values 2 i and 2 i + 1 of the 2 V that lie in a row
-                    auto value = [&](int i) -> float& { return f[i < V ? b + i : 8 + b + i - V]; };
+            for (int j = 0; j < 8; ++j) f[j] = widen<T>(x.v + 2 * j);
+            if (norm) {
+                uint64_t sum2 = mul2(f[0], f[0]);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float u = value(2 * i), v = value(2 * i + 1);
-                        value(2 * i) = u * c[b + i] - v * s[b + i];
-                        value(2 * i + 1) = v * c[b + i] + u * s[b + i];
-                    }
-                } else {
+                for (int j = 1; j < 8; ++j) sum2 = fma2(f[j], f[j], sum2);
+                float sum, rest;
+                split(sum2, sum, rest);
+                sum += rest;
+                for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                const float inv = __frsqrt_rn(fmaf(sum, a.one_over_D, a.eps));
+                const uint64_t inv2 = two(inv, inv);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float u = f[b + i], v = f[8 + b + i];
-                        f[b + i] = u * c[b + i] - v * s[b + i];
-                        f[8 + b + i] = v * c[b + i] + u * s[b + i];
-                    }
-                }
+                for (int j = 0; j < 8; ++j) f[j] = mul2(f[j], inv2);
             }
-        if (h < p.heads) {
-            T* dst = static_cast<T*>(p.out) + n * p.o_token + h * p.o_head;
             Values y;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) y.v[i] = from_f32<T>(f[i]);
-#pragma unroll
-            for (int g = 0; g < 8 / V; ++g)
-                if (in(g)) {
-                    put<T, V>(dst + at(g), y.v + V * g);
-                    put<T, V>(dst + other(g), y.v + 8 + V * g);
+            for (int j = 0; j < 8; ++j) {
+                uint64_t r = mul2(f[j], own[j]);
+                if (V == 1) {   // (pairs of one instruction may differ in whether they are turned)
+                    const uint64_t with = fma2(f[j ^ 4], cross[j], r);
+                    float r0, r1, w0, w1;
+                    split(r, r0, r1);
+                    split(with, w0, w1);
+                    r = two(turns[(2 * j) & (G - 1)] ? w0 : r0, turns[(2 * j + 1) & (G - 1)] ? w1 : r1);
+                } else if (turns[2 * j % 8 / V]) {   // (else nothing of the other end counts, not even a NaN)
+                    if (INTERLEAVED) {
+                        float u, v;
+                        split(f[j], u, v);
+                        r = fma2(two(v, u), cross[j], r);
+                    } else {
+                        r = fma2(f[j ^ 4], cross[j], r);
+                    }
                 }
+                narrow<T>(r, y.v + 2 * j);
+            }
+            if (h < p.heads)
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+                    if (in[g]) {
+                        put<T, V>(dst + at[g], y.v + V * g);
+                        put<T, V>(dst + other[g], y.v + 8 + V * g);
+                    }
+            x = ahead;
+            h = later;
+            dst += step_o;
         }
-        x = ahead;
     }
 }
 
@@ -265,6 +356,7 @@ us_status us_qk_norm_rope(const us_rotary* r, const int32_t* positions, int64_t 
     a.N = N;
     a.D = D; a.rotary = r->rotary_dim;
     a.eps = eps;
+    a.one_over_D = 1.f / (float)D;
     while ((16 << a.log2_lanes) < D) ++a.log2_lanes;
     // A token's rounds go to as many warps as fill the GPU; each finds the sines and cosines anew.
     const int64_t slots = 32 >> a.log2_lanes, rounds = (a.part[0].heads + slots - 1) / slots + (a.part[1].heads + slots - 1) / slots;
