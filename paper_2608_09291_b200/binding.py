@@ -514,6 +514,8 @@ class Rotary:
         self.pair_axis = torch.tensor([int(a) for a in pair_axis], dtype=torch.uint8).to(device) if self.axes > 1 else None
         if self.turns.is_cuda:
             torch.cuda.synchronize(self.turns.device)
+        self._struct = us_rotary(self.turns.data_ptr(), self.pair_axis.data_ptr() if self.axes > 1 else None, rotary_dim, self.axes, self.interleaved)
+        self._address = ctypes.addressof(self._struct)
 
 
 def qk_norm_rope(q, k, positions, rotary: Rotary, q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None, k_out=None, stream=None):
@@ -521,10 +523,7 @@ def qk_norm_rope(q, k, positions, rotary: Rotary, q_weight=None, k_weight=None, 
     head_dim), k (N, n_kv_heads, head_dim) or None: float16, bfloat16 or float32, any token and head strides: columns of a stacked projection's output
     need no copy. positions: int32 (N,), or (axes, N) for a rotary of several axes; any value. Weights: (head_dim,) of any of the types. q_out and k_out
     may be q and k themselves."""
-    if q.dim() != 3 or q.size(2) != rotary.head_dim:
-        raise ValueError("q must be a (N, heads, head_dim) tensor, head_dim as the rotary's")
-    return (_ext or _native()).qk_norm_rope(q, k, positions, rotary.turns, rotary.pair_axis, rotary.axes, rotary.rotary_dim, rotary.interleaved, q_weight, k_weight,
-                                            eps, q_out, k_out, stream)
+    return (_ext or _native()).qk_norm_rope(q, k, positions, rotary._address, rotary.turns, rotary.head_dim, q_weight, k_weight, eps, q_out, k_out, stream)
 
 
 # ---- the cache of keys and values in 8 bits ----

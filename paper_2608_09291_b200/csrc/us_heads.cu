@@ -135,14 +135,15 @@ __device__ __forceinline__ void narrow<__half>(uint64_t x, __half* v)
 // V: pairs that lie side by side in memory (8, 4 or 1), which divide rotary / 2 and D / 2. A lane's values: v[0 .. 7] the first ends of its pairs, v[8 .. 15] the
 // others; interleaved, V of the 2 V values of a group each. Weight, sine and cosine are one factor each: with own = w cos and cross = +- (the other end's w) sin
 // y = x own + (the other end's x) cross, two values an instruction.
-template <class T, int V, bool INTERLEAVED>
-__global__ void __launch_bounds__(kHeadsThreads) us_heads_kernel(const __grid_constant__ HeadsCall a)
+// LOG: of the lanes a head has, where that is known (0: it is not).
+template <class T, int V, bool INTERLEAVED, int LOG>
+__global__ void __launch_bounds__(kHeadsThreads, sizeof(T) == 2 && V == 8 ? 5 : 4) us_heads_kernel(const __grid_constant__ HeadsCall a)
 {
-    constexpr int G = 8 / V;
+    constexpr int G = 8 / V, DEEP = 2;   // rounds under way
     __shared__ float weights[2][256];   // of lane l: its 16 at l + 16 i
-    __shared__ float turned[16][kHeadsThreads];
+    __shared__ __align__(16) float2 turned[kHeadsThreads / 32][128];   // of a warp's token: cosine and sine of each pair (1, 0 behind the turned ones)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31, lanes = 1 << a.log2_lanes, slot = lane >> a.log2_lanes, slots = 32 >> a.log2_lanes;
+    const int lane = threadIdx.x & 31, log2_lanes = LOG ? LOG : a.log2_lanes, lanes = 1 << log2_lanes, slot = lane >> log2_lanes, slots = 32 >> log2_lanes;
     const int l = lane & (lanes - 1), p0 = 8 * l, half = a.rotary / 2;   // the lane's first pair
     const uint32_t warp = blockIdx.x * (kHeadsThreads / 32) + (threadIdx.x >> 5);   // (fewer than 2^31: more than one a token only where there are few)
     const uint32_t n = warp / (uint32_t)a.per_token;
@@ -159,18 +160,17 @@ __global__ void __launch_bounds__(kHeadsThreads) us_heads_kernel(const __grid_co
         at[g] = INTERLEAVED || !turns[g] ? 2 * p : p;
         other[g] = INTERLEAVED || !turns[g] ? 2 * p + V : p + half;
     }
-    uint64_t step[8];
-    uint32_t axis[2] = {0, 0};   // of the pairs, a byte each
+    uint64_t step[4];   // of pairs lane, lane + 32, ...
+    uint32_t axis[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        step[i] = p0 + i < half ? __ldg(a.turns + p0 + i) : 0;   // (constant since the handle was made)
-        if (a.axis && p0 + i < half) axis[i >> 2] |= (uint32_t)__ldg(a.axis + p0 + i) << (8 * (i & 3));
+    for (int i = 0; i < 4; ++i) {
+        const int p = lane + 32 * i;
+        step[i] = p < half ? __ldg(a.turns + p) : 0;   // (constant since the handle was made)
+        axis[i] = p < half && a.axis ? __ldg(a.axis + p) : 0;
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     struct Values { __align__(16) T v[16]; };
-    auto fetch = [&](const T* src, bool there, Values& x) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x.v[i] = from_f32<T>(0.f);
+    auto fetch = [&](const T* src, bool there, Values& x) {   // (values that are not there stay 0; a head that is not there is not stored)
         if (!there) return;
 #pragma unroll
         for (int g = 0; g < G; ++g)
@@ -180,14 +180,25 @@ __global__ void __launch_bounds__(kHeadsThreads) us_heads_kernel(const __grid_co
             }
     };
     // rounds: queries' first, then keys'
-    const int first = (a.part[0].heads + slots - 1) >> (5 - a.log2_lanes), rounds = first + ((a.part[1].heads + slots - 1) >> (5 - a.log2_lanes));
-    Values x, ahead;
-    {
-        const bool keys = share >= first;
+    const int first = (a.part[0].heads + slots - 1) >> (5 - log2_lanes), rounds = first + ((a.part[1].heads + slots - 1) >> (5 - log2_lanes));
+    Values x[DEEP];   // of the round that is next, and of those behind
+#pragma unroll
+    for (int k = 0; k < DEEP; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[k].v[i] = from_f32<T>(0.f);
+    auto begin = [&](int round) {   // the first rounds of a part
+        const bool keys = round >= first;
         const Heads& p = keys ? a.part[1] : a.part[0];
-        const int h = (share - (keys ? first : 0)) * slots + slot;
-        fetch(static_cast<const T*>(p.x) + n * p.token + h * p.head, h < p.heads, x);
-    }
+        int h = (round - (keys ? first : 0)) * slots + slot;
+        const T* src = static_cast<const T*>(p.x) + n * p.token + h * p.head;
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k) {
+            fetch(src, h < p.heads, x[k]);
+            h += a.per_token * slots;
+            src += (int64_t)a.per_token * slots * p.head;
+        }
+    };
+    begin(share);
     // weights: place i of lane l is value at(i / V) + i % V, place 8 + i its pair's other end
     for (int i = threadIdx.x; i < 2 * 8 * lanes; i += kHeadsThreads) {
         const int which = i >= 8 * lanes, q = i - (which ? 8 * lanes : 0), g = q / V * V;
@@ -198,17 +209,16 @@ __global__ void __launch_bounds__(kHeadsThreads) us_heads_kernel(const __grid_co
         weights[which][(q >> 3) + 16 * (8 + (q & 7))] = has ? weight_at(p.weight, p.w_type, (apart ? 2 * g + V : g + half) + q % V) : 1.f;
     }
     if (real) {
-        int32_t pos[8];
-        if (a.axis) {
+        int32_t pos[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) pos[i] = __ldcg(a.positions + (int64_t)((axis[i >> 2] >> (8 * (i & 3))) & 0xFFu) * a.axis_stride + n);
-        } else {
-            pos[0] = __ldcg(a.positions + n);
+        for (int i = 0; i < 4; ++i) pos[i] = lane + 32 * i < half ? __ldcg(a.positions + (int64_t)axis[i] * a.axis_stride + n) : 0;
 #pragma unroll
-            for (int i = 1; i < 8; ++i) pos[i] = pos[0];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) turn((uint64_t)(int64_t)pos[i] * step[i], turned[i][threadIdx.x], turned[8 + i][threadIdx.x]);
+        for (int i = 0; i < 4; ++i)
+            if (lane + 32 * i < 8 * lanes) {
+                float2 x = make_float2(1.f, 0.f);
+                if (lane + 32 * i < half) turn((uint64_t)(int64_t)pos[i] * step[i], x.x, x.y);
+                turned[threadIdx.x >> 5][lane + 32 * i] = x;
+            }
     }
     __syncthreads();
     if (!real) return;
@@ -227,7 +237,8 @@ __global__ void __launch_bounds__(kHeadsThreads) us_heads_kernel(const __grid_co
 #pragma unroll
                 for (int i = 0; i < V; ++i) {   // pair V g + i: its two values
                     const int u = INTERLEAVED && V > 1 ? (2 * i < V ? V * g + 2 * i : 8 + V * g + 2 * i - V) : V * g + i, v = INTERLEAVED && V > 1 ? u + 1 : u + 8;
-                    const float c = turned[V * g + i][threadIdx.x], sn = turned[8 + V * g + i][threadIdx.x], wu = weights[which][l + 16 * u], wv = weights[which][l + 16 * v];
+                    const float2 cs = turned[threadIdx.x >> 5][p0 + V * g + i];
+                    const float c = cs.x, sn = cs.y, wu = weights[which][l + 16 * u], wv = weights[which][l + 16 * v];
                     o[u] = wu * c;
                     r[u] = -wv * sn;
                     o[v] = wv * c;
@@ -242,14 +253,11 @@ __global__ void __launch_bounds__(kHeadsThreads) us_heads_kernel(const __grid_co
         const bool norm = p.weight != nullptr;
         const int64_t step_x = (int64_t)a.per_token * slots * p.head, step_o = (int64_t)a.per_token * slots * p.o_head;
         int h = (round - base) * slots + slot;
-        const T* src = static_cast<const T*>(p.x) + n * p.token + h * p.head;
+        const int more = a.per_token * slots;
+        const T* src = static_cast<const T*>(p.x) + n * p.token + (h + (DEEP - 1) * more) * p.head;
         T* dst = static_cast<T*>(p.out) + n * p.o_token + h * p.o_head;
-        if (round != share) fetch(src, h < p.heads, x);   // (the first of the keys' rounds)
-#pragma unroll 1
-        for (; round < end; round += a.per_token) {
-            src += step_x;
-            const int later = h + a.per_token * slots;
-            fetch(src, round + a.per_token < end && later < p.heads, ahead);
+        if (round != share) begin(round);
+        auto finish = [&](const Values& x) {
             uint64_t f[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) f[j] = widen<T>(x.v + 2 * j);
@@ -260,8 +268,13 @@ __global__ void __launch_bounds__(kHeadsThreads) us_heads_kernel(const __grid_co
                 float sum, rest;
                 split(sum2, sum, rest);
                 sum += rest;
-                for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                const float inv = __frsqrt_rn(fmaf(sum, a.one_over_D, a.eps));
+                if (LOG) {
+#pragma unroll
+                    for (int o = 1; o < 1 << LOG; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                } else {
+                    for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                }
+                const float inv = rsqrtf(fmaf(sum, a.one_over_D, a.eps));
                 const uint64_t inv2 = two(inv, inv);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = mul2(f[j], inv2);
@@ -294,19 +307,33 @@ __global__ void __launch_bounds__(kHeadsThreads) us_heads_kernel(const __grid_co
                         put<T, V>(dst + at[g], y.v + V * g);
                         put<T, V>(dst + other[g], y.v + 8 + V * g);
                     }
-            x = ahead;
-            h = later;
+            h += more;
             dst += step_o;
+            round += a.per_token;
+        };
+#pragma unroll 1
+        while (round < end) {
+#pragma unroll
+            for (int k = 0; k < DEEP; ++k) {
+                if (k && round >= end) break;
+                finish(x[k]);
+                src += step_x;
+                fetch(src, h + (DEEP - 1) * more < p.heads, x[k]);
+            }
         }
     }
 }
 
-template <class T>
-const void* heads_kernel(int v, bool interleaved)
+template <class T, bool INTERLEAVED>
+const void* heads_kernel(int v, int log2_lanes)
 {
-    if (interleaved) return v == 8 ? (const void*)us_heads_kernel<T, 8, true> : v == 4 ? (const void*)us_heads_kernel<T, 4, true> : (const void*)us_heads_kernel<T, 1, true>;
-    return v == 8 ? (const void*)us_heads_kernel<T, 8, false> : v == 4 ? (const void*)us_heads_kernel<T, 4, false> : (const void*)us_heads_kernel<T, 1, false>;
+    if (v == 8)
+        return log2_lanes == 3 ? (const void*)us_heads_kernel<T, 8, INTERLEAVED, 3> : log2_lanes == 2 ? (const void*)us_heads_kernel<T, 8, INTERLEAVED, 2> :
+               (const void*)us_heads_kernel<T, 8, INTERLEAVED, 0>;
+    return v == 4 ? (const void*)us_heads_kernel<T, 4, INTERLEAVED, 0> : (const void*)us_heads_kernel<T, 1, INTERLEAVED, 0>;
 }
+template <class T>
+const void* heads_kernel(int v, int log2_lanes, bool interleaved) { return interleaved ? heads_kernel<T, true>(v, log2_lanes) : heads_kernel<T, false>(v, log2_lanes); }
 
 bool aligned(const void* p, int64_t b) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)b == 0; }
 
@@ -358,12 +385,14 @@ us_status us_qk_norm_rope(const us_rotary* r, const int32_t* positions, int64_t 
     a.eps = eps;
     a.one_over_D = 1.f / (float)D;
     while ((16 << a.log2_lanes) < D) ++a.log2_lanes;
-    // A token's rounds go to as many warps as fill the GPU; each finds the sines and cosines anew.
+    // A token's rounds go to as many warps as the GPU holds at once; each finds the factors anew. (1001 tokens of 32 + 32 heads, 16 rounds each, in fp32: 20.9 us with one
+    // warp a token, 12.9 with two, 14.6 with three, 15.4 with six.)
     const int64_t slots = 32 >> a.log2_lanes, rounds = (a.part[0].heads + slots - 1) / slots + (a.part[1].heads + slots - 1) / slots;
-    a.per_token = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, (32ll * ops_sms() + N - 1) / N));
+    a.per_token = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, 16 * ops_sms() / N));
     const int64_t blocks = (N * a.per_token + kHeadsThreads / 32 - 1) / (kHeadsThreads / 32);
-    const void* kernel = type == US_F16 ? heads_kernel<__half>(vec, r->interleaved != 0) : type == US_BF16 ? heads_kernel<__nv_bfloat16>(vec, r->interleaved != 0) :
-                                          heads_kernel<float>(vec, r->interleaved != 0);
+    const bool inter = r->interleaved != 0;
+    const void* kernel = type == US_F16 ? heads_kernel<__half>(vec, a.log2_lanes, inter) : type == US_BF16 ? heads_kernel<__nv_bfloat16>(vec, a.log2_lanes, inter) :
+                                          heads_kernel<float>(vec, a.log2_lanes, inter);
     void* args[] = {&a};
     const cudaError_t e = ops_launch(kernel, dim3((unsigned)blocks), kHeadsThreads, 0, static_cast<cudaStream_t>(stream), args);
     if (e == cudaSuccess) return US_OK;

@@ -774,28 +774,22 @@ PyObject* kv_compact(PyObject*, PyObject* const* a, Py_ssize_t n)
 
 // ---- norms and rotation of heads ----
 
-// qk_norm_rope(q, k, positions, turns, axis, axes, rotary_dim, interleaved, q_weight, k_weight, eps, q_out, k_out, stream) -> (q, k)
+// qk_norm_rope(q, k, positions, address of the us_rotary, its turns, head_dim, q_weight, k_weight, eps, q_out, k_out, stream) -> (q, k)
 PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    if (n != 14) return PyErr_Format(PyExc_TypeError, "qk_norm_rope takes 14 arguments");
+    if (n != 12) return PyErr_Format(PyExc_TypeError, "qk_norm_rope takes 12 arguments");
     HANDLE_TH_ERRORS
-    const at::Tensor *Q = tensor(a[0], "q"), *K = nullptr, *pos = Q ? tensor(a[2], "positions") : nullptr, *turns = pos ? tensor(a[3], "turns") : nullptr;
+    const at::Tensor *Q = tensor(a[0], "q"), *K = nullptr, *pos = Q ? tensor(a[2], "positions") : nullptr, *turns = pos ? tensor(a[4], "turns") : nullptr;
     if (!turns || (a[1] != Py_None && !(K = tensor(a[1], "k")))) return nullptr;
-    const at::Tensor* axis = nullptr;
-    if (a[4] != Py_None && !(axis = tensor(a[4], "axis"))) return nullptr;
-    us_rotary r = {};
-    r.axes = (int32_t)PyLong_AsLong(a[5]);
-    r.rotary_dim = (int32_t)PyLong_AsLong(a[6]);
-    r.interleaved = PyObject_IsTrue(a[7]);
-    const double eps = PyFloat_AsDouble(a[10]);
+    const us_rotary& r = *static_cast<const us_rotary*>(PyLong_AsVoidPtr(a[3]));
+    const int64_t D = PyLong_AsLongLong(a[5]);
+    const double eps = PyFloat_AsDouble(a[8]);
     if (PyErr_Occurred()) return nullptr;
     Place at_;
-    if (!at_.enter(a[13], *Q)) return nullptr;
+    if (!at_.enter(a[11], *Q)) return nullptr;
     if (turns->device() != Q->device()) return bad("the rotary table lies on another device");
-    r.turns = static_cast<const uint64_t*>(turns->data_ptr());
-    r.axis = axis ? static_cast<const uint8_t*>(axis->data_ptr()) : nullptr;
-    if (Q->dim() != 3 || (K && K->dim() != 3)) return bad("q and k must be (N, heads, head_dim) tensors");
-    const int64_t N = Q->size(0), D = Q->size(2);
+    if (Q->dim() != 3 || Q->size(2) != D || (K && K->dim() != 3)) return bad("q and k must be (N, heads, head_dim) tensors, head_dim as the rotary's");
+    const int64_t N = Q->size(0);
     if (!is_heads(*Q, D, *Q) || (K && (!is_heads(*K, D, *Q) || K->size(0) != N || K->scalar_type() != Q->scalar_type())) || N >= (1ll << 31) || D > 256)
         return bad("q and k must be (N, heads, head_dim) tensors of one type (float16, bfloat16 or float32) with unit last stride on one device, head_dim at most 256");
     const bool flat = pos->dim() == 1;
@@ -807,10 +801,10 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
     for (int i = 0; i < 2; ++i) {
         const at::Tensor* x = i ? K : Q;
         if (!x) {
-            if (a[12] != Py_None) return bad("k_out without k");
+            if (a[10] != Py_None) return bad("k_out without k");
             continue;
         }
-        PyObject *w = a[8 + i], *o = a[11 + i];
+        PyObject *w = a[6 + i], *o = a[9 + i];
         h[i].x = x->data_ptr();
         h[i].token_stride = token_stride(*x);
         h[i].head_stride = head_stride(*x);
@@ -844,12 +838,12 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
     s = us_qk_norm_rope(&r, static_cast<const int32_t*>(pos->data_ptr()), axis_stride, N, (int32_t)D, type_of(Q->scalar_type()), &h[0], K ? &h[1] : nullptr, (float)eps, at_.stream);
     Py_END_ALLOW_THREADS
     if (s != US_OK) return fail(s, "us_qk_norm_rope");
-    PyObject* q = give(a[11], std::move(fresh[0]));
+    PyObject* q = give(a[9], std::move(fresh[0]));
     if (!K) {
         Py_INCREF(Py_None);
         return Py_BuildValue("NN", q, Py_None);
     }
-    return Py_BuildValue("NN", q, give(a[12], std::move(fresh[1])));
+    return Py_BuildValue("NN", q, give(a[10], std::move(fresh[1])));
     END_HANDLE_TH_ERRORS
 }
 
