@@ -567,7 +567,8 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
     // The kernel that joins the parts may start once this one's CTAs are past the wait: it reads lengths and token counts before its own.
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // (kOwn: started behind the groups' kernels, whose blocks are all past that wait: what they wait for is complete, their rows are waited for below.)
+    if (MODE != kOwn) asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const KvPool& p = a.pool;
     const KvRange range = kv_range<R, MODE>(a, blockIdx.x, lane, warp == 0);
@@ -920,6 +921,26 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                 ok = false;
                 break;
             }
+            const bool whole = n == it.tiles;
+            // (kOwn) the rows of the prefix, on their way while the warps' sums are put together: a thread has one of D of every row, or of every second
+            constexpr int PRE = MODE == kOwn ? R * D / 128 : 1;
+            float pre[PRE];
+            float2 pre_stat[PRE];
+            bool joined = false;
+            if constexpr (MODE == kOwn) {
+                if (whole) asm volatile("griddepcontrol.wait;" ::: "memory");
+                joined = whole && kv_has_prefix<MODE>(a.rows, s, it.seq.len);
+#pragma unroll
+                for (int k = 0; k < PRE; ++k) {
+                    const int r = row0 + k * (128 / D) + (int)threadIdx.x / D;
+                    if (joined && r < it.rows) {
+                        const int tok = r / a.G, qh = h * a.G + r - tok * a.G;
+                        const float* row = a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+                        pre[k] = __ldcg(row + threadIdx.x % D);
+                        pre_stat[k] = __ldcg(reinterpret_cast<const float2*>(row + D));
+                    }
+                }
+            }
             // each in turn adds what it has, relative to the largest maximum; place (2 j + e) * 8 + g of a row holds
             // d = (D / 8) g + 2 j + e, so that a warp's 32 accesses meet 32 banks
             float w[NT][2];
@@ -960,23 +981,24 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                             }
                 bar_consumers();
             }
-            const bool whole = n == it.tiles;
             float* part = a.part + ((int64_t)blockIdx.x * 2 + (tile == 0 ? 1 : 0)) * S::kPart;   // 1: the item begins here
             const int rows = min(R, it.rows - row0);
-            const bool joined = whole && kv_has_prefix<MODE>(a.rows, s, it.seq.len);
-            for (int i = threadIdx.x; i < rows * D; i += 128) {
+#pragma unroll(MODE == kOwn ? PRE : 1)
+            for (int k = 0; k < (MODE == kOwn ? PRE : R * D / 128); ++k) {
+                const int i = (int)threadIdx.x + 128 * k;
+                if (i >= rows * D) break;
                 const int r = i / D, d = i - r * D;
                 float big = stats[4 * R + r].x, sum = stats[4 * R + r].y;
                 float acc = sums[r * S::kPitch + (d % (D / 8)) * 8 + d / (D / 8)];
                 if (whole) {
                     const int tok = (row0 + r) / a.G, qh = h * a.G + (row0 + r) - tok * a.G;
-                    float* row = MODE == kAlone ? nullptr : a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
                     if (MODE == kGroups) {
+                        float* row = a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
                         row[d] = acc;
                         if (d == 0) *reinterpret_cast<float2*>(row + D) = make_float2(big, sum);
                         continue;
                     }
-                    if (MODE == kOwn && joined) kv_add_part(big, sum, acc, __ldcg(reinterpret_cast<const float2*>(row + D)), __ldcg(row + d));
+                    if (MODE == kOwn && joined) kv_add_part(big, sum, acc, pre_stat[MODE == kOwn ? k : 0], pre[MODE == kOwn ? k : 0]);
                     o_put<BF16>(a.out, (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + d, sum == 0.f ? 0.f : acc / sum);
                     if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(big, sum);
                 } else {
@@ -998,6 +1020,8 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
         *dead = 1;
         atomicExch(p.err, kErrTimeout);
     }
+    // (what follows in the stream waits for this grid, or for the one that joins its parts: it may not end before the groups' kernels)
+    if (MODE == kOwn) asm volatile("griddepcontrol.wait;" ::: "memory");
     __syncthreads();
 }
 

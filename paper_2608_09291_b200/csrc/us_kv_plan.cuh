@@ -24,6 +24,7 @@ inline bool rows_vec(const void* x, int32_t type, int64_t token, int64_t head)
 struct AttendPlan {
     const void *kernel, *join;
     int rows, stages, smem, ctas;
+    int join_blocks;   // (prompts) of a row tile and head
     int splits;        // (prompts) of the cache's length
     int64_t tiles;     // (prompts) row tiles, at most; 0: the kernel for few rows
     int64_t scratch;
@@ -33,7 +34,9 @@ AttendPlan prompt_shape(int64_t N, int64_t S, int64_t G, int64_t Hkv, int64_t lo
 {
     AttendPlan p = {};
     p.kernel = (const void*)us_kv_prompt_kernel<D, BF16, MODE>;
-    p.join = (const void*)us_kv_prompt_join_kernel<D, BF16, MODE>;
+    if constexpr (MODE == kGroups) p.join = (const void*)us_kv_rows_join_kernel<D>;
+    else p.join = (const void*)us_kv_prompt_join_kernel<D, BF16, MODE>;
+    p.join_blocks = MODE == kGroups ? D / 4 : D / 16;
     p.smem = PrShape<D>::kSmem;
     p.tiles = N * G / kPrRows + S;
     // a tile's walk over the cache is split where the tiles would leave SMs idle, in parts of at least four units
@@ -100,7 +103,7 @@ inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, cons
 {
     const int64_t G = x.heads / h->pool.Hkv;
     if (pl.tiles > 0) {
-        const int64_t blocks = pl.tiles * h->pool.Hkv * std::max(pl.splits, h->pool.D / 16);
+        const int64_t blocks = pl.tiles * h->pool.Hkv * std::max(pl.splits, pl.join_blocks);
         if (blocks >= (1ll << 31)) return US_ERR_UNSUPPORTED;
         KvPrompt a = {};
         a.pool = h->pool;
@@ -124,7 +127,7 @@ inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, cons
         cudaError_t e = ops_kernel_allow(pl.kernel, pl.smem);
         const int threads = PrShape<128>::kThreads;
         if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.splits)), threads, pl.smem, st, args);
-        if (e == cudaSuccess && pl.splits > 1) e = ops_launch(pl.join, dim3((unsigned)(pl.tiles * h->pool.Hkv * (h->pool.D / 16))), kPrRows, 0, st, args);
+        if (e == cudaSuccess && pl.splits > 1) e = ops_launch(pl.join, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.join_blocks)), kPrRows, 0, st, args);
         return kv_cuda(e);
     }
     if (!kv_maps(h)) return US_ERR_CUDA;

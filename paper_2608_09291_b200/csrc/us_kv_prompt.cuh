@@ -691,14 +691,8 @@ __global__ void __launch_bounds__(kPrRows) us_kv_prompt_join_kernel(const __grid
         }
     }
     const int r = it.row0 + local, tok = r / a.G, qh = h * a.G + r - tok * a.G;
-    if (MODE != kAlone) {
-        float* row = a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
-        if (MODE == kGroups) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(row + 4 * (c0 + i)) = acc[i];
-            if (c0 == 0) *reinterpret_cast<float2*>(row + D) = make_float2(big, sum);
-            return;
-        }
+    if (MODE == kOwn) {
+        const float* row = a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
         if (kv_has_prefix<MODE>(a.rows, it.s, it.seq.len)) {
             const float2 stat = __ldcg(reinterpret_cast<const float2*>(row + D));
             const float own = big, own_sum = sum;
@@ -722,6 +716,51 @@ __global__ void __launch_bounds__(kPrRows) us_kv_prompt_join_kernel(const __grid
         o_put<BF16>(a.out, at + 4 * i + 3, sum == 0.f ? 0.f : acc[i].w / sum);
     }
     if (a.lse && c0 == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(big, sum);
+}
+
+// (kGroups) The same into the rows: a thread a row, four of D a block, all parts' loads at once (64 sequences' rows of 64 heads, nine parts each: MEASURED).
+template <int D>
+__global__ void __launch_bounds__(kPrRows) us_kv_rows_join_kernel(const __grid_constant__ KvPrompt a)
+{
+    using S = PrShape<D>;
+    constexpr int MOST = 16;   // parts
+    const int lane = threadIdx.x & 31, local = threadIdx.x, c = (int)(blockIdx.x % (D / 4));
+    const uint32_t u = blockIdx.x / (D / 4), index = u / (uint32_t)a.pool.Hkv;
+    const int h = (int)(u - index * a.pool.Hkv);
+    PrItem it;
+    const bool have = pr_item<kGroups>(a, index, lane, it, false);   // (complete, as above)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!have || local >= it.rows) return;
+    const float* part = a.part + (int64_t)u * a.splits * S::kPart;
+    float m[MOST], l[MOST];
+    float4 x[MOST];
+#pragma unroll
+    for (int s = 0; s < MOST; ++s) {
+        m[s] = -INFINITY;
+        l[s] = 0.f;
+        x[s] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (s < a.splits) {
+            m[s] = __ldcg(part + s * S::kPart + kPrRows * D + local);
+            l[s] = __ldcg(part + s * S::kPart + kPrRows * D + kPrRows + local);
+            x[s] = __ldcg(reinterpret_cast<const float4*>(part + s * S::kPart + (c * kPrRows + local) * 4));
+        }
+    }
+    float big = -INFINITY, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int s = 0; s < MOST; ++s) big = fmaxf(big, m[s]);
+#pragma unroll
+    for (int s = 0; s < MOST; ++s) {
+        const float w = kv_weight(m[s], l[s], big == -INFINITY ? 0.f : big);
+        sum += w * l[s];          // (a part that is NaN has no maximum, and so no weight: its NaN comes from here)
+        if (w == 0.f) continue;   // (a part without units has no sums)
+        acc.x += w * x[s].x; acc.y += w * x[s].y; acc.z += w * x[s].z; acc.w += w * x[s].w;
+    }
+    const int r = it.row0 + local, tok = r / a.G, qh = h * a.G + r - tok * a.G;
+    float* row = a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+    *reinterpret_cast<float4*>(row + 4 * c) = acc;
+    if (c == 0) *reinterpret_cast<float2*>(row + D) = make_float2(big, sum);
 }
 
 }  // namespace us
