@@ -536,6 +536,227 @@ __device__ __forceinline__ void kv_add_part(float& big, float& sum, float& acc, 
     big = top;
 }
 
+// 32 tokens of a warp, from tok0 on: scores, softmax and sums of 8 NT rows (see below). load_k gives a lane 16 bytes of each of tokens g and g + 8 of group b (D / 64 such
+// pieces), load_v the lane's D / 8 columns of token 2 t, 2 t + 1, 2 t + 8 or 2 t + 9 (q). edge: some row does not see all of them; a group that is not there has
+// a step of -1.
+template <int D, int NT, bool BF16, class LoadK, class LoadV>
+__device__ __forceinline__ void kv_step(LoadK load_k, LoadV load_v, const uint32_t (&qf)[NT][D / 16][2], const float (&f)[NT][2], const int (&lo)[NT][2], const int (&hi)[NT][2],
+                                        const float (&stk)[2], const float (&stv)[2], bool edge, int tok0, int g, float (&m)[NT][2], float (&r)[NT][2], float (&l)[NT][2],
+                                        float (&o)[D / 16][NT][4])
+{
+    constexpr int MT = D / 16;
+    float sc[2][NT][4];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sc[b][nt][c] = 0.f;
+    // scores: two times 16 tokens x 8 NT rows
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+        uint32_t xs[2][4], ys[2][4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            uint4 x, y;
+            load_k(b, c, x, y);
+            xs[b][0] = x.x; xs[b][1] = x.y; xs[b][2] = x.z; xs[b][3] = x.w;
+            ys[b][0] = y.x; ys[b][1] = y.y; ys[b][2] = y.z; ys[b][3] = y.w;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const uint32_t xw = xs[b][j] ^ 0x80808080u, yw = ys[b][j] ^ 0x80808080u;
+                const uint32_t a0 = f16_low(xw), a1 = f16_low(yw), a2 = f16_high(xw), a3 = f16_high(yw);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_f16(sc[b][nt], a0, a1, a2, a3, qf[nt][4 * c + j][0], qf[nt][4 * c + j][1]);
+            }
+    }
+    // e = s - m + 7: more than 15 where m is more than 2^8 behind (or nothing was seen yet), or with V's step and r added
+    const float lv[2] = {kv_log2_above(stv[0]), kv_log2_above(stv[1])};
+    float e[2][NT][4];
+    bool behind = false;
+    auto exponents = [&]() {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) e[b][nt][c] = fmaf(sc[b][nt][c], f[nt][c & 1] * stk[b], 7.f - m[nt][c & 1]);
+        if (edge)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int tk = tok0 + 16 * b + g + 8 * (c >> 1);
+                        if (tk < lo[nt][c & 1] || tk >= hi[nt][c & 1] || stk[b] < 0.f) e[b][nt][c] = -INFINITY;
+                    }
+    };
+    exponents();
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) behind |= e[b][nt][c] > fminf(15.f, 15.f - (lv[b] + r[nt][c & 1]));
+    if (__any_sync(0xffffffffu, behind)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float x = -INFINITY, y = -INFINITY;   // largest scores, and with V's steps
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        if (e[b][nt][c + 2 * q] > -INFINITY) {
+                            const float sco = sc[b][nt][c + 2 * q] * (f[nt][c] * stk[b]);
+                            x = fmaxf(x, sco);
+                            y = fmaxf(y, sco + lv[b]);
+                        }
+#pragma unroll
+                for (int i = 4; i <= 16; i *= 2) {
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, i));
+                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, i));
+                }
+                x = fmaxf(x, m[nt][c]);
+                y = fmaxf(y, m[nt][c] - r[nt][c]);
+                const float rn = x == -INFINITY ? 0.f : fmaxf(x - y, -126.f);   // (at most 126: kv_log2_above)
+                const float by = x == -INFINITY ? 0.f : m[nt][c] - x, alpha = exp2_fast(by + (rn - r[nt][c]));
+                l[nt][c] *= exp2_fast(by);
+                m[nt][c] = x;
+                r[nt][c] = rn;
+#pragma unroll
+                for (int k = 0; k < MT; ++k) { o[k][nt][c] *= alpha; o[k][nt][c + 2] *= alpha; }
+            }
+        exponents();
+    }
+    // (fp16 output: what the rounding of p leaves is multiplied, too; else its 2^-12 would be as much as the output's own: an error
+    // of 2.9e-4 against 64 bits, 2.1e-4 with it. 64 sequences of up to 8192 tokens, 16 rows a cache head: 171 us without, 182 with.
+    // bf16's own rounding is eight times as large: 1.7e-3 either way)
+    constexpr bool REST = !BF16;
+    uint32_t pf[2][NT][2], pr[2][NT][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float rel[2];   // V's step for each row; where a row sees none of the group 0, whatever the step is
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                rel[c] = stv[b] * exp2_fast(r[nt][c]);
+                if (edge && (tok0 + 16 * b >= hi[nt][c] || tok0 + 16 * b + 16 <= lo[nt][c] || stk[b] < 0.f)) rel[c] = 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                e[b][nt][c] = exp2_fast(e[b][nt][c]);
+                l[nt][c & 1] += e[b][nt][c];
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float p0 = e[b][nt][2 * c] * rel[0], p1 = e[b][nt][2 * c + 1] * rel[1];
+                const uint32_t h = half2_bits(p0, p1);
+                pf[b][nt][c] = transpose8(h);
+                if (REST) {
+                    const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                    pr[b][nt][c] = transpose8(half2_bits(p0 - r.x, p1 - r.y));
+                }
+            }
+        }
+    }
+    // sums: 16 of D x 8 NT rows at a time; a lane holds the same D columns of its four tokens
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        uint32_t w[4][D / 32];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load_v(b, q, w[q]);
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            const uint32_t x0 = prmt(w[0][k], w[1][k], 0x5140u) ^ 0x80808080u, x1 = prmt(w[0][k], w[1][k], 0x7362u) ^ 0x80808080u;
+            const uint32_t y0 = prmt(w[2][k], w[3][k], 0x5140u) ^ 0x80808080u, y1 = prmt(w[2][k], w[3][k], 0x7362u) ^ 0x80808080u;
+            const uint32_t a0 = f16_low(x0), a1 = f16_high(x0), a2 = f16_low(y0), a3 = f16_high(y0);
+            const uint32_t b0 = f16_low(x1), b1 = f16_high(x1), b2 = f16_low(y1), b3 = f16_high(y1);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                mma_f16(o[2 * k][nt], a0, a1, a2, a3, pf[b][nt][0], pf[b][nt][1]);
+                mma_f16(o[2 * k + 1][nt], b0, b1, b2, b3, pf[b][nt][0], pf[b][nt][1]);
+                if (REST) {
+                    mma_f16(o[2 * k][nt], a0, a1, a2, a3, pr[b][nt][0], pr[b][nt][1]);
+                    mma_f16(o[2 * k + 1][nt], b0, b1, b2, b3, pr[b][nt][0], pr[b][nt][1]);
+                }
+            }
+        }
+    }
+}
+
+// The query rows row0 .. of an item as fragments: rows g of every 8, the lane's D/4 columns (t); fp16 times a power of two that brings bf16 into range. Of rows 2 t and
+// 2 t + 1: the scores' factors, and the first token that they see and the one behind the last.
+template <int D, int NT, bool BF16>
+__device__ __forceinline__ void kv_queries(const KvAttend& a, const KvItem& it, int row0, int h, int g, int t, uint32_t (&qf)[NT][D / 16][2], float (&f)[NT][2], int (&lo)[NT][2],
+                                           int (&hi)[NT][2])
+{
+    constexpr int KS = D / 16;
+    const int pos0 = it.seq.len - it.seq.n;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int r = row0 + 8 * nt + g;
+        float v[D / 4];
+        const bool in = r < it.rows;
+        const int tok = in ? r / a.G : 0, qh = h * a.G + (in ? r - tok * a.G : 0);
+        const int64_t at = (it.seq.first + tok) * a.q_token + (int64_t)qh * a.q_head + t * (D / 4);
+        if (in && a.q_vec) {
+            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + at);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                const uint4 w = __ldcg(src + i);
+                const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (BF16) {
+                        v[8 * i + 2 * j] = __uint_as_float(ww[j] << 16);
+                        v[8 * i + 2 * j + 1] = __uint_as_float(ww[j] & 0xFFFF0000u);
+                    } else {
+                        const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&ww[j]));
+                        v[8 * i + 2 * j] = u.x;
+                        v[8 * i + 2 * j + 1] = u.y;
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < D / 4; ++i) v[i] = in ? q_at<BF16>(a.q, at + i) : 0.f;
+        }
+        float mul = 1.f, back = 1.f;
+        if (BF16) {
+            uint32_t big = 0;
+#pragma unroll
+            for (int i = 0; i < D / 4; ++i) big = max(big, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+            // largest magnitude in [2^14, 2^15); exponents so that both factors are normal numbers
+            const int e = max(-112, min(114, (int)(big >> 23) - 127 - 14));
+            mul = __uint_as_float((uint32_t)(127 - e) << 23);
+            back = __uint_as_float((uint32_t)(127 + e) << 23);
+        }
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+            qf[nt][j][0] = half2_bits(v[4 * j] * mul, v[4 * j + 1] * mul);
+            qf[nt][j][1] = half2_bits(v[4 * j + 2] * mul, v[4 * j + 3] * mul);
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            f[nt][c] = __shfl_sync(0xffffffffu, back, 4 * (2 * t + c)) * a.scale2;
+            const int rr = row0 + 8 * nt + 2 * t + c;
+            const int pos = pos0 + rr / a.G;
+            const bool real = rr < it.rows;   // (rows past the last are zero queries that see everything; never stored)
+            hi[nt][c] = real ? (a.causal ? pos + 1 : it.seq.len) : 0x7FFFFFFF;
+            lo[nt][c] = real && a.window > 0 ? pos - a.window + 1 : -0x7FFFFFFF;
+        }
+    }
+}
+
 template <int D, int NT>
 struct KvShape {
     static constexpr int R = 8 * NT;
@@ -661,62 +882,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
             float f[NT][2];
             int lo[NT][2], hi[NT][2];
             const int pos0 = it.seq.len - it.seq.n;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const int r = row0 + 8 * nt + g;
-                float v[D / 4];
-                const bool in = r < it.rows;
-                const int tok = in ? r / a.G : 0, qh = h * a.G + (in ? r - tok * a.G : 0);
-                const int64_t at = (it.seq.first + tok) * a.q_token + (int64_t)qh * a.q_head + t * (D / 4);
-                if (in && a.q_vec) {
-                    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + at);
-#pragma unroll
-                    for (int i = 0; i < D / 32; ++i) {
-                        const uint4 w = __ldcg(src + i);
-                        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (BF16) {
-                                v[8 * i + 2 * j] = __uint_as_float(ww[j] << 16);
-                                v[8 * i + 2 * j + 1] = __uint_as_float(ww[j] & 0xFFFF0000u);
-                            } else {
-                                const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&ww[j]));
-                                v[8 * i + 2 * j] = u.x;
-                                v[8 * i + 2 * j + 1] = u.y;
-                            }
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < D / 4; ++i) v[i] = in ? q_at<BF16>(a.q, at + i) : 0.f;
-                }
-                float mul = 1.f, back = 1.f;
-                if (BF16) {
-                    uint32_t big = 0;
-#pragma unroll
-                    for (int i = 0; i < D / 4; ++i) big = max(big, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-                    big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
-                    big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
-                    // largest magnitude in [2^14, 2^15); exponents so that both factors are normal numbers
-                    const int e = max(-112, min(114, (int)(big >> 23) - 127 - 14));
-                    mul = __uint_as_float((uint32_t)(127 - e) << 23);
-                    back = __uint_as_float((uint32_t)(127 + e) << 23);
-                }
-#pragma unroll
-                for (int j = 0; j < KS; ++j) {
-                    qf[nt][j][0] = half2_bits(v[4 * j] * mul, v[4 * j + 1] * mul);
-                    qf[nt][j][1] = half2_bits(v[4 * j + 2] * mul, v[4 * j + 3] * mul);
-                }
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    f[nt][c] = __shfl_sync(0xffffffffu, back, 4 * (2 * t + c)) * a.scale2;
-                    const int rr = row0 + 8 * nt + 2 * t + c;
-                    const int pos = pos0 + rr / a.G;
-                    const bool real = rr < it.rows;   // (rows past the last are zero queries that see everything; never stored)
-                    hi[nt][c] = real ? (a.causal ? pos + 1 : it.seq.len) : 0x7FFFFFFF;
-                    lo[nt][c] = real && a.window > 0 ? pos - a.window + 1 : -0x7FFFFFFF;
-                }
-            }
+            kv_queries<D, NT, BF16>(a, it, row0, h, g, t, qf, f, lo, hi);
             // tokens that no row sees are in front of it.lo or from the last row's bound on; all rows see [all_lo, all_hi)
             int all_lo = -0x7FFFFFFF, all_hi = 0x7FFFFFFF;
 #pragma unroll
@@ -747,160 +913,23 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                 if (tok0 + 32 > it.lo && tok0 < last_hi && !(st0.x < 0.f && st1.x < 0.f)) {
                     const bool edge = tok0 < all_lo || tok0 + 32 > all_hi || st0.x < 0.f || st1.x < 0.f;
                     const uint32_t kb = smem_u32(ring + (size_t)stage * S::kStage), vb = kb + S::kHalf;
-                    float sc[2][NT][4];
-#pragma unroll
-                    for (int b = 0; b < 2; ++b)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) sc[b][nt][c] = 0.f;
-                    // scores: two times 16 tokens x 8 NT rows
-#pragma unroll
-                    for (int c = 0; c < D / 64; ++c) {
-                        uint32_t xs[2][4], ys[2][4];
-#pragma unroll
-                        for (int b = 0; b < 2; ++b) {
+                    kv_step<D, NT, BF16>(
+                        [&](int b, int c, uint4& x, uint4& y) {
                             const int kr = 32 * warp + 16 * b + g, chunk = D == 128 ? ((2 * t + c) ^ (kr & 7)) : (t ^ ((kr >> 1) & 3));
-                            const uint4 x = lds128(kb + (uint32_t)(kr * D + 16 * chunk)), y = lds128(kb + (uint32_t)((kr + 8) * D + 16 * chunk));
-                            xs[b][0] = x.x; xs[b][1] = x.y; xs[b][2] = x.z; xs[b][3] = x.w;
-                            ys[b][0] = y.x; ys[b][1] = y.y; ys[b][2] = y.z; ys[b][3] = y.w;
-                        }
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-#pragma unroll
-                            for (int b = 0; b < 2; ++b) {
-                                const uint32_t xw = xs[b][j] ^ 0x80808080u, yw = ys[b][j] ^ 0x80808080u;
-                                const uint32_t a0 = f16_low(xw), a1 = f16_low(yw), a2 = f16_high(xw), a3 = f16_high(yw);
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) mma_f16(sc[b][nt], a0, a1, a2, a3, qf[nt][4 * c + j][0], qf[nt][4 * c + j][1]);
-                            }
-                    }
-                    // e = s - m + 7: more than 15 where m is more than 2^8 behind (or nothing was seen yet), or with V's step and r added
-                    const float lv[2] = {kv_log2_above(stv[0]), kv_log2_above(stv[1])};
-                    float e[2][NT][4];
-                    bool behind = false;
-                    auto exponents = [&]() {
-#pragma unroll
-                        for (int b = 0; b < 2; ++b)
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) e[b][nt][c] = fmaf(sc[b][nt][c], f[nt][c & 1] * stk[b], 7.f - m[nt][c & 1]);
-                        if (edge)
-#pragma unroll
-                            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                    for (int c = 0; c < 4; ++c) {
-                                        const int tk = tok0 + 16 * b + g + 8 * (c >> 1);
-                                        if (tk < lo[nt][c & 1] || tk >= hi[nt][c & 1] || stk[b] < 0.f) e[b][nt][c] = -INFINITY;
-                                    }
-                    };
-                    exponents();
-#pragma unroll
-                    for (int b = 0; b < 2; ++b)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) behind |= e[b][nt][c] > fminf(15.f, 15.f - (lv[b] + r[nt][c & 1]));
-                    if (__any_sync(0xffffffffu, behind)) {
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                float x = -INFINITY, y = -INFINITY;   // largest scores, and with V's steps
-#pragma unroll
-                                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                                    for (int q = 0; q < 2; ++q)
-                                        if (e[b][nt][c + 2 * q] > -INFINITY) {
-                                            const float sco = sc[b][nt][c + 2 * q] * (f[nt][c] * stk[b]);
-                                            x = fmaxf(x, sco);
-                                            y = fmaxf(y, sco + lv[b]);
-                                        }
-#pragma unroll
-                                for (int i = 4; i <= 16; i *= 2) {
-                                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, i));
-                                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, i));
-                                }
-                                x = fmaxf(x, m[nt][c]);
-                                y = fmaxf(y, m[nt][c] - r[nt][c]);
-                                const float rn = x == -INFINITY ? 0.f : fmaxf(x - y, -126.f);   // (at most 126: kv_log2_above)
-                                const float by = x == -INFINITY ? 0.f : m[nt][c] - x, alpha = exp2_fast(by + (rn - r[nt][c]));
-                                l[nt][c] *= exp2_fast(by);
-                                m[nt][c] = x;
-                                r[nt][c] = rn;
-#pragma unroll
-                                for (int k = 0; k < MT; ++k) { o[k][nt][c] *= alpha; o[k][nt][c + 2] *= alpha; }
-                            }
-                        exponents();
-                    }
-                    // (fp16 output: what the rounding of p leaves is multiplied, too; else its 2^-12 would be as much as the output's own: an error
-                    // of 2.9e-4 against 64 bits, 2.1e-4 with it. 64 sequences of up to 8192 tokens, 16 rows a cache head: 171 us without, 182 with.
-                    // bf16's own rounding is eight times as large: 1.7e-3 either way)
-                    constexpr bool REST = !BF16;
-                    uint32_t pf[2][NT][2], pr[2][NT][2];
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            float rel[2];   // V's step for each row; where a row sees none of the group 0, whatever the step is
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                rel[c] = stv[b] * exp2_fast(r[nt][c]);
-                                if (edge && (tok0 + 16 * b >= hi[nt][c] || tok0 + 16 * b + 16 <= lo[nt][c] || stk[b] < 0.f)) rel[c] = 0.f;
-                            }
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                e[b][nt][c] = exp2_fast(e[b][nt][c]);
-                                l[nt][c & 1] += e[b][nt][c];
-                            }
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                const float p0 = e[b][nt][2 * c] * rel[0], p1 = e[b][nt][2 * c + 1] * rel[1];
-                                const uint32_t h = half2_bits(p0, p1);
-                                pf[b][nt][c] = transpose8(h);
-                                if (REST) {
-                                    const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&h));
-                                    pr[b][nt][c] = transpose8(half2_bits(p0 - r.x, p1 - r.y));
-                                }
-                            }
-                        }
-                    }
-                    // sums: 16 of D x 8 NT rows at a time; a lane holds the same D columns of its four tokens
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const int v0 = 32 * warp + 16 * b + 2 * t;
-                        uint32_t w[4][D / 32];
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int r = v0 + (q & 1) + 8 * (q >> 1);
+                            x = lds128(kb + (uint32_t)(kr * D + 16 * chunk));
+                            y = lds128(kb + (uint32_t)((kr + 8) * D + 16 * chunk));
+                        },
+                        [&](int b, int q, uint32_t (&w)[D / 32]) {
+                            const int r = 32 * warp + 16 * b + 2 * t + (q & 1) + 8 * (q >> 1);
                             if (D == 128) {
                                 const uint4 x = lds128(vb + (uint32_t)(r * D + 16 * (g ^ (r & 7))));
-                                w[q][0] = x.x; w[q][1] = x.y; w[q][D / 32 - 2] = x.z; w[q][D / 32 - 1] = x.w;
+                                w[0] = x.x; w[1] = x.y; w[D / 32 - 2] = x.z; w[D / 32 - 1] = x.w;
                             } else {
                                 const uint2 x = lds64(vb + (uint32_t)(r * D + 16 * ((g >> 1) ^ ((r >> 1) & 3)) + 8 * (g & 1)));
-                                w[q][0] = x.x; w[q][1] = x.y;
+                                w[0] = x.x; w[1] = x.y;
                             }
-                        }
-#pragma unroll
-                        for (int k = 0; k < D / 32; ++k) {
-                            const uint32_t x0 = prmt(w[0][k], w[1][k], 0x5140u) ^ 0x80808080u, x1 = prmt(w[0][k], w[1][k], 0x7362u) ^ 0x80808080u;
-                            const uint32_t y0 = prmt(w[2][k], w[3][k], 0x5140u) ^ 0x80808080u, y1 = prmt(w[2][k], w[3][k], 0x7362u) ^ 0x80808080u;
-                            const uint32_t a0 = f16_low(x0), a1 = f16_high(x0), a2 = f16_low(y0), a3 = f16_high(y0);
-                            const uint32_t b0 = f16_low(x1), b1 = f16_high(x1), b2 = f16_low(y1), b3 = f16_high(y1);
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                mma_f16(o[2 * k][nt], a0, a1, a2, a3, pf[b][nt][0], pf[b][nt][1]);
-                                mma_f16(o[2 * k + 1][nt], b0, b1, b2, b3, pf[b][nt][0], pf[b][nt][1]);
-                                if (REST) {
-                                    mma_f16(o[2 * k][nt], a0, a1, a2, a3, pr[b][nt][0], pr[b][nt][1]);
-                                    mma_f16(o[2 * k + 1][nt], b0, b1, b2, b3, pr[b][nt][0], pr[b][nt][1]);
-                                }
-                            }
-                        }
-                    }
+                        },
+                        qf, f, lo, hi, stk, stv, edge, tok0, g, m, r, l, o);
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(b_empty + 8u * stage);
@@ -970,21 +999,29 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
             for (int turn = 0; turn < 4; ++turn) {
                 if (warp == turn)
 #pragma unroll
-                    for (int k = 0; k < MT; ++k)
+                    for (int nt = 0; nt < NT; ++nt) {
+                        // (all loads before the first store: a store might be to what a later load reads, for all that is known here)
+                        float* base[2] = {sums + (8 * nt + 2 * t) * S::kPitch + g, sums + (8 * nt + 2 * t + 1) * S::kPitch + g};
+                        const float back[2] = {exp2_fast(-r[nt][0]), exp2_fast(-r[nt][1])};
+                        float old[MT][4];
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
+                        for (int k = 0; k < MT; ++k)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) old[k][c] = turn ? base[c & 1][(2 * k + (c >> 1)) * 8] : 0.f;
+#pragma unroll
+                        for (int k = 0; k < MT; ++k)
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
-                                float* at = sums + (8 * nt + 2 * t + (c & 1)) * S::kPitch + (2 * k + (c >> 1)) * 8 + g;
-                                const float x = w[nt][c & 1] == 0.f ? 0.f : o[k][nt][c] * exp2_fast(-r[nt][c & 1]) * w[nt][c & 1];
-                                *at = turn ? *at + x : x;
+                                const float x = w[nt][c & 1] == 0.f ? 0.f : o[k][nt][c] * back[c & 1] * w[nt][c & 1];
+                                base[c & 1][(2 * k + (c >> 1)) * 8] = turn ? old[k][c] + x : x;
                             }
+                    }
                 bar_consumers();
             }
             float* part = a.part + ((int64_t)blockIdx.x * 2 + (tile == 0 ? 1 : 0)) * S::kPart;   // 1: the item begins here
             const int rows = min(R, it.rows - row0);
-#pragma unroll(MODE == kOwn ? PRE : 1)
-            for (int k = 0; k < (MODE == kOwn ? PRE : R * D / 128); ++k) {
+#pragma unroll
+            for (int k = 0; k < R * D / 128; ++k) {
                 const int i = (int)threadIdx.x + 128 * k;
                 if (i >= rows * D) break;
                 const int r = i / D, d = i - r * D;
@@ -1211,6 +1248,189 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
     };
     if (range.u0 < range.u1) walk();
     wait();
+}
+
+// Attention over the sequences' own tokens beside the kernel of their groups: short contexts, of which a block's shared memory, barriers and joins take longer than the
+// tokens (6 us an item; 64 sequences of up to 512 tokens, 64/8 heads, by themselves: 26 us). A warp has an item (sequence, 8 rows, head) from its queries to its output, with K and V
+// straight from memory to the registers that the products read: a row's 128 (64) bytes are four lanes' pieces. K of the next 32 tokens is on its way during the product with V, V during
+// the next scores. Nothing here waits for another warp. Sums go to rows where the sequence has a prefix, else to the output.
+constexpr int kShortWarps = 4;
+template <int D, bool BF16>
+__global__ void __launch_bounds__(32 * kShortWarps, 2) us_kv_short_kernel(const __grid_constant__ KvAttend a)
+{
+    constexpr int R = 8, C = D / 8;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const KvPool& p = a.pool;
+    // (Started behind the groups' kernel, whose blocks are all past its wait: what that waits for is complete.)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const uint32_t w = blockIdx.x * kShortWarps + (threadIdx.x >> 5), index = w / (uint32_t)p.Hkv;
+    const int h = (int)(w - index * (uint32_t)p.Hkv);
+    KvItem it;
+    int s = -1, row0 = 0;
+    {
+        uint32_t before = 0;
+        bool any = false;
+        for (int base = 0; base < a.seqs.S; base += 32) {
+            KvSeq mine = {0, 0, 0};
+            if (base + lane < a.seqs.S) {
+                bool wrong;
+                mine = kv_seq(a.seqs, p, base + lane, wrong);
+                any |= wrong;
+            }
+            const uint32_t cnt = ((uint32_t)mine.n * (uint32_t)a.G + R - 1) / R;
+            uint32_t sum = cnt;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t v = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += v;
+            }
+            const uint32_t who = __ballot_sync(0xffffffffu, index >= before + sum - cnt && index < before + sum);
+            if (who) {
+                const int l = __ffs(who) - 1;
+                s = base + l;
+                row0 = R * (int)(index - before - __shfl_sync(0xffffffffu, sum - cnt, l));
+                KvSeq q;
+                q.first = __shfl_sync(0xffffffffu, mine.first, l);
+                q.len = __shfl_sync(0xffffffffu, mine.len, l);
+                q.n = __shfl_sync(0xffffffffu, mine.n, l);
+                it = kv_item<R>(a, q);
+                if (w) break;
+            }
+            before += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        if (any && w == 0) atomicExch(p.err, kErrIndex);   // (the first warp looks at all of them)
+    }
+    if (s >= 0) {
+        const int pos0 = it.seq.len - it.seq.n, end = a.causal ? min(it.seq.len, pos0 + (min(row0 + R, it.rows) - 1) / a.G + 1) : it.seq.len;   // behind the last token that a row sees
+        const int32_t* table = a.seqs.table + (int64_t)s * a.seqs.table_stride;
+        // blocks and steps of 32 groups of 16 tokens, a lane each
+        int32_t blk;
+        float sk, sv;
+        auto look = [&](int from) {
+            const int tok = from + 16 * lane;
+            blk = -1;
+            sk = -1.f;
+            sv = 0.f;
+            if (tok < end) {
+                blk = __ldcg(table + (tok >> a.log2_T));
+                if (blk < 0 || blk >= p.blocks) {
+                    atomicExch(p.err, kErrIndex);
+                    blk = -1;
+                } else {
+                    sk = __ldcg(p.k_step + (int64_t)blk * p.Hkv + h);
+                    sv = __ldcg(p.v_step + (int64_t)blk * p.Hkv + h);
+                }
+            }
+        };
+        uint4 kx[2][D / 64][2];
+        uint32_t vx[2][4][D / 32];
+        auto place = [&](int b, int tok0) -> int64_t {   // of group b's first code; -1: not there
+            const int32_t x = __shfl_sync(0xffffffffu, blk, ((tok0 >> 4) + b) & 31);
+            return x < 0 ? -1 : ((((int64_t)x * p.Hkv + h) << a.log2_T) + ((tok0 + 16 * b) & (p.T - 1))) * D;
+        };
+        auto fetch_k = [&](int tok0) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int64_t at = place(b, tok0);
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) {
+                    const int chunk = D == 128 ? 2 * t + c : t;
+                    kx[b][c][0] = kx[b][c][1] = make_uint4(0, 0, 0, 0);
+                    if (at >= 0) {
+                        kx[b][c][0] = __ldcg(reinterpret_cast<const uint4*>(p.k + at + g * D + 16 * chunk));
+                        kx[b][c][1] = __ldcg(reinterpret_cast<const uint4*>(p.k + at + (g + 8) * D + 16 * chunk));
+                    }
+                }
+            }
+        };
+        auto fetch_v = [&](int tok0) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int64_t at = place(b, tok0);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int8_t* src = p.v + at + (2 * t + (q & 1) + 8 * (q >> 1)) * D + C * g;
+                    if (D == 128) {
+                        const uint4 x = at >= 0 ? __ldcg(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
+                        vx[b][q][0] = x.x; vx[b][q][1] = x.y; vx[b][q][D / 32 - 2] = x.z; vx[b][q][D / 32 - 1] = x.w;
+                    } else {
+                        const uint2 x = at >= 0 ? __ldcg(reinterpret_cast<const uint2*>(src)) : make_uint2(0, 0);
+                        vx[b][q][0] = x.x; vx[b][q][1] = x.y;
+                    }
+                }
+            }
+        };
+        look(0);
+        uint32_t qf[1][D / 16][2];
+        float f[1][2], m[1][2], r[1][2], l[1][2], o[D / 16][1][4];
+        int lo[1][2], hi[1][2];
+        kv_queries<D, 1, BF16>(a, it, row0, h, g, t, qf, f, lo, hi);
+        const int all_hi = __reduce_min_sync(0xffffffffu, min(hi[0][0], hi[0][1]));
+#pragma unroll
+        for (int c = 0; c < 2; ++c) { m[0][c] = -INFINITY; r[0][c] = l[0][c] = 0.f; }
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[i][0][c] = 0.f;
+        if (end > 0) {
+            fetch_k(0);
+            fetch_v(0);
+        }
+#pragma unroll 1
+        for (int tok0 = 0; tok0 < end; tok0 += 32) {
+            float stk[2], stv[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                stk[b] = __shfl_sync(0xffffffffu, sk, ((tok0 >> 4) + b) & 31);
+                stv[b] = __shfl_sync(0xffffffffu, sv, ((tok0 >> 4) + b) & 31);
+            }
+            const int next = tok0 + 32;
+            if (next < end && (next & 511) == 0) look(next);
+            kv_step<D, 1, BF16>(
+                [&](int b, int c, uint4& x, uint4& y) {
+                    x = kx[b][c][0];
+                    y = kx[b][c][1];
+                },
+                [&](int b, int q, uint32_t (&v)[D / 32]) {
+                    if (b == 0 && q == 0 && next < end) fetch_k(next);   // (the scores are done with this one's)
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) v[i] = vx[b][q][i];
+                },
+                qf, f, lo, hi, stk, stv, next > all_hi || stk[0] < 0.f || stk[1] < 0.f, tok0, g, m, r, l, o);
+            if (next < end) fetch_v(next);
+        }
+        const bool joined = kv_has_prefix<kOwn>(a.rows, s, it.seq.len);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float sum = l[0][c];
+            sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+            const int rr = row0 + 2 * t + c;
+            if (rr >= it.rows) continue;
+            const int tok = rr / a.G, qh = h * a.G + rr - tok * a.G;
+            const float back = exp2_fast(-r[0][c]);
+            float y[C];   // columns C g ..
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                y[2 * k] = o[k][0][c] * back;
+                y[2 * k + 1] = o[k][0][c + 2] * back;
+            }
+            float* row = a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+            // (a row without a prefix is complete here; should a group have it all the same, as a padded one, its join is told to leave it alone)
+            if (g == 0) *reinterpret_cast<float2*>(row + D) = joined ? make_float2(m[0][c], sum) : make_float2(INFINITY, 0.f);
+            if (joined) {
+#pragma unroll
+                for (int i = 0; i < C; i += 4) *reinterpret_cast<float4*>(row + C * g + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+                continue;
+            }
+#pragma unroll
+            for (int i = 0; i < C; ++i) o_put<BF16>(a.out, (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + C * g + i, sum == 0.f ? 0.f : y[i] / sum);
+            if (a.lse && g == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(m[0][c], sum);
+        }
+    }
+    // (What follows in the stream waits for this grid alone: it may not end before the groups' kernel. One block is enough: the others make room.)
+    if (blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 }  // namespace us

@@ -26,6 +26,7 @@ struct AttendPlan {
     int rows, stages, smem, ctas;
     int join_blocks;   // (prompts) of a row tile and head
     int splits;        // (prompts) of the cache's length
+    int beside;        // (prompts of groups) the kernel of the own tokens runs beside it
     int64_t tiles;     // (prompts) row tiles, at most; 0: the kernel for few rows
     int64_t scratch;
 };
@@ -98,8 +99,15 @@ inline us_status attend_check(us_kv* h, const us_kv_seqs* q, int64_t N, const At
     if (s != US_OK) return s;
     return N * (x.heads / h->pool.Hkv) >= (1ll << 31) - (1 << 16) ? US_ERR_UNSUPPORTED : US_OK;
 }
-// rows: see KvRows (unused by kAlone's kernels).
-inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, const AttendPlan& pl, const KvRows& rows, void* scratch, cudaStream_t st)
+// What runs beside the groups' kernel.
+struct Beside {
+    const void *kernel, *join;
+    KvSeqs own;
+    int64_t blocks;
+};
+// rows: see KvRows (unused by kAlone's kernels). beside: (prompts of groups) what runs beside them, and joins all.
+inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, const AttendPlan& pl, const KvRows& rows, void* scratch, cudaStream_t st,
+                            const Beside* beside = nullptr)
 {
     const int64_t G = x.heads / h->pool.Hkv;
     if (pl.tiles > 0) {
@@ -115,10 +123,11 @@ inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, cons
         a.scale2 = (float)(std::fabs((double)x.scale) * 1.4426950408889634);
         a.negative = x.scale < 0.f;
         a.Hq = x.heads; a.G = (int32_t)G;
-        a.causal = x.causal != 0; a.window = x.window;
+        a.causal = x.causal != 0 && !q.groups; a.window = x.window;   // (a group's rows see all of their prefix)
         a.q_vec = rows_vec(x.q, x.type, x.q_token, x.q_head);
         a.o_vec = rows_vec(x.out, x.type, x.o_token, x.o_head);
         a.splits = pl.splits;
+        a.beside = pl.beside;
         a.rows = rows;
         while ((1 << a.log2_T) < h->pool.T) ++a.log2_T;
         const us_status s = kv_error_word(&a.pool.err);
@@ -127,7 +136,23 @@ inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, cons
         cudaError_t e = ops_kernel_allow(pl.kernel, pl.smem);
         const int threads = PrShape<128>::kThreads;
         if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.splits)), threads, pl.smem, st, args);
-        if (e == cudaSuccess && pl.splits > 1) e = ops_launch(pl.join, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.join_blocks)), kPrRows, 0, st, args);
+        if (e == cudaSuccess && beside) {
+            KvAttend o = {};
+            o.pool = a.pool;
+            o.seqs = beside->own;
+            o.q = a.q; o.q_token = a.q_token; o.q_head = a.q_head;
+            o.out = a.out; o.o_token = a.o_token; o.o_head = a.o_head;
+            o.lse = a.lse;
+            o.scale2 = (float)((double)x.scale * 1.4426950408889634);
+            o.Hq = a.Hq; o.G = a.G;
+            o.causal = x.causal != 0;
+            o.q_vec = a.q_vec;
+            o.log2_T = a.log2_T;
+            o.rows = rows;
+            void* more[] = {&o};
+            e = ops_launch(beside->kernel, dim3((unsigned)beside->blocks), 32 * kShortWarps, 0, st, more);
+            if (e == cudaSuccess) e = ops_launch(beside->join, dim3((unsigned)(pl.tiles * h->pool.Hkv * (h->pool.D / 4))), 256, 0, st, args);
+        } else if (e == cudaSuccess && pl.splits > 1) e = ops_launch(pl.join, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.join_blocks)), kPrRows, 0, st, args);
         return kv_cuda(e);
     }
     if (!kv_maps(h)) return US_ERR_CUDA;
@@ -141,7 +166,7 @@ inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, cons
     a.part = static_cast<float*>(scratch);
     a.scale2 = (float)((double)x.scale * 1.4426950408889634);
     a.Hq = x.heads; a.G = (int32_t)G;
-    a.causal = x.causal != 0; a.window = x.window;
+    a.causal = x.causal != 0 && !q.groups; a.window = x.window;
     a.q_vec = rows_vec(x.q, x.type, x.q_token, x.q_head);
     a.stages = pl.stages;
     a.ctas = pl.ctas;

@@ -41,6 +41,7 @@ struct KvPrompt {
     int32_t q_vec, o_vec;
     int32_t log2_T;
     int32_t splits;
+    int32_t beside;          // (kGroups) the kernel of the own tokens runs beside it: leaves parts, whatever their number
     KvRows rows;
 };
 
@@ -422,7 +423,8 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             const float inv = l == 0.f ? 0.f : keep / l;
             if (MODE == kOwn) more = l == 0.f ? 0.f : more / l;
             float* part = a.part + (((int64_t)index * p.Hkv + h) * a.splits + split) * S::kPart;
-            if (real && a.splits > 1) {
+            const bool parts = a.splits > 1 || (MODE == kGroups && a.beside);
+            if (real && parts) {
                 part[kPrRows * D + local] = m;
                 part[kPrRows * D + kPrRows + local] = l;
             } else if (MODE == kGroups) {
@@ -432,7 +434,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             }
             uint16_t* dst = static_cast<uint16_t*>(a.out) + (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head;
 #pragma unroll 1
-            for (int c = 0; c < (n == 0 && a.splits > 1 ? 0 : D / 32); ++c) {   // (a part without units has no sums)
+            for (int c = 0; c < (n == 0 && parts ? 0 : D / 32); ++c) {   // (a part without units has no sums)
                 uint32_t x[32];
                 if (n > 0) {
                     tc_ld32(t_o + 32u * c, x);
@@ -443,7 +445,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                     for (int i = 0; i < 32; ++i) x[i] = 0;
                 }
                 if (!real) continue;
-                if (a.splits > 1) {
+                if (parts) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         *reinterpret_cast<float4*>(part + ((8 * c + i) * kPrRows + local) * 4) =
@@ -761,6 +763,65 @@ __global__ void __launch_bounds__(kPrRows) us_kv_rows_join_kernel(const __grid_c
     float* row = a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
     *reinterpret_cast<float4*>(row + 4 * c) = acc;
     if (c == 0) *reinterpret_cast<float2*>(row + D) = make_float2(big, sum);
+}
+
+// The last step beside: the groups' parts and the rows of the own tokens. A thread has four of D of a row: 64 rows and 16 of D a block, all loads at once.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) us_kv_shared_join_kernel(const __grid_constant__ KvPrompt a)
+{
+    using S = PrShape<D>;
+    constexpr int MOST = 16, PER = 4 * (D / 16);   // parts; blocks of a row tile and head
+    const int lane = threadIdx.x & 31, b = (int)(blockIdx.x % PER), local = 64 * (b & 3) + ((int)threadIdx.x & 63), c = 4 * (b >> 2) + ((int)threadIdx.x >> 6);
+    const uint32_t u = blockIdx.x / PER, index = u / (uint32_t)a.pool.Hkv;
+    const int h = (int)(u - index * a.pool.Hkv);
+    PrItem it;
+    const bool have = pr_item<kGroups>(a, index, lane, it, false);   // (complete, as above)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!have || local >= it.rows) return;
+    const int r = it.row0 + local, tok = r / a.G, qh = h * a.G + r - tok * a.G;
+    const float* row = a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+    const float* part = a.part + (int64_t)u * a.splits * S::kPart;
+    float m[MOST + 1], l[MOST + 1];
+    float4 x[MOST + 1];
+    const float2 stat = __ldcg(reinterpret_cast<const float2*>(row + D));
+    m[MOST] = stat.x;
+    l[MOST] = stat.y;
+    x[MOST] = __ldcg(reinterpret_cast<const float4*>(row + 4 * c));
+#pragma unroll
+    for (int s = 0; s < MOST; ++s) {
+        m[s] = -INFINITY;
+        l[s] = 0.f;
+        x[s] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (s < a.splits) {
+            m[s] = __ldcg(part + s * S::kPart + kPrRows * D + local);
+            l[s] = __ldcg(part + s * S::kPart + kPrRows * D + kPrRows + local);
+            x[s] = __ldcg(reinterpret_cast<const float4*>(part + s * S::kPart + (c * kPrRows + local) * 4));
+        }
+    }
+    if (stat.x == INFINITY && stat.y == 0.f) return;   // (a padded row: it has its output)
+    float big = -INFINITY, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int s = 0; s <= MOST; ++s) big = fmaxf(big, m[s]);
+#pragma unroll
+    for (int s = 0; s <= MOST; ++s) {
+        const float w = kv_weight(m[s], l[s], big == -INFINITY ? 0.f : big);
+        sum += w * l[s];          // (a part that is NaN has no maximum, and so no weight: its NaN comes from here)
+        if (w == 0.f) continue;   // (a part without units has no sums)
+        acc.x += w * x[s].x; acc.y += w * x[s].y; acc.z += w * x[s].z; acc.w += w * x[s].w;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float y[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+    uint16_t* out = static_cast<uint16_t*>(a.out) + (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + 4 * c;
+    uint16_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(sum == 0.f ? 0.f : y[i])) : __half_as_ushort(__float2half_rn(sum == 0.f ? 0.f : y[i]));
+    if (a.o_vec) *reinterpret_cast<uint2*>(out) = make_uint2(v[0] | ((uint32_t)v[1] << 16), v[2] | ((uint32_t)v[3] << 16));
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = v[i];
+    if (a.lse && c == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(big, sum);
 }
 
 }  // namespace us

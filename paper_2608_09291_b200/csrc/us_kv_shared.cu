@@ -11,7 +11,10 @@ namespace {
 struct SharedPlan {
     AttendPlan groups, own;
     int64_t rows, first, bytes;   // bytes of the rows; where the own part's scratch begins; in all
+    const void *short_kernel, *join;   // the own tokens' kernel runs beside the groups', and another joins what they leave; nullptr: the own tokens' kernel joins
+    int64_t short_blocks;
 };
+constexpr int64_t kShort = 2048;
 int64_t pitch(const us_kv* h) { return h->pool.D + 4; }
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q, int64_t N, int32_t heads, bool bf16)
@@ -23,6 +26,34 @@ SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q,
     if (p->n_seqs > 0) {
         r.groups = attend_plan<kGroups>(h->pool.D, bf16, N, p->n_seqs, G, h->pool.Hkv, p->table_width * T, sms);
         r.rows = N * heads * pitch(h) * 4;
+    }
+    const int64_t longest = q->table_width * T;
+    if (p->n_seqs > 0 && r.groups.tiles > 0 && r.own.tiles == 0 && longest <= kShort) {
+        // Many rows a group, short contexts of their own: the first kernel is bound by its softmax, the second by latency, so they share the GPU. The number of parts that
+        // a prefix is cut in says how many SMs the groups take, and the one is chosen with which both are expected to end first. Times in us (64 sequences of 64/8 heads behind 1024
+        // to 8192 tokens): a row tile's unit 2.9, beginning and end 12; a warp's item 3 and 0.8 for 32 tokens, half of the longest, of which an SM has eight at a time.
+        const int64_t row_tiles = std::max<int64_t>(p->n_seqs, (N * G + kPrRows - 1) / kPrRows) * h->pool.Hkv, units = (p->table_width * T + kPrTile - 1) / kPrTile;
+        const double own = (double)std::max<int64_t>(q->n_seqs, (N * G + 7) / 8) * h->pool.Hkv * (3 + 0.8 * (double)longest / 64) / 8;
+        double best = 0;
+        for (int s = 1; s <= 16 && (s == 1 || s * 4 <= units); ++s) {
+            const int64_t blocks = row_tiles * s, left = std::max<int64_t>(1, sms - blocks);
+            const double t = std::max(std::ceil((double)blocks / (double)sms) * (12 + 2.9 * std::ceil((double)units / s)), 4 + own / (double)left);
+            if (s == 1 || t < best) {
+                best = t;
+                r.groups.splits = s;
+            }
+        }
+        r.groups.beside = 1;
+        r.groups.scratch = r.groups.tiles * h->pool.Hkv * r.groups.splits * (h->pool.D == 128 ? PrShape<128>::kPart : PrShape<64>::kPart) * 4;
+        r.own.scratch = 0;
+        r.short_blocks = ((N * G / 8 + q->n_seqs) * h->pool.Hkv + kShortWarps - 1) / kShortWarps;
+        if (h->pool.D == 128) {
+            r.short_kernel = bf16 ? (const void*)us_kv_short_kernel<128, true> : (const void*)us_kv_short_kernel<128, false>;
+            r.join = bf16 ? (const void*)us_kv_shared_join_kernel<128, true> : (const void*)us_kv_shared_join_kernel<128, false>;
+        } else {
+            r.short_kernel = bf16 ? (const void*)us_kv_short_kernel<64, true> : (const void*)us_kv_short_kernel<64, false>;
+            r.join = bf16 ? (const void*)us_kv_shared_join_kernel<64, true> : (const void*)us_kv_shared_join_kernel<64, false>;
+        }
     }
     r.first = up16(r.rows) + up16(r.groups.scratch);
     r.bytes = r.first + r.own.scratch;
@@ -75,11 +106,12 @@ us_status us_kv_shared_attention(us_kv* h, const us_kv_seqs* prefixes, const us_
     g.cu = q->cu_tokens;
     g.groups = prefixes->cu_tokens;
     g.members = q->n_seqs;
-    AttendArgs y = x;
-    y.causal = 0;
-    y.out = nullptr;
-    y.lse = nullptr;
-    s = attend_run(h, g, y, pl.groups, rows, mem + up16(pl.rows), st);
+    if (pl.join) {
+        if (pl.short_blocks >= (1ll << 31)) return US_ERR_UNSUPPORTED;
+        const Beside beside = {pl.short_kernel, pl.join, kv_seqs(q, N), pl.short_blocks};
+        return attend_run(h, g, x, pl.groups, rows, mem + up16(pl.rows), st, &beside);
+    }
+    s = attend_run(h, g, x, pl.groups, rows, mem + up16(pl.rows), st);   // (writes rows alone)
     if (s != US_OK) return s;
     return attend_run(h, kv_seqs(q, N), x, pl.own, rows, mem + pl.first, st);
 }
