@@ -22,8 +22,8 @@ struct KvSeqs {
     int32_t members;          // sequences of all groups
 };
 // What attention is part of: itself (kAlone); of attention behind shared prefixes, the groups over their prefixes, whose sums go to rows (kGroups), or the sequences over
-// their own tokens, whose sums are joined with those (kOwn).
-enum { kAlone = 0, kGroups = 1, kOwn = 2 };
+// their own tokens, whose sums are joined with those (kOwn); or the groups behind the sequences, joined with the sequences' rows (kLast).
+enum { kAlone = 0, kGroups = 1, kOwn = 2, kLast = 3 };
 
 struct KvPool {
     int8_t *k, *v;
@@ -46,7 +46,7 @@ __device__ __forceinline__ KvSeq kv_seq(const KvSeqs& q, const KvPool& p, int s,
     const int32_t len = __ldcg(q.lengths + s);
     int64_t a = s, b = (int64_t)s + 1;
     bool off = false;
-    if (MODE == kGroups) {
+    if (MODE == kGroups || MODE == kLast) {
         a = __ldcg(q.groups + s);
         b = __ldcg(q.groups + s + 1);
         off = a < 0 || b < a || b > q.members;
@@ -54,7 +54,7 @@ __device__ __forceinline__ KvSeq kv_seq(const KvSeqs& q, const KvPool& p, int s,
         b = max(a, min(b, (int64_t)q.members));
     }
     if (q.cu) { a = __ldcg(q.cu + a); b = __ldcg(q.cu + b); }
-    wrong = off || len < 0 || len > most || a < 0 || b < a || b > q.N || (MODE != kGroups && len > 0 && b - a > len);
+    wrong = off || len < 0 || len > most || a < 0 || b < a || b > q.N || (MODE != kGroups && MODE != kLast && len > 0 && b - a > len);
     r.len = (int32_t)max((int64_t)0, min((int64_t)len, most));
     r.first = max((int64_t)0, min(a, q.N));
     r.n = (int32_t)max((int64_t)0, min(b, q.N) - r.first);
@@ -326,7 +326,8 @@ __global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int
 // side: their chains of products overlap), with sums of their own that are joined at an item's end.
 // Bound by memory: 64 sequences of up to 8192 tokens, 64/8 heads, bf16: 98 us inside a graph, 5.7 TB/s (109 called); one of 131072 tokens, fp16:
 // 55 us, 4.9 TB/s (59 called).
-// The sums over a prefix, for each (new token, query head): D sums, then their maximum and sum; kOwn: for the sequences that are in a group.
+// The sums over a prefix (kLast: over the own tokens), for each (new token, query head): D sums, then their maximum and sum (infinity and 0 for a row that has its
+// output already); kOwn: for the sequences that are in a group.
 struct KvRows {
     float* at;
     const int32_t* groups;
@@ -335,8 +336,9 @@ struct KvRows {
 template <int MODE>
 __device__ __forceinline__ bool kv_has_prefix(const KvRows& r, int s, int len)
 {
-    return MODE == kOwn && len > 0 && s >= __ldcg(r.groups) && s < __ldcg(r.groups + r.n_groups);
+    return MODE == kLast || (MODE == kOwn && len > 0 && s >= __ldcg(r.groups) && s < __ldcg(r.groups + r.n_groups));
 }
+__device__ __forceinline__ bool kv_row_done(float2 stat) { return stat.x == INFINITY && stat.y == 0.f; }
 constexpr int kKvTile = 128;
 constexpr int kKvStart = 4;   // what an item's queries, sums and output cost, in units
 struct KvAttend {
@@ -356,6 +358,7 @@ struct KvAttend {
     int32_t stages;
     int32_t ctas;
     int32_t log2_T;
+    int32_t behind;          // (the kernel of short contexts) launched behind the groups' kernel
     KvRows rows;
 };
 
@@ -788,8 +791,9 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
     // The kernel that joins the parts may start once this one's CTAs are past the wait: it reads lengths and token counts before its own.
-    // (kOwn: started behind the groups' kernels, whose blocks are all past that wait: what they wait for is complete, their rows are waited for below.)
-    if (MODE != kOwn) asm volatile("griddepcontrol.wait;" ::: "memory");
+    // (kOwn, kLast: started behind kernels whose blocks are all past that wait: what they wait for is complete, their rows are waited for below.)
+    constexpr bool JOINS = MODE == kOwn || MODE == kLast;
+    if (!JOINS) asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const KvPool& p = a.pool;
     const KvRange range = kv_range<R, MODE>(a, blockIdx.x, lane, warp == 0);
@@ -951,12 +955,12 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                 break;
             }
             const bool whole = n == it.tiles;
-            // (kOwn) the rows of the prefix, on their way while the warps' sums are put together: a thread has one of D of every row, or of every second
-            constexpr int PRE = MODE == kOwn ? R * D / 128 : 1;
+            // (kOwn, kLast) the other part's rows, on their way while the warps' sums are put together: a thread has one of D of every row, or of every second
+            constexpr int PRE = JOINS ? R * D / 128 : 1;
             float pre[PRE];
             float2 pre_stat[PRE];
             bool joined = false;
-            if constexpr (MODE == kOwn) {
+            if constexpr (JOINS) {
                 if (whole) asm volatile("griddepcontrol.wait;" ::: "memory");
                 joined = whole && kv_has_prefix<MODE>(a.rows, s, it.seq.len);
 #pragma unroll
@@ -1035,7 +1039,8 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                         if (d == 0) *reinterpret_cast<float2*>(row + D) = make_float2(big, sum);
                         continue;
                     }
-                    if (MODE == kOwn && joined) kv_add_part(big, sum, acc, pre_stat[MODE == kOwn ? k : 0], pre[MODE == kOwn ? k : 0]);
+                    if (MODE == kLast && kv_row_done(pre_stat[JOINS ? k : 0])) continue;
+                    if (JOINS && joined) kv_add_part(big, sum, acc, pre_stat[JOINS ? k : 0], pre[JOINS ? k : 0]);
                     o_put<BF16>(a.out, (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + d, sum == 0.f ? 0.f : acc / sum);
                     if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(big, sum);
                 } else {
@@ -1058,7 +1063,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
         atomicExch(p.err, kErrTimeout);
     }
     // (what follows in the stream waits for this grid, or for the one that joins its parts: it may not end before the groups' kernels)
-    if (MODE == kOwn) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (JOINS) asm volatile("griddepcontrol.wait;" ::: "memory");
     __syncthreads();
 }
 
@@ -1136,8 +1141,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
                         if (lane == 0) *reinterpret_cast<float2*>(row + D) = make_float2(all, total);
                         continue;
                     }
-                    if (MODE == kOwn && joined) {
+                    if ((MODE == kOwn || MODE == kLast) && joined) {
                         const float2 stat = __ldcg(reinterpret_cast<const float2*>(row + D));
+                        if (MODE == kLast && kv_row_done(stat)) continue;
                         const float big = all, sum = total;
 #pragma unroll
                         for (int i = 0; i < C; ++i) {
@@ -1214,7 +1220,11 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
                     if (d == 0) *reinterpret_cast<float2*>(own + D) = make_float2(all, total);
                     continue;
                 }
-                if (MODE == kOwn && joined) kv_add_part(all, total, y, __ldcg(reinterpret_cast<const float2*>(own + D)), __ldcg(own + d));
+                if ((MODE == kOwn || MODE == kLast) && joined) {
+                    const float2 stat = __ldcg(reinterpret_cast<const float2*>(own + D));
+                    if (MODE == kLast && kv_row_done(stat)) continue;
+                    kv_add_part(all, total, y, stat, __ldcg(own + d));
+                }
                 o_put<BF16>(a.out, (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + d, total == 0.f ? 0.f : y / total);
                 if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(all, total);
             }
@@ -1250,7 +1260,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
     wait();
 }
 
-// Attention over the sequences' own tokens beside the kernel of their groups: short contexts, of which a block's shared memory, barriers and joins take longer than the
+// Attention over the sequences' own tokens beside the kernel of their groups, or in front of it: short contexts, of which a block's shared memory, barriers and joins take longer than the
 // tokens (6 us an item; 64 sequences of up to 512 tokens, 64/8 heads, by themselves: 26 us). A warp has an item (sequence, 8 rows, head) from its queries to its output, with K and V
 // straight from memory to the registers that the products read: a row's 128 (64) bytes are four lanes' pieces. K of the next 32 tokens is on its way during the product with V, V during
 // the next scores. Nothing here waits for another warp. Sums go to rows where the sequence has a prefix, else to the output.
@@ -1261,7 +1271,8 @@ __global__ void __launch_bounds__(32 * kShortWarps, 2) us_kv_short_kernel(const 
     constexpr int R = 8, C = D / 8;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const KvPool& p = a.pool;
-    // (Started behind the groups' kernel, whose blocks are all past its wait: what that waits for is complete.)
+    // (Behind the groups' kernel: its blocks are all past the wait, so what that waits for is complete.)
+    if (!a.behind) asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t w = blockIdx.x * kShortWarps + (threadIdx.x >> 5), index = w / (uint32_t)p.Hkv;
     const int h = (int)(w - index * (uint32_t)p.Hkv);
@@ -1430,7 +1441,7 @@ __global__ void __launch_bounds__(32 * kShortWarps, 2) us_kv_short_kernel(const 
         }
     }
     // (What follows in the stream waits for this grid alone: it may not end before the groups' kernel. One block is enough: the others make room.)
-    if (blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (a.behind && blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 }  // namespace us

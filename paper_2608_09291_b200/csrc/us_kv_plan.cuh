@@ -62,6 +62,15 @@ AttendPlan attend_shape(int sms)
 }
 template <int D, int NT, int MODE>
 AttendPlan attend_shape(bool bf16, int sms) { return bf16 ? attend_shape<D, NT, true, MODE>(sms) : attend_shape<D, NT, false, MODE>(sms); }
+// The kernel for few rows.
+template <int MODE>
+AttendPlan few_plan(int D, bool bf16, int64_t N, int64_t S, int64_t G, int sms)
+{
+    // rows a cache head has on average: 8 a tile are enough for them, or 16
+    const bool few = N * G <= 8 * S;
+    if (D == 128) return few ? attend_shape<128, 1, MODE>(bf16, sms) : attend_shape<128, 2, MODE>(bf16, sms);
+    return few ? attend_shape<64, 1, MODE>(bf16, sms) : attend_shape<64, 2, MODE>(bf16, sms);
+}
 template <int MODE>
 AttendPlan attend_plan(int D, bool bf16, int64_t N, int64_t S, int64_t G, int64_t Hkv, int64_t longest, int sms)
 {
@@ -71,12 +80,8 @@ AttendPlan attend_plan(int D, bool bf16, int64_t N, int64_t S, int64_t G, int64_
         if (D == 128) return bf16 ? prompt_shape<128, true, MODE>(N, S, G, Hkv, longest, sms) : prompt_shape<128, false, MODE>(N, S, G, Hkv, longest, sms);
         return bf16 ? prompt_shape<64, true, MODE>(N, S, G, Hkv, longest, sms) : prompt_shape<64, false, MODE>(N, S, G, Hkv, longest, sms);
     }
-    // rows a cache head has on average: 8 a tile are enough for them, or 16
-    const bool few = N * G <= 8 * S;
-    if (D == 128) return few ? attend_shape<128, 1, MODE>(bf16, sms) : attend_shape<128, 2, MODE>(bf16, sms);
-    return few ? attend_shape<64, 1, MODE>(bf16, sms) : attend_shape<64, 2, MODE>(bf16, sms);
+    return few_plan<MODE>(D, bf16, N, S, G, sms);
 }
-
 
 struct AttendArgs {
     const void* q;
@@ -99,12 +104,38 @@ inline us_status attend_check(us_kv* h, const us_kv_seqs* q, int64_t N, const At
     if (s != US_OK) return s;
     return N * (x.heads / h->pool.Hkv) >= (1ll << 31) - (1 << 16) ? US_ERR_UNSUPPORTED : US_OK;
 }
-// What runs beside the groups' kernel.
+// What a call of attention passes to either kernel for few rows.
+inline us_status attend_args(const us_kv* h, const KvSeqs& q, const AttendArgs& x, const KvRows& rows, KvAttend* a)
+{
+    *a = KvAttend{};
+    a->pool = h->pool;
+    a->seqs = q;
+    a->q = x.q; a->q_token = x.q_token; a->q_head = x.q_head;
+    a->out = x.out; a->o_token = x.o_token; a->o_head = x.o_head;
+    a->lse = x.lse;
+    a->scale2 = (float)((double)x.scale * 1.4426950408889634);
+    a->Hq = x.heads; a->G = x.heads / h->pool.Hkv;
+    a->causal = x.causal != 0 && !q.groups; a->window = x.window;   // (a group's rows see all of their prefix)
+    a->q_vec = rows_vec(x.q, x.type, x.q_token, x.q_head);
+    a->rows = rows;
+    while ((1 << a->log2_T) < h->pool.T) ++a->log2_T;
+    return kv_error_word(&a->pool.err);
+}
+// The kernel of short contexts, beside the groups' kernel or in front of it; join: of both.
 struct Beside {
     const void *kernel, *join;
     KvSeqs own;
     int64_t blocks;
 };
+inline us_status short_run(us_kv* h, const AttendArgs& x, const Beside& b, const KvRows& rows, bool behind, cudaStream_t st)
+{
+    KvAttend a;
+    const us_status s = attend_args(h, b.own, x, rows, &a);
+    if (s != US_OK) return s;
+    a.behind = behind;
+    void* args[] = {&a};
+    return kv_cuda(ops_launch(b.kernel, dim3((unsigned)b.blocks), 32 * kShortWarps, 0, st, args));
+}
 // rows: see KvRows (unused by kAlone's kernels). beside: (prompts of groups) what runs beside them, and joins all.
 inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, const AttendPlan& pl, const KvRows& rows, void* scratch, cudaStream_t st,
                             const Beside* beside = nullptr)
@@ -137,43 +168,20 @@ inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, cons
         const int threads = PrShape<128>::kThreads;
         if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.splits)), threads, pl.smem, st, args);
         if (e == cudaSuccess && beside) {
-            KvAttend o = {};
-            o.pool = a.pool;
-            o.seqs = beside->own;
-            o.q = a.q; o.q_token = a.q_token; o.q_head = a.q_head;
-            o.out = a.out; o.o_token = a.o_token; o.o_head = a.o_head;
-            o.lse = a.lse;
-            o.scale2 = (float)((double)x.scale * 1.4426950408889634);
-            o.Hq = a.Hq; o.G = a.G;
-            o.causal = x.causal != 0;
-            o.q_vec = a.q_vec;
-            o.log2_T = a.log2_T;
-            o.rows = rows;
-            void* more[] = {&o};
-            e = ops_launch(beside->kernel, dim3((unsigned)beside->blocks), 32 * kShortWarps, 0, st, more);
-            if (e == cudaSuccess) e = ops_launch(beside->join, dim3((unsigned)(pl.tiles * h->pool.Hkv * (h->pool.D / 4))), 256, 0, st, args);
+            const us_status s = short_run(h, x, *beside, rows, true, st);
+            if (s != US_OK) return s;
+            e = ops_launch(beside->join, dim3((unsigned)(pl.tiles * h->pool.Hkv * (h->pool.D / 4))), 256, 0, st, args);
         } else if (e == cudaSuccess && pl.splits > 1) e = ops_launch(pl.join, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.join_blocks)), kPrRows, 0, st, args);
         return kv_cuda(e);
     }
     if (!kv_maps(h)) return US_ERR_CUDA;
-    KvAttend a = {};
+    KvAttend a;
+    const us_status s = attend_args(h, q, x, rows, &a);
+    if (s != US_OK) return s;
     a.k_map = h->k_map; a.v_map = h->v_map;
-    a.pool = h->pool;
-    a.seqs = q;
-    a.q = x.q; a.q_token = x.q_token; a.q_head = x.q_head;
-    a.out = x.out; a.o_token = x.o_token; a.o_head = x.o_head;
-    a.lse = x.lse;
     a.part = static_cast<float*>(scratch);
-    a.scale2 = (float)((double)x.scale * 1.4426950408889634);
-    a.Hq = x.heads; a.G = (int32_t)G;
-    a.causal = x.causal != 0 && !q.groups; a.window = x.window;
-    a.q_vec = rows_vec(x.q, x.type, x.q_token, x.q_head);
     a.stages = pl.stages;
     a.ctas = pl.ctas;
-    a.rows = rows;
-    while ((1 << a.log2_T) < h->pool.T) ++a.log2_T;
-    const us_status s = kv_error_word(&a.pool.err);
-    if (s != US_OK) return s;
     cudaError_t e = ops_kernel_allow(pl.kernel, pl.smem);
     void* args[] = {&a};
     if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)pl.ctas), 160, pl.smem, st, args);

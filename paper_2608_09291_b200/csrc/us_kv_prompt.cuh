@@ -799,7 +799,7 @@ __global__ void __launch_bounds__(256) us_kv_shared_join_kernel(const __grid_con
             x[s] = __ldcg(reinterpret_cast<const float4*>(part + s * S::kPart + (c * kPrRows + local) * 4));
         }
     }
-    if (stat.x == INFINITY && stat.y == 0.f) return;   // (a padded row: it has its output)
+    if (kv_row_done(stat)) return;   // (a padded row: it has its output)
     float big = -INFINITY, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll

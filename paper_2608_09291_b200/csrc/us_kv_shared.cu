@@ -11,10 +11,10 @@ namespace {
 struct SharedPlan {
     AttendPlan groups, own;
     int64_t rows, first, bytes;   // bytes of the rows; where the own part's scratch begins; in all
-    const void *short_kernel, *join;   // the own tokens' kernel runs beside the groups', and another joins what they leave; nullptr: the own tokens' kernel joins
+    const void *short_kernel, *join;   // short contexts: their kernel, in front of the groups' (which joins) or (join) beside it; nullptr: behind it, and joins
     int64_t short_blocks;
 };
-constexpr int64_t kShort = 2048;
+constexpr int64_t kShort = 2048;   // tokens that a warp reads by itself (a table's width says how many there may be)
 int64_t pitch(const us_kv* h) { return h->pool.D + 4; }
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q, int64_t N, int32_t heads, bool bf16)
@@ -28,12 +28,20 @@ SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q,
         r.rows = N * heads * pitch(h) * 4;
     }
     const int64_t longest = q->table_width * T;
-    if (p->n_seqs > 0 && r.groups.tiles > 0 && r.own.tiles == 0 && longest <= kShort) {
+    if (p->n_seqs > 0 && r.own.tiles == 0 && longest <= kShort) {
+        r.short_blocks = ((N * G / 8 + q->n_seqs) * h->pool.Hkv + kShortWarps - 1) / kShortWarps;
+        r.short_kernel = h->pool.D == 128 ? (bf16 ? (const void*)us_kv_short_kernel<128, true> : (const void*)us_kv_short_kernel<128, false>) :
+                                            (bf16 ? (const void*)us_kv_short_kernel<64, true> : (const void*)us_kv_short_kernel<64, false>);
+        r.own.scratch = 0;
+        if (r.groups.tiles == 0) r.groups = few_plan<kLast>(h->pool.D, bf16, N, p->n_seqs, G, sms);
+    }
+    if (r.short_kernel && r.groups.tiles > 0) {
         // Many rows a group, short contexts of their own: the first kernel is bound by its softmax, the second by latency, so they share the GPU. The number of parts that
-        // a prefix is cut in says how many SMs the groups take, and the one is chosen with which both are expected to end first. Times in us (64 sequences of 64/8 heads behind 1024
-        // to 8192 tokens): a row tile's unit 2.9, beginning and end 12; a warp's item 3 and 0.8 for 32 tokens, half of the longest, of which an SM has eight at a time.
+        // a prefix is cut in says how many SMs the groups take, and the one is chosen with which both are expected to end first. Times in us: a row tile's unit 2.9, beginning and
+        // end 12; a warp's item 4 and 2.4 for 32 tokens, half of the longest, while the other kernel runs, of which an SM has eight at a time. (64 sequences of 64/8
+        // heads behind 8192 tokens, with up to 512 of their own: 51, 47, 60, 71 us for 5, 6, 7, 8 parts, 77 one behind the other.)
         const int64_t row_tiles = std::max<int64_t>(p->n_seqs, (N * G + kPrRows - 1) / kPrRows) * h->pool.Hkv, units = (p->table_width * T + kPrTile - 1) / kPrTile;
-        const double own = (double)std::max<int64_t>(q->n_seqs, (N * G + 7) / 8) * h->pool.Hkv * (3 + 0.8 * (double)longest / 64) / 8;
+        const double own = (double)std::max<int64_t>(q->n_seqs, (N * G + 7) / 8) * h->pool.Hkv * (4 + 2.4 * (double)longest / 64) / 8;
         double best = 0;
         for (int s = 1; s <= 16 && (s == 1 || s * 4 <= units); ++s) {
             const int64_t blocks = row_tiles * s, left = std::max<int64_t>(1, sms - blocks);
@@ -45,15 +53,8 @@ SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q,
         }
         r.groups.beside = 1;
         r.groups.scratch = r.groups.tiles * h->pool.Hkv * r.groups.splits * (h->pool.D == 128 ? PrShape<128>::kPart : PrShape<64>::kPart) * 4;
-        r.own.scratch = 0;
-        r.short_blocks = ((N * G / 8 + q->n_seqs) * h->pool.Hkv + kShortWarps - 1) / kShortWarps;
-        if (h->pool.D == 128) {
-            r.short_kernel = bf16 ? (const void*)us_kv_short_kernel<128, true> : (const void*)us_kv_short_kernel<128, false>;
-            r.join = bf16 ? (const void*)us_kv_shared_join_kernel<128, true> : (const void*)us_kv_shared_join_kernel<128, false>;
-        } else {
-            r.short_kernel = bf16 ? (const void*)us_kv_short_kernel<64, true> : (const void*)us_kv_short_kernel<64, false>;
-            r.join = bf16 ? (const void*)us_kv_shared_join_kernel<64, true> : (const void*)us_kv_shared_join_kernel<64, false>;
-        }
+        r.join = h->pool.D == 128 ? (bf16 ? (const void*)us_kv_shared_join_kernel<128, true> : (const void*)us_kv_shared_join_kernel<128, false>) :
+                                    (bf16 ? (const void*)us_kv_shared_join_kernel<64, true> : (const void*)us_kv_shared_join_kernel<64, false>);
     }
     r.first = up16(r.rows) + up16(r.groups.scratch);
     r.bytes = r.first + r.own.scratch;
@@ -106,10 +107,12 @@ us_status us_kv_shared_attention(us_kv* h, const us_kv_seqs* prefixes, const us_
     g.cu = q->cu_tokens;
     g.groups = prefixes->cu_tokens;
     g.members = q->n_seqs;
-    if (pl.join) {
+    if (pl.short_kernel) {
         if (pl.short_blocks >= (1ll << 31)) return US_ERR_UNSUPPORTED;
         const Beside beside = {pl.short_kernel, pl.join, kv_seqs(q, N), pl.short_blocks};
-        return attend_run(h, g, x, pl.groups, rows, mem + up16(pl.rows), st, &beside);
+        if (pl.join) return attend_run(h, g, x, pl.groups, rows, mem + up16(pl.rows), st, &beside);
+        s = short_run(h, x, beside, rows, false, st);
+        return s != US_OK ? s : attend_run(h, g, x, pl.groups, rows, mem + up16(pl.rows), st);
     }
     s = attend_run(h, g, x, pl.groups, rows, mem + up16(pl.rows), st);   // (writes rows alone)
     if (s != US_OK) return s;

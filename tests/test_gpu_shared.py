@@ -224,12 +224,14 @@ def test_nan_stays_in_its_rows(b, new, S, wide):
 
 
 def test_without_prefixes_it_is_attention(b):
-    cache, args, _, _, _ = run(b, [0], [3], [100, 5, 64], [1] * 3, 4, 2, 128, 64, F16)
+    cache, args, out, _, (ref, bound) = run(b, [0], [3], [100, 5, 64], [1] * 3, 4, 2, 128, 64, F16)
     q, _, _, _, table, lengths, _ = args
     want = cache.attention(q, table, lengths)
     none = torch.zeros(0, 1, dtype=torch.int32, device="cuda")
     assert torch.equal(cache.shared_attention(q, none, ints([]), ints([0]), table, lengths), want)
-    assert torch.equal(cache.shared_attention(*args), want)
+    # (an empty prefix: the same sums, which another kernel may add in another order; each side is within the bound, and so they are within two of each other)
+    check(want, ref, bound)
+    check(out, ref, bound)
 
 
 def test_after_a_fork(b):
