@@ -1264,9 +1264,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
 // tokens (6 us an item; 64 sequences of up to 512 tokens, 64/8 heads, by themselves: 26 us). A warp has an item (sequence, 8 rows, head) from its queries to its output, with K and V
 // straight from memory to the registers that the products read: a row's 128 (64) bytes are four lanes' pieces. K of the next 32 tokens is on its way during the product with V, V during
 // the next scores. Nothing here waits for another warp. Sums go to rows where the sequence has a prefix, else to the output.
-constexpr int kShortWarps = 4;
+// At most 176 registers a thread: a quarter of an SM that has two warps of us_kv_attend_kernel (and one where it has three none) has as many left, so that the groups' blocks start
+// beside this kernel's.
 template <int D, bool BF16>
-__global__ void __launch_bounds__(32 * kShortWarps, 2) us_kv_short_kernel(const __grid_constant__ KvAttend a)
+__global__ void __launch_bounds__(32, 12) us_kv_short_kernel(const __grid_constant__ KvAttend a)
 {
     constexpr int R = 8, C = D / 8;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -1274,7 +1275,7 @@ __global__ void __launch_bounds__(32 * kShortWarps, 2) us_kv_short_kernel(const 
     // (Behind the groups' kernel: its blocks are all past the wait, so what that waits for is complete.)
     if (!a.behind) asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const uint32_t w = blockIdx.x * kShortWarps + (threadIdx.x >> 5), index = w / (uint32_t)p.Hkv;
+    const uint32_t w = blockIdx.x, index = w / (uint32_t)p.Hkv;
     const int h = (int)(w - index * (uint32_t)p.Hkv);
     KvItem it;
     int s = -1, row0 = 0;
@@ -1372,6 +1373,10 @@ __global__ void __launch_bounds__(32 * kShortWarps, 2) us_kv_short_kernel(const 
             }
         };
         look(0);
+        if (end > 0) {
+            fetch_k(0);
+            fetch_v(0);
+        }
         uint32_t qf[1][D / 16][2];
         float f[1][2], m[1][2], r[1][2], l[1][2], o[D / 16][1][4];
         int lo[1][2], hi[1][2];
@@ -1383,10 +1388,6 @@ __global__ void __launch_bounds__(32 * kShortWarps, 2) us_kv_short_kernel(const 
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
             for (int c = 0; c < 4; ++c) o[i][0][c] = 0.f;
-        if (end > 0) {
-            fetch_k(0);
-            fetch_v(0);
-        }
 #pragma unroll 1
         for (int tok0 = 0; tok0 < end; tok0 += 32) {
             float stk[2], stv[2];

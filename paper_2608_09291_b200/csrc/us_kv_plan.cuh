@@ -134,7 +134,8 @@ inline us_status short_run(us_kv* h, const AttendArgs& x, const Beside& b, const
     if (s != US_OK) return s;
     a.behind = behind;
     void* args[] = {&a};
-    return kv_cuda(ops_launch(b.kernel, dim3((unsigned)b.blocks), 32 * kShortWarps, 0, st, args));
+    const cudaError_t e = ops_kernel_beside(b.kernel);
+    return kv_cuda(e != cudaSuccess ? e : ops_launch(b.kernel, dim3((unsigned)b.blocks), 32, 0, st, args));
 }
 // rows: see KvRows (unused by kAlone's kernels). beside: (prompts of groups) what runs beside them, and joins all.
 inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, const AttendPlan& pl, const KvRows& rows, void* scratch, cudaStream_t st,

@@ -56,6 +56,22 @@ cudaError_t ops_kernel_allow(const void* kernel, int most)
     return e;
 }
 
+cudaError_t ops_kernel_beside(const void* kernel)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    std::lock_guard<std::mutex> hold(g_lock);
+    if (g_allowed.count({dev, kernel})) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (e != cudaSuccess) return e;
+    try {
+        g_allowed.insert({dev, kernel});
+    } catch (const std::bad_alloc&) {   // (the next call sets the attribute again)
+    }
+    return e;
+}
+
 cudaError_t ops_symbol(void** kept, const void* symbol, void** address)
 {
     int dev = 0;
