@@ -24,36 +24,39 @@ __device__ __forceinline__ void give_up(const Pages& a, int32_t b)
     }
 }
 
-// Children's rows (a warp a row): the parent's blocks, each held once more; then, unless they are kept, the parents' rows, whose blocks are held once less.
-__global__ void __launch_bounds__(256) us_kv_fork_kernel(Pages a, KvSeqs q, const int32_t* parents, int children, int32_t* table, int64_t stride, int32_t* lengths,
-                                                         int give)
+// Children's rows (blockIdx.y; a thread an entry, kEntries a block): the parent's blocks, each held once more; then, unless they are kept, the parents' rows, whose
+// blocks are held once less. Bound by three trips to memory, one behind the other: 2.3 us inside a graph.
+constexpr int kEntries = 128;
+__global__ void __launch_bounds__(kEntries) us_kv_fork_kernel(Pages a, KvSeqs q, const int32_t* parents, int children, int32_t* table, int64_t stride, int32_t* lengths,
+                                                              int give)
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lane = threadIdx.x & 31;
-    const int64_t w = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    if (w >= (int64_t)children + (give ? q.S : 0)) return;
-    const bool child = w < children;
-    int64_t s = child ? __ldcg(parents + w) : w - children;
-    bool bad = s < -1 || s >= q.S;
-    int32_t len = bad || s < 0 ? 0 : __ldcg(q.lengths + s);
-    if (len < 0 || len > (int64_t)q.width << a.log2_T) {
-        bad = true;
-        len = 0;
-    }
-    const int n = blocks_of(len, a.log2_T);
-    for (int j = lane; j < (child ? q.width : n); j += 32) {
-        int32_t b = 0;
-        if (j < n) {
-            b = __ldcg(q.table + s * q.table_stride + j);
-            if (!in_pool(a, b)) bad = true;
-            else if (child) atomicAdd(a.refs + b, 1);
-            else give_up(a, b);
+    const int64_t rows = (int64_t)children + (give ? q.S : 0);
+    const int j = (int)(blockIdx.x * kEntries + threadIdx.x);
+    for (int64_t w = blockIdx.y; w < rows; w += gridDim.y) {
+        const bool child = w < children;
+        const int64_t s = child ? __ldcg(parents + w) : w - children;
+        bool bad = s < -1 || s >= q.S;
+        int32_t len = bad || s < 0 ? 0 : __ldcg(q.lengths + s);
+        if (len < 0 || len > (int64_t)q.width << a.log2_T) {
+            bad = true;
+            len = 0;
         }
-        if (child) table[w * stride + j] = b;
+        const int n = blocks_of(len, a.log2_T);
+        if (j < (child ? q.width : n)) {
+            int32_t b = 0;
+            if (j < n) {
+                b = __ldcg(q.table + s * q.table_stride + j);
+                if (!in_pool(a, b)) bad = true;
+                else if (child) atomicAdd(a.refs + b, 1);
+                else give_up(a, b);
+            }
+            if (child) table[w * stride + j] = b;
+        }
+        if (child && j == 0) lengths[w] = len;
+        if (bad) wrong(a);
     }
-    if (child && lane == 0) lengths[w] = len;
-    if (bad) wrong(a);
 }
 
 // Exclusive sum over the 1024 threads of a block, and the total.
@@ -99,9 +102,10 @@ __device__ __forceinline__ void sixteen(const Pages& a, int64_t b, int32_t (&r)[
 //   1. Each sequence's last block, if new tokens go into it and other entries hold it, too: how many of the batch do, and which first.
 //   2. What each needs: a copy of that block (all but the first, if nobody else holds it), and blocks behind it; a sum over the sequences says which
 //      of the free blocks, lowest first, are whose.
-//   3. The free blocks, 16384 counts at a time, until there are enough.
+//   3. The free blocks, 16384 counts at a time (the first are on their way from the beginning), until there are enough.
 //   4. Tables, counts and lengths; what is to be copied is left for the next kernel.
-// Bound by its trips to memory, one behind the other.
+// A thread has a sequence, or several 1024 apart; what it knows of them waits in shared memory, in scratch where there are more than 1024.
+// Bound by its trips to memory, one behind the other: MEASURED_EXTEND.
 struct Extend {
     int32_t* table;
     int64_t stride;
@@ -110,23 +114,29 @@ struct Extend {
     const int32_t* tokens;
     int32_t each;
     int32_t *count, *first, *list;          // of blocks
-    int32_t *need, *at, *src, *dst, *held;  // of sequences; need: blocks behind the last, + 2^30 for a copy
+    int32_t *need, *at, *src, *dst, *held;  // of sequences; need: blocks behind the last, + 2^30 for a copy; -1: left as it is
 };
 constexpr int32_t kCopy = 1 << 30;
 __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
 {
     __shared__ uint32_t sums[32];
     __shared__ unsigned long long sums64[32];
+    __shared__ int32_t near[3][1024];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int64_t most = (int64_t)e.width << a.log2_T;
+    const int lane = threadIdx.x & 31;
+    const bool few = e.S <= 1024;
+    int32_t *need_of = few ? near[0] : e.need, *at_of = few ? near[1] : e.at, *last_of = few ? near[2] : e.src;
+    int32_t r[16];
+    sixteen(a, 16 * threadIdx.x, r);
     // 1.
     for (int s = threadIdx.x; s < e.S; s += 1024) {
         const int64_t len = __ldcg(e.lengths + s), n = e.tokens ? __ldcg(e.tokens + s) : e.each;
         int32_t need = 0, last = -1;
         if (len < 0 || n < 0 || len + n > most) {
             wrong(a);
-            need = -1;   // (left as it is)
+            need = -1;
         } else if (n > 0) {
             const int have = blocks_of(len, a.log2_T);
             need = blocks_of(len + n, a.log2_T) - have;
@@ -142,14 +152,14 @@ __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
                 }
             }
         }
-        e.need[s] = need;
-        e.src[s] = last;
+        need_of[s] = need;
+        last_of[s] = last;
     }
     __syncthreads();
     for (int s = threadIdx.x; s < e.S; s += 1024)
-        if (e.src[s] >= 0) {
-            atomicAdd(e.count + e.src[s], 1);
-            atomicMin(e.first + e.src[s], s);
+        if (last_of[s] >= 0) {
+            atomicAdd(e.count + last_of[s], 1);
+            atomicMin(e.first + last_of[s], s);
         }
     __syncthreads();
     // 2.
@@ -157,25 +167,24 @@ __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
     for (int base = 0; base < e.S; base += 1024) {
         const int s = base + threadIdx.x;
         unsigned long long mine = 0, sum;
-        if (s < e.S && e.need[s] >= 0) {
-            mine = e.need[s];
-            const int32_t b = e.src[s];
+        if (s < e.S && need_of[s] >= 0) {
+            mine = need_of[s];
+            const int32_t b = last_of[s];
             if (b >= 0 && !(__ldcg(e.count + b) >= __ldcg(a.refs + b) && __ldcg(e.first + b) == s)) {
-                e.need[s] |= kCopy;
+                need_of[s] |= kCopy;
                 ++mine;
             }
         }
         const unsigned long long before = block_sum(mine, sums64, sum);
-        if (s < e.S) e.at[s] = (int32_t)min(total + before, 1ull << 30);   // (a pool has fewer blocks than that)
+        if (s < e.S) at_of[s] = (int32_t)min(total + before, 1ull << 30);   // (a pool has fewer blocks than that)
         total += sum;
     }
     // 3.
     const uint32_t wanted = (uint32_t)min(total, (unsigned long long)a.pool.blocks);
     uint32_t found = 0;
     for (int64_t b0 = 0; b0 < a.pool.blocks && found < wanted; b0 += 16384) {
-        int32_t r[16];
         const int64_t b = b0 + 16 * threadIdx.x;
-        sixteen(a, b, r);
+        if (b0) sixteen(a, b, r);
         uint32_t n = 0, sum;
 #pragma unroll
         for (int i = 0; i < 16; ++i) n += r[i] <= 0;
@@ -189,42 +198,54 @@ __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
         found += sum;
     }
     __syncthreads();
-    // 4. (a warp a sequence)
-    const int lane = threadIdx.x & 31;
-    for (int s = threadIdx.x >> 5; s < e.S; s += 32) {
-        const int32_t what = e.need[s];
-        const int32_t last = e.src[s];
-        int32_t dst = -1, held = 0;
-        if (what >= 0) {
-            const int need = what & (kCopy - 1), copy = what & kCopy ? 1 : 0;
-            const uint32_t at = e.at[s];
-            const int32_t len = e.lengths[s], n = e.tokens ? __ldcg(e.tokens + s) : e.each;
+    // 4. (a sequence's blocks: its thread, or all of the warp where one of its sequences gets many)
+    for (int base = threadIdx.x & ~31; base < e.S; base += 1024) {
+        const int s = base + lane;
+        const int32_t what = s < e.S ? need_of[s] : -1;
+        int32_t dst = -1, held = 0, have = 0, n = 0;
+        uint32_t from = 0;
+        bool fits = what >= 0;
+        if (fits) {
+            const uint32_t need = what & (kCopy - 1), copy = what & kCopy ? 1 : 0, at = (uint32_t)at_of[s];
             if (need + copy > 0 && at + need + copy > found) {
-                if (lane == 0) atomicExch(a.pool.err, kErrFull);
+                atomicExch(a.pool.err, kErrFull);
+                fits = false;
             } else {
-                const int have = blocks_of(len, a.log2_T);
-                int32_t* row = e.table + s * e.stride;
+                const int32_t len = e.lengths[s], more = e.tokens ? __ldcg(e.tokens + s) : e.each;
+                have = blocks_of(len, a.log2_T);
                 if (copy) {
                     dst = e.list[at];
                     held = len & ((1 << a.log2_T) - 1);
-                    if (lane == 0) {
-                        row[have - 1] = dst;
-                        a.refs[dst] = 1;
-                        atomicSub(a.refs + last, 1);
-                    }
+                    e.table[s * e.stride + have - 1] = dst;
+                    a.refs[dst] = 1;
+                    atomicSub(a.refs + last_of[s], 1);
                 }
-                for (int j = lane; j < need; j += 32) {
-                    const int32_t b = e.list[at + copy + j];
-                    row[have + j] = b;
-                    a.refs[b] = 1;
-                }
-                __syncwarp();
-                if (lane == 0) e.lengths[s] = len + n;
+                n = (int32_t)need;
+                from = at + copy;
+                e.lengths[s] = len + more;
             }
         }
-        if (lane == 0) {
+        if (s < e.S) {
+            e.src[s] = last_of[s];
             e.dst[s] = dst;
             e.held[s] = held;
+        }
+        const uint32_t many = __ballot_sync(0xffffffffu, n > 4);
+        if (n <= 4)
+            for (int j = 0; j < n; ++j) {
+                const int32_t b = e.list[from + j];
+                e.table[s * e.stride + have + j] = b;
+                a.refs[b] = 1;
+            }
+        for (uint32_t m = many; m; m &= m - 1) {
+            const int l = __ffs(m) - 1;
+            const int count = __shfl_sync(0xffffffffu, n, l), first = __shfl_sync(0xffffffffu, have, l);
+            const uint32_t where = __shfl_sync(0xffffffffu, from, l);
+            for (int j = lane; j < count; j += 32) {
+                const int32_t b = e.list[where + j];
+                e.table[(int64_t)(base + l) * e.stride + first + j] = b;
+                a.refs[b] = 1;
+            }
         }
     }
 }
@@ -318,20 +339,17 @@ __global__ void __launch_bounds__(1024) us_kv_compact_kernel(Pages a, int32_t* m
     }
 }
 
-// A table's entries after the blocks have moved: a warp a row.
-__global__ void __launch_bounds__(256) us_kv_remap_kernel(Pages a, const int32_t* map, int32_t* table, KvSeqs q)
+// A table's entries after the blocks have moved (a row blockIdx.y, a thread an entry).
+__global__ void __launch_bounds__(kEntries) us_kv_remap_kernel(Pages a, const int32_t* map, int32_t* table, KvSeqs q)
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lane = threadIdx.x & 31;
-    const int64_t s = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-    if (s >= q.S) return;
-    const int32_t len = __ldcg(q.lengths + s);
-    if (len < 0 || len > (int64_t)q.width << a.log2_T) {
-        if (lane == 0) wrong(a);
-        return;
-    }
-    for (int j = lane; j < blocks_of(len, a.log2_T); j += 32) {
+    const int j = (int)(blockIdx.x * kEntries + threadIdx.x);
+    for (int64_t s = blockIdx.y; s < q.S; s += gridDim.y) {
+        const int32_t len = __ldcg(q.lengths + s);
+        const bool bad = len < 0 || len > (int64_t)q.width << a.log2_T;
+        if (bad && j == 0) wrong(a);
+        if (bad || j >= blocks_of(len, a.log2_T)) continue;
         int32_t* at = table + s * q.table_stride + j;
         const int32_t b = *at;
         if (in_pool(a, b)) *at = __ldcg(map + b);
@@ -339,7 +357,7 @@ __global__ void __launch_bounds__(256) us_kv_remap_kernel(Pages a, const int32_t
     }
 }
 
-dim3 warps(int64_t n) { return dim3((unsigned)((n + 7) / 8)); }
+dim3 entries(int64_t rows, int64_t width) { return dim3((unsigned)std::max<int64_t>(1, (width + kEntries - 1) / kEntries), (unsigned)std::min<int64_t>(rows, 65535)); }
 
 bool refs_ok(const int32_t* refs) { return refs && kv_aligned(refs, 16); }
 // What all calls' kernels get, on the pool's device.
@@ -394,7 +412,7 @@ us_status us_kv_fork(us_kv* h, int32_t* refs, const us_kv_seqs* q, const int32_t
     if (rows == 0) return US_OK;
     KvSeqs k = kv_seqs(&one, 0);
     void* args[] = {&a, &k, &parents, &n_children, &table, &table_stride, &lengths, &give};
-    return kv_cuda(ops_launch((const void*)us_kv_fork_kernel, warps(rows), 256, 0, static_cast<cudaStream_t>(stream), args));
+    return kv_cuda(ops_launch((const void*)us_kv_fork_kernel, entries(rows, q->table_width), kEntries, 0, static_cast<cudaStream_t>(stream), args));
 }
 
 us_status us_kv_release(us_kv* h, int32_t* refs, const us_kv_seqs* q, void* stream)
@@ -475,5 +493,5 @@ us_status us_kv_remap(us_kv* h, const int32_t* map, int32_t* table, int64_t tabl
     if (s != US_OK) return s;
     KvSeqs k = kv_seqs(&q, 0);
     void* args[] = {&a, &map, &table, &k};
-    return kv_cuda(ops_launch((const void*)us_kv_remap_kernel, warps(n_seqs), 256, 0, static_cast<cudaStream_t>(stream), args));
+    return kv_cuda(ops_launch((const void*)us_kv_remap_kernel, entries(n_seqs, table_width), kEntries, 0, static_cast<cudaStream_t>(stream), args));
 }

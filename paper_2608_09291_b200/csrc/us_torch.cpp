@@ -755,17 +755,16 @@ PyObject* kv_compact(PyObject*, PyObject* const* a, Py_ssize_t n)
         if (q[(size_t)i].n_seqs > 0 && (q[(size_t)i].table_width < 1 || (int64_t)q[(size_t)i].table_width * pool->size(2) >= (1ll << 31) - (1 << 16)))
             return bad("a table is empty or too wide");
     }
-    const int64_t bytes = us_kv_compact_scratch(static_cast<us_kv*>(h));
-    at::Tensor scratch = at::detail::empty_cuda({bytes}, at::kByte, pool->device(), std::nullopt);
-    at::Tensor map = at::detail::empty_cuda({pool->size(0)}, at::kInt, pool->device(), std::nullopt);
+    const int64_t bytes = us_kv_compact_scratch(static_cast<us_kv*>(h)), map_bytes = (4 * pool->size(0) + 15) / 16 * 16;
+    at::Tensor scratch = at::detail::empty_cuda({map_bytes + bytes}, at::kByte, pool->device(), std::nullopt);   // the map first
+    int32_t* map = static_cast<int32_t*>(scratch.data_ptr());
     at::Tensor used = at::detail::empty_cuda(at::IntArrayRef{}, at::kInt, pool->device(), std::nullopt);
     us_status s;
     Py_BEGIN_ALLOW_THREADS
-    const int32_t* to = static_cast<const int32_t*>(map.data_ptr());
-    s = us_kv_compact(static_cast<us_kv*>(h), refs, static_cast<int32_t*>(map.data_ptr()), static_cast<int32_t*>(used.data_ptr()), scratch.data_ptr(), bytes, at_.stream);
+    s = us_kv_compact(static_cast<us_kv*>(h), refs, map, static_cast<int32_t*>(used.data_ptr()), static_cast<uint8_t*>(scratch.data_ptr()) + map_bytes, bytes, at_.stream);
     for (const us_kv_seqs& t : q)
         if (s == US_OK)
-            s = us_kv_remap(static_cast<us_kv*>(h), to, const_cast<int32_t*>(t.block_table), t.table_stride, t.table_width, t.lengths, t.n_seqs, at_.stream);
+            s = us_kv_remap(static_cast<us_kv*>(h), map, const_cast<int32_t*>(t.block_table), t.table_stride, t.table_width, t.lengths, t.n_seqs, at_.stream);
     Py_END_ALLOW_THREADS
     if (s != US_OK) return fail(s, "us_kv_compact");
     return THPVariable_Wrap(std::move(used));
