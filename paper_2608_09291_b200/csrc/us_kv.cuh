@@ -22,7 +22,7 @@ struct KvSeqs {
     int32_t members;          // sequences of all groups
 };
 // What attention is part of: itself (kAlone); of attention behind shared prefixes, the groups over their prefixes, whose sums go to rows (kGroups), or the sequences over
-// their own tokens, whose sums are joined with those (kOwn); or the groups behind the sequences, joined with the sequences' rows (kLast).
+// their own tokens, whose sums are joined with those (kOwn); kLast: the join of the groups' parts and rows with the rows of the sequences' own tokens.
 enum { kAlone = 0, kGroups = 1, kOwn = 2, kLast = 3 };
 
 struct KvPool {
@@ -326,17 +326,17 @@ __global__ void __launch_bounds__(256) us_kv_read_kernel(KvPool p, KvSeqs q, int
 // side: their chains of products overlap), with sums of their own that are joined at an item's end.
 // Bound by memory: 64 sequences of up to 8192 tokens, 64/8 heads, bf16: 98 us inside a graph, 5.7 TB/s (109 called); one of 131072 tokens, fp16:
 // 55 us, 4.9 TB/s (59 called).
-// The sums over a prefix (kLast: over the own tokens), for each (new token, query head): D sums, then their maximum and sum (infinity and 0 for a row that has its
-// output already); kOwn: for the sequences that are in a group.
+// The sums over a prefix (`own`: over the own tokens), for each (new token, query head): D sums, then their maximum and sum (of own tokens: infinity and 0 for a row that
+// has its output already); kOwn: for the sequences that are in a group.
 struct KvRows {
-    float* at;
+    float *at, *own;
     const int32_t* groups;
     int32_t n_groups, pitch;
 };
 template <int MODE>
 __device__ __forceinline__ bool kv_has_prefix(const KvRows& r, int s, int len)
 {
-    return MODE == kLast || (MODE == kOwn && len > 0 && s >= __ldcg(r.groups) && s < __ldcg(r.groups + r.n_groups));
+    return MODE == kOwn && len > 0 && s >= __ldcg(r.groups) && s < __ldcg(r.groups + r.n_groups);
 }
 __device__ __forceinline__ bool kv_row_done(float2 stat) { return stat.x == INFINITY && stat.y == 0.f; }
 constexpr int kKvTile = 128;
@@ -358,7 +358,6 @@ struct KvAttend {
     int32_t stages;
     int32_t ctas;
     int32_t log2_T;
-    int32_t behind;          // (the kernel of short contexts) launched behind the groups' kernel
     KvRows rows;
 };
 
@@ -791,9 +790,8 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
     // The kernel that joins the parts may start once this one's CTAs are past the wait: it reads lengths and token counts before its own.
-    // (kOwn, kLast: started behind kernels whose blocks are all past that wait: what they wait for is complete, their rows are waited for below.)
-    constexpr bool JOINS = MODE == kOwn || MODE == kLast;
-    if (!JOINS) asm volatile("griddepcontrol.wait;" ::: "memory");
+    // (kOwn: started behind the groups' kernels, whose blocks are all past that wait: what they wait for is complete, their rows are waited for below.)
+    if (MODE != kOwn) asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const KvPool& p = a.pool;
     const KvRange range = kv_range<R, MODE>(a, blockIdx.x, lane, warp == 0);
@@ -955,12 +953,12 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                 break;
             }
             const bool whole = n == it.tiles;
-            // (kOwn, kLast) the other part's rows, on their way while the warps' sums are put together: a thread has one of D of every row, or of every second
-            constexpr int PRE = JOINS ? R * D / 128 : 1;
+            // (kOwn) the rows of the prefix, on their way while the warps' sums are put together: a thread has one of D of every row, or of every second
+            constexpr int PRE = MODE == kOwn ? R * D / 128 : 1;
             float pre[PRE];
             float2 pre_stat[PRE];
             bool joined = false;
-            if constexpr (JOINS) {
+            if constexpr (MODE == kOwn) {
                 if (whole) asm volatile("griddepcontrol.wait;" ::: "memory");
                 joined = whole && kv_has_prefix<MODE>(a.rows, s, it.seq.len);
 #pragma unroll
@@ -1003,28 +1001,20 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
             for (int turn = 0; turn < 4; ++turn) {
                 if (warp == turn)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        // (all loads before the first store: a store might be to what a later load reads, for all that is known here)
-                        float* base[2] = {sums + (8 * nt + 2 * t) * S::kPitch + g, sums + (8 * nt + 2 * t + 1) * S::kPitch + g};
-                        const float back[2] = {exp2_fast(-r[nt][0]), exp2_fast(-r[nt][1])};
-                        float old[MT][4];
+                    for (int k = 0; k < MT; ++k)
 #pragma unroll
-                        for (int k = 0; k < MT; ++k)
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) old[k][c] = turn ? base[c & 1][(2 * k + (c >> 1)) * 8] : 0.f;
-#pragma unroll
-                        for (int k = 0; k < MT; ++k)
+                        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
-                                const float x = w[nt][c & 1] == 0.f ? 0.f : o[k][nt][c] * back[c & 1] * w[nt][c & 1];
-                                base[c & 1][(2 * k + (c >> 1)) * 8] = turn ? old[k][c] + x : x;
+                                float* at = sums + (8 * nt + 2 * t + (c & 1)) * S::kPitch + (2 * k + (c >> 1)) * 8 + g;
+                                const float x = w[nt][c & 1] == 0.f ? 0.f : o[k][nt][c] * exp2_fast(-r[nt][c & 1]) * w[nt][c & 1];
+                                *at = turn ? *at + x : x;
                             }
-                    }
                 bar_consumers();
             }
             float* part = a.part + ((int64_t)blockIdx.x * 2 + (tile == 0 ? 1 : 0)) * S::kPart;   // 1: the item begins here
             const int rows = min(R, it.rows - row0);
-#pragma unroll
+#pragma unroll(MODE == kOwn ? PRE : 1)
             for (int k = 0; k < R * D / 128; ++k) {
                 const int i = (int)threadIdx.x + 128 * k;
                 if (i >= rows * D) break;
@@ -1039,8 +1029,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                         if (d == 0) *reinterpret_cast<float2*>(row + D) = make_float2(big, sum);
                         continue;
                     }
-                    if (MODE == kLast && kv_row_done(pre_stat[JOINS ? k : 0])) continue;
-                    if (JOINS && joined) kv_add_part(big, sum, acc, pre_stat[JOINS ? k : 0], pre[JOINS ? k : 0]);
+                    if (MODE == kOwn && joined) kv_add_part(big, sum, acc, pre_stat[MODE == kOwn ? k : 0], pre[MODE == kOwn ? k : 0]);
                     o_put<BF16>(a.out, (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + d, sum == 0.f ? 0.f : acc / sum);
                     if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(big, sum);
                 } else {
@@ -1063,7 +1052,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
         atomicExch(p.err, kErrTimeout);
     }
     // (what follows in the stream waits for this grid, or for the one that joins its parts: it may not end before the groups' kernels)
-    if (JOINS) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (MODE == kOwn) asm volatile("griddepcontrol.wait;" ::: "memory");
     __syncthreads();
 }
 
@@ -1096,7 +1085,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
         wait();
         const int h = item % a.pool.Hkv, row0 = item / a.pool.Hkv * R, rows = min(R, it.rows - row0);
         const int np = c1 - c0 + 1;
-        const bool joined = kv_has_prefix<MODE>(a.rows, s, it.seq.len);
+        const bool joined = MODE == kLast || kv_has_prefix<MODE>(a.rows, s, it.seq.len);   // with the other part's rows
+        const float* others = MODE == kLast ? a.rows.own : a.rows.at;
         if (np <= kJoinFew) {
 #pragma unroll 1
             for (int r0 = warp; r0 < rows; r0 += 2 * kJoinWarps) {   // two rows a warp at a time: all loads first
@@ -1134,8 +1124,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
                         for (int i = 0; i < C; ++i) y[i] += e == 0.f ? 0.f : e * x[b][k][i];
                     }
                     const int tok = (row0 + r) / a.G, qh = h * a.G + (row0 + r) - tok * a.G;
-                    float* row = MODE == kAlone ? nullptr : a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+                    const int64_t at = ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+                    const float* row = others + at;
                     if (MODE == kGroups) {
+                        float* row = a.rows.at + at;
 #pragma unroll
                         for (int i = 0; i < C; ++i) row[lane + 32 * i] = y[i];
                         if (lane == 0) *reinterpret_cast<float2*>(row + D) = make_float2(all, total);
@@ -1214,8 +1206,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
                     y += e == 0.f ? 0.f : e * accs[k][d];
                 }
                 const int tok = (row0 + row) / a.G, qh = h * a.G + (row0 + row) - tok * a.G;
-                float* own = MODE == kAlone ? nullptr : a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+                const int64_t at = ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+                const float* own = others + at;
                 if (MODE == kGroups) {
+                    float* own = a.rows.at + at;
                     own[d] = y;
                     if (d == 0) *reinterpret_cast<float2*>(own + D) = make_float2(all, total);
                     continue;
@@ -1229,6 +1223,50 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
                 if (a.lse && d == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(all, total);
             }
             __syncthreads();
+        }
+    };
+    // (kLast) The rows of an item that was not cut, a warp a row.
+    auto whole = [&](const KvItem& it, int item) {
+        wait();
+        const int h = item % a.pool.Hkv, row0 = item / a.pool.Hkv * R, rows = min(R, it.rows - row0);
+        for (int r = warp; r < rows; r += kJoinWarps) {
+            const int tok = (row0 + r) / a.G, qh = h * a.G + (row0 + r) - tok * a.G;
+            const int64_t at = ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+            const float2 there = __ldcg(reinterpret_cast<const float2*>(a.rows.at + at + D)), own = __ldcg(reinterpret_cast<const float2*>(a.rows.own + at + D));
+            float x[C], y[C], big = there.x, sum = there.y;
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                x[i] = __ldcg(a.rows.own + at + lane + 32 * i);
+                y[i] = __ldcg(a.rows.at + at + lane + 32 * i);
+            }
+            if (kv_row_done(own)) continue;
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                big = there.x;
+                sum = there.y;
+                kv_add_part(big, sum, y[i], own, x[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < C; ++i) o_put<BF16>(a.out, (it.seq.first + tok) * a.o_token + (int64_t)qh * a.o_head + lane + 32 * i, sum == 0.f ? 0.f : y[i] / sum);
+            if (a.lse && lane == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(big, sum);
+        }
+    };
+    auto walk_whole = [&]() {   // the items whose tokens' units are all this CTA's
+        int s = range.s;
+        KvItem it = range.item;
+        long long start = range.u0 - range.in_seq;
+        int item = kv_div(range.in_seq, it.cost());
+        while (true) {
+            while (item >= it.row_tiles * a.pool.Hkv) {
+                start += (long long)it.row_tiles * a.pool.Hkv * it.cost();
+                item = 0;
+                if (++s >= a.seqs.S) return;
+                it = kv_item<R, MODE>(a, s);
+            }
+            const long long first = start + (long long)item * it.cost() + kKvStart;
+            if (first >= range.u1) return;
+            if (first >= range.u0 && first + it.tiles <= range.u1) whole(it, item);
+            ++item;
         }
     };
     auto walk = [&]() {
@@ -1256,11 +1294,14 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 5) us_kv_join_kernel(const __
         const long long first = start + (long long)item * it.cost() + kKvStart, end = first + it.tiles;
         if (first >= range.u0 && first < range.u1 && end > range.u1) join(it, s, item, me, range.shares.owner(end - 1));
     };
-    if (range.u0 < range.u1) walk();
+    if (range.u0 < range.u1) {
+        if (MODE == kLast) walk_whole();
+        walk();
+    }
     wait();
 }
 
-// Attention over the sequences' own tokens beside the kernel of their groups, or in front of it: short contexts, of which a block's shared memory, barriers and joins take longer than the
+// Attention over the sequences' own tokens beside the kernel of their groups: short contexts, of which a block's shared memory, barriers and joins take longer than the
 // tokens (6 us an item; 64 sequences of up to 512 tokens, 64/8 heads, by themselves: 26 us). A warp has an item (sequence, 8 rows, head) from its queries to its output, with K and V
 // straight from memory to the registers that the products read: a row's 128 (64) bytes are four lanes' pieces. K of the next 32 tokens is on its way during the product with V, V during
 // the next scores. Nothing here waits for another warp. Sums go to rows where the sequence has a prefix, else to the output.
@@ -1272,8 +1313,7 @@ __global__ void __launch_bounds__(32, 12) us_kv_short_kernel(const __grid_consta
     constexpr int R = 8, C = D / 8;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const KvPool& p = a.pool;
-    // (Behind the groups' kernel: its blocks are all past the wait, so what that waits for is complete.)
-    if (!a.behind) asm volatile("griddepcontrol.wait;" ::: "memory");
+    // (Behind the groups' kernel, whose blocks are all past their wait: what that waits for is complete.)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t w = blockIdx.x, index = w / (uint32_t)p.Hkv;
     const int h = (int)(w - index * (uint32_t)p.Hkv);
@@ -1428,7 +1468,7 @@ __global__ void __launch_bounds__(32, 12) us_kv_short_kernel(const __grid_consta
                 y[2 * k] = o[k][0][c] * back;
                 y[2 * k + 1] = o[k][0][c + 2] * back;
             }
-            float* row = a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+            float* row = a.rows.own + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
             // (a row without a prefix is complete here; should a group have it all the same, as a padded one, its join is told to leave it alone)
             if (g == 0) *reinterpret_cast<float2*>(row + D) = joined ? make_float2(m[0][c], sum) : make_float2(INFINITY, 0.f);
             if (joined) {
@@ -1442,7 +1482,7 @@ __global__ void __launch_bounds__(32, 12) us_kv_short_kernel(const __grid_consta
         }
     }
     // (What follows in the stream waits for this grid alone: it may not end before the groups' kernel. One block is enough: the others make room.)
-    if (a.behind && blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 }  // namespace us

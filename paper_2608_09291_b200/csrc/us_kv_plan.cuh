@@ -71,6 +71,9 @@ AttendPlan few_plan(int D, bool bf16, int64_t N, int64_t S, int64_t G, int sms)
     if (D == 128) return few ? attend_shape<128, 1, MODE>(bf16, sms) : attend_shape<128, 2, MODE>(bf16, sms);
     return few ? attend_shape<64, 1, MODE>(bf16, sms) : attend_shape<64, 2, MODE>(bf16, sms);
 }
+// The join of groups with few rows and their sequences' own tokens.
+template <int D, int NT>
+const void* last_join(bool bf16) { return bf16 ? (const void*)us_kv_join_kernel<D, NT, true, kLast> : (const void*)us_kv_join_kernel<D, NT, false, kLast>; }
 template <int MODE>
 AttendPlan attend_plan(int D, bool bf16, int64_t N, int64_t S, int64_t G, int64_t Hkv, int64_t longest, int sms)
 {
@@ -121,23 +124,22 @@ inline us_status attend_args(const us_kv* h, const KvSeqs& q, const AttendArgs& 
     while ((1 << a->log2_T) < h->pool.T) ++a->log2_T;
     return kv_error_word(&a->pool.err);
 }
-// The kernel of short contexts, beside the groups' kernel or in front of it; join: of both.
+// The kernel of short contexts, beside the groups' kernel; join: of both.
 struct Beside {
     const void *kernel, *join;
     KvSeqs own;
     int64_t blocks;
 };
-inline us_status short_run(us_kv* h, const AttendArgs& x, const Beside& b, const KvRows& rows, bool behind, cudaStream_t st)
+inline us_status short_run(us_kv* h, const AttendArgs& x, const Beside& b, const KvRows& rows, cudaStream_t st)
 {
     KvAttend a;
     const us_status s = attend_args(h, b.own, x, rows, &a);
     if (s != US_OK) return s;
-    a.behind = behind;
     void* args[] = {&a};
     const cudaError_t e = ops_kernel_beside(b.kernel);
     return kv_cuda(e != cudaSuccess ? e : ops_launch(b.kernel, dim3((unsigned)b.blocks), 32, 0, st, args));
 }
-// rows: see KvRows (unused by kAlone's kernels). beside: (prompts of groups) what runs beside them, and joins all.
+// rows: see KvRows (unused by kAlone's kernels). beside: (groups) what runs beside them, and joins all.
 inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, const AttendPlan& pl, const KvRows& rows, void* scratch, cudaStream_t st,
                             const Beside* beside = nullptr)
 {
@@ -169,7 +171,7 @@ inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, cons
         const int threads = PrShape<128>::kThreads;
         if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.splits)), threads, pl.smem, st, args);
         if (e == cudaSuccess && beside) {
-            const us_status s = short_run(h, x, *beside, rows, true, st);
+            const us_status s = short_run(h, x, *beside, rows, st);
             if (s != US_OK) return s;
             e = ops_launch(beside->join, dim3((unsigned)(pl.tiles * h->pool.Hkv * (h->pool.D / 4))), 256, 0, st, args);
         } else if (e == cudaSuccess && pl.splits > 1) e = ops_launch(pl.join, dim3((unsigned)(pl.tiles * h->pool.Hkv * pl.join_blocks)), kPrRows, 0, st, args);
@@ -186,6 +188,14 @@ inline us_status attend_run(us_kv* h, const KvSeqs& q, const AttendArgs& x, cons
     cudaError_t e = ops_kernel_allow(pl.kernel, pl.smem);
     void* args[] = {&a};
     if (e == cudaSuccess) e = ops_launch(pl.kernel, dim3((unsigned)pl.ctas), 160, pl.smem, st, args);
+    if (beside) {
+        if (e == cudaSuccess) {
+            const us_status b = short_run(h, x, *beside, rows, st);
+            if (b != US_OK) return b;
+        }
+        if (e == cudaSuccess) e = ops_launch(beside->join, dim3((unsigned)pl.ctas), 32 * kJoinWarps, 0, st, args);
+        return kv_cuda(e);
+    }
     // (an item of one unit is never cut)
     if (e == cudaSuccess && (int64_t)q.width * h->pool.T > kKvTile) e = ops_launch(pl.join, dim3((unsigned)pl.ctas), 32 * kJoinWarps, 0, st, args);
     return kv_cuda(e);

@@ -780,7 +780,7 @@ __global__ void __launch_bounds__(256) us_kv_shared_join_kernel(const __grid_con
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (!have || local >= it.rows) return;
     const int r = it.row0 + local, tok = r / a.G, qh = h * a.G + r - tok * a.G;
-    const float* row = a.rows.at + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
+    const float* row = a.rows.own + ((it.seq.first + tok) * a.Hq + qh) * a.rows.pitch;
     const float* part = a.part + (int64_t)u * a.splits * S::kPart;
     float m[MOST + 1], l[MOST + 1];
     float4 x[MOST + 1];

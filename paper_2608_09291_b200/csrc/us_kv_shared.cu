@@ -11,7 +11,7 @@ namespace {
 struct SharedPlan {
     AttendPlan groups, own;
     int64_t rows, first, bytes;   // bytes of the rows; where the own part's scratch begins; in all
-    const void *short_kernel, *join;   // short contexts: their kernel, in front of the groups' (which joins) or (join) beside it; nullptr: behind it, and joins
+    const void *short_kernel, *join;   // short contexts: their kernel runs beside the groups', another joins what they leave; nullptr: the own tokens' kernel does
     int64_t short_blocks;
 };
 constexpr int64_t kShort = 2048;   // tokens that a warp reads by itself (a table's width says how many there may be)
@@ -25,7 +25,7 @@ SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q,
     r.own = attend_plan<kOwn>(h->pool.D, bf16, N, q->n_seqs, G, h->pool.Hkv, q->table_width * T, sms);
     if (p->n_seqs > 0) {
         r.groups = attend_plan<kGroups>(h->pool.D, bf16, N, p->n_seqs, G, h->pool.Hkv, p->table_width * T, sms);
-        r.rows = N * heads * pitch(h) * 4;
+        r.rows = N * heads * pitch(h) * 4;   // (twice, where the own tokens have rows, too)
     }
     const int64_t longest = q->table_width * T;
     if (p->n_seqs > 0 && r.own.tiles == 0 && longest <= kShort) {
@@ -33,7 +33,11 @@ SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q,
         r.short_kernel = h->pool.D == 128 ? (bf16 ? (const void*)us_kv_short_kernel<128, true> : (const void*)us_kv_short_kernel<128, false>) :
                                             (bf16 ? (const void*)us_kv_short_kernel<64, true> : (const void*)us_kv_short_kernel<64, false>);
         r.own.scratch = 0;
-        if (r.groups.tiles == 0) r.groups = few_plan<kLast>(h->pool.D, bf16, N, p->n_seqs, G, sms);
+        if (r.groups.tiles == 0) {
+            const bool eight = r.groups.rows == 8;
+            if (h->pool.D == 128) r.join = eight ? last_join<128, 1>(bf16) : last_join<128, 2>(bf16);
+            else r.join = eight ? last_join<64, 1>(bf16) : last_join<64, 2>(bf16);
+        }
     }
     if (r.short_kernel && r.groups.tiles > 0) {
         // Many rows a group, short contexts of their own: the first kernel is bound by its softmax, the second by latency, so they share the GPU. The number of parts that
@@ -56,6 +60,7 @@ SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q,
         r.join = h->pool.D == 128 ? (bf16 ? (const void*)us_kv_shared_join_kernel<128, true> : (const void*)us_kv_shared_join_kernel<128, false>) :
                                     (bf16 ? (const void*)us_kv_shared_join_kernel<64, true> : (const void*)us_kv_shared_join_kernel<64, false>);
     }
+    if (r.short_kernel) r.rows *= 2;
     r.first = up16(r.rows) + up16(r.groups.scratch);
     r.bytes = r.first + r.own.scratch;
     return r;
@@ -110,9 +115,8 @@ us_status us_kv_shared_attention(us_kv* h, const us_kv_seqs* prefixes, const us_
     if (pl.short_kernel) {
         if (pl.short_blocks >= (1ll << 31)) return US_ERR_UNSUPPORTED;
         const Beside beside = {pl.short_kernel, pl.join, kv_seqs(q, N), pl.short_blocks};
-        if (pl.join) return attend_run(h, g, x, pl.groups, rows, mem + up16(pl.rows), st, &beside);
-        s = short_run(h, x, beside, rows, false, st);
-        return s != US_OK ? s : attend_run(h, g, x, pl.groups, rows, mem + up16(pl.rows), st);
+        rows.own = rows.at + N * n_heads * pitch(h);
+        return attend_run(h, g, x, pl.groups, rows, mem + up16(pl.rows), st, &beside);
     }
     s = attend_run(h, g, x, pl.groups, rows, mem + up16(pl.rows), st);   // (writes rows alone)
     if (s != US_OK) return s;
