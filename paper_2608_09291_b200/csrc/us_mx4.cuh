@@ -1323,6 +1323,7 @@ __global__ void __launch_bounds__(EPI ? 384 : 192, 1) us_mx4_pair_kernel(const _
                 else mx4_pair_store<__nv_bfloat16>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
             }
         }
+        if (EPI) asm volatile("cp.async.wait_all;" ::: "memory");   // (nothing may be in flight when the block ends)
     };
     // With an epilogue the warps from 4 on have the sums, 2 and 3 only fill their group. Registers of a thread: 168 at launch; 128 x 72 + 256 x 216 = 384 x 168.
     if (!EPI || warp < 4) {
