@@ -29,7 +29,7 @@ SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q,
     }
     const int64_t longest = q->table_width * T;
     if (p->n_seqs > 0 && r.own.tiles == 0 && longest <= kShort) {
-        r.short_blocks = (N * G / 8 + q->n_seqs) * h->pool.Hkv;
+        r.short_blocks = (q->cu_tokens ? N * G / 8 + q->n_seqs : N * ((G + 7) / 8)) * h->pool.Hkv;   // a warp an item: as many as there may be
         r.short_kernel = h->pool.D == 128 ? (bf16 ? (const void*)us_kv_short_kernel<128, true> : (const void*)us_kv_short_kernel<128, false>) :
                                             (bf16 ? (const void*)us_kv_short_kernel<64, true> : (const void*)us_kv_short_kernel<64, false>);
         r.own.scratch = 0;
