@@ -720,7 +720,8 @@ __global__ void __launch_bounds__(kPrRows) us_kv_prompt_join_kernel(const __grid
     if (a.lse && c0 == 0) a.lse[(it.seq.first + tok) * a.Hq + qh] = kv_lse(big, sum);
 }
 
-// (kGroups) The same into the rows: a thread a row, four of D a block, all parts' loads at once (64 sequences' rows of 64 heads, nine parts each: MEASURED).
+// (kGroups) The same into the rows: a thread a row, four of D a block, all parts' loads at once (64 sequences' rows of 64 heads, nine parts each, from memory: 9 us;
+// 16 of D a block, two parts at a time: 14).
 template <int D>
 __global__ void __launch_bounds__(kPrRows) us_kv_rows_join_kernel(const __grid_constant__ KvPrompt a)
 {

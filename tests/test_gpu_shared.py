@@ -337,3 +337,29 @@ def test_refusals(b):
         with pytest.raises(ValueError):
             cache.shared_attention(*a)
     assert cache.shared_attention(q[:0], ptable, plen, cu_seqs, table[:0], lengths[:0]).shape == (0, 4, 128)
+
+
+@pytest.mark.parametrize("new,S,wide", [(1, 2, None), (1, 40, None), (1, 3, 12), (30, 4, None)])
+def test_offsets_past_32_bits(b, new, S, wide):
+    """Prefix and own tokens in blocks behind 4 GB of a pool; every kind of kernels; and copies to and from there."""
+    T, Hkv, D = 256, 8, 128
+    blocks = 17000                                      # 4.4e9 bytes of K
+    codes = [torch.zeros(blocks, Hkv, T, D, dtype=torch.int8, device="cuda") for _ in range(2)]
+    steps = [torch.full((blocks, Hkv), 1 / 32, device="cuda") for _ in range(2)]
+    g = gen(1)
+    far = blocks - 50
+    for c in codes:
+        c[far:] = (torch.randn(50, Hkv, T, D, device="cuda", generator=g) * 32).round().clamp(-127, 127).to(torch.int8)
+    cache = b.KVCache(*codes, *steps)
+    ptable, table = ints([[far, far + 1]]), torch.zeros(S, wide or 1, dtype=torch.int32, device="cuda")
+    table[:, 0] = far + 2 + torch.arange(S, device="cuda").int()
+    own = [new + 20] * S
+    q = torch.randn(S * new, Hkv, D, device="cuda", generator=g).bfloat16()
+    out = cache.shared_attention(q, ptable, ints([300]), ints([0, S]), table, ints(own), None if new == 1 else sums([new] * S))
+    cache.check()
+    ref, bound, _ = reference(cache, ptable, [300], [0] * S, table, own, [new] * S, q, D ** -0.5)
+    check(out, ref, bound)
+    cache.copy_blocks(ints([far, 3]), ints([1, far + 49]))
+    cache.check()
+    for c in codes:
+        assert torch.equal(c[1], c[far]) and not c[far + 49].any()
