@@ -431,8 +431,9 @@ us_status us_kv_destroy(us_kv* h);
  *   tokens held and the steps; the first free block of the sequence's share): new tokens may be appended. Where the sequences of the call are the only ones that hold it, the first of
  *   them keeps it. If the free blocks do not suffice (US_ERR_OUT_OF_BLOCKS), the first sequence that does not fit and all behind it that need blocks stay as they are; so does a
  *   sequence with an entry or length that does not fit. scratch: us_kv_extend_scratch bytes, 16-byte aligned, for one call at a time; need not be cleared.
- * us_kv_compact: the blocks in use become the pool's first `used` (device int32) ones: those behind move to the free places in front, both in order. map[b]
- *   (device, n_blocks int32) is where block b's tokens are now (b itself where it did not move): us_kv_remap takes every table there. scratch: us_kv_compact_scratch.
+ * us_kv_compact: the blocks in use become the pool's first `used` (device int32) ones: those behind move to the free places in front, both in order. The entries of the
+ *   n_tables tables (tables: host array; block_table is written, cu_tokens not read) follow them. map[b] (device, n_blocks int32) is where block b's tokens are now (b itself where it did
+ *   not move): us_kv_remap takes a further table there. Every table that is in use has to follow. scratch: us_kv_compact_scratch bytes.
  * us_kv_copy_blocks: block src[i] (all its tokens and steps) to block dst[i], i < n; dst[i] = -1: nothing. No block is twice in dst, or in dst and src.
  * All are enqueue-only on `stream`. Errors: INVALID_ARG, SCRATCH_TOO_SMALL, CUDA.
  */
@@ -443,9 +444,9 @@ int64_t us_kv_extend_scratch(const us_kv* h, int32_t n_seqs);
 us_status us_kv_extend(us_kv* h, int32_t* refs, int32_t* table, int64_t table_stride, int32_t table_width, int32_t* lengths, int32_t n_seqs,
                        const int32_t* tokens, int32_t tokens_each, void* scratch, int64_t scratch_bytes, void* stream);
 int64_t us_kv_compact_scratch(const us_kv* h);
-us_status us_kv_compact(us_kv* h, int32_t* refs, int32_t* map, int32_t* used, void* scratch, int64_t scratch_bytes, void* stream);
-us_status us_kv_remap(us_kv* h, const int32_t* map, int32_t* table, int64_t table_stride, int32_t table_width, const int32_t* lengths, int32_t n_seqs,
-                      void* stream);
+us_status us_kv_compact(us_kv* h, int32_t* refs, const us_kv_seqs* tables, int32_t n_tables, int32_t* map, int32_t* used, void* scratch,
+                        int64_t scratch_bytes, void* stream);
+us_status us_kv_remap(us_kv* h, const int32_t* map, const us_kv_seqs* table, void* stream);
 us_status us_kv_copy_blocks(us_kv* h, const int32_t* src, const int32_t* dst, int64_t n, void* stream);
 
 /*

@@ -117,8 +117,8 @@ _lib.us_kv_extend_scratch.restype = _i64
 _lib.us_kv_extend.argtypes = [_vp, _vp, _vp, _i64, _i32, _vp, _i32, _vp, _i32, _vp, _i64, _vp]
 _lib.us_kv_compact_scratch.argtypes = [_vp]
 _lib.us_kv_compact_scratch.restype = _i64
-_lib.us_kv_compact.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _vp]
-_lib.us_kv_remap.argtypes = [_vp, _vp, _vp, _i64, _i32, _vp, _i32, _vp]
+_lib.us_kv_compact.argtypes = [_vp, _vp, _seqs, _i32, _vp, _vp, _vp, _i64, _vp]
+_lib.us_kv_remap.argtypes = [_vp, _vp, _seqs, _vp]
 _lib.us_kv_copy_blocks.argtypes = [_vp, _vp, _vp, _i64, _vp]
 
 

@@ -250,13 +250,39 @@ __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
     }
 }
 
+// A table's entry j of sequence s after the blocks have moved.
+__device__ __forceinline__ void remap(const Pages& a, const int32_t* map, const KvSeqs& q, int64_t s, int j)
+{
+    const int32_t len = __ldcg(q.lengths + s);
+    const bool bad = len < 0 || len > (int64_t)q.width << a.log2_T;
+    if (bad && j == 0) wrong(a);
+    if (bad || j >= blocks_of(len, a.log2_T)) return;
+    int32_t* at = const_cast<int32_t*>(q.table) + s * q.table_stride + j;
+    const int32_t b = *at;
+    if (in_pool(a, b)) *at = __ldcg(map + b);
+    else wrong(a);
+}
+// Tables whose entries follow the blocks in the launch that moves them.
+constexpr int kTables = 4;
+struct Tables {
+    KvSeqs q[kTables];
+    const int32_t* map;
+    int32_t n;
+};
+
 // Copies of blocks: the first `held` tokens (or all) of block src[i] and the steps to block dst[i], where dst[i] >= 0. A warp has 4 KB of a head at a time.
 // Bound by memory.
-__global__ void __launch_bounds__(256) us_kv_copy_kernel(Pages a, const int32_t* src, const int32_t* dst, const int32_t* held, int64_t n, const int32_t* n_device)
+__global__ void __launch_bounds__(256) us_kv_copy_kernel(Pages a, const int32_t* src, const int32_t* dst, const int32_t* held, int64_t n, const int32_t* n_device,
+                                                         const __grid_constant__ Tables tables)
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (n_device) n = __ldcg(n_device);
+    for (int t = 0; t < tables.n; ++t) {
+        const KvSeqs& q = tables.q[t];
+        for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < (int64_t)q.S * q.width; i += (int64_t)gridDim.x * blockDim.x)
+            remap(a, tables.map, q, i / q.width, (int)(i % q.width));
+    }
     const KvPool& p = a.pool;
     const int lane = threadIdx.x & 31, size = p.D << a.log2_T, chunks = (size + 4095) / 4096;
     const int64_t units = n * 2 * p.Hkv * chunks, step = ((int64_t)gridDim.x * blockDim.x) >> 5;
@@ -339,22 +365,13 @@ __global__ void __launch_bounds__(1024) us_kv_compact_kernel(Pages a, int32_t* m
     }
 }
 
-// A table's entries after the blocks have moved (a row blockIdx.y, a thread an entry).
-__global__ void __launch_bounds__(kEntries) us_kv_remap_kernel(Pages a, const int32_t* map, int32_t* table, KvSeqs q)
+// A row blockIdx.y, a thread an entry.
+__global__ void __launch_bounds__(kEntries) us_kv_remap_kernel(Pages a, const int32_t* map, KvSeqs q)
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int j = (int)(blockIdx.x * kEntries + threadIdx.x);
-    for (int64_t s = blockIdx.y; s < q.S; s += gridDim.y) {
-        const int32_t len = __ldcg(q.lengths + s);
-        const bool bad = len < 0 || len > (int64_t)q.width << a.log2_T;
-        if (bad && j == 0) wrong(a);
-        if (bad || j >= blocks_of(len, a.log2_T)) continue;
-        int32_t* at = table + s * q.table_stride + j;
-        const int32_t b = *at;
-        if (in_pool(a, b)) *at = __ldcg(map + b);
-        else wrong(a);
-    }
+    for (int64_t s = blockIdx.y; s < q.S; s += gridDim.y) remap(a, map, q, s, j);
 }
 
 dim3 entries(int64_t rows, int64_t width) { return dim3((unsigned)std::max<int64_t>(1, (width + kEntries - 1) / kEntries), (unsigned)std::min<int64_t>(rows, 65535)); }
@@ -371,11 +388,12 @@ us_status begin(us_kv* h, int32_t* refs, Pages* a)
     while ((1 << a->log2_T) < h->pool.T) ++a->log2_T;
     return kv_error_word(&a->pool.err);
 }
-us_status copy(const Pages& a, const int32_t* src, const int32_t* dst, const int32_t* held, int64_t n, const int32_t* n_device, cudaStream_t st)
+us_status copy(const Pages& a, const int32_t* src, const int32_t* dst, const int32_t* held, int64_t n, const int32_t* n_device, cudaStream_t st, const Tables* tables = nullptr)
 {
+    Tables none = {};
     const int64_t chunks = ((int64_t)a.pool.D * a.pool.T + 4095) / 4096, units = n * 2 * a.pool.Hkv * chunks;
     const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((units + 7) / 8, 8 * ops_sms())));
-    void* args[] = {const_cast<Pages*>(&a), &src, &dst, &held, &n, &n_device};
+    void* args[] = {const_cast<Pages*>(&a), &src, &dst, &held, &n, &n_device, tables ? const_cast<Tables*>(tables) : &none};
     return kv_cuda(ops_launch((const void*)us_kv_copy_kernel, grid, 256, 0, st, args));
 }
 
@@ -464,34 +482,45 @@ us_status us_kv_extend(us_kv* h, int32_t* refs, int32_t* table, int64_t table_st
 
 int64_t us_kv_compact_scratch(const us_kv* h) { return h ? 4 * (2 * (int64_t)h->pool.blocks + 1) : -1; }
 
-us_status us_kv_compact(us_kv* h, int32_t* refs, int32_t* map, int32_t* used, void* scratch, int64_t scratch_bytes, void* stream)
+// A table as the kernels see it, its entries to be written.
+static bool table_ok(const us_kv* h, const us_kv_seqs* t)
 {
-    if (!h || !refs_ok(refs) || !map || !used || !kv_aligned(map, 4) || !kv_aligned(used, 4)) return US_ERR_INVALID_ARG;
+    us_kv_seqs q = *t;
+    q.cu_tokens = nullptr;
+    return kv_seqs_ok(h, &q, q.n_seqs);
+}
+
+us_status us_kv_compact(us_kv* h, int32_t* refs, const us_kv_seqs* tables, int32_t n_tables, int32_t* map, int32_t* used, void* scratch, int64_t scratch_bytes, void* stream)
+{
+    if (!h || !refs_ok(refs) || n_tables < 0 || (n_tables > 0 && !tables) || !map || !used || !kv_aligned(map, 4) || !kv_aligned(used, 4)) return US_ERR_INVALID_ARG;
+    for (int i = 0; i < n_tables; ++i)   // (all of them before a block moves)
+        if (!table_ok(h, tables + i)) return US_ERR_INVALID_ARG;
     if (!scratch || !kv_aligned(scratch, 16) || scratch_bytes < us_kv_compact_scratch(h)) return US_ERR_SCRATCH_TOO_SMALL;
     Pages a;
-    const us_status s = begin(h, refs, &a);
+    us_status s = begin(h, refs, &a);
     if (s != US_OK) return s;
     int32_t *src = static_cast<int32_t*>(scratch), *dst = src + a.pool.blocks, *moves = dst + a.pool.blocks;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     void* args[] = {&a, &map, &used, &src, &dst, &moves};
-    const us_status k = kv_cuda(ops_launch((const void*)us_kv_compact_kernel, dim3(1), 1024, 0, st, args));
-    return k != US_OK ? k : copy(a, src, dst, nullptr, a.pool.blocks, moves, st);
+    s = kv_cuda(ops_launch((const void*)us_kv_compact_kernel, dim3(1), 1024, 0, st, args));
+    Tables here = {};
+    here.map = map;
+    int i = 0;
+    for (; i < n_tables && here.n < kTables; ++i)
+        if (tables[i].n_seqs > 0) here.q[here.n++] = kv_seqs(tables + i, 0);
+    if (s == US_OK) s = copy(a, src, dst, nullptr, a.pool.blocks, moves, st, &here);
+    for (; s == US_OK && i < n_tables; ++i) s = us_kv_remap(h, map, tables + i, stream);
+    return s;
 }
 
-us_status us_kv_remap(us_kv* h, const int32_t* map, int32_t* table, int64_t table_stride, int32_t table_width, const int32_t* lengths, int32_t n_seqs, void* stream)
+us_status us_kv_remap(us_kv* h, const int32_t* map, const us_kv_seqs* table, void* stream)
 {
-    us_kv_seqs q = {};
-    q.block_table = table;
-    q.table_stride = table_stride;
-    q.lengths = lengths;
-    q.n_seqs = n_seqs;
-    q.table_width = table_width;
-    if (!kv_seqs_ok(h, &q, n_seqs) || !map || !kv_aligned(map, 4)) return US_ERR_INVALID_ARG;
-    if (n_seqs == 0) return US_OK;
+    if (!h || !table || !table_ok(h, table) || !map || !kv_aligned(map, 4)) return US_ERR_INVALID_ARG;
+    if (table->n_seqs == 0) return US_OK;
     Pages a;
     const us_status s = begin(h, nullptr, &a);
     if (s != US_OK) return s;
-    KvSeqs k = kv_seqs(&q, 0);
-    void* args[] = {&a, &map, &table, &k};
-    return kv_cuda(ops_launch((const void*)us_kv_remap_kernel, entries(n_seqs, table_width), kEntries, 0, static_cast<cudaStream_t>(stream), args));
+    KvSeqs q = kv_seqs(table, 0);
+    void* args[] = {&a, &map, &q};
+    return kv_cuda(ops_launch((const void*)us_kv_remap_kernel, entries(q.S, q.width), kEntries, 0, static_cast<cudaStream_t>(stream), args));
 }

@@ -748,12 +748,10 @@ PyObject* kv_compact(PyObject*, PyObject* const* a, Py_ssize_t n)
     if (!PyTuple_Check(a[3])) return bad("tables must be (table, lengths) pairs");
     const Py_ssize_t tables = PyTuple_GET_SIZE(a[3]);
     std::vector<us_kv_seqs> q((size_t)tables);
-    for (Py_ssize_t i = 0; i < tables; ++i) {   // (all of them are looked at before a block moves)
+    for (Py_ssize_t i = 0; i < tables; ++i) {
         PyObject* t = PyTuple_GET_ITEM(a[3], i);
         if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 2) return bad("tables must be (table, lengths) pairs");
         if (!take_seqs(PyTuple_GET_ITEM(t, 0), PyTuple_GET_ITEM(t, 1), Py_None, -1, *pool, &q[(size_t)i])) return nullptr;
-        if (q[(size_t)i].n_seqs > 0 && (q[(size_t)i].table_width < 1 || (int64_t)q[(size_t)i].table_width * pool->size(2) >= (1ll << 31) - (1 << 16)))
-            return bad("a table is empty or too wide");
     }
     const int64_t bytes = us_kv_compact_scratch(static_cast<us_kv*>(h)), map_bytes = (4 * pool->size(0) + 15) / 16 * 16;
     at::Tensor scratch = at::detail::empty_cuda({map_bytes + bytes}, at::kByte, pool->device(), std::nullopt);   // the map first
@@ -761,10 +759,8 @@ PyObject* kv_compact(PyObject*, PyObject* const* a, Py_ssize_t n)
     at::Tensor used = at::detail::empty_cuda(at::IntArrayRef{}, at::kInt, pool->device(), std::nullopt);
     us_status s;
     Py_BEGIN_ALLOW_THREADS
-    s = us_kv_compact(static_cast<us_kv*>(h), refs, map, static_cast<int32_t*>(used.data_ptr()), static_cast<uint8_t*>(scratch.data_ptr()) + map_bytes, bytes, at_.stream);
-    for (const us_kv_seqs& t : q)
-        if (s == US_OK)
-            s = us_kv_remap(static_cast<us_kv*>(h), map, const_cast<int32_t*>(t.block_table), t.table_stride, t.table_width, t.lengths, t.n_seqs, at_.stream);
+    s = us_kv_compact(static_cast<us_kv*>(h), refs, q.data(), (int32_t)tables, map, static_cast<int32_t*>(used.data_ptr()), static_cast<uint8_t*>(scratch.data_ptr()) + map_bytes, bytes,
+                      at_.stream);
     Py_END_ALLOW_THREADS
     if (s != US_OK) return fail(s, "us_kv_compact");
     return THPVariable_Wrap(std::move(used));

@@ -270,7 +270,8 @@ def test_compact(b, blocks, fill):
         m.refs[x] += 1
     pages.refs.copy_(ints(m.refs))
     before = [x.clone() for x in cache.read(table, lengths, 16 * width)]
-    used = pages.compact([(table, lengths), (twin, twin_n)])
+    more = [(table[s:s + 1].clone(), lengths[s:s + 1].clone()) for s in (0, 1, 2, 1, 0)]
+    used = pages.compact([(table, lengths), (twin, twin_n), (table[:0], lengths[:0])] + more)
     pages.check()
     n = len(ids)
     src, dst = [i for i in range(n, blocks) if m.refs[i]], [i for i in range(n) if not m.refs[i]]
@@ -281,6 +282,8 @@ def test_compact(b, blocks, fill):
     assert used.dim() == 0 and int(used) == n and all(m.refs[:n]) and not any(m.refs[n:])
     same(cache, pages, m, table, lengths, [[to.get(x, x) if j < len(p) else x for j, x in enumerate(row)] for p, row in zip(per, rows)], lengths.tolist())
     assert torch.equal(twin[0, :len(per[0])], table[0, :len(per[0])])
+    for (t, _), s in zip(more, (0, 1, 2, 1, 0)):   # (more tables than one launch takes)
+        assert torch.equal(t[0, :len(per[s])], table[s, :len(per[s])])
     for x, y in zip(before, cache.read(table, lengths, 16 * width)):
         assert torch.equal(x, y)
 

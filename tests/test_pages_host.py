@@ -49,15 +49,18 @@ def test_other_refusals(b, h):
     lib = b._lib
     q = b.us_kv_seqs(block_table=P, table_stride=10, lengths=P, cu_tokens=None, n_seqs=3, table_width=10)
     assert lib.us_kv_release(h, None, ctypes.byref(q), None) == INVALID and lib.us_kv_release(h, P, None, None) == INVALID and lib.us_kv_release(None, P, ctypes.byref(q), None) == INVALID
-    for a in ((None, P, P, P, 1 << 30), (P + 4, P, P, P, 1 << 30), (P, None, P, P, 1 << 30), (P, P, None, P, 1 << 30), (P, P, P + 1, P, 1 << 30)):
+    q = ctypes.byref(q)
+    bad = ctypes.byref(b.us_kv_seqs(block_table=P, table_stride=9, lengths=P, cu_tokens=None, n_seqs=3, table_width=10))
+    for a in ((None, q, 1, P, P, P, 1 << 30), (P + 4, q, 1, P, P, P, 1 << 30), (P, None, 1, P, P, P, 1 << 30), (P, q, -1, P, P, P, 1 << 30), (P, bad, 1, P, P, P, 1 << 30),
+              (P, q, 1, None, P, P, 1 << 30), (P, q, 1, P, None, P, 1 << 30), (P, q, 1, P, P + 1, P, 1 << 30)):
         assert lib.us_kv_compact(h, *a, None) == INVALID
-    for a in ((P, P, P, None, 1 << 30), (P, P, P, P, 800), (P, P, P, P + 4, 1 << 30)):
+    for a in ((P, q, 1, P, P, None, 1 << 30), (P, None, 0, P, P, P, 800), (P, q, 1, P, P, P + 4, 1 << 30)):
         assert lib.us_kv_compact(h, *a, None) == TOO_SMALL
-    assert lib.us_kv_remap(h, None, P, 10, 10, P, 3, None) == INVALID and lib.us_kv_remap(h, P, P, 9, 10, P, 3, None) == INVALID
+    assert lib.us_kv_remap(h, None, q, None) == INVALID and lib.us_kv_remap(h, P, bad, None) == INVALID and lib.us_kv_remap(h, P, None, None) == INVALID
     for a in ((None, P, 1), (P, None, 1), (P, P, -1), (P + 2, P, 1), (P, P, 1 << 31)):
         assert lib.us_kv_copy_blocks(h, *a, None) == INVALID
     assert lib.us_kv_copy_blocks(None, P, P, 1, None) == INVALID and lib.us_kv_copy_blocks(h, None, None, 0, None) == 0
-    assert _fork(b, None) == INVALID and _extend(b, None) == INVALID and lib.us_kv_compact(None, P, P, P, P, 1 << 30, None) == INVALID
+    assert _fork(b, None) == INVALID and _extend(b, None) == INVALID and lib.us_kv_compact(None, P, None, 0, P, P, P, 1 << 30, None) == INVALID
     assert lib.us_kv_extend_scratch(None, 1) == -1 and lib.us_kv_extend_scratch(h, -1) == -1 and lib.us_kv_extend_scratch(h, 5) >= 4 * 5
     assert lib.us_kv_compact_scratch(None) == -1 and lib.us_kv_compact_scratch(h) >= 800
     assert "free blocks" in b.us_status_string(10)
