@@ -1319,9 +1319,17 @@ __global__ void __launch_bounds__(32, 12) us_kv_short_kernel(const __grid_consta
     const int h = (int)(w - index * (uint32_t)p.Hkv);
     KvItem it;
     int s = -1, row0 = 0;
-    {
+    bool any = false;
+    if (!a.seqs.cu) {   // a row each: nothing to add up
+        const uint32_t tiles = ((uint32_t)a.G + R - 1) / R;
+        if (index < (uint32_t)a.seqs.S * tiles) {
+            s = (int)(index / tiles);
+            row0 = R * (int)(index - (uint32_t)s * tiles);
+            it = kv_item<R>(a, kv_seq(a.seqs, p, s, any));
+            if (any) atomicExch(p.err, kErrIndex);
+        }
+    } else {
         uint32_t before = 0;
-        bool any = false;
         for (int base = 0; base < a.seqs.S; base += 32) {
             KvSeq mine = {0, 0, 0};
             if (base + lane < a.seqs.S) {
