@@ -429,8 +429,8 @@ us_status us_kv_destroy(us_kv* h);
  * us_kv_extend: room for tokens[s] more (device int32, or NULL: tokens_each for all) tokens of each sequence: free blocks, the lowest first, sequence by
  *   sequence, go to the table, and lengths[s] grows. Before that, a last block that is partly filled and that other entries hold, too, is replaced by a copy (of the
  *   tokens held and the steps; the first free block of the sequence's share): new tokens may be appended. Where the sequences of the call are the only ones that hold it, the first of
- *   them keeps it. If the free blocks do not suffice (US_ERR_OUT_OF_BLOCKS), the first sequence that does not fit and all behind it that need blocks stay as they are; so does a
- *   sequence with an entry or length that does not fit. scratch: us_kv_extend_scratch bytes, 16-byte aligned, for one call at a time; need not be cleared.
+ *   them keeps it. If the free blocks do not suffice (US_ERR_OUT_OF_BLOCKS), the first sequence that does not fit and all behind it that need blocks stay as they are; so does
+ *   one that would keep a block which one of those holds, and a sequence with an entry or length that does not fit. scratch: us_kv_extend_scratch bytes, 16-byte aligned, for one call at a time; need not be cleared.
  * us_kv_compact: the blocks in use become the pool's first `used` (device int32) ones: those behind move to the free places in front, both in order. The entries of the
  *   n_tables tables (tables: host array; block_table is written, cu_tokens not read) follow them. map[b] (device, n_blocks int32) is where block b's tokens are now (b itself where it did
  *   not move): us_kv_remap takes a further table there. Every table that is in use has to follow. scratch: us_kv_compact_scratch bytes.

@@ -198,6 +198,13 @@ __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
         found += sum;
     }
     __syncthreads();
+    // (Where blocks are short: a block that a sequence would keep for itself, and that another one goes on holding for want of a copy, is not written into.)
+    const bool want = total > found;
+    if (want) {
+        for (int s = threadIdx.x; s < e.S; s += 1024)
+            if (need_of[s] >= kCopy && (uint32_t)at_of[s] + (need_of[s] & (kCopy - 1)) + 1u > found) atomicExch(e.count + last_of[s], -1);
+        __syncthreads();
+    }
     // 4. (a sequence's blocks: its thread, or all of the warp where one of its sequences gets many)
     for (int base = threadIdx.x & ~31; base < e.S; base += 1024) {
         const int s = base + lane;
@@ -207,7 +214,8 @@ __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
         bool fits = what >= 0;
         if (fits) {
             const uint32_t need = what & (kCopy - 1), copy = what & kCopy ? 1 : 0, at = (uint32_t)at_of[s];
-            if (need + copy > 0 && at + need + copy > found) {
+            const bool stuck = want && !copy && last_of[s] >= 0 && __ldcg(e.count + last_of[s]) < 0;
+            if (stuck || (need + copy > 0 && at + need + copy > found)) {
                 atomicExch(a.pool.err, kErrFull);
                 fits = false;
             } else {

@@ -90,7 +90,7 @@ def test_parts(b, D, rotary, interleaved, dtype):
     run(b, 19, 5, 3, D, dtype, rotary=rotary, interleaved=interleaved, seed=D)
 
 
-@pytest.mark.parametrize("Hq,Hk", [(1, 0), (1, 1), (7, 1), (64, 8), (33, 0), (3, 5)])
+@pytest.mark.parametrize("Hq,Hk", [(1, 0), (1, 1), (7, 1), (64, 8), (33, 0), (3, 5), (0, 3)])
 @pytest.mark.parametrize("norm", [False, True])
 def test_heads(b, Hq, Hk, norm):
     run(b, 40, Hq, Hk, 128, BF16, norm=norm, seed=Hq)

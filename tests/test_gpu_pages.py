@@ -48,11 +48,21 @@ class Model:
             plan.append((need, part))
         free = [i for i, r in enumerate(self.refs) if r == 0]
         at, ok = 0, True
+        ends, stuck = [], set()   # blocks that a sequence goes on holding for want of a copy: nobody else writes into them
+        for need, part in plan:
+            at += need + part
+            ends.append(at)
+        for s, (need, part) in enumerate(plan):
+            if part and ends[s] > len(free):
+                stuck.add(table[s][self.count(lengths[s]) - 1])
+        keeps = {x: who[0] for x, who in last.items()}
+        at = 0
         for s, (need, part) in enumerate(plan):
             all_ = need + part
             here = free[at:at + all_]
             at += all_
-            if len(here) < all_:
+            block = table[s][self.count(lengths[s]) - 1] if lengths[s] else None
+            if len(here) < all_ or (not part and block in stuck and keeps.get(block) == s):
                 ok = False
                 continue
             have = self.count(lengths[s])
@@ -176,6 +186,26 @@ def test_who_keeps_the_last_block(b):
         m.extend(arow, an, [1, 1])
         same(cache, pages, m, again, k, arow, an)
         pages.check()
+
+
+@pytest.mark.parametrize("spare", [0, 1, 2])
+def test_a_block_is_not_written_while_another_holds_it(b, spare):
+    """Three children, fewer free blocks than copies: the one that would write on in the parents' block waits, too, unless all others have theirs."""
+    cache, pages, m = make(b, 2 + spare, 16)
+    rows, lens = [[0] * 3], [0]
+    table, lengths = ints(rows), ints(lens)
+    pages.extend(table, lengths, 21)
+    m.extend(rows, lens, [21])
+    child, n = pages.fork(table, lengths, ints([0, 0, 0]))
+    crow, cn = m.fork(rows, lens, [0, 0, 0], False)
+    pages.extend(child, n)
+    assert m.extend(crow, cn, [1, 1, 1]) == (spare == 2)
+    assert cn == {0: [21, 21, 21], 1: [21, 22, 21], 2: [22, 22, 22]}[spare]
+    if spare < 2:
+        with pytest.raises(b.UsError, match="free blocks"):
+            pages.check()
+    same(cache, pages, m, child, n, crow, cn)
+    pages.check()
 
 
 @pytest.mark.parametrize("blocks", [1, 15, 16, 17, 16383, 16385, 40000])
