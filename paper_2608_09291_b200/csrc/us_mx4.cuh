@@ -673,11 +673,11 @@ __device__ __forceinline__ void mx4_scalars(const void* p, int32_t type, int64_t
     for (int k = 0; k < N; ++k) v[k] = type == kF16 ? __half2float(__ushort_as_half(h[k])) : __uint_as_float((uint32_t)h[k] << 16);
 }
 // Weight rows m .. m + 3 of a split product (of which the matrix has some): a thread always has the same, so that their bias is fetched once, and the residual of its first
-// tokens while it waits for the other ranks.
+// token while it waits for the other ranks, of the others one ahead. (The code of what follows is there once: three times, unrolled, it took longer to fetch than the loads.)
 template <int EPI>
 struct Mx4Four {
-    static constexpr int K = 4 / (EPI ? EPI : 1), AHEAD = 3;
-    float bias[4], res[AHEAD][K];
+    static constexpr int K = 4 / (EPI ? EPI : 1);
+    float bias[4], res[K];
     __device__ __forceinline__ int64_t columns(const Mx4Params& p) const { return EPI == 2 ? p.M >> 1 : p.M; }
     __device__ __forceinline__ void residual(const Mx4Params& p, int64_t n, int64_t m, float (&v)[K]) const
     {
@@ -974,10 +974,7 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
 #pragma unroll
             for (int k = 0; k < 4; ++k) four.bias[k] = 0.f;
             if (p.e.bias && i < hi) mx4_scalars(p.e.bias, p.e.bias_type, m, p.M, four.bias);
-            if (p.e.residual)
-#pragma unroll
-                for (int k = 0; k < four.AHEAD; ++k)
-                    if (i + 192 * k < hi) four.residual(p, n0 + ((i + 192 * k) >> 5), m, four.res[k]);
+            if (p.e.residual && i < hi) four.residual(p, n0 + (i >> 5), m, four.res);
         }
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         auto sum = [&](int i, float (&v)[4]) {
@@ -993,16 +990,12 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
         };
         float v[4];
         if constexpr (EPI > 0) {
-#pragma unroll
-            for (int k = 0; k < four.AHEAD; ++k) {
-                if (i >= hi) break;
-                sum(i, v);
-                four.store(p, n0 + (i >> 5), m, v, four.res[k]);
-                i += 192;
-            }
+#pragma unroll 1
             for (; i < hi; i += 192) {
                 float r[four.K];
-                if (p.e.residual) four.residual(p, n0 + (i >> 5), m, r);
+#pragma unroll
+                for (int k = 0; k < four.K; ++k) r[k] = four.res[k];
+                if (p.e.residual && i + 192 < hi) four.residual(p, n0 + ((i + 192) >> 5), m, four.res);
                 sum(i, v);
                 four.store(p, n0 + (i >> 5), m, v, r);
             }
