@@ -116,7 +116,7 @@ us_status product(const void* X, int32_t x_type, int64_t ldx, const void* x_mx, 
         p.e.residual = e->residual; p.e.r_type = e->residual_type; p.e.ldr = N > 1 ? e->ldr : 0;
         p.e.r_vec = e->residual && rows_vec(e->residual, p.e.ldr, size_of(e->residual_type));
         p.e.act = e->act;
-const int64_t slot = 64 * ((e->gated ? 64 : 128) * size_of(e->residual_type) + 16), fit = Mx4Pair::kAhead / slot;
+        const int64_t slot = 64 * ((e->gated ? 64 : 128) * size_of(e->residual_type) + 16), fit = Mx4Pair::kAhead / slot;
         p.e.slots = fit >= 4 ? 4 : fit >= 2 ? 2 : 1;
     }
     const cudaError_t er = ops_kernel_allow(pl.kernel, (int)kWholeSm);
