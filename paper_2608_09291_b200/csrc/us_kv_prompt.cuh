@@ -11,7 +11,9 @@
 //             needs no scaling. P takes the place of S.
 // P has 11 bits, for fp16 outputs, too: a second product of what its rounding leaves (it fits beside P, in the other half of S's place) takes
 // the error against 64 bits from 2.9e-4 to 2.1e-4, and the softmax threads' time from 714 to 937 us (three prompts of up to 2000 tokens, fp16);
-// V's codes are rounded to half a 127th of their largest.
+// V's codes are rounded to half a 127th of their largest. Behind shared prefixes (kGroups, kOwn) that product is there, whatever the type: a single token's row
+// meets this kernel only because others share its prefix, and its output has to be what it is alone (64 sequences of 8 rows a cache head behind 8192 tokens, 512 of their own: 59.6 us
+// without, 60.5 with; 16 behind 4096: 26.1, 28.1; 8 of 20 new tokens and 4 rows behind 3000: 75.9, 87.7; fp16 2.8e-4 and 2.1e-4 against 64 bits).
 // m follows the true maximum only where it is 2^8 behind; p carries 2^7, see us_kv.cuh. The scores' conversions, the
 // 16384 exponentials (16 a cycle) and the two products (1024 cycles) of a tile and unit are each about 1000 cycles, and overlap.
 // Three prompts of up to 2000 tokens, to contexts of up to 4500 (64/8 heads of 128, bf16): 723 us, 696 inside a graph; one of 8192 tokens: 1250 to
@@ -145,11 +147,21 @@ __device__ __forceinline__ void pr_units(const KvPrompt& a, const PrItem& it, in
     u1 = hi > lo ? (hi + kPrTile - 1) / kPrTile : u0;
 }
 
+// Whether what p's rounding leaves is multiplied, too: behind shared prefixes.
+template <int MODE>
+constexpr bool kPrRest = MODE != kAlone;
+__device__ __forceinline__ uint32_t half2_rest(float a, float b, uint32_t rounded)
+{
+    const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&rounded));
+    return half2_bits(a - r.x, b - r.y);
+}
+
 template <int D, bool BF16, int MODE = kAlone>
 __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(const __grid_constant__ KvPrompt a)
 {
     using S = PrShape<D>;
     constexpr int HALVES = D / 64;   // 128-byte columns of fp16
+    constexpr bool REST = kPrRest<MODE>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[24];
     __shared__ float4 steps[4][8];   // of a unit's 16-token groups: K's step (-1: not there), V's, its log2 (-126 to 128), its inverse
@@ -372,6 +384,11 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                             sum = fmaf(p0 + p1, back * st[2 * c + g].w, sum);   // (p without V's step)
                         }
                         tc_st16_lanes(t_s + 16u * c, y);
+                        if constexpr (REST) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) y[i] = half2_rest(__uint_as_float(x[c][2 * i]), __uint_as_float(x[c][2 * i + 1]), y[i]);
+                            tc_st16_lanes(t_s + 64u + 16u * c, y);
+                        }
                         if (c == 1) publish(0);
                     }
                     l += sum;
@@ -379,7 +396,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                     const float away = exp2_fast(lead);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        uint32_t y[16];
+                        uint32_t y[16], z[REST ? 16 : 1];
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
                             const float2 kv = *reinterpret_cast<const float2*>(&st[2 * c + g]);
@@ -395,10 +412,14 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
                                     l += e[b];
                                 }
                                 // (a group that is not there has no step)
-                                y[8 * g + i] = (sees[c] >> (16 * g)) & 0xFFFFu ? half2_bits(e[0] == 0.f ? 0.f : e[0] * rel, e[1] == 0.f ? 0.f : e[1] * rel) : 0u;
+                                const bool there = ((sees[c] >> (16 * g)) & 0xFFFFu) != 0;
+                                const float p0 = e[0] == 0.f ? 0.f : e[0] * rel, p1 = e[1] == 0.f ? 0.f : e[1] * rel;
+                                y[8 * g + i] = there ? half2_bits(p0, p1) : 0u;
+                                if (REST) z[REST ? 8 * g + i : 0] = there ? half2_rest(p0, p1, y[8 * g + i]) : 0u;
                             }
                         }
                         tc_st16_lanes(t_s + 16u * c, y);
+                        if constexpr (REST) tc_st16_lanes(t_s + 64u + 16u * c, z);
                         if (c == 1) publish(0);
                     }
                 }
@@ -607,6 +628,9 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
             const uint32_t d = tm + 256u + 128u * i, a0 = tm + 128u * i + 32u * half;
 #pragma unroll
             for (int k = 0; k < 4; ++k) tc_mma_f16_ts(leader, d, a0 + 8u * k, b0 + 128u * k, id_o, more || half > 0 || k > 0);
+            if (REST)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) tc_mma_f16_ts(leader, d, a0 + 64u + 8u * k, b0 + 128u * k, id_o, 1);
         };
         for (int i = 0; i < nq && ok; ++i) ok = ops_wait_warp(b_q + 8u * i, 0, kMxWait, dead);
         if (ok) ok = ops_wait_warp(b_kf, 0, kMxWait, dead);
