@@ -976,6 +976,7 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
             if (p.e.bias && i < hi) mx4_scalars(p.e.bias, p.e.bias_type, m, p.M, four.bias);
             if (p.e.residual && i < hi) four.residual(p, n0 + (i >> 5), m, four.res);
         }
+        __syncwarp();   // (an aligned barrier takes whole warps: not all lanes of one had something to fetch, nor to add below)
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         auto sum = [&](int i, float (&v)[4]) {
 #pragma unroll
@@ -1005,6 +1006,7 @@ __global__ void __launch_bounds__(192, NB <= 64 ? 4 : 1) us_mx4_product_kernel(c
                 mx4_store4(p, n0 + (i >> 5), 128 * (int64_t)mt + 4 * (i & 31), v);
             }
         }
+        __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
 }
