@@ -368,7 +368,8 @@ us_status us_mx4_linear_epilogue(const void* X, int32_t x_type, int64_t ldx, int
  *     new codes = clamp(RNE(x / step'), -127, 127) (quotient exact; 0 where step' = 0)
  *   Infinities and NaN do not count in max|new|; they are stored as +-127 (0 where step' = 0) and 0. K, V: us_type rows (token, head) of
  *   head_dim elements, strides in elements. A block that gets tokens must belong to one sequence only. Places behind the
- *   sequence's end keep what they hold.
+ *   sequence's end keep what they hold. us_kv_append_granted: a sequence with more new tokens than granted[s] (device, n_seqs int32, or NULL) is left out: what
+ *   us_kv_extend_granted wrote there keeps sequences that it had no room for, and the blocks that they share, as they are.
  * us_kv_read: the values of the first `tokens` places of every sequence, [n_seqs][tokens][n_kv_heads][head_dim] of us_type; zero
  *   from a sequence's end on. cu_tokens is not read.
  * us_kv_attention: for each new token and query head (n_heads, a multiple of n_kv_heads: head h reads cache head
@@ -396,6 +397,9 @@ us_status us_kv_create(void* k_codes, void* v_codes, void* k_steps, void* v_step
                        int32_t block_tokens, int32_t head_dim, us_kv** out);
 us_status us_kv_append(us_kv* h, const us_kv_seqs* seqs, int64_t N, const void* K, const void* V, int32_t type,
                        int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, void* stream);
+us_status us_kv_append_granted(us_kv* h, const us_kv_seqs* seqs, int64_t N, const void* K, const void* V, int32_t type,
+                               int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                               const int32_t* granted, void* stream);
 us_status us_kv_read(us_kv* h, const us_kv_seqs* seqs, int64_t tokens, void* K, void* V, int32_t type, void* stream);
 int64_t us_kv_attention_scratch(const us_kv* h, const us_kv_seqs* seqs, int64_t N, int32_t n_heads);
 us_status us_kv_attention(us_kv* h, const us_kv_seqs* seqs, int64_t N, const void* Q, int32_t type, int32_t n_heads,
@@ -432,6 +436,8 @@ us_status us_kv_destroy(us_kv* h);
  *   tokens held and the steps; the first free block of the sequence's share): new tokens may be appended. Where the sequences of the call are the only ones that hold it, the first of
  *   them keeps it. If the free blocks do not suffice (US_ERR_OUT_OF_BLOCKS), the first sequence that does not fit and all behind it that need blocks stay as they are; so does
  *   one that would keep a block which one of those holds, and a sequence with an entry or length that does not fit. scratch: us_kv_extend_scratch bytes, 16-byte aligned, for one call at a time; need not be cleared.
+ *   us_kv_extend_granted writes, too, by how many tokens each sequence has grown: granted[s] (device, n_seqs int32, or NULL) is tokens[s], or 0 where it stays as it is. Such a
+ *   sequence's last tokens are old ones, maybe in blocks of others: us_kv_append_granted leaves it out.
  * us_kv_compact: the blocks in use become the pool's first `used` (device int32) ones: those behind move to the free places in front, both in order. The entries of the
  *   n_tables tables (tables: host array; block_table is written, cu_tokens not read) follow them. map[b] (device, n_blocks int32) is where block b's tokens are now (b itself where it did
  *   not move): us_kv_remap takes a further table there. Every table that is in use has to follow. scratch: us_kv_compact_scratch bytes.
@@ -444,6 +450,8 @@ us_status us_kv_release(us_kv* h, int32_t* refs, const us_kv_seqs* seqs, void* s
 int64_t us_kv_extend_scratch(const us_kv* h, int32_t n_seqs);
 us_status us_kv_extend(us_kv* h, int32_t* refs, int32_t* table, int64_t table_stride, int32_t table_width, int32_t* lengths, int32_t n_seqs,
                        const int32_t* tokens, int32_t tokens_each, void* scratch, int64_t scratch_bytes, void* stream);
+us_status us_kv_extend_granted(us_kv* h, int32_t* refs, int32_t* table, int64_t table_stride, int32_t table_width, int32_t* lengths, int32_t n_seqs,
+                               const int32_t* tokens, int32_t tokens_each, int32_t* granted, void* scratch, int64_t scratch_bytes, void* stream);
 int64_t us_kv_compact_scratch(const us_kv* h);
 us_status us_kv_compact(us_kv* h, int32_t* refs, const us_kv_seqs* tables, int32_t n_tables, int32_t* map, int32_t* used, void* scratch,
                         int64_t scratch_bytes, void* stream);

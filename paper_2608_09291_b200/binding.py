@@ -31,9 +31,9 @@ EXPORTS = ["us_encode", "us_get_stats", "us_decode", "us_get_row_order", "us_spm
            "us_last_error", "us_debug_withhold_copy", "us_stage_timers", "us_destroy", "us_spmm_bytes", "us_launch_info", "us_launch_kernel",
            "us_mx4_bytes", "us_mx4_quantize", "us_mx4_dequantize", "us_mx4_pack", "us_mx4_unpack", "us_mx4_matmul",
            "us_mx4_linear_scratch", "us_mx4_linear", "us_mx4_matmul_epilogue", "us_mx4_linear_epilogue", "us_mx4_last_error",
-           "us_kv_create", "us_kv_append", "us_kv_read", "us_kv_attention_scratch", "us_kv_attention", "us_kv_shared_attention_scratch",
+           "us_kv_create", "us_kv_append", "us_kv_append_granted", "us_kv_read", "us_kv_attention_scratch", "us_kv_attention", "us_kv_shared_attention_scratch",
            "us_kv_shared_attention", "us_kv_last_error", "us_kv_destroy",
-           "us_kv_fork", "us_kv_release", "us_kv_extend_scratch", "us_kv_extend", "us_kv_compact_scratch", "us_kv_compact", "us_kv_remap", "us_kv_copy_blocks",
+           "us_kv_fork", "us_kv_release", "us_kv_extend_scratch", "us_kv_extend", "us_kv_extend_granted", "us_kv_compact_scratch", "us_kv_compact", "us_kv_remap", "us_kv_copy_blocks",
            "us_qk_norm_rope",
            "us_status_string"]
 
@@ -101,6 +101,7 @@ class us_kv_seqs(ctypes.Structure):
 _seqs = ctypes.POINTER(us_kv_seqs)
 _lib.us_kv_create.argtypes = [_vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, ctypes.POINTER(_vp)]
 _lib.us_kv_append.argtypes = [_vp, _seqs, _i64, _vp, _vp, _i32, _i64, _i64, _i64, _i64, _vp]
+_lib.us_kv_append_granted.argtypes = [_vp, _seqs, _i64, _vp, _vp, _i32, _i64, _i64, _i64, _i64, _vp, _vp]
 _lib.us_kv_read.argtypes = [_vp, _seqs, _i64, _vp, _vp, _i32, _vp]
 _lib.us_kv_attention_scratch.argtypes = [_vp, _seqs, _i64, _i32]
 _lib.us_kv_attention_scratch.restype = _i64
@@ -115,6 +116,7 @@ _lib.us_kv_release.argtypes = [_vp, _vp, _seqs, _vp]
 _lib.us_kv_extend_scratch.argtypes = [_vp, _i32]
 _lib.us_kv_extend_scratch.restype = _i64
 _lib.us_kv_extend.argtypes = [_vp, _vp, _vp, _i64, _i32, _vp, _i32, _vp, _i32, _vp, _i64, _vp]
+_lib.us_kv_extend_granted.argtypes = [_vp, _vp, _vp, _i64, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _i64, _vp]
 _lib.us_kv_compact_scratch.argtypes = [_vp]
 _lib.us_kv_compact_scratch.restype = _i64
 _lib.us_kv_compact.argtypes = [_vp, _vp, _seqs, _i32, _vp, _vp, _vp, _i64, _vp]
@@ -569,10 +571,11 @@ class KVCache:
         steps = [torch.zeros((n_blocks, n_kv_heads), dtype=torch.float32, device=device) for _ in range(2)]
         return cls(*codes, *steps)
 
-    def append(self, k, v, block_table, lengths, cu_tokens=None, stream=None):
+    def append(self, k, v, block_table, lengths, cu_tokens=None, stream=None, granted=None):
         """Writes new tokens, the last ones of their sequences: k, v (N, n_kv_heads, head_dim) float16, bfloat16 or float32 (any token and
-        head strides). Finite values are expected; others do not count for a step."""
-        _ext.kv_append(self.handle, self.k_codes, k, v, block_table, lengths, cu_tokens, stream)
+        head strides). Finite values are expected; others do not count for a step. granted: what `KVPages.extend` wrote there: sequences that it had no room
+        for are left out."""
+        _ext.kv_append(self.handle, self.k_codes, k, v, block_table, lengths, cu_tokens, stream, granted)
 
     def read(self, block_table, lengths, tokens: int, dtype=None, stream=None):
         """(K, V): values of the first `tokens` places of each sequence, (S, tokens, n_kv_heads, head_dim), float32 unless another type is
@@ -627,7 +630,9 @@ class KVPages:
     block that nobody holds is free. Calls that need free blocks take the lowest ones, sequence by sequence. Nothing waits for the host, and every call can
     be captured into a graph; calls on one KVPages follow one another on the device.
 
-    A batch starts with a table of zeros and lengths of 0; `extend` makes room for new tokens, `KVCache.append` then writes them."""
+    A batch starts with a table of zeros and lengths of 0; `extend` makes room for new tokens, `KVCache.append` then writes them. Both take `granted` (int32 (S,)):
+    `extend` leaves there by how many tokens each sequence has grown, and `append` passes over those that the pool had no room for. Without it the last
+    tokens of such a sequence, which are old ones and may lie in blocks of others, would be written over."""
 
     def __init__(self, cache: KVCache, refs=None):
         import torch
@@ -637,10 +642,11 @@ class KVPages:
             raise ValueError("refs must be a contiguous int32 (n_blocks,) tensor on the cache's device, 16-byte aligned")
         self.cache, self.refs = cache, refs
 
-    def extend(self, block_table, lengths, tokens=1, stream=None):
+    def extend(self, block_table, lengths, tokens=1, stream=None, granted=None):
         """Room for `tokens` (a number, or int32 (S,)) more tokens of each sequence: block_table and lengths are written. A last block that would be written into
-        and that others hold, too, is replaced by a copy. Sequences for which the pool has no blocks left stay as they are (see `check`)."""
-        _ext.kv_extend(self.cache.handle, self.cache.k_codes, self.refs, block_table, lengths, tokens, stream)
+        and that others hold, too, is replaced by a copy. Sequences for which the pool has no blocks left stay as they are (see `check`). granted, an int32 (S,)
+        tensor, gets how many tokens each has grown by: tokens - granted are still to come once blocks are free."""
+        _ext.kv_extend(self.cache.handle, self.cache.k_codes, self.refs, block_table, lengths, tokens, stream, granted)
 
     def fork(self, block_table, lengths, parents, keep=False, stream=None):
         """(block_table, lengths) of a new batch: row i continues sequence parents[i] (int32; -1: an empty one) and shares its blocks. The old batch is given up

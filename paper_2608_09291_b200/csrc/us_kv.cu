@@ -121,7 +121,13 @@ us_status us_kv_destroy(us_kv* h)
 us_status us_kv_append(us_kv* h, const us_kv_seqs* q, int64_t N, const void* K, const void* V, int32_t type, int64_t k_token_stride, int64_t k_head_stride,
                        int64_t v_token_stride, int64_t v_head_stride, void* stream)
 {
-    if (!seqs_ok(h, q, N) || type < 0 || type > 2) return US_ERR_INVALID_ARG;
+    return us_kv_append_granted(h, q, N, K, V, type, k_token_stride, k_head_stride, v_token_stride, v_head_stride, nullptr, stream);
+}
+
+us_status us_kv_append_granted(us_kv* h, const us_kv_seqs* q, int64_t N, const void* K, const void* V, int32_t type, int64_t k_token_stride, int64_t k_head_stride,
+                               int64_t v_token_stride, int64_t v_head_stride, const int32_t* granted, void* stream)
+{
+    if (!seqs_ok(h, q, N) || type < 0 || type > 2 || !aligned(granted, 4)) return US_ERR_INVALID_ARG;
     if (N == 0 || q->n_seqs == 0) return US_OK;
     if (!strides_ok(K, type, k_token_stride, k_head_stride, N, h->pool.Hkv, h->pool.D) ||
         !strides_ok(V, type, v_token_stride, v_head_stride, N, h->pool.Hkv, h->pool.D)) return US_ERR_INVALID_ARG;
@@ -133,6 +139,7 @@ us_status us_kv_append(us_kv* h, const us_kv_seqs* q, int64_t N, const void* K, 
     a.x[0] = K; a.x[1] = V;
     a.token_stride[0] = k_token_stride; a.token_stride[1] = v_token_stride;
     a.head_stride[0] = k_head_stride; a.head_stride[1] = v_head_stride;
+    a.granted = granted;
     a.vec = rows_vec(K, type, k_token_stride, k_head_stride) && rows_vec(V, type, v_token_stride, v_head_stride);
     s = error_word(&a.pool.err);
     if (s != US_OK) return s;

@@ -117,6 +117,7 @@ struct KvAppend {
     KvSeqs seqs;
     const void* x[2];              // K, V: new tokens
     int64_t token_stride[2], head_stride[2];
+    const int32_t* granted;        // (or nullptr) tokens that each sequence has room for: one that has more new ones is left out
     int32_t vec;                   // rows take 16-byte loads
     int32_t log2_T;
 };
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(128) us_kv_append_kernel(const __grid_constant
             bool wrong;
             mine = kv_seq(a.seqs, p, base + lane, wrong);
             any_wrong |= wrong;
-            if (mine.n > 0 && mine.n <= mine.len && !wrong) cnt = ((mine.len - 1) >> a.log2_T) - ((mine.len - mine.n) >> a.log2_T) + 1;
+            if (mine.n > 0 && mine.n <= mine.len && !wrong && (!a.granted || __ldcg(a.granted + base + lane) >= mine.n)) cnt = ((mine.len - 1) >> a.log2_T) - ((mine.len - mine.n) >> a.log2_T) + 1;
         }
         uint32_t sum = cnt;
 #pragma unroll

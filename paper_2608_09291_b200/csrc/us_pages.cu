@@ -115,6 +115,7 @@ struct Extend {
     int32_t each;
     int32_t *count, *first, *list;          // of blocks
     int32_t *need, *at, *src, *dst, *held;  // of sequences; need: blocks behind the last, + 2^30 for a copy; -1: left as it is
+    int32_t* granted;                       // (or nullptr) by how many tokens each has grown
 };
 constexpr int32_t kCopy = 1 << 30;
 __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
@@ -209,7 +210,7 @@ __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
     for (int base = threadIdx.x & ~31; base < e.S; base += 1024) {
         const int s = base + lane;
         const int32_t what = s < e.S ? need_of[s] : -1;
-        int32_t dst = -1, held = 0, have = 0, n = 0;
+        int32_t dst = -1, held = 0, have = 0, n = 0, more = 0;
         uint32_t from = 0;
         bool fits = what >= 0;
         if (fits) {
@@ -219,7 +220,8 @@ __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
                 atomicExch(a.pool.err, kErrFull);
                 fits = false;
             } else {
-                const int32_t len = e.lengths[s], more = e.tokens ? __ldcg(e.tokens + s) : e.each;
+                const int32_t len = e.lengths[s];
+                more = e.tokens ? __ldcg(e.tokens + s) : e.each;
                 have = blocks_of(len, a.log2_T);
                 if (copy) {
                     dst = e.list[at];
@@ -237,6 +239,7 @@ __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
             e.src[s] = last_of[s];
             e.dst[s] = dst;
             e.held[s] = held;
+            if (e.granted) e.granted[s] = more;
         }
         const uint32_t many = __ballot_sync(0xffffffffu, n > 4);
         if (n <= 4)
@@ -454,13 +457,19 @@ int64_t us_kv_extend_scratch(const us_kv* h, int32_t n_seqs)
 us_status us_kv_extend(us_kv* h, int32_t* refs, int32_t* table, int64_t table_stride, int32_t table_width, int32_t* lengths, int32_t n_seqs,
                        const int32_t* tokens, int32_t tokens_each, void* scratch, int64_t scratch_bytes, void* stream)
 {
+    return us_kv_extend_granted(h, refs, table, table_stride, table_width, lengths, n_seqs, tokens, tokens_each, nullptr, scratch, scratch_bytes, stream);
+}
+
+us_status us_kv_extend_granted(us_kv* h, int32_t* refs, int32_t* table, int64_t table_stride, int32_t table_width, int32_t* lengths, int32_t n_seqs,
+                               const int32_t* tokens, int32_t tokens_each, int32_t* granted, void* scratch, int64_t scratch_bytes, void* stream)
+{
     us_kv_seqs q = {};
     q.block_table = table;
     q.table_stride = table_stride;
     q.lengths = lengths;
     q.n_seqs = n_seqs;
     q.table_width = table_width;
-    if (!kv_seqs_ok(h, &q, n_seqs) || (tokens ? !kv_aligned(tokens, 4) : tokens_each < 0) || !refs_ok(refs)) return US_ERR_INVALID_ARG;
+    if (!kv_seqs_ok(h, &q, n_seqs) || (tokens ? !kv_aligned(tokens, 4) : tokens_each < 0) || !kv_aligned(granted, 4) || !refs_ok(refs)) return US_ERR_INVALID_ARG;
     if (n_seqs == 0) return US_OK;
     if (!scratch || !kv_aligned(scratch, 16) || scratch_bytes < us_kv_extend_scratch(h, n_seqs)) return US_ERR_SCRATCH_TOO_SMALL;
     Pages a;
@@ -482,6 +491,7 @@ us_status us_kv_extend(us_kv* h, int32_t* refs, int32_t* table, int64_t table_st
     e.src = e.at + n_seqs;
     e.dst = e.src + n_seqs;
     e.held = e.dst + n_seqs;
+    e.granted = granted;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     void* args[] = {&a, &e};
     const us_status k = kv_cuda(ops_launch((const void*)us_kv_extend_kernel, dim3(1), 1024, 0, st, args));

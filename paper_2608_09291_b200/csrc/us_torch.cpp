@@ -466,10 +466,25 @@ bool is_heads(const at::Tensor& t, int64_t D, const at::Tensor& on)
 int64_t token_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : 0; }
 int64_t head_stride(const at::Tensor& t) { return t.size(1) > 1 ? t.stride(1) : 0; }
 
-// kv_append(handle, pool, k, v, table, lengths, cu, stream)
+// The (S,) tensor of tokens that sequences have room for; nullptr for None.
+bool take_granted(PyObject* o, int64_t S, const at::Tensor& on, int32_t** p)
+{
+    *p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t = tensor(o, "granted");
+    if (!t) return false;
+    if (t->dim() != 1 || !is_ints(*t, on) || t->size(0) != S || !t->is_contiguous()) {
+        PyErr_SetString(PyExc_ValueError, "granted must be a contiguous int32 tensor with an entry for each sequence, on the cache's device");
+        return false;
+    }
+    *p = static_cast<int32_t*>(t->data_ptr());
+    return true;
+}
+
+// kv_append(handle, pool, k, v, table, lengths, cu, stream, granted)
 PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    if (n != 8) return PyErr_Format(PyExc_TypeError, "kv_append takes 8 arguments");
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "kv_append takes 9 arguments");
     HANDLE_TH_ERRORS
     void* h = a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]);
     if (PyErr_Occurred()) return nullptr;
@@ -482,11 +497,12 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n)
         k->size(0) != v->size(0) || k->scalar_type() != v->scalar_type())
         return bad("k and v must be (N, n_kv_heads, head_dim) tensors of one type (float16, bfloat16 or float32) with unit last stride on the cache's device");
     us_kv_seqs q;
-    if (!take_seqs(a[4], a[5], a[6], k->size(0), *pool, &q)) return nullptr;
+    int32_t* granted;
+    if (!take_seqs(a[4], a[5], a[6], k->size(0), *pool, &q) || !take_granted(a[8], q.n_seqs, *pool, &granted)) return nullptr;
     us_status s;
     Py_BEGIN_ALLOW_THREADS
-    s = us_kv_append(static_cast<us_kv*>(h), &q, k->size(0), k->data_ptr(), v->data_ptr(), type_of(k->scalar_type()), token_stride(*k), head_stride(*k),
-                     token_stride(*v), head_stride(*v), at_.stream);
+    s = us_kv_append_granted(static_cast<us_kv*>(h), &q, k->size(0), k->data_ptr(), v->data_ptr(), type_of(k->scalar_type()), token_stride(*k), head_stride(*k),
+                             token_stride(*v), head_stride(*v), granted, at_.stream);
     Py_END_ALLOW_THREADS
     if (s != US_OK) return fail(s, "us_kv_append");
     Py_RETURN_NONE;
@@ -692,10 +708,10 @@ PyObject* kv_release(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// kv_extend(handle, pool, refs, table, lengths, tokens, stream); tokens: a number, or one for each sequence
+// kv_extend(handle, pool, refs, table, lengths, tokens, stream, granted); tokens: a number, or one for each sequence
 PyObject* kv_extend(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    if (n != 7) return PyErr_Format(PyExc_TypeError, "kv_extend takes 7 arguments");
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "kv_extend takes 8 arguments");
     HANDLE_TH_ERRORS
     void* h = a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]);
     if (PyErr_Occurred()) return nullptr;
@@ -718,13 +734,15 @@ PyObject* kv_extend(PyObject*, PyObject* const* a, Py_ssize_t n)
         if (PyErr_Occurred()) return nullptr;
         if (each < 0 || each > 0x7FFFFFFF) return bad("tokens must be 0 or more");
     }
+    int32_t* granted;
+    if (!take_granted(a[7], q.n_seqs, *pool, &granted)) return nullptr;
     at::Tensor scratch;
     const int64_t bytes = us_kv_extend_scratch(static_cast<us_kv*>(h), q.n_seqs);
     if (q.n_seqs > 0) scratch = at::detail::empty_cuda({bytes}, at::kByte, pool->device(), std::nullopt);
     us_status s;
     Py_BEGIN_ALLOW_THREADS
-    s = us_kv_extend(static_cast<us_kv*>(h), refs, const_cast<int32_t*>(q.block_table), q.table_stride, q.table_width, const_cast<int32_t*>(q.lengths), q.n_seqs, tokens,
-                     (int32_t)each, q.n_seqs > 0 ? scratch.data_ptr() : nullptr, bytes, at_.stream);
+    s = us_kv_extend_granted(static_cast<us_kv*>(h), refs, const_cast<int32_t*>(q.block_table), q.table_stride, q.table_width, const_cast<int32_t*>(q.lengths), q.n_seqs, tokens,
+                             (int32_t)each, granted, q.n_seqs > 0 ? scratch.data_ptr() : nullptr, bytes, at_.stream);
     Py_END_ALLOW_THREADS
     if (s != US_OK) return fail(s, "us_kv_extend");
     Py_RETURN_NONE;
