@@ -431,6 +431,8 @@ us_status us_kv_destroy(us_kv* h);
  *   empty one); 0 behind its blocks. The children's entries are counted and, with keep = 0, the parents' no more (their table is not to be used from then on). The
  *   new table and lengths do not overlap the old ones. A parent out of range gives an empty sequence.
  * us_kv_release: the sequences' entries are counted no more. Table and lengths are left as they are.
+ *   An entry whose block nobody holds is an error in all three (US_ERR_DEVICE_INDEX): fork's children have it all the same, release leaves its count at 0, extend leaves a sequence
+ *   that would write into it as it is.
  * us_kv_extend: room for tokens[s] more (device int32, or NULL: tokens_each for all) tokens of each sequence: free blocks, the lowest first, sequence by
  *   sequence, go to the table, and lengths[s] grows. Before that, a last block that is partly filled and that other entries hold, too, is replaced by a copy (of the
  *   tokens held and the steps; the first free block of the sequence's share): new tokens may be appended. Where the sequences of the call are the only ones that hold it, the first of

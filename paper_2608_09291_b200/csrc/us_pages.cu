@@ -25,8 +25,17 @@ __device__ __forceinline__ void give_up(const Pages& a, int32_t b)
 }
 
 // Children's rows (blockIdx.y; a thread an entry, kEntries a block): the parent's blocks, each held once more; then, unless they are kept, the parents' rows, whose
-// blocks are held once less. Bound by three trips to memory, one behind the other: 2.3 us inside a graph.
+// blocks are held once less. Where they are given up, a parent's first child takes its entries over, and only a parent without one gives them up: so an entry's own count is there
+// whenever it is looked at, in whatever order the rows are done, and a count of 0 says that nobody holds the block. Bound by four trips to memory, one
+// behind the other (the last is the counts' answers): 8 children of one parent 2.2 us inside a graph, 256 of 16 3.6.
 constexpr int kEntries = 128;
+// Whether s is among the first n parents (all threads of a block).
+__device__ __forceinline__ bool among(const int32_t* parents, int64_t n, int64_t s)
+{
+    bool is = false;
+    for (int64_t i = threadIdx.x; i < n && !is; i += kEntries) is = __ldcg(parents + i) == s;
+    return __syncthreads_or(is) != 0;
+}
 __global__ void __launch_bounds__(kEntries) us_kv_fork_kernel(Pages a, KvSeqs q, const int32_t* parents, int children, int32_t* table, int64_t stride, int32_t* lengths,
                                                               int give)
 {
@@ -44,13 +53,16 @@ __global__ void __launch_bounds__(kEntries) us_kv_fork_kernel(Pages a, KvSeqs q,
             len = 0;
         }
         const int n = blocks_of(len, a.log2_T);
+        const int32_t entry = j < n ? __ldcg(q.table + s * q.table_stride + j) : 0;   // (on its way meanwhile)
+        const bool other = give && among(parents, child ? w : children, s);           // another child takes the parent's entries over
         if (j < (child ? q.width : n)) {
-            int32_t b = 0;
+            const int32_t b = entry;
             if (j < n) {
-                b = __ldcg(q.table + s * q.table_stride + j);
                 if (!in_pool(a, b)) bad = true;
-                else if (child) atomicAdd(a.refs + b, 1);
-                else give_up(a, b);
+                else if (!child) {
+                    if (!other) give_up(a, b);
+                } else if (give && !other) bad |= __ldcg(a.refs + b) <= 0;
+                else bad |= atomicAdd(a.refs + b, 1) <= 0;
             }
             if (child) table[w * stride + j] = b;
         }
@@ -143,10 +155,11 @@ __global__ void __launch_bounds__(1024) us_kv_extend_kernel(Pages a, Extend e)
             need = blocks_of(len + n, a.log2_T) - have;
             if (len & ((1 << a.log2_T) - 1)) {
                 const int32_t b = __ldcg(e.table + s * e.stride + have - 1);
-                if (!in_pool(a, b)) {
+                const int32_t held = in_pool(a, b) ? __ldcg(a.refs + b) : 0;
+                if (held <= 0) {
                     wrong(a);
                     need = -1;
-                } else if (__ldcg(a.refs + b) > 1) {
+                } else if (held > 1) {
                     last = b;
                     e.count[b] = 0;
                     e.first[b] = 0x7FFFFFFF;
@@ -385,6 +398,9 @@ __global__ void __launch_bounds__(kEntries) us_kv_remap_kernel(Pages a, const in
     for (int64_t s = blockIdx.y; s < q.S; s += gridDim.y) remap(a, map, q, s, j);
 }
 
+// Children that every row looks through; more: a launch for them, and one that gives the parents up. (As many parents as children, tables of 16 blocks: 1024 5.2 us and 6.5 in two
+// launches, 2048 10.3 and 9.1, 4096 25.1 and 14.6.)
+constexpr int kLooked = 1024;
 dim3 entries(int64_t rows, int64_t width) { return dim3((unsigned)std::max<int64_t>(1, (width + kEntries - 1) / kEntries), (unsigned)std::min<int64_t>(rows, 65535)); }
 
 bool refs_ok(const int32_t* refs) { return refs && kv_aligned(refs, 16); }
@@ -439,6 +455,10 @@ us_status us_kv_fork(us_kv* h, int32_t* refs, const us_kv_seqs* q, const int32_t
     int32_t give = keep == 0;
     const int64_t rows = (int64_t)n_children + (give ? q->n_seqs : 0);
     if (rows == 0) return US_OK;
+    if (give && n_children > kLooked) {
+        const us_status k = us_kv_fork(h, refs, q, parents, n_children, table, table_stride, lengths, 1, stream);
+        return k != US_OK ? k : us_kv_release(h, refs, q, stream);
+    }
     KvSeqs k = kv_seqs(&one, 0);
     void* args[] = {&a, &k, &parents, &n_children, &table, &table_stride, &lengths, &give};
     return kv_cuda(ops_launch((const void*)us_kv_fork_kernel, entries(rows, q->table_width), kEntries, 0, static_cast<cudaStream_t>(stream), args));
