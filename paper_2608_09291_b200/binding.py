@@ -596,8 +596,8 @@ class KVCache:
                          stream=None):
         """Attention of sequences behind prefixes that groups of them share: a prefix's keys and values are read once for its group. prefix_table (groups, width)
         and prefix_lengths (groups,) describe the prefixes, cu_seqs int32 (groups + 1,) says whose sequences are whose: [cu_seqs[g], cu_seqs[g + 1]). block_table, lengths
-        and cu_tokens are of the sequences' own tokens, the new ones included; the rest is as for `attention`, and what the softmax's weights have beyond 11 bits is
-        multiplied for both types and any number of rows.
+        and cu_tokens are of the sequences' own tokens, the new ones included; the rest is as for `attention`, but that what the softmax's weights have
+        beyond 11 bits is multiplied for float16 and any number of rows.
 
         After `KVPages.fork` of a prompt of p whole blocks: prefix_table = table[:1, :p], block_table = table[:, p:], lengths - p * block_tokens."""
         return _ext.kv_shared_attention(self.handle, self.k_codes, q, block_table, lengths, cu_tokens, self.head_dim ** -0.5 if scale is None else scale,

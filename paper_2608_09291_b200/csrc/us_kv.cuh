@@ -541,8 +541,8 @@ __device__ __forceinline__ void kv_add_part(float& big, float& sum, float& acc, 
 
 // 32 tokens of a warp, from tok0 on: scores, softmax and sums of 8 NT rows (see below). load_k gives a lane 16 bytes of each of tokens g and g + 8 of group b (D / 64 such
 // pieces), load_v the lane's D / 8 columns of token 2 t, 2 t + 1, 2 t + 8 or 2 t + 9 (q). edge: some row does not see all of them; a group that is not there has
-// a step of -1. REST: what the rounding of p leaves is multiplied, too.
-template <int D, int NT, bool REST, class LoadK, class LoadV>
+// a step of -1.
+template <int D, int NT, bool BF16, class LoadK, class LoadV>
 __device__ __forceinline__ void kv_step(LoadK load_k, LoadV load_v, const uint32_t (&qf)[NT][D / 16][2], const float (&f)[NT][2], const int (&lo)[NT][2], const int (&hi)[NT][2],
                                         const float (&stk)[2], const float (&stv)[2], bool edge, int tok0, int g, float (&m)[NT][2], float (&r)[NT][2], float (&l)[NT][2],
                                         float (&o)[D / 16][NT][4])
@@ -637,6 +637,10 @@ __device__ __forceinline__ void kv_step(LoadK load_k, LoadV load_v, const uint32
             }
         exponents();
     }
+    // (fp16 output: what the rounding of p leaves is multiplied, too; else its 2^-12 would be as much as the output's own: an error
+    // of 2.9e-4 against 64 bits, 2.1e-4 with it. 64 sequences of up to 8192 tokens, 16 rows a cache head: 171 us without, 182 with.
+    // bf16's own rounding is eight times as large: 1.7e-3 either way)
+    constexpr bool REST = !BF16;
     uint32_t pf[2][NT][2], pr[2][NT][2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -766,13 +770,6 @@ struct KvShape {
     static constexpr int kMaxStages = 8;
     static constexpr int kPart = R * (D + 2);                 // floats of a part
 };
-
-// Whether what the rounding of p to 11 bits leaves is multiplied, too. fp16 output: else its 2^-12 would be as much as the output's own: an error of 2.9e-4 against 64
-// bits, 2.1e-4 with it (64 sequences of up to 8192 tokens, 16 rows a cache head: 171 us without, 182 with). bf16's own rounding is eight times as large: 1.7e-3 either
-// way. Behind shared prefixes it always is: there the output is the sums' one rounding in either type (without it 1 of 10 bf16 values is a neighbour of that, with it 1 of 1400;
-// 4 sequences behind 1000 tokens, 256 of their own, 4 rows a cache head: 23.4 and 24.4 us).
-template <bool BF16, int MODE>
-constexpr bool kKvRest = !BF16 || MODE != kAlone;
 
 template <int D, int NT, bool BF16, int MODE = kAlone>
 __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_constant__ KvAttend a)
@@ -919,7 +916,7 @@ __global__ void __launch_bounds__(160, 2) us_kv_attend_kernel(const __grid_const
                 if (tok0 + 32 > it.lo && tok0 < last_hi && !(st0.x < 0.f && st1.x < 0.f)) {
                     const bool edge = tok0 < all_lo || tok0 + 32 > all_hi || st0.x < 0.f || st1.x < 0.f;
                     const uint32_t kb = smem_u32(ring + (size_t)stage * S::kStage), vb = kb + S::kHalf;
-                    kv_step<D, NT, kKvRest<BF16, MODE>>(
+                    kv_step<D, NT, BF16>(
                         [&](int b, int c, uint4& x, uint4& y) {
                             const int kr = 32 * warp + 16 * b + g, chunk = D == 128 ? ((2 * t + c) ^ (kr & 7)) : (t ^ ((kr >> 1) & 3));
                             x = lds128(kb + (uint32_t)(kr * D + 16 * chunk));
@@ -1450,7 +1447,7 @@ __global__ void __launch_bounds__(32, 12) us_kv_short_kernel(const __grid_consta
             }
             const int next = tok0 + 32;
             if (next < end && (next & 511) == 0) look(next);
-            kv_step<D, 1, kKvRest<BF16, kOwn>>(
+            kv_step<D, 1, BF16>(
                 [&](int b, int c, uint4& x, uint4& y) {
                     x = kx[b][c][0];
                     y = kx[b][c][1];

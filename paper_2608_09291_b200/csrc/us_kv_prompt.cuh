@@ -11,9 +11,10 @@
 //             needs no scaling. P takes the place of S.
 // P has 11 bits, for fp16 outputs, too: a second product of what its rounding leaves (it fits beside P, in the other half of S's place) takes
 // the error against 64 bits from 2.9e-4 to 2.1e-4, and the softmax threads' time from 714 to 937 us (three prompts of up to 2000 tokens, fp16);
-// V's codes are rounded to half a 127th of their largest. Behind shared prefixes (kGroups, kOwn) that product is there, whatever the type: a single token's row
-// meets this kernel only because others share its prefix, and its output has to be what it is alone (64 sequences of 8 rows a cache head behind 8192 tokens, 512 of their own: 59.6 us
-// without, 60.5 with; 16 behind 4096: 26.1, 28.1; 8 of 20 new tokens and 4 rows behind 3000: 75.9, 87.7; fp16 2.8e-4 and 2.1e-4 against 64 bits).
+// V's codes are rounded to half a 127th of their largest. Behind shared prefixes (kGroups, kOwn) fp16 has that product: a single token's row
+// meets this kernel only because others share its prefix, and is to be as exact as alone (64 sequences of 8 rows a cache head behind 8192 tokens, 512 of their own: 59.9 us
+// without, 60.5 with; 16 behind 4096: 25.8, 28.2; 8 of 20 new tokens and 4 rows behind 3000: 75.9, 87.7; 2.8e-4 and 2.1e-4 against 64 bits). bf16 goes without: its own rounding is eight
+// times as large (1.67e-3 and 1.66e-3; 64 sequences behind 8192 tokens, up to 512 of their own: 48.2 us, 57.4 with it).
 // m follows the true maximum only where it is 2^8 behind; p carries 2^7, see us_kv.cuh. The scores' conversions, the
 // 16384 exponentials (16 a cycle) and the two products (1024 cycles) of a tile and unit are each about 1000 cycles, and overlap.
 // Three prompts of up to 2000 tokens, to contexts of up to 4500 (64/8 heads of 128, bf16): 723 us, 696 inside a graph; one of 8192 tokens: 1250 to
@@ -147,9 +148,9 @@ __device__ __forceinline__ void pr_units(const KvPrompt& a, const PrItem& it, in
     u1 = hi > lo ? (hi + kPrTile - 1) / kPrTile : u0;
 }
 
-// Whether what p's rounding leaves is multiplied, too: behind shared prefixes.
-template <int MODE>
-constexpr bool kPrRest = MODE != kAlone;
+// Whether what p's rounding leaves is multiplied, too.
+template <bool BF16, int MODE>
+constexpr bool kPrRest = MODE != kAlone && !BF16;
 __device__ __forceinline__ uint32_t half2_rest(float a, float b, uint32_t rounded)
 {
     const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&rounded));
@@ -161,7 +162,7 @@ __global__ void __launch_bounds__(PrShape<D>::kThreads, 1) us_kv_prompt_kernel(c
 {
     using S = PrShape<D>;
     constexpr int HALVES = D / 64;   // 128-byte columns of fp16
-    constexpr bool REST = kPrRest<MODE>;
+    constexpr bool REST = kPrRest<BF16, MODE>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[24];
     __shared__ float4 steps[4][8];   // of a unit's 16-token groups: K's step (-1: not there), V's, its log2 (-126 to 128), its inverse
