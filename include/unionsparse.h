@@ -411,6 +411,7 @@ us_status us_kv_attention(us_kv* h, const us_kv_seqs* seqs, int64_t N, const voi
  *   in no group have no prefix; n_seqs = 0: none have. A token of a sequence sees its group's whole prefix and, of its sequence's own tokens (seqs: lengths and
  *   table are of those; new tokens included), what it sees above. A sequence of length 0 may have rows: they give 0. No windows. If cu entries fall or pass the
  *   number of sequences (US_ERR_DEVICE_INDEX), the outputs of the call may be anything. scratch: us_kv_shared_attention_scratch bytes.
+ *   table_width says which kernels run: own contexts in tables of up to 512 tokens (1024 where there are more than 32 sequences) are read beside the prefixes, wider ones behind.
  *   Accuracy: as for calls of few rows, whatever their number, where n_seqs > 0 for prefixes: the output's own rounding is all that shows (US_F16 2.1e-4, US_BF16 1.7e-3 of the
  *   output's norm).
  */

@@ -599,7 +599,8 @@ class KVCache:
         and cu_tokens are of the sequences' own tokens, the new ones included; the rest is as for `attention`, but that what the softmax's weights have
         beyond 11 bits is multiplied for float16 and any number of rows.
 
-        After `KVPages.fork` of a prompt of p whole blocks: prefix_table = table[:1, :p], block_table = table[:, p:], lengths - p * block_tokens."""
+        After `KVPages.fork` of a prompt of p whole blocks: prefix_table = table[:1, :p], block_table = table[:, p:], lengths - p * block_tokens. The tables' widths, not
+        the lengths on the device, say which kernels run: columns that no sequence needs (table[:, p:p + n] has n) make a call slower where own contexts are short."""
         return _ext.kv_shared_attention(self.handle, self.k_codes, q, block_table, lengths, cu_tokens, self.head_dim ** -0.5 if scale is None else scale,
                                         causal, 0, out, lse, stream, prefix_table, prefix_lengths, cu_seqs)
 

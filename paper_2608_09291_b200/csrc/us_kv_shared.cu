@@ -14,7 +14,13 @@ struct SharedPlan {
     const void *short_kernel, *join;   // short contexts: their kernel runs beside the groups', another joins what they leave; nullptr: the own tokens' kernel does
     int64_t short_blocks;
 };
-constexpr int64_t kShort = 2048;   // tokens that a warp reads by itself (a table's width says how many there may be)
+// Tokens (of a table's width) up to which a sequence's own are read by a warp for itself, beside the groups' kernel, and not by the kernel that cuts them into units, behind it.
+// A warp takes 32 in 2.4 us; the other kernel has 2 to 50 us more to begin with, the more the more sequences. us beside and behind, contexts as long as their table,
+// S x query heads / cache heads x head size behind P tokens. Up to 32 sequences 512 tokens: 4 x 32/8 x 128 behind 1000 34.1, 30.2 (256 tokens 23.9, 25.9); 16 x 64/8 x 128 behind 8192
+// 41.8, 38.6 (256: 27.4, 36.2); 32 x 64/8 x 128 behind 8192 54.5, 52.1 (768: 74.4, 56.9). More sequences 1024: 40 x 32/8 x 128 behind 1000 63.6, 65.7; 64 x 64/8 x 128 behind 8192
+// 103.7, 94.2 (768: 82.1, 88.2); 200 x 64/8 x 128 behind 1000 145, 160. Heads without groups cross earlier (16 x 32/32 x 128 behind 8192: 256 tokens 69.7, 62.6), heads of 64
+// later (64 x 32/4 x 64 behind 1000: 1024 tokens 36.4, 40.6).
+int64_t short_tokens(int64_t sequences) { return sequences > 32 ? 1024 : 512; }
 int64_t pitch(const us_kv* h) { return h->pool.D + 4; }
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q, int64_t N, int32_t heads, bool bf16)
@@ -28,7 +34,7 @@ SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q,
         r.rows = N * heads * pitch(h) * 4;   // (twice, where the own tokens have rows, too)
     }
     const int64_t longest = q->table_width * T;
-    if (p->n_seqs > 0 && r.own.tiles == 0 && longest <= kShort) {
+    if (p->n_seqs > 0 && r.own.tiles == 0 && longest <= short_tokens(q->n_seqs)) {
         r.short_blocks = (q->cu_tokens ? N * G / 8 + q->n_seqs : N * ((G + 7) / 8)) * h->pool.Hkv;   // a warp an item: as many as there may be
         r.short_kernel = h->pool.D == 128 ? (bf16 ? (const void*)us_kv_short_kernel<128, true> : (const void*)us_kv_short_kernel<128, false>) :
                                             (bf16 ? (const void*)us_kv_short_kernel<64, true> : (const void*)us_kv_short_kernel<64, false>);
@@ -43,7 +49,9 @@ SharedPlan shared_plan(const us_kv* h, const us_kv_seqs* p, const us_kv_seqs* q,
         // Many rows a group, short contexts of their own: the first kernel is bound by its softmax, the second by latency, so they share the GPU. The number of parts that
         // a prefix is cut in says how many SMs the groups take, and the one is chosen with which both are expected to end first. Times in us: a row tile's unit 2.9, beginning and
         // end 12; a warp's item 4 and 2.4 for 32 tokens, half of the longest, while the other kernel runs, of which an SM has eight at a time. (64 sequences of 64/8
-        // heads behind 8192 tokens, with up to 512 of their own: 51, 47, 60, 71 us for 5, 6, 7, 8 parts, 77 one behind the other.)
+        // heads behind 8192 tokens, bf16, with up to 512 of their own: 52, 48, 53, 73 us for 5, 6, 7, 8 parts, 77 one behind the other. Of 13 batches, 16 to 100 sequences behind 1000
+        // to 16000 tokens, heads of 64 and 128 in groups of 1, 4 and 8, both types, its number is within 5 % of the best in 11; 64 x 64/8 x 128 behind 8192, 128 of their own: 8 parts
+        // 50.5, 7 43.0; 64 x 32/4 x 64 behind 8192, 256 of their own: 16 parts 32.1, 14 25.4. A unit takes fp16 2.9, bf16 2.3.)
         const int64_t row_tiles = std::max<int64_t>(p->n_seqs, (N * G + kPrRows - 1) / kPrRows) * h->pool.Hkv, units = (p->table_width * T + kPrTile - 1) / kPrTile;
         const double own = (double)std::max<int64_t>(q->n_seqs, (N * G + 7) / 8) * h->pool.Hkv * (4 + 2.4 * (double)longest / 64) / 8;
         double best = 0;
