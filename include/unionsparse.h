@@ -467,8 +467,8 @@ us_status us_kv_copy_blocks(us_kv* h, const int32_t* src, const int32_t* dst, in
  * For each token n and head x (head_dim values, even, at most 256): y = x / sqrt(mean x^2 + eps) * weight where the call has weights, else
  * y = x; then of the first rotary_dim values the pairs (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if `interleaved`, i < rotary_dim / 2, are turned:
  *     y_a' = y_a cos t - y_b sin t,  y_b' = y_b cos t + y_a sin t,  t = positions[axis[i]][n] * frequency_i
- * computed in fp32 and rounded once. turns[i] (device) is frequency_i / (2 pi) turns in units of 2^-64, modulo 1, so that t is exact for every
- * position. axis (device; may be NULL with axes = 1): the axis of each pair, below `axes`; a larger one reads outside the positions. turns and axis have
+ * computed in fp32 and rounded once. turns[i] (device) is frequency_i / (2 pi) turns in units of 2^-64, modulo 1: whole turns of a position drop out without a rounding, and t has
+ * the error of turns[i], as many times as the position says, and no other. axis (device; may be NULL with axes = 1): the axis of each pair, below `axes`; a larger one reads outside the positions. turns and axis have
  * to be complete before the stream's latest work was launched, and stay as they are.
  * positions: axes rows of N int32 values, axis_stride apart. q, k: rows (token, head) of `type`, strides in elements; k may be NULL; out may be x
  * itself, otherwise they do not overlap. weight: head_dim values of weight_type, or NULL. Errors: INVALID_ARG, CUDA.

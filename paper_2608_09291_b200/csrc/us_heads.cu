@@ -7,8 +7,8 @@ namespace {
 
 // A head x of D values: y = x / sqrt(mean x^2 + eps) * w (where there are weights), and of y's first `rotary` values the pairs (i, i + rotary/2), or
 // (2i, 2i + 1), turned by position * frequency_i.
-//   * Turns are counted in 2^-64: position * turns wraps at a whole turn by itself, so that the angle of a far position is as good as a near
-//     one's (in 32-bit arithmetic 131072 radians are known to 2^-7). What is left after quarter turns goes through two short polynomials.
+//   * Turns are counted in 2^-64: position * turns wraps at a whole turn by itself, so that the angle of a far position has the frequency's own error and no
+//     other (53 bits: below 2^-51 of position * frequency; in 32-bit arithmetic 131072 radians are known to 2^-7). What is left after quarter turns goes through two short polynomials.
 //   * A lane has eight pairs in registers, as two pieces of eight values: both ends of a pair are its own. 1 to 16 lanes have a head (a power of two, D / 16
 //     of them have values), a warp 32 / lanes heads at a time: a round. The sines and cosines of a lane's pairs are found once for all rounds that the warp
 //     walks over; the values of the next round are on their way meanwhile. Sines, cosines and weights wait in shared memory.
@@ -41,8 +41,9 @@ __device__ __forceinline__ float weight_at(const void* w, int32_t type, int i)
     return type == US_F32 ? static_cast<const float*>(w)[i] : type == US_F16 ? __half2float(static_cast<const __half*>(w)[i]) :
                             __bfloat162float(static_cast<const __nv_bfloat16*>(w)[i]);
 }
-// cos and sin of `part` / 2^64 turns. With x = the rest of a quarter turn in half turns, |x| <= 1/4: sin(pi x) = x S(x^2), cos(pi x) = C(x^2), polynomials fitted here;
-// off by 1.5 2^-24 and 2^-24 at most, in fp32 arithmetic.
+// cos and sin of `part` / 2^64 turns. With x = the rest of a quarter turn in half turns, |x| <= 1/4: sin(pi x) = x S(x^2), cos(pi x) = C(x^2). S and C: of the polynomials of degree 3 and 4
+// in u = x^2 those whose largest distance from sin(pi x) / x and cos(pi x) over u = 0 .. 1/16 is least (Remez's exchange), coefficients rounded to fp32. In fp32 arithmetic sine and
+// cosine are off by 1.7 2^-24 and 1.25 2^-24 at most (32 million arguments against 64 bits).
 __device__ __forceinline__ void turn(uint64_t part, float& c, float& s)
 {
     const uint64_t r = part + (1ull << 61);                                    // quarters: the nearest one, and -1/8 .. 1/8 turn from it

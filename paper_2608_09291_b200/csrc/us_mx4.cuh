@@ -519,8 +519,10 @@ __device__ __forceinline__ float mx4_sigmoid_times(float x, float z)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
     return x * r;
 }
-// x (1 + erf(x / sqrt 2)) / 2. With a = |x| / sqrt 2 and t = 1 / (1 + a / 2): erfc(a) = t 2^(Q(t) - a^2 log2 e); Q is a polynomial fitted here to log2(erfc(a) e^(a^2) / t) over
-// a = 0 .. 14, so that the tail is as exact relative to itself (2^-22, in fp32 arithmetic) as the middle. A third of erfcf's instructions (4096 x 22016 x 4096, 16-bit results: 195 us, silu 166).
+// x (1 + erf(x / sqrt 2)) / 2. With a = |x| / sqrt 2 and t = 1 / (1 + a / 2): erfc(a) = t 2^(Q(t) - a^2 log2 e), the form of erfcc in Numerical Recipes (Press, Teukolsky, Vetterling,
+// Flannery) to base 2. Q: of the polynomials of degree 9 the one whose largest distance from log2(erfc(a) e^(a^2) / t) over t = 1/8 .. 1 (a = 0 .. 14) is least (Remez's exchange), 2^-23.4 with its
+// coefficients in fp32. The exponent is rounded at its own size: relative to itself the tail is off by 2^-20.7 down to x = -2, from there on by up to (x^2 + 2) 2^-23 (2^-19 at -6,
+// 2^-17 at -13), far below a rounding to 16 bits. A third of erfcf's instructions (4096 x 22016 x 4096, 16-bit results: 195 us, silu 165).
 __device__ __forceinline__ float mx4_gelu_fast(float x)
 {
     const float a = fabsf(x), d = fmaf(a, 0.35355339f, 1.f);
@@ -561,8 +563,6 @@ __device__ __forceinline__ void mx4_activate(int32_t act, float (&v)[N])
 // token) nor its loads (8 rows or 16 a lane) meet a bank twice.
 constexpr int kMxPitch = 132;
 __device__ __forceinline__ int mx4_place(int row) { return row ^ (((row >> 5) & 3) << 2); }
-// What follows the product, on `tokens` tokens of a tile, and out in whole lines: a thread has 16 bytes of a token's output at a time, always the same columns. This way
-// its code is there once for all tokens, whatever f is.
 template <int EPI>
 __device__ __forceinline__ int mx4_columns(const Mx4Params& p, int64_t m0)   // of the output that the tile has (0: a pair's rows end with its first block)
 {
@@ -570,6 +570,8 @@ __device__ __forceinline__ int mx4_columns(const Mx4Params& p, int64_t m0)   // 
 }
 template <int EPI>
 __device__ __forceinline__ bool mx4_whole(const Mx4Params& p, int64_t m0) { return p.y_vec && mx4_columns<EPI>(p, m0) == 128 / EPI && (!p.e.residual || p.e.r_vec); }
+// What follows the product, on `tokens` tokens of a tile, and out in whole lines: a thread has 16 bytes of a token's output at a time, always the same columns. This way
+// its code is there once for all tokens, whatever f is.
 template <class T, int EPI, int THREADS>
 __device__ __forceinline__ void mx4_finish(const Mx4Params& p, const float* b, int tokens, int64_t n0, int64_t m0, int tid)
 {
@@ -699,17 +701,17 @@ struct Mx4Four {
             if (EPI == 2) y[i] *= v[2 * i + 1];
             if (p.e.residual) y[i] += r[i];
         }
-        if (EPI == 1) {
-            const float all[4] = {y[0], y[1], y[K - 2], y[K - 1]};
-            return mx4_store4(p, n, m, all);
-        }
+        if constexpr (EPI == 1) {
+            mx4_store4(p, n, m, y);
+        } else {
 #pragma unroll
-        for (int i = 0; i < K; ++i) {
-            const int64_t c = (m >> 1) + i, at = n * p.ldy + c;
-            if (c >= p.M >> 1) break;
-            if (p.y_type == kF32) static_cast<float*>(p.Y)[at] = y[i];
-            else if (p.y_type == kF16) static_cast<__half*>(p.Y)[at] = __float2half_rn(y[i]);
-            else static_cast<__nv_bfloat16*>(p.Y)[at] = __float2bfloat16_rn(y[i]);
+            for (int i = 0; i < K; ++i) {
+                const int64_t c = (m >> 1) + i, at = n * p.ldy + c;
+                if (c >= p.M >> 1) break;
+                if (p.y_type == kF32) static_cast<float*>(p.Y)[at] = y[i];
+                else if (p.y_type == kF16) static_cast<__half*>(p.Y)[at] = __float2half_rn(y[i]);
+                else static_cast<__nv_bfloat16*>(p.Y)[at] = __float2bfloat16_rn(y[i]);
+            }
         }
     }
 };
@@ -1115,7 +1117,7 @@ __device__ __forceinline__ void mx4_pair_store(const Mx4Params& p, uint32_t tm, 
 // With an epilogue: eight warps, `half` 0 or 1 with 32 tokens of every 64, a thread a weight row. All sums go to registers at once (128 a thread), so that the next
 // tile's products begin before anything is computed from them. What follows is computed there, too, 64 tokens at a time, and passes rounded through shared
 // memory on its way out: the products' operands take three quarters of shared memory's bandwidth (through it in fp32, and all that
-// follows behind it: 204 us for 4096 x 22016 x 4096 gated silu, 180 this way, 162 the product alone; with a residual and bias 175 to 192; with four warps that finish
+// follows behind it: 204 us for 4096 x 22016 x 4096 gated silu, 173 this way, 162 the product alone; with a residual and bias 188, call after call under the power cap 205; with four warps that finish
 // before the next tile begins 420). The residual of 64 tokens comes to a slot of shared memory by asynchronous
 // copies; as many slots as there is room for (p.e.slots) are under way while the products run.
 __device__ __forceinline__ void bar_finish() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -1290,15 +1292,14 @@ __global__ void __launch_bounds__(EPI ? 384 : 192, 1) us_mx4_pair_kernel(const _
     const uint32_t tm = *(volatile uint32_t*)misc;
     bool ok = true;
     auto sums = [&](auto finish) {
-        const int quarter = warp & 3;
         const uint32_t free_bar = cluster_addr(b_free, 0);
         asm volatile("griddepcontrol.wait;" ::: "memory");
         uint32_t n = 0;
         for (int tile = blockIdx.x >> 1; tile < p.tiles; tile += gridDim.x >> 1, ++n) {
             const int pair = tile / p.col_tiles, n0 = (tile - pair * p.col_tiles) * NB, nn = min(NB, p.N - n0);
             const int64_t m0 = 128 * (int64_t)(2 * pair + rank);
-            float bias = 0.f;   // (on its way while the tile's products run)
-            bool whole = false;
+            [[maybe_unused]] float bias = 0.f;   // (on its way while the tile's products run)
+            [[maybe_unused]] bool whole = false;
             if constexpr (EPI > 0) {
                 const int64_t m = m0 + finish.row;
                 if (p.e.bias && m < p.M) bias = mx4_scalar(p.e.bias, p.e.bias_type, m);
@@ -1313,6 +1314,7 @@ __global__ void __launch_bounds__(EPI ? 384 : 192, 1) us_mx4_pair_kernel(const _
             if constexpr (EPI > 0) {
                 finish.tile(tm, m0, n0, nn, free_bar, bias, whole);
             } else {
+                const int quarter = warp & 3;
                 if (p.y_type == kF32) mx4_pair_store<float>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
                 else if (p.y_type == kF16) mx4_pair_store<__half>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
                 else mx4_pair_store<__nv_bfloat16>(p, tm, quarter, lane, m0, n0, nn, out, free_bar);
